@@ -405,6 +405,151 @@ int moara_step_static_scratch(const moara_hparams* hp, int m, int n, int r, int 
                               float* exp_avg_sq, float* mag_avg, float* mag_avg_sq, int64_t t,
                               float lr, void* stream);
 
+/* ---- the parameters beside the projected weights ------------------------
+ *
+ * A training program also holds parameters that have no projector (embedding,
+ * head, norm gains, biases).  The calls below take their gradients' part of the
+ * clipping norm and apply AdamW to them, many tensors in one launch.  They use
+ * no registered module and none of the context's hyper-parameters. */
+
+#define MOARA_DTYPE_BLOCK8 2    /* 8-bit moments with a scale per MOARA_ADAMW_BLOCK
+                                   entries (state_dtype of a moara_adamw_tensor)  */
+#define MOARA_ADAMW_BLOCK  256
+
+typedef struct moara_adamw_hparams {
+    float beta1;            /* in [0, 1)                                          */
+    float beta2;            /* in [0, 1)                                          */
+    float eps;              /* >= 0, added to sqrt(v_hat)                         */
+    uint64_t seed;          /* of the rounding of 8-bit moments                   */
+} moara_adamw_hparams;
+
+/* One tensor of n >= 0 contiguous entries.  Pointers are device pointers,
+ * aligned to their type (16-byte alignment of all of them is faster); an n of 0
+ * is skipped.
+ *   param       fp32 or bf16 (param_dtype), updated in place; bf16 is computed in
+ *               fp32 and stored rounded to nearest even
+ *   grad        fp32 or bf16 (grad_dtype), read
+ *   param_bf16  bf16 copy of the new parameter, written, or NULL; with an fp32
+ *               param only
+ *   exp_avg, exp_avg_sq   first and second moment, zeroed by the caller before
+ *               step 1: n floats (MOARA_DTYPE_F32), or n bytes
+ *               (MOARA_DTYPE_BLOCK8) with exp_avg_scale, exp_avg_sq_scale:
+ *               ceil(n / MOARA_ADAMW_BLOCK) floats each
+ *   id          which random bits the 8-bit rounding takes; a tensor of its own
+ *               each, so that the result does not depend on how tensors are
+ *               grouped into calls
+ *   weight_decay >= 0; lr_scale: factor on the call's learning rate
+ *
+ * MOARA_DTYPE_BLOCK8: entry i of block i / 256 (of the flattened tensor) is
+ * scale * y(code) with y in [0, 1.875]: 3 mantissa bits, and a sign and 4 exponent
+ * bits for exp_avg (largest exponent 0, subnormal below 2^-14) or 5 exponent bits
+ * for exp_avg_sq (subnormal below 2^-30).  scale = the block's largest magnitude
+ * / 1.875, in fp32, so that a block whose entries all decay alike decays exactly.
+ * Codes are rounded stochastically (unbiased: with beta2 = 0.999 an entry moves by
+ * less than half a code step per step, and rounding to nearest would never move
+ * it) with 16 bits of a hash of (seed, id, t, i): the same call gives the same
+ * result.  An exp_avg_sq > 0 takes at least the smallest code, so that no
+ * denominator vanishes below a moment that does not.  A block whose largest
+ * magnitude is below 2^-100 is stored as zero; one that holds a NaN or infinity
+ * becomes non-finite as a whole. */
+typedef struct moara_adamw_tensor {
+    int64_t n;
+    void* param;
+    const void* grad;
+    uint16_t* param_bf16;
+    void* exp_avg;
+    void* exp_avg_sq;
+    float* exp_avg_scale;
+    float* exp_avg_sq_scale;
+    int param_dtype, grad_dtype, state_dtype;
+    uint32_t id;
+    float weight_decay;
+    float lr_scale;
+} moara_adamw_tensor;
+
+/* One AdamW step (decoupled weight decay, bias correction) at step t (1-based)
+ * of every listed tensor:
+ *   g = *grad_scale * G;  m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - l wd) - l (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps),  l = lr lr_scale
+ * grad_scale: device float read stream-ordered (a clipping coefficient:
+ * moara_grad_norm's out + 2, or moara_clip_state's state + 1), or NULL for 1.
+ * The array of descriptors is host memory and free again on return. */
+int moara_adamw_step(moara_ctx* ctx, int count, const moara_adamw_tensor* tensors, const moara_adamw_hparams* hp,
+                     int64_t t, float lr, const float* grad_scale, void* stream);
+
+/* The moments of every listed tensor as n floats each (of 8-bit moments, the
+ * values that the codes stand for): exp_avg[i], exp_avg_sq[i] are device pointers
+ * of tensor i; NULL leaves one out.  tensors' param and grad are not read. */
+int moara_adamw_moments(moara_ctx* ctx, int count, const moara_adamw_tensor* tensors, float* const* exp_avg,
+                        float* const* exp_avg_sq, void* stream);
+
+/* Norm of `count` gradients and the clipping coefficient of `max_norm`:
+ *   out[0] = sum of squares of the listed gradients (n[i] entries of dtype[i] at G[i])
+ *   out[1] = sqrt(out[0] + *extra_sq)       extra_sq: device float, or NULL for 0
+ *   out[2] = min(1, max_norm / (out[1] + 1e-6)), or 1 for max_norm <= 0
+ * as torch.nn.utils.clip_grad_norm_ (a NaN norm gives a NaN coefficient).  out is
+ * 3 device floats; out + 0 is what moara_set_clip_extra takes and out + 2 what
+ * moara_adamw_step takes.  Squares are summed in fp32 per thread, then in fp64, in
+ * a fixed order.  workspace: moara_grad_norm_workspace_bytes(count) device bytes,
+ * 16-byte aligned, zeroed by the caller once before the first call that uses it,
+ * and in use by one call at a time. */
+int moara_grad_norm_workspace_bytes(int count, size_t* out);
+int moara_grad_norm(moara_ctx* ctx, int count, const void* const* G, const int64_t* n, const int* dtype,
+                    float max_norm, const float* extra_sq, float* out, void* workspace, size_t workspace_bytes,
+                    void* stream);
+
+/* ---- MXFP4 operands and products ----------------------------------------
+ *
+ * A rows x cols matrix in 4 bits (OCP Microscaling: E2M1 elements, one E8M0 scale
+ * per 32 consecutive entries of a row), as the tensor cores read it:
+ *   q   rows x ceil(cols / 32) * 16 bytes: two codes per byte, the even column in
+ *       the low half; code = sign << 3 | magnitude, magnitudes 0, 0.5, 1, 1.5, 2,
+ *       3, 4, 6; codes behind the last column are zero
+ *   sf  ceil(rows / 128) x ceil(cols / 128) tiles of 512 bytes: the scale
+ *       2^(byte - 127) of row i and 32-column block b is at byte
+ *       (i / 128 * ceil(cols / 128) + b / 4) * 512 + i % 32 * 16 + i % 128 / 32 * 4 + b % 4;
+ *       scales of rows and blocks that do not exist are 127
+ * Both are device buffers of the caller, 16-byte aligned. */
+int moara_fp4_bytes(int rows, int cols, size_t* q_bytes, size_t* sf_bytes);
+
+/* Quantises X (rows x cols, fp32 or bf16, row pitch ld >= cols entries, aligned to
+ * its type) by rows into q / sf (rows x cols), and by columns into qt / sft, the
+ * operand of X^T (cols x rows), from one read of X.  Either pair may be NULL.
+ * A block's scale is the smallest power of two (2^-127 at least) with
+ * max |x| <= 6 scale: no entry saturates (the Microscaling format leaves the rule
+ * open; rounding the largest entry down to a power of two instead gives the same mean
+ * square error but shrinks the values two to three times as much).  Entries are
+ * rounded to nearest, ties to the even code.  A block that holds a NaN or infinity takes
+ * the scale 255 (NaN): its products are NaN. */
+int moara_fp4_quantize(moara_ctx* ctx, const void* X, int dtype, int rows, int cols, int64_t ld, void* q, void* sf,
+                       void* qt, void* sft, void* stream);
+
+/* The values of q / sf into out (rows x cols, fp32 or bf16, which holds them
+ * exactly, row pitch ldo >= cols). */
+int moara_fp4_dequantize(moara_ctx* ctx, const void* q, const void* sf, int rows, int cols, void* out, int dtype,
+                         int64_t ldo, void* stream);
+
+/* D (M x N, fp32 or bf16, row pitch ldd >= N) = A B^T for MXFP4 operands A (M x K)
+ * and B (N x K): exact products, fp32 accumulation, one rounding to D's type.  The
+ * products of a weight W (n x k) with activations x (m x k) and their gradient dy
+ * are y = x W^T, dx = dy (W^T)^T with the operand of W^T, and dW = dy^T (x^T)^T
+ * with those of dy^T and x^T, whose bf16 result is a gradient for
+ * moara_step_grouped.  workspace: moara_fp4_workspace_bytes(M, N, K) device bytes,
+ * 16-byte aligned (NULL where that is 0), in use by one call at a time.
+ * MOARA_ERR_UNSUPPORTED without tensor-core state. */
+int moara_fp4_workspace_bytes(int M, int N, int K, size_t* out);
+int moara_fp4_product(moara_ctx* ctx, int M, int N, int K, const void* a_q, const void* a_sf, const void* b_q,
+                      const void* b_sf, void* D, int d_dtype, int64_t ldd, void* workspace, size_t workspace_bytes,
+                      void* stream);
+
+/* The same product with A given as X (M x K, fp32 or bf16, row pitch ldx >= K),
+ * quantised by rows on the way, with the result of moara_fp4_quantize and
+ * moara_fp4_product.  workspace: moara_fp4_linear_workspace_bytes(M, N, K). */
+int moara_fp4_linear_workspace_bytes(int M, int N, int K, size_t* out);
+int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_dtype, int64_t ldx, const void* b_q,
+                     const void* b_sf, void* D, int d_dtype, int64_t ldd, void* workspace, size_t workspace_bytes,
+                     void* stream);
+
 #ifdef __cplusplus
 }
 #endif

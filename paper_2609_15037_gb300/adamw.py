@@ -1,0 +1,178 @@
+"""AdamW over the parameters that have no projector, and the norm of their
+gradients: host-side bookkeeping over moara_adamw_step, moara_adamw_moments and
+moara_grad_norm.  Every computation happens in the library's kernels."""
+
+from __future__ import annotations
+
+import contextlib
+
+import numpy as np
+import torch
+
+from . import binding as B
+
+_TYPES = {torch.float32: B.MOARA_DTYPE_F32, torch.bfloat16: B.MOARA_DTYPE_BF16}
+_STATES = {"f32": B.MOARA_DTYPE_F32, "block8": B.MOARA_DTYPE_BLOCK8}
+_DESC = np.dtype(B.moara_adamw_tensor)
+
+
+def stream_handle(stream, device):
+    """A cudaStream_t: `stream`, or torch's current stream on `device` for None."""
+    return torch.cuda.current_stream(device).cuda_stream if stream is None else int(stream)
+
+
+def allocating_on(stream, device):
+    """Context in which torch allocates for work on `stream` (None: the current one)."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device))
+
+
+class AdamWGroup:
+    """Tensors that take AdamW steps together, with their moments.
+
+    Streams are cudaStream_t handles; None is torch's current stream."""
+
+    def __init__(self, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, device=0):
+        self.device = device
+        self.hp = B.moara_adamw_hparams(beta1, beta2, eps, seed)
+        self.ctx = None
+        self.ctx = B.moara_create(B.moara_default_hparams(), device)
+        self.params, self.copies, self.states = [], [], []
+        self._desc = np.zeros(0, _DESC)
+        self._types = []
+        self._workspace = {}
+
+    def _check(self, x, what, n=None, dtypes=tuple(_TYPES)):
+        if x.dtype not in dtypes or not x.is_contiguous() or x.device.type != "cuda" or x.device.index != self.device:
+            raise ValueError(f"{what}: a contiguous tensor of {dtypes} on cuda:{self.device} is needed")
+        if n is not None and x.numel() != n:
+            raise ValueError(f"{what}: {x.numel()} entries, expected {n}")
+        return x
+
+    def add(self, param, copy=None, state="f32", weight_decay=0.0, lr_scale=1.0, exp_avg=None, exp_avg_sq=None,
+            exp_avg_scale=None, exp_avg_sq_scale=None, id=None):
+        """Registers `param` (fp32 or bf16, updated in place) and returns its
+        index.  copy: a bf16 tensor that receives the new values of an fp32
+        param.  state: "f32" or "block8" moments, zero unless given (layouts of
+        moara.h).  id: which random bits the 8-bit rounding takes (default: the
+        index)."""
+        if state not in _STATES:
+            raise ValueError(f"state must be one of {tuple(_STATES)}")
+        n = self._check(param, "param").numel()
+        if copy is not None:
+            self._check(copy, "copy", n, (torch.bfloat16,))
+        dev = torch.device("cuda", self.device)
+        code = torch.uint8 if state == "block8" else torch.float32
+        blocks = -(-n // B.MOARA_ADAMW_BLOCK)
+
+        def kept(x, what, size, dtype):
+            return torch.zeros(size, dtype=dtype, device=dev) if x is None else self._check(x, what, size, (dtype,))
+        s = {"exp_avg": kept(exp_avg, "exp_avg", n, code), "exp_avg_sq": kept(exp_avg_sq, "exp_avg_sq", n, code)}
+        if state == "block8":
+            s["exp_avg_scale"] = kept(exp_avg_scale, "exp_avg_scale", blocks, torch.float32)
+            s["exp_avg_sq_scale"] = kept(exp_avg_sq_scale, "exp_avg_sq_scale", blocks, torch.float32)
+        i = len(self.params)
+        if i == len(self._desc):
+            self._desc = np.concatenate([self._desc, np.zeros(max(16, i), _DESC)])
+        d = self._desc[i]
+        d["n"], d["param"] = n, param.data_ptr()
+        d["param_bf16"] = 0 if copy is None else copy.data_ptr()
+        for key, x in s.items():
+            d[key] = x.data_ptr()
+        d["param_dtype"], d["state_dtype"] = _TYPES[param.dtype], _STATES[state]
+        d["id"] = i if id is None else id
+        d["weight_decay"], d["lr_scale"] = weight_decay, lr_scale
+        self.params.append(param)
+        self.copies.append(copy)
+        self.states.append(s)
+        return i
+
+    def _chosen(self, ids):
+        return self._desc[:len(self.params)] if ids is None else self._desc[list(ids)]
+
+    def step(self, grads, t, lr, grad_scale=None, ids=None, stream=None):
+        """One AdamW step at step t (1-based): grads[i] (fp32 or bf16) of every
+        registered tensor, or of those in ids.  grad_scale: a one-element
+        float32 device tensor that multiplies every gradient, or None."""
+        d = self._chosen(ids)
+        if len(grads) != len(d):
+            raise ValueError(f"{len(grads)} gradients for {len(d)} tensors")
+        sizes = d["n"].tolist()
+        for g, n in zip(grads, sizes):
+            if g.dtype not in _TYPES or g.numel() != n or not g.is_contiguous() or g.get_device() != self.device:
+                self._check(g, "grad", n)
+        d["grad"] = [g.data_ptr() for g in grads]
+        d["grad_dtype"] = [_TYPES[g.dtype] for g in grads]
+        scale = 0 if grad_scale is None else self._check(grad_scale, "grad_scale", 1, (torch.float32,)).data_ptr()
+        B.moara_adamw_step(self.ctx, len(d), d.ctypes.data, self.hp, t, lr, scale, stream_handle(stream, self.device))
+
+    def moments(self, exp_avg=None, exp_avg_sq=None, ids=None, stream=None):
+        """The moments as fp32 tensors (lists, one per tensor); into the given
+        ones, if any."""
+        d = self._chosen(ids)
+        sizes = d["n"].tolist()
+        with allocating_on(stream, self.device):
+            outs = [[torch.empty(n, device=f"cuda:{self.device}") for n in sizes] if x is None else x
+                    for x in (exp_avg, exp_avg_sq)]
+        for out in outs:
+            if len(out) != len(d):
+                raise ValueError(f"{len(out)} outputs for {len(d)} tensors")
+            for x, n in zip(out, sizes):
+                self._check(x, "output", n, (torch.float32,))
+        ptrs = [np.array([x.data_ptr() for x in out], dtype=np.uint64) for out in outs]
+        B.moara_adamw_moments(self.ctx, len(d), d.ctypes.data, ptrs[0].ctypes.data, ptrs[1].ctypes.data,
+                              stream_handle(stream, self.device))
+        return outs[0], outs[1]
+
+    def _norm_workspace(self, count, handle, stream):
+        need = B.moara_grad_norm_workspace_bytes(count)
+        ws = self._workspace.get(handle)
+        if ws is None or ws.numel() < need:
+            with allocating_on(stream, self.device):
+                ws = torch.zeros(need, dtype=torch.uint8, device=f"cuda:{self.device}")
+                # memory of a recorded graph is the graph's own
+                if not torch.cuda.is_current_stream_capturing():
+                    self._workspace[handle] = ws
+        return ws
+
+    def grad_norm(self, grads, max_norm=0.0, extra_sq=None, out=None, stream=None):
+        """{sum of squares, norm, clipping coefficient} of any gradients (fp32 or
+        bf16), a float32 tensor of three.  extra_sq: a one-element float32 device
+        tensor added to the sum under the root, or None.  The first element is
+        what MoaraGroup.set_clip_extra takes, the last what step takes."""
+        for g in grads:
+            if g.dtype not in _TYPES or not g.is_contiguous() or g.get_device() != self.device:
+                self._check(g, "grad")
+        n = len(grads)
+        table = np.array([[g.data_ptr() for g in grads], [g.numel() for g in grads]], dtype=np.int64)
+        types = np.array([_TYPES[g.dtype] for g in grads], dtype=np.int32)
+        handle = stream_handle(stream, self.device)
+        ws = self._norm_workspace(n, handle, stream)
+        extra = 0 if extra_sq is None else self._check(extra_sq, "extra_sq", 1, (torch.float32,)).data_ptr()
+        if out is None:
+            with allocating_on(stream, self.device):
+                out = torch.empty(3, device=f"cuda:{self.device}")
+        self._check(out, "out", 3, (torch.float32,))
+        B.moara_grad_norm(self.ctx, n, table.ctypes.data, table.ctypes.data + 8 * n, types.ctypes.data, max_norm,
+                          extra, out.data_ptr(), ws.data_ptr(), ws.numel(), handle)
+        return out
+
+    def state_dict(self):
+        return [{k: v.detach().clone() for k, v in s.items()} for s in self.states]
+
+    def load_state_dict(self, sd):
+        for s, new in zip(self.states, sd):
+            for k, v in s.items():
+                v.copy_(new[k])
+
+    def close(self):
+        if self.ctx:
+            B.moara_destroy(self.ctx)
+            self.ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

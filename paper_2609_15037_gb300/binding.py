@@ -28,6 +28,8 @@ MOARA_ERR_UNSUPPORTED = -9
 
 MOARA_DTYPE_F32 = 0
 MOARA_DTYPE_BF16 = 1
+MOARA_DTYPE_BLOCK8 = 2
+MOARA_ADAMW_BLOCK = 256
 MOARA_REFRESH_SRC_V = 0
 MOARA_REFRESH_SRC_G = 1
 MOARA_PREC_AUTO = 0
@@ -64,6 +66,22 @@ class moara_module_desc(ctypes.Structure):
         ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
         ("mag_avg", ctypes.c_void_p), ("mag_avg_sq", ctypes.c_void_p),
         ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+    ]
+
+
+class moara_adamw_hparams(ctypes.Structure):
+    _fields_ = [("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
+                ("seed", ctypes.c_uint64)]
+
+
+class moara_adamw_tensor(ctypes.Structure):
+    _fields_ = [
+        ("n", ctypes.c_int64),
+        ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("param_bf16", ctypes.c_void_p),
+        ("exp_avg", ctypes.c_void_p), ("exp_avg_sq", ctypes.c_void_p),
+        ("exp_avg_scale", ctypes.c_void_p), ("exp_avg_sq_scale", ctypes.c_void_p),
+        ("param_dtype", ctypes.c_int), ("grad_dtype", ctypes.c_int), ("state_dtype", ctypes.c_int),
+        ("id", ctypes.c_uint32), ("weight_decay", ctypes.c_float), ("lr_scale", ctypes.c_float),
     ]
 
 
@@ -104,6 +122,17 @@ def _load():
         "moara_profile_read": (i32, [vp, P(ctypes.c_double), P(i64)]),
         "moara_step_static_scratch": (i32, [P(moara_hparams), i32, i32, i32, i32, vp, vp, vp, vp,
                                             vp, vp, vp, i64, f32, vp]),
+        "moara_adamw_step": (i32, [vp, i32, vp, P(moara_adamw_hparams), i64, f32, vp, vp]),
+        "moara_adamw_moments": (i32, [vp, i32, vp, vp, vp, vp]),
+        "moara_grad_norm_workspace_bytes": (i32, [i32, P(sz)]),
+        "moara_grad_norm": (i32, [vp, i32, vp, vp, vp, f32, vp, vp, vp, sz, vp]),
+        "moara_fp4_bytes": (i32, [i32, i32, P(sz), P(sz)]),
+        "moara_fp4_quantize": (i32, [vp, vp, i32, i32, i32, i64, vp, vp, vp, vp, vp]),
+        "moara_fp4_dequantize": (i32, [vp, vp, vp, i32, i32, vp, i32, i64, vp]),
+        "moara_fp4_workspace_bytes": (i32, [i32, i32, i32, P(sz)]),
+        "moara_fp4_product": (i32, [vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, i64, vp, sz, vp]),
+        "moara_fp4_linear_workspace_bytes": (i32, [i32, i32, i32, P(sz)]),
+        "moara_fp4_linear": (i32, [vp, i32, i32, i32, vp, i32, i64, vp, vp, vp, i32, i64, vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -282,6 +311,78 @@ def moara_step_static_scratch(hp, m, n, r, grad_dtype, G, W, P, exp_avg, exp_avg
                                           int(t), float(lr), stream)
 
 
+# ------------------------------------- the parameters beside the projected weights
+def moara_adamw_step(ctx, count, tensors, hp, t, lr, grad_scale=0, stream=0):
+    """tensors: address of `count` moara_adamw_tensor descriptors in host memory."""
+    _check(_lib.moara_adamw_step(ctx, count, tensors, ctypes.byref(hp), int(t), float(lr),
+                                 grad_scale or None, stream), ctx, "moara_adamw_step")
+
+
+def moara_adamw_moments(ctx, count, tensors, exp_avg, exp_avg_sq, stream=0):
+    """tensors, exp_avg, exp_avg_sq: host addresses of `count` descriptors and
+    of as many device addresses each."""
+    _check(_lib.moara_adamw_moments(ctx, count, tensors, exp_avg, exp_avg_sq, stream), ctx,
+           "moara_adamw_moments")
+
+
+def moara_grad_norm_workspace_bytes(count):
+    out = ctypes.c_size_t()
+    _check(_lib.moara_grad_norm_workspace_bytes(count, ctypes.byref(out)),
+           what="moara_grad_norm_workspace_bytes")
+    return out.value
+
+
+def moara_grad_norm(ctx, count, grads, sizes, dtypes, max_norm, extra_sq, out, workspace, workspace_bytes,
+                    stream=0):
+    """grads, sizes, dtypes: host addresses of `count` device addresses, int64
+    sizes and int types."""
+    _check(_lib.moara_grad_norm(ctx, count, grads, sizes, dtypes, float(max_norm), extra_sq or None, out,
+                                workspace, workspace_bytes, stream), ctx, "moara_grad_norm")
+
+
+# --------------------------------------------------- MXFP4 operands and products
+def moara_fp4_bytes(rows, cols):
+    """(bytes of q, bytes of sf) of a rows x cols operand."""
+    q, sf = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(_lib.moara_fp4_bytes(rows, cols, ctypes.byref(q), ctypes.byref(sf)), what="moara_fp4_bytes")
+    return q.value, sf.value
+
+
+def moara_fp4_quantize(ctx, X, dtype, rows, cols, ld, q=0, sf=0, qt=0, sft=0, stream=0):
+    _check(_lib.moara_fp4_quantize(ctx, X, dtype, rows, cols, ld, q or None, sf or None, qt or None,
+                                   sft or None, stream), ctx, "moara_fp4_quantize")
+
+
+def moara_fp4_dequantize(ctx, q, sf, rows, cols, out, dtype, ldo, stream=0):
+    _check(_lib.moara_fp4_dequantize(ctx, q, sf, rows, cols, out, dtype, ldo, stream), ctx,
+           "moara_fp4_dequantize")
+
+
+def moara_fp4_workspace_bytes(M, N, K):
+    out = ctypes.c_size_t()
+    _check(_lib.moara_fp4_workspace_bytes(M, N, K, ctypes.byref(out)), what="moara_fp4_workspace_bytes")
+    return out.value
+
+
+def moara_fp4_product(ctx, M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, workspace=0, workspace_bytes=0,
+                      stream=0):
+    _check(_lib.moara_fp4_product(ctx, M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, workspace or None,
+                                  workspace_bytes, stream), ctx, "moara_fp4_product")
+
+
+def moara_fp4_linear_workspace_bytes(M, N, K):
+    out = ctypes.c_size_t()
+    _check(_lib.moara_fp4_linear_workspace_bytes(M, N, K, ctypes.byref(out)),
+           what="moara_fp4_linear_workspace_bytes")
+    return out.value
+
+
+def moara_fp4_linear(ctx, M, N, K, X, x_dtype, ldx, b_q, b_sf, D, d_dtype, ldd, workspace=0,
+                     workspace_bytes=0, stream=0):
+    _check(_lib.moara_fp4_linear(ctx, M, N, K, X, x_dtype, ldx, b_q, b_sf, D, d_dtype, ldd, workspace or None,
+                                 workspace_bytes, stream), ctx, "moara_fp4_linear")
+
+
 PHASES = ["decompose", "project", "backproject", "refresh", "tc_project",
           "tc_backproject", "tc_decompose", "tc_refresh", "tc_decompose_overlap", "clip_norm"]
 
@@ -307,4 +408,7 @@ EXPORTED = [
     "moara_flatten_shape",
     "moara_last_error", "moara_status_string", "moara_launch_count", "moara_set_wait_limit",
     "moara_profile_enable", "moara_profile_read", "moara_step_static_scratch",
+    "moara_adamw_step", "moara_adamw_moments", "moara_grad_norm_workspace_bytes", "moara_grad_norm",
+    "moara_fp4_bytes", "moara_fp4_quantize", "moara_fp4_dequantize", "moara_fp4_workspace_bytes",
+    "moara_fp4_product", "moara_fp4_linear_workspace_bytes", "moara_fp4_linear",
 ]

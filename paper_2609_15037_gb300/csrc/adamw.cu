@@ -1,0 +1,391 @@
+// AdamW over many tensors in one launch, with moments in fp32 or in 8 bits, and
+// the norm of many gradients.
+//
+// Both are one pass over the data.  Per entry the step moves 28 bytes (fp32
+// parameter and moments, bf16 gradient and copy) or 10 (bf16 parameter and
+// gradient, 8-bit moments) and does some twenty to sixty operations, so DRAM
+// bounds the first and DRAM and the integer pipe together the second; the norm
+// reads its bytes and does one FMA per entry.  Short tensors are all latency:
+// every tensor of a call is in the launch's parameter block, so a call costs one
+// launch.
+#include <cuda_bf16.h>
+
+#include "ops.h"
+
+namespace moara {
+namespace {
+
+// ---------------------------------------------------------------------------
+// 8-bit moments.  y = |x| * (1.875 / top) lies in [0, 1.875] up to rounding.
+// Scaled by 2^-112 (exp_avg) or 2^-96 (exp_avg_sq) its largest exponent lands on
+// the fp32 exponent field 15 or 31 and everything below field 1 is an fp32
+// subnormal, so the code is bits >> 20 of an fp32 number: exponent field and 3
+// mantissa bits, subnormals included, with no case distinction.  Adding 20
+// random bits before the shift rounds up with the probability of the part
+// cut off.  Every operation is a single fp32 rounding (no contraction), so
+// that the codes follow from the formulas alone.
+// ---------------------------------------------------------------------------
+constexpr float kCodeTop = 1.875f;
+constexpr float kCodeUnit = 1.0f / 1.875f;
+
+template <bool SIGNED> __device__ __forceinline__ float code_down() { return SIGNED ? 0x1p-112f : 0x1p-96f; }
+template <bool SIGNED> __device__ __forceinline__ float code_up() { return SIGNED ? 0x1p112f : 0x1p96f; }
+
+template <bool SIGNED> __device__ __forceinline__ float decode8(uint32_t code, float scale) {
+    const uint32_t mag = SIGNED ? code & 127u : code;
+    const float y = __fmul_rn(__fmul_rn(__uint_as_float(mag << 20), code_up<SIGNED>()), scale);
+    return SIGNED && (code & 128u) ? -y : y;
+}
+
+template <bool SIGNED> __device__ __forceinline__ uint32_t encode8(float x, float inv, uint32_t r16) {
+    const float z = __fmul_rn(__fmul_rn(fabsf(x), inv), code_down<SIGNED>());
+    const uint32_t c = (__float_as_uint(z) + (r16 << 4)) >> 20;
+    if (SIGNED) return min(c, 127u) | ((__float_as_uint(x) >> 31) << 7);
+    return max(min(c, 255u), x > 0.0f ? 1u : 0u);
+}
+
+// 32-bit xor-shift-multiply mixing
+__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
+    x ^= x >> 16;
+    x *= 0x85EBCA6Bu;
+    x ^= x >> 13;
+    x *= 0xC2B2AE35u;
+    return x ^ (x >> 16);
+}
+
+// four consecutive entries at i; those at or behind n read as zero
+template <bool FULL> __device__ __forceinline__ void load4(const float* p, long long i, long long n, float (&v)[4]) {
+    if (FULL) {
+        const float4 w = __ldcs(reinterpret_cast<const float4*>(p + i));
+        v[0] = w.x; v[1] = w.y; v[2] = w.z; v[3] = w.w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = i + e < n ? p[i + e] : 0.0f;
+    }
+}
+
+template <bool FULL>
+__device__ __forceinline__ void load4(const __nv_bfloat16* p, long long i, long long n, float (&v)[4]) {
+    if (FULL) {
+        const uint2 w = __ldcs(reinterpret_cast<const uint2*>(p + i));
+        v[0] = __uint_as_float(w.x << 16); v[1] = __uint_as_float(w.x & 0xFFFF0000u);
+        v[2] = __uint_as_float(w.y << 16); v[3] = __uint_as_float(w.y & 0xFFFF0000u);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = i + e < n ? __bfloat162float(p[i + e]) : 0.0f;
+    }
+}
+
+template <bool FULL> __device__ __forceinline__ uint32_t load4(const uint8_t* p, long long i, long long n) {
+    if (FULL) return __ldcs(reinterpret_cast<const unsigned int*>(p + i));
+    uint32_t w = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (i + e < n) w |= static_cast<uint32_t>(p[i + e]) << (8 * e);
+    return w;
+}
+
+template <bool FULL> __device__ __forceinline__ void store4(float* p, long long i, long long n, const float (&v)[4]) {
+    if (FULL) {
+        __stcs(reinterpret_cast<float4*>(p + i), make_float4(v[0], v[1], v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < n) p[i + e] = v[e];
+    }
+}
+
+__device__ __forceinline__ uint32_t bf16x2(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <bool FULL>
+__device__ __forceinline__ void store4(__nv_bfloat16* p, long long i, long long n, const float (&v)[4]) {
+    if (FULL) {
+        __stcs(reinterpret_cast<uint2*>(p + i), make_uint2(bf16x2(v[0], v[1]), bf16x2(v[2], v[3])));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < n) p[i + e] = __float2bfloat16_rn(v[e]);
+    }
+}
+
+template <bool FULL> __device__ __forceinline__ void store4(uint8_t* p, long long i, long long n, uint32_t w) {
+    if (FULL) {
+        __stcs(reinterpret_cast<unsigned int*>(p + i), w);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (i + e < n) p[i + e] = static_cast<uint8_t>(w >> (8 * e));
+    }
+}
+
+__device__ __forceinline__ float sqrt_fast(float x) {     // a few ulp, subnormals kept
+    float y;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The scale of 256 values, 8 per lane: the largest magnitude as bits, so that a
+// NaN is the largest.
+template <class V> __device__ __forceinline__ float warp_top(const V& a, const V& b) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        top = max(top, __float_as_uint(a[e]) & 0x7FFFFFFFu);
+        top = max(top, __float_as_uint(b[e]) & 0x7FFFFFFFu);
+    }
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+}
+
+// One warp, 256 entries from i0 on: lane l has i0 + 4l .. +3 and i0 + 128 + 4l .. +3.
+template <class PT, class GT, bool B8, bool FULL>
+__device__ __forceinline__ void adam_tile(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, int lane) {
+    const long long n = t.n;
+    const long long at[2] = {i0 + 4 * lane, i0 + 128 + 4 * lane};
+    PT* const pp = static_cast<PT*>(t.p);
+    const GT* const gp = static_cast<const GT*>(t.g);
+    float p[2][4], g[2][4], m[2][4], v[2][4];
+    uint32_t mc[2], vc[2];
+    float ms = 0.0f, vs = 0.0f;
+    if (B8) {
+        ms = t.ms[i0 >> 8];
+        vs = t.vs[i0 >> 8];
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        load4<FULL>(gp, at[h], n, g[h]);
+        load4<FULL>(pp, at[h], n, p[h]);
+        if (B8) {
+            mc[h] = load4<FULL>(static_cast<const uint8_t*>(t.m), at[h], n);
+            vc[h] = load4<FULL>(static_cast<const uint8_t*>(t.v), at[h], n);
+        } else {
+            load4<FULL>(static_cast<const float*>(t.m), at[h], n, m[h]);
+            load4<FULL>(static_cast<const float*>(t.v), at[h], n, v[h]);
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (B8) {
+                m[h][e] = decode8<true>((mc[h] >> (8 * e)) & 255u, ms);
+                v[h][e] = decode8<false>((vc[h] >> (8 * e)) & 255u, vs);
+            }
+            const float gg = __fmul_rn(g[h][e], coef);
+            m[h][e] = __fadd_rn(__fmul_rn(m[h][e], b.b1), __fmul_rn(gg, b.c1));
+            v[h][e] = __fadd_rn(__fmul_rn(v[h][e], b.b2), __fmul_rn(__fmul_rn(gg, gg), b.c2));
+            const float den = __fmaf_rn(sqrt_fast(v[h][e]), b.rbc2, b.eps);
+            p[h][e] = __fmaf_rn(p[h][e], t.keep, -__fdividef(__fmul_rn(m[h][e], t.step), den));
+        }
+        store4<FULL>(pp, at[h], n, p[h]);
+        if (t.copy != nullptr) store4<FULL>(reinterpret_cast<__nv_bfloat16*>(t.copy), at[h], n, p[h]);
+        if (!B8) {
+            store4<FULL>(static_cast<float*>(t.m), at[h], n, m[h]);
+            store4<FULL>(static_cast<float*>(t.v), at[h], n, v[h]);
+        }
+    }
+    if (B8) {
+        const float mt = warp_top(m[0], m[1]), vt = warp_top(v[0], v[1]);
+        const bool mf = !(mt < 0x1p-100f), vf = !(vt < 0x1p-100f);
+        const float mi = mf ? __fdiv_rn(kCodeTop, mt) : 0.0f, vi = vf ? __fdiv_rn(kCodeTop, vt) : 0.0f;
+        const uint32_t key = mix32(t.key ^ static_cast<uint32_t>(static_cast<unsigned long long>(i0) >> 32));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t mw = 0, vw = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t r = mix32(static_cast<uint32_t>(at[h] + e) ^ key);
+                mw |= encode8<true>(m[h][e], mi, r & 0xFFFFu) << (8 * e);
+                vw |= encode8<false>(v[h][e], vi, r >> 16) << (8 * e);
+            }
+            store4<FULL>(static_cast<uint8_t*>(t.m), at[h], n, mw);
+            store4<FULL>(static_cast<uint8_t*>(t.v), at[h], n, vw);
+        }
+        if (lane == 0) {
+            t.ms[i0 >> 8] = mf ? __fmul_rn(mt, kCodeUnit) : 0.0f;
+            t.vs[i0 >> 8] = vf ? __fmul_rn(vt, kCodeUnit) : 0.0f;
+        }
+    }
+}
+
+template <class PT, class GT, bool B8>
+__device__ __forceinline__ void adam_any(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, int lane) {
+    if ((t.kind & kAdamVector) && i0 + MOARA_ADAMW_BLOCK <= t.n)
+        adam_tile<PT, GT, B8, true>(t, b, coef, i0, lane);
+    else
+        adam_tile<PT, GT, B8, false>(t, b, coef, i0, lane);
+}
+
+// Largest i < count with start(i) <= c.
+template <class F> __device__ __forceinline__ int find_tensor(int count, uint32_t c, F start) {
+    int lo = 0, hi = count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (start(mid) <= c) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+__global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ AdamBatch b) {
+    const uint32_t c = blockIdx.x;
+    const int q = find_tensor(b.count, c, [&](int i) { return b.start[i]; });
+    const AdamTensor& t = b.t[q];
+    const int lane = threadIdx.x & 31;
+    const long long i0 = static_cast<long long>(c - b.start[q]) * kAdamChunk + (threadIdx.x >> 5) * MOARA_ADAMW_BLOCK;
+    if (i0 >= t.n) return;
+    const float coef = b.scale != nullptr ? *b.scale : 1.0f;
+    switch (t.kind & 7u) {
+        case 0: adam_any<float, float, false>(t, b, coef, i0, lane); break;
+        case 1: adam_any<__nv_bfloat16, float, false>(t, b, coef, i0, lane); break;
+        case 2: adam_any<float, __nv_bfloat16, false>(t, b, coef, i0, lane); break;
+        case 3: adam_any<__nv_bfloat16, __nv_bfloat16, false>(t, b, coef, i0, lane); break;
+        case 4: adam_any<float, float, true>(t, b, coef, i0, lane); break;
+        case 5: adam_any<__nv_bfloat16, float, true>(t, b, coef, i0, lane); break;
+        case 6: adam_any<float, __nv_bfloat16, true>(t, b, coef, i0, lane); break;
+        default: adam_any<__nv_bfloat16, __nv_bfloat16, true>(t, b, coef, i0, lane); break;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Moments as fp32.
+// ---------------------------------------------------------------------------
+template <bool SIGNED>
+__device__ __forceinline__ void moment_tile(const void* x, const float* scale, float* out, int block8, long long i0,
+                                            long long n, int lane) {
+    if (out == nullptr) return;
+    const bool full = i0 + MOARA_ADAMW_BLOCK <= n && (reinterpret_cast<uintptr_t>(out) & 15) == 0 &&
+                      (reinterpret_cast<uintptr_t>(x) & 15) == 0;
+    const float s = block8 ? scale[i0 >> 8] : 0.0f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const long long i = i0 + 128 * h + 4 * lane;
+        float v[4];
+        if (block8) {
+            const uint8_t* c = static_cast<const uint8_t*>(x);
+            const uint32_t w = full ? load4<true>(c, i, n) : load4<false>(c, i, n);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = decode8<SIGNED>((w >> (8 * e)) & 255u, s);
+        } else if (full) {
+            load4<true>(static_cast<const float*>(x), i, n, v);
+        } else {
+            load4<false>(static_cast<const float*>(x), i, n, v);
+        }
+        if (full) store4<true>(out, i, n, v); else store4<false>(out, i, n, v);
+    }
+}
+
+__global__ void __launch_bounds__(256) k_moments(const __grid_constant__ MomentBatch b) {
+    const uint32_t c = blockIdx.x;
+    const int q = find_tensor(b.count, c, [&](int i) { return b.start[i]; });
+    const MomentTensor& t = b.t[q];
+    const int lane = threadIdx.x & 31;
+    const long long i0 = static_cast<long long>(c - b.start[q]) * kAdamChunk + (threadIdx.x >> 5) * MOARA_ADAMW_BLOCK;
+    if (i0 >= t.n) return;
+    moment_tile<true>(t.m, t.ms, t.om, t.block8, i0, t.n, lane);
+    moment_tile<false>(t.v, t.vs, t.ov, t.block8, i0, t.n, lane);
+}
+
+// ---------------------------------------------------------------------------
+// Gradient norm.  A thread sums at most 32 squares of a chunk in fp32 and adds
+// the chunk sums in fp64; CTA sums go to the workspace, and the CTA that draws
+// the last ticket adds them in order.  Which CTA that is does not change the
+// result: chunks belong to CTAs by index.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ double cta_sum(double v, double* red) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    double t = 0.0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t += red[i];
+    return t;
+}
+
+template <class T>
+__device__ __forceinline__ float chunk_squares(const T* g, long long e0, long long n, bool vector) {
+    float s = 0.0f;
+    if (vector && e0 + kGradChunk <= n) {
+        constexpr int V = kGradChunk / 256 / 4;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            float v[4];
+            load4<true>(g, e0 + 4 * (threadIdx.x + 256 * k), n, v);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s = fmaf(v[e], v[e], s);
+        }
+    } else {
+        const long long e1 = min(e0 + static_cast<long long>(kGradChunk), n);
+        for (long long i = e0 + threadIdx.x; i < e1; i += 256) {
+            const float x = static_cast<float>(g[i]);
+            s = fmaf(x, x, s);
+        }
+    }
+    return s;
+}
+
+__global__ void __launch_bounds__(256) k_grad_norm(const __grid_constant__ NormBatch b) {
+    __shared__ double red[8];
+    __shared__ bool finish;
+    double acc = 0.0;
+    for (uint32_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
+        const int q = find_tensor(b.count, c, [&](int i) { return b.t[i].start; });
+        const NormTensor& t = b.t[q];
+        const long long e0 = static_cast<long long>(c - t.start) * kGradChunk;
+        const bool vec = (t.kind & kAdamVector) != 0;
+        acc += (t.kind & kAdamGradBf16) ? chunk_squares(static_cast<const __nv_bfloat16*>(t.g), e0, t.n, vec)
+                                        : chunk_squares(static_cast<const float*>(t.g), e0, t.n, vec);
+    }
+    const double sum = cta_sum(acc, red);
+    if (threadIdx.x == 0) {
+        b.partials[b.first + blockIdx.x] = sum;
+        __threadfence();
+        const unsigned int order = b.last ? atomicAdd(b.ticket, 1u) : 0u;
+        finish = b.last && order == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!finish) return;
+    __threadfence();
+    double part = 0.0;
+    for (int i = threadIdx.x; i < b.first + static_cast<int>(gridDim.x); i += 256) part += __ldcg(b.partials + i);
+    const double total = cta_sum(part, red);
+    if (threadIdx.x == 0) {
+        *b.ticket = 0;
+        const double norm = sqrt(total + (b.extra != nullptr ? static_cast<double>(*b.extra) : 0.0));
+        const double coef = static_cast<double>(b.max_norm) / (norm + 1e-6);
+        b.out[0] = static_cast<float>(total);
+        b.out[1] = static_cast<float>(norm);
+        b.out[2] = b.max_norm > 0.0f && !(coef >= 1.0) ? static_cast<float>(coef) : 1.0f;
+    }
+}
+
+}  // namespace
+
+uint32_t adamw_key(uint64_t seed, uint32_t id, int64_t t) {
+    uint32_t k = mix32(mix32(static_cast<uint32_t>(seed)) ^ static_cast<uint32_t>(seed >> 32));
+    k = mix32(k ^ id);
+    return mix32(k ^ static_cast<uint32_t>(t));
+}
+
+cudaError_t launch_adamw(const AdamBatch& b, cudaStream_t s, int64_t* launches) {
+    k_adamw<<<b.start[b.count], 256, 0, s>>>(b);
+    ++*launches;
+    return cudaGetLastError();
+}
+
+cudaError_t launch_moments(const MomentBatch& b, cudaStream_t s, int64_t* launches) {
+    k_moments<<<b.start[b.count], 256, 0, s>>>(b);
+    ++*launches;
+    return cudaGetLastError();
+}
+
+cudaError_t launch_grad_norm(const NormBatch& b, int ctas, cudaStream_t s, int64_t* launches) {
+    k_grad_norm<<<ctas, 256, 0, s>>>(b);
+    ++*launches;
+    return cudaGetLastError();
+}
+
+}  // namespace moara

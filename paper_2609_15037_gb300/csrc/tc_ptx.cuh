@@ -328,5 +328,48 @@ __host__ __device__ constexpr uint32_t idesc_bf16(int M, int N, int a_mn, int b_
            (static_cast<uint32_t>(M >> 4) << 24);
 }
 
+// ---------------------------------------------------------------- block-scaled fp4
+// Untiled bulk copy of `bytes` (a multiple of 16, both sides 16-byte aligned).
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile(
+        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+        "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
+        : "memory");
+}
+
+// 512 bytes of scales (32 rows of 16 bytes, no swizzle) into four TMEM columns,
+// the same for each of the four lane quadrants.  Ordered before the MMAs that
+// the same thread issues after it.
+__device__ __forceinline__ void tmem_cp_scales(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+
+// D[tmem] (+)= (A * scale A) (B * scale B)^T, both E2M1 with an E8M0 scale per 32
+// entries of K, K = 64, issued by one thread.
+__device__ __forceinline__ void mma_mxf4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                         uint32_t sfa_tmem, uint32_t sfb_tmem, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(
+            d_tmem),
+        "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa_tmem), "r"(sfb_tmem), "r"(accumulate)
+        : "memory");
+}
+
+// Shared-memory matrix descriptor without swizzle: 8-row groups of 16-byte rows,
+// `sbo` bytes apart.
+__device__ __forceinline__ uint64_t smem_desc_plain(uint32_t saddr, uint32_t sbo) {
+    return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | static_cast<uint64_t>((sbo >> 4) & 0x3FFFu) << 32 |
+           static_cast<uint64_t>(1) << 46;
+}
+
+// Instruction descriptor of kind::mxf4: E2M1 operands, K-major, E8M0 scales.  half: which
+// two bytes of a scale word the MMA's 64 entries of K take (0 or 1).
+__host__ __device__ constexpr uint32_t idesc_mxf4(int M, int N, int half) {
+    return (static_cast<uint32_t>(2 * half) << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(N >> 3) << 17) |
+           (1u << 23) | (static_cast<uint32_t>(M >> 4) << 24) | (static_cast<uint32_t>(2 * half) << 29);
+}
+
 }  // namespace ptx
 }  // namespace moara
