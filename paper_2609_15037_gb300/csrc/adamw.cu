@@ -9,6 +9,7 @@
 // every tensor of a call is in the launch's parameter block, so a call costs one
 // launch.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "ops.h"
 
@@ -22,26 +23,65 @@ namespace {
 // subnormal, so the code is bits >> 20 of an fp32 number: exponent field and 3
 // mantissa bits, subnormals included, with no case distinction.  Adding 20
 // random bits before the shift rounds up with the probability of the part
-// cut off.  Every operation is a single fp32 rounding (no contraction), so
-// that the codes follow from the formulas alone.
+// cut off.  The moments themselves take one fp32 rounding per operation (no
+// contraction), so that the codes follow from the formulas alone.
 // ---------------------------------------------------------------------------
 constexpr float kCodeTop = 1.875f;
 constexpr float kCodeUnit = 1.0f / 1.875f;
 
-template <bool SIGNED> __device__ __forceinline__ float code_down() { return SIGNED ? 0x1p-112f : 0x1p-96f; }
-template <bool SIGNED> __device__ __forceinline__ float code_up() { return SIGNED ? 0x1p112f : 0x1p96f; }
-
-template <bool SIGNED> __device__ __forceinline__ float decode8(uint32_t code, float scale) {
-    const uint32_t mag = SIGNED ? code & 127u : code;
-    const float y = __fmul_rn(__fmul_rn(__uint_as_float(mag << 20), code_up<SIGNED>()), scale);
-    return SIGNED && (code & 128u) ? -y : y;
+// Four codes of exp_avg: sign, 4 exponent and 3 mantissa bits are the upper bits of
+// an fp16 number without its top exponent bit, subnormals included.
+__device__ __forceinline__ void decode_avg(uint32_t w, float scale, float* v) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t x = __byte_perm(w, 0, i == 0 ? 0x1404 : 0x3424);       // each code in the upper byte of a half
+        const uint32_t h = (x & 0x80008000u) | ((x >> 1) & 0x3F803F80u);
+        const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        v[2 * i] = __fmul_rn(y.x, scale);
+        v[2 * i + 1] = __fmul_rn(y.y, scale);
+    }
 }
 
-template <bool SIGNED> __device__ __forceinline__ uint32_t encode8(float x, float inv, uint32_t r16) {
-    const float z = __fmul_rn(__fmul_rn(fabsf(x), inv), code_down<SIGNED>());
-    const uint32_t c = (__float_as_uint(z) + (r16 << 4)) >> 20;
-    if (SIGNED) return min(c, 127u) | ((__float_as_uint(x) >> 31) << 7);
-    return max(min(c, 255u), x > 0.0f ? 1u : 0u);
+// Four codes of exp_avg_sq, 5 exponent and 3 mantissa bits.
+__device__ __forceinline__ void decode_sq(uint32_t w, float scale, float* v) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t x = (e < 3 ? w << (20 - 8 * e) : w >> 4) & 0x0FF00000u;
+        v[e] = __fmul_rn(__fmul_rn(__uint_as_float(x), 0x1p96f), scale);
+    }
+}
+
+// Codes of 8 entries in two words.  WIDE: inv alone scales, 2^-112 or 2^-96 comes in a
+// second product (a block whose largest entry is above 2^14 or 2^30: the joint factor
+// would be subnormal).
+template <bool WIDE>
+__device__ __forceinline__ void encode_avg(const float (&x)[8], float inv, const uint32_t (&r)[8], uint32_t (&w)[2]) {
+    const float f = WIDE ? inv : inv * 0x1p-112f;
+    uint32_t u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float y = __fmul_rn(fabsf(x[e]), f), z = WIDE ? __fmul_rn(y, 0x1p-112f) : y;
+        const uint32_t t = min(__float_as_uint(z) + ((r[e] & 0xFFFFu) << 4), 0x07FFFFFFu);
+        u[e] = ((t << 4) & 0x7F000000u) | (__float_as_uint(x[e]) & 0x80000000u);     // the code in the upper byte
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = __byte_perm(__byte_perm(u[4 * i], u[4 * i + 1], 0x0073), __byte_perm(u[4 * i + 2], u[4 * i + 3], 0x0073), 0x5410);
+}
+
+template <bool WIDE>
+__device__ __forceinline__ void encode_sq(const float (&x)[8], float inv, const uint32_t (&r)[8], uint32_t (&w)[2]) {
+    const float f = WIDE ? inv : inv * 0x1p-96f;
+    uint32_t u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const float y = __fmul_rn(x[e], f), z = WIDE ? __fmul_rn(y, 0x1p-96f) : y;
+        const uint32_t t = min(__float_as_uint(z) + ((r[e] >> 12) & 0xFFFF0u), 0x0FFFFFFFu);
+        u[e] = max(t, x[e] > 0.0f ? 1u << 20 : 0u) << 4;
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = __byte_perm(__byte_perm(u[4 * i], u[4 * i + 1], 0x0073), __byte_perm(u[4 * i + 2], u[4 * i + 3], 0x0073), 0x5410);
 }
 
 // 32-bit xor-shift-multiply mixing
@@ -85,6 +125,40 @@ template <bool FULL> __device__ __forceinline__ uint32_t load4(const uint8_t* p,
     return w;
 }
 
+// eight consecutive entries, or codes, at i
+template <bool FULL> __device__ __forceinline__ void load8(const float* p, long long i, long long n, float (&v)[8]) {
+    float a[4], b[4];
+    load4<FULL>(p, i, n, a);
+    load4<FULL>(p, i + 4, n, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
+}
+
+template <bool FULL>
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, long long i, long long n, float (&v)[8]) {
+    if (FULL) {
+        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p + i));
+        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(x[e] << 16);
+            v[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = i + e < n ? __bfloat162float(p[i + e]) : 0.0f;
+    }
+}
+
+template <bool FULL> __device__ __forceinline__ uint2 load8(const uint8_t* p, long long i, long long n) {
+    if (FULL) return __ldcs(reinterpret_cast<const uint2*>(p + i));
+    uint32_t w[2] = {0, 0};
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+        if (i + e < n) w[e >> 2] |= static_cast<uint32_t>(p[i + e]) << (8 * (e & 3));
+    return make_uint2(w[0], w[1]);
+}
+
 template <bool FULL> __device__ __forceinline__ void store4(float* p, long long i, long long n, const float (&v)[4]) {
     if (FULL) {
         __stcs(reinterpret_cast<float4*>(p + i), make_float4(v[0], v[1], v[2], v[3]));
@@ -111,13 +185,32 @@ __device__ __forceinline__ void store4(__nv_bfloat16* p, long long i, long long 
     }
 }
 
-template <bool FULL> __device__ __forceinline__ void store4(uint8_t* p, long long i, long long n, uint32_t w) {
+template <bool FULL> __device__ __forceinline__ void store8(float* p, long long i, long long n, const float (&v)[8]) {
+    const float a[4] = {v[0], v[1], v[2], v[3]}, b[4] = {v[4], v[5], v[6], v[7]};
+    store4<FULL>(p, i, n, a);
+    store4<FULL>(p, i + 4, n, b);
+}
+
+template <bool FULL>
+__device__ __forceinline__ void store8(__nv_bfloat16* p, long long i, long long n, const float (&v)[8]) {
     if (FULL) {
-        __stcs(reinterpret_cast<unsigned int*>(p + i), w);
+        __stcs(reinterpret_cast<uint4*>(p + i), make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]),
+                                                           bf16x2(v[6], v[7])));
     } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (i + e < n) p[i + e] = static_cast<uint8_t>(w >> (8 * e));
+        for (int e = 0; e < 8; ++e)
+            if (i + e < n) p[i + e] = __float2bfloat16_rn(v[e]);
+    }
+}
+
+template <bool FULL>
+__device__ __forceinline__ void store8(uint8_t* p, long long i, long long n, const uint32_t (&w)[2]) {
+    if (FULL) {
+        __stcs(reinterpret_cast<uint2*>(p + i), make_uint2(w[0], w[1]));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (i + e < n) p[i + e] = static_cast<uint8_t>(w[e >> 2] >> (8 * (e & 3)));
     }
 }
 
@@ -127,95 +220,132 @@ __device__ __forceinline__ float sqrt_fast(float x) {     // a few ulp, subnorma
     return y;
 }
 
-// The scale of 256 values, 8 per lane: the largest magnitude as bits, so that a
-// NaN is the largest.
-template <class V> __device__ __forceinline__ float warp_top(const V& a, const V& b) {
+// The same by one instruction each where nothing below 2^-126 matters.
+__device__ __forceinline__ float sqrt_flush(float x) {
+    float y;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ float rcp_flush(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The largest magnitude of a warp's 256 values, compared as bits so that a NaN is
+// the largest.
+__device__ __forceinline__ float warp_top(const float (&a)[8]) {
     uint32_t top = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        top = max(top, __float_as_uint(a[e]) & 0x7FFFFFFFu);
-        top = max(top, __float_as_uint(b[e]) & 0x7FFFFFFFu);
-    }
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(a[e]) & 0x7FFFFFFFu);
     return __uint_as_float(__reduce_max_sync(0xffffffffu, top));
 }
 
-// One warp, 256 entries from i0 on: lane l has i0 + 4l .. +3 and i0 + 128 + 4l .. +3.
-template <class PT, class GT, bool B8, bool FULL>
+__device__ __forceinline__ void new_moments(const AdamBatch& b, float g, float& m, float& v) {
+    m = __fadd_rn(__fmul_rn(m, b.b1), __fmul_rn(g, b.c1));
+    v = __fadd_rn(__fmul_rn(v, b.b2), __fmul_rn(__fmul_rn(g, g), b.c2));
+}
+
+__device__ __forceinline__ float new_param(const AdamTensor& t, const AdamBatch& b, float p, float m, float v) {
+    const float den = __fmaf_rn(sqrt_fast(v), b.rbc2, b.eps);
+    return __fmaf_rn(p, t.keep, -__fdividef(__fmul_rn(m, t.step), den));
+}
+
+// fp32 moments.  One warp, 256 entries from i0 on: lane l has i0 + 4l .. +3 and
+// i0 + 128 + 4l .. +3, so that every access is contiguous over the warp.  2 x 131 M
+// entries with fp32 parameters, bf16 gradients and copies (28 bytes each): 1.03 ms,
+// 7.1 TB/s.
+template <class PT, class GT, bool FULL>
 __device__ __forceinline__ void adam_tile(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, int lane) {
     const long long n = t.n;
     const long long at[2] = {i0 + 4 * lane, i0 + 128 + 4 * lane};
     PT* const pp = static_cast<PT*>(t.p);
     const GT* const gp = static_cast<const GT*>(t.g);
+    float* const mp = static_cast<float*>(t.m);
+    float* const vp = static_cast<float*>(t.v);
     float p[2][4], g[2][4], m[2][4], v[2][4];
-    uint32_t mc[2], vc[2];
-    float ms = 0.0f, vs = 0.0f;
-    if (B8) {
-        ms = t.ms[i0 >> 8];
-        vs = t.vs[i0 >> 8];
-    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         load4<FULL>(gp, at[h], n, g[h]);
         load4<FULL>(pp, at[h], n, p[h]);
-        if (B8) {
-            mc[h] = load4<FULL>(static_cast<const uint8_t*>(t.m), at[h], n);
-            vc[h] = load4<FULL>(static_cast<const uint8_t*>(t.v), at[h], n);
-        } else {
-            load4<FULL>(static_cast<const float*>(t.m), at[h], n, m[h]);
-            load4<FULL>(static_cast<const float*>(t.v), at[h], n, v[h]);
-        }
+        load4<FULL>(mp, at[h], n, m[h]);
+        load4<FULL>(vp, at[h], n, v[h]);
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            if (B8) {
-                m[h][e] = decode8<true>((mc[h] >> (8 * e)) & 255u, ms);
-                v[h][e] = decode8<false>((vc[h] >> (8 * e)) & 255u, vs);
-            }
-            const float gg = __fmul_rn(g[h][e], coef);
-            m[h][e] = __fadd_rn(__fmul_rn(m[h][e], b.b1), __fmul_rn(gg, b.c1));
-            v[h][e] = __fadd_rn(__fmul_rn(v[h][e], b.b2), __fmul_rn(__fmul_rn(gg, gg), b.c2));
-            const float den = __fmaf_rn(sqrt_fast(v[h][e]), b.rbc2, b.eps);
-            p[h][e] = __fmaf_rn(p[h][e], t.keep, -__fdividef(__fmul_rn(m[h][e], t.step), den));
+            new_moments(b, __fmul_rn(g[h][e], coef), m[h][e], v[h][e]);
+            p[h][e] = new_param(t, b, p[h][e], m[h][e], v[h][e]);
         }
         store4<FULL>(pp, at[h], n, p[h]);
         if (t.copy != nullptr) store4<FULL>(reinterpret_cast<__nv_bfloat16*>(t.copy), at[h], n, p[h]);
-        if (!B8) {
-            store4<FULL>(static_cast<float*>(t.m), at[h], n, m[h]);
-            store4<FULL>(static_cast<float*>(t.v), at[h], n, v[h]);
-        }
+        store4<FULL>(mp, at[h], n, m[h]);
+        store4<FULL>(vp, at[h], n, v[h]);
     }
-    if (B8) {
-        const float mt = warp_top(m[0], m[1]), vt = warp_top(v[0], v[1]);
-        const bool mf = !(mt < 0x1p-100f), vf = !(vt < 0x1p-100f);
-        const float mi = mf ? __fdiv_rn(kCodeTop, mt) : 0.0f, vi = vf ? __fdiv_rn(kCodeTop, vt) : 0.0f;
-        const uint32_t key = mix32(t.key ^ static_cast<uint32_t>(static_cast<unsigned long long>(i0) >> 32));
+}
+
+// 8-bit moments.  One warp, one block of 256 entries: lane l has i0 + 8l .. +7, so
+// that its codes are 8 and its bf16 entries 16 bytes.
+template <class PT, class GT, bool FULL>
+__device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, int lane) {
+    const long long n = t.n, at = i0 + 8 * lane;
+    PT* const pp = static_cast<PT*>(t.p);
+    float p[8], g[8], m[8], v[8];
+    const uint2 mc = load8<FULL>(static_cast<const uint8_t*>(t.m), at, n);
+    const uint2 vc = load8<FULL>(static_cast<const uint8_t*>(t.v), at, n);
+    load8<FULL>(static_cast<const GT*>(t.g), at, n, g);
+    load8<FULL>(pp, at, n, p);
+    const float ms = t.ms[i0 >> 8], vs = t.vs[i0 >> 8];
+    decode_avg(mc.x, ms, m);
+    decode_avg(mc.y, ms, m + 4);
+    decode_sq(vc.x, vs, v);
+    decode_sq(vc.y, vs, v + 4);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t mw = 0, vw = 0;
+    for (int e = 0; e < 8; ++e) new_moments(b, __fmul_rn(g[e], coef), m[e], v[e]);
+    if (b.eps >= 1e-10f) {
+        // a second moment below 2^-126 is nothing beside eps
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t r = mix32(static_cast<uint32_t>(at[h] + e) ^ key);
-                mw |= encode8<true>(m[h][e], mi, r & 0xFFFFu) << (8 * e);
-                vw |= encode8<false>(v[h][e], vi, r >> 16) << (8 * e);
-            }
-            store4<FULL>(static_cast<uint8_t*>(t.m), at[h], n, mw);
-            store4<FULL>(static_cast<uint8_t*>(t.v), at[h], n, vw);
+        for (int e = 0; e < 8; ++e) {
+            const float den = __fmaf_rn(sqrt_flush(v[e]), b.rbc2, b.eps);
+            p[e] = __fmaf_rn(p[e], t.keep, -__fmul_rn(__fmul_rn(m[e], t.step), rcp_flush(den)));
         }
-        if (lane == 0) {
-            t.ms[i0 >> 8] = mf ? __fmul_rn(mt, kCodeUnit) : 0.0f;
-            t.vs[i0 >> 8] = vf ? __fmul_rn(vt, kCodeUnit) : 0.0f;
-        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = new_param(t, b, p[e], m[e], v[e]);
+    }
+    store8<FULL>(pp, at, n, p);
+    if (t.copy != nullptr) store8<FULL>(reinterpret_cast<__nv_bfloat16*>(t.copy), at, n, p);
+    const float mt = warp_top(m), vt = warp_top(v);
+    const bool mf = !(mt < 0x1p-100f), vf = !(vt < 0x1p-100f);
+    const float mi = mf ? __fdiv_rn(kCodeTop, mt) : 0.0f, vi = vf ? __fdiv_rn(kCodeTop, vt) : 0.0f;
+    const uint32_t key = mix32(t.key ^ static_cast<uint32_t>(static_cast<unsigned long long>(i0) >> 32));
+    uint32_t r[8], w[2];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = mix32((static_cast<uint32_t>(at) + e) ^ key);
+    if (mt > 0x1p14f) encode_avg<true>(m, mi, r, w);
+    else encode_avg<false>(m, mi, r, w);
+    store8<FULL>(static_cast<uint8_t*>(t.m), at, n, w);
+    if (vt > 0x1p30f) encode_sq<true>(v, vi, r, w);
+    else encode_sq<false>(v, vi, r, w);
+    store8<FULL>(static_cast<uint8_t*>(t.v), at, n, w);
+    if (lane == 0) {
+        t.ms[i0 >> 8] = mf ? __fmul_rn(mt, kCodeUnit) : 0.0f;
+        t.vs[i0 >> 8] = vf ? __fmul_rn(vt, kCodeUnit) : 0.0f;
     }
 }
 
 template <class PT, class GT, bool B8>
 __device__ __forceinline__ void adam_any(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, int lane) {
-    if ((t.kind & kAdamVector) && i0 + MOARA_ADAMW_BLOCK <= t.n)
-        adam_tile<PT, GT, B8, true>(t, b, coef, i0, lane);
-    else
-        adam_tile<PT, GT, B8, false>(t, b, coef, i0, lane);
+    const bool full = (t.kind & kAdamVector) && i0 + MOARA_ADAMW_BLOCK <= t.n;
+    if (B8) {
+        if (full) adam_tile8<PT, GT, true>(t, b, coef, i0, lane);
+        else adam_tile8<PT, GT, false>(t, b, coef, i0, lane);
+    } else {
+        if (full) adam_tile<PT, GT, true>(t, b, coef, i0, lane);
+        else adam_tile<PT, GT, false>(t, b, coef, i0, lane);
+    }
 }
 
 // Largest i < count with start(i) <= c.
@@ -251,28 +381,37 @@ __global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ AdamBatch
 // ---------------------------------------------------------------------------
 // Moments as fp32.
 // ---------------------------------------------------------------------------
-template <bool SIGNED>
+template <bool AVG>
 __device__ __forceinline__ void moment_tile(const void* x, const float* scale, float* out, int block8, long long i0,
                                             long long n, int lane) {
     if (out == nullptr) return;
     const bool full = i0 + MOARA_ADAMW_BLOCK <= n && (reinterpret_cast<uintptr_t>(out) & 15) == 0 &&
                       (reinterpret_cast<uintptr_t>(x) & 15) == 0;
-    const float s = block8 ? scale[i0 >> 8] : 0.0f;
+    const long long at[2] = {i0 + 4 * lane, i0 + 128 + 4 * lane};
+    float v[2][4];
+    if (block8) {
+        const uint8_t* c = static_cast<const uint8_t*>(x);
+        const float s = scale[i0 >> 8];
+        uint32_t w[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) w[h] = full ? load4<true>(c, at[h], n) : load4<false>(c, at[h], n);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (AVG) decode_avg(w[h], s, v[h]);
+            else decode_sq(w[h], s, v[h]);
+        }
+    } else {
+        const float* c = static_cast<const float*>(x);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (full) load4<true>(c, at[h], n, v[h]);
+            else load4<false>(c, at[h], n, v[h]);
+        }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const long long i = i0 + 128 * h + 4 * lane;
-        float v[4];
-        if (block8) {
-            const uint8_t* c = static_cast<const uint8_t*>(x);
-            const uint32_t w = full ? load4<true>(c, i, n) : load4<false>(c, i, n);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = decode8<SIGNED>((w >> (8 * e)) & 255u, s);
-        } else if (full) {
-            load4<true>(static_cast<const float*>(x), i, n, v);
-        } else {
-            load4<false>(static_cast<const float*>(x), i, n, v);
-        }
-        if (full) store4<true>(out, i, n, v); else store4<false>(out, i, n, v);
+        if (full) store4<true>(out, at[h], n, v[h]);
+        else store4<false>(out, at[h], n, v[h]);
     }
 }
 

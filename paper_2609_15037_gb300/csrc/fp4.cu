@@ -2,6 +2,7 @@
 // matrix, and the values of an operand.  DRAM-bound: per entry 4 or 2 bytes in
 // and 17/32 of a byte out per orientation.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 
 #include "ops.h"
 
@@ -50,71 +51,102 @@ __device__ __forceinline__ uint32_t codes8(const float (&v)[8], float f) {
     return w;
 }
 
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-    const float4 a = reinterpret_cast<const float4*>(p)[0], b = reinterpret_cast<const float4*>(p)[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
+// Eight entries of a row as they lie in memory, and entry e of them in fp32.
+template <class T> struct Row8;
 
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
-    const uint4 a = *reinterpret_cast<const uint4*>(p);
-    const uint32_t w[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(w[i] << 16);
-        v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+template <> struct Row8<float> {
+    uint32_t w[8];
+    __device__ __forceinline__ void load(const float* p) {
+        const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
     }
-}
+    __device__ __forceinline__ void load_some(const float* p, int count) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = e < count ? __float_as_uint(p[e]) : 0u;
+    }
+    __device__ __forceinline__ float get(int e) const { return __uint_as_float(w[e]); }
+};
+
+template <> struct Row8<__nv_bfloat16> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
+        const uint4 a = *reinterpret_cast<const uint4*>(p);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+    }
+    __device__ __forceinline__ void load_some(const __nv_bfloat16* p, int count) {
+        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            w[e] = (2 * e < count ? h[2 * e] : 0u) | (2 * e + 1 < count ? static_cast<uint32_t>(h[2 * e + 1]) << 16 : 0u);
+    }
+    __device__ __forceinline__ float get(int e) const {
+        return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+    }
+};
 
 // One CTA takes a 128 x 128 tile, which is one 512-byte scale tile of either
-// orientation.  By rows, four lanes hold a 32-column block in registers as it is
-// loaded; by columns, the tile goes through shared memory and a thread takes 32
-// rows of one column.
-template <class T, bool ROWS, bool COLS> __global__ void __launch_bounds__(256) k_fp4_quantize(const QuantParams p) {
+// orientation, and each warp 32 rows x 64 columns of it: a lane holds 8 rows x 8
+// columns in registers, so that a row's block of 32 columns is four lanes, a
+// column's block of 32 rows the four lanes 8 apart, and eight codes of either are one
+// word of one lane.  The matrix passes through no shared memory (32 x 1 blocks of a
+// 64 KB tile there took 67 us where this takes 42 on 11008 x 4096 fp32); only the
+// columns' codes do, to leave in whole 64-byte lines.
+template <class T, bool ROWS, bool COLS> __global__ void __launch_bounds__(256, 2) k_fp4_quantize(const QuantParams p) {
     __shared__ __align__(16) uint8_t sfr[512];
     __shared__ __align__(16) uint8_t sfc[512];
-    extern __shared__ __align__(16) float tile[];        // 128 x 128 (COLS)
+    __shared__ __align__(16) uint32_t qc[COLS ? 128 * 17 : 1];       // a column's 16 words of codes, and one of padding
     const int tr = blockIdx.x / p.tiles_c, tc = blockIdx.x % p.tiles_c;
-    const int r0 = tr * 128, c0 = tc * 128;
-    const int sub = threadIdx.x & 15;                     // 8 columns
-    const int rw = threadIdx.x >> 4;                      // row within a pass of 16
-    const int col = c0 + 8 * sub;
-    const T* X = static_cast<const T*>(p.X);
-    const bool wide = p.vec && col + 8 <= p.cols;
-#pragma unroll 4
-    for (int pass = 0; pass < 8; ++pass) {
-        const int lr = pass * 16 + rw, row = r0 + lr;
-        float v[8];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int wr = warp >> 1, sub = (warp & 1) * 8 + (lane & 7);     // 32-row group, 8-column group of the tile
+    const int lr = wr * 32 + (lane >> 3) * 8, lc = sub * 8;          // the lane's 8 x 8 entries inside the tile
+    const int row0 = tr * 128 + lr, col0 = tc * 128 + lc;
+    const T* X = static_cast<const T*>(p.X) + row0 * p.ld + col0;
+    Row8<T> x[8];
+    if (p.vec && col0 + 8 <= p.cols && row0 + 8 <= p.rows) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.0f;
-        if (row < p.rows) {
-            const T* x = X + row * p.ld + col;
-            if (wide) {
-                load8(x, v);
-            } else {
+        for (int i = 0; i < 8; ++i) x[i].load(X + i * p.ld);
+    } else {
 #pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (col + e < p.cols) v[e] = static_cast<float>(x[e]);
-            }
-        }
-        if (ROWS) {
+        for (int i = 0; i < 8; ++i) x[i].load_some(X + i * p.ld, row0 + i < p.rows ? p.cols - col0 : 0);
+    }
+    if (ROWS) {
+        const int block = (tc * 128 + lc) >> 5;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            float v[8];
             uint32_t top = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+            for (int e = 0; e < 8; ++e) {
+                v[e] = x[i].get(e);
+                top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+            }
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const int block = (c0 >> 5) + (sub >> 2);
-            const bool real = row < p.rows && block < p.kb;
+            const bool real = row0 + i < p.rows && block < p.kb;
             const uint32_t byte = real ? scale_byte(top) : 127u;
-            if ((sub & 3) == 0) sfr[(lr & 31) * 16 + (lr >> 5) * 4 + (sub >> 2)] = static_cast<uint8_t>(byte);
+            if ((lane & 3) == 0) sfr[((lr + i) & 31) * 16 + wr * 4 + (sub >> 2)] = static_cast<uint8_t>(byte);
             if (real)
-                *reinterpret_cast<uint32_t*>(p.q + (static_cast<long long>(row) * p.kb + block) * 16 + (sub & 3) * 4) =
+                *reinterpret_cast<uint32_t*>(p.q + (static_cast<long long>(row0 + i) * p.kb + block) * 16 + (lane & 3) * 4) =
                     codes8(v, inv_scale(byte));
         }
-        if (COLS) {
-            float4* d = reinterpret_cast<float4*>(tile + lr * 128 + 8 * sub);
-            d[0] = make_float4(v[0], v[1], v[2], v[3]);
-            d[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    if (COLS) {
+        const bool rows_real = tr * 4 + wr < p.kbt;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float v[8];
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                v[i] = x[i].get(e);
+                top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
+            }
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 8));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 16));
+            const uint32_t byte = rows_real && col0 + e < p.cols ? scale_byte(top) : 127u;
+            if (lane < 8) sfc[((lc + e) & 31) * 16 + ((lc + e) >> 5) * 4 + wr] = static_cast<uint8_t>(byte);
+            qc[(lc + e) * 17 + wr * 4 + (lane >> 3)] = codes8(v, inv_scale(byte));
         }
     }
     __syncthreads();
@@ -122,37 +154,19 @@ template <class T, bool ROWS, bool COLS> __global__ void __launch_bounds__(256) 
         p.sf[(static_cast<long long>(tr) * p.tiles_c + tc) * 128 + threadIdx.x] =
             reinterpret_cast<const uint32_t*>(sfr)[threadIdx.x];
     if (COLS) {
+        if (threadIdx.x >= 128)
+            p.sft[(static_cast<long long>(tc) * p.tiles_r + tr) * 128 + threadIdx.x - 128] =
+                reinterpret_cast<const uint32_t*>(sfc)[threadIdx.x - 128];
+        // four lanes a column, 16 bytes (one block) each
+        const int cols = min(128, p.cols - tc * 128), block = tr * 4 + (threadIdx.x & 3);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int lc = threadIdx.x & 127, blk = (threadIdx.x >> 7) + 2 * u;
-            const int cc = c0 + lc, block = (r0 >> 5) + blk;
-            float v[32];
-            uint32_t top = 0;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-                v[e] = tile[(blk * 32 + e) * 128 + lc];
-                top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-            }
-            const bool real = cc < p.cols && block < p.kbt;
-            const uint32_t byte = real ? scale_byte(top) : 127u;
-            sfc[(lc & 31) * 16 + (lc >> 5) * 4 + blk] = static_cast<uint8_t>(byte);
-            if (real) {
-                const float f = inv_scale(byte);
-                uint32_t w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float x[8] = {v[8 * k],     v[8 * k + 1], v[8 * k + 2], v[8 * k + 3],
-                                        v[8 * k + 4], v[8 * k + 5], v[8 * k + 6], v[8 * k + 7]};
-                    w[k] = codes8(x, f);
-                }
-                *reinterpret_cast<uint4*>(p.qt + (static_cast<long long>(cc) * p.kbt + block) * 16) =
+            const int c = u * 64 + (threadIdx.x >> 2);
+            const uint32_t* w = qc + c * 17 + (threadIdx.x & 3) * 4;
+            if (c < cols && block < p.kbt)
+                *reinterpret_cast<uint4*>(p.qt + (static_cast<long long>(tc * 128 + c) * p.kbt + block) * 16) =
                     make_uint4(w[0], w[1], w[2], w[3]);
-            }
         }
-        __syncthreads();
-        if (threadIdx.x < 128)
-            p.sft[(static_cast<long long>(tc) * p.tiles_r + tr) * 128 + threadIdx.x] =
-                reinterpret_cast<const uint32_t*>(sfc)[threadIdx.x];
     }
 }
 
@@ -164,60 +178,80 @@ __device__ __forceinline__ float scale_value(uint32_t byte) {
     return byte == 0u ? 0x1p-127f : __uint_as_float(byte << 23);
 }
 
-__device__ __forceinline__ float code_value(uint32_t c) {
-    const uint32_t m = c & 7u;
-    // magnitudes as fp32 bits: 0, 0.5, then exponent and one mantissa bit
-    const float a = m < 2u ? 0.5f * static_cast<float>(m) : __uint_as_float(((m >> 1) + 126u) << 23 | (m & 1u) << 22);
-    return c & 8u ? -a : a;
+// Eight codes as fp32, by the hardware's conversion of two of them to fp16 (exact).
+__device__ __forceinline__ void values8(uint32_t w, float f, float (&v)[8]) {
+    uint32_t h[4];
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+        : "r"(w));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
+        v[2 * i] = a.x * f;
+        v[2 * i + 1] = a.y * f;
+    }
 }
+
+// A CTA takes 32 rows x 512 columns: a thread 8 columns of eight rows, whose loads
+// are issued together.
+constexpr int VALUE_ROWS = 8;
 
 template <class T>
 __global__ void __launch_bounds__(256) k_fp4_values(const uint8_t* q, const uint8_t* sf, int rows, int cols, int kb,
-                                                    int tiles_c, T* out, long long ldo, int vec) {
-    const long long per_row = 4LL * kb;
-    const long long i = blockIdx.x * 256LL + threadIdx.x;
-    if (i >= per_row * rows) return;
-    const int row = static_cast<int>(i / per_row), s = static_cast<int>(i % per_row);
-    const int block = s >> 2, col = 8 * s;
-    const uint32_t w = *reinterpret_cast<const uint32_t*>(q + (static_cast<long long>(row) * kb + block) * 16 + (s & 3) * 4);
-    const float f = scale_value(
-        sf[(static_cast<long long>(row >> 7) * tiles_c + (block >> 2)) * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4 + (block & 3)]);
-    float v[8];
+                                                    int tiles_c, T* out, long long ldo, int vec, int parts) {
+    const int part = blockIdx.x % parts, group = blockIdx.x / parts;
+    const int s = part * 64 + (threadIdx.x & 63), block = s >> 2, col = 8 * s;
+    const int row0 = group * (4 * VALUE_ROWS) + (threadIdx.x >> 6);
+    if (block >= kb) return;
+    uint32_t w[VALUE_ROWS], sb[VALUE_ROWS];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = code_value((w >> (4 * e)) & 15u) * f;
-    T* o = out + row * ldo + col;
-    if (vec && col + 8 <= cols) {
-        if (sizeof(T) == 4) {
-            reinterpret_cast<float4*>(o)[0] = make_float4(v[0], v[1], v[2], v[3]);
-            reinterpret_cast<float4*>(o)[1] = make_float4(v[4], v[5], v[6], v[7]);
-        } else {
-            uint32_t h[4];
+    for (int i = 0; i < VALUE_ROWS; ++i) {
+        const int row = row0 + 4 * i;
+        w[i] = sb[i] = 0;
+        if (row >= rows) continue;
+        w[i] = *reinterpret_cast<const uint32_t*>(q + (static_cast<long long>(row) * kb + block) * 16 + (s & 3) * 4);
+        sb[i] = sf[(static_cast<long long>(row >> 7) * tiles_c + (block >> 2)) * 512 + (row & 31) * 16 +
+                   ((row & 127) >> 5) * 4 + (block & 3)];
+    }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-                h[k] = *reinterpret_cast<const uint32_t*>(&b);
+    for (int i = 0; i < VALUE_ROWS; ++i) {
+        const int row = row0 + 4 * i;
+        if (row >= rows) return;
+        float v[8];
+        values8(w[i], scale_value(sb[i]), v);
+        T* o = out + row * ldo + col;
+        if (vec && col + 8 <= cols) {
+            if (sizeof(T) == 4) {
+                __stcs(reinterpret_cast<float4*>(o), make_float4(v[0], v[1], v[2], v[3]));
+                __stcs(reinterpret_cast<float4*>(o) + 1, make_float4(v[4], v[5], v[6], v[7]));
+            } else {
+                uint32_t h[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
+                    h[k] = *reinterpret_cast<const uint32_t*>(&b);
+                }
+                __stcs(reinterpret_cast<uint4*>(o), make_uint4(h[0], h[1], h[2], h[3]));
             }
-            *reinterpret_cast<uint4*>(o) = make_uint4(h[0], h[1], h[2], h[3]);
-        }
-    } else {
+        } else {
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (col + e < cols) o[e] = static_cast<T>(v[e]);
+            for (int e = 0; e < 8; ++e)
+                if (col + e < cols) o[e] = static_cast<T>(v[e]);
+        }
     }
 }
 
 template <class T>
 cudaError_t quantize_as(const QuantParams& p, cudaStream_t s) {
     const unsigned int grid = static_cast<unsigned int>(p.tiles_r) * p.tiles_c;
-    constexpr int SMEM = 128 * 128 * 4;
-    if (p.qt == nullptr) {
-        k_fp4_quantize<T, true, false><<<grid, 256, 0, s>>>(p);
-        return cudaGetLastError();
-    }
-    auto fn = p.q != nullptr ? k_fp4_quantize<T, true, true> : k_fp4_quantize<T, false, true>;
-    const cudaError_t e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e != cudaSuccess) return e;
-    fn<<<grid, 256, SMEM, s>>>(p);
+    if (p.qt == nullptr) k_fp4_quantize<T, true, false><<<grid, 256, 0, s>>>(p);
+    else if (p.q == nullptr) k_fp4_quantize<T, false, true><<<grid, 256, 0, s>>>(p);
+    else k_fp4_quantize<T, true, true><<<grid, 256, 0, s>>>(p);
     return cudaGetLastError();
 }
 
@@ -246,18 +280,19 @@ cudaError_t launch_fp4_quantize(const void* X, int dtype, int rows, int cols, in
 cudaError_t launch_fp4_dequantize(const void* q, const void* sf, int rows, int cols, void* out, int dtype, int64_t ldo,
                                   cudaStream_t s, int64_t* launches) {
     const int kb = fp4_blocks(cols);
-    const long long grid = (4LL * kb * rows + 255) / 256;
+    const int parts = (4 * kb - 1) / 64 + 1;
+    const unsigned int grid = static_cast<unsigned int>(parts) * ((rows - 1) / (4 * VALUE_ROWS) + 1);
     const bool bf = dtype == MOARA_DTYPE_BF16;
     const int vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ldo % (bf ? 8 : 4) == 0;
     const uint8_t* qq = static_cast<const uint8_t*>(q);
     const uint8_t* ss = static_cast<const uint8_t*>(sf);
     ++*launches;
     if (bf)
-        k_fp4_values<__nv_bfloat16><<<static_cast<unsigned int>(grid), 256, 0, s>>>(
-            qq, ss, rows, cols, kb, fp4_tiles(cols), static_cast<__nv_bfloat16*>(out), ldo, vec);
+        k_fp4_values<__nv_bfloat16><<<grid, 256, 0, s>>>(qq, ss, rows, cols, kb, fp4_tiles(cols),
+                                                         static_cast<__nv_bfloat16*>(out), ldo, vec, parts);
     else
-        k_fp4_values<float><<<static_cast<unsigned int>(grid), 256, 0, s>>>(qq, ss, rows, cols, kb, fp4_tiles(cols),
-                                                                            static_cast<float*>(out), ldo, vec);
+        k_fp4_values<float><<<grid, 256, 0, s>>>(qq, ss, rows, cols, kb, fp4_tiles(cols), static_cast<float*>(out), ldo,
+                                                 vec, parts);
     return cudaGetLastError();
 }
 
