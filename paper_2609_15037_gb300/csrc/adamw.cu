@@ -51,9 +51,18 @@ __device__ __forceinline__ void decode_sq(uint32_t w, float scale, float* v) {
     }
 }
 
-// Codes of 8 entries in two words.  WIDE: inv alone scales, 2^-112 or 2^-96 comes in a
-// second product (a block whose largest entry is above 2^14 or 2^30: the joint factor
-// would be subnormal).
+// The upper bytes of eight words.
+__device__ __forceinline__ void upper_bytes(const uint32_t (&u)[8], uint32_t (&w)[2]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = __byte_perm(__byte_perm(u[4 * i], u[4 * i + 1], 0x0073), __byte_perm(u[4 * i + 2], u[4 * i + 3], 0x0073), 0x5410);
+}
+
+// Codes of 8 entries in two words.  y is at most two units above 1.875, whose code has
+// 20 zero bits below it, so no random number carries it beyond the largest code.
+// WIDE (a block whose largest entry is above 2^14 or 2^30): 2^-112 or 2^-96 comes in a
+// second product, because the joint factor would be subnormal; such a factor is
+// inexact, so that the code is limited too.
 template <bool WIDE>
 __device__ __forceinline__ void encode_avg(const float (&x)[8], float inv, const uint32_t (&r)[8], uint32_t (&w)[2]) {
     const float f = WIDE ? inv : inv * 0x1p-112f;
@@ -61,37 +70,44 @@ __device__ __forceinline__ void encode_avg(const float (&x)[8], float inv, const
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float y = __fmul_rn(fabsf(x[e]), f), z = WIDE ? __fmul_rn(y, 0x1p-112f) : y;
-        const uint32_t t = min(__float_as_uint(z) + ((r[e] & 0xFFFFu) << 4), 0x07FFFFFFu);
-        u[e] = ((t << 4) & 0x7F000000u) | (__float_as_uint(x[e]) & 0x80000000u);     // the code in the upper byte
+        uint32_t t = __float_as_uint(z) + (r[e] & 0xFFFFu) * 16u;
+        if (WIDE) t = min(t, 0x07FFFFFFu);
+        u[e] = (t << 4) | (__float_as_uint(x[e]) & 0x80000000u);      // the code in the upper byte
     }
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-        w[i] = __byte_perm(__byte_perm(u[4 * i], u[4 * i + 1], 0x0073), __byte_perm(u[4 * i + 2], u[4 * i + 3], 0x0073), 0x5410);
+    upper_bytes(u, w);
 }
 
 template <bool WIDE>
 __device__ __forceinline__ void encode_sq(const float (&x)[8], float inv, const uint32_t (&r)[8], uint32_t (&w)[2]) {
+    constexpr uint32_t ONE = 1u << 20;                                // the smallest code
     const float f = WIDE ? inv : inv * 0x1p-96f;
-    uint32_t u[8];
+    uint32_t u[8], low = ONE;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float y = __fmul_rn(x[e], f), z = WIDE ? __fmul_rn(y, 0x1p-96f) : y;
-        const uint32_t t = min(__float_as_uint(z) + ((r[e] >> 12) & 0xFFFF0u), 0x0FFFFFFFu);
-        u[e] = max(t, x[e] > 0.0f ? 1u << 20 : 0u) << 4;
+        u[e] = __float_as_uint(z) + ((r[e] >> 12) & 0xFFFF0u);
+        if (WIDE) u[e] = min(u[e], 0x0FFFFFFFu);
+        low = min(low, u[e]);
+    }
+    if (low < ONE) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (x[e] > 0.0f) u[e] = max(u[e], ONE);
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-        w[i] = __byte_perm(__byte_perm(u[4 * i], u[4 * i + 1], 0x0073), __byte_perm(u[4 * i + 2], u[4 * i + 3], 0x0073), 0x5410);
+    for (int e = 0; e < 8; ++e) u[e] <<= 4;
+    upper_bytes(u, w);
 }
 
 // 32-bit xor-shift-multiply mixing
-__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) {
-    x ^= x >> 16;
+__host__ __device__ __forceinline__ uint32_t mix32_rest(uint32_t x) {
     x *= 0x85EBCA6Bu;
     x ^= x >> 13;
     x *= 0xC2B2AE35u;
     return x ^ (x >> 16);
 }
+
+__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x) { return mix32_rest(x ^ (x >> 16)); }
 
 // four consecutive entries at i; those at or behind n read as zero
 template <bool FULL> __device__ __forceinline__ void load4(const float* p, long long i, long long n, float (&v)[4]) {
@@ -125,30 +141,39 @@ template <bool FULL> __device__ __forceinline__ uint32_t load4(const uint8_t* p,
     return w;
 }
 
-// eight consecutive entries, or codes, at i
-template <bool FULL> __device__ __forceinline__ void load8(const float* p, long long i, long long n, float (&v)[8]) {
-    float a[4], b[4];
-    load4<FULL>(p, i, n, a);
-    load4<FULL>(p, i + 4, n, b);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = a[e], v[4 + e] = b[e];
-}
+// eight consecutive entries at i as they lie in memory, and eight codes
+template <class T, bool FULL> struct Raw8;
 
-template <bool FULL>
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, long long i, long long n, float (&v)[8]) {
-    if (FULL) {
-        const uint4 w = __ldcs(reinterpret_cast<const uint4*>(p + i));
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+template <bool FULL> struct Raw8<float, FULL> {
+    float w[8];
+    __device__ __forceinline__ void load(const float* p, long long i, long long n) {
+        float a[4], b[4];
+        load4<FULL>(p, i, n, a);
+        load4<FULL>(p, i + 4, n, b);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[2 * e] = __uint_as_float(x[e] << 16);
-            v[2 * e + 1] = __uint_as_float(x[e] & 0xFFFF0000u);
-        }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = i + e < n ? __bfloat162float(p[i + e]) : 0.0f;
+        for (int e = 0; e < 4; ++e) w[e] = a[e], w[4 + e] = b[e];
     }
-}
+    __device__ __forceinline__ float get(int e) const { return w[e]; }
+};
+
+template <bool FULL> struct Raw8<__nv_bfloat16, FULL> {
+    uint32_t w[4];
+    __device__ __forceinline__ void load(const __nv_bfloat16* p, long long i, long long n) {
+        if (FULL) {
+            const uint4 a = __ldcs(reinterpret_cast<const uint4*>(p + i));
+            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
+        } else {
+            const uint16_t* h = reinterpret_cast<const uint16_t*>(p + i);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                w[e] = (i + 2 * e < n ? h[2 * e] : 0u) |
+                       (i + 2 * e + 1 < n ? static_cast<uint32_t>(h[2 * e + 1]) << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ float get(int e) const {
+        return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+    }
+};
 
 template <bool FULL> __device__ __forceinline__ uint2 load8(const uint8_t* p, long long i, long long n) {
     if (FULL) return __ldcs(reinterpret_cast<const uint2*>(p + i));
@@ -233,13 +258,19 @@ __device__ __forceinline__ float rcp_flush(float x) {
     return y;
 }
 
-// The largest magnitude of a warp's 256 values, compared as bits so that a NaN is
-// the largest.
+// The largest magnitude of a warp's 256 values; a NaN is the largest (over the lanes
+// as bits).
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
 __device__ __forceinline__ float warp_top(const float (&a)[8]) {
-    uint32_t top = 0;
+    float top = fabsf(a[0]);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(a[e]) & 0x7FFFFFFFu);
-    return __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+    for (int e = 1; e < 8; ++e) top = max_nan(top, fabsf(a[e]));
+    return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
 }
 
 __device__ __forceinline__ void new_moments(const AdamBatch& b, float g, float& m, float& v) {
@@ -287,17 +318,34 @@ __device__ __forceinline__ void adam_tile(const AdamTensor& t, const AdamBatch& 
 }
 
 // 8-bit moments.  One warp, one block of 256 entries: lane l has i0 + 8l .. +7, so
-// that its codes are 8 and its bf16 entries 16 bytes.
+// that its codes are 8 and its bf16 entries 16 bytes.  What a block reads is loaded
+// while the block in front of it is computed.
+template <class PT, class GT, bool FULL> struct Block8 {
+    Raw8<PT, FULL> p;
+    Raw8<GT, FULL> g;
+    uint2 mc, vc;
+    float ms, vs;
+    __device__ __forceinline__ void load(const AdamTensor& t, long long i0, int lane) {
+        const long long at = i0 + 8 * lane;
+        g.load(static_cast<const GT*>(t.g), at, t.n);
+        p.load(static_cast<const PT*>(t.p), at, t.n);
+        mc = load8<FULL>(static_cast<const uint8_t*>(t.m), at, t.n);
+        vc = load8<FULL>(static_cast<const uint8_t*>(t.v), at, t.n);
+        ms = t.ms[i0 >> 8];
+        vs = t.vs[i0 >> 8];
+    }
+};
+
 template <class PT, class GT, bool FULL>
-__device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, int lane) {
+__device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamBatch& b, const Block8<PT, GT, FULL>& in,
+                                           float coef, long long i0, int lane) {
     const long long n = t.n, at = i0 + 8 * lane;
     PT* const pp = static_cast<PT*>(t.p);
     float p[8], g[8], m[8], v[8];
-    const uint2 mc = load8<FULL>(static_cast<const uint8_t*>(t.m), at, n);
-    const uint2 vc = load8<FULL>(static_cast<const uint8_t*>(t.v), at, n);
-    load8<FULL>(static_cast<const GT*>(t.g), at, n, g);
-    load8<FULL>(pp, at, n, p);
-    const float ms = t.ms[i0 >> 8], vs = t.vs[i0 >> 8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = in.p.get(e), g[e] = in.g.get(e);
+    const uint2 mc = in.mc, vc = in.vc;
+    const float ms = in.ms, vs = in.vs;
     decode_avg(mc.x, ms, m);
     decode_avg(mc.y, ms, m + 4);
     decode_sq(vc.x, vs, v);
@@ -321,9 +369,12 @@ __device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamBatch&
     const bool mf = !(mt < 0x1p-100f), vf = !(vt < 0x1p-100f);
     const float mi = mf ? __fdiv_rn(kCodeTop, mt) : 0.0f, vi = vf ? __fdiv_rn(kCodeTop, vt) : 0.0f;
     const uint32_t key = mix32(t.key ^ static_cast<uint32_t>(static_cast<unsigned long long>(i0) >> 32));
+    // mix32(entry ^ key): the entries differ in their lowest three bits only, which
+    // the first xor-shift does not move
     uint32_t r[8], w[2];
+    const uint32_t x = static_cast<uint32_t>(at) ^ key, y = x ^ (x >> 16);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = mix32((static_cast<uint32_t>(at) + e) ^ key);
+    for (int e = 0; e < 8; ++e) r[e] = mix32_rest(y ^ e);
     if (mt > 0x1p14f) encode_avg<true>(m, mi, r, w);
     else encode_avg<false>(m, mi, r, w);
     store8<FULL>(static_cast<uint8_t*>(t.m), at, n, w);
@@ -336,15 +387,34 @@ __device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamBatch&
     }
 }
 
+// A warp's blocks below `end`, `stride` entries apart; returns the first one behind.
+template <class PT, class GT, bool FULL>
+__device__ __forceinline__ long long adam_blocks8(const AdamTensor& t, const AdamBatch& b, float coef, long long i0,
+                                                  long long stride, long long end) {
+    const int lane = threadIdx.x & 31;
+    if (i0 >= end) return i0;
+    Block8<PT, GT, FULL> in;
+    in.load(t, i0, lane);
+    while (true) {
+        const long long next = i0 + stride;
+        const bool more = next < end;
+        Block8<PT, GT, FULL> ahead;
+        if (more) ahead.load(t, next, lane);
+        adam_tile8<PT, GT, FULL>(t, b, in, coef, i0, lane);
+        i0 = next;
+        if (!more) return i0;
+        in = ahead;
+    }
+}
+
 template <class PT, class GT, bool B8>
-__device__ __forceinline__ void adam_any(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, int lane) {
-    const bool full = (t.kind & kAdamVector) && i0 + MOARA_ADAMW_BLOCK <= t.n;
+__device__ __forceinline__ void adam_any(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, long long stride) {
     if (B8) {
-        if (full) adam_tile8<PT, GT, true>(t, b, coef, i0, lane);
-        else adam_tile8<PT, GT, false>(t, b, coef, i0, lane);
+        if (t.kind & kAdamVector) i0 = adam_blocks8<PT, GT, true>(t, b, coef, i0, stride, t.n - MOARA_ADAMW_BLOCK + 1);
+        adam_blocks8<PT, GT, false>(t, b, coef, i0, stride, t.n);
     } else {
-        if (full) adam_tile<PT, GT, true>(t, b, coef, i0, lane);
-        else adam_tile<PT, GT, false>(t, b, coef, i0, lane);
+        if ((t.kind & kAdamVector) && i0 + MOARA_ADAMW_BLOCK <= t.n) adam_tile<PT, GT, true>(t, b, coef, i0, threadIdx.x & 31);
+        else adam_tile<PT, GT, false>(t, b, coef, i0, threadIdx.x & 31);
     }
 }
 
@@ -358,23 +428,23 @@ template <class F> __device__ __forceinline__ int find_tensor(int count, uint32_
     return lo;
 }
 
-__global__ void __launch_bounds__(256) k_adamw(const __grid_constant__ AdamBatch b) {
+__global__ void __launch_bounds__(256, 4) k_adamw(const __grid_constant__ AdamBatch b) {
     const uint32_t c = blockIdx.x;
     const int q = find_tensor(b.count, c, [&](int i) { return b.start[i]; });
     const AdamTensor& t = b.t[q];
-    const int lane = threadIdx.x & 31;
     const long long i0 = static_cast<long long>(c - b.start[q]) * kAdamChunk + (threadIdx.x >> 5) * MOARA_ADAMW_BLOCK;
+    const long long stride = static_cast<long long>(b.start[q + 1] - b.start[q]) * kAdamChunk;
     if (i0 >= t.n) return;
     const float coef = b.scale != nullptr ? *b.scale : 1.0f;
     switch (t.kind & 7u) {
-        case 0: adam_any<float, float, false>(t, b, coef, i0, lane); break;
-        case 1: adam_any<__nv_bfloat16, float, false>(t, b, coef, i0, lane); break;
-        case 2: adam_any<float, __nv_bfloat16, false>(t, b, coef, i0, lane); break;
-        case 3: adam_any<__nv_bfloat16, __nv_bfloat16, false>(t, b, coef, i0, lane); break;
-        case 4: adam_any<float, float, true>(t, b, coef, i0, lane); break;
-        case 5: adam_any<__nv_bfloat16, float, true>(t, b, coef, i0, lane); break;
-        case 6: adam_any<float, __nv_bfloat16, true>(t, b, coef, i0, lane); break;
-        default: adam_any<__nv_bfloat16, __nv_bfloat16, true>(t, b, coef, i0, lane); break;
+        case 0: adam_any<float, float, false>(t, b, coef, i0, stride); break;
+        case 1: adam_any<__nv_bfloat16, float, false>(t, b, coef, i0, stride); break;
+        case 2: adam_any<float, __nv_bfloat16, false>(t, b, coef, i0, stride); break;
+        case 3: adam_any<__nv_bfloat16, __nv_bfloat16, false>(t, b, coef, i0, stride); break;
+        case 4: adam_any<float, float, true>(t, b, coef, i0, stride); break;
+        case 5: adam_any<__nv_bfloat16, float, true>(t, b, coef, i0, stride); break;
+        case 6: adam_any<float, __nv_bfloat16, true>(t, b, coef, i0, stride); break;
+        default: adam_any<__nv_bfloat16, __nv_bfloat16, true>(t, b, coef, i0, stride); break;
     }
 }
 

@@ -51,7 +51,20 @@ __device__ __forceinline__ uint32_t codes8(const float (&v)[8], float f) {
     return w;
 }
 
-// Eight entries of a row as they lie in memory, and entry e of them in fp32.
+// Eight entries of a row as they lie in memory, their fp32 values, and the largest
+// magnitude of several, with a NaN above all (bf16: of two columns at a time).
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t max_nan2(uint32_t a, uint32_t b) {
+    uint32_t y;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+    return y;
+}
+
 template <class T> struct Row8;
 
 template <> struct Row8<float> {
@@ -66,6 +79,23 @@ template <> struct Row8<float> {
         for (int e = 0; e < 8; ++e) w[e] = e < count ? __float_as_uint(p[e]) : 0u;
     }
     __device__ __forceinline__ float get(int e) const { return __uint_as_float(w[e]); }
+    // bits of the largest magnitude of the row's eight entries
+    __device__ __forceinline__ uint32_t top() const {
+        float t = fabsf(get(0));
+#pragma unroll
+        for (int e = 1; e < 8; ++e) t = max_nan(t, fabsf(get(e)));
+        return __float_as_uint(t);
+    }
+    // and of each column of eight rows
+    static __device__ __forceinline__ void tops(const Row8 (&x)[8], uint32_t (&t)[8]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float y = fabsf(x[0].get(e));
+#pragma unroll
+            for (int i = 1; i < 8; ++i) y = max_nan(y, fabsf(x[i].get(e)));
+            t[e] = __float_as_uint(y);
+        }
+    }
 };
 
 template <> struct Row8<__nv_bfloat16> {
@@ -83,6 +113,21 @@ template <> struct Row8<__nv_bfloat16> {
     __device__ __forceinline__ float get(int e) const {
         return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
     }
+    static __device__ __forceinline__ uint32_t size(uint32_t x) { return x & 0x7FFF7FFFu; }
+    __device__ __forceinline__ uint32_t top() const {
+        const uint32_t t = max_nan2(max_nan2(size(w[0]), size(w[1])), max_nan2(size(w[2]), size(w[3])));
+        return max(t << 16, t & 0xFFFF0000u);
+    }
+    static __device__ __forceinline__ void tops(const Row8 (&x)[8], uint32_t (&t)[8]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            uint32_t y = size(x[0].w[e]);
+#pragma unroll
+            for (int i = 1; i < 8; ++i) y = max_nan2(y, size(x[i].w[e]));
+            t[2 * e] = y << 16;
+            t[2 * e + 1] = y & 0xFFFF0000u;
+        }
+    }
 };
 
 // One CTA takes a 128 x 128 tile, which is one 512-byte scale tile of either
@@ -92,7 +137,8 @@ template <> struct Row8<__nv_bfloat16> {
 // word of one lane.  The matrix passes through no shared memory (32 x 1 blocks of a
 // 64 KB tile there took 67 us where this takes 42 on 11008 x 4096 fp32); only the
 // columns' codes do, to leave in whole 64-byte lines.
-template <class T, bool ROWS, bool COLS> __global__ void __launch_bounds__(256, 2) k_fp4_quantize(const QuantParams p) {
+template <class T, bool ROWS, bool COLS>
+__global__ void __launch_bounds__(256, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2) k_fp4_quantize(const QuantParams p) {
     __shared__ __align__(16) uint8_t sfr[512];
     __shared__ __align__(16) uint8_t sfc[512];
     __shared__ __align__(16) uint32_t qc[COLS ? 128 * 17 : 1];       // a column's 16 words of codes, and one of padding
@@ -115,12 +161,9 @@ template <class T, bool ROWS, bool COLS> __global__ void __launch_bounds__(256, 
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             float v[8];
-            uint32_t top = 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                v[e] = x[i].get(e);
-                top = max(top, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-            }
+            for (int e = 0; e < 8; ++e) v[e] = x[i].get(e);
+            uint32_t top = x[i].top();
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
             const bool real = row0 + i < p.rows && block < p.kb;
@@ -133,15 +176,14 @@ template <class T, bool ROWS, bool COLS> __global__ void __launch_bounds__(256, 
     }
     if (COLS) {
         const bool rows_real = tr * 4 + wr < p.kbt;
+        uint32_t tops[8];
+        Row8<T>::tops(x, tops);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             float v[8];
-            uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                v[i] = x[i].get(e);
-                top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-            }
+            for (int i = 0; i < 8; ++i) v[i] = x[i].get(e);
+            uint32_t top = tops[e];
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 8));
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 16));
             const uint32_t byte = rows_real && col0 + e < p.cols ? scale_byte(top) : 127u;

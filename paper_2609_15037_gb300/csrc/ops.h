@@ -12,7 +12,12 @@ namespace moara {
 
 // ------------------------------------------------------------------- AdamW
 constexpr int kAdamTensors = 360;      // per launch: the parameter block holds at most 32764 bytes
-constexpr int kAdamChunk = 2048;       // entries of one CTA
+constexpr int kAdamChunk = 2048;       // entries that one CTA takes at a time
+// Chunk of 8-bit moments in a call with many entries: a CTA's search for its tensor and
+// its addresses are spread over eight blocks per warp.  Below kAdamMany entries the
+// GPU is not full with so many entries a CTA.
+constexpr int kAdamLong = 8 * kAdamChunk;
+constexpr long long kAdamMany = 152LL * 8 * kAdamLong;
 
 struct AdamTensor {
     long long n;
@@ -33,7 +38,7 @@ constexpr uint32_t kAdamParamBf16 = 1, kAdamGradBf16 = 2, kAdamBlock8 = 4, kAdam
 struct AdamBatch {
     AdamTensor t[kAdamTensors];
     uint32_t start[kAdamTensors + 1];  // first chunk of each tensor
-    int count;
+    int count, chunk8;
     float b1, b2, c1, c2;              // betas, 1 - betas
     float rbc2;                        // 1 / sqrt(1 - beta2^t)
     float eps;

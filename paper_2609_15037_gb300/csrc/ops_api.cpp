@@ -137,6 +137,9 @@ int moara_adamw_step(moara_ctx* ctx, int count, const moara_adamw_tensor* tensor
     b.rbc2 = static_cast<float>(1.0 / std::sqrt(bc2));
     b.eps = hp->eps;
     b.scale = grad_scale;
+    long long entries = 0;
+    for (int i = 0; i < count; ++i) entries += tensors[i].n < moara::kAdamMany ? tensors[i].n : moara::kAdamMany;
+    b.chunk8 = entries < moara::kAdamMany ? moara::kAdamChunk : moara::kAdamLong;
     long long chunks = 0;
     b.count = 0;
     auto flush = [&]() -> cudaError_t {
@@ -150,7 +153,7 @@ int moara_adamw_step(moara_ctx* ctx, int count, const moara_adamw_tensor* tensor
     for (int i = 0; i < count; ++i) {
         const moara_adamw_tensor& d = tensors[i];
         if (d.n == 0) continue;
-        const long long c = chunks_of(d.n, moara::kAdamChunk);
+        const long long c = chunks_of(d.n, d.state_dtype == MOARA_DTYPE_BLOCK8 ? b.chunk8 : moara::kAdamChunk);
         if (b.count == moara::kAdamTensors || chunks + c > INT_MAX) {
             const cudaError_t e = flush();
             if (e != cudaSuccess) return cuda_fail(ctx, e, "AdamW launch");
