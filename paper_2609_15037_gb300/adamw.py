@@ -14,11 +14,22 @@ from . import binding as B
 _TYPES = {torch.float32: B.MOARA_DTYPE_F32, torch.bfloat16: B.MOARA_DTYPE_BF16}
 _STATES = {"f32": B.MOARA_DTYPE_F32, "block8": B.MOARA_DTYPE_BLOCK8}
 _DESC = np.dtype(B.moara_adamw_tensor)
+_FLOATS = set(_TYPES)
+_data_ptr, _numel, _is_contiguous, _get_device = (
+    getattr(torch.Tensor, f) for f in ("data_ptr", "numel", "is_contiguous", "get_device"))
+
+
+def _current_stream(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+# the same without building a Stream object (1 us of a call's 5 to 10)
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
 
 
 def stream_handle(stream, device):
     """A cudaStream_t: `stream`, or torch's current stream on `device` for None."""
-    return torch.cuda.current_stream(device).cuda_stream if stream is None else int(stream)
+    return _current_stream(device) if stream is None else int(stream)
 
 
 def allocating_on(stream, device):
@@ -38,9 +49,10 @@ class AdamWGroup:
         self.hp = B.moara_adamw_hparams(beta1, beta2, eps, seed)
         self.ctx = None
         self.ctx = B.moara_create(B.moara_default_hparams(), device)
+        self._dev = torch.device("cuda", device)
         self.params, self.copies, self.states = [], [], []
         self._desc = np.zeros(0, _DESC)
-        self._types = []
+        self._sizes = []
         self._workspace = {}
 
     def _check(self, x, what, n=None, dtypes=tuple(_TYPES)):
@@ -62,7 +74,7 @@ class AdamWGroup:
         n = self._check(param, "param").numel()
         if copy is not None:
             self._check(copy, "copy", n, (torch.bfloat16,))
-        dev = torch.device("cuda", self.device)
+        dev = self._dev
         code = torch.uint8 if state == "block8" else torch.float32
         blocks = -(-n // B.MOARA_ADAMW_BLOCK)
 
@@ -85,11 +97,24 @@ class AdamWGroup:
         d["weight_decay"], d["lr_scale"] = weight_decay, lr_scale
         self.params.append(param)
         self.copies.append(copy)
+        self._sizes.append(n)
         self.states.append(s)
         return i
 
     def _chosen(self, ids):
         return self._desc[:len(self.params)] if ids is None else self._desc[list(ids)]
+
+    def _read(self, grads):
+        """Addresses, sizes and types (a number, or a list) of gradients.  Calls of many short
+        tensors are bound by this, so each property is one pass over the list."""
+        sizes = list(map(_numel, grads))
+        types = [g.dtype for g in grads]
+        kinds = set(types)
+        if not kinds <= _FLOATS or not all(map(_is_contiguous, grads)) or set(map(_get_device, grads)) - {self.device}:
+            for g in grads:
+                self._check(g, "grad")
+        kinds = _TYPES[kinds.pop()] if len(kinds) == 1 else [_TYPES[t] for t in types]
+        return list(map(_data_ptr, grads)), sizes, kinds
 
     def step(self, grads, t, lr, grad_scale=None, ids=None, stream=None):
         """One AdamW step at step t (1-based): grads[i] (fp32 or bf16) of every
@@ -98,12 +123,12 @@ class AdamWGroup:
         d = self._chosen(ids)
         if len(grads) != len(d):
             raise ValueError(f"{len(grads)} gradients for {len(d)} tensors")
-        sizes = d["n"].tolist()
-        for g, n in zip(grads, sizes):
-            if g.dtype not in _TYPES or g.numel() != n or not g.is_contiguous() or g.get_device() != self.device:
+        ptrs, sizes, types = self._read(grads)
+        if sizes != (self._sizes if ids is None else d["n"].tolist()):
+            for g, n in zip(grads, d["n"].tolist()):
                 self._check(g, "grad", n)
-        d["grad"] = [g.data_ptr() for g in grads]
-        d["grad_dtype"] = [_TYPES[g.dtype] for g in grads]
+        d["grad"] = ptrs
+        d["grad_dtype"] = types
         scale = 0 if grad_scale is None else self._check(grad_scale, "grad_scale", 1, (torch.float32,)).data_ptr()
         B.moara_adamw_step(self.ctx, len(d), d.ctypes.data, self.hp, t, lr, scale, stream_handle(stream, self.device))
 
@@ -113,14 +138,17 @@ class AdamWGroup:
         d = self._chosen(ids)
         sizes = d["n"].tolist()
         with allocating_on(stream, self.device):
-            outs = [[torch.empty(n, device=f"cuda:{self.device}") for n in sizes] if x is None else x
+            outs = [[torch.empty(n, device=self._dev) for n in sizes] if x is None else x
                     for x in (exp_avg, exp_avg_sq)]
+        ptrs = []
         for out in outs:
             if len(out) != len(d):
                 raise ValueError(f"{len(out)} outputs for {len(d)} tensors")
-            for x, n in zip(out, sizes):
-                self._check(x, "output", n, (torch.float32,))
-        ptrs = [np.array([x.data_ptr() for x in out], dtype=np.uint64) for out in outs]
+            at, have, types = self._read(out)
+            if have != sizes or types != B.MOARA_DTYPE_F32 and len(out):
+                for x, n in zip(out, sizes):
+                    self._check(x, "output", n, (torch.float32,))
+            ptrs.append(np.array(at, dtype=np.uint64))
         B.moara_adamw_moments(self.ctx, len(d), d.ctypes.data, ptrs[0].ctypes.data, ptrs[1].ctypes.data,
                               stream_handle(stream, self.device))
         return outs[0], outs[1]
@@ -130,7 +158,7 @@ class AdamWGroup:
         ws = self._workspace.get(handle)
         if ws is None or ws.numel() < need:
             with allocating_on(stream, self.device):
-                ws = torch.zeros(need, dtype=torch.uint8, device=f"cuda:{self.device}")
+                ws = torch.zeros(need, dtype=torch.uint8, device=self._dev)
                 # memory of a recorded graph is the graph's own
                 if not torch.cuda.is_current_stream_capturing():
                     self._workspace[handle] = ws
@@ -141,21 +169,22 @@ class AdamWGroup:
         bf16), a float32 tensor of three.  extra_sq: a one-element float32 device
         tensor added to the sum under the root, or None.  The first element is
         what MoaraGroup.set_clip_extra takes, the last what step takes."""
-        for g in grads:
-            if g.dtype not in _TYPES or not g.is_contiguous() or g.get_device() != self.device:
-                self._check(g, "grad")
+        ptrs, sizes, types = self._read(grads)
         n = len(grads)
-        table = np.array([[g.data_ptr() for g in grads], [g.numel() for g in grads]], dtype=np.int64)
-        types = np.array([_TYPES[g.dtype] for g in grads], dtype=np.int32)
+        table = np.array((ptrs, sizes), dtype=np.int64)
+        kinds = np.empty(n, dtype=np.int32)
+        kinds[:] = types
         handle = stream_handle(stream, self.device)
         ws = self._norm_workspace(n, handle, stream)
         extra = 0 if extra_sq is None else self._check(extra_sq, "extra_sq", 1, (torch.float32,)).data_ptr()
         if out is None:
             with allocating_on(stream, self.device):
-                out = torch.empty(3, device=f"cuda:{self.device}")
-        self._check(out, "out", 3, (torch.float32,))
-        B.moara_grad_norm(self.ctx, n, table.ctypes.data, table.ctypes.data + 8 * n, types.ctypes.data, max_norm,
-                          extra, out.data_ptr(), ws.data_ptr(), ws.numel(), handle)
+                out = torch.empty(3, device=self._dev)
+        else:
+            self._check(out, "out", 3, (torch.float32,))
+        at = table.ctypes.data
+        B.moara_grad_norm(self.ctx, n, at, at + 8 * n, kinds.ctypes.data, max_norm, extra, out.data_ptr(),
+                          ws.data_ptr(), ws.numel(), handle)
         return out
 
     def state_dict(self):

@@ -15,16 +15,29 @@ class Fp4Matrix:
 
     def __init__(self, rows, cols, q=None, sf=None, device=0):
         self.rows, self.cols = rows, cols
-        sizes = B.moara_fp4_bytes(rows, cols)
+        self._sizes = sizes = B.moara_fp4_bytes(rows, cols)
+        self._gap = -sizes[0] % 256
+        self._both = None
+        if q is None and sf is None:
+            # one allocation: the codes, and the scales from the next 256 bytes on
+            self._both = torch.empty(sizes[0] + self._gap + sizes[1], dtype=torch.uint8,
+                                     device=torch.device("cuda", device))
+            at = self._both.data_ptr()
+            self._ptrs = at, at + sizes[0] + self._gap
+            return
+        for x, size in zip((q, sf), sizes):
+            if x is None or x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size:
+                raise ValueError(f"q and sf, contiguous uint8 tensors of {sizes} bytes, or neither are needed")
+        self._q, self._sf = q, sf
+        self._ptrs = q.data_ptr(), sf.data_ptr()
 
-        def kept(x, size):
-            if x is None:
-                return torch.empty(size, dtype=torch.uint8, device=f"cuda:{device}")
-            if x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size:
-                raise ValueError(f"a contiguous uint8 tensor of {size} bytes is needed")
-            return x
-        self.q, self.sf = kept(q, sizes[0]), kept(sf, sizes[1])
-        self._ptrs = self.q.data_ptr(), self.sf.data_ptr()
+    @property
+    def q(self):
+        return self._q if self._both is None else self._both[:self._sizes[0]]
+
+    @property
+    def sf(self):
+        return self._sf if self._both is None else self._both[self._sizes[0] + self._gap:]
 
 
 class Fp4Group:
@@ -45,6 +58,7 @@ class Fp4Group:
         self.device = device
         self.ctx = None
         self.ctx = B.moara_create(B.moara_default_hparams(), device)
+        self._dev = torch.device("cuda", device)
 
     def _strided(self, x, what):
         """(address, type, row pitch) of a matrix whose rows are contiguous."""
@@ -59,14 +73,18 @@ class Fp4Group:
         if out is None:
             if dtype not in _TYPES:
                 raise ValueError("dtype must be float32 or bfloat16")
+            if stream is None:
+                return torch.empty((rows, cols), dtype=dtype, device=self._dev)
             with allocating_on(stream, self.device):
-                return torch.empty(rows, cols, dtype=dtype, device=f"cuda:{self.device}")
+                return torch.empty((rows, cols), dtype=dtype, device=self._dev)
         if tuple(out.shape) != (rows, cols):
             raise ValueError(f"out: shape {(rows, cols)} is needed")
         return out
 
     def _matrix(self, m, rows, cols, stream):
         if m is None:
+            if stream is None:
+                return Fp4Matrix(rows, cols, device=self.device)
             with allocating_on(stream, self.device):
                 return Fp4Matrix(rows, cols, device=self.device)
         if (m.rows, m.cols) != (rows, cols):
@@ -123,8 +141,10 @@ class Fp4Group:
     def _workspace(self, size, stream):
         if size == 0:
             return None, 0
+        if stream is None:
+            return torch.empty(size, dtype=torch.uint8, device=self._dev), size
         with allocating_on(stream, self.device):
-            return torch.empty(size, dtype=torch.uint8, device=f"cuda:{self.device}"), size
+            return torch.empty(size, dtype=torch.uint8, device=self._dev), size
 
     def status(self, stream=None):
         """Reads and clears the device status word (0, or an error a kernel recorded)."""
