@@ -4,6 +4,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "fp4.cuh"
 #include "ops.h"
 
 namespace moara {
@@ -22,114 +23,6 @@ struct QuantParams {
     uint32_t* sft;
 };
 
-// Scale byte of a block from its largest magnitude's bits: the exponent field of
-// top / 1.5 rounded up to a power of two, two binades lower (6 = 1.5 * 2^2).
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
-    if (top >= 0x7F800000u) return 255u;
-    const int e = static_cast<int>((top + 0x3FFFFFu) >> 23) - 2;
-    return static_cast<uint32_t>(max(e, 0));
-}
-
-// 2^(127 - byte), the factor into the block's grid (0 for a NaN scale)
-__device__ __forceinline__ float inv_scale(uint32_t byte) {
-    return byte == 255u ? 0.0f : __uint_as_float((254u - byte) << 23);
-}
-
-// Eight codes, entry 0 in the low half of byte 0; products with a power of two are
-// exact, so the conversion is the only rounding (to nearest, ties to even).
-__device__ __forceinline__ uint32_t codes8(const float (&v)[8], float f) {
-    uint32_t w;
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
-        "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
-        : "=r"(w)
-        : "f"(v[0] * f), "f"(v[1] * f), "f"(v[2] * f), "f"(v[3] * f), "f"(v[4] * f), "f"(v[5] * f), "f"(v[6] * f),
-          "f"(v[7] * f));
-    return w;
-}
-
-// Eight entries of a row as they lie in memory, their fp32 values, and the largest
-// magnitude of several, with a NaN above all (bf16: of two columns at a time).
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float y;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
-    return y;
-}
-
-__device__ __forceinline__ uint32_t max_nan2(uint32_t a, uint32_t b) {
-    uint32_t y;
-    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
-    return y;
-}
-
-template <class T> struct Row8;
-
-template <> struct Row8<float> {
-    uint32_t w[8];
-    __device__ __forceinline__ void load(const float* p) {
-        const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
-    }
-    __device__ __forceinline__ void load_some(const float* p, int count) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = e < count ? __float_as_uint(p[e]) : 0u;
-    }
-    __device__ __forceinline__ float get(int e) const { return __uint_as_float(w[e]); }
-    // bits of the largest magnitude of the row's eight entries
-    __device__ __forceinline__ uint32_t top() const {
-        float t = fabsf(get(0));
-#pragma unroll
-        for (int e = 1; e < 8; ++e) t = max_nan(t, fabsf(get(e)));
-        return __float_as_uint(t);
-    }
-    // and of each column of eight rows
-    static __device__ __forceinline__ void tops(const Row8 (&x)[8], uint32_t (&t)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float y = fabsf(x[0].get(e));
-#pragma unroll
-            for (int i = 1; i < 8; ++i) y = max_nan(y, fabsf(x[i].get(e)));
-            t[e] = __float_as_uint(y);
-        }
-    }
-};
-
-template <> struct Row8<__nv_bfloat16> {
-    uint32_t w[4];
-    __device__ __forceinline__ void load(const __nv_bfloat16* p) {
-        const uint4 a = *reinterpret_cast<const uint4*>(p);
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-    }
-    __device__ __forceinline__ void load_some(const __nv_bfloat16* p, int count) {
-        const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            w[e] = (2 * e < count ? h[2 * e] : 0u) | (2 * e + 1 < count ? static_cast<uint32_t>(h[2 * e + 1]) << 16 : 0u);
-    }
-    __device__ __forceinline__ float get(int e) const {
-        return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
-    }
-    static __device__ __forceinline__ uint32_t size(uint32_t x) { return x & 0x7FFF7FFFu; }
-    __device__ __forceinline__ uint32_t top() const {
-        const uint32_t t = max_nan2(max_nan2(size(w[0]), size(w[1])), max_nan2(size(w[2]), size(w[3])));
-        return max(t << 16, t & 0xFFFF0000u);
-    }
-    static __device__ __forceinline__ void tops(const Row8 (&x)[8], uint32_t (&t)[8]) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            uint32_t y = size(x[0].w[e]);
-#pragma unroll
-            for (int i = 1; i < 8; ++i) y = max_nan2(y, size(x[i].w[e]));
-            t[2 * e] = y << 16;
-            t[2 * e + 1] = y & 0xFFFF0000u;
-        }
-    }
-};
-
 // One CTA takes a 128 x 128 tile, which is one 512-byte scale tile of either
 // orientation, and each warp 32 rows x 64 columns of it: a lane holds 8 rows x 8
 // columns in registers, so that a row's block of 32 columns is four lanes, a
@@ -142,6 +35,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2
     __shared__ __align__(16) uint8_t sfr[512];
     __shared__ __align__(16) uint8_t sfc[512];
     __shared__ __align__(16) uint32_t qc[COLS ? 128 * 17 : 1];       // a column's 16 words of codes, and one of padding
+    asm volatile("griddepcontrol.launch_dependents;");       // a product behind it may set itself up
     const int tr = blockIdx.x / p.tiles_c, tc = blockIdx.x % p.tiles_c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wr = warp >> 1, sub = (warp & 1) * 8 + (lane & 7);     // 32-row group, 8-column group of the tile
@@ -239,35 +133,46 @@ __device__ __forceinline__ void values8(uint32_t w, float f, float (&v)[8]) {
     }
 }
 
-// A CTA takes 32 rows x 512 columns: a thread 8 columns of eight rows, whose loads
-// are issued together.
+struct ValueParams {
+    const uint8_t* q;
+    const uint8_t* sf;
+    int rows, cols, kb, tiles_c;
+    int parts;             // CTAs along a row
+    void* out;
+    long long ldo;
+};
+
+__device__ __forceinline__ uint32_t scale_at(const ValueParams& p, int row, int block) {
+    return p.sf[(static_cast<long long>(row >> 7) * p.tiles_c + (block >> 2)) * 512 + (row & 31) * 16 +
+                ((row & 127) >> 5) * 4 + (block & 3)];
+}
+
+// Rows of `out` on 16-byte boundaries.  A CTA takes 32 rows x 512 columns: a thread 8
+// columns of eight rows, whose loads are issued together.
 constexpr int VALUE_ROWS = 8;
 
-template <class T>
-__global__ void __launch_bounds__(256) k_fp4_values(const uint8_t* q, const uint8_t* sf, int rows, int cols, int kb,
-                                                    int tiles_c, T* out, long long ldo, int vec, int parts) {
-    const int part = blockIdx.x % parts, group = blockIdx.x / parts;
+template <class T> __global__ void __launch_bounds__(256) k_fp4_values(const ValueParams p) {
+    const int part = blockIdx.x % p.parts, group = blockIdx.x / p.parts;
     const int s = part * 64 + (threadIdx.x & 63), block = s >> 2, col = 8 * s;
     const int row0 = group * (4 * VALUE_ROWS) + (threadIdx.x >> 6);
-    if (block >= kb) return;
+    if (block >= p.kb) return;
     uint32_t w[VALUE_ROWS], sb[VALUE_ROWS];
 #pragma unroll
     for (int i = 0; i < VALUE_ROWS; ++i) {
         const int row = row0 + 4 * i;
         w[i] = sb[i] = 0;
-        if (row >= rows) continue;
-        w[i] = *reinterpret_cast<const uint32_t*>(q + (static_cast<long long>(row) * kb + block) * 16 + (s & 3) * 4);
-        sb[i] = sf[(static_cast<long long>(row >> 7) * tiles_c + (block >> 2)) * 512 + (row & 31) * 16 +
-                   ((row & 127) >> 5) * 4 + (block & 3)];
+        if (row >= p.rows) continue;
+        w[i] = *reinterpret_cast<const uint32_t*>(p.q + (static_cast<long long>(row) * p.kb + block) * 16 + (s & 3) * 4);
+        sb[i] = scale_at(p, row, block);
     }
 #pragma unroll
     for (int i = 0; i < VALUE_ROWS; ++i) {
         const int row = row0 + 4 * i;
-        if (row >= rows) return;
+        if (row >= p.rows) return;
         float v[8];
         values8(w[i], scale_value(sb[i]), v);
-        T* o = out + row * ldo + col;
-        if (vec && col + 8 <= cols) {
+        T* o = static_cast<T*>(p.out) + row * p.ldo + col;
+        if (col + 8 <= p.cols) {
             if (sizeof(T) == 4) {
                 __stcs(reinterpret_cast<float4*>(o), make_float4(v[0], v[1], v[2], v[3]));
                 __stcs(reinterpret_cast<float4*>(o) + 1, make_float4(v[4], v[5], v[6], v[7]));
@@ -283,8 +188,65 @@ __global__ void __launch_bounds__(256) k_fp4_values(const uint8_t* q, const uint
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (col + e < cols) o[e] = static_cast<T>(v[e]);
+                if (col + e < p.cols) o[e] = static_cast<T>(v[e]);
         }
+    }
+}
+
+// Rows on any boundary.  A CTA takes 8 rows x 512 columns, a warp 64 of the columns, a lane
+// two of them, which in a row of bf16 that begins between two words are the second
+// of one byte of codes and the first of the next: one word is stored.  11007 x 4097
+// into bf16 took 127 us with the eight columns of a lane stored one by one.
+template <class T> __global__ void __launch_bounds__(256) k_fp4_values_any(const ValueParams p) {
+    const int part = blockIdx.x % p.parts, row0 = blockIdx.x / p.parts * VALUE_ROWS;
+    const int j = part * 256 + threadIdx.x;                              // byte of codes
+    if (2 * j >= p.cols) return;
+    float2 v[VALUE_ROWS];
+#pragma unroll
+    for (int i = 0; i < VALUE_ROWS; ++i) {
+        const int row = row0 + i;
+        v[i] = make_float2(0.0f, 0.0f);
+        if (row >= p.rows) continue;
+        const uint8_t* q = p.q + static_cast<long long>(row) * p.kb * 16 + j;
+        const T* o = static_cast<const T*>(p.out) + row * p.ldo;
+        const int odd = sizeof(T) == 2 ? static_cast<int>(reinterpret_cast<uintptr_t>(o) >> 1 & 1) : 0;
+        uint32_t w = q[0], s0 = scale_at(p, row, j >> 4), s1 = s0;
+        if (odd) {
+            const bool more = 2 * j + 2 < p.cols;
+            w = w >> 4 | (more ? static_cast<uint32_t>(q[1]) << 4 : 0u);
+            if (more && ((j + 1) & 15) == 0) s1 = scale_at(p, row, (j + 1) >> 4);
+        }
+        uint32_t h;
+        asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+            "mov.b32 {b0, b1, b2, b3}, %1;\n\t"
+            "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t}"
+            : "=r"(h)
+            : "r"(w));
+        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h));
+        v[i] = make_float2(a.x * scale_value(s0), a.y * scale_value(s1));
+    }
+#pragma unroll
+    for (int i = 0; i < VALUE_ROWS; ++i) {
+        const int row = row0 + i;
+        if (row >= p.rows) return;
+        T* o = static_cast<T*>(p.out) + row * p.ldo;
+        if (sizeof(T) == 4) {
+            o[2 * j] = static_cast<T>(v[i].x);
+            if (2 * j + 1 < p.cols) o[2 * j + 1] = static_cast<T>(v[i].y);
+            continue;
+        }
+        const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(o) >> 1 & 1), c = 2 * j + odd;
+        if (odd && j == 0) {
+            uint32_t h;
+            asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+                "mov.b32 {b0, b1, b2, b3}, %1;\n\t"
+                "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t}"
+                : "=r"(h)
+                : "r"(static_cast<uint32_t>(p.q[static_cast<long long>(row) * p.kb * 16])));
+            o[0] = static_cast<T>(__low2float(*reinterpret_cast<const __half2*>(&h)) * scale_value(scale_at(p, row, 0)));
+        }
+        if (c + 1 < p.cols) *reinterpret_cast<__nv_bfloat162*>(o + c) = __floats2bfloat162_rn(v[i].x, v[i].y);
+        else if (c < p.cols) o[c] = static_cast<T>(v[i].x);
     }
 }
 
@@ -321,20 +283,24 @@ cudaError_t launch_fp4_quantize(const void* X, int dtype, int rows, int cols, in
 
 cudaError_t launch_fp4_dequantize(const void* q, const void* sf, int rows, int cols, void* out, int dtype, int64_t ldo,
                                   cudaStream_t s, int64_t* launches) {
-    const int kb = fp4_blocks(cols);
-    const int parts = (4 * kb - 1) / 64 + 1;
-    const unsigned int grid = static_cast<unsigned int>(parts) * ((rows - 1) / (4 * VALUE_ROWS) + 1);
+    ValueParams p{};
+    p.q = static_cast<const uint8_t*>(q);
+    p.sf = static_cast<const uint8_t*>(sf);
+    p.rows = rows;
+    p.cols = cols;
+    p.kb = fp4_blocks(cols);
+    p.tiles_c = fp4_tiles(cols);
+    p.parts = (cols - 1) / 512 + 1;
+    p.out = out;
+    p.ldo = ldo;
     const bool bf = dtype == MOARA_DTYPE_BF16;
-    const int vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ldo % (bf ? 8 : 4) == 0;
-    const uint8_t* qq = static_cast<const uint8_t*>(q);
-    const uint8_t* ss = static_cast<const uint8_t*>(sf);
+    const bool vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ldo % (bf ? 8 : 4) == 0;
+    const int per = vec ? 4 * VALUE_ROWS : VALUE_ROWS;
+    const unsigned int grid = static_cast<unsigned int>(p.parts) * ((rows - 1) / per + 1);
+    auto fn = vec ? (bf ? k_fp4_values<__nv_bfloat16> : k_fp4_values<float>)
+                  : (bf ? k_fp4_values_any<__nv_bfloat16> : k_fp4_values_any<float>);
+    fn<<<grid, 256, 0, s>>>(p);
     ++*launches;
-    if (bf)
-        k_fp4_values<__nv_bfloat16><<<grid, 256, 0, s>>>(qq, ss, rows, cols, kb, fp4_tiles(cols),
-                                                         static_cast<__nv_bfloat16*>(out), ldo, vec, parts);
-    else
-        k_fp4_values<float><<<grid, 256, 0, s>>>(qq, ss, rows, cols, kb, fp4_tiles(cols), static_cast<float*>(out), ldo,
-                                                 vec, parts);
     return cudaGetLastError();
 }
 

@@ -4,6 +4,8 @@
 
 #include <algorithm>
 
+#include "fp4.cuh"
+#include "launch.cuh"
 #include "ops.h"
 #include "tc_ptx.cuh"
 
@@ -12,41 +14,10 @@ namespace {
 
 // A stage holds 256 entries of K of both operands (128 bytes a row, one row of the
 // 128-byte swizzle) and their scales, two 512-byte tiles per 128 rows.
-constexpr int BM = 128, BN = 256, BK = 256;
-constexpr int A_BYTES = BM * BK / 2, B_BYTES = BN * BK / 2;
-constexpr int SFA_BYTES = 1024, SFB_BYTES = 2048;
-constexpr int STAGE_BYTES = A_BYTES + B_BYTES + SFA_BYTES + SFB_BYTES;
-constexpr int STAGES = 4;
-constexpr int EPI_WARPS = 8;
-constexpr int THREADS = (2 + EPI_WARPS) * 32;
-constexpr int SMEM = 1024 + STAGES * STAGE_BYTES + 256;
-// tensor memory: the accumulator, then each stage's scales (A: 2 x 4 columns,
-// B: 2 x 8)
-constexpr int TMEM_SF = BN, TMEM_STAGE = 24;
-static_assert(TMEM_SF + STAGES * TMEM_STAGE <= 512, "tensor memory");
-static_assert(STAGE_BYTES % 1024 == 0 && SMEM <= 227 * 1024, "stages stay on the swizzle's 1024-byte lines");
+constexpr int BK = 256;
+constexpr int OPERAND = 128 * BK / 2;              // 16 KB: 128 rows of either operand
+constexpr int SF_BYTES = 1024;                     // the scales of 128 rows
 constexpr long long kWait = 1LL << 32;
-
-struct ProductParams {
-    CUtensorMap amap, bmap;
-    const uint8_t* asf;
-    const uint8_t* bsf;
-    void* D;
-    long long ldd;
-    int M, N, K;
-    int tiles_m, tiles_n;
-    int ct;                // scale tiles along K
-    int bf16;
-    int vec;               // rows of D are 16-byte aligned
-    int* status;
-};
-
-struct Ctl {
-    uint64_t full[STAGES], empty[STAGES];
-    uint64_t accf, acce, drain;
-    uint32_t tmem;
-    int abort;
-};
 
 __device__ __forceinline__ bool drained(uint32_t bar, uint32_t parity) {
     const long long t0 = clock64();
@@ -69,163 +40,287 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-__device__ __forceinline__ void store16(const ProductParams& p, int row, int col, const float (&v)[16]) {
-    const long long at = row * p.ldd + col;
-    if (p.vec && col + 16 <= p.N) {
-        if (p.bf16) {
-            uint4* o = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.D) + at);
-            o[0] = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
-            o[1] = make_uint4(pack2(v[8], v[9]), pack2(v[10], v[11]), pack2(v[12], v[13]), pack2(v[14], v[15]));
-        } else {
-            float4* o = reinterpret_cast<float4*>(static_cast<float*>(p.D) + at);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = make_float4(v[4 * e], v[4 * e + 1], v[4 * e + 2], v[4 * e + 3]);
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        if (col + e >= p.N) continue;
-        if (p.bf16) static_cast<__nv_bfloat16*>(p.D)[at + e] = __float2bfloat16_rn(v[e]);
-        else static_cast<float*>(p.D)[at + e] = v[e];
-    }
+// ---------------------------------------------------------------------------
+// Products with few tiles.  The weight's rows are the MMA's 128 rows, up to 128 rows
+// of A (tokens) its columns, so that a single token costs columns and not rows;
+// a cluster of up to eight CTAs shares K, and each adds the others' sums for its
+// share of the tokens through shared memory.  Bound by latency (launch, one trip
+// to memory, the sums) up to some hundred tokens, then by the operands' way from L2.
+// With QUANT, A comes as it is (at most 16 rows) and the four epilogue warps
+// quantise a stage's rows into shared memory, so that a token's product is one
+// launch; every CTA of a K range does that again, which pays while it is 256
+// entries per row and stage.
+// ---------------------------------------------------------------------------
+constexpr int F_THREADS = 6 * 32;                  // TMA, MMA, four epilogue warps
+constexpr int F_STAGES = 4;                        // at most
+constexpr int F_TMEM = 256, F_TMEM_SF = 128, F_TMEM_STAGE = 16;
+constexpr int F_QUANT = 16;                        // most rows that are quantised on the way
+static_assert(F_TMEM_SF + F_STAGES * F_TMEM_STAGE <= F_TMEM, "tensor memory");
+
+struct FewParams {
+    CUtensorMap wmap, xmap;
+    const uint8_t* wsf;
+    const uint8_t* xsf;
+    const void* X;         // QUANT
+    long long ldx;
+    int xvec;              // rows of X may be read 16 bytes at a time
+    void* D;
+    long long ldd;
+    int M, N, K;           // rows of A, rows of B, entries
+    int tiles_n;
+    int ct;                // scale tiles along K
+    int nt;                // tokens of a tile, a multiple of 16
+    int stages;
+    int split;             // CTAs of a cluster
+    int early;             // the launch in front wrote A only: B may be read before it has ended
+    int bf16;
+    int vec;               // four entries of a row of D may be written at once
+    int ctl;               // offset of the barriers in shared memory
+    int* status;
+};
+
+struct FewCtl {
+    uint64_t full[F_STAGES], empty[F_STAGES];
+    uint64_t accf, drain;
+    uint32_t tmem;
+    int abort;
+};
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+                 : "r"(a));
+    return v;
 }
 
-// Warp 0 loads, warp 1 issues copies of scales and MMAs, eight warps drain.
-__global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constant__ ProductParams p) {
+// Eight entries of row `row` from column `col` on, zero outside.
+template <class T>
+__device__ __forceinline__ void load_x(const FewParams& p, int row, int col, Row8<T>& x) {
+    const T* src = static_cast<const T*>(p.X) + row * p.ldx + col;
+    if (p.xvec && col + 8 <= p.K) x.load(src);
+    else x.load_some(src, p.K - col);
+}
+
+template <bool QUANT, class T>
+__global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ FewParams p) {
     extern __shared__ uint8_t raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-    Ctl* ctl = reinterpret_cast<Ctl*>(smem + STAGES * STAGE_BYTES);
+    FewCtl* ctl = reinterpret_cast<FewCtl*>(smem + p.ctl);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rank = blockIdx.x % p.split, tile = blockIdx.x / p.split;
+    const int n0 = tile % p.tiles_n * 128, m0 = tile / p.tiles_n * 128;
+    const int steps = (p.K + BK - 1) / BK;
+    const int k0 = static_cast<int>(static_cast<long long>(steps) * rank / p.split);
+    const int k1 = static_cast<int>(static_cast<long long>(steps) * (rank + 1) / p.split);
+    const int x_bytes = p.nt * (BK / 2), stage_bytes = OPERAND + x_bytes + 2 * SF_BYTES;
     volatile int* abort_flag = &ctl->abort;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < STAGES; ++s) {
-            ptx::mbar_init(ptx::smem_u32(&ctl->full[s]), 1);
+        for (int s = 0; s < p.stages; ++s) {
+            ptx::mbar_init(ptx::smem_u32(&ctl->full[s]), QUANT ? 5 : 1);
             ptx::mbar_init(ptx::smem_u32(&ctl->empty[s]), 1);
         }
         ptx::mbar_init(ptx::smem_u32(&ctl->accf), 1);
-        ptx::mbar_init(ptx::smem_u32(&ctl->acce), EPI_WARPS);
         ptx::mbar_init(ptx::smem_u32(&ctl->drain), 1);
         ctl->abort = 0;
         ptx::fence_barrier_init();
     }
     if (warp == 1) {
-        ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
+        ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), F_TMEM);
         ptx::tmem_relinquish();
     }
     ptx::tc_fence_before();
     __syncthreads();
     ptx::tc_fence_after();
     const uint32_t tmem = ctl->tmem;
-    const int tiles = p.tiles_m * p.tiles_n;
-    const int steps = (p.K + BK - 1) / BK;
 
     if (warp == 0) {
         if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0, issued = 0, last = 0;
-            bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-                int m0, n0;
-                grouped_tile<BM, BN, 16>(p, t, m0, n0);
-                const int nt = n0 + 128 < p.N ? 2 : 1;             // scale tiles along N
-                for (int k = 0; k < steps; ++k) {
-                    if (!ptx::mbar_wait(ptx::smem_u32(&ctl->empty[stage]), phase ^ 1, abort_flag, p.status,
-                                        MOARA_ERR_DEVICE_TIMEOUT, kWait)) {
-                        ok = false;
-                        break;
-                    }
-                    const uint32_t fb = ptx::smem_u32(&ctl->full[stage]);
-                    const uint32_t a = ptx::smem_u32(smem + stage * STAGE_BYTES);
-                    const uint32_t b = a + A_BYTES, sa = b + B_BYTES, sb = sa + SFA_BYTES;
-                    const int at = 2 * k;                           // first scale tile along K
-                    const uint32_t sfb = min(2, p.ct - at) * 512u;
-                    ptx::mbar_arrive_expect_tx(fb, A_BYTES + B_BYTES + sfb * (1 + nt));
-                    ptx::tma_load_2d(a, &p.amap, fb, k * (BK / 2), m0);
-                    ptx::tma_load_2d(b, &p.bmap, fb, k * (BK / 2), n0);
-                    ptx::bulk_load(sa, p.asf + (static_cast<long long>(m0 >> 7) * p.ct + at) * 512, sfb, fb);
-                    for (int j = 0; j < nt; ++j)
-                        ptx::bulk_load(sb + j * 1024, p.bsf + (static_cast<long long>((n0 >> 7) + j) * p.ct + at) * 512,
-                                       sfb, fb);
-                    issued |= 1u << stage;
-                    last = (last & ~(1u << stage)) | (phase << stage);
-                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
-                }
+            uint32_t issued = 0, last = 0;
+            // this CTA's copies of step k: the weight's, and the tokens'
+            auto load_w = [&](int k, int stage) {
+                const uint32_t fb = ptx::smem_u32(&ctl->full[stage]), w = ptx::smem_u32(smem + stage * stage_bytes);
+                const uint32_t sf = min(2, p.ct - 2 * k) * 512u;
+                ptx::mbar_arrive_expect_tx(fb, OPERAND + sf + (QUANT ? 0 : x_bytes + sf));
+                ptx::tma_load_2d(w, &p.wmap, fb, k * (BK / 2), n0);
+                ptx::bulk_load(w + OPERAND + x_bytes, p.wsf + (static_cast<long long>(n0 >> 7) * p.ct + 2 * k) * 512, sf, fb);
+            };
+            auto load_t = [&](int k, int stage) {
+                if (QUANT) return;
+                const uint32_t fb = ptx::smem_u32(&ctl->full[stage]), w = ptx::smem_u32(smem + stage * stage_bytes);
+                const uint32_t sf = min(2, p.ct - 2 * k) * 512u;
+                ptx::tma_load_2d(w + OPERAND, &p.xmap, fb, k * (BK / 2), m0);
+                ptx::bulk_load(w + OPERAND + x_bytes + SF_BYTES,
+                               p.xsf + (static_cast<long long>(m0 >> 7) * p.ct + 2 * k) * 512, sf, fb);
+            };
+            if (!p.early) asm volatile("griddepcontrol.wait;" ::: "memory");
+            const int ahead = min(p.stages, k1 - k0);
+            for (int i = 0; i < ahead; ++i) load_w(k0 + i, i);
+            if (p.early) asm volatile("griddepcontrol.wait;" ::: "memory");
+            for (int i = 0; i < ahead; ++i) {
+                load_t(k0 + i, i);
+                issued |= 1u << i;
             }
-            for (int s = 0; s < STAGES; ++s)
+            int stage = 0;
+            uint32_t phase = 0;
+            for (int k = k0 + ahead; k < k1; ++k) {
+                if (!ptx::mbar_wait(ptx::smem_u32(&ctl->empty[stage]), phase, abort_flag, p.status,
+                                    MOARA_ERR_DEVICE_TIMEOUT, kWait))
+                    break;
+                load_w(k, stage);
+                load_t(k, stage);
+                last = (last & ~(1u << stage)) | ((phase ^ 1) << stage);
+                if (++stage == p.stages) { stage = 0; phase ^= 1; }
+            }
+            for (int s = 0; s < p.stages; ++s)
                 if (issued & (1u << s)) drained(ptx::smem_u32(&ctl->full[s]), (last >> s) & 1);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0, acc = 0;
-            bool ok = true;
-            for (int t = blockIdx.x; t < tiles && ok; t += gridDim.x, acc ^= 1) {
-                int m0, n0;
-                grouped_tile<BM, BN, 16>(p, t, m0, n0);
-                const int nt = n0 + 128 < p.N ? 2 : 1;
-                ok = ptx::mbar_wait(ptx::smem_u32(&ctl->acce), acc ^ 1, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT,
-                                    kWait);
-                if (!ok) break;
-                ptx::tc_fence_after();
-                for (int k = 0; k < steps; ++k) {
-                    if (!ptx::mbar_wait(ptx::smem_u32(&ctl->full[stage]), phase, abort_flag, p.status,
-                                        MOARA_ERR_DEVICE_TIMEOUT, kWait)) {
-                        ok = false;
-                        break;
-                    }
-                    ptx::tc_fence_after();
-                    const uint32_t a = ptx::smem_u32(smem + stage * STAGE_BYTES);
-                    const uint32_t b = a + A_BYTES, sa = b + B_BYTES, sb = sa + SFA_BYTES;
-                    const uint32_t ta = tmem + TMEM_SF + stage * TMEM_STAGE, tb = ta + 8;
-                    const int mmas = min(4, (p.K - k * BK + 63) / 64);
-                    for (int h = 0; h < (mmas + 1) / 2; ++h) {
-                        ptx::tmem_cp_scales(ta + 4 * h, ptx::smem_desc_plain(sa + 512 * h, 128));
-                        for (int j = 0; j < nt; ++j)
-                            ptx::tmem_cp_scales(tb + 8 * h + 4 * j, ptx::smem_desc_plain(sb + 1024 * j + 512 * h, 128));
-                    }
-                    for (int i = 0; i < mmas; ++i)
-                        ptx::mma_mxf4(tmem, ptx::smem_desc_sw128(a + 32 * i, 16, 1024),
-                                      ptx::smem_desc_sw128(b + 32 * i, 16, 1024), ptx::idesc_mxf4(BM, 128 * nt, i & 1),
-                                      ta + 4 * (i >> 1), tb + 8 * (i >> 1), (k | i) != 0);
-                    ptx::mma_commit(ptx::smem_u32(&ctl->empty[stage]));
-                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
-                }
-                ptx::mma_commit(ptx::smem_u32(&ctl->accf));
-            }
-            ptx::mma_commit(ptx::smem_u32(&ctl->drain));
-            drained(ptx::smem_u32(&ctl->drain), 0);
-        }
-    } else {
-        // lane quadrant warp % 4, column half (warp - 2) / 4
-        const int quad = warp & 3, half = (warp - 2) >> 2;
-        uint32_t acc = 0;
-        for (int t = blockIdx.x; t < tiles; t += gridDim.x, acc ^= 1) {
-            int m0, n0;
-            grouped_tile<BM, BN, 16>(p, t, m0, n0);
-            const bool got = ptx::mbar_wait(ptx::smem_u32(&ctl->accf), acc, abort_flag, p.status,
-                                            MOARA_ERR_DEVICE_TIMEOUT, kWait);
-            if (!__all_sync(0xffffffffu, got)) break;
+        const bool leader = ptx::elect_one();
+        const uint32_t base = ptx::smem_u32(smem);
+        int stage = 0;
+        uint32_t phase = 0;
+        for (int k = k0; k < k1; ++k) {
+            if (!ptx::mbar_wait(ptx::smem_u32(&ctl->full[stage]), phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT,
+                                kWait))
+                break;
             ptx::tc_fence_after();
-            const int row = m0 + quad * 32 + lane;
-            for (int c = 0; c < 8; ++c) {
-                const int col = n0 + half * 128 + c * 16;
-                if (col >= p.N) break;                              // warp-uniform
+            if (leader) {
+                const uint32_t w = base + stage * stage_bytes, sw = w + OPERAND + x_bytes;
+                const uint32_t tw = tmem + F_TMEM_SF + stage * F_TMEM_STAGE, tx = tw + 8;
+                const uint64_t dsw = ptx::smem_desc_plain(sw, 128), dsx = ptx::smem_desc_plain(sw + SF_BYTES, 128);
+                const uint64_t dw = ptx::smem_desc_sw128(w, 16, 1024), dx = ptx::smem_desc_sw128(w + OPERAND, 16, 1024);
+                const int mmas = min(4, (p.K - k * BK + 63) / 64);
+                const uint32_t idesc = ptx::idesc_mxf4(128, 0, 0) | static_cast<uint32_t>(p.nt >> 3) << 17;
+                const uint32_t half = ptx::idesc_mxf4(0, 0, 1) ^ ptx::idesc_mxf4(0, 0, 0);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (2 * h >= mmas) break;
+                    ptx::tmem_cp_scales(tw + 4 * h, dsw + 32 * h);
+                    ptx::tmem_cp_scales(tx + 4 * h, dsx + 32 * h);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < mmas)
+                        ptx::mma_mxf4(tmem, dw + 2 * i, dx + 2 * i, i & 1 ? idesc | half : idesc, tw + 4 * (i >> 1),
+                                      tx + 4 * (i >> 1), (k - k0) | i);
+                ptx::mma_commit(ptx::smem_u32(&ctl->empty[stage]));
+            }
+            __syncwarp();
+            if (++stage == p.stages) { stage = 0; phase ^= 1; }
+        }
+        if (leader) {
+            ptx::mma_commit(ptx::smem_u32(&ctl->accf));
+            ptx::mma_commit(ptx::smem_u32(&ctl->drain));
+        }
+        __syncwarp();
+        drained(ptx::smem_u32(&ctl->drain), 0);
+    } else {
+        const int quad = warp & 3;
+        if (QUANT) {
+            // a warp takes every fourth row: lane l has columns 8l .. +7 of the stage,
+            // four lanes a block
+            constexpr int PER = F_QUANT / 4;
+            Row8<T> x[PER];
+            auto fetch = [&](int k) {
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int row = quad + 4 * i;
+                    if (row < p.M) load_x<T>(p, row, k * BK + 8 * lane, x[i]);
+                }
+            };
+            fetch(k0);
+            int stage = 0;
+            uint32_t phase = 0;
+            for (int k = k0; k < k1; ++k) {
+                const bool got = ptx::mbar_wait(ptx::smem_u32(&ctl->empty[stage]), phase ^ 1, abort_flag, p.status,
+                                                MOARA_ERR_DEVICE_TIMEOUT, kWait);
+                if (!__all_sync(0xffffffffu, got)) break;
+                uint8_t* rows = smem + stage * stage_bytes + OPERAND;
+                uint8_t* sf = rows + x_bytes + SF_BYTES;
+#pragma unroll
+                for (int i = 0; i < PER; ++i) {
+                    const int row = quad + 4 * i;
+                    if (row >= p.M) break;                          // warp-uniform
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = x[i].get(e);
+                    uint32_t top = x[i].top();
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                    const uint32_t byte = scale_byte(top);
+                    // the 128-byte swizzle: 16-byte chunk ^ row % 8
+                    *reinterpret_cast<uint32_t*>(rows + row * 128 + (((lane >> 2) ^ (row & 7)) << 4) + (lane & 3) * 4) =
+                        codes8(v, inv_scale(byte));
+                    if ((lane & 3) == 0) sf[(lane >> 4) * 512 + row * 16 + ((lane >> 2) & 3)] = static_cast<uint8_t>(byte);
+                }
+                if (k + 1 < k1) fetch(k + 1);
+                ptx::fence_proxy_async_smem();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->full[stage]));
+                if (++stage == p.stages) { stage = 0; phase ^= 1; }
+            }
+        }
+        const bool got = ptx::mbar_wait(ptx::smem_u32(&ctl->accf), 0, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT,
+                                        kWait);
+        if (__all_sync(0xffffffffu, got)) {
+            // sums [token][128 rows of the weight] over the stages, which are all consumed
+            ptx::tc_fence_after();
+            float* part = reinterpret_cast<float*>(smem) + quad * 32 + lane;
+            const int tokens = min(p.nt, p.M - m0);
+            for (int c = 0; c < tokens; c += 16) {
                 float v[16];
                 __syncwarp();
-                ptx::tmem_ld16(tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * 128 + c * 16, v);
-                if (row < p.M) store16(p, row, col, v);
+                ptx::tmem_ld16(tmem + (static_cast<uint32_t>(quad * 32) << 16) + c, v);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (c + e < tokens) part[(c + e) * 128] = v[e];
             }
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->acce));
         }
     }
     ptx::tc_fence_before();
-    __syncthreads();
+    __syncwarp();
+    ptx::cluster_sync();                                            // every CTA's sums are in its shared memory
+    {
+        const int tokens = min(p.nt, p.M - m0), share = (tokens + p.split - 1) / p.split;
+        const int t1 = min(tokens, (rank + 1) * share), col = n0 + 4 * lane;
+        const uint32_t own = ptx::smem_u32(smem) + 16 * lane;
+        uint32_t from[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) from[r] = ptx::mapa(own, r < p.split ? r : 0);
+        for (int t = rank * share + warp; t < t1; t += F_THREADS / 32) {
+            float4 part[8];                                         // requested together
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < p.split) part[r] = ld_cluster_f4(from[r] + t * 512);
+            float4 sum = part[0];
+#pragma unroll
+            for (int r = 1; r < 8; ++r) {
+                if (r >= p.split) break;
+                sum.x += part[r].x; sum.y += part[r].y; sum.z += part[r].z; sum.w += part[r].w;
+            }
+            const long long at = (m0 + t) * p.ldd + col;
+            const float v[4] = {sum.x, sum.y, sum.z, sum.w};
+            if (p.vec && col + 4 <= p.N) {
+                if (p.bf16)
+                    *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p.D) + at) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+                else
+                    *reinterpret_cast<float4*>(static_cast<float*>(p.D) + at) = sum;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (col + e >= p.N) continue;
+                    if (p.bf16) static_cast<__nv_bfloat16*>(p.D)[at + e] = __float2bfloat16_rn(v[e]);
+                    else static_cast<float*>(p.D)[at + e] = v[e];
+                }
+            }
+        }
+    }
+    __syncwarp();
+    ptx::cluster_sync();                                            // no CTA leaves while another reads its sums
     if (warp == 1) {
         ptx::tc_fence_after();
-        ptx::tmem_dealloc(tmem, 512);
+        ptx::tmem_dealloc(tmem, F_TMEM);
     }
 }
 
@@ -235,15 +330,20 @@ __global__ void __launch_bounds__(THREADS, 1) k_fp4_product(const __grid_constan
 // the even CTA issues.  The accumulator is not doubled (256 columns, beside which
 // the scales of every stage live): eight warps take it whole into registers,
 // which costs some hundred cycles between two tiles, and store it beside the next
-// tile's MMAs.
+// tile's MMAs, through 2 KB of shared memory each: rows of 64 bytes whatever their
+// alignment.
 // ---------------------------------------------------------------------------
 constexpr int P_BM = 256, P_BN = 256;
-constexpr int P_OPERAND = 128 * BK / 2;                            // 16 KB: 128 rows of A or B
-constexpr int P_STAGE = 2 * P_OPERAND + SFA_BYTES + SFB_BYTES;
+constexpr int EPI_WARPS = 8;
+constexpr int P_THREADS = (2 + EPI_WARPS) * 32;
+// tensor memory: the accumulator, then each stage's scales (A: 2 x 4 columns, B: 2 x 8)
+constexpr int P_TMEM_STAGE = 24;
+constexpr int P_STAGE = 2 * OPERAND + 3 * SF_BYTES;
 constexpr int P_STAGES = 6;
-constexpr int P_SMEM = 1024 + P_STAGES * P_STAGE + 256;
+constexpr int P_OUT = 32 * 64;                                     // a warp's staging of D: 32 rows of 64 bytes
+constexpr int P_SMEM = P_STAGES * P_STAGE + EPI_WARPS * P_OUT + 256;
 static_assert(P_STAGE % 1024 == 0 && P_SMEM <= 227 * 1024, "stages stay on the swizzle's 1024-byte lines");
-static_assert(P_BN + P_STAGES * TMEM_STAGE <= 512, "tensor memory");
+static_assert(P_BN + P_STAGES * P_TMEM_STAGE <= 512, "tensor memory");
 
 struct PairParams {
     CUtensorMap amap, bmap, samap, sbmap;
@@ -252,7 +352,7 @@ struct PairParams {
     int M, N, K;
     int tiles_m, tiles_n;
     int bf16;
-    int vec;               // bytes to which rows of D are aligned: 32, 16 or 0
+    int unit;              // bytes to which rows of D are aligned, at most 16
     int* status;
 };
 
@@ -263,50 +363,75 @@ struct PairCtl {
     int abort;
 };
 
-// 128 columns of one row of D.
-__device__ __forceinline__ void store128(const PairParams& p, int row, int col, const uint32_t (&v)[128]) {
-    const long long at = row * p.ldd + col;
-    if (p.bf16) {
-        __nv_bfloat16* d = static_cast<__nv_bfloat16*>(p.D) + at;
+// 64 bytes of 32 rows from a warp's staging to D, UNIT bytes of a lane at a time, so that
+// a store covers whole sectors whatever the rows' alignment.  left: bytes of the rows
+// that exist.  ODD: rows of bf16 that begin between two words were staged from their
+// second entry on.
+template <class U, int ES, bool ODD>
+__device__ __forceinline__ void store_rows(const uint8_t* stage, uint8_t* d, long long pitch, int rows, int left, int lane) {
+    constexpr int UNIT = sizeof(U), PER = 64 / UNIT, AT = 32 / PER;              // lanes a row, rows at a time
+    const int b = lane % PER * UNIT;
+    const uint8_t* from = stage + (b & 15);
+#pragma unroll 8
+    for (int i = 0; i < 32; i += AT) {
+        const int r = i + lane / PER;
+        if (r >= rows) continue;
+        const uint8_t* x = from + r * 64 + (((b >> 4) ^ ((r >> 1) & 3)) << 4);
+        uint8_t* to = d + r * pitch + b;
+        const int skip = ODD ? static_cast<int>(reinterpret_cast<uintptr_t>(to) & 2) : 0;
+        to += skip;
+        if (b + UNIT + skip <= left) {
+            *reinterpret_cast<U*>(to) = *reinterpret_cast<const U*>(x);
+        } else if (UNIT > ES) {
 #pragma unroll
-        for (int c = 0; c < 128; c += 16) {
-            uint32_t w[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w[e] = pack2(__uint_as_float(v[c + 2 * e]), __uint_as_float(v[c + 2 * e + 1]));
-            if (p.vec == 32 && col + c + 16 <= p.N) {
-                ptx::st_global_256(d + c, w);
-            } else if (p.vec == 16 && col + c + 16 <= p.N) {
-                reinterpret_cast<uint4*>(d + c)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                reinterpret_cast<uint4*>(d + c)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (col + c + e < p.N) d[c + e] = __float2bfloat16_rn(__uint_as_float(v[c + e]));
-            }
-        }
-    } else {
-        float* d = static_cast<float*>(p.D) + at;
-#pragma unroll
-        for (int c = 0; c < 128; c += 8) {
-            const uint32_t w[8] = {v[c], v[c + 1], v[c + 2], v[c + 3], v[c + 4], v[c + 5], v[c + 6], v[c + 7]};
-            if (p.vec == 32 && col + c + 8 <= p.N) {
-                ptx::st_global_256(d + c, w);
-            } else if (p.vec == 16 && col + c + 8 <= p.N) {
-                reinterpret_cast<uint4*>(d + c)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                reinterpret_cast<uint4*>(d + c)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (col + c + e < p.N) d[c + e] = __uint_as_float(w[e]);
+            for (int e = 0; e < UNIT; e += ES) {
+                if (b + skip + e >= left) continue;
+                if (ES == 2) *reinterpret_cast<uint16_t*>(to + e) = *reinterpret_cast<const uint16_t*>(x + e);
+                else *reinterpret_cast<uint32_t*>(to + e) = *reinterpret_cast<const uint32_t*>(x + e);
             }
         }
     }
 }
 
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_fp4_pair(const __grid_constant__ PairParams p) {
-    extern __shared__ uint8_t raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
-    PairCtl* ctl = reinterpret_cast<PairCtl*>(smem + P_STAGES * P_STAGE);
+// 256 bytes (64 words of lane = row) of a warp's 32 rows of D from row, col on.
+template <int ES>
+__device__ __forceinline__ void store_words(const PairParams& p, uint8_t* stage, int row, int col, uint32_t (&w)[64], int lane) {
+    constexpr int COLS = 64 / ES;                                   // of a 64-byte chunk
+    const int rows = p.M - row;
+    const long long pitch = p.ldd * ES;
+    uint8_t* d = static_cast<uint8_t*>(p.D) + row * pitch + static_cast<long long>(col) * ES;
+    if (ES == 2 && p.unit == 2) {
+        uint8_t* first = d + lane * pitch;
+        if (reinterpret_cast<uintptr_t>(first) & 2) {
+            if (lane < rows && col < p.N) *reinterpret_cast<uint16_t*>(first) = static_cast<uint16_t>(w[0]);
+#pragma unroll
+            for (int e = 0; e < 64; ++e) w[e] = __funnelshift_r(w[e], e < 63 ? w[e + 1] : 0u, 16);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        if (col + c * COLS >= p.N || rows <= 0) break;              // warp-uniform
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int x = 16 * c + 4 * j;
+            *reinterpret_cast<uint4*>(stage + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[x], w[x + 1], w[x + 2], w[x + 3]);
+        }
+        __syncwarp();
+        // up to the end of the rows, or of these 256 bytes
+        const int left = (min(p.N - col, 4 * COLS) - c * COLS) * ES;
+        uint8_t* to = d + 64 * c;
+        if (p.unit == 16) store_rows<uint4, ES, false>(stage, to, pitch, rows, left, lane);
+        else if (p.unit == 8) store_rows<uint2, ES, false>(stage, to, pitch, rows, left, lane);
+        else if (p.unit == 4) store_rows<uint32_t, ES, false>(stage, to, pitch, rows, left, lane);
+        else if (ES == 2) store_rows<uint32_t, ES, true>(stage, to, pitch, rows, left, lane);
+    }
+}
+
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant__ PairParams p) {
+    extern __shared__ __align__(1024) uint8_t smem[];             // there is no room to align it here
+    uint8_t* staging = smem + P_STAGES * P_STAGE;
+    PairCtl* ctl = reinterpret_cast<PairCtl*>(staging + EPI_WARPS * P_OUT);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int crank = static_cast<int>(ptx::cluster_ctarank());
     volatile int* abort_flag = &ctl->abort;
@@ -351,7 +476,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_fp4_pa
                     const uint32_t own = ptx::smem_u32(&ctl->full[stage]), fb = ptx::mapa(own, 0);
                     if (crank == 0) ptx::mbar_arrive_expect_tx(own, 2 * P_STAGE);
                     const uint32_t a = ptx::smem_u32(smem + stage * P_STAGE);
-                    const uint32_t b = a + P_OPERAND, sa = b + P_OPERAND, sb = sa + SFA_BYTES;
+                    const uint32_t b = a + OPERAND, sa = b + OPERAND, sb = sa + SF_BYTES;
                     ptx::tma_load_2d_pair(a, &p.amap, fb, k * (BK / 2), m0 + 128 * crank);
                     ptx::tma_load_2d_pair(b, &p.bmap, fb, k * (BK / 2), n0 + 128 * crank);
                     ptx::tma_load_2d_pair(sa, &p.samap, fb, k * 256, (m0 >> 7) + crank);
@@ -376,8 +501,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_fp4_pa
                     return false;
                 ptx::tc_fence_after();
                 if (leader) {
-                    const uint32_t sa = base + stage * P_STAGE + 2 * P_OPERAND, sb = sa + SFA_BYTES;
-                    const uint32_t ta = tmem + P_BN + stage * TMEM_STAGE, tb = ta + 8;
+                    const uint32_t sa = base + stage * P_STAGE + 2 * OPERAND, sb = sa + SF_BYTES;
+                    const uint32_t ta = tmem + P_BN + stage * P_TMEM_STAGE, tb = ta + 8;
                     const uint64_t da = ptx::smem_desc_plain(sa, 128), db = ptx::smem_desc_plain(sb, 128);
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -405,9 +530,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_fp4_pa
                 const bool last = k + 1 == steps;
                 if (leader) {
                     const uint32_t a = base + stage * P_STAGE;
-                    const uint32_t ta = tmem + P_BN + stage * TMEM_STAGE, tb = ta + 8;
+                    const uint32_t ta = tmem + P_BN + stage * P_TMEM_STAGE, tb = ta + 8;
                     const uint64_t da = ptx::smem_desc_sw128(a, 16, 1024);
-                    const uint64_t db = ptx::smem_desc_sw128(a + P_OPERAND, 16, 1024);
+                    const uint64_t db = ptx::smem_desc_sw128(a + OPERAND, 16, 1024);
                     const int mmas = last ? tail : 4;
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
@@ -429,6 +554,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_fp4_pa
     } else {
         // lane quadrant warp % 4, column half (warp - 2) / 4
         const int quad = warp & 3, half = (warp - 2) >> 2;
+        uint8_t* out = staging + (warp - 2) * P_OUT;
         const uint32_t release = ptx::mapa(ptx::smem_u32(&ctl->acce), 0);
         uint32_t acc = 0;
         for (int t = first; t < tiles; t += stride, acc ^= 1) {
@@ -438,13 +564,29 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) k_fp4_pa
                                             MOARA_ERR_DEVICE_TIMEOUT, kWait);
             if (!__all_sync(0xffffffffu, got)) break;
             ptx::tc_fence_after();
-            uint32_t v[128];
-            ptx::tmem_ld128(tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * 128, v);
+            const uint32_t from = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * 128;
+            const int row = m0 + crank * 128 + quad * 32, col = n0 + half * 128;
+            uint32_t w[64];
+            if (p.bf16) {
+                // both halves are rounded into 64 words before anything is stored
+                uint32_t v[64];
+                ptx::tmem_ld64(from, v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) w[e] = pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+                ptx::tmem_ld64(from + 64, v);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) w[32 + e] = pack2(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1]));
+            } else {
+                ptx::tmem_ld64(from, w);
+                store_words<4>(p, out, row, col, w, lane);
+                __syncwarp();
+                ptx::tmem_ld64(from + 64, w);
+            }
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive_remote(release);
-            const int row = m0 + crank * 128 + quad * 32 + lane;
-            if (row < p.M) store128(p, row, n0 + half * 128, v);
+            if (p.bf16) store_words<2>(p, out, row, col, w, lane);
+            else store_words<4>(p, out, row, col + 64, w, lane);
         }
     }
     ptx::tc_fence_before();
@@ -509,45 +651,73 @@ cudaError_t launch_pair(const Fp4Product& a, int* status, cudaStream_t s) {
     p.tiles_n = (a.N - 1) / P_BN + 1;
     p.bf16 = a.dtype == MOARA_DTYPE_BF16;
     const uintptr_t d = reinterpret_cast<uintptr_t>(a.D), pitch = static_cast<uintptr_t>(a.ldd) * (p.bf16 ? 2 : 4);
-    p.vec = (d | pitch) % 32 == 0 ? 32 : (d | pitch) % 16 == 0 ? 16 : 0;
+    p.unit = static_cast<int>(((d | pitch | 16) & (~(d | pitch | 16) + 1)));
     p.status = status;
     const cudaError_t e = cudaFuncSetAttribute(k_fp4_pair, cudaFuncAttributeMaxDynamicSharedMemorySize, P_SMEM);
     if (e != cudaSuccess) return e;
     const long long tiles = static_cast<long long>(p.tiles_m) * p.tiles_n;
-    k_fp4_pair<<<2 * static_cast<unsigned int>(std::min<long long>(tiles, 76)), THREADS, P_SMEM, s>>>(p);
+    k_fp4_pair<<<2 * static_cast<unsigned int>(std::min<long long>(tiles, 76)), P_THREADS, P_SMEM, s>>>(p);
     return cudaGetLastError();
+}
+
+// X: A as it is (quantised on the way), or null.
+template <bool QUANT, class T>
+cudaError_t launch_few(const Fp4Product& a, bool early, int* status, cudaStream_t s) {
+    FewParams p{};
+    p.nt = std::min(128, (a.M + 15) / 16 * 16);
+    if (!encode(&p.wmap, a.bq, a.N, a.K, 128)) return cudaErrorInvalidValue;
+    if (!QUANT && !encode(&p.xmap, a.aq, a.M, a.K, p.nt)) return cudaErrorInvalidValue;
+    p.wsf = static_cast<const uint8_t*>(a.bsf);
+    p.xsf = static_cast<const uint8_t*>(a.asf);
+    p.X = a.X;
+    p.ldx = a.ldx;
+    p.xvec = (reinterpret_cast<uintptr_t>(a.X) & 15) == 0 && a.ldx * static_cast<int64_t>(sizeof(T)) % 16 == 0;
+    p.D = a.D;
+    p.ldd = a.ldd;
+    p.M = a.M;
+    p.N = a.N;
+    p.K = a.K;
+    p.tiles_n = (a.N - 1) / 128 + 1;
+    p.ct = fp4_tiles(a.K);
+    p.bf16 = a.dtype == MOARA_DTYPE_BF16;
+    const uintptr_t size = p.bf16 ? 2 : 4;
+    p.vec = (reinterpret_cast<uintptr_t>(a.D) | static_cast<uintptr_t>(a.ldd) * size) % (4 * size) == 0;
+    p.early = early;
+    p.status = status;
+    const int steps = (a.K - 1) / BK + 1;
+    const long long tiles = static_cast<long long>(p.tiles_n) * ((a.M - 1) / 128 + 1);
+    // K over more CTAs while they are at most 5/4 of the SMs: with N = K = 4096 a token
+    // takes 4.9 us in clusters of four (128 CTAs) and 7.2 in clusters of eight (256), with N
+    // = 11008 6.6 in clusters of two (172) and 7.9 without
+    p.split = 1;
+    while (p.split < 8 && 2 * p.split <= steps && tiles * 2 * p.split <= 190) p.split *= 2;
+    p.stages = std::min(p.nt > 64 ? F_STAGES - 1 : F_STAGES, (steps - 1) / p.split + 1);    // two CTAs fit an SM
+    const int stage = OPERAND + p.nt * (BK / 2) + 2 * SF_BYTES;
+    p.ctl = (std::max(p.stages * stage, p.nt * 512) + 15) / 16 * 16;
+    const int smem = 1024 + p.ctl + static_cast<int>(sizeof(FewCtl));
+    const cudaError_t e = cudaFuncSetAttribute(k_fp4_few<QUANT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    if (e != cudaSuccess) return e;
+    return launch_if(early, k_fp4_few<QUANT, T>, dim3(static_cast<unsigned int>(tiles * p.split)), dim3(F_THREADS), smem,
+                     s, p.split, p);
+}
+
+// Pairs where their tiles occupy half of the GPU, the other form below that.
+bool large(const Fp4Product& a) {
+    return static_cast<long long>((a.M - 1) / P_BM + 1) * ((a.N - 1) / P_BN + 1) >= 38 && a.M > 128;
 }
 
 }  // namespace
 
 size_t fp4_product_workspace(int, int, int) { return 0; }
 
-cudaError_t launch_fp4_product(const Fp4Product& a, int* status, cudaStream_t s, int64_t* launches) {
-    if (a.M > 128) {
-        ++*launches;
-        return launch_pair(a, status, s);
-    }
-    ProductParams p{};
-    if (!encode(&p.amap, a.aq, a.M, a.K, BM) || !encode(&p.bmap, a.bq, a.N, a.K, BN)) return cudaErrorInvalidValue;
-    p.asf = static_cast<const uint8_t*>(a.asf);
-    p.bsf = static_cast<const uint8_t*>(a.bsf);
-    p.D = a.D;
-    p.ldd = a.ldd;
-    p.M = a.M;
-    p.N = a.N;
-    p.K = a.K;
-    p.tiles_m = (a.M - 1) / BM + 1;
-    p.tiles_n = (a.N - 1) / BN + 1;
-    p.ct = fp4_tiles(a.K);
-    p.bf16 = a.dtype == MOARA_DTYPE_BF16;
-    p.vec = (reinterpret_cast<uintptr_t>(a.D) & 15) == 0 && a.ldd % (p.bf16 ? 8 : 4) == 0;
-    p.status = status;
-    const cudaError_t e = cudaFuncSetAttribute(k_fp4_product, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM);
-    if (e != cudaSuccess) return e;
-    const long long tiles = static_cast<long long>(p.tiles_m) * p.tiles_n;
-    k_fp4_product<<<static_cast<unsigned int>(std::min<long long>(tiles, 152)), THREADS, SMEM, s>>>(p);
+bool fp4_quantizes(int M, int N, int K) { return M <= F_QUANT; }
+
+cudaError_t launch_fp4_product(const Fp4Product& a, bool early, int* status, cudaStream_t s, int64_t* launches) {
     ++*launches;
-    return cudaGetLastError();
+    if (a.X != nullptr)
+        return a.x_dtype == MOARA_DTYPE_BF16 ? launch_few<true, __nv_bfloat16>(a, false, status, s)
+                                             : launch_few<true, float>(a, false, status, s);
+    return large(a) ? launch_pair(a, status, s) : launch_few<false, float>(a, early, status, s);
 }
 
 }  // namespace moara

@@ -102,8 +102,10 @@ int check_product(moara_ctx* ctx, int M, int N, int K, const void* bq, const voi
     return MOARA_OK;
 }
 
-size_t linear_operand_bytes(int M, int K) {
-    return align_up(moara::fp4_q_bytes(M, K), 256) + align_up(moara::fp4_sf_bytes(M, K), 256);
+size_t linear_workspace(int M, int N, int K) {
+    if (moara::fp4_quantizes(M, N, K)) return moara::fp4_product_workspace(M, N, K);
+    return align_up(moara::fp4_q_bytes(M, K), 256) + align_up(moara::fp4_sf_bytes(M, K), 256) +
+           moara::fp4_product_workspace(M, N, K);
 }
 
 }  // namespace
@@ -338,8 +340,8 @@ int moara_fp4_product(moara_ctx* ctx, int M, int N, int K, const void* a_q, cons
     if (rc == MOARA_OK) rc = check_operand(ctx, "A", a_q, a_sf);
     if (rc != MOARA_OK) return rc;
     DeviceGuard g(ctx->device);
-    const moara::Fp4Product p{M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, workspace};
-    const cudaError_t e = moara::launch_fp4_product(p, ctx->d_status, static_cast<cudaStream_t>(stream), &ctx->launches);
+    const moara::Fp4Product p{M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, nullptr, 0, 0};
+    const cudaError_t e = moara::launch_fp4_product(p, false, ctx->d_status, static_cast<cudaStream_t>(stream), &ctx->launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "product launch");
     return MOARA_OK;
 }
@@ -347,7 +349,7 @@ int moara_fp4_product(moara_ctx* ctx, int M, int N, int K, const void* a_q, cons
 int moara_fp4_linear_workspace_bytes(int M, int N, int K, size_t* out) {
     if (out == nullptr) return MOARA_ERR_INVALID_ARG;
     if (M < 1 || N < 1 || K < 1) return MOARA_ERR_SHAPE;
-    *out = linear_operand_bytes(M, K) + moara::fp4_product_workspace(M, N, K);
+    *out = linear_workspace(M, N, K);
     return MOARA_OK;
 }
 
@@ -356,19 +358,25 @@ int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_d
                      void* stream) {
     if (ctx == nullptr) return MOARA_ERR_INVALID_ARG;
     if (M < 1 || N < 1 || K < 1) return fail(ctx, MOARA_ERR_SHAPE, "M, N and K must be >= 1");
-    const size_t operand = linear_operand_bytes(M, K);
     int rc = check_product(ctx, M, N, K, b_q, b_sf, D, d_dtype, ldd, workspace, workspace_bytes,
-                           operand + moara::fp4_product_workspace(M, N, K));
+                           linear_workspace(M, N, K));
     if (rc == MOARA_OK) rc = check_strided(ctx, "X", X, x_dtype, K, ldx);
     if (rc != MOARA_OK) return rc;
     DeviceGuard g(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    char* q = static_cast<char*>(workspace);
-    char* sf = q + align_up(moara::fp4_q_bytes(M, K), 256);
-    cudaError_t e = moara::launch_fp4_quantize(X, x_dtype, M, K, ldx, q, sf, nullptr, nullptr, s, &ctx->launches);
-    if (e != cudaSuccess) return cuda_fail(ctx, e, "quantisation launch");
-    const moara::Fp4Product p{M, N, K, q, sf, b_q, b_sf, D, d_dtype, ldd, q + operand};
-    e = moara::launch_fp4_product(p, ctx->d_status, s, &ctx->launches);
+    moara::Fp4Product p{M, N, K, nullptr, nullptr, b_q, b_sf, D, d_dtype, ldd, X, x_dtype, ldx};
+    cudaError_t e = cudaSuccess;
+    const bool apart = !moara::fp4_quantizes(M, N, K);
+    if (apart) {
+        char* q = static_cast<char*>(workspace);
+        char* sf = q + align_up(moara::fp4_q_bytes(M, K), 256);
+        e = moara::launch_fp4_quantize(X, x_dtype, M, K, ldx, q, sf, nullptr, nullptr, s, &ctx->launches);
+        if (e != cudaSuccess) return cuda_fail(ctx, e, "quantisation launch");
+        p.aq = q;
+        p.asf = sf;
+        p.X = nullptr;
+    }
+    e = moara::launch_fp4_product(p, apart, ctx->d_status, s, &ctx->launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "product launch");
     return MOARA_OK;
 }
