@@ -51,8 +51,10 @@ class AdamWGroup:
         self.ctx = B.moara_create(B.moara_default_hparams(), device)
         self._dev = torch.device("cuda", device)
         self.params, self.copies, self.states = [], [], []
-        self._desc = np.zeros(0, _DESC)
         self._sizes = []
+        self._room = 0
+        self._grow(0)
+        self._norm_room, self._norm_at = 0, [0, 0, 0]
         self._workspace = {}
 
     def _check(self, x, what, n=None, dtypes=tuple(_TYPES)):
@@ -85,8 +87,7 @@ class AdamWGroup:
             s["exp_avg_scale"] = kept(exp_avg_scale, "exp_avg_scale", blocks, torch.float32)
             s["exp_avg_sq_scale"] = kept(exp_avg_sq_scale, "exp_avg_sq_scale", blocks, torch.float32)
         i = len(self.params)
-        if i == len(self._desc):
-            self._desc = np.concatenate([self._desc, np.zeros(max(16, i), _DESC)])
+        self._grow(i + 1)
         d = self._desc[i]
         d["n"], d["param"] = n, param.data_ptr()
         d["param_bf16"] = 0 if copy is None else copy.data_ptr()
@@ -101,8 +102,30 @@ class AdamWGroup:
         self.states.append(s)
         return i
 
+    def _grow(self, count):
+        """Room for `count` descriptors; all of them, their address and the fields that a step
+        fills in are kept (a view costs a microsecond)."""
+        if count > self._room:
+            grown = np.zeros(max(16, 2 * count), _DESC)
+            grown[:self._room] = self._table[:self._room]
+            self._table, self._room = grown, len(grown)
+        elif count == 0:
+            self._table = np.zeros(0, _DESC)
+        self._desc = self._table[:count]
+        self._all = self._desc, self._desc["grad"], self._desc["grad_dtype"], self._table.ctypes.data
+
     def _chosen(self, ids):
-        return self._desc[:len(self.params)] if ids is None else self._desc[list(ids)]
+        """The descriptors of a call, their grad and grad_dtype fields, their address."""
+        if ids is None:
+            return self._all
+        d = self._desc[list(ids)]
+        return d, d["grad"], d["grad_dtype"], d.ctypes.data
+
+    def _scalar(self, x, what):
+        """Address of a one-element float32 tensor."""
+        if x.dtype is not torch.float32 or x.numel() != 1 or x.get_device() != self.device:
+            self._check(x, what, 1, (torch.float32,))
+        return x.data_ptr()
 
     def _read(self, grads):
         """Addresses, sizes and types (a number, or a list) of gradients.  Calls of many short
@@ -120,23 +143,23 @@ class AdamWGroup:
         """One AdamW step at step t (1-based): grads[i] (fp32 or bf16) of every
         registered tensor, or of those in ids.  grad_scale: a one-element
         float32 device tensor that multiplies every gradient, or None."""
-        d = self._chosen(ids)
+        d, at_grad, at_type, at = self._chosen(ids)
         if len(grads) != len(d):
             raise ValueError(f"{len(grads)} gradients for {len(d)} tensors")
         ptrs, sizes, types = self._read(grads)
         if sizes != (self._sizes if ids is None else d["n"].tolist()):
             for g, n in zip(grads, d["n"].tolist()):
                 self._check(g, "grad", n)
-        d["grad"] = ptrs
-        d["grad_dtype"] = types
-        scale = 0 if grad_scale is None else self._check(grad_scale, "grad_scale", 1, (torch.float32,)).data_ptr()
-        B.moara_adamw_step(self.ctx, len(d), d.ctypes.data, self.hp, t, lr, scale, stream_handle(stream, self.device))
+        at_grad[:] = ptrs
+        at_type[:] = types
+        scale = 0 if grad_scale is None else self._scalar(grad_scale, "grad_scale")
+        B.moara_adamw_step(self.ctx, len(ptrs), at, self.hp, t, lr, scale, stream_handle(stream, self.device))
 
     def moments(self, exp_avg=None, exp_avg_sq=None, ids=None, stream=None):
         """The moments as fp32 tensors (lists, one per tensor); into the given
         ones, if any."""
-        d = self._chosen(ids)
-        sizes = d["n"].tolist()
+        d, _, _, at = self._chosen(ids)
+        sizes = self._sizes if ids is None else d["n"].tolist()
         with allocating_on(stream, self.device):
             outs = [[torch.empty(n, device=self._dev) for n in sizes] if x is None else x
                     for x in (exp_avg, exp_avg_sq)]
@@ -144,24 +167,24 @@ class AdamWGroup:
         for out in outs:
             if len(out) != len(d):
                 raise ValueError(f"{len(out)} outputs for {len(d)} tensors")
-            at, have, types = self._read(out)
+            addresses, have, types = self._read(out)
             if have != sizes or types != B.MOARA_DTYPE_F32 and len(out):
                 for x, n in zip(out, sizes):
                     self._check(x, "output", n, (torch.float32,))
-            ptrs.append(np.array(at, dtype=np.uint64))
-        B.moara_adamw_moments(self.ctx, len(d), d.ctypes.data, ptrs[0].ctypes.data, ptrs[1].ctypes.data,
+            ptrs.append(np.array(addresses, dtype=np.uint64))
+        B.moara_adamw_moments(self.ctx, len(d), at, ptrs[0].ctypes.data, ptrs[1].ctypes.data,
                               stream_handle(stream, self.device))
         return outs[0], outs[1]
 
     def _norm_workspace(self, count, handle, stream):
-        need = B.moara_grad_norm_workspace_bytes(count)
-        ws = self._workspace.get(handle)
-        if ws is None or ws.numel() < need:
+        ws, room = self._workspace.get(handle, (None, -1))
+        if count > room:
+            need = B.moara_grad_norm_workspace_bytes(count)
             with allocating_on(stream, self.device):
                 ws = torch.zeros(need, dtype=torch.uint8, device=self._dev)
                 # memory of a recorded graph is the graph's own
                 if not torch.cuda.is_current_stream_capturing():
-                    self._workspace[handle] = ws
+                    self._workspace[handle] = ws, count
         return ws
 
     def grad_norm(self, grads, max_norm=0.0, extra_sq=None, out=None, stream=None):
@@ -171,20 +194,25 @@ class AdamWGroup:
         what MoaraGroup.set_clip_extra takes, the last what step takes."""
         ptrs, sizes, types = self._read(grads)
         n = len(grads)
-        table = np.array((ptrs, sizes), dtype=np.int64)
-        kinds = np.empty(n, dtype=np.int32)
-        kinds[:] = types
+        if n > self._norm_room:
+            self._norm_room = room = 2 * n
+            self._norm = np.zeros(room, np.int64), np.zeros(room, np.int64), np.zeros(room, np.int32)
+            self._norm_at = [x.ctypes.data for x in self._norm]
+        if n:
+            a, b, c = self._norm
+            a[:n], b[:n], c[:n] = ptrs, sizes, types
         handle = stream_handle(stream, self.device)
         ws = self._norm_workspace(n, handle, stream)
-        extra = 0 if extra_sq is None else self._check(extra_sq, "extra_sq", 1, (torch.float32,)).data_ptr()
-        if out is None:
+        extra = 0 if extra_sq is None else self._scalar(extra_sq, "extra_sq")
+        if out is None and stream is None:
+            out = torch.empty(3, device=self._dev)
+        elif out is None:
             with allocating_on(stream, self.device):
                 out = torch.empty(3, device=self._dev)
         else:
             self._check(out, "out", 3, (torch.float32,))
-        at = table.ctypes.data
-        B.moara_grad_norm(self.ctx, n, at, at + 8 * n, kinds.ctypes.data, max_norm, extra, out.data_ptr(),
-                          ws.data_ptr(), ws.numel(), handle)
+        a, b, c = self._norm_at
+        B.moara_grad_norm(self.ctx, n, a, b, c, max_norm, extra, out.data_ptr(), ws.data_ptr(), ws.numel(), handle)
         return out
 
     def state_dict(self):

@@ -273,12 +273,12 @@ __device__ __forceinline__ float warp_top(const float (&a)[8]) {
     return __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));
 }
 
-__device__ __forceinline__ void new_moments(const AdamBatch& b, float g, float& m, float& v) {
+__device__ __forceinline__ void new_moments(const AdamCall& b, float g, float& m, float& v) {
     m = __fadd_rn(__fmul_rn(m, b.b1), __fmul_rn(g, b.c1));
     v = __fadd_rn(__fmul_rn(v, b.b2), __fmul_rn(__fmul_rn(g, g), b.c2));
 }
 
-__device__ __forceinline__ float new_param(const AdamTensor& t, const AdamBatch& b, float p, float m, float v) {
+__device__ __forceinline__ float new_param(const AdamTensor& t, const AdamCall& b, float p, float m, float v) {
     const float den = __fmaf_rn(sqrt_fast(v), b.rbc2, b.eps);
     return __fmaf_rn(p, t.keep, -__fdividef(__fmul_rn(m, t.step), den));
 }
@@ -288,7 +288,7 @@ __device__ __forceinline__ float new_param(const AdamTensor& t, const AdamBatch&
 // entries with fp32 parameters, bf16 gradients and copies (28 bytes each): 1.03 ms,
 // 7.1 TB/s.
 template <class PT, class GT, bool FULL>
-__device__ __forceinline__ void adam_tile(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, int lane) {
+__device__ __forceinline__ void adam_tile(const AdamTensor& t, const AdamCall& b, float coef, long long i0, int lane) {
     const long long n = t.n;
     const long long at[2] = {i0 + 4 * lane, i0 + 128 + 4 * lane};
     PT* const pp = static_cast<PT*>(t.p);
@@ -337,7 +337,7 @@ template <class PT, class GT, bool FULL> struct Block8 {
 };
 
 template <class PT, class GT, bool FULL>
-__device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamBatch& b, const Block8<PT, GT, FULL>& in,
+__device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamCall& b, const Block8<PT, GT, FULL>& in,
                                            float coef, long long i0, int lane) {
     const long long n = t.n, at = i0 + 8 * lane;
     PT* const pp = static_cast<PT*>(t.p);
@@ -389,7 +389,7 @@ __device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamBatch&
 
 // A warp's blocks below `end`, `stride` entries apart; returns the first one behind.
 template <class PT, class GT, bool FULL>
-__device__ __forceinline__ long long adam_blocks8(const AdamTensor& t, const AdamBatch& b, float coef, long long i0,
+__device__ __forceinline__ long long adam_blocks8(const AdamTensor& t, const AdamCall& b, float coef, long long i0,
                                                   long long stride, long long end) {
     const int lane = threadIdx.x & 31;
     if (i0 >= end) return i0;
@@ -408,7 +408,7 @@ __device__ __forceinline__ long long adam_blocks8(const AdamTensor& t, const Ada
 }
 
 template <class PT, class GT, bool B8>
-__device__ __forceinline__ void adam_any(const AdamTensor& t, const AdamBatch& b, float coef, long long i0, long long stride) {
+__device__ __forceinline__ void adam_any(const AdamTensor& t, const AdamCall& b, float coef, long long i0, long long stride) {
     if (B8) {
         if (t.kind & kAdamVector) i0 = adam_blocks8<PT, GT, true>(t, b, coef, i0, stride, t.n - MOARA_ADAMW_BLOCK + 1);
         adam_blocks8<PT, GT, false>(t, b, coef, i0, stride, t.n);
@@ -428,7 +428,7 @@ template <class F> __device__ __forceinline__ int find_tensor(int count, uint32_
     return lo;
 }
 
-__global__ void __launch_bounds__(256, 4) k_adamw(const __grid_constant__ AdamBatch b) {
+template <int CAP> __global__ void __launch_bounds__(256, 4) k_adamw(const __grid_constant__ AdamBatchOf<CAP> b) {
     const uint32_t c = blockIdx.x;
     const int q = find_tensor(b.count, c, [&](int i) { return b.start[i]; });
     const AdamTensor& t = b.t[q];
@@ -536,7 +536,7 @@ __device__ __forceinline__ float chunk_squares(const T* g, long long e0, long lo
     return s;
 }
 
-__global__ void __launch_bounds__(256) k_grad_norm(const __grid_constant__ NormBatch b) {
+template <int CAP> __global__ void __launch_bounds__(256) k_grad_norm(const __grid_constant__ NormBatchOf<CAP> b) {
     __shared__ double red[8];
     __shared__ bool finish;
     double acc = 0.0;
@@ -580,7 +580,15 @@ uint32_t adamw_key(uint64_t seed, uint32_t id, int64_t t) {
 }
 
 cudaError_t launch_adamw(const AdamBatch& b, cudaStream_t s, int64_t* launches) {
-    k_adamw<<<b.start[b.count], 256, 0, s>>>(b);
+    if (b.count <= kAdamFew) {
+        AdamBatchOf<kAdamFew> f;
+        static_cast<AdamCall&>(f) = b;
+        for (int i = 0; i < b.count; ++i) f.t[i] = b.t[i];
+        for (int i = 0; i <= b.count; ++i) f.start[i] = b.start[i];
+        k_adamw<kAdamFew><<<b.start[b.count], 256, 0, s>>>(f);
+    } else {
+        k_adamw<kAdamTensors><<<b.start[b.count], 256, 0, s>>>(b);
+    }
     ++*launches;
     return cudaGetLastError();
 }
@@ -592,7 +600,14 @@ cudaError_t launch_moments(const MomentBatch& b, cudaStream_t s, int64_t* launch
 }
 
 cudaError_t launch_grad_norm(const NormBatch& b, int ctas, cudaStream_t s, int64_t* launches) {
-    k_grad_norm<<<ctas, 256, 0, s>>>(b);
+    if (b.count <= kNormFew) {
+        NormBatchOf<kNormFew> f;
+        static_cast<NormCall&>(f) = b;
+        for (int i = 0; i < b.count; ++i) f.t[i] = b.t[i];
+        k_grad_norm<kNormFew><<<ctas, 256, 0, s>>>(f);
+    } else {
+        k_grad_norm<kNormTensors><<<ctas, 256, 0, s>>>(b);
+    }
     ++*launches;
     return cudaGetLastError();
 }

@@ -13,18 +13,24 @@ from .adamw import _TYPES, allocating_on, stream_handle
 class Fp4Matrix:
     """A rows x cols matrix in MXFP4 (layouts of moara.h): codes `q`, scales `sf`."""
 
+    __slots__ = "rows", "cols", "_sizes", "_ptrs", "_both", "_start", "_q", "_sf"
+
     def __init__(self, rows, cols, q=None, sf=None, device=0):
         self.rows, self.cols = rows, cols
-        self._sizes = sizes = B.moara_fp4_bytes(rows, cols)
-        self._gap = -sizes[0] % 256
-        self._both = None
+        if rows < 1 or cols < 1:
+            B.moara_fp4_bytes(rows, cols)                   # raises
+        # moara_fp4_bytes, without the call
+        nq = rows * ((cols + 31) // 32) * 16
+        sizes = self._sizes = nq, (rows + 127) // 128 * ((cols + 127) // 128) * 512
         if q is None and sf is None:
             # one allocation: the codes, and the scales from the next 256 bytes on
-            self._both = torch.empty(sizes[0] + self._gap + sizes[1], dtype=torch.uint8,
-                                     device=torch.device("cuda", device))
-            at = self._both.data_ptr()
-            self._ptrs = at, at + sizes[0] + self._gap
+            start = self._start = (nq + 255) // 256 * 256
+            both = self._both = torch.empty(start + sizes[1], dtype=torch.uint8,
+                                            device=device if isinstance(device, torch.device) else torch.device("cuda", device))
+            at = both.data_ptr()
+            self._ptrs = at, at + start
             return
+        self._both = None
         for x, size in zip((q, sf), sizes):
             if x is None or x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size:
                 raise ValueError(f"q and sf, contiguous uint8 tensors of {sizes} bytes, or neither are needed")
@@ -37,7 +43,7 @@ class Fp4Matrix:
 
     @property
     def sf(self):
-        return self._sf if self._both is None else self._both[self._sizes[0] + self._gap:]
+        return self._sf if self._both is None else self._both[self._start:]
 
 
 class Fp4Group:
@@ -84,9 +90,9 @@ class Fp4Group:
     def _matrix(self, m, rows, cols, stream):
         if m is None:
             if stream is None:
-                return Fp4Matrix(rows, cols, device=self.device)
+                return Fp4Matrix(rows, cols, device=self._dev)
             with allocating_on(stream, self.device):
-                return Fp4Matrix(rows, cols, device=self.device)
+                return Fp4Matrix(rows, cols, device=self._dev)
         if (m.rows, m.cols) != (rows, cols):
             raise ValueError(f"out: an operand of {rows} x {cols} is needed")
         return m
