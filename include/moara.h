@@ -534,17 +534,15 @@ int moara_fp4_dequantize(moara_ctx* ctx, const void* q, const void* sf, int rows
  * products of a weight W (n x k) with activations x (m x k) and their gradient dy
  * are y = x W^T, dx = dy (W^T)^T with the operand of W^T, and dW = dy^T (x^T)^T
  * with those of dy^T and x^T, whose bf16 result is a gradient for
- * moara_step_grouped.  workspace: moara_fp4_workspace_bytes(M, N, K) device bytes,
- * 16-byte aligned (NULL where that is 0), in use by one call at a time.
- * MOARA_ERR_UNSUPPORTED without tensor-core state. */
-int moara_fp4_workspace_bytes(int M, int N, int K, size_t* out);
+ * moara_step_grouped.  MOARA_ERR_UNSUPPORTED without tensor-core state. */
 int moara_fp4_product(moara_ctx* ctx, int M, int N, int K, const void* a_q, const void* a_sf, const void* b_q,
-                      const void* b_sf, void* D, int d_dtype, int64_t ldd, void* workspace, size_t workspace_bytes,
-                      void* stream);
+                      const void* b_sf, void* D, int d_dtype, int64_t ldd, void* stream);
 
 /* The same product with A given as X (M x K, fp32 or bf16, row pitch ldx >= K),
  * quantised by rows on the way, with the result of moara_fp4_quantize and
- * moara_fp4_product.  workspace: moara_fp4_linear_workspace_bytes(M, N, K). */
+ * moara_fp4_product.  workspace: moara_fp4_linear_workspace_bytes(M, N, K) device
+ * bytes, 16-byte aligned (NULL where that is 0: up to 16 rows), in use by one call
+ * at a time. */
 int moara_fp4_linear_workspace_bytes(int M, int N, int K, size_t* out);
 int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_dtype, int64_t ldx, const void* b_q,
                      const void* b_sf, void* D, int d_dtype, int64_t ldd, void* workspace, size_t workspace_bytes,

@@ -9,14 +9,14 @@ import contextlib
 import numpy as np
 import torch
 
+from . import _host
 from . import binding as B
 
 _TYPES = {torch.float32: B.MOARA_DTYPE_F32, torch.bfloat16: B.MOARA_DTYPE_BF16}
 _STATES = {"f32": B.MOARA_DTYPE_F32, "block8": B.MOARA_DTYPE_BLOCK8}
 _DESC = np.dtype(B.moara_adamw_tensor)
-_FLOATS = set(_TYPES)
-_data_ptr, _numel, _is_contiguous, _get_device = (
-    getattr(torch.Tensor, f) for f in ("data_ptr", "numel", "is_contiguous", "get_device"))
+_SIZE = _DESC.itemsize
+_N, _GRAD, _GRAD_DTYPE = (_DESC.fields[f][1] for f in ("n", "grad", "grad_dtype"))
 
 
 def _current_stream(device):
@@ -51,7 +51,6 @@ class AdamWGroup:
         self.ctx = B.moara_create(B.moara_default_hparams(), device)
         self._dev = torch.device("cuda", device)
         self.params, self.copies, self.states = [], [], []
-        self._sizes = []
         self._room = 0
         self._grow(0)
         self._norm_room, self._norm_at = 0, [0, 0, 0]
@@ -98,13 +97,11 @@ class AdamWGroup:
         d["weight_decay"], d["lr_scale"] = weight_decay, lr_scale
         self.params.append(param)
         self.copies.append(copy)
-        self._sizes.append(n)
         self.states.append(s)
         return i
 
     def _grow(self, count):
-        """Room for `count` descriptors; all of them, their address and the fields that a step
-        fills in are kept (a view costs a microsecond)."""
+        """Room for `count` descriptors; they and their address are kept."""
         if count > self._room:
             grown = np.zeros(max(16, 2 * count), _DESC)
             grown[:self._room] = self._table[:self._room]
@@ -112,14 +109,14 @@ class AdamWGroup:
         elif count == 0:
             self._table = np.zeros(0, _DESC)
         self._desc = self._table[:count]
-        self._all = self._desc, self._desc["grad"], self._desc["grad_dtype"], self._table.ctypes.data
+        self._all = self._desc, self._table.ctypes.data
 
     def _chosen(self, ids):
-        """The descriptors of a call, their grad and grad_dtype fields, their address."""
+        """The descriptors of a call, and their address."""
         if ids is None:
             return self._all
         d = self._desc[list(ids)]
-        return d, d["grad"], d["grad_dtype"], d.ctypes.data
+        return d, d.ctypes.data
 
     def _scalar(self, x, what):
         """Address of a one-element float32 tensor."""
@@ -127,54 +124,45 @@ class AdamWGroup:
             self._check(x, what, 1, (torch.float32,))
         return x.data_ptr()
 
-    def _read(self, grads):
-        """Addresses, sizes and types (a number, or a list) of gradients.  Calls of many short
-        tensors are bound by this, so each property is one pass over the list."""
-        sizes = list(map(_numel, grads))
-        types = [g.dtype for g in grads]
-        kinds = set(types)
-        if not kinds <= _FLOATS or not all(map(_is_contiguous, grads)) or set(map(_get_device, grads)) - {self.device}:
-            for g in grads:
-                self._check(g, "grad")
-        kinds = _TYPES[kinds.pop()] if len(kinds) == 1 else [_TYPES[t] for t in types]
-        return list(map(_data_ptr, grads)), sizes, kinds
+    def _read(self, xs, what, addresses, types, sizes, given):
+        """Addresses, types and sizes of tensors into (or, with `given`, sizes against)
+        arrays given as (address, stride)."""
+        bad = _host.read(xs if isinstance(xs, (list, tuple)) else list(xs), self.device, *addresses, *types, *sizes, given)
+        if bad >= 0:
+            raise ValueError(f"{what} {bad}: a contiguous float32 or bfloat16 tensor on cuda:{self.device}"
+                             + (" with its tensor's number of entries" if given else "") + " is needed")
 
     def step(self, grads, t, lr, grad_scale=None, ids=None, stream=None):
         """One AdamW step at step t (1-based): grads[i] (fp32 or bf16) of every
         registered tensor, or of those in ids.  grad_scale: a one-element
         float32 device tensor that multiplies every gradient, or None."""
-        d, at_grad, at_type, at = self._chosen(ids)
+        d, at = self._chosen(ids)
         if len(grads) != len(d):
             raise ValueError(f"{len(grads)} gradients for {len(d)} tensors")
-        ptrs, sizes, types = self._read(grads)
-        if sizes != (self._sizes if ids is None else d["n"].tolist()):
-            for g, n in zip(grads, d["n"].tolist()):
-                self._check(g, "grad", n)
-        at_grad[:] = ptrs
-        at_type[:] = types
+        self._read(grads, "gradient", (at + _GRAD, _SIZE), (at + _GRAD_DTYPE, _SIZE), (at + _N, _SIZE), True)
         scale = 0 if grad_scale is None else self._scalar(grad_scale, "grad_scale")
-        B.moara_adamw_step(self.ctx, len(ptrs), at, self.hp, t, lr, scale, stream_handle(stream, self.device))
+        B.moara_adamw_step(self.ctx, len(d), at, self.hp, t, lr, scale, stream_handle(stream, self.device))
 
     def moments(self, exp_avg=None, exp_avg_sq=None, ids=None, stream=None):
         """The moments as fp32 tensors (lists, one per tensor); into the given
         ones, if any."""
-        d, _, _, at = self._chosen(ids)
-        sizes = self._sizes if ids is None else d["n"].tolist()
-        with allocating_on(stream, self.device):
-            outs = [[torch.empty(n, device=self._dev) for n in sizes] if x is None else x
-                    for x in (exp_avg, exp_avg_sq)]
-        ptrs = []
-        for out in outs:
-            if len(out) != len(d):
-                raise ValueError(f"{len(out)} outputs for {len(d)} tensors")
-            addresses, have, types = self._read(out)
-            if have != sizes or types != B.MOARA_DTYPE_F32 and len(out):
-                for x, n in zip(out, sizes):
-                    self._check(x, "output", n, (torch.float32,))
-            ptrs.append(np.array(addresses, dtype=np.uint64))
-        B.moara_adamw_moments(self.ctx, len(d), at, ptrs[0].ctypes.data, ptrs[1].ctypes.data,
-                              stream_handle(stream, self.device))
-        return outs[0], outs[1]
+        d, at = self._chosen(ids)
+        n = len(d)
+        if exp_avg is None or exp_avg_sq is None:
+            sizes = d["n"].tolist()
+            with allocating_on(stream, self.device):
+                exp_avg, exp_avg_sq = ([torch.empty(k, device=self._dev) for k in sizes] if x is None else x
+                                       for x in (exp_avg, exp_avg_sq))
+        ptrs, types = np.zeros((2, n), np.uint64), np.zeros(n, np.int32)
+        to, kinds = ptrs.ctypes.data, types.ctypes.data
+        for k, out in enumerate((exp_avg, exp_avg_sq)):
+            if len(out) != n:
+                raise ValueError(f"{len(out)} outputs for {n} tensors")
+            self._read(out, "output", (to + 8 * n * k, 8), (kinds, 4), (at + _N, _SIZE), True)
+            if types.any():
+                raise ValueError("the moments' outputs are float32")
+        B.moara_adamw_moments(self.ctx, len(d), at, to, to + 8 * n, stream_handle(stream, self.device))
+        return exp_avg, exp_avg_sq
 
     def _norm_workspace(self, count, handle, stream):
         ws, room = self._workspace.get(handle, (None, -1))
@@ -192,15 +180,13 @@ class AdamWGroup:
         bf16), a float32 tensor of three.  extra_sq: a one-element float32 device
         tensor added to the sum under the root, or None.  The first element is
         what MoaraGroup.set_clip_extra takes, the last what step takes."""
-        ptrs, sizes, types = self._read(grads)
         n = len(grads)
         if n > self._norm_room:
-            self._norm_room = room = 2 * n
-            self._norm = np.zeros(room, np.int64), np.zeros(room, np.int64), np.zeros(room, np.int32)
+            self._norm_room = 2 * n
+            self._norm = np.zeros(2 * n, np.uint64), np.zeros(2 * n, np.int64), np.zeros(2 * n, np.int32)
             self._norm_at = [x.ctypes.data for x in self._norm]
-        if n:
-            a, b, c = self._norm
-            a[:n], b[:n], c[:n] = ptrs, sizes, types
+        a, b, c = self._norm_at
+        self._read(grads, "gradient", (a, 8), (c, 4), (b, 8), False)
         handle = stream_handle(stream, self.device)
         ws = self._norm_workspace(n, handle, stream)
         extra = 0 if extra_sq is None else self._scalar(extra_sq, "extra_sq")
@@ -211,7 +197,6 @@ class AdamWGroup:
                 out = torch.empty(3, device=self._dev)
         else:
             self._check(out, "out", 3, (torch.float32,))
-        a, b, c = self._norm_at
         B.moara_grad_norm(self.ctx, n, a, b, c, max_norm, extra, out.data_ptr(), ws.data_ptr(), ws.numel(), handle)
         return out
 

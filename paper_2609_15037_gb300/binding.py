@@ -129,8 +129,7 @@ def _load():
         "moara_fp4_bytes": (i32, [i32, i32, P(sz), P(sz)]),
         "moara_fp4_quantize": (i32, [vp, vp, i32, i32, i32, i64, vp, vp, vp, vp, vp]),
         "moara_fp4_dequantize": (i32, [vp, vp, vp, i32, i32, vp, i32, i64, vp]),
-        "moara_fp4_workspace_bytes": (i32, [i32, i32, i32, P(sz)]),
-        "moara_fp4_product": (i32, [vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, i64, vp, sz, vp]),
+        "moara_fp4_product": (i32, [vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, i64, vp]),
         "moara_fp4_linear_workspace_bytes": (i32, [i32, i32, i32, P(sz)]),
         "moara_fp4_linear": (i32, [vp, i32, i32, i32, vp, i32, i64, vp, vp, vp, i32, i64, vp, sz, vp]),
     }
@@ -358,16 +357,9 @@ def moara_fp4_dequantize(ctx, q, sf, rows, cols, out, dtype, ldo, stream=0):
            "moara_fp4_dequantize")
 
 
-def moara_fp4_workspace_bytes(M, N, K):
-    out = ctypes.c_size_t()
-    _check(_lib.moara_fp4_workspace_bytes(M, N, K, ctypes.byref(out)), what="moara_fp4_workspace_bytes")
-    return out.value
-
-
-def moara_fp4_product(ctx, M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, workspace=0, workspace_bytes=0,
-                      stream=0):
-    _check(_lib.moara_fp4_product(ctx, M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, workspace or None,
-                                  workspace_bytes, stream), ctx, "moara_fp4_product")
+def moara_fp4_product(ctx, M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, stream=0):
+    _check(_lib.moara_fp4_product(ctx, M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, stream), ctx,
+           "moara_fp4_product")
 
 
 def moara_fp4_linear_workspace_bytes(M, N, K):
@@ -409,6 +401,6 @@ EXPORTED = [
     "moara_last_error", "moara_status_string", "moara_launch_count", "moara_set_wait_limit",
     "moara_profile_enable", "moara_profile_read", "moara_step_static_scratch",
     "moara_adamw_step", "moara_adamw_moments", "moara_grad_norm_workspace_bytes", "moara_grad_norm",
-    "moara_fp4_bytes", "moara_fp4_quantize", "moara_fp4_dequantize", "moara_fp4_workspace_bytes",
-    "moara_fp4_product", "moara_fp4_linear_workspace_bytes", "moara_fp4_linear",
+    "moara_fp4_bytes", "moara_fp4_quantize", "moara_fp4_dequantize", "moara_fp4_product",
+    "moara_fp4_linear_workspace_bytes", "moara_fp4_linear",
 ]

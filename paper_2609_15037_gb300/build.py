@@ -2,7 +2,9 @@
 
 Each translation unit under csrc/ compiles to an object in _build/ (in
 parallel); the objects link into paper_2609_15037_gb300/libmoara.so.  A unit is
-recompiled only when it or a header is newer than its object.
+recompiled only when it or a header is newer than its object.  host.cpp, the
+Python module that reads lists of tensors, is built apart from it against
+torch's headers into paper_2609_15037_gb300/_host.so.
 """
 
 from __future__ import annotations
@@ -14,6 +16,7 @@ import platform
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -36,8 +39,13 @@ def _nvcc():
     return exe
 
 
+HOST_SRC = os.path.join(CSRC, "host.cpp")
+HOST = os.path.join(PKG, "_host.so")
+
+
 def _sources():
-    return sorted(glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cpp")))
+    return sorted(s for s in glob.glob(os.path.join(CSRC, "*.cu")) + glob.glob(os.path.join(CSRC, "*.cpp"))
+                  if s != HOST_SRC)
 
 
 def _headers():
@@ -59,12 +67,38 @@ def _compile(src, verbose_ptxas=False):
     return obj, p.stderr
 
 
+def _build_host():
+    """_host.so: again when its source, torch or the interpreter is another one."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    python = sysconfig.get_paths()["include"]
+    cxx = shutil.which("g++") or "g++"
+    key = "\n".join([HOST, torch.__version__, sys.version, str(os.path.getmtime(HOST_SRC))])
+    stamp = os.path.join(OUT_DIR, "host.stamp")
+    if os.path.exists(HOST) and os.path.exists(stamp) and open(stamp).read() == key:
+        return
+    tmp = HOST + ".tmp"
+    cmd = [cxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", os.path.join(root, "include"),
+           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-isystem", python,
+           HOST_SRC, "-o", tmp, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    p = subprocess.run(cmd, capture_output=True, text=True)
+    if p.returncode != 0:
+        raise RuntimeError(f"g++ failed for host.cpp:\n{p.stdout}\n{p.stderr}")
+    os.replace(tmp, HOST)
+    with open(stamp, "w") as f:
+        f.write(key)
+
+
 def build(verbose_ptxas=False, jobs=None):
-    """Compile every CUDA/C++ unit for sm_103a and link libmoara.so."""
+    """Compile every CUDA/C++ unit for sm_103a, link libmoara.so, and build _host.so."""
     os.makedirs(OUT_DIR, exist_ok=True)
     srcs = _sources()
-    with cf.ThreadPoolExecutor(max_workers=jobs or min(8, len(srcs))) as ex:
+    with cf.ThreadPoolExecutor(max_workers=jobs or min(8, len(srcs) + 1)) as ex:
+        host = ex.submit(_build_host)
         results = list(ex.map(lambda s: _compile(s, verbose_ptxas), srcs))
+        host.result()
     objs = [r[0] for r in results]
     if verbose_ptxas:
         for _, log in results:

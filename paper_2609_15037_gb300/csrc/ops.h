@@ -130,9 +130,8 @@ struct Fp4Product {
     int x_dtype;
     int64_t ldx;
 };
-// Whether a product of these sizes quantises A itself, and the workspace it needs.
-bool fp4_quantizes(int M, int N, int K);
-size_t fp4_product_workspace(int M, int N, int K);
+// Whether a product of M rows can quantise A itself.
+bool fp4_quantizes(int M);
 // early: the launch in front wrote A and nothing else, and lets this one begin beside it.
 // status: device word for MOARA_ERR_DEVICE_TIMEOUT
 cudaError_t launch_fp4_product(const Fp4Product& p, bool early, int* status, cudaStream_t s, int64_t* launches);

@@ -88,24 +88,19 @@ int check_operand(moara_ctx* ctx, const char* what, const void* q, const void* s
 }
 
 int check_product(moara_ctx* ctx, int M, int N, int K, const void* bq, const void* bsf, const void* D, int d_dtype,
-                  int64_t ldd, const void* workspace, size_t have, size_t need) {
+                  int64_t ldd) {
     if (ctx->tc == nullptr) return fail(ctx, MOARA_ERR_UNSUPPORTED, "no tensor-core state on this device");
     int rc = check_matrix(ctx, "A", M, K);
     if (rc == MOARA_OK) rc = check_matrix(ctx, "B", N, K);
     if (rc == MOARA_OK) rc = check_matrix(ctx, "D", M, N);
     if (rc == MOARA_OK) rc = check_operand(ctx, "B", bq, bsf);
     if (rc == MOARA_OK) rc = check_strided(ctx, "D", D, d_dtype, N, ldd);
-    if (rc != MOARA_OK) return rc;
-    if (need > 0 && (workspace == nullptr || have < need))
-        return fail(ctx, MOARA_ERR_WORKSPACE, "the product needs %zu bytes of workspace", need);
-    if (need > 0 && !aligned16(workspace)) return fail(ctx, MOARA_ERR_ALIGN, "workspace is not 16-byte aligned");
-    return MOARA_OK;
+    return rc;
 }
 
-size_t linear_workspace(int M, int N, int K) {
-    if (moara::fp4_quantizes(M, N, K)) return moara::fp4_product_workspace(M, N, K);
-    return align_up(moara::fp4_q_bytes(M, K), 256) + align_up(moara::fp4_sf_bytes(M, K), 256) +
-           moara::fp4_product_workspace(M, N, K);
+// The operand of A between its quantisation and its product.
+size_t linear_workspace(int M, int K) {
+    return moara::fp4_quantizes(M) ? 0 : align_up(moara::fp4_q_bytes(M, K), 256) + moara::fp4_sf_bytes(M, K);
 }
 
 }  // namespace
@@ -323,20 +318,10 @@ int moara_fp4_dequantize(moara_ctx* ctx, const void* q, const void* sf, int rows
     return MOARA_OK;
 }
 
-int moara_fp4_workspace_bytes(int M, int N, int K, size_t* out) {
-    if (out == nullptr) return MOARA_ERR_INVALID_ARG;
-    if (M < 1 || N < 1 || K < 1) return MOARA_ERR_SHAPE;
-    *out = moara::fp4_product_workspace(M, N, K);
-    return MOARA_OK;
-}
-
 int moara_fp4_product(moara_ctx* ctx, int M, int N, int K, const void* a_q, const void* a_sf, const void* b_q,
-                      const void* b_sf, void* D, int d_dtype, int64_t ldd, void* workspace, size_t workspace_bytes,
-                      void* stream) {
+                      const void* b_sf, void* D, int d_dtype, int64_t ldd, void* stream) {
     if (ctx == nullptr) return MOARA_ERR_INVALID_ARG;
-    if (M < 1 || N < 1 || K < 1) return fail(ctx, MOARA_ERR_SHAPE, "M, N and K must be >= 1");
-    int rc = check_product(ctx, M, N, K, b_q, b_sf, D, d_dtype, ldd, workspace, workspace_bytes,
-                           moara::fp4_product_workspace(M, N, K));
+    int rc = check_product(ctx, M, N, K, b_q, b_sf, D, d_dtype, ldd);
     if (rc == MOARA_OK) rc = check_operand(ctx, "A", a_q, a_sf);
     if (rc != MOARA_OK) return rc;
     DeviceGuard g(ctx->device);
@@ -349,7 +334,7 @@ int moara_fp4_product(moara_ctx* ctx, int M, int N, int K, const void* a_q, cons
 int moara_fp4_linear_workspace_bytes(int M, int N, int K, size_t* out) {
     if (out == nullptr) return MOARA_ERR_INVALID_ARG;
     if (M < 1 || N < 1 || K < 1) return MOARA_ERR_SHAPE;
-    *out = linear_workspace(M, N, K);
+    *out = linear_workspace(M, K);
     return MOARA_OK;
 }
 
@@ -357,16 +342,18 @@ int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_d
                      const void* b_sf, void* D, int d_dtype, int64_t ldd, void* workspace, size_t workspace_bytes,
                      void* stream) {
     if (ctx == nullptr) return MOARA_ERR_INVALID_ARG;
-    if (M < 1 || N < 1 || K < 1) return fail(ctx, MOARA_ERR_SHAPE, "M, N and K must be >= 1");
-    int rc = check_product(ctx, M, N, K, b_q, b_sf, D, d_dtype, ldd, workspace, workspace_bytes,
-                           linear_workspace(M, N, K));
+    int rc = check_product(ctx, M, N, K, b_q, b_sf, D, d_dtype, ldd);
     if (rc == MOARA_OK) rc = check_strided(ctx, "X", X, x_dtype, K, ldx);
     if (rc != MOARA_OK) return rc;
+    const size_t need = linear_workspace(M, K);
+    if (need > 0 && (workspace == nullptr || workspace_bytes < need))
+        return fail(ctx, MOARA_ERR_WORKSPACE, "the product needs %zu bytes of workspace", need);
+    if (need > 0 && !aligned16(workspace)) return fail(ctx, MOARA_ERR_ALIGN, "workspace is not 16-byte aligned");
     DeviceGuard g(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     moara::Fp4Product p{M, N, K, nullptr, nullptr, b_q, b_sf, D, d_dtype, ldd, X, x_dtype, ldx};
     cudaError_t e = cudaSuccess;
-    const bool apart = !moara::fp4_quantizes(M, N, K);
+    const bool apart = !moara::fp4_quantizes(M);
     if (apart) {
         char* q = static_cast<char*>(workspace);
         char* sf = q + align_up(moara::fp4_q_bytes(M, K), 256);

@@ -4,10 +4,15 @@ moara_fp4_linear.  Every computation happens in the library's kernels."""
 
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import binding as B
 from .adamw import _TYPES, allocating_on, stream_handle
+
+
+_linear_bytes = functools.lru_cache(maxsize=4096)(B.moara_fp4_linear_workspace_bytes)
 
 
 class Fp4Matrix:
@@ -125,9 +130,7 @@ class Fp4Group:
         m, n, k = a.rows, b.rows, a.cols
         out = self._out(out, m, n, dtype, stream)
         ptr, dt, ld = self._strided(out, "out")
-        ws, size = self._workspace(B.moara_fp4_workspace_bytes(m, n, k), stream)
-        B.moara_fp4_product(self.ctx, m, n, k, *a._ptrs, *b._ptrs, ptr, dt, ld, ws.data_ptr() if size else 0, size,
-                            stream_handle(stream, self.device))
+        B.moara_fp4_product(self.ctx, m, n, k, *a._ptrs, *b._ptrs, ptr, dt, ld, stream_handle(stream, self.device))
         return out
 
     def linear(self, x, b, dtype=torch.bfloat16, out=None, stream=None):
@@ -139,7 +142,7 @@ class Fp4Group:
         n = b.rows
         out = self._out(out, m, n, dtype, stream)
         ptr, dt, ld = self._strided(out, "out")
-        ws, size = self._workspace(B.moara_fp4_linear_workspace_bytes(m, n, k), stream)
+        ws, size = self._workspace(_linear_bytes(m, n, k), stream)
         B.moara_fp4_linear(self.ctx, m, n, k, xp, xd, ldx, *b._ptrs, ptr, dt, ld, ws.data_ptr() if size else 0, size,
                            stream_handle(stream, self.device))
         return out

@@ -309,12 +309,12 @@ def test_refusals(M, fp4):
     d = D.data_ptr()
     big = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
     ws = (big.data_ptr(), big.numel())
-    assert P(64, 64, 0, q, sf, q, sf, d, 0, 64, *ws) == M.MOARA_ERR_SHAPE
-    assert P(64, 64, 96, q, sf, q, sf, d, 0, 63, *ws) == M.MOARA_ERR_SHAPE
-    assert P(64, 64, 96, q, sf, q, sf, d, 5, 64, *ws) == M.MOARA_ERR_INVALID_ARG
-    assert P(64, 64, 96, None, sf, q, sf, d, 0, 64, *ws) == M.MOARA_ERR_INVALID_ARG
-    assert P(64, 64, 96, q, sf, q + 1, sf, d, 0, 64, *ws) == M.MOARA_ERR_ALIGN
-    assert P(64, 64, 96, q, sf, q, sf, d + 2, 0, 64, *ws) == M.MOARA_ERR_ALIGN
+    assert P(64, 64, 0, q, sf, q, sf, d, 0, 64) == M.MOARA_ERR_SHAPE
+    assert P(64, 64, 96, q, sf, q, sf, d, 0, 63) == M.MOARA_ERR_SHAPE
+    assert P(64, 64, 96, q, sf, q, sf, d, 5, 64) == M.MOARA_ERR_INVALID_ARG
+    assert P(64, 64, 96, None, sf, q, sf, d, 0, 64) == M.MOARA_ERR_INVALID_ARG
+    assert P(64, 64, 96, q, sf, q + 1, sf, d, 0, 64) == M.MOARA_ERR_ALIGN
+    assert P(64, 64, 96, q, sf, q, sf, d + 2, 0, 64) == M.MOARA_ERR_ALIGN
     L = lambda *a: code(lambda: M.moara_fp4_linear(fp4.ctx, *a))  # noqa: E731
     assert L(64, 64, 96, X, 0, 96, q, sf, d, 0, 64, ws[0], 64) == M.MOARA_ERR_WORKSPACE
     assert L(64, 64, 96, X, 0, 95, q, sf, d, 0, 64, *ws) == M.MOARA_ERR_SHAPE

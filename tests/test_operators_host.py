@@ -30,7 +30,7 @@ def test_fp4_bytes(M, rows, cols, q, sf):
 
 
 def test_host_sizes_refuse(M):
-    for call in (lambda: M.moara_fp4_bytes(0, 1), lambda: M.moara_fp4_workspace_bytes(1, 0, 1),
+    for call in (lambda: M.moara_fp4_bytes(0, 1), lambda: M.moara_fp4_linear_workspace_bytes(1, 0, 1),
                  lambda: M.moara_fp4_linear_workspace_bytes(1, 1, -1)):
         with pytest.raises(M.MoaraError) as ei:
             call()
@@ -47,7 +47,7 @@ def test_null_context_is_refused(M):
     assert lib.moara_adamw_moments(None, 0, None, None, None, None) == M.MOARA_ERR_INVALID_ARG
     assert lib.moara_grad_norm(None, 0, None, None, None, 0.0, None, None, None, 0, None) == M.MOARA_ERR_INVALID_ARG
     assert lib.moara_fp4_quantize(None, None, 0, 1, 1, 1, None, None, None, None, None) == M.MOARA_ERR_INVALID_ARG
-    assert lib.moara_fp4_product(None, 1, 1, 1, None, None, None, None, None, 0, 1, None, 0, None) == M.MOARA_ERR_INVALID_ARG
+    assert lib.moara_fp4_product(None, 1, 1, 1, None, None, None, None, None, 0, 1, None) == M.MOARA_ERR_INVALID_ARG
 
 
 def test_e2m1_rounding_by_hand():
