@@ -3,8 +3,7 @@
 Each translation unit under csrc/ compiles to an object in _build/ (in
 parallel); the objects link into paper_2609_15037_gb300/libmoara.so.  A unit is
 recompiled only when it or a header is newer than its object.  host.cpp, the
-Python module that reads lists of tensors, is built apart from it against
-torch's headers into paper_2609_15037_gb300/_host.so.
+Python module that reads tensors, is built apart from it against torch's headers into paper_2609_15037_gb300/_host.so.
 """
 
 from __future__ import annotations
@@ -73,7 +72,7 @@ def _build_host():
     root = os.path.dirname(torch.__file__)
     python = sysconfig.get_paths()["include"]
     cxx = shutil.which("g++") or "g++"
-    key = "\n".join([HOST, torch.__version__, sys.version, str(os.path.getmtime(HOST_SRC))])
+    key = "\n".join([HOST, torch.__version__, sys.version, *(str(os.path.getmtime(f)) for f in (HOST_SRC, os.path.join(ROOT, "include", "moara.h")))])
     stamp = os.path.join(OUT_DIR, "host.stamp")
     if os.path.exists(HOST) and os.path.exists(stamp) and open(stamp).read() == key:
         return
@@ -82,7 +81,7 @@ def _build_host():
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            "-isystem", os.path.join(root, "include"),
            "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-isystem", python,
-           HOST_SRC, "-o", tmp, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+           "-I", os.path.join(ROOT, "include"), HOST_SRC, "-o", tmp, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
     p = subprocess.run(cmd, capture_output=True, text=True)
     if p.returncode != 0:
         raise RuntimeError(f"g++ failed for host.cpp:\n{p.stdout}\n{p.stderr}")

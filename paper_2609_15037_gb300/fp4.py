@@ -4,15 +4,24 @@ moara_fp4_linear.  Every computation happens in the library's kernels."""
 
 from __future__ import annotations
 
-import functools
+import ctypes
 
 import torch
 
+from . import _host
 from . import binding as B
 from .adamw import _TYPES, allocating_on, stream_handle
 
 
-_linear_bytes = functools.lru_cache(maxsize=4096)(B.moara_fp4_linear_workspace_bytes)
+def _address(name):
+    return ctypes.cast(getattr(B.lib, name), ctypes.c_void_p).value
+
+
+_ENTRIES = {
+    "moara_fp4_dequantize": (_host.fp4_dequantize, _address("moara_fp4_dequantize")),
+    "moara_fp4_product": (_host.fp4_product, _address("moara_fp4_product")),
+    "moara_fp4_linear": (_host.fp4_linear, _address("moara_fp4_linear"), _address("moara_fp4_linear_workspace_bytes")),
+}
 
 
 class Fp4Matrix:
@@ -30,15 +39,14 @@ class Fp4Matrix:
         if q is None and sf is None:
             # one allocation: the codes, and the scales from the next 256 bytes on
             start = self._start = (nq + 255) // 256 * 256
-            both = self._both = torch.empty(start + sizes[1], dtype=torch.uint8,
-                                            device=device if isinstance(device, torch.device) else torch.device("cuda", device))
-            at = both.data_ptr()
+            self._both, at = _host.bytes(start + sizes[1], device)
             self._ptrs = at, at + start
             return
         self._both = None
         for x, size in zip((q, sf), sizes):
-            if x is None or x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size:
-                raise ValueError(f"q and sf, contiguous uint8 tensors of {sizes} bytes, or neither are needed")
+            if (x is None or x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size
+                    or x.get_device() != device):
+                raise ValueError(f"q and sf, contiguous uint8 tensors of {sizes} bytes on cuda:{device}, or neither are needed")
         self._q, self._sf = q, sf
         self._ptrs = q.data_ptr(), sf.data_ptr()
 
@@ -69,46 +77,39 @@ class Fp4Group:
         self.device = device
         self.ctx = None
         self.ctx = B.moara_create(B.moara_default_hparams(), device)
-        self._dev = torch.device("cuda", device)
-
-    def _strided(self, x, what):
-        """(address, type, row pitch) of a matrix whose rows are contiguous."""
-        if x.dim() != 2 or x.dtype not in _TYPES or x.get_device() != self.device:
-            raise ValueError(f"{what}: a float32 or bfloat16 matrix on cuda:{self.device} is needed")
-        rows, cols = x.shape
-        if cols > 1 and x.stride(1) != 1:
-            raise ValueError(f"{what}: the entries of a row must be contiguous")
-        return x.data_ptr(), _TYPES[x.dtype], x.stride(0) if rows > 1 else max(cols, 1)
-
-    def _out(self, out, rows, cols, dtype, stream):
-        if out is None:
-            if dtype not in _TYPES:
-                raise ValueError("dtype must be float32 or bfloat16")
-            if stream is None:
-                return torch.empty((rows, cols), dtype=dtype, device=self._dev)
-            with allocating_on(stream, self.device):
-                return torch.empty((rows, cols), dtype=dtype, device=self._dev)
-        if tuple(out.shape) != (rows, cols):
-            raise ValueError(f"out: shape {(rows, cols)} is needed")
-        return out
 
     def _matrix(self, m, rows, cols, stream):
         if m is None:
             if stream is None:
-                return Fp4Matrix(rows, cols, device=self._dev)
+                return Fp4Matrix(rows, cols, device=self.device)
             with allocating_on(stream, self.device):
-                return Fp4Matrix(rows, cols, device=self._dev)
+                return Fp4Matrix(rows, cols, device=self.device)
         if (m.rows, m.cols) != (rows, cols):
             raise ValueError(f"out: an operand of {rows} x {cols} is needed")
         return m
+
+    def _call(self, name, *args, out, dtype, stream):
+        """A call of the native module: the entry's address, its arguments, where its output
+        goes.  Its tensor, or the entry's error raised."""
+        if out is None and dtype not in _TYPES:
+            raise ValueError("dtype must be float32 or bfloat16")
+        fn, entry, *more = _ENTRIES[name]
+        tail = out, _TYPES.get(dtype, 0), self.device, stream_handle(stream, self.device), *more
+        if stream is None:
+            got = fn(entry, self.ctx, *args, *tail)
+        else:
+            with allocating_on(stream, self.device):
+                got = fn(entry, self.ctx, *args, *tail)
+        if got.__class__ is int:
+            B._check(got, self.ctx, name)
+        return got
 
     def quantize(self, x, rows=True, cols=False, out=None, out_cols=None, stream=None):
         """The operand of x (rows), of its transpose (cols), or both from one
         read of x; into out and out_cols where they are given."""
         if not rows and not cols:
             raise ValueError("rows, cols or both")
-        ptr, dtype, ld = self._strided(x, "x")
-        m, k = x.shape
+        ptr, dtype, m, k, ld = _host.matrix(x, self.device)
         a = self._matrix(out, m, k, stream) if rows else None
         b = self._matrix(out_cols, k, m, stream) if cols else None
         q, sf = a._ptrs if rows else (0, 0)
@@ -118,42 +119,18 @@ class Fp4Group:
 
     def dequantize(self, a, dtype=torch.bfloat16, out=None, stream=None):
         """The values of an operand (bfloat16 holds them exactly)."""
-        out = self._out(out, a.rows, a.cols, dtype, stream)
-        ptr, dt, ld = self._strided(out, "out")
-        B.moara_fp4_dequantize(self.ctx, *a._ptrs, a.rows, a.cols, ptr, dt, ld, stream_handle(stream, self.device))
-        return out
+        return self._call("moara_fp4_dequantize", *a._ptrs, a.rows, a.cols, out=out, dtype=dtype, stream=stream)
 
     def product(self, a, b, dtype=torch.bfloat16, out=None, stream=None):
         """a b^T of two operands with the same number of columns."""
         if a.cols != b.cols:
             raise ValueError(f"{a.cols} and {b.cols} columns")
-        m, n, k = a.rows, b.rows, a.cols
-        out = self._out(out, m, n, dtype, stream)
-        ptr, dt, ld = self._strided(out, "out")
-        B.moara_fp4_product(self.ctx, m, n, k, *a._ptrs, *b._ptrs, ptr, dt, ld, stream_handle(stream, self.device))
-        return out
+        return self._call("moara_fp4_product", a.rows, b.rows, a.cols, *a._ptrs, *b._ptrs, out=out, dtype=dtype,
+                          stream=stream)
 
     def linear(self, x, b, dtype=torch.bfloat16, out=None, stream=None):
         """x b^T with x (float32 or bfloat16) quantised by rows on the way."""
-        xp, xd, ldx = self._strided(x, "x")
-        m, k = x.shape
-        if k != b.cols:
-            raise ValueError(f"{k} and {b.cols} columns")
-        n = b.rows
-        out = self._out(out, m, n, dtype, stream)
-        ptr, dt, ld = self._strided(out, "out")
-        ws, size = self._workspace(_linear_bytes(m, n, k), stream)
-        B.moara_fp4_linear(self.ctx, m, n, k, xp, xd, ldx, *b._ptrs, ptr, dt, ld, ws.data_ptr() if size else 0, size,
-                           stream_handle(stream, self.device))
-        return out
-
-    def _workspace(self, size, stream):
-        if size == 0:
-            return None, 0
-        if stream is None:
-            return torch.empty(size, dtype=torch.uint8, device=self._dev), size
-        with allocating_on(stream, self.device):
-            return torch.empty(size, dtype=torch.uint8, device=self._dev), size
+        return self._call("moara_fp4_linear", x, b.rows, b.cols, *b._ptrs, out=out, dtype=dtype, stream=stream)
 
     def status(self, stream=None):
         """Reads and clears the device status word (0, or an error a kernel recorded)."""
