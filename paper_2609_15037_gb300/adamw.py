@@ -5,6 +5,7 @@ moara_grad_norm.  Every computation happens in the library's kernels."""
 from __future__ import annotations
 
 import contextlib
+import struct
 
 import numpy as np
 import torch
@@ -15,7 +16,8 @@ from . import binding as B
 _TYPES = {torch.float32: B.MOARA_DTYPE_F32, torch.bfloat16: B.MOARA_DTYPE_BF16}
 _STATES = {"f32": B.MOARA_DTYPE_F32, "block8": B.MOARA_DTYPE_BLOCK8}
 _DESC = np.dtype(B.moara_adamw_tensor)
-_SIZE = _DESC.itemsize
+_PACK = struct.Struct("<q7Q3iI2f")          # the same as one record
+_SIZE = _PACK.size
 _N, _GRAD, _GRAD_DTYPE = (_DESC.fields[f][1] for f in ("n", "grad", "grad_dtype"))
 
 
@@ -75,26 +77,20 @@ class AdamWGroup:
         n = self._check(param, "param").numel()
         if copy is not None:
             self._check(copy, "copy", n, (torch.bfloat16,))
-        dev = self._dev
         code = torch.uint8 if state == "block8" else torch.float32
         blocks = -(-n // B.MOARA_ADAMW_BLOCK)
 
         def kept(x, what, size, dtype):
-            return torch.zeros(size, dtype=dtype, device=dev) if x is None else self._check(x, what, size, (dtype,))
+            return torch.zeros(size, dtype=dtype, device=self._dev) if x is None else self._check(x, what, size, (dtype,))
         s = {"exp_avg": kept(exp_avg, "exp_avg", n, code), "exp_avg_sq": kept(exp_avg_sq, "exp_avg_sq", n, code)}
         if state == "block8":
             s["exp_avg_scale"] = kept(exp_avg_scale, "exp_avg_scale", blocks, torch.float32)
             s["exp_avg_sq_scale"] = kept(exp_avg_sq_scale, "exp_avg_sq_scale", blocks, torch.float32)
         i = len(self.params)
         self._grow(i + 1)
-        d = self._desc[i]
-        d["n"], d["param"] = n, param.data_ptr()
-        d["param_bf16"] = 0 if copy is None else copy.data_ptr()
-        for key, x in s.items():
-            d[key] = x.data_ptr()
-        d["param_dtype"], d["state_dtype"] = _TYPES[param.dtype], _STATES[state]
-        d["id"] = i if id is None else id
-        d["weight_decay"], d["lr_scale"] = weight_decay, lr_scale
+        at = [x.data_ptr() for x in s.values()] + [0] * (4 - len(s))
+        _PACK.pack_into(self._table, i * _SIZE, n, param.data_ptr(), 0, 0 if copy is None else copy.data_ptr(), *at,
+                        _TYPES[param.dtype], 0, _STATES[state], i if id is None else id, weight_decay, lr_scale)
         self.params.append(param)
         self.copies.append(copy)
         self.states.append(s)

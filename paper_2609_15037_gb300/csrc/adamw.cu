@@ -11,6 +11,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "launch.cuh"
 #include "ops.h"
 
 namespace moara {
@@ -434,6 +435,7 @@ template <int CAP> __global__ void __launch_bounds__(256, 4) k_adamw(const __gri
     const AdamTensor& t = b.t[q];
     const long long i0 = static_cast<long long>(c - b.start[q]) * kAdamChunk + (threadIdx.x >> 5) * MOARA_ADAMW_BLOCK;
     const long long stride = static_cast<long long>(b.start[q + 1] - b.start[q]) * kAdamChunk;
+    pdl_begin();
     if (i0 >= t.n) return;
     const float coef = b.scale != nullptr ? *b.scale : 1.0f;
     switch (t.kind & 7u) {
@@ -491,6 +493,7 @@ __global__ void __launch_bounds__(256) k_moments(const __grid_constant__ MomentB
     const MomentTensor& t = b.t[q];
     const int lane = threadIdx.x & 31;
     const long long i0 = static_cast<long long>(c - b.start[q]) * kAdamChunk + (threadIdx.x >> 5) * MOARA_ADAMW_BLOCK;
+    pdl_begin();
     if (i0 >= t.n) return;
     moment_tile<true>(t.m, t.ms, t.om, t.block8, i0, t.n, lane);
     moment_tile<false>(t.v, t.vs, t.ov, t.block8, i0, t.n, lane);
@@ -540,6 +543,7 @@ template <int CAP> __global__ void __launch_bounds__(256) k_grad_norm(const __gr
     __shared__ double red[8];
     __shared__ bool finish;
     double acc = 0.0;
+    pdl_begin();
     for (uint32_t c = blockIdx.x; c < b.chunks; c += gridDim.x) {
         const int q = find_tensor(b.count, c, [&](int i) { return b.t[i].start; });
         const NormTensor& t = b.t[q];
@@ -580,36 +584,31 @@ uint32_t adamw_key(uint64_t seed, uint32_t id, int64_t t) {
 }
 
 cudaError_t launch_adamw(const AdamBatch& b, cudaStream_t s, int64_t* launches) {
+    ++*launches;
     if (b.count <= kAdamFew) {
         AdamBatchOf<kAdamFew> f;
         static_cast<AdamCall&>(f) = b;
         for (int i = 0; i < b.count; ++i) f.t[i] = b.t[i];
         for (int i = 0; i <= b.count; ++i) f.start[i] = b.start[i];
-        k_adamw<kAdamFew><<<b.start[b.count], 256, 0, s>>>(f);
-    } else {
-        k_adamw<kAdamTensors><<<b.start[b.count], 256, 0, s>>>(b);
+        return launch(k_adamw<kAdamFew>, dim3(b.start[b.count]), dim3(256), 0, s, 1, f);
     }
-    ++*launches;
-    return cudaGetLastError();
+    return launch(k_adamw<kAdamTensors>, dim3(b.start[b.count]), dim3(256), 0, s, 1, b);
 }
 
 cudaError_t launch_moments(const MomentBatch& b, cudaStream_t s, int64_t* launches) {
-    k_moments<<<b.start[b.count], 256, 0, s>>>(b);
     ++*launches;
-    return cudaGetLastError();
+    return launch(k_moments, dim3(b.start[b.count]), dim3(256), 0, s, 1, b);
 }
 
 cudaError_t launch_grad_norm(const NormBatch& b, int ctas, cudaStream_t s, int64_t* launches) {
+    ++*launches;
     if (b.count <= kNormFew) {
         NormBatchOf<kNormFew> f;
         static_cast<NormCall&>(f) = b;
         for (int i = 0; i < b.count; ++i) f.t[i] = b.t[i];
-        k_grad_norm<kNormFew><<<ctas, 256, 0, s>>>(f);
-    } else {
-        k_grad_norm<kNormTensors><<<ctas, 256, 0, s>>>(b);
+        return launch(k_grad_norm<kNormFew>, dim3(ctas), dim3(256), 0, s, 1, f);
     }
-    ++*launches;
-    return cudaGetLastError();
+    return launch(k_grad_norm<kNormTensors>, dim3(ctas), dim3(256), 0, s, 1, b);
 }
 
 }  // namespace moara

@@ -5,6 +5,7 @@
 #include <cuda_fp16.h>
 
 #include "fp4.cuh"
+#include "launch.cuh"
 #include "ops.h"
 
 namespace moara {
@@ -35,7 +36,9 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2
     __shared__ __align__(16) uint8_t sfr[512];
     __shared__ __align__(16) uint8_t sfc[512];
     __shared__ __align__(16) uint32_t qc[COLS ? 128 * 17 : 1];       // a column's 16 words of codes, and one of padding
-    asm volatile("griddepcontrol.launch_dependents;");       // a product behind it may set itself up
+    // in this order: a product behind it that begins early finds what earlier launches
+    // wrote complete
+    asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
     const int tr = blockIdx.x / p.tiles_c, tc = blockIdx.x % p.tiles_c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wr = warp >> 1, sub = (warp & 1) * 8 + (lane & 7);     // 32-row group, 8-column group of the tile
@@ -253,10 +256,10 @@ template <class T> __global__ void __launch_bounds__(256) k_fp4_values_any(const
 template <class T>
 cudaError_t quantize_as(const QuantParams& p, cudaStream_t s) {
     const unsigned int grid = static_cast<unsigned int>(p.tiles_r) * p.tiles_c;
-    if (p.qt == nullptr) k_fp4_quantize<T, true, false><<<grid, 256, 0, s>>>(p);
-    else if (p.q == nullptr) k_fp4_quantize<T, false, true><<<grid, 256, 0, s>>>(p);
-    else k_fp4_quantize<T, true, true><<<grid, 256, 0, s>>>(p);
-    return cudaGetLastError();
+    const auto fn = p.qt == nullptr  ? k_fp4_quantize<T, true, false>
+                    : p.q == nullptr ? k_fp4_quantize<T, false, true>
+                                     : k_fp4_quantize<T, true, true>;
+    return launch(fn, dim3(grid), dim3(256), 0, s, 1, p);
 }
 
 }  // namespace
@@ -299,9 +302,8 @@ cudaError_t launch_fp4_dequantize(const void* q, const void* sf, int rows, int c
     const unsigned int grid = static_cast<unsigned int>(p.parts) * ((rows - 1) / per + 1);
     auto fn = vec ? (bf ? k_fp4_values<__nv_bfloat16> : k_fp4_values<float>)
                   : (bf ? k_fp4_values_any<__nv_bfloat16> : k_fp4_values_any<float>);
-    fn<<<grid, 256, 0, s>>>(p);
     ++*launches;
-    return cudaGetLastError();
+    return launch_if(false, fn, dim3(grid), dim3(256), 0, s, 1, p);
 }
 
 }  // namespace moara

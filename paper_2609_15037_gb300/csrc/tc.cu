@@ -2033,10 +2033,12 @@ TcState* tc_create(int device, int* d_status) {
     TcState* st = new TcState();
     st->device = device;
     st->d_status = d_status;
-    cudaDeviceProp prop{};
-    if (cudaGetDeviceProperties(&prop, device) == cudaSuccess) {
-        st->sms = prop.multiProcessorCount;
-        if (prop.major != 10 || prop.minor != 3) {   // these kernels are built for sm_103a only
+    int major = 0, minor = 0, sms = 0;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device) == cudaSuccess &&
+        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, device) == cudaSuccess &&
+        cudaDeviceGetAttribute(&minor, cudaDevAttrComputeCapabilityMinor, device) == cudaSuccess) {
+        st->sms = sms;
+        if (major != 10 || minor != 3) {   // these kernels are built for sm_103a only
             delete st;
             return nullptr;
         }
