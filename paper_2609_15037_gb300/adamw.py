@@ -5,6 +5,7 @@ moara_grad_norm.  Every computation happens in the library's kernels."""
 from __future__ import annotations
 
 import contextlib
+import ctypes
 import struct
 
 import numpy as np
@@ -18,7 +19,17 @@ _STATES = {"f32": B.MOARA_DTYPE_F32, "block8": B.MOARA_DTYPE_BLOCK8}
 _DESC = np.dtype(B.moara_adamw_tensor)
 _PACK = struct.Struct("<q7Q3iI2f")          # the same as one record
 _SIZE = _PACK.size
-_N, _GRAD, _GRAD_DTYPE = (_DESC.fields[f][1] for f in ("n", "grad", "grad_dtype"))
+
+
+def entry_address(name):
+    return ctypes.cast(getattr(B.lib, name), ctypes.c_void_p).value
+
+
+_STEP, _MOMENTS, _NORM = (entry_address("moara_" + f) for f in ("adamw_step", "adamw_moments", "grad_norm"))
+
+
+def _listed(xs):
+    return xs if isinstance(xs, (list, tuple)) else list(xs)
 
 
 def _current_stream(device):
@@ -55,7 +66,6 @@ class AdamWGroup:
         self.params, self.copies, self.states = [], [], []
         self._room = 0
         self._grow(0)
-        self._norm_room, self._norm_at = 0, [0, 0, 0]
         self._workspace = {}
 
     def _check(self, x, what, n=None, dtypes=tuple(_TYPES)):
@@ -114,30 +124,15 @@ class AdamWGroup:
         d = self._desc[list(ids)]
         return d, d.ctypes.data
 
-    def _scalar(self, x, what):
-        """Address of a one-element float32 tensor."""
-        if x.dtype is not torch.float32 or x.numel() != 1 or x.get_device() != self.device:
-            self._check(x, what, 1, (torch.float32,))
-        return x.data_ptr()
-
-    def _read(self, xs, what, addresses, types, sizes, given):
-        """Addresses, types and sizes of tensors into (or, with `given`, sizes against)
-        arrays given as (address, stride)."""
-        bad = _host.read(xs if isinstance(xs, (list, tuple)) else list(xs), self.device, *addresses, *types, *sizes, given)
-        if bad >= 0:
-            raise ValueError(f"{what} {bad}: a contiguous float32 or bfloat16 tensor on cuda:{self.device}"
-                             + (" with its tensor's number of entries" if given else "") + " is needed")
-
     def step(self, grads, t, lr, grad_scale=None, ids=None, stream=None):
         """One AdamW step at step t (1-based): grads[i] (fp32 or bf16) of every
         registered tensor, or of those in ids.  grad_scale: a one-element
         float32 device tensor that multiplies every gradient, or None."""
         d, at = self._chosen(ids)
-        if len(grads) != len(d):
-            raise ValueError(f"{len(grads)} gradients for {len(d)} tensors")
-        self._read(grads, "gradient", (at + _GRAD, _SIZE), (at + _GRAD_DTYPE, _SIZE), (at + _N, _SIZE), True)
-        scale = 0 if grad_scale is None else self._scalar(grad_scale, "grad_scale")
-        B.moara_adamw_step(self.ctx, len(d), at, self.hp, t, lr, scale, stream_handle(stream, self.device))
+        code = _host.adamw_step(_STEP, self.ctx, len(d), at, _listed(grads), ctypes.addressof(self.hp), t, lr, grad_scale,
+                                self.device, stream_handle(stream, self.device))
+        if code:
+            B._check(code, self.ctx, "moara_adamw_step")
 
     def moments(self, exp_avg=None, exp_avg_sq=None, ids=None, stream=None):
         """The moments as fp32 tensors (lists, one per tensor); into the given
@@ -149,15 +144,10 @@ class AdamWGroup:
             with allocating_on(stream, self.device):
                 exp_avg, exp_avg_sq = ([torch.empty(k, device=self._dev) for k in sizes] if x is None else x
                                        for x in (exp_avg, exp_avg_sq))
-        ptrs, types = np.zeros((2, n), np.uint64), np.zeros(n, np.int32)
-        to, kinds = ptrs.ctypes.data, types.ctypes.data
-        for k, out in enumerate((exp_avg, exp_avg_sq)):
-            if len(out) != n:
-                raise ValueError(f"{len(out)} outputs for {n} tensors")
-            self._read(out, "output", (to + 8 * n * k, 8), (kinds, 4), (at + _N, _SIZE), True)
-            if types.any():
-                raise ValueError("the moments' outputs are float32")
-        B.moara_adamw_moments(self.ctx, len(d), at, to, to + 8 * n, stream_handle(stream, self.device))
+        code = _host.adamw_moments(_MOMENTS, self.ctx, n, at, _listed(exp_avg), _listed(exp_avg_sq), self.device,
+                                   stream_handle(stream, self.device))
+        if code:
+            B._check(code, self.ctx, "moara_adamw_moments")
         return exp_avg, exp_avg_sq
 
     def _norm_workspace(self, count, handle, stream):
@@ -176,25 +166,17 @@ class AdamWGroup:
         bf16), a float32 tensor of three.  extra_sq: a one-element float32 device
         tensor added to the sum under the root, or None.  The first element is
         what MoaraGroup.set_clip_extra takes, the last what step takes."""
-        n = len(grads)
-        if n > self._norm_room:
-            self._norm_room = 2 * n
-            self._norm = np.zeros(2 * n, np.uint64), np.zeros(2 * n, np.int64), np.zeros(2 * n, np.int32)
-            self._norm_at = [x.ctypes.data for x in self._norm]
-        a, b, c = self._norm_at
-        self._read(grads, "gradient", (a, 8), (c, 4), (b, 8), False)
         handle = stream_handle(stream, self.device)
-        ws = self._norm_workspace(n, handle, stream)
-        extra = 0 if extra_sq is None else self._scalar(extra_sq, "extra_sq")
-        if out is None and stream is None:
-            out = torch.empty(3, device=self._dev)
-        elif out is None:
-            with allocating_on(stream, self.device):
-                out = torch.empty(3, device=self._dev)
+        ws = self._norm_workspace(len(grads), handle, stream)
+        args = (_NORM, self.ctx, _listed(grads), max_norm, extra_sq, out, ws.data_ptr(), ws.numel(), self.device, handle)
+        if stream is None:
+            got = _host.grad_norm(*args)
         else:
-            self._check(out, "out", 3, (torch.float32,))
-        B.moara_grad_norm(self.ctx, n, a, b, c, max_norm, extra, out.data_ptr(), ws.data_ptr(), ws.numel(), handle)
-        return out
+            with allocating_on(stream, self.device):
+                got = _host.grad_norm(*args)
+        if got.__class__ is int:
+            B._check(got, self.ctx, "moara_grad_norm")
+        return got
 
     def state_dict(self):
         return [{k: v.detach().clone() for k, v in s.items()} for s in self.states]

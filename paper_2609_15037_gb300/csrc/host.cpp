@@ -1,71 +1,137 @@
 // Python module _host: tensors as the C entries take them, where marshalling in Python
-// costs more than the kernels.  read() takes lists (five attribute calls a tensor are
-// 18 us of a step of 65 short tensors whose kernel takes 2.3); the fp4 calls take
-// the matrices of one entry, allocate its output and call it by its address.
+// costs more than the kernels (five attribute calls a tensor are 18 us of a step of 65
+// short tensors whose kernel takes 2.3).  Each call checks its tensors, allocates its
+// output where none is given, and calls the entry, whose address it is given.
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <optional>
+#include <vector>
 
 #include "moara.h"
 
 namespace {
 
-// Address of the entry for tensor i of an array (or of a field of an array of
-// structs), or null for no array.
-struct Field {
-    char* base;
-    Py_ssize_t stride;
-    template <class T> T* at(Py_ssize_t i) const { return reinterpret_cast<T*>(base + i * stride); }
+// A contiguous fp32 or bf16 tensor on cuda:`device`: its type (0 fp32, 1 bf16), or -1.
+int flat_type(const at::Tensor& t, long device) {
+    const at::ScalarType type = t.scalar_type();
+    if (t.layout() != at::kStrided || !t.is_cuda() || t.get_device() != device || !t.is_contiguous()) return -1;
+    return type == at::kFloat ? 0 : type == at::kBFloat16 ? 1 : -1;
+}
+
+// Tensors of a list or tuple, one at a time.  False with a Python error set for
+// anything else.
+struct Tensors {
+    PyObject* list;
+    Py_ssize_t n = 0;
+    explicit Tensors(PyObject* o) : list(o) {
+        if (!PyList_Check(o) && !PyTuple_Check(o)) PyErr_SetString(PyExc_TypeError, "a list or tuple of tensors is needed");
+        else n = PySequence_Fast_GET_SIZE(o);
+    }
+    // tensor i, its address and type; or null, with an error set that names `what`
+    const at::Tensor* get(Py_ssize_t i, const char* what, long device, int64_t entries, void*& at, int& type) const {
+        PyObject* o = PySequence_Fast_GET_ITEM(list, i);
+        if (THPVariable_Check(o)) {
+            const at::Tensor& t = THPVariable_Unpack(o);
+            type = flat_type(t, device);
+            if (type >= 0 && (entries < 0 || t.numel() == entries)) {
+                at = const_cast<void*>(t.const_data_ptr());
+                return &t;
+            }
+        }
+        if (entries < 0)
+            PyErr_Format(PyExc_ValueError, "%s %zd: a contiguous float32 or bfloat16 tensor on cuda:%ld is needed", what, i, device);
+        else
+            PyErr_Format(PyExc_ValueError, "%s %zd: a contiguous float32 or bfloat16 tensor of %lld entries on cuda:%ld is needed",
+                         what, i, static_cast<long long>(entries), device);
+        return nullptr;
+    }
 };
 
-// read(tensors, device, addresses, stride, types, stride, sizes, stride, given)
-//
-// For each tensor of the list or tuple: its address as uint64, its type as int32 (0
-// fp32, 1 bf16) and its number of entries as int64, into arrays given by the
-// address of their first entry and their stride in bytes.  With `given`, the
-// sizes are compared instead.  Returns the position of the first entry that is no
-// contiguous fp32 or bf16 tensor on cuda:`device` (or has another size), or -1.
-PyObject* read(PyObject*, PyObject* const* args, Py_ssize_t count) {
-    if (count != 9) {
-        PyErr_SetString(PyExc_TypeError, "read takes nine arguments");
-        return nullptr;
+bool arguments(Py_ssize_t have, Py_ssize_t want) {
+    if (have != want) PyErr_Format(PyExc_TypeError, "%zd arguments are needed", want);
+    return have == want;
+}
+
+template <class F> F entry(PyObject* o) { return reinterpret_cast<F>(PyLong_AsVoidPtr(o)); }
+
+// A float32 scalar on the device, or null for None; an error is set for anything else.
+float* scalar_of(PyObject* o, const char* what, long device) {
+    if (o == Py_None) return nullptr;
+    if (THPVariable_Check(o)) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (flat_type(t, device) == 0 && t.numel() == 1) return const_cast<float*>(t.const_data_ptr<float>());
     }
-    PyObject* list = args[0];
-    if (!PyList_Check(list) && !PyTuple_Check(list)) {
-        PyErr_SetString(PyExc_TypeError, "a list or tuple of tensors is needed");
-        return nullptr;
-    }
-    const long device = PyLong_AsLong(args[1]);
-    Field f[3];
-    for (int k = 0; k < 3; ++k) {
-        f[k].base = static_cast<char*>(PyLong_AsVoidPtr(args[2 + 2 * k]));
-        f[k].stride = PyLong_AsSsize_t(args[3 + 2 * k]);
-    }
-    const int given = PyObject_IsTrue(args[8]);
-    if (given < 0 || PyErr_Occurred()) return nullptr;
-    const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+    PyErr_Format(PyExc_ValueError, "%s: a one-element float32 tensor on cuda:%ld is needed", what, device);
+    return nullptr;
+}
+
+PyObject* caught(const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+    return nullptr;
+}
+
+// adamw_step(entry, ctx, count, descriptors, gradients, hparams, t, lr, grad_scale, device, stream)
+// -> error code.  The gradients' addresses and types go into the descriptors.
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 11)) return nullptr;
     try {
+        const auto fn = entry<decltype(&moara_adamw_step)>(a[0]);
+        const Py_ssize_t n = PyLong_AsSsize_t(a[2]);
+        auto* d = static_cast<moara_adamw_tensor*>(PyLong_AsVoidPtr(a[3]));
+        const Tensors grads(a[4]);
+        const long device = PyLong_AsLong(a[9]);
+        float* scale = scalar_of(a[8], "grad_scale", device);
+        if (PyErr_Occurred()) return nullptr;
+        if (grads.n != n) return PyErr_Format(PyExc_ValueError, "%zd gradients for %zd tensors", grads.n, n);
         for (Py_ssize_t i = 0; i < n; ++i) {
-            PyObject* o = PySequence_Fast_GET_ITEM(list, i);
-            if (!THPVariable_Check(o)) return PyLong_FromSsize_t(i);
-            const at::Tensor& t = THPVariable_Unpack(o);
-            const at::ScalarType type = t.scalar_type();
-            if (t.layout() != at::kStrided || !t.is_cuda() || t.get_device() != device || !t.is_contiguous() ||
-                (type != at::kFloat && type != at::kBFloat16))
-                return PyLong_FromSsize_t(i);
-            if (given && *f[2].at<int64_t>(i) != t.numel()) return PyLong_FromSsize_t(i);
-            *f[0].at<uint64_t>(i) = reinterpret_cast<uint64_t>(t.const_data_ptr());
-            *f[1].at<int32_t>(i) = type == at::kBFloat16;
-            if (!given) *f[2].at<int64_t>(i) = t.numel();
+            void* at;
+            if (grads.get(i, "gradient", device, d[i].n, at, d[i].grad_dtype) == nullptr) return nullptr;
+            d[i].grad = at;
         }
+        const int64_t t = PyLong_AsLongLong(a[6]);
+        const double lr = PyFloat_AsDouble(a[7]);
+        auto* hp = static_cast<moara_adamw_hparams*>(PyLong_AsVoidPtr(a[5]));
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        void* stream = PyLong_AsVoidPtr(a[10]);
+        if (PyErr_Occurred()) return nullptr;
+        return PyLong_FromLong(fn(ctx, static_cast<int>(n), d, hp, t, static_cast<float>(lr), scale, stream));
     } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
+        return caught(e);
     }
-    return PyLong_FromLong(-1);
+}
+
+// adamw_moments(entry, ctx, count, descriptors, exp_avg, exp_avg_sq, device, stream) -> error code
+PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 8)) return nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_adamw_moments)>(a[0]);
+        const Py_ssize_t n = PyLong_AsSsize_t(a[2]);
+        auto* d = static_cast<moara_adamw_tensor*>(PyLong_AsVoidPtr(a[3]));
+        const Tensors outs[2] = {Tensors(a[4]), Tensors(a[5])};
+        const long device = PyLong_AsLong(a[6]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        void* stream = PyLong_AsVoidPtr(a[7]);
+        if (PyErr_Occurred()) return nullptr;
+        std::vector<float*> to[2];
+        for (int k = 0; k < 2; ++k) {
+            if (outs[k].n != n) return PyErr_Format(PyExc_ValueError, "%zd outputs for %zd tensors", outs[k].n, n);
+            to[k].resize(n);
+            for (Py_ssize_t i = 0; i < n; ++i) {
+                void* at;
+                int type;
+                if (outs[k].get(i, "output", device, d[i].n, at, type) == nullptr) return nullptr;
+                if (type != 0) return PyErr_Format(PyExc_ValueError, "output %zd: the moments are float32", i);
+                to[k][i] = static_cast<float*>(at);
+            }
+        }
+        return PyLong_FromLong(fn(ctx, static_cast<int>(n), d, to[0].data(), to[1].data(), stream));
+    } catch (const std::exception& e) {
+        return caught(e);
+    }
 }
 
 // A matrix whose rows are contiguous.
@@ -109,8 +175,6 @@ const char* output_of(PyObject* o, int64_t rows, int64_t cols, int dtype, long d
     return wrong;
 }
 
-template <class F> F entry(PyObject* o) { return reinterpret_cast<F>(PyLong_AsVoidPtr(o)); }
-
 // The result of an entry: the tensor, or its error code.
 PyObject* finish(PyObject* held, const char* wrong, int code) {
     if (wrong != nullptr || PyErr_Occurred()) {
@@ -123,9 +187,50 @@ PyObject* finish(PyObject* held, const char* wrong, int code) {
     return PyLong_FromLong(code);
 }
 
-bool arguments(Py_ssize_t have, Py_ssize_t want) {
-    if (have != want) PyErr_Format(PyExc_TypeError, "%zd arguments are needed", want);
-    return have == want;
+// grad_norm(entry, ctx, gradients, max_norm, extra_sq, out, workspace, bytes, device, stream)
+// -> the three floats (a new tensor for out = None), or an error code
+PyObject* grad_norm(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 10)) return nullptr;
+    PyObject* held = nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_grad_norm)>(a[0]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        const Tensors grads(a[2]);
+        const double max_norm = PyFloat_AsDouble(a[3]);
+        const long device = PyLong_AsLong(a[8]);
+        float* extra = scalar_of(a[4], "extra_sq", device);
+        void* ws = PyLong_AsVoidPtr(a[6]);
+        const size_t size = PyLong_AsSize_t(a[7]);
+        void* stream = PyLong_AsVoidPtr(a[9]);
+        if (PyErr_Occurred()) return nullptr;
+        const Py_ssize_t n = grads.n;
+        std::vector<const void*> p(n);
+        std::vector<int64_t> sizes(n);
+        std::vector<int> types(n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            void* at;
+            const at::Tensor* t = grads.get(i, "gradient", device, -1, at, types[i]);
+            if (t == nullptr) return nullptr;
+            p[i] = at;
+            sizes[i] = t->numel();
+        }
+        at::Tensor out;
+        if (a[5] == Py_None) {
+            out = at::empty({3}, at::TensorOptions().dtype(at::kFloat).device(at::kCUDA, static_cast<at::DeviceIndex>(device)));
+            held = THPVariable_Wrap(out);
+        } else {
+            if (!THPVariable_Check(a[5]) || flat_type(THPVariable_Unpack(a[5]), device) != 0 || THPVariable_Unpack(a[5]).numel() != 3)
+                return PyErr_Format(PyExc_ValueError, "out: a contiguous float32 tensor of three on cuda:%ld is needed", device);
+            held = a[5];
+            Py_INCREF(held);
+            out = THPVariable_Unpack(held);
+        }
+        return finish(held, nullptr, fn(ctx, static_cast<int>(n), p.data(), sizes.data(), types.data(), static_cast<float>(max_norm),
+                                        extra, out.data_ptr<float>(), ws, size, stream));
+    } catch (const std::exception& e) {
+        Py_XDECREF(held);
+        return caught(e);
+    }
 }
 
 // fp4_product(entry, ctx, m, n, k, a_q, a_sf, b_q, b_sf, out, bf16, device, stream)
@@ -143,8 +248,7 @@ PyObject* fp4_product(PyObject*, PyObject* const* a, Py_ssize_t count) {
         return finish(held, wrong, code);
     } catch (const std::exception& e) {
         Py_XDECREF(held);
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
+        return caught(e);
     }
 }
 
@@ -173,8 +277,7 @@ PyObject* fp4_linear(PyObject*, PyObject* const* a, Py_ssize_t count) {
         return finish(held, wrong, code);
     } catch (const std::exception& e) {
         Py_XDECREF(held);
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
+        return caught(e);
     }
 }
 
@@ -193,8 +296,54 @@ PyObject* fp4_dequantize(PyObject*, PyObject* const* a, Py_ssize_t count) {
         return finish(held, wrong, code);
     } catch (const std::exception& e) {
         Py_XDECREF(held);
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
+        return caught(e);
+    }
+}
+
+// A buffer for an operand, the codes and from the next 256 bytes on the scales.
+struct Operand {
+    at::Tensor both;
+    char* q;
+    char* sf;
+    Operand(int64_t rows, int64_t cols, long device) {
+        size_t nq = rows * ((cols + 31) / 32) * 16, ns = ((rows + 127) / 128) * ((cols + 127) / 128) * 512;
+        const size_t start = (nq + 255) / 256 * 256;
+        both = at::empty({static_cast<int64_t>(start + ns)},
+                         at::TensorOptions().dtype(at::kByte).device(at::kCUDA, static_cast<at::DeviceIndex>(device)));
+        q = static_cast<char*>(both.data_ptr());
+        sf = q + start;
+    }
+    // (buffer, address of the codes, address of the scales)
+    PyObject* tuple() const {
+        return Py_BuildValue("(NKK)", THPVariable_Wrap(both), reinterpret_cast<unsigned long long>(q),
+                             reinterpret_cast<unsigned long long>(sf));
+    }
+};
+
+// fp4_quantize(entry, ctx, x, rows, cols, device, stream): quantises into new buffers, by
+// rows and by columns as asked -> ((buffer, q, sf) or None, the same, rows, columns), or
+// an error code.  Zero rows or columns are refused by the entry itself.
+PyObject* fp4_quantize(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 7)) return nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_fp4_quantize)>(a[0]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        const int rows = PyObject_IsTrue(a[3]), cols = PyObject_IsTrue(a[4]);
+        const long device = PyLong_AsLong(a[5]);
+        void* stream = PyLong_AsVoidPtr(a[6]);
+        Matrix x{};
+        const char* wrong = matrix_of(a[2], device, x);
+        if (wrong != nullptr || PyErr_Occurred()) return finish(nullptr, wrong, 0);
+        std::optional<Operand> r, c;
+        if (rows) r.emplace(x.rows, x.cols, device);
+        if (cols) c.emplace(x.cols, x.rows, device);
+        const int code = fn(ctx, x.p, x.dtype, x.rows, x.cols, x.ld, rows ? r->q : nullptr, rows ? r->sf : nullptr,
+                            cols ? c->q : nullptr, cols ? c->sf : nullptr, stream);
+        if (code != MOARA_OK) return PyLong_FromLong(code);
+        PyObject* none = Py_None;
+        return Py_BuildValue("(NNii)", rows ? r->tuple() : Py_NewRef(none), cols ? c->tuple() : Py_NewRef(none), x.rows, x.cols);
+    } catch (const std::exception& e) {
+        return caught(e);
     }
 }
 
@@ -206,8 +355,7 @@ PyObject* matrix(PyObject*, PyObject* const* a, Py_ssize_t count) {
         const char* wrong = matrix_of(a[0], PyLong_AsLong(a[1]), m);
         if (wrong != nullptr || PyErr_Occurred()) return finish(nullptr, wrong, 0);
     } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
+        return caught(e);
     }
     return Py_BuildValue("(KiiiL)", reinterpret_cast<unsigned long long>(m.p), m.dtype, m.rows, m.cols,
                          static_cast<long long>(m.ld));
@@ -224,15 +372,17 @@ PyObject* bytes(PyObject*, PyObject* const* a, Py_ssize_t count) {
         const unsigned long long at = reinterpret_cast<unsigned long long>(t.data_ptr());
         return Py_BuildValue("(NK)", THPVariable_Wrap(t), at);
     } catch (const std::exception& e) {
-        PyErr_SetString(PyExc_RuntimeError, e.what());
-        return nullptr;
+        return caught(e);
     }
 }
 
 #define MOARA_METHOD(name, doc) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, doc}
 
 PyMethodDef methods[] = {
-    MOARA_METHOD(read, "read(tensors, device, addresses, stride, types, stride, sizes, stride, given) -> first misfit, or -1"),
+    MOARA_METHOD(adamw_step, "moara_adamw_step with a list of gradients -> error code"),
+    MOARA_METHOD(adamw_moments, "moara_adamw_moments into two lists of tensors -> error code"),
+    MOARA_METHOD(grad_norm, "moara_grad_norm of a list of gradients -> tensor of three, or an error code"),
+    MOARA_METHOD(fp4_quantize, "moara_fp4_quantize into new operands -> their buffers, or an error code"),
     MOARA_METHOD(fp4_product, "moara_fp4_product into a matrix or a new one -> the matrix, or an error code"),
     MOARA_METHOD(fp4_linear, "moara_fp4_linear into a matrix or a new one -> the matrix, or an error code"),
     MOARA_METHOD(fp4_dequantize, "moara_fp4_dequantize into a matrix or a new one -> the matrix, or an error code"),

@@ -4,23 +4,18 @@ moara_fp4_linear.  Every computation happens in the library's kernels."""
 
 from __future__ import annotations
 
-import ctypes
-
 import torch
 
 from . import _host
 from . import binding as B
-from .adamw import _TYPES, allocating_on, stream_handle
+from .adamw import _TYPES, allocating_on, entry_address, stream_handle
 
 
-def _address(name):
-    return ctypes.cast(getattr(B.lib, name), ctypes.c_void_p).value
-
-
+_QUANTIZE = entry_address("moara_fp4_quantize")
 _ENTRIES = {
-    "moara_fp4_dequantize": (_host.fp4_dequantize, _address("moara_fp4_dequantize")),
-    "moara_fp4_product": (_host.fp4_product, _address("moara_fp4_product")),
-    "moara_fp4_linear": (_host.fp4_linear, _address("moara_fp4_linear"), _address("moara_fp4_linear_workspace_bytes")),
+    "moara_fp4_dequantize": (_host.fp4_dequantize, entry_address("moara_fp4_dequantize")),
+    "moara_fp4_product": (_host.fp4_product, entry_address("moara_fp4_product")),
+    "moara_fp4_linear": (_host.fp4_linear, entry_address("moara_fp4_linear"), entry_address("moara_fp4_linear_workspace_bytes")),
 }
 
 
@@ -49,6 +44,17 @@ class Fp4Matrix:
                 raise ValueError(f"q and sf, contiguous uint8 tensors of {sizes} bytes on cuda:{device}, or neither are needed")
         self._q, self._sf = q, sf
         self._ptrs = q.data_ptr(), sf.data_ptr()
+
+    @classmethod
+    def _of(cls, buffer, rows, cols):
+        """The operand in a buffer of the native module: (tensor, address of q, of sf)."""
+        self = cls.__new__(cls)
+        self.rows, self.cols = rows, cols
+        self._both, q, sf = buffer
+        self._ptrs = q, sf
+        self._start = sf - q
+        self._sizes = rows * ((cols + 31) // 32) * 16, 0
+        return self
 
     @property
     def q(self):
@@ -109,6 +115,14 @@ class Fp4Group:
         read of x; into out and out_cols where they are given."""
         if not rows and not cols:
             raise ValueError("rows, cols or both")
+        if out is None and out_cols is None and stream is None:
+            got = _host.fp4_quantize(_QUANTIZE, self.ctx, x, rows, cols, self.device, stream_handle(None, self.device))
+            if got.__class__ is int:
+                B._check(got, self.ctx, "moara_fp4_quantize")
+            r, c, m, k = got
+            a = Fp4Matrix._of(r, m, k) if rows else None
+            b = Fp4Matrix._of(c, k, m) if cols else None
+            return (a, b) if rows and cols else a if rows else b
         ptr, dtype, m, k, ld = _host.matrix(x, self.device)
         a = self._matrix(out, m, k, stream) if rows else None
         b = self._matrix(out_cols, k, m, stream) if cols else None
