@@ -53,7 +53,7 @@ def check_moment8(codes, scales, ref, signed, bits):
         code = code & 127
         low = np.zeros_like(code)
     else:
-        low = (ref > 0).astype(np.int64)
+        low = (ref > 2.0 ** -150).astype(np.int64)              # what rounds to an fp32 above zero
     floor = np.clip(np.floor(want).astype(np.int64), low, 127 if signed else 255)
     near = np.abs(want - np.round(want)) < 2.0 ** -12
     assert np.array_equal(code[~near], floor[~near])
@@ -367,4 +367,102 @@ def test_refusals(M):
     assert M.moara_launch_count(opt.ctx) == before
     torch.cuda.synchronize()
     assert torch.equal(p, torch.ones(100, device="cuda"))
+    opt.close()
+
+
+def check_last(opt, i, p0, g, m0, v0, first, t, eps=EPS, wd=0.0, ident=None):
+    """The entries from `first` (a multiple of 256) of tensor i on, from their values before the step."""
+    st, n = opt.states[i], len(g)
+    s = slice(first // 256, first // 256 + -(-n // 256))
+    bits = o.random_bits(n, opt.hp.seed, i if ident is None else ident, t, first=first)
+    rp, rm, rv = o.adamw(p0, g, m0, v0, t, LR, B1, B2, eps, wd)
+    check_moment8(st["exp_avg"][first:first + n].cpu().numpy(), f64(st["exp_avg_scale"][s]), rm, True, bits & 0xFFFF)
+    check_moment8(st["exp_avg_sq"][first:first + n].cpu().numpy(), f64(st["exp_avg_sq_scale"][s]), rv, False, bits >> 16)
+    got = f64(opt.params[i][first:first + n])
+    den = np.sqrt(rv / (1 - B2 ** t)) + eps
+    slack = 4 * U * (np.abs(B1 * m0) + np.abs((1 - B1) * g)) / (1 - B1 ** t) / den * LR
+    bf = 2.0 ** -8 if opt.params[i].dtype == torch.bfloat16 else 0.0
+    assert np.all(np.abs(got - rp) <= 3 * U * np.abs(p0) + 16 * U * np.abs(rp - p0) + slack + bf * np.abs(rp))
+
+
+@pytest.mark.parametrize("param,grad", [("bf16", "bf16"), ("f32", "f32")])
+def test_long_calls(M, param, grad):
+    """A call with so many entries that a CTA takes several pieces of a tensor: the
+    ends of a long tensor that no block divides, and the short ones beside it."""
+    rng = np.random.default_rng(8)
+    sizes = [300, 152 * 8 * 16384 + 2048 * 7 + 1003, 5000, 256]
+    opt = M.AdamWGroup(0.9, 0.999, EPS, SEED)
+    ps = [torch.randn(n, device="cuda").to(DT[param]) for n in sizes]
+    for p in ps:
+        opt.add(p, state="block8")
+    gs = [torch.randn(n, device="cuda").to(DT[grad]) for n in sizes]
+    opt.step(gs, 1, LR)
+    gs = [torch.randn(n, device="cuda").to(DT[grad]) for n in sizes]
+    m, v = opt.moments()
+    before = [p.clone() for p in ps]
+    opt.step(gs, 2, LR)
+    for i, n in enumerate(sizes):
+        for first in {0, n // 2 // 256 * 256, max(0, (n - 700) // 256 * 256)}:
+            part = slice(first, min(n, first + 3 * 256 + 19))
+            if part.stop < n:
+                part = slice(first, first + 3 * 256)
+            check_last(opt, i, f64(before[i][part]), f64(gs[i][part]), f64(m[i][part]), f64(v[i][part]), first, 2)
+    opt.close()
+
+
+def test_offsets_behind_32_bits(M):
+    """A tensor of more than 2^32 entries: its last ones, and the norm of its gradient."""
+    n = (1 << 32) + 1000
+    opt = M.AdamWGroup(0.9, 0.999, EPS, SEED)
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    tail = torch.randn(1000, device="cuda").bfloat16()
+    p[-1000:], g[-1000:] = 1.0, tail
+    opt.add(p, state="block8", id=3)
+    opt.step([g], 5, LR)
+    zero = np.zeros(1000)
+    check_last(opt, 0, zero + 1.0, f64(tail), zero, zero, 1 << 32, 5, ident=3)
+    assert not p[:-1000].any() and not opt.states[0]["exp_avg"][:1 << 32].any()
+    want = (f64(tail) ** 2).sum()
+    assert abs(opt.grad_norm([g])[0].item() / want - 1) <= 33 * U
+    m, _ = opt.moments()
+    assert (m[0][-1000:] != 0).any() and not m[0][:-1000].any()
+    opt.close()
+
+
+@pytest.mark.parametrize("size", [1e-28, 1e-6, 3e4, 1e8, 1e16])
+@pytest.mark.parametrize("eps", [1e-8, 1e-12])
+def test_scales_of_moments(M, size, eps):
+    """Gradients from those whose moments are stored as zero to those whose code factors
+    leave fp32's normal numbers, with the exact and the quick form of the update."""
+    rng = np.random.default_rng(9)
+    opt = M.AdamWGroup(0.9, 0.999, eps, SEED)
+    p, g = make(rng, 1500, "f32", 1.0), make(rng, 1500, "f32", size)
+    before = f64(p)
+    opt.add(p, state="block8")
+    opt.step([g], 3, LR)
+    zero = np.zeros(1500)
+    check_last(opt, 0, before, f64(g), zero, zero, 0, 3, eps=eps)
+    opt.close()
+
+
+def test_moments_of_many_tensors(M):
+    """More tensors than one launch takes, into given outputs and into new ones."""
+    rng = np.random.default_rng(10)
+    sizes = [int(x) for x in rng.integers(0, 600, 1100)]
+    opt = M.AdamWGroup(seed=2)
+    for i, n in enumerate(sizes):
+        opt.add(torch.zeros(n, device="cuda"), state="block8" if i % 2 else "f32")
+    opt.step([make(rng, n, "f32", 1.0) for n in sizes], 1, LR)
+    m, v = opt.moments()
+    out = [[torch.full((n,), 7.0, device="cuda") for n in sizes] for _ in range(2)]
+    opt.moments(*out)
+    for i, n in enumerate(sizes):
+        st = opt.states[i]
+        if i % 2:
+            want = o.decode8(st["exp_avg"].cpu().numpy(), f64(st["exp_avg_scale"]), True)
+            assert np.allclose(f64(m[i]), want, rtol=2 * U, atol=1e-38)
+        else:
+            assert torch.equal(m[i], st["exp_avg"]) and torch.equal(v[i], st["exp_avg_sq"])
+        assert torch.equal(out[0][i], m[i]) and torch.equal(out[1][i], v[i])
     opt.close()

@@ -320,3 +320,59 @@ def test_refusals(M, fp4):
     assert L(64, 64, 96, X, 0, 95, q, sf, d, 0, 64, *ws) == M.MOARA_ERR_SHAPE
     assert L(64, 64, 96, X, 0, 96, q, sf, d, 0, 64, ws[0] + 8, ws[1] - 8) == M.MOARA_ERR_ALIGN
     assert M.moara_launch_count(fp4.ctx) == before
+
+
+PAIRS = [(1300, 2501, 200), (2047, 1281, 1), (2560, 1026, 4097), (300, 9732, 520), (8300, 300, 96), (257, 9729, 33),
+         (2000, 5003, 31), (4000, 1540, 260)]
+
+
+@pytest.mark.parametrize("shape", PAIRS)
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_large_product(M, fp4, shape, dtype):
+    """Shapes of the 2-CTA pairs, with rows of the output on every alignment; the
+    reference on the device, whose fp64 products and sums it takes."""
+    m, n, k = shape
+    rng = np.random.default_rng(m + n)
+    x, w = matrix(rng, m, k, "bf16"), matrix(rng, n, k, "f32")
+    A, W = fp4.quantize(x), fp4.quantize(w)
+    a, b = (fp4.dequantize(y, dtype=torch.float32).double() for y in (A, W))
+    ref, size = a @ b.t(), a.abs() @ b.abs().t()
+    bound = (k / 64 + 8) * 2.0 ** -23 * size + 1e-42
+    if dtype == "bf16":
+        bound = bound * 1.01 + 2.0 ** -8 * ref.abs() + 1e-40
+    got = fp4.product(A, W, dtype=DT[dtype])
+    assert ((got.double() - ref).abs() <= bound).all()
+    for pitch, offset in ((1, 0), (2, 0), (3, 1), (4, 2), (8, 0)):
+        buf = torch.full((m * (n + pitch) + offset,), 7.0, dtype=DT[dtype], device="cuda")
+        out = buf[offset:].view(m, n + pitch)
+        fp4.product(A, W, out=out[:, :n])
+        assert torch.equal(out[:, :n], got) and (out[:, n:] == 7).all() and (buf[:offset] == 7).all()
+    assert torch.equal(fp4.linear(x, W, dtype=DT[dtype]), got)
+
+
+@pytest.mark.parametrize("m", [1, 5, 16, 17])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("pitch,offset", [(3, 0), (8, 1), (8, 0)])
+def test_linear_reads_strided_rows(M, fp4, m, dtype, pitch, offset):
+    """x as a slice of wider rows, whose surroundings are NaN."""
+    rng = np.random.default_rng(m)
+    n, k = 200, 1003
+    x, W = matrix(rng, m, k, dtype, pitch, offset), fp4.quantize(matrix(rng, n, k, "f32"))
+    assert torch.equal(fp4.linear(x, W), fp4.product(fp4.quantize(x), W))
+
+
+@pytest.mark.parametrize("shape", [(33, 700), (1, 70), (130, 1025)])
+def test_values_on_any_boundary(M, fp4, shape):
+    """Values into rows of every alignment, in both types."""
+    rng = np.random.default_rng(5)
+    x = matrix(rng, *shape, "f32")
+    A = fp4.quantize(x)
+    want = o.operand(f64(x))[2]
+    m, k = shape
+    for dtype in ("f32", "bf16"):
+        for pitch, offset in ((0, 0), (1, 0), (1, 1), (2, 1), (4, 0), (5, 3)):
+            buf = torch.full((m * (k + pitch) + offset,), 7.0, dtype=DT[dtype], device="cuda")
+            out = buf[offset:].view(m, k + pitch)
+            fp4.dequantize(A, out=out[:, :k])
+            same(f64(out)[:, :k], want)
+            assert (out[:, k:] == 7).all() and (buf[:offset] == 7).all()
