@@ -64,12 +64,11 @@ class AdamWGroup:
         self.ctx = B.moara_create(B.moara_default_hparams(), device)
         self._dev = torch.device("cuda", device)
         self.params, self.copies, self.states = [], [], []
-        self._room = 0
-        self._grow(0)
+        self._table, self._room, self._all = np.zeros(0, _DESC), 0, None
         self._workspace = {}
 
     def _check(self, x, what, n=None, dtypes=tuple(_TYPES)):
-        if x.dtype not in dtypes or not x.is_contiguous() or x.device.type != "cuda" or x.device.index != self.device:
+        if x.dtype not in dtypes or x.get_device() != self.device or not x.is_contiguous():
             raise ValueError(f"{what}: a contiguous tensor of {dtypes} on cuda:{self.device} is needed")
         if n is not None and x.numel() != n:
             raise ValueError(f"{what}: {x.numel()} entries, expected {n}")
@@ -107,21 +106,20 @@ class AdamWGroup:
         return i
 
     def _grow(self, count):
-        """Room for `count` descriptors; they and their address are kept."""
+        """Room for `count` descriptors."""
         if count > self._room:
             grown = np.zeros(max(16, 2 * count), _DESC)
             grown[:self._room] = self._table[:self._room]
             self._table, self._room = grown, len(grown)
-        elif count == 0:
-            self._table = np.zeros(0, _DESC)
-        self._desc = self._table[:count]
-        self._all = self._desc, self._table.ctypes.data
+        self._all = None
 
     def _chosen(self, ids):
         """The descriptors of a call, and their address."""
+        if self._all is None:                       # they and their address are kept
+            self._all = self._table[:len(self.params)], self._table.ctypes.data
         if ids is None:
             return self._all
-        d = self._desc[list(ids)]
+        d = self._all[0][list(ids)]
         return d, d.ctypes.data
 
     def step(self, grads, t, lr, grad_scale=None, ids=None, stream=None):

@@ -340,7 +340,7 @@ def test_refusals(M):
     assert code(lambda: opt.step([g], 1, float("nan"))) == M.MOARA_ERR_INVALID_ARG
 
     def edited(**kw):
-        d = opt._desc[:1].copy()
+        d = opt._chosen([0])[0]
         d["grad"], d["grad_dtype"] = g.data_ptr(), 0
         for k, v in kw.items():
             d[k] = v
