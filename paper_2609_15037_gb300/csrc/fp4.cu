@@ -25,14 +25,41 @@ struct QuantParams {
 };
 
 // One CTA takes a 128 x 128 tile, which is one 512-byte scale tile of either
-// orientation, and each warp 32 rows x 64 columns of it: a lane holds 8 rows x 8
-// columns in registers, so that a row's block of 32 columns is four lanes, a
-// column's block of 32 rows the four lanes 8 apart, and eight codes of either are one
-// word of one lane.  The matrix passes through no shared memory (32 x 1 blocks of a
-// 64 KB tile there took 67 us where this takes 42 on 11008 x 4096 fp32); only the
-// columns' codes do, to leave in whole 64-byte lines.
+// orientation.  A lane holds 8 rows x 16 bytes of columns (8 of bf16, 4 of fp32) in
+// registers and a warp 32 rows x 8 lanes of them, so that a row's block of 32 columns is
+// four or eight lanes, a column's block of 32 rows the four lanes 8 apart, and a
+// lane's codes of either are one word, or half of one.  The matrix passes through no
+// shared memory (32 x 1 blocks of a 64 KB tile there took 67 us on 11008 x 4096 fp32, where
+// this takes 38: 5.9 TB/s); only the columns' codes do, to leave in whole 64-byte
+// lines.  Every lane working out every scale of its rows and columns took 45 us.
+template <class T> struct Quant {
+    static constexpr int N = 16 / sizeof(T);                         // columns of a lane
+    static constexpr int ACROSS = 128 / (8 * N);                     // warps across a tile
+    static constexpr int THREADS = 4 * ACROSS * 32;
+    static constexpr int BLOCK = 32 / N;                             // lanes of a row's block
+};
+
+// The maxima of V values over L lanes STEP apart, each in one lane: lane j of them (j
+// counted in steps) is left with values j * V / L .. in t[0 .. V / L - 1].  Half of the
+// values change lanes in each round, so a lane works out V / L scales, not V.
+template <int V, int L, int STEP> __device__ __forceinline__ void scatter_max(uint32_t (&t)[V], int lane) {
+    int have = V;
+#pragma unroll
+    for (int o = L / 2; o > 0; o /= 2) {
+        const bool upper = (lane & (o * STEP)) != 0;
+        have /= 2;
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            if (i >= have) break;
+            const uint32_t keep = upper ? t[i + have] : t[i], send = upper ? t[i] : t[i + have];
+            t[i] = max(keep, __shfl_xor_sync(0xffffffffu, send, o * STEP));
+        }
+    }
+}
+
 template <class T, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(256, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2) k_fp4_quantize(const QuantParams p) {
+__global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2) k_fp4_quantize(const QuantParams p) {
+    constexpr int N = Quant<T>::N, BLOCK = Quant<T>::BLOCK, THREADS = Quant<T>::THREADS;
     __shared__ __align__(16) uint8_t sfr[512];
     __shared__ __align__(16) uint8_t sfc[512];
     __shared__ __align__(16) uint32_t qc[COLS ? 128 * 17 : 1];       // a column's 16 words of codes, and one of padding
@@ -41,12 +68,12 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2
     asm volatile("griddepcontrol.wait;\n\tgriddepcontrol.launch_dependents;" ::: "memory");
     const int tr = blockIdx.x / p.tiles_c, tc = blockIdx.x % p.tiles_c;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int wr = warp >> 1, sub = (warp & 1) * 8 + (lane & 7);     // 32-row group, 8-column group of the tile
-    const int lr = wr * 32 + (lane >> 3) * 8, lc = sub * 8;          // the lane's 8 x 8 entries inside the tile
+    const int wr = warp / Quant<T>::ACROSS, sub = warp % Quant<T>::ACROSS * 8 + (lane & 7);     // row group, column group
+    const int lr = wr * 32 + (lane >> 3) * 8, lc = sub * N;          // the lane's entries inside the tile
     const int row0 = tr * 128 + lr, col0 = tc * 128 + lc;
     const T* X = static_cast<const T*>(p.X) + row0 * p.ld + col0;
-    Row8<T> x[8];
-    if (p.vec && col0 + 8 <= p.cols && row0 + 8 <= p.rows) {
+    Row<T, N> x[8];
+    if (p.vec && col0 + N <= p.cols && row0 + 8 <= p.rows) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i].load(X + i * p.ld);
     } else {
@@ -55,37 +82,61 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2
     }
     if (ROWS) {
         const int block = (tc * 128 + lc) >> 5;
+        constexpr int OWN = 8 / BLOCK;                               // rows whose scale this lane works out
+        uint32_t half = 0, tops[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) tops[i] = x[i].top();
+        scatter_max<8, BLOCK, 1>(tops, lane);
+        float factor[OWN];
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            const int r = lane % BLOCK * OWN + i;
+            const uint32_t byte = row0 + r < p.rows && block < p.kb ? scale_byte(tops[i]) : 127u;
+            sfr[((lr + r) & 31) * 16 + wr * 4 + lc / 32] = static_cast<uint8_t>(byte);
+            factor[i] = inv_scale(byte);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            float v[8];
+            float v[N];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = x[i].get(e);
-            uint32_t top = x[i].top();
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const bool real = row0 + i < p.rows && block < p.kb;
-            const uint32_t byte = real ? scale_byte(top) : 127u;
-            if ((lane & 3) == 0) sfr[((lr + i) & 31) * 16 + wr * 4 + (sub >> 2)] = static_cast<uint8_t>(byte);
-            if (real)
-                *reinterpret_cast<uint32_t*>(p.q + (static_cast<long long>(row0 + i) * p.kb + block) * 16 + (lane & 3) * 4) =
-                    codes8(v, inv_scale(byte));
+            for (int e = 0; e < N; ++e) v[e] = x[i].get(e);
+            const float f = __shfl_sync(0xffffffffu, factor[i % OWN], i / OWN, BLOCK);
+            uint8_t* q = p.q + static_cast<long long>(row0 + i) * p.kb * 16 + block * 16;
+            if constexpr (N == 8) {
+                if (block < p.kb && row0 + i < p.rows) *reinterpret_cast<uint32_t*>(q + lane % 4 * 4) = codes8(v, f);
+            } else if (i % 2 == 0) {
+                half = codes4(v, f);
+            } else {
+                // two lanes hold a word of two rows: each takes one row's
+                const uint32_t low = half & 0xFFFFu, high = codes4(v, f) & 0xFFFFu, odd = lane & 1;
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, odd ? low : high, 1);
+                if (block < p.kb && row0 + i - 1 + static_cast<int>(odd) < p.rows)
+                    *reinterpret_cast<uint32_t*>(q - (odd ? 0 : static_cast<long long>(p.kb) * 16) + lane % 8 / 2 * 4) =
+                        odd ? other | high << 16 : low | other << 16;
+            }
         }
     }
     if (COLS) {
         const bool rows_real = tr * 4 + wr < p.kbt;
-        uint32_t tops[8];
-        Row8<T>::tops(x, tops);
+        uint32_t tops[N];
+        Row<T, N>::tops(x, tops);
+        scatter_max<N, 4, 8>(tops, lane);
+        constexpr int OWN = N / 4;                                   // columns whose scale this lane works out
+        float factor[OWN];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int i = 0; i < OWN; ++i) {
+            const int c = lc + (lane >> 3) * OWN + i;
+            const uint32_t byte = rows_real && tc * 128 + c < p.cols ? scale_byte(tops[i]) : 127u;
+            sfc[(c & 31) * 16 + (c >> 5) * 4 + wr] = static_cast<uint8_t>(byte);
+            factor[i] = inv_scale(byte);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = x[i].get(e);
-            uint32_t top = tops[e];
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 8));
-            top = max(top, __shfl_xor_sync(0xffffffffu, top, 16));
-            const uint32_t byte = rows_real && col0 + e < p.cols ? scale_byte(top) : 127u;
-            if (lane < 8) sfc[((lc + e) & 31) * 16 + ((lc + e) >> 5) * 4 + wr] = static_cast<uint8_t>(byte);
-            qc[(lc + e) * 17 + wr * 4 + (lane >> 3)] = codes8(v, inv_scale(byte));
+            const float f = __shfl_sync(0xffffffffu, factor[e % OWN], (lane & 7) | e / OWN * 8);
+            qc[(lc + e) * 17 + wr * 4 + (lane >> 3)] = codes8(v, f);
         }
     }
     __syncthreads();
@@ -93,14 +144,14 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2
         p.sf[(static_cast<long long>(tr) * p.tiles_c + tc) * 128 + threadIdx.x] =
             reinterpret_cast<const uint32_t*>(sfr)[threadIdx.x];
     if (COLS) {
-        if (threadIdx.x >= 128)
+        if (threadIdx.x >= 128 && threadIdx.x < 256)
             p.sft[(static_cast<long long>(tc) * p.tiles_r + tr) * 128 + threadIdx.x - 128] =
                 reinterpret_cast<const uint32_t*>(sfc)[threadIdx.x - 128];
         // four lanes a column, 16 bytes (one block) each
         const int cols = min(128, p.cols - tc * 128), block = tr * 4 + (threadIdx.x & 3);
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int c = u * 64 + (threadIdx.x >> 2);
+        for (int u = 0; u < 512 / THREADS; ++u) {
+            const int c = u * (THREADS / 4) + (threadIdx.x >> 2);
             const uint32_t* w = qc + c * 17 + (threadIdx.x & 3) * 4;
             if (c < cols && block < p.kbt)
                 *reinterpret_cast<uint4*>(p.qt + (static_cast<long long>(tc * 128 + c) * p.kbt + block) * 16) =
@@ -261,7 +312,7 @@ cudaError_t quantize_as(const QuantParams& p, cudaStream_t s) {
     const auto fn = p.qt == nullptr  ? k_fp4_quantize<T, true, false>
                     : p.q == nullptr ? k_fp4_quantize<T, false, true>
                                      : k_fp4_quantize<T, true, true>;
-    return launch(fn, dim3(grid), dim3(256), 0, s, 1, p);
+    return launch(fn, dim3(grid), dim3(Quant<T>::THREADS), 0, s, 1, p);
 }
 
 }  // namespace

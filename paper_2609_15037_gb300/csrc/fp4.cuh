@@ -1,5 +1,5 @@
-// Rounding to MXFP4 in registers: a block's scale, eight codes, and eight entries of
-// a row in fp32 or bf16.
+// Rounding to MXFP4 in registers: a block's scale, codes, and entries of a row in
+// fp32 or bf16.
 #pragma once
 
 #include <cuda_bf16.h>
@@ -37,7 +37,19 @@ __device__ __forceinline__ uint32_t codes8(const float (&v)[8], float f) {
     return w;
 }
 
-// Eight entries of a row as they lie in memory, their fp32 values, and the largest
+// Four codes in the lower half.
+__device__ __forceinline__ uint32_t codes4(const float (&v)[4], float f) {
+    uint32_t w;
+    asm("{\n\t.reg .b8 b0, b1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "mov.b32 %0, {b0, b1, b0, b1};\n\t}"
+        : "=r"(w)
+        : "f"(v[0] * f), "f"(v[1] * f), "f"(v[2] * f), "f"(v[3] * f));
+    return w;
+}
+
+// Entries of a row as they lie in memory, their fp32 values, and the largest
 // magnitude of several, with a NaN above all (bf16: of two columns at a time).
 __device__ __forceinline__ float max_nan(float a, float b) {
     float y;
@@ -51,31 +63,33 @@ __device__ __forceinline__ uint32_t max_nan2(uint32_t a, uint32_t b) {
     return y;
 }
 
-template <class T> struct Row8;
+template <class T, int N> struct Row;
 
-template <> struct Row8<float> {
-    uint32_t w[8];
+template <int N> struct Row<float, N> {
+    uint32_t w[N];
     __device__ __forceinline__ void load(const float* p) {
-        const uint4 a = reinterpret_cast<const uint4*>(p)[0], b = reinterpret_cast<const uint4*>(p)[1];
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-        w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+#pragma unroll
+        for (int e = 0; e < N; e += 4) {
+            const uint4 a = *reinterpret_cast<const uint4*>(p + e);
+            w[e] = a.x; w[e + 1] = a.y; w[e + 2] = a.z; w[e + 3] = a.w;
+        }
     }
     __device__ __forceinline__ void load_some(const float* p, int count) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = e < count ? __float_as_uint(p[e]) : 0u;
+        for (int e = 0; e < N; ++e) w[e] = e < count ? __float_as_uint(p[e]) : 0u;
     }
     __device__ __forceinline__ float get(int e) const { return __uint_as_float(w[e]); }
-    // bits of the largest magnitude of the row's eight entries
+    // bits of the largest magnitude of the row's entries
     __device__ __forceinline__ uint32_t top() const {
         float t = fabsf(get(0));
 #pragma unroll
-        for (int e = 1; e < 8; ++e) t = max_nan(t, fabsf(get(e)));
+        for (int e = 1; e < N; ++e) t = max_nan(t, fabsf(get(e)));
         return __float_as_uint(t);
     }
     // and of each column of eight rows
-    static __device__ __forceinline__ void tops(const Row8 (&x)[8], uint32_t (&t)[8]) {
+    static __device__ __forceinline__ void tops(const Row (&x)[8], uint32_t (&t)[N]) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < N; ++e) {
             float y = fabsf(x[0].get(e));
 #pragma unroll
             for (int i = 1; i < 8; ++i) y = max_nan(y, fabsf(x[i].get(e)));
@@ -84,7 +98,7 @@ template <> struct Row8<float> {
     }
 };
 
-template <> struct Row8<__nv_bfloat16> {
+template <> struct Row<__nv_bfloat16, 8> {
     uint32_t w[4];
     __device__ __forceinline__ void load(const __nv_bfloat16* p) {
         const uint4 a = *reinterpret_cast<const uint4*>(p);
@@ -104,7 +118,7 @@ template <> struct Row8<__nv_bfloat16> {
         const uint32_t t = max_nan2(max_nan2(size(w[0]), size(w[1])), max_nan2(size(w[2]), size(w[3])));
         return max(t << 16, t & 0xFFFF0000u);
     }
-    static __device__ __forceinline__ void tops(const Row8 (&x)[8], uint32_t (&t)[8]) {
+    static __device__ __forceinline__ void tops(const Row (&x)[8], uint32_t (&t)[8]) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             uint32_t y = size(x[0].w[e]);

@@ -97,7 +97,7 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
 
 // Eight entries of row `row` from column `col` on, zero outside.
 template <class T>
-__device__ __forceinline__ void load_x(const FewParams& p, int row, int col, Row8<T>& x) {
+__device__ __forceinline__ void load_x(const FewParams& p, int row, int col, Row<T, 8>& x) {
     const T* src = static_cast<const T*>(p.X) + row * p.ldx + col;
     if (p.xvec && col + 8 <= p.K) x.load(src);
     else x.load_some(src, p.K - col);
@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
             // a warp takes every fourth row: lane l has columns 8l .. +7 of the stage,
             // four lanes a block
             constexpr int PER = F_QUANT / 4;
-            Row8<T> x[PER];
+            Row<T, 8> x[PER];
             auto fetch = [&](int k) {
 #pragma unroll
                 for (int i = 0; i < PER; ++i) {
