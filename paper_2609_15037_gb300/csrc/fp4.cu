@@ -58,7 +58,7 @@ template <int V, int L, int STEP> __device__ __forceinline__ void scatter_max(ui
 }
 
 template <class T, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 2 && !(ROWS && COLS) ? 3 : 2) k_fp4_quantize(const QuantParams p) {
+__global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 ? 2 : ROWS && COLS ? 3 : 4) k_fp4_quantize(const QuantParams p) {
     constexpr int N = Quant<T>::N, BLOCK = Quant<T>::BLOCK, THREADS = Quant<T>::THREADS;
     __shared__ __align__(16) uint8_t sfr[512];
     __shared__ __align__(16) uint8_t sfc[512];
