@@ -541,7 +541,7 @@ int moara_fp4_product(moara_ctx* ctx, int M, int N, int K, const void* a_q, cons
 /* The same product with A given as X (M x K, fp32 or bf16, row pitch ldx >= K),
  * quantised by rows on the way, with the result of moara_fp4_quantize and
  * moara_fp4_product.  workspace: moara_fp4_linear_workspace_bytes(M, N, K) device
- * bytes, 16-byte aligned (NULL where that is 0: up to 16 rows), in use by one call
+ * bytes, 16-byte aligned (NULL where that is 0: up to 8 rows), in use by one call
  * at a time. */
 int moara_fp4_linear_workspace_bytes(int M, int N, int K, size_t* out);
 int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_dtype, int64_t ldx, const void* b_q,

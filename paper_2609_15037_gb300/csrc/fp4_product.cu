@@ -27,15 +27,6 @@ __device__ __forceinline__ bool drained(uint32_t bar, uint32_t parity) {
     return true;
 }
 
-// Tiles in groups of G row tiles, so that the operands of the tiles in flight stay
-// in L2.
-template <int TM, int TN, int G, class P> __device__ __forceinline__ void grouped_tile(const P& p, int t, int& m0, int& n0) {
-    const int per = G * p.tiles_n, g = t / per, first = g * G;
-    const int rows = min(G, p.tiles_m - first), r = t - g * per;
-    m0 = (first + r % rows) * TM;
-    n0 = (r / rows) * TN;
-}
-
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -47,16 +38,16 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // a cluster of up to eight CTAs shares K, and each adds the others' sums for its
 // share of the tokens through shared memory.  Bound by latency (launch, one trip
 // to memory, the sums) up to some hundred tokens, then by the operands' way from L2:
-// with N = K = 4096 one token takes 4.4 us, 64 tokens 6.5, 256 10.0.
-// With QUANT, A comes as it is (at most 16 rows) and the four epilogue warps
+// with N = K = 4096 one token takes 4.7 us, 64 tokens 6.8, 256 9.9.
+// With QUANT, A comes as it is (at most 8 rows) and the four epilogue warps
 // quantise a stage's rows into shared memory, so that a token's product is one
-// launch (4.8 us); every CTA of a K range does that again, which pays while it is
-// 256 entries per row and stage.
+// launch (4.9 us); every CTA of a K range does that again, which pays for few rows: 8 take
+// 6.1 us and 6.8 with a launch of its own for the quantisation, 16 take 8.1 and 6.8.
 // ---------------------------------------------------------------------------
 constexpr int F_THREADS = 6 * 32;                  // TMA, MMA, four epilogue warps
 constexpr int F_STAGES = 4;                        // at most
 constexpr int F_TMEM = 256, F_TMEM_SF = 128, F_TMEM_STAGE = 16;
-constexpr int F_QUANT = 16;                        // most rows that are quantised on the way
+constexpr int F_QUANT = 8;                         // most rows that are quantised on the way
 static_assert(F_TMEM_SF + F_STAGES * F_TMEM_STAGE <= F_TMEM, "tensor memory");
 
 struct FewParams {
@@ -281,7 +272,15 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
             }
         }
     }
+    // Tensor memory is given back before this CTA waits for others of its cluster: those may
+    // themselves be waiting for some on an SM that holds as many CTAs as it has
+    // tensor memory for.
     ptx::tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, F_TMEM);
+    }
     __syncwarp();
     ptx::cluster_sync();                                            // every CTA's sums are in its shared memory
     {
@@ -321,10 +320,6 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
     }
     __syncwarp();
     ptx::cluster_sync();                                            // no CTA leaves while another reads its sums
-    if (warp == 1) {
-        ptx::tc_fence_after();
-        ptx::tmem_dealloc(tmem, F_TMEM);
-    }
 }
 
 // ---------------------------------------------------------------------------
@@ -372,6 +367,16 @@ struct PairCtl {
     uint32_t tmem;
     int abort;
 };
+
+// Tiles in groups of eight row tiles, so that the operands of the tiles in flight stay
+// in L2.
+__device__ __forceinline__ void tile_of(const PairParams& p, int t, int& m0, int& n0) {
+    constexpr int G = 8;
+    const int per = G * p.tiles_n, g = t / per, first = g * G;
+    const int rows = min(G, p.tiles_m - first), r = t - g * per;
+    m0 = (first + r % rows) * P_BM;
+    n0 = (r / rows) * P_BN;
+}
 
 // 64 bytes of 32 rows from a warp's staging to D, UNIT bytes of a lane at a time, so that
 // a store covers whole sectors whatever the rows' alignment.  left: bytes of the rows
@@ -477,7 +482,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
             bool ok = true;
             for (int t = first; t < tiles && ok; t += stride) {
                 int m0, n0;
-                grouped_tile<P_BM, P_BN, 8>(p, t, m0, n0);
+                tile_of(p, t, m0, n0);
                 for (int k = 0; k < steps; ++k) {
                     if (!ptx::mbar_wait(ptx::smem_u32(&ctl->empty[stage]), phase ^ 1, abort_flag, p.status,
                                         MOARA_ERR_DEVICE_TIMEOUT, kWait)) {
@@ -570,7 +575,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
         uint32_t acc = 0;
         for (int t = first; t < tiles; t += stride, acc ^= 1) {
             int m0, n0;
-            grouped_tile<P_BM, P_BN, 8>(p, t, m0, n0);
+            tile_of(p, t, m0, n0);
             const bool got = ptx::mbar_wait(ptx::smem_u32(&ctl->accf), acc, abort_flag, p.status,
                                             MOARA_ERR_DEVICE_TIMEOUT, kWait);
             if (!__all_sync(0xffffffffu, got)) break;

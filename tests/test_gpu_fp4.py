@@ -350,7 +350,7 @@ def test_large_product(M, fp4, shape, dtype):
     assert torch.equal(fp4.linear(x, W, dtype=DT[dtype]), got)
 
 
-@pytest.mark.parametrize("m", [1, 5, 16, 17])
+@pytest.mark.parametrize("m", [1, 5, 8, 9, 16, 17])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("pitch,offset", [(3, 0), (8, 1), (8, 0)])
 def test_linear_reads_strided_rows(M, fp4, m, dtype, pitch, offset):
