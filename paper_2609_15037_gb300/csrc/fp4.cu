@@ -191,6 +191,7 @@ struct ValueParams {
     const uint8_t* q;
     const uint8_t* sf;
     int rows, cols, kb, tiles_c;
+    int lanes;             // log2 of the threads along a row, up to as many as it needs
     int parts;             // CTAs along a row
     void* out;
     long long ldo;
@@ -201,21 +202,21 @@ __device__ __forceinline__ uint32_t scale_at(const ValueParams& p, int row, int 
                 ((row & 127) >> 5) * 4 + (block & 3)];
 }
 
-// Rows of `out` on 16-byte boundaries.  A CTA takes 16 rows x 512 columns: a thread 8
-// columns of four rows, whose loads are issued together.  11008 x 4096 into bf16: 15.8 us,
-// 7.2 TB/s.
-constexpr int VALUE_ROWS = 4;
+// Rows of `out` on 16-byte boundaries.  A thread takes 8 columns of four rows, whose
+// loads are issued together; a CTA up to 512 columns, and more rows of a narrow matrix.
+// 11008 x 4096 into bf16: 15.8 us, 7.2 TB/s.
+constexpr int VALUE_ROWS = 4, VALUE_LANES = 64;
 
 template <class T> __global__ void __launch_bounds__(256) k_fp4_values(const ValueParams p) {
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int part = blockIdx.x % p.parts, group = blockIdx.x / p.parts;
-    const int s = part * 64 + (threadIdx.x & 63), block = s >> 2, col = 8 * s;
-    const int row0 = group * (4 * VALUE_ROWS) + (threadIdx.x >> 6);
+    const int part = blockIdx.x % p.parts, group = blockIdx.x / p.parts, step = 256 >> p.lanes;
+    const int s = (part << p.lanes) + (threadIdx.x & ((1 << p.lanes) - 1)), block = s >> 2, col = 8 * s;
+    const int row0 = group * (step * VALUE_ROWS) + (threadIdx.x >> p.lanes);
     if (block >= p.kb) return;
     uint32_t w[VALUE_ROWS], sb[VALUE_ROWS];
 #pragma unroll
     for (int i = 0; i < VALUE_ROWS; ++i) {
-        const int row = row0 + 4 * i;
+        const int row = row0 + step * i;
         w[i] = sb[i] = 0;
         if (row >= p.rows) continue;
         w[i] = *reinterpret_cast<const uint32_t*>(p.q + (static_cast<long long>(row) * p.kb + block) * 16 + (s & 3) * 4);
@@ -223,7 +224,7 @@ template <class T> __global__ void __launch_bounds__(256) k_fp4_values(const Val
     }
 #pragma unroll
     for (int i = 0; i < VALUE_ROWS; ++i) {
-        const int row = row0 + 4 * i;
+        const int row = row0 + step * i;
         if (row >= p.rows) return;
         float v[8];
         values8(w[i], scale_value(sb[i]), v);
@@ -249,61 +250,84 @@ template <class T> __global__ void __launch_bounds__(256) k_fp4_values(const Val
     }
 }
 
-// Rows on any boundary.  A CTA takes 4 rows x 512 columns, a warp 64 of the columns, a lane
-// two of them, which in a row of bf16 that begins between two words are the second
-// of one byte of codes and the first of the next: one word is stored.  11007 x 4097
-// into bf16: 71 us, and 127 with the eight columns of a lane stored one by one.
+// Rows on any boundary.  A thread works out 8 columns of four rows; a row's words are
+// stored one to a lane, through shared memory, so that a store is contiguous.  In a row
+// of bf16 that begins between two words a thread takes its columns one further on: the
+// first code of its neighbour is its eighth.  11007 x 4097 into bf16 took 127 us with the
+// columns of a thread stored one by one, 74 with two columns to a thread, and takes 45.
 template <class T> __global__ void __launch_bounds__(256) k_fp4_values_any(const ValueParams p) {
+    constexpr int WORDS = 2 * sizeof(T), SHIFT = sizeof(T) == 2 ? 2 : 3;          // of a thread's columns
+    __shared__ __align__(16) uint32_t staged[256 * WORDS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int part = blockIdx.x % p.parts, row0 = blockIdx.x / p.parts * VALUE_ROWS;
-    const int j = part * 256 + threadIdx.x;                              // byte of codes
-    if (2 * j >= p.cols) return;
-    float2 v[VALUE_ROWS];
+    const int lanes = 1 << p.lanes, at_once = 32 >> p.lanes, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int part = blockIdx.x % p.parts, group = blockIdx.x / p.parts;
+    const int s = part * lanes + (lane & (lanes - 1)), block = s >> 2;
+    const int row0 = (group * 8 + warp) * at_once * VALUE_ROWS;
+    uint8_t* const out = static_cast<uint8_t*>(p.out);
+    const long long pitch = p.ldo * static_cast<long long>(sizeof(T));
+    auto odd_row = [&](int row) {
+        return sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(out + row * pitch) & 2) != 0;
+    };
+    uint32_t w[VALUE_ROWS], next[VALUE_ROWS], s0[VALUE_ROWS], s1[VALUE_ROWS];
 #pragma unroll
     for (int i = 0; i < VALUE_ROWS; ++i) {
-        const int row = row0 + i;
-        v[i] = make_float2(0.0f, 0.0f);
-        if (row >= p.rows) continue;
-        const uint8_t* q = p.q + static_cast<long long>(row) * p.kb * 16 + j;
-        const T* o = static_cast<const T*>(p.out) + row * p.ldo;
-        const int odd = sizeof(T) == 2 ? static_cast<int>(reinterpret_cast<uintptr_t>(o) >> 1 & 1) : 0;
-        uint32_t w = q[0], s0 = scale_at(p, row, j >> 4), s1 = s0;
-        if (odd) {
-            const bool more = 2 * j + 2 < p.cols;
-            w = w >> 4 | (more ? static_cast<uint32_t>(q[1]) << 4 : 0u);
-            if (more && ((j + 1) & 15) == 0) s1 = scale_at(p, row, (j + 1) >> 4);
+        const int row = row0 + i * at_once + (lane >> p.lanes);
+        w[i] = next[i] = s0[i] = s1[i] = 0;
+        if (row >= p.rows || block >= p.kb) continue;
+        const uint8_t* q = p.q + (static_cast<long long>(row) * p.kb + block) * 16 + (s & 3) * 4;
+        w[i] = *reinterpret_cast<const uint32_t*>(q);
+        s0[i] = scale_at(p, row, block);
+        if (sizeof(T) == 2 && s + 1 < 4 * p.kb) {
+            next[i] = q[4];
+            s1[i] = (s & 3) == 3 ? scale_at(p, row, block + 1) : s0[i];
         }
-        uint32_t h;
-        asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-            "mov.b32 {b0, b1, b2, b3}, %1;\n\t"
-            "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t}"
-            : "=r"(h)
-            : "r"(w));
-        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h));
-        v[i] = make_float2(a.x * scale_value(s0), a.y * scale_value(s1));
     }
+    uint32_t* const mine = staged + warp * (32 * WORDS);
 #pragma unroll
     for (int i = 0; i < VALUE_ROWS; ++i) {
-        const int row = row0 + i;
-        if (row >= p.rows) return;
-        T* o = static_cast<T*>(p.out) + row * p.ldo;
-        if (sizeof(T) == 4) {
-            o[2 * j] = static_cast<T>(v[i].x);
-            if (2 * j + 1 < p.cols) o[2 * j + 1] = static_cast<T>(v[i].y);
-            continue;
+        const int row = row0 + i * at_once + (lane >> p.lanes);
+        const bool odd = row < p.rows && odd_row(row);
+        float v[9];
+        {
+            float x[8];
+            values8(w[i], scale_value(s0[i]), x);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = x[e];
         }
-        const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(o) >> 1 & 1), c = 2 * j + odd;
-        if (odd && j == 0) {
-            uint32_t h;
-            asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-                "mov.b32 {b0, b1, b2, b3}, %1;\n\t"
-                "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t}"
-                : "=r"(h)
-                : "r"(static_cast<uint32_t>(p.q[static_cast<long long>(row) * p.kb * 16])));
-            o[0] = static_cast<T>(__low2float(*reinterpret_cast<const __half2*>(&h)) * scale_value(scale_at(p, row, 0)));
+        if (sizeof(T) == 2) {
+            float x[8];
+            values8(next[i], scale_value(s1[i]), x);
+            v[8] = x[0];
+            if (odd && s == 0) *reinterpret_cast<T*>(out + row * pitch) = static_cast<T>(v[0]);
         }
-        if (c + 1 < p.cols) *reinterpret_cast<__nv_bfloat162*>(o + c) = __floats2bfloat162_rn(v[i].x, v[i].y);
-        else if (c < p.cols) o[c] = static_cast<T>(v[i].x);
+        __syncwarp();
+        uint32_t h[8];
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) {
+            if (sizeof(T) == 4) {
+                h[k] = __float_as_uint(v[k]);
+            } else {
+                const __nv_bfloat162 y = __floats2bfloat162_rn(odd ? v[2 * k + 1] : v[2 * k], odd ? v[2 * k + 2] : v[2 * k + 1]);
+                h[k] = *reinterpret_cast<const uint32_t*>(&y);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < WORDS; k += 4)
+            *reinterpret_cast<uint4*>(mine + lane * WORDS + k) = make_uint4(h[k], h[k + 1], h[k + 2], h[k + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int k = 0; k < WORDS; ++k) {
+            const int x = k * 32 + lane, r = row0 + i * at_once + (x >> (p.lanes + SHIFT));
+            const int word = x & ((lanes << SHIFT) - 1);
+            if (r >= p.rows) break;
+            uint8_t* row_at = out + r * pitch;
+            const int shift = odd_row(r) ? 1 : 0;
+            const int col = part * lanes * 8 + word * (4 / static_cast<int>(sizeof(T))) + shift;
+            if (col + static_cast<int>(4 / sizeof(T)) <= p.cols)
+                *reinterpret_cast<uint32_t*>(row_at + static_cast<long long>(col) * sizeof(T)) = mine[x];
+            else if (sizeof(T) == 2 && col < p.cols)
+                *reinterpret_cast<uint16_t*>(row_at + static_cast<long long>(col) * 2) = static_cast<uint16_t>(mine[x]);
+        }
     }
 }
 
@@ -347,12 +371,14 @@ cudaError_t launch_fp4_dequantize(const void* q, const void* sf, int rows, int c
     p.cols = cols;
     p.kb = fp4_blocks(cols);
     p.tiles_c = fp4_tiles(cols);
-    p.parts = (cols - 1) / 512 + 1;
     p.out = out;
     p.ldo = ldo;
     const bool bf = dtype == MOARA_DTYPE_BF16;
     const bool vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ldo % (bf ? 8 : 4) == 0;
-    const int per = vec ? 4 * VALUE_ROWS : VALUE_ROWS;
+    const int units = 4 * p.kb;
+    while ((1 << p.lanes) < units && (1 << p.lanes) < (vec ? VALUE_LANES : 32)) ++p.lanes;
+    p.parts = ((units - 1) >> p.lanes) + 1;
+    const int per = (256 >> p.lanes) * VALUE_ROWS;
     const unsigned int grid = static_cast<unsigned int>(p.parts) * ((rows - 1) / per + 1);
     auto fn = vec ? (bf ? k_fp4_values<__nv_bfloat16> : k_fp4_values<float>)
                   : (bf ? k_fp4_values_any<__nv_bfloat16> : k_fp4_values_any<float>);
