@@ -38,7 +38,9 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // a cluster of up to eight CTAs shares K, and each adds the others' sums for its
 // share of the tokens through shared memory.  Bound by latency (launch, one trip
 // to memory, the sums) up to some hundred tokens, then by the operands' way from L2:
-// with N = K = 4096 one token takes 4.7 us, 64 tokens 6.8, 256 9.9.
+// with N = K = 4096 one token takes 4.7 us, 64 tokens 6.8, 256 9.7.  (A warp per two rows of
+// the weight without tensor cores takes 4.7 us for a token there and 7.2 against 6.0 with
+// N = 11008: the conversions bound it.)
 // With QUANT, A comes as it is (at most 8 rows) and the four epilogue warps
 // quantise a stage's rows into shared memory, so that a token's product is one
 // launch (4.9 us); every CTA of a K range does that again, which pays for few rows: 8 take
@@ -727,15 +729,17 @@ cudaError_t launch_few(const Fp4Product& a, bool early, int* status, cudaStream_
     if (e != cudaSuccess) return e;
     // begins beside the end of the launch in front where it is short or leaves room: a token
     // through 4096 x 4096 4.4 instead of 4.9 us in a row of them.  Otherwise two of its CTAs
-    // share an SM while others idle (512 x 4096 x 4096: 13.4 us instead of 12.5)
+    // share an SM while others idle (128 x 4096 x 4096: 8.8 us instead of 8.0)
     const bool overlap = early || p.nt <= 32 || tiles * p.split <= 76;
     return launch_if(overlap, k_fp4_few<QUANT, T>, dim3(static_cast<unsigned int>(tiles * p.split)), dim3(F_THREADS), smem,
                      s, p.split, p);
 }
 
-// Pairs where their tiles occupy half of the GPU, the other form below that.
+// Pairs where their tiles occupy a quarter of the GPU and more, the other form below
+// that: with 32 tiles (512 x 4096 x 4096) 10.0 us against 12.6, with 24 (1500 x 1003 x 2049)
+// 11.9 against 14.2, with 16 (512 x 2048 x 4096) 9.8 against 9.7.
 bool large(const Fp4Product& a) {
-    return static_cast<long long>((a.M - 1) / P_BM + 1) * ((a.N - 1) / P_BN + 1) >= 38 && a.M > 128;
+    return static_cast<long long>((a.M - 1) / P_BM + 1) * ((a.N - 1) / P_BN + 1) >= 19 && a.M > 128;
 }
 
 }  // namespace
