@@ -10,30 +10,21 @@ from . import _host
 from . import binding as B
 from .adamw import _TYPES, allocating_on, entry_address, stream_handle
 
-
-_QUANTIZE = entry_address("moara_fp4_quantize")
-_ENTRIES = {
-    "moara_fp4_dequantize": (_host.fp4_dequantize, entry_address("moara_fp4_dequantize")),
-    "moara_fp4_product": (_host.fp4_product, entry_address("moara_fp4_product")),
-    "moara_fp4_linear": (_host.fp4_linear, entry_address("moara_fp4_linear"), entry_address("moara_fp4_linear_workspace_bytes")),
-}
+_QUANTIZE, _DEQUANTIZE, _PRODUCT, _LINEAR, _LINEAR_BYTES = (
+    entry_address("moara_fp4_" + f) for f in ("quantize", "dequantize", "product", "linear", "linear_workspace_bytes"))
 
 
 class Fp4Matrix:
     """A rows x cols matrix in MXFP4 (layouts of moara.h): codes `q`, scales `sf`."""
 
-    __slots__ = "rows", "cols", "_sizes", "_ptrs", "_both", "_start", "_q", "_sf"
+    __slots__ = "rows", "cols", "_ptrs", "_both", "_q", "_sf"
 
     def __init__(self, rows, cols, q=None, sf=None, device=0):
         self.rows, self.cols = rows, cols
-        if rows < 1 or cols < 1:
-            B.moara_fp4_bytes(rows, cols)                   # raises
-        # moara_fp4_bytes, without the call
-        nq = rows * ((cols + 31) // 32) * 16
-        sizes = self._sizes = nq, (rows + 127) // 128 * ((cols + 127) // 128) * 512
+        sizes = B.moara_fp4_bytes(rows, cols)
         if q is None and sf is None:
             # one allocation: the codes, and the scales from the next 256 bytes on
-            start = self._start = (nq + 255) // 256 * 256
+            start = (sizes[0] + 255) // 256 * 256
             self._both, at = _host.bytes(start + sizes[1], device)
             self._ptrs = at, at + start
             return
@@ -45,24 +36,20 @@ class Fp4Matrix:
         self._q, self._sf = q, sf
         self._ptrs = q.data_ptr(), sf.data_ptr()
 
-    @classmethod
-    def _of(cls, buffer, rows, cols):
-        """The operand in a buffer of the native module: (tensor, address of q, of sf)."""
-        self = cls.__new__(cls)
-        self.rows, self.cols = rows, cols
-        self._both, q, sf = buffer
-        self._ptrs = q, sf
-        self._start = sf - q
-        self._sizes = rows * ((cols + 31) // 32) * 16, 0
-        return self
-
     @property
     def q(self):
-        return self._q if self._both is None else self._both[:self._sizes[0]]
+        return self._q if self._both is None else self._both[:B.moara_fp4_bytes(self.rows, self.cols)[0]]
 
     @property
     def sf(self):
-        return self._sf if self._both is None else self._both[self._start:]
+        return self._sf if self._both is None else self._both[self._ptrs[1] - self._ptrs[0]:]
+
+
+def _operand(buffer, rows, cols):
+    """The operand in a buffer of the native module: (tensor, address of q, of sf)."""
+    a = Fp4Matrix.__new__(Fp4Matrix)
+    a.rows, a.cols, a._both, a._ptrs = rows, cols, buffer[0], buffer[1:]
+    return a
 
 
 class Fp4Group:
@@ -94,18 +81,15 @@ class Fp4Group:
             raise ValueError(f"out: an operand of {rows} x {cols} is needed")
         return m
 
-    def _call(self, name, *args, out, dtype, stream):
-        """A call of the native module: the entry's address, its arguments, where its output
-        goes.  Its tensor, or the entry's error raised."""
-        if out is None and dtype not in _TYPES:
+    def _bf16(self, out, dtype):
+        """Whether a new output is bf16 (an output that is given has its own type)."""
+        bf16 = _TYPES.get(dtype)
+        if bf16 is None and out is None:
             raise ValueError("dtype must be float32 or bfloat16")
-        fn, entry, *more = _ENTRIES[name]
-        tail = out, _TYPES.get(dtype, 0), self.device, stream_handle(stream, self.device), *more
-        if stream is None:
-            got = fn(entry, self.ctx, *args, *tail)
-        else:
-            with allocating_on(stream, self.device):
-                got = fn(entry, self.ctx, *args, *tail)
+        return bf16
+
+    def _done(self, got, name):
+        """What a call of the native module gave: a tensor, or an error code to raise."""
         if got.__class__ is int:
             B._check(got, self.ctx, name)
         return got
@@ -120,9 +104,10 @@ class Fp4Group:
             if got.__class__ is int:
                 B._check(got, self.ctx, "moara_fp4_quantize")
             r, c, m, k = got
-            a = Fp4Matrix._of(r, m, k) if rows else None
-            b = Fp4Matrix._of(c, k, m) if cols else None
-            return (a, b) if rows and cols else a if rows else b
+            if not cols:
+                return _operand(r, m, k)
+            b = _operand(c, k, m)
+            return (_operand(r, m, k), b) if rows else b
         ptr, dtype, m, k, ld = _host.matrix(x, self.device)
         a = self._matrix(out, m, k, stream) if rows else None
         b = self._matrix(out_cols, k, m, stream) if cols else None
@@ -133,18 +118,32 @@ class Fp4Group:
 
     def dequantize(self, a, dtype=torch.bfloat16, out=None, stream=None):
         """The values of an operand (bfloat16 holds them exactly)."""
-        return self._call("moara_fp4_dequantize", *a._ptrs, a.rows, a.cols, out=out, dtype=dtype, stream=stream)
+        args = (_DEQUANTIZE, self.ctx, *a._ptrs, a.rows, a.cols, out, self._bf16(out, dtype), self.device,
+                stream_handle(stream, self.device))
+        if stream is None:
+            return self._done(_host.fp4_dequantize(*args), "moara_fp4_dequantize")
+        with allocating_on(stream, self.device):
+            return self._done(_host.fp4_dequantize(*args), "moara_fp4_dequantize")
 
     def product(self, a, b, dtype=torch.bfloat16, out=None, stream=None):
         """a b^T of two operands with the same number of columns."""
         if a.cols != b.cols:
             raise ValueError(f"{a.cols} and {b.cols} columns")
-        return self._call("moara_fp4_product", a.rows, b.rows, a.cols, *a._ptrs, *b._ptrs, out=out, dtype=dtype,
-                          stream=stream)
+        args = (_PRODUCT, self.ctx, a.rows, b.rows, a.cols, *a._ptrs, *b._ptrs, out, self._bf16(out, dtype),
+                self.device, stream_handle(stream, self.device))
+        if stream is None:
+            return self._done(_host.fp4_product(*args), "moara_fp4_product")
+        with allocating_on(stream, self.device):
+            return self._done(_host.fp4_product(*args), "moara_fp4_product")
 
     def linear(self, x, b, dtype=torch.bfloat16, out=None, stream=None):
         """x b^T with x (float32 or bfloat16) quantised by rows on the way."""
-        return self._call("moara_fp4_linear", x, b.rows, b.cols, *b._ptrs, out=out, dtype=dtype, stream=stream)
+        args = (_LINEAR, self.ctx, x, b.rows, b.cols, *b._ptrs, out, self._bf16(out, dtype), self.device,
+                stream_handle(stream, self.device), _LINEAR_BYTES)
+        if stream is None:
+            return self._done(_host.fp4_linear(*args), "moara_fp4_linear")
+        with allocating_on(stream, self.device):
+            return self._done(_host.fp4_linear(*args), "moara_fp4_linear")
 
     def status(self, stream=None):
         """Reads and clears the device status word (0, or an error a kernel recorded)."""
