@@ -506,20 +506,31 @@ __global__ void __launch_bounds__(256) k_moments(const __grid_constant__ MomentB
 // Gradient norm.  A thread sums at most 32 squares of a chunk in fp32 and adds
 // the chunk sums in fp64; CTA sums go to the workspace, and the CTA that draws
 // the last ticket adds them in order.  Which CTA that is does not change the
-// result: chunks belong to CTAs by index.  DRAM-bound: 374 M bf16 entries 110 us (6.8
-// TB/s), fp32 212 us (7.0 TB/s); 65 gradients of 4096 entries 5.8 us, the chain of
+// result: chunks belong to CTAs by index.  DRAM-bound: 374 M bf16 entries 107 us (7.0
+// TB/s), fp32 207 us (7.2 TB/s); 65 gradients of 4096 entries 4.3 us, the chain of
 // launch, sums, ticket and the last CTA's sum.
 // ---------------------------------------------------------------------------
+// The sum over 256 threads, in thread 0.
 __device__ __forceinline__ double cta_sum(double v, double* red) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     __syncthreads();
     if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
     __syncthreads();
-    double t = 0.0;
+    if (threadIdx.x < 32) {
+        v = red[threadIdx.x & 7];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t += red[i];
-    return t;
+        for (int o = 4; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    }
+    return v;
+}
+
+// Adds one at a counter; what this thread wrote before is visible to whoever reads the
+// counter this way afterwards.
+__device__ __forceinline__ unsigned int draw_ticket(unsigned int* ticket) {
+    unsigned int order;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(order) : "l"(ticket) : "memory");
+    return order;
 }
 
 template <class T>
@@ -536,7 +547,17 @@ __device__ __forceinline__ float chunk_squares(const T* g, long long e0, long lo
         }
     } else {
         const long long e1 = min(e0 + static_cast<long long>(kGradChunk), n);
-        for (long long i = e0 + threadIdx.x; i < e1; i += 256) {
+        long long i = e0;
+        if (vector) {
+#pragma unroll 4
+            for (; i + 1024 <= e1; i += 1024) {
+                float v[4];
+                load4<true>(g, i + 4 * threadIdx.x, n, v);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s = fmaf(v[e], v[e], s);
+            }
+        }
+        for (i += threadIdx.x; i < e1; i += 256) {
             const float x = static_cast<float>(g[i]);
             s = fmaf(x, x, s);
         }
@@ -560,23 +581,23 @@ template <int CAP> __global__ void __launch_bounds__(256) k_grad_norm(const __gr
     const double sum = cta_sum(acc, red);
     if (threadIdx.x == 0) {
         b.partials[b.first + blockIdx.x] = sum;
-        __threadfence();
-        const unsigned int order = b.last ? atomicAdd(b.ticket, 1u) : 0u;
-        finish = b.last && order == gridDim.x - 1;
+        finish = b.last && draw_ticket(b.ticket) == gridDim.x - 1;
     }
     __syncthreads();
     if (!finish) return;
-    __threadfence();
     double part = 0.0;
     for (int i = threadIdx.x; i < b.first + static_cast<int>(gridDim.x); i += 256) part += __ldcg(b.partials + i);
     const double total = cta_sum(part, red);
     if (threadIdx.x == 0) {
         *b.ticket = 0;
-        const double norm = sqrt(total + (b.extra != nullptr ? static_cast<double>(*b.extra) : 0.0));
-        const double coef = static_cast<double>(b.max_norm) / (norm + 1e-6);
+        // an fp64 root and quotient are a microsecond of dependent operations here: fp32 ones,
+        // but for a sum that fp32 does not hold
+        const double all = total + (b.extra != nullptr ? static_cast<double>(*b.extra) : 0.0);
+        const float norm = all < 1e38 ? __fsqrt_rn(static_cast<float>(all)) : static_cast<float>(sqrt(all));
+        const float coef = __fdiv_rn(b.max_norm, norm + 1e-6f);
         b.out[0] = static_cast<float>(total);
-        b.out[1] = static_cast<float>(norm);
-        b.out[2] = b.max_norm > 0.0f && !(coef >= 1.0) ? static_cast<float>(coef) : 1.0f;
+        b.out[1] = norm;
+        b.out[2] = b.max_norm > 0.0f && !(coef >= 1.0f) ? coef : 1.0f;
     }
 }
 
