@@ -452,6 +452,10 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int crank = static_cast<int>(ptx::cluster_ctarank());
     volatile int* abort_flag = &ctl->abort;
+    if ((ptx::smem_u32(smem) & 1023u) != 0) {                       // the same in every CTA
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, MOARA_ERR_ALIGN);
+        return;
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < P_STAGES; ++s) {
             ptx::mbar_init(ptx::smem_u32(&ctl->full[s]), 1);

@@ -304,6 +304,7 @@ def test_refusals(M, fp4):
     assert Q(X, 0, 64, 96, 96) == M.MOARA_ERR_INVALID_ARG and Q(X, 0, 64, 96, 96, q) == M.MOARA_ERR_INVALID_ARG
     assert Q(X + 2, 0, 64, 96, 96, q, sf) == M.MOARA_ERR_ALIGN and Q(X, 0, 64, 96, 96, q + 8, sf) == M.MOARA_ERR_ALIGN
     assert Q(X, 0, 2 ** 31 - 1, 2 ** 31 - 1, 2 ** 31, q, sf) == M.MOARA_ERR_SHAPE
+    assert Q(X, 0, 2 ** 31 - 100, 1, 1, q, sf) == M.MOARA_ERR_SHAPE
     P = lambda *a: code(lambda: M.moara_fp4_product(fp4.ctx, *a))  # noqa: E731
     D = torch.zeros(64, 64, device="cuda")
     d = D.data_ptr()
