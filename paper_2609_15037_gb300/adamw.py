@@ -149,13 +149,13 @@ class AdamWGroup:
         return exp_avg, exp_avg_sq
 
     def _norm_workspace(self, count, handle, stream):
-        ws, room = self._workspace.get(handle, (None, -1))
-        if count > room:
-            need = B.moara_grad_norm_workspace_bytes(count)
-            with allocating_on(stream, self.device):
-                ws = torch.zeros(need, dtype=torch.uint8, device=self._dev)
-                # memory of a recorded graph is the graph's own
-                if not torch.cuda.is_current_stream_capturing():
+        with allocating_on(stream, self.device):
+            # a recorded graph has its own, which no later call replaces or shares
+            recorded = torch.cuda.is_current_stream_capturing()
+            ws, room = (None, -1) if recorded else self._workspace.get(handle, (None, -1))
+            if count > room:
+                ws = torch.zeros(B.moara_grad_norm_workspace_bytes(count), dtype=torch.uint8, device=self._dev)
+                if not recorded:
                     self._workspace[handle] = ws, count
         return ws
 
@@ -164,9 +164,10 @@ class AdamWGroup:
         bf16), a float32 tensor of three.  extra_sq: a one-element float32 device
         tensor added to the sum under the root, or None.  The first element is
         what MoaraGroup.set_clip_extra takes, the last what step takes."""
+        grads = _listed(grads)
         handle = stream_handle(stream, self.device)
         ws = self._norm_workspace(len(grads), handle, stream)
-        args = (_NORM, self.ctx, _listed(grads), max_norm, extra_sq, out, ws.data_ptr(), ws.numel(), self.device, handle)
+        args = (_NORM, self.ctx, grads, max_norm, extra_sq, out, ws.data_ptr(), ws.numel(), self.device, handle)
         if stream is None:
             got = _host.grad_norm(*args)
         else:
@@ -180,6 +181,10 @@ class AdamWGroup:
         return [{k: v.detach().clone() for k, v in s.items()} for s in self.states]
 
     def load_state_dict(self, sd):
+        """Into the registered tensors' moments; nothing is taken of one that does not fit."""
+        like = [{k: (v.dtype, v.shape) for k, v in s.items()} for s in sd]
+        if like != [{k: (v.dtype, v.shape) for k, v in s.items()} for s in self.states]:
+            raise ValueError("load_state_dict: the moments of other tensors")
         for s, new in zip(self.states, sd):
             for k, v in s.items():
                 v.copy_(new[k])

@@ -317,6 +317,51 @@ def test_other_stream_and_capture(M):
         assert torch.equal(a, b)
 
 
+def test_recorded_norm_keeps_its_workspace(M):
+    """A graph recorded after a call on its stream, replayed after a call there that
+    needs a larger workspace and after others have taken freed memory."""
+    rng = np.random.default_rng(17)
+    g = [make(rng, 5000, "f32", 1.0) for _ in range(3)]
+    opt = M.AdamWGroup()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    out = torch.zeros(3, device="cuda")
+    with torch.cuda.stream(s):
+        first = opt.grad_norm(iter(g[:1]), 1.0).clone()
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            opt.grad_norm(g[:1], 1.0, out=out)
+        many = opt.grad_norm(g * 700, 1.0)
+        taken = [torch.full((512 << i,), 255, dtype=torch.uint8, device="cuda") for i in range(12)]
+        for _ in range(2):
+            out.zero_()
+            graph.replay()
+            s.synchronize()
+            assert torch.equal(out, first)
+        assert torch.equal(opt.grad_norm(g * 700, 1.0), many)
+    assert all(bool((x == 255).all()) for x in taken)
+    opt.close()
+
+
+def test_state_dict_of_others_is_refused(M):
+    a, b = M.AdamWGroup(), M.AdamWGroup()
+    for opt, sizes, state in ((a, (300, 7), "block8"), (b, (300,), "block8")):
+        for n in sizes:
+            opt.add(torch.ones(n, device="cuda"), state=state)
+    sd = a.state_dict()
+    for bad in (sd[:1], sd + sd[:1], sd[::-1], [sd[0], {"exp_avg": sd[1]["exp_avg"]}],
+                [sd[0], {k: v.float() for k, v in sd[1].items()}]):
+        with pytest.raises(ValueError):
+            a.load_state_dict(bad)
+    with pytest.raises(ValueError):
+        b.load_state_dict(sd)
+    a.step([torch.ones(300, device="cuda"), torch.ones(7, device="cuda")], 1, LR)
+    a.load_state_dict(sd)
+    assert all(torch.equal(x, y) for s, new in zip(a.states, sd) for x, y in zip(s.values(), new.values()))
+    a.close(), b.close()
+
+
 def test_refusals(M):
     opt = M.AdamWGroup()
     p = torch.ones(100, device="cuda")
