@@ -359,7 +359,7 @@ struct PairParams {
     int M, N, K;
     int tiles_m, tiles_n;
     int bf16;
-    int unit;              // bytes to which rows of D are aligned, at most 16
+    int vec;               // rows of D begin on 16-byte lines
     int* status;
 };
 
@@ -380,50 +380,72 @@ __device__ __forceinline__ void tile_of(const PairParams& p, int t, int& m0, int
     n0 = (r / rows) * P_BN;
 }
 
-// 64 bytes of 32 rows from a warp's staging to D, UNIT bytes of a lane at a time, so that
-// a store covers whole sectors whatever the rows' alignment.  left: bytes of the rows
-// that exist.  ODD: rows of bf16 that begin between two words were staged from their
-// second entry on.
-template <class U, int ES, bool ODD>
+// Bytes from an address to the next 16-byte line.
+__device__ __forceinline__ int to_line(const uint8_t* at) {
+    return static_cast<int>(-reinterpret_cast<uintptr_t>(at) & 15);
+}
+
+// 64 bytes of 32 rows from a warp's staging to D, 16 bytes a lane.  left: bytes of the
+// rows that exist.  ANY: each row was staged from its first whole line on.
+template <int ES, bool ANY>
 __device__ __forceinline__ void store_rows(const uint8_t* stage, uint8_t* d, long long pitch, int rows, int left, int lane) {
-    constexpr int UNIT = sizeof(U), PER = 64 / UNIT, AT = 32 / PER;              // lanes a row, rows at a time
-    const int b = lane % PER * UNIT;
-    const uint8_t* from = stage + (b & 15);
-#pragma unroll 8
-    for (int i = 0; i < 32; i += AT) {
-        const int r = i + lane / PER;
-        if (r >= rows) continue;
-        const uint8_t* x = from + r * 64 + (((b >> 4) ^ ((r >> 1) & 3)) << 4);
-        uint8_t* to = d + r * pitch + b;
-        const int skip = ODD ? static_cast<int>(reinterpret_cast<uintptr_t>(to) & 2) : 0;
-        to += skip;
-        if (b + UNIT + skip <= left) {
-            __stcs(reinterpret_cast<U*>(to), *reinterpret_cast<const U*>(x));       // D does not displace the operands in L2
-        } else if (UNIT > ES) {
+    const int b = lane % 4 * 16;
 #pragma unroll
-            for (int e = 0; e < UNIT; e += ES) {
-                if (b + skip + e >= left) continue;
-                if (ES == 2) *reinterpret_cast<uint16_t*>(to + e) = *reinterpret_cast<const uint16_t*>(x + e);
-                else *reinterpret_cast<uint32_t*>(to + e) = *reinterpret_cast<const uint32_t*>(x + e);
-            }
+    for (int i = 0; i < 32; i += 8) {
+        const int r = i + lane / 4;
+        if (r >= rows) continue;
+        const uint8_t* x = stage + r * 64 + (((b >> 4) ^ ((r >> 1) & 3)) << 4);
+        uint8_t* to = d + r * pitch + b;
+        const int skip = ANY ? to_line(to) : 0;
+        to += skip;
+        if (b + 16 + skip <= left) {
+            __stcs(reinterpret_cast<uint4*>(to), *reinterpret_cast<const uint4*>(x));   // D does not displace the operands in L2
+        } else {
+            const int end = left - (b + skip), eight = end & 8, four = end & 4;     // less than a line, or nothing
+            if (end <= 0) continue;
+            if (eight) *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(x);
+            if (four) *reinterpret_cast<uint32_t*>(to + eight) = *reinterpret_cast<const uint32_t*>(x + eight);
+            if (ES == 2 && (end & 2))
+                *reinterpret_cast<uint16_t*>(to + eight + four) = *reinterpret_cast<const uint16_t*>(x + eight + four);
         }
     }
 }
 
-// 256 bytes (64 words of lane = row) of a warp's 32 rows of D from row, col on.
+// 256 bytes (64 words of lane = row) of a warp's 32 rows of D from row, col on.  Rows on
+// other boundaries than 16 bytes leave as whole lines too, after their words were moved up
+// in the registers: 7195 x 8923 x 246 into bf16 51.5 us, into fp32 91; stored by words or
+// halves where they lie, 96 and 122 (N = 8928, whose rows are aligned: 37 and 60).
 template <int ES>
 __device__ __forceinline__ void store_words(const PairParams& p, uint8_t* stage, int row, int col, uint32_t (&w)[64], int lane) {
     constexpr int COLS = 64 / ES;                                   // of a 64-byte chunk
     const int rows = p.M - row;
     const long long pitch = p.ldd * ES;
     uint8_t* d = static_cast<uint8_t*>(p.D) + row * pitch + static_cast<long long>(col) * ES;
-    if (ES == 2 && p.unit == 2) {
+    if (!p.vec) {
+        // what a row has in front of its first line, and the rest from there on
         uint8_t* first = d + lane * pitch;
-        if (reinterpret_cast<uintptr_t>(first) & 2) {
-            if (lane < rows && col < p.N) *reinterpret_cast<uint16_t*>(first) = static_cast<uint16_t>(w[0]);
+        const int skip = to_line(first), have = lane < rows ? min(p.N - col, 4 * COLS) * ES : 0;
+        const int half = skip & 2, four = skip & 4, eight = skip & 8;
+        const bool all = skip <= have;
+        if (!all) {                                                 // the last columns of D
 #pragma unroll
-            for (int e = 0; e < 64; ++e) w[e] = __funnelshift_r(w[e], e < 63 ? w[e + 1] : 0u, 16);
+            for (int e = 0; e < 16 / ES; ++e) {
+                if (e * ES >= have) continue;
+                if (ES == 2) *reinterpret_cast<uint16_t*>(first + 2 * e) = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+                else *reinterpret_cast<uint32_t*>(first + 4 * e) = w[e];
+            }
         }
+        if (ES == 2) {
+            if (all && half) *reinterpret_cast<uint16_t*>(first) = static_cast<uint16_t>(w[0]);
+#pragma unroll
+            for (int e = 0; e < 64; ++e) w[e] = __funnelshift_r(w[e], e < 63 ? w[e + 1] : 0u, half * 8);
+        }
+        if (all && four) *reinterpret_cast<uint32_t*>(first + half) = w[0];
+#pragma unroll
+        for (int e = 0; e < 63; ++e) w[e] = four ? w[e + 1] : w[e];
+        if (all && eight) *reinterpret_cast<uint2*>(first + half + four) = make_uint2(w[0], w[1]);
+#pragma unroll
+        for (int e = 0; e < 62; ++e) w[e] = eight ? w[e + 2] : w[e];
     }
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
@@ -438,10 +460,8 @@ __device__ __forceinline__ void store_words(const PairParams& p, uint8_t* stage,
         // up to the end of the rows, or of these 256 bytes
         const int left = (min(p.N - col, 4 * COLS) - c * COLS) * ES;
         uint8_t* to = d + 64 * c;
-        if (p.unit == 16) store_rows<uint4, ES, false>(stage, to, pitch, rows, left, lane);
-        else if (p.unit == 8) store_rows<uint2, ES, false>(stage, to, pitch, rows, left, lane);
-        else if (p.unit == 4) store_rows<uint32_t, ES, false>(stage, to, pitch, rows, left, lane);
-        else if (ES == 2) store_rows<uint32_t, ES, true>(stage, to, pitch, rows, left, lane);
+        if (p.vec) store_rows<ES, false>(stage, to, pitch, rows, left, lane);
+        else store_rows<ES, true>(stage, to, pitch, rows, left, lane);
     }
 }
 
@@ -685,7 +705,7 @@ cudaError_t launch_pair(const Fp4Product& a, int* status, cudaStream_t s) {
     p.tiles_n = (a.N - 1) / P_BN + 1;
     p.bf16 = a.dtype == MOARA_DTYPE_BF16;
     const uintptr_t d = reinterpret_cast<uintptr_t>(a.D), pitch = static_cast<uintptr_t>(a.ldd) * (p.bf16 ? 2 : 4);
-    p.unit = static_cast<int>(((d | pitch | 16) & (~(d | pitch | 16) + 1)));
+    p.vec = (d | pitch) % 16 == 0;
     p.status = status;
     const cudaError_t e = allow_shared<1>(k_fp4_pair);
     if (e != cudaSuccess) return e;
