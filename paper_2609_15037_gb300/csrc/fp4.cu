@@ -2,7 +2,6 @@
 // matrix, and the values of an operand.  DRAM-bound: per entry 4 or 2 bytes in
 // and 17/32 of a byte out per orientation.
 #include <cuda_bf16.h>
-#include <cuda_fp16.h>
 
 #include "fp4.cuh"
 #include "launch.cuh"
@@ -73,9 +72,18 @@ __global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 ? 2 : ROWS &
     const int row0 = tr * 128 + lr, col0 = tc * 128 + lc;
     const T* X = static_cast<const T*>(p.X) + row0 * p.ld + col0;
     Row<T, N> x[8];
-    if (p.vec && col0 + N <= p.cols && row0 + 8 <= p.rows) {
+    const bool whole = col0 + N <= p.cols && row0 + 8 <= p.rows;
+    // rows on other boundaries: by lines of 16 bytes, while they lie inside the matrix
+    constexpr uintptr_t LINE = 15;
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(p.X);
+    const uintptr_t end = reinterpret_cast<uintptr_t>(static_cast<const T*>(p.X) + (p.rows - 1) * p.ld + p.cols);
+    if (whole && p.vec) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i].load(X + i * p.ld);
+    } else if (whole && (reinterpret_cast<uintptr_t>(X) & ~LINE) >= begin &&
+               (reinterpret_cast<uintptr_t>(X + 7 * p.ld) & ~LINE) + 32 <= end) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i].load_any(X + i * p.ld);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i].load_some(X + i * p.ld, row0 + i < p.rows ? p.cols - col0 : 0);
@@ -161,172 +169,133 @@ __global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 ? 2 : ROWS &
 }
 
 // ---------------------------------------------------------------------------
-// Values of an operand: a thread takes 8 columns.
+// Values of an operand.  Every value is a bf16 number (a code of two bits of exponent and
+// one of mantissa times a power of two from 2^-127 on), so the products are taken two at
+// a time in bf16, exactly, whatever the output's type.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ float scale_value(uint32_t byte) {
-    if (byte == 255u) return __uint_as_float(0x7FC00000u);
-    return byte == 0u ? 0x1p-127f : __uint_as_float(byte << 23);
+// Bytes of the pair {a, b} by the nibbles of sel; a nibble's highest bit asks for the
+// byte's highest bit eight times.
+__device__ __forceinline__ uint32_t permute(uint32_t a, uint32_t b, uint32_t sel) {
+    uint32_t y;
+    asm("prmt.b32 %0, %1, %2, %3;" : "=r"(y) : "r"(a), "r"(b), "r"(sel));
+    return y;
 }
 
-// Eight codes as fp32, by the hardware's conversion of two of them to fp16 (exact).
-__device__ __forceinline__ void values8(uint32_t w, float f, float (&v)[8]) {
-    uint32_t h[4];
-    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
-        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
-        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
-        : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
-        : "r"(w));
+// Eight codes as bf16: 0, 1/2, 1, 3/2, 2, 3, 4, 6 from a table of each byte, then the signs.
+__device__ __forceinline__ void values8(uint32_t w, uint32_t (&h)[4]) {
+    const uint32_t sizes = w & 0x77777777u, even = w << 4;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
-        v[2 * i] = a.x * f;
-        v[2 * i + 1] = a.y * f;
+    for (int i = 0; i < 2; ++i) {
+        const uint32_t sel = sizes >> (16 * i), sign = permute(even, w, i == 0 ? 0xD9C8u : 0xFBEAu);
+        const uint32_t low = permute(0xC0800000u, 0xC0804000u, sel);
+        const uint32_t high = permute(0x3F3F3F00u, 0x40404040u, sel) | (sign & 0x80808080u);
+        h[2 * i] = permute(low, high, 0x5140u);
+        h[2 * i + 1] = permute(low, high, 0x7362u);
     }
+}
+
+// A scale twice as bf16: 2^-127 and NaN are the exponents' ends with the same bit beside them.
+__device__ __forceinline__ uint32_t scale_value(uint32_t byte) {
+    const uint32_t y = byte << 7 | (((byte + 1) & 0xFEu) == 0 ? 0x40u : 0u);
+    return permute(y, y, 0x1010u);
+}
+
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t y;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
+    return y;
 }
 
 struct ValueParams {
     const uint8_t* q;
     const uint8_t* sf;
     int rows, cols, kb, tiles_c;
+    int units;             // threads that a row needs, at most
     int lanes;             // log2 of the threads along a row, up to as many as it needs
     int parts;             // CTAs along a row
     void* out;
     long long ldo;
 };
 
-__device__ __forceinline__ uint32_t scale_at(const ValueParams& p, int row, int block) {
-    return p.sf[(static_cast<long long>(row >> 7) * p.tiles_c + (block >> 2)) * 512 + (row & 31) * 16 +
-                ((row & 127) >> 5) * 4 + (block & 3)];
-}
-
-// Rows of `out` on 16-byte boundaries.  A thread takes 8 columns of four rows, whose
-// loads are issued together; a CTA up to 512 columns, and more rows of a narrow matrix.
-// 11008 x 4096 into bf16: 15.8 us, 7.2 TB/s.
+// A thread takes 16 bytes of the output (8 columns of bf16, 4 of fp32) of four adjacent
+// rows, whose loads are issued together and whose scales lie 16 bytes apart; a CTA up to 64
+// threads of a row, and more rows of a narrow matrix.  11008 x 4096 into bf16: 13.5 us, 8.5
+// TB/s with what L2 keeps; conversions to fp32, products and packing there took 15.8, 95
+// instructions for 16 bytes.
+// ANY: rows of `out` on any boundary.  A thread's 16 bytes are a line of the output all the
+// same: their codes are the last of the thread's in front and the first of its own.  4978 x 5370
+// into bf16: 14.3 us (4992 x 5376: 8.3); rows' words one to a lane through shared memory 25.7.
 constexpr int VALUE_ROWS = 4, VALUE_LANES = 64;
 
-template <class T> __global__ void __launch_bounds__(256) k_fp4_values(const ValueParams p) {
+template <class T, bool ANY> __global__ void __launch_bounds__(256) k_fp4_values(const ValueParams p) {
+    constexpr int N = 16 / sizeof(T), PER = 32 / N;                  // columns of a thread, threads of a block
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int part = blockIdx.x % p.parts, group = blockIdx.x / p.parts, step = 256 >> p.lanes;
-    const int s = (part << p.lanes) + (threadIdx.x & ((1 << p.lanes) - 1)), block = s >> 2, col = 8 * s;
-    const int row0 = group * (step * VALUE_ROWS) + (threadIdx.x >> p.lanes);
-    if (block >= p.kb) return;
-    uint32_t w[VALUE_ROWS], sb[VALUE_ROWS];
+    const int s = (part << p.lanes) + (threadIdx.x & ((1 << p.lanes) - 1));
+    const int row0 = (group * step + (threadIdx.x >> p.lanes)) * VALUE_ROWS, rows = p.rows - row0;
+    if (s >= p.units || rows <= 0) return;
+    const long long pitch = static_cast<long long>(p.kb) * 16;
+    const uint8_t* const q0 = p.q + row0 * pitch;
+    const uint8_t* const sf0 =
+        p.sf + static_cast<long long>(row0 >> 7) * p.tiles_c * 512 + (row0 & 31) * 16 + ((row0 & 127) >> 5) * 4;
+    // codes (in the low bits) and scales of the columns from N * unit on
+    auto fetch = [&](int unit, uint32_t (&w)[VALUE_ROWS], uint32_t (&byte)[VALUE_ROWS]) {
+        const int block = unit / PER;
+        const uint8_t* q = q0 + static_cast<long long>(unit) * (N / 2);
+        const uint8_t* sf = sf0 + static_cast<long long>(block >> 2) * 512 + (block & 3);
 #pragma unroll
-    for (int i = 0; i < VALUE_ROWS; ++i) {
-        const int row = row0 + step * i;
-        w[i] = sb[i] = 0;
-        if (row >= p.rows) continue;
-        w[i] = *reinterpret_cast<const uint32_t*>(p.q + (static_cast<long long>(row) * p.kb + block) * 16 + (s & 3) * 4);
-        sb[i] = scale_at(p, row, block);
-    }
+        for (int i = 0; i < VALUE_ROWS; ++i) {
+            w[i] = byte[i] = 0;
+            if (i >= rows || unit < 0 || block >= p.kb) continue;
+            w[i] = N == 8 ? *reinterpret_cast<const uint32_t*>(q) : *reinterpret_cast<const uint16_t*>(q);
+            byte[i] = sf[16 * i];
+            q += pitch;
+        }
+    };
+    uint32_t w[VALUE_ROWS], sb[VALUE_ROWS], before[VALUE_ROWS], sbefore[VALUE_ROWS];
+    fetch(s, w, sb);
+    if (ANY) fetch(s - 1, before, sbefore);
+    T* o = static_cast<T*>(p.out) + row0 * p.ldo + N * static_cast<long long>(s);
 #pragma unroll
-    for (int i = 0; i < VALUE_ROWS; ++i) {
-        const int row = row0 + step * i;
-        if (row >= p.rows) return;
-        float v[8];
-        values8(w[i], scale_value(sb[i]), v);
-        T* o = static_cast<T*>(p.out) + row * p.ldo + col;
-        if (col + 8 <= p.cols) {
-            if (sizeof(T) == 4) {
-                __stcs(reinterpret_cast<float4*>(o), make_float4(v[0], v[1], v[2], v[3]));
-                __stcs(reinterpret_cast<float4*>(o) + 1, make_float4(v[4], v[5], v[6], v[7]));
-            } else {
-                uint32_t h[4];
+    for (int i = 0; i < VALUE_ROWS; ++i, o += p.ldo) {
+        if (i >= rows) return;
+        // entries of the row's first line that are not the row's
+        const int n = ANY ? static_cast<int>(reinterpret_cast<uintptr_t>(o) & 15) / static_cast<int>(sizeof(T)) : 0;
+        const uint32_t f = scale_value(sb[i]);
+        uint32_t h[4];
+        if (ANY) {
+            values8(N == 8 ? __funnelshift_l(before[i], w[i], 4 * n) : (w[i] << 16 | before[i]) >> (16 - 4 * n), h);
+            const uint32_t pf = scale_value(sbefore[i]);
+            // of each column's scale, which two bytes of {f, pf}
+            uint32_t sel[4];
+            sel[0] = 0x10101010u | __funnelshift_lc(0x44444444u, 0u, 8 * n);
+            sel[2] = 0x10101010u | __funnelshift_lc(0x44444444u, 0u, max(8 * n - 32, 0));
+            sel[1] = sel[0] >> 16;
+            sel[3] = sel[2] >> 16;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * k], v[2 * k + 1]);
-                    h[k] = *reinterpret_cast<const uint32_t*>(&b);
-                }
-                __stcs(reinterpret_cast<uint4*>(o), make_uint4(h[0], h[1], h[2], h[3]));
-            }
+            for (int k = 0; k < N / 2; ++k) h[k] = mul_bf16x2(h[k], permute(f, pf, sel[k]));
+        } else {
+            values8(w[i], h);
+#pragma unroll
+            for (int k = 0; k < N / 2; ++k) h[k] = mul_bf16x2(h[k], f);
+        }
+        if (N == 4) {
+            h[3] = h[1] & 0xFFFF0000u;
+            h[2] = h[1] << 16;
+            h[1] = h[0] & 0xFFFF0000u;
+            h[0] = h[0] << 16;
+        }
+        const int col = N * s - n;
+        T* to = o - n;
+        if (col >= 0 && col + N <= p.cols) {
+            __stcs(reinterpret_cast<uint4*>(to), make_uint4(h[0], h[1], h[2], h[3]));
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (col + e < p.cols) o[e] = static_cast<T>(v[e]);
-        }
-    }
-}
-
-// Rows on any boundary.  A thread works out 8 columns of four rows; a row's words are
-// stored one to a lane, through shared memory, so that a store is contiguous.  In a row
-// of bf16 that begins between two words a thread takes its columns one further on: the
-// first code of its neighbour is its eighth.  11007 x 4097 into bf16 took 127 us with the
-// columns of a thread stored one by one, 74 with two columns to a thread, and takes 45.
-template <class T> __global__ void __launch_bounds__(256) k_fp4_values_any(const ValueParams p) {
-    constexpr int WORDS = 2 * sizeof(T), SHIFT = sizeof(T) == 2 ? 2 : 3;          // of a thread's columns
-    __shared__ __align__(16) uint32_t staged[256 * WORDS];
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int lanes = 1 << p.lanes, at_once = 32 >> p.lanes, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int part = blockIdx.x % p.parts, group = blockIdx.x / p.parts;
-    const int s = part * lanes + (lane & (lanes - 1)), block = s >> 2;
-    const int row0 = (group * 8 + warp) * at_once * VALUE_ROWS;
-    uint8_t* const out = static_cast<uint8_t*>(p.out);
-    const long long pitch = p.ldo * static_cast<long long>(sizeof(T));
-    auto odd_row = [&](int row) {
-        return sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(out + row * pitch) & 2) != 0;
-    };
-    uint32_t w[VALUE_ROWS], next[VALUE_ROWS], s0[VALUE_ROWS], s1[VALUE_ROWS];
-#pragma unroll
-    for (int i = 0; i < VALUE_ROWS; ++i) {
-        const int row = row0 + i * at_once + (lane >> p.lanes);
-        w[i] = next[i] = s0[i] = s1[i] = 0;
-        if (row >= p.rows || block >= p.kb) continue;
-        const uint8_t* q = p.q + (static_cast<long long>(row) * p.kb + block) * 16 + (s & 3) * 4;
-        w[i] = *reinterpret_cast<const uint32_t*>(q);
-        s0[i] = scale_at(p, row, block);
-        if (sizeof(T) == 2 && s + 1 < 4 * p.kb) {
-            next[i] = q[4];
-            s1[i] = (s & 3) == 3 ? scale_at(p, row, block + 1) : s0[i];
-        }
-    }
-    uint32_t* const mine = staged + warp * (32 * WORDS);
-#pragma unroll
-    for (int i = 0; i < VALUE_ROWS; ++i) {
-        const int row = row0 + i * at_once + (lane >> p.lanes);
-        const bool odd = row < p.rows && odd_row(row);
-        float v[9];
-        {
-            float x[8];
-            values8(w[i], scale_value(s0[i]), x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = x[e];
-        }
-        if (sizeof(T) == 2) {
-            float x[8];
-            values8(next[i], scale_value(s1[i]), x);
-            v[8] = x[0];
-            if (odd && s == 0) *reinterpret_cast<T*>(out + row * pitch) = static_cast<T>(v[0]);
-        }
-        __syncwarp();
-        uint32_t h[8];
-#pragma unroll
-        for (int k = 0; k < WORDS; ++k) {
-            if (sizeof(T) == 4) {
-                h[k] = __float_as_uint(v[k]);
-            } else {
-                const __nv_bfloat162 y = __floats2bfloat162_rn(odd ? v[2 * k + 1] : v[2 * k], odd ? v[2 * k + 2] : v[2 * k + 1]);
-                h[k] = *reinterpret_cast<const uint32_t*>(&y);
+            for (int e = 0; e < N; ++e) {
+                if (col + e < 0 || col + e >= p.cols) continue;
+                if constexpr (N == 4) reinterpret_cast<uint32_t*>(to)[e] = h[e];
+                else reinterpret_cast<uint16_t*>(to)[e] = static_cast<uint16_t>(h[e / 2] >> (16 * (e & 1)));
             }
-        }
-#pragma unroll
-        for (int k = 0; k < WORDS; k += 4)
-            *reinterpret_cast<uint4*>(mine + lane * WORDS + k) = make_uint4(h[k], h[k + 1], h[k + 2], h[k + 3]);
-        __syncwarp();
-#pragma unroll
-        for (int k = 0; k < WORDS; ++k) {
-            const int x = k * 32 + lane, r = row0 + i * at_once + (x >> (p.lanes + SHIFT));
-            const int word = x & ((lanes << SHIFT) - 1);
-            if (r >= p.rows) break;
-            uint8_t* row_at = out + r * pitch;
-            const int shift = odd_row(r) ? 1 : 0;
-            const int col = part * lanes * 8 + word * (4 / static_cast<int>(sizeof(T))) + shift;
-            if (col + static_cast<int>(4 / sizeof(T)) <= p.cols)
-                *reinterpret_cast<uint32_t*>(row_at + static_cast<long long>(col) * sizeof(T)) = mine[x];
-            else if (sizeof(T) == 2 && col < p.cols)
-                *reinterpret_cast<uint16_t*>(row_at + static_cast<long long>(col) * 2) = static_cast<uint16_t>(mine[x]);
         }
     }
 }
@@ -375,13 +344,13 @@ cudaError_t launch_fp4_dequantize(const void* q, const void* sf, int rows, int c
     p.ldo = ldo;
     const bool bf = dtype == MOARA_DTYPE_BF16;
     const bool vec = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ldo % (bf ? 8 : 4) == 0;
-    const int units = 4 * p.kb;
-    while ((1 << p.lanes) < units && (1 << p.lanes) < (vec ? VALUE_LANES : 32)) ++p.lanes;
-    p.parts = ((units - 1) >> p.lanes) + 1;
+    p.units = (cols - 1) / (bf ? 8 : 4) + (vec ? 1 : 2);
+    while ((1 << p.lanes) < p.units && (1 << p.lanes) < VALUE_LANES) ++p.lanes;
+    p.parts = ((p.units - 1) >> p.lanes) + 1;
     const int per = (256 >> p.lanes) * VALUE_ROWS;
     const unsigned int grid = static_cast<unsigned int>(p.parts) * ((rows - 1) / per + 1);
-    auto fn = vec ? (bf ? k_fp4_values<__nv_bfloat16> : k_fp4_values<float>)
-                  : (bf ? k_fp4_values_any<__nv_bfloat16> : k_fp4_values_any<float>);
+    auto fn = vec ? (bf ? k_fp4_values<__nv_bfloat16, false> : k_fp4_values<float, false>)
+                  : (bf ? k_fp4_values<__nv_bfloat16, true> : k_fp4_values<float, true>);
     ++*launches;
     // begins early, but lets nothing begin beside itself: CTAs that wait would take its own
     // CTAs' places (both orientations of a 509 x 2049 matrix 19.2 us instead of 16.6)

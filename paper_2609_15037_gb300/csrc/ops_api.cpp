@@ -68,8 +68,8 @@ int check_adamw(moara_ctx* ctx, int i, const moara_adamw_tensor& t, float lr) {
 
 int check_matrix(moara_ctx* ctx, const char* what, int rows, int cols) {
     if (rows < 1 || cols < 1) return fail(ctx, MOARA_ERR_SHAPE, "%s: rows and columns must be >= 1", what);
-    // indexes run up to a tile behind the last row and column
-    if (rows > INT_MAX - 512 || cols > INT_MAX - 512 ||
+    // indexes run up to a CTA's share behind the last row and column
+    if (rows > INT_MAX - 2048 || cols > INT_MAX - 2048 ||
         static_cast<long long>(moara::fp4_tiles(rows)) * moara::fp4_tiles(cols) > INT_MAX / 64)
         return fail(ctx, MOARA_ERR_SHAPE, "%s: the matrix is too large", what);
     return MOARA_OK;
