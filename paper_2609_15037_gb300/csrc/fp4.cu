@@ -73,17 +73,18 @@ __global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 ? 2 : ROWS &
     const T* X = static_cast<const T*>(p.X) + row0 * p.ld + col0;
     Row<T, N> x[8];
     const bool whole = col0 + N <= p.cols && row0 + 8 <= p.rows;
-    // rows on other boundaries: by lines of 16 bytes, while they lie inside the matrix
-    constexpr uintptr_t LINE = 15;
+    // rows on other boundaries: by lines of 8 bytes, while they lie inside the matrix.  Eight
+    // rows further a row begins on the same byte of its line.
+    constexpr uintptr_t LINE = 7;
     const uintptr_t begin = reinterpret_cast<uintptr_t>(p.X);
     const uintptr_t end = reinterpret_cast<uintptr_t>(static_cast<const T*>(p.X) + (p.rows - 1) * p.ld + p.cols);
     if (whole && p.vec) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i].load(X + i * p.ld);
     } else if (whole && (reinterpret_cast<uintptr_t>(X) & ~LINE) >= begin &&
-               (reinterpret_cast<uintptr_t>(X + 7 * p.ld) & ~LINE) + 32 <= end) {
+               (reinterpret_cast<uintptr_t>(X + 7 * p.ld) & ~LINE) + 24 <= end) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i].load_any(X + i * p.ld);
+        for (int i = 0; i < 8; ++i) x[i].load_any(X + i * p.ld, static_cast<int>((begin + i * p.ld * sizeof(T)) & LINE));
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i].load_some(X + i * p.ld, row0 + i < p.rows ? p.cols - col0 : 0);

@@ -63,21 +63,20 @@ __device__ __forceinline__ uint32_t max_nan2(uint32_t a, uint32_t b) {
     return y;
 }
 
-// The 16 bytes at p, on any boundary of an entry, from the two lines of 16 bytes that
-// hold them.  Both orientations of 4978 x 5370 in bf16 take 18.6 us, entry by entry 25.0
-// (4992 x 5376, whose rows are aligned: 13.9).
-template <int SIZE> __device__ __forceinline__ void load_lines(const void* p, uint32_t (&w)[4]) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-    const uint4* line = reinterpret_cast<const uint4*>(at & ~static_cast<uintptr_t>(15));
-    const uint4 a = line[0], b = line[1];
-    uint32_t t[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    const bool eight = (at & 8) != 0, four = (at & 4) != 0;
-#pragma unroll
-    for (int e = 0; e < 6; ++e) t[e] = eight ? t[e + 2] : t[e];
+// The 16 bytes at p, on any boundary of an entry, from the three lines of 8 bytes that
+// hold them.  offset: p's place in the first, the same in every thread.  Both orientations
+// of 4199 x 12909 take 36.2 us in bf16 and 52.8 in fp32 (12912 columns, whose rows are
+// aligned: 31.6 and 44.3); from two lines of 16 bytes 36.9 and 59.5, from words 38.5 and
+// 61.1; of 4978 x 5370 in bf16 18.2, entry by entry 25.0.
+template <int SIZE> __device__ __forceinline__ void load_lines(const void* p, int offset, uint32_t (&w)[4]) {
+    const uint2* line = reinterpret_cast<const uint2*>(reinterpret_cast<uintptr_t>(p) - offset);
+    const uint2 a = line[0], b = line[1], c = line[2];
+    uint32_t t[6] = {a.x, a.y, b.x, b.y, c.x, c.y};
+    const bool four = (offset & 4) != 0;
 #pragma unroll
     for (int e = 0; e < 5; ++e) t[e] = four ? t[e + 1] : t[e];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = SIZE == 2 ? __funnelshift_r(t[e], t[e + 1], (at & 2) * 8) : t[e];
+    for (int e = 0; e < 4; ++e) w[e] = SIZE == 2 ? __funnelshift_r(t[e], t[e + 1], (offset & 2) * 8) : t[e];
 }
 
 template <class T, int N> struct Row;
@@ -91,7 +90,7 @@ template <int N> struct Row<float, N> {
             w[e] = a.x; w[e + 1] = a.y; w[e + 2] = a.z; w[e + 3] = a.w;
         }
     }
-    __device__ __forceinline__ void load_any(const float* p) { load_lines<4>(p, w); }
+    __device__ __forceinline__ void load_any(const float* p, int offset) { load_lines<4>(p, offset, w); }
     __device__ __forceinline__ void load_some(const float* p, int count) {
 #pragma unroll
         for (int e = 0; e < N; ++e) w[e] = e < count ? __float_as_uint(p[e]) : 0u;
@@ -122,7 +121,7 @@ template <> struct Row<__nv_bfloat16, 8> {
         const uint4 a = *reinterpret_cast<const uint4*>(p);
         w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
     }
-    __device__ __forceinline__ void load_any(const __nv_bfloat16* p) { load_lines<2>(p, w); }
+    __device__ __forceinline__ void load_any(const __nv_bfloat16* p, int offset) { load_lines<2>(p, offset, w); }
     __device__ __forceinline__ void load_some(const __nv_bfloat16* p, int count) {
         const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
 #pragma unroll

@@ -377,3 +377,62 @@ def test_values_on_any_boundary(M, fp4, shape):
             fp4.dequantize(A, out=out[:, :k])
             same(f64(out)[:, :k], want)
             assert (out[:, k:] == 7).all() and (buf[:offset] == 7).all()
+
+
+def placed(m, k, dtype, first, pitch):
+    """An m x k matrix that begins `first` entries into its memory, whose surroundings are NaN."""
+    whole = torch.full((first + m * pitch + 64,), float("nan"), device="cuda", dtype=dtype)
+    return whole, whole[first:first + m * pitch].view(m, pitch)[:, :k]
+
+
+def surroundings_kept(whole, x):
+    kept = whole.clone()
+    kept[x.storage_offset():].as_strided(x.shape, x.stride()).fill_(float("nan"))
+    return bool(torch.isnan(kept).all())
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("first,extra", [(0, 1), (1, 0), (2, 3), (3, 6), (4, 4), (5, 9), (6, 2), (7, 5)])
+def test_boundaries_of_rows(M, fp4, dtype, first, extra):
+    """Rows that begin on every byte of a line give the bits that aligned rows give, and
+    nothing beside them is written or read into the result."""
+    m, k, n = 301, 1091, 5003
+    x = torch.randn(m, k, device="cuda").to(dtype)
+    # the pitch 1104 is aligned
+    a, at = fp4.quantize(placed_copy(x, 0, 1104), rows=True, cols=True)
+    b, bt = fp4.quantize(placed_copy(x, first, k + extra), rows=True, cols=True)
+    for y, z in ((a, b), (at, bt)):
+        assert torch.equal(y.q, z.q) and torch.equal(y.sf, z.sf)
+    for op in (a, at):
+        want = torch.empty(op.rows, 1104 if op.cols == k else 304, device="cuda", dtype=dtype)[:, :op.cols]
+        fp4.dequantize(op, out=want)
+        whole, got = placed(op.rows, op.cols, dtype, first, op.cols + extra)
+        fp4.dequantize(op, out=got)
+        assert torch.equal(got, want) and surroundings_kept(whole, got)
+    w = fp4.quantize(torch.randn(n, k, device="cuda"))               # 2 x 20 tiles: pairs
+    want = torch.empty(m, 5008, device="cuda", dtype=dtype)[:, :n]
+    fp4.product(a, w, out=want)
+    whole, got = placed(m, n, dtype, first, n + extra)
+    fp4.product(a, w, out=got)
+    assert torch.equal(got, want) and surroundings_kept(whole, got)
+
+
+def placed_copy(x, first, pitch):
+    y = placed(*x.shape, x.dtype, first, pitch)[1]
+    y.copy_(x)
+    return y
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("last", range(1, 10))
+def test_last_columns_of_pairs(M, fp4, dtype, last):
+    """A last tile, or half of one, of a few columns on every boundary."""
+    m, k = 2305, 64                                                  # 10 x 3 tiles
+    a = fp4.quantize(torch.randn(m, k, device="cuda"))
+    for n in (512 + last, 640 + last):
+        w = fp4.quantize(torch.randn(n, k, device="cuda"))
+        want = torch.empty(m, 784, device="cuda", dtype=dtype)[:, :n]
+        fp4.product(a, w, out=want)
+        whole, got = placed(m, n, dtype, last, n)
+        fp4.product(a, w, out=got)
+        assert torch.equal(got, want) and surroundings_kept(whole, got)
