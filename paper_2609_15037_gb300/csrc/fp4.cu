@@ -222,7 +222,7 @@ struct ValueParams {
 // rows, whose loads are issued together and whose scales lie 16 bytes apart; a CTA up to 64
 // threads of a row, and more rows of a narrow matrix.  11008 x 4096 into bf16: 13.5 us, 8.5
 // TB/s with what L2 keeps; conversions to fp32, products and packing there took 15.8, 95
-// instructions for 16 bytes.
+// instructions for 16 bytes instead of 65.
 // ANY: rows of `out` on any boundary.  A thread's 16 bytes are a line of the output all the
 // same: their codes are the last of the thread's in front and the first of its own.  4978 x 5370
 // into bf16: 14.3 us (4992 x 5376: 8.3); rows' words one to a lane through shared memory 25.7.
