@@ -38,6 +38,7 @@ def _current_stream(device):
 
 # the same without building a Stream object (1 us of a call's 5 to 10)
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
+_recording = torch.cuda.is_current_stream_capturing
 
 
 def stream_handle(stream, device):
@@ -148,16 +149,17 @@ class AdamWGroup:
             B._check(code, self.ctx, "moara_adamw_moments")
         return exp_avg, exp_avg_sq
 
-    def _norm_workspace(self, count, handle, stream):
-        with allocating_on(stream, self.device):
-            # a recorded graph has its own, which no later call replaces or shares
-            recorded = torch.cuda.is_current_stream_capturing()
-            ws, room = (None, -1) if recorded else self._workspace.get(handle, (None, -1))
-            if count > room:
-                ws = torch.zeros(B.moara_grad_norm_workspace_bytes(count), dtype=torch.uint8, device=self._dev)
-                if not recorded:
-                    self._workspace[handle] = ws, count
-        return ws
+    def _norm_workspace(self, count, handle):
+        """(tensor, address, bytes, gradients that it serves); zero before its first call."""
+        # a recorded graph has its own, which no later call replaces or shares
+        recorded = _recording()
+        kept = None if recorded else self._workspace.get(handle)
+        if kept is None or count > kept[3]:
+            ws = torch.zeros(B.moara_grad_norm_workspace_bytes(count), dtype=torch.uint8, device=self._dev)
+            kept = ws, ws.data_ptr(), ws.numel(), count
+            if not recorded:
+                self._workspace[handle] = kept
+        return kept
 
     def grad_norm(self, grads, max_norm=0.0, extra_sq=None, out=None, stream=None):
         """{sum of squares, norm, clipping coefficient} of any gradients (fp32 or
@@ -165,14 +167,14 @@ class AdamWGroup:
         tensor added to the sum under the root, or None.  The first element is
         what MoaraGroup.set_clip_extra takes, the last what step takes."""
         grads = _listed(grads)
-        handle = stream_handle(stream, self.device)
-        ws = self._norm_workspace(len(grads), handle, stream)
-        args = (_NORM, self.ctx, grads, max_norm, extra_sq, out, ws.data_ptr(), ws.numel(), self.device, handle)
         if stream is None:
-            got = _host.grad_norm(*args)
+            handle = _current_stream(self.device)
+            ws = self._norm_workspace(len(grads), handle)
+            got = _host.grad_norm(_NORM, self.ctx, grads, max_norm, extra_sq, out, ws[1], ws[2], self.device, handle)
         else:
             with allocating_on(stream, self.device):
-                got = _host.grad_norm(*args)
+                ws = self._norm_workspace(len(grads), int(stream))
+                got = _host.grad_norm(_NORM, self.ctx, grads, max_norm, extra_sq, out, ws[1], ws[2], self.device, int(stream))
         if got.__class__ is int:
             B._check(got, self.ctx, "moara_grad_norm")
         return got
