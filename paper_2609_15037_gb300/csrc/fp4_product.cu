@@ -742,9 +742,16 @@ cudaError_t launch_few(const Fp4Product& a, bool early, int* status, cudaStream_
     const long long tiles = static_cast<long long>(p.tiles_n) * ((a.M - 1) / 128 + 1);
     // K over more CTAs while they are at most 5/4 of the SMs: with N = K = 4096 a token
     // takes 4.9 us in clusters of four (128 CTAs) and 7.2 in clusters of eight (256), with N
-    // = 11008 6.6 in clusters of two (172) and 7.9 without
+    // = 11008 6.6 in clusters of two (172) and 7.9 without.  Beyond half of the SMs the sums of
+    // more than 32 tokens only repay a long K: 128 tokens, N = 2048, K = 2048 take 6.2 us in
+    // clusters of four (64 CTAs) and 8.7 in clusters of eight; N = 4864, K = 2048 7.5 in
+    // clusters of two (76) and 8.6 of four, but K = 11008 12.9 and 12.0
     p.split = 1;
-    while (p.split < 8 && 2 * p.split <= steps && tiles * 2 * p.split <= 190) p.split *= 2;
+    const auto pays = [&](int split) {
+        const long long ctas = tiles * split;
+        return split <= steps && (ctas <= 76 || (ctas <= 190 && (p.nt <= 32 || split * split <= steps)));
+    };
+    while (p.split < 8 && pays(2 * p.split)) p.split *= 2;
     p.stages = std::min(p.nt > 64 ? F_STAGES - 1 : F_STAGES, (steps - 1) / p.split + 1);    // two CTAs fit an SM
     const int stage = OPERAND + p.nt * (BK / 2) + 2 * SF_BYTES;
     p.ctl = (std::max(p.stages * stage, p.nt * 512) + 15) / 16 * 16;
