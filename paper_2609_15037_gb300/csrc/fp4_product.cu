@@ -97,7 +97,8 @@ __device__ __forceinline__ void load_x(const FewParams& p, int row, int col, Row
     else x.load_some(src, p.K - col);
 }
 
-template <bool QUANT, class T>
+// MANY: a CTA's share of the tokens is added up and stored four tokens at a time.
+template <bool QUANT, class T, bool MANY>
 __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ FewParams p) {
     extern __shared__ uint8_t raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
@@ -289,20 +290,8 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
         const int tokens = min(p.nt, p.M - m0), share = (tokens + p.split - 1) / p.split;
         const int t1 = min(tokens, (rank + 1) * share), col = n0 + 4 * lane;
         const uint32_t own = ptx::smem_u32(smem) + 16 * lane;
-        uint32_t from[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) from[r] = ptx::mapa(own, r < p.split ? r : 0);
-        for (int t = rank * share + warp; t < t1; t += F_THREADS / 32) {
-            float4 part[8];                                         // requested together
-#pragma unroll
-            for (int r = 0; r < 8; ++r)
-                if (r < p.split) part[r] = ld_cluster_f4(from[r] + t * 512);
-            float4 sum = part[0];
-#pragma unroll
-            for (int r = 1; r < 8; ++r) {
-                if (r >= p.split) break;
-                sum.x += part[r].x; sum.y += part[r].y; sum.z += part[r].z; sum.w += part[r].w;
-            }
+        constexpr int WARPS = F_THREADS / 32;
+        auto put = [&](int t, const float4& sum) {
             const long long at = (m0 + t) * p.ldd + col;
             const float v[4] = {sum.x, sum.y, sum.z, sum.w};
             if (p.vec && col + 4 <= p.N) {
@@ -317,6 +306,46 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
                     if (p.bf16) static_cast<__nv_bfloat16*>(p.D)[at + e] = __float2bfloat16_rn(v[e]);
                     else static_cast<float*>(p.D)[at + e] = v[e];
                 }
+            }
+        };
+        // what is read together: a token from each of up to eight CTAs, or four of many tokens
+        // from one or two (128 x 8192 x 600: 7.0 us, token by token 9.2); in one kernel the two
+        // take a single token 0.1 us longer
+        if constexpr (MANY) {
+            const uint32_t a = ptx::mapa(own, 0), b = ptx::mapa(own, p.split - 1);
+            for (int t0 = rank * share + warp; t0 < t1; t0 += 4 * WARPS) {
+                float4 x[4], y[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = min(t0 + i * WARPS, t1 - 1);
+                    x[i] = ld_cluster_f4(a + t * 512);
+                    if (p.split == 2) y[i] = ld_cluster_f4(b + t * 512);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (t0 + i * WARPS >= t1) break;
+                    if (p.split == 2) {
+                        x[i].x += y[i].x; x[i].y += y[i].y; x[i].z += y[i].z; x[i].w += y[i].w;
+                    }
+                    put(t0 + i * WARPS, x[i]);
+                }
+            }
+        } else {
+            uint32_t from[8];
+#pragma unroll
+            for (int r = 0; r < 8; ++r) from[r] = ptx::mapa(own, r < p.split ? r : 0);
+            for (int t = rank * share + warp; t < t1; t += WARPS) {
+                float4 part[8];
+#pragma unroll
+                for (int r = 0; r < 8; ++r)
+                    if (r < p.split) part[r] = ld_cluster_f4(from[r] + t * 512);
+                float4 sum = part[0];
+#pragma unroll
+                for (int r = 1; r < 8; ++r) {
+                    if (r >= p.split) break;
+                    sum.x += part[r].x; sum.y += part[r].y; sum.z += part[r].z; sum.w += part[r].w;
+                }
+                put(t, sum);
             }
         }
     }
@@ -756,21 +785,26 @@ cudaError_t launch_few(const Fp4Product& a, bool early, int* status, cudaStream_
     const int stage = OPERAND + p.nt * (BK / 2) + 2 * SF_BYTES;
     p.ctl = (std::max(p.stages * stage, p.nt * 512) + 15) / 16 * 16;
     const int smem = 1024 + p.ctl + static_cast<int>(sizeof(FewCtl));
-    const cudaError_t e = allow_shared<QUANT ? sizeof(T) : 0>(k_fp4_few<QUANT, T>);
+    const int share = (std::min(p.nt, a.M) - 1) / p.split + 1;
+    const bool many = !QUANT && p.split <= 2 && share > 2 * (F_THREADS / 32);
+    const auto fn = many ? k_fp4_few<QUANT, T, !QUANT> : k_fp4_few<QUANT, T, false>;
+    const cudaError_t e = many ? allow_shared<8>(fn) : allow_shared<QUANT ? sizeof(T) : 0>(fn);
     if (e != cudaSuccess) return e;
     // begins beside the end of the launch in front where it is short or leaves room: a token
     // through 4096 x 4096 4.4 instead of 4.9 us in a row of them.  Otherwise two of its CTAs
     // share an SM while others idle (128 x 4096 x 4096: 8.8 us instead of 8.0)
     const bool overlap = early || p.nt <= 32 || tiles * p.split <= 76;
-    return launch_if(overlap, k_fp4_few<QUANT, T>, dim3(static_cast<unsigned int>(tiles * p.split)), dim3(F_THREADS), smem,
+    return launch_if(overlap, fn, dim3(static_cast<unsigned int>(tiles * p.split)), dim3(F_THREADS), smem,
                      s, p.split, p);
 }
 
-// Pairs where their tiles occupy a quarter of the GPU and more, the other form below
-// that: with 32 tiles (512 x 4096 x 4096) 10.0 us against 12.6, with 24 (1500 x 1003 x 2049)
-// 11.9 against 14.2, with 16 (512 x 2048 x 4096) 9.8 against 9.7.
+// Pairs where their tiles occupy a quarter of the GPU and more, and a sixth where K is
+// short; the other form, which shares K, below that.  20 tiles (512 x 2560 x 4096): 9.7 us against
+// 10.3; 16 (512 x 2048): 9.6 against 8.9, but with K = 2048 7.3 against 7.7; 12 (512 x 1536 x 2048) 7.3
+// against 7.5.
 bool large(const Fp4Product& a) {
-    return static_cast<long long>((a.M - 1) / P_BM + 1) * ((a.N - 1) / P_BN + 1) >= 19 && a.M > 128;
+    const long long tiles = static_cast<long long>((a.M - 1) / P_BM + 1) * ((a.N - 1) / P_BN + 1);
+    return tiles >= (a.K <= 2048 ? 12 : 19) && a.M > 128;
 }
 
 }  // namespace
