@@ -156,6 +156,15 @@ def test_product(M, fp4, shape, dtype):
         assert torch.equal(fp4.linear(src, W, dtype=DT[dtype]), got)
 
 
+@pytest.mark.parametrize("shape", [(12, 128, 64), (13, 131, 64), (25, 128, 600), (48, 2600, 2048), (100, 9001, 300),
+                                   (128, 2060, 2300), (260, 40, 100), (385, 200, 600), (1025, 640, 2049), (1030, 640, 2048)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_product_at_the_ends_of_its_forms(M, fp4, shape, dtype):
+    """Around the sizes where the tokens of a CTA are added up four at a time, K is shared
+    by more CTAs, and pairs take over; last tiles of few tokens."""
+    test_product(M, fp4, shape, dtype)
+
+
 @pytest.mark.parametrize("shape", [(1, 300, 520), (40, 300, 520), (300, 300, 520)])
 def test_scales_of_the_whole_range(M, fp4, shape):
     """Scales 2^-127 to 2^126 on both sides, block by block, whose products stay
