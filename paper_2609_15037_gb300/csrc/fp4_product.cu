@@ -38,7 +38,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // a cluster of up to eight CTAs shares K, and each adds the others' sums for its
 // share of the tokens through shared memory.  Bound by latency (launch, one trip
 // to memory, the sums) up to some hundred tokens, then by the operands' way from L2:
-// with N = K = 4096 one token takes 4.7 us, 64 tokens 6.8, 256 9.7.  (A warp per two rows of
+// with N = K = 4096 one token takes 4.7 us, 48 tokens 6.3, 128 8.1, 256 8.9.  (A warp per two rows of
 // the weight without tensor cores takes 4.7 us for a token there and 7.2 against 6.0 with
 // N = 11008: the conversions bound it.)
 // With QUANT, A comes as it is (at most 8 rows) and the four epilogue warps
