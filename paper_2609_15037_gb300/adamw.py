@@ -7,6 +7,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import struct
+import types
 
 import numpy as np
 import torch
@@ -56,6 +57,8 @@ def allocating_on(stream, device):
 class AdamWGroup:
     """Tensors that take AdamW steps together, with their moments.
 
+    A registered tensor whose storage is replaced (an assignment to .data, module.to) is
+    followed to its new place and type, and refused where it no longer fits.
     Streams are cudaStream_t handles; None is torch's current stream."""
 
     def __init__(self, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, device=0):
@@ -65,6 +68,7 @@ class AdamWGroup:
         self.ctx = B.moara_create(B.moara_default_hparams(), device)
         self._dev = torch.device("cuda", device)
         self.params, self.copies, self.states = [], [], []
+        self._kept = []         # of each tensor: param, copy, and the four tensors of its moments
         self._table, self._room, self._all = np.zeros(0, _DESC), 0, None
         self._workspace = {}
 
@@ -75,6 +79,22 @@ class AdamWGroup:
             raise ValueError(f"{what}: {x.numel()} entries, expected {n}")
         return x
 
+    def _check_kept(self, kept, n, state):
+        """Checks a tensor's (param, copy, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale), the
+        last two None for f32 moments; their addresses."""
+        param, copy, *moments = kept
+        self._check(param, "param", n)
+        if copy is not None:
+            self._check(copy, "copy", n, (torch.bfloat16,))
+        code = torch.uint8 if state == "block8" else torch.float32
+        self._check(moments[0], "exp_avg", n, (code,))
+        self._check(moments[1], "exp_avg_sq", n, (code,))
+        if state == "block8":
+            blocks = -(-n // B.MOARA_ADAMW_BLOCK)
+            self._check(moments[2], "exp_avg_scale", blocks, (torch.float32,))
+            self._check(moments[3], "exp_avg_sq_scale", blocks, (torch.float32,))
+        return [0 if x is None else x.data_ptr() for x in kept]
+
     def add(self, param, copy=None, state="f32", weight_decay=0.0, lr_scale=1.0, exp_avg=None, exp_avg_sq=None,
             exp_avg_scale=None, exp_avg_sq_scale=None, id=None):
         """Registers `param` (fp32 or bf16, updated in place) and returns its
@@ -84,26 +104,26 @@ class AdamWGroup:
         index)."""
         if state not in _STATES:
             raise ValueError(f"state must be one of {tuple(_STATES)}")
-        n = self._check(param, "param").numel()
-        if copy is not None:
-            self._check(copy, "copy", n, (torch.bfloat16,))
-        code = torch.uint8 if state == "block8" else torch.float32
+        n = param.numel()
         blocks = -(-n // B.MOARA_ADAMW_BLOCK)
 
-        def kept(x, what, size, dtype):
-            return torch.zeros(size, dtype=dtype, device=self._dev) if x is None else self._check(x, what, size, (dtype,))
-        s = {"exp_avg": kept(exp_avg, "exp_avg", n, code), "exp_avg_sq": kept(exp_avg_sq, "exp_avg_sq", n, code)}
+        def kept(x, size, dtype):
+            return torch.zeros(size, dtype=dtype, device=self._dev) if x is None else x
+        code = torch.uint8 if state == "block8" else torch.float32
+        s = {"exp_avg": kept(exp_avg, n, code), "exp_avg_sq": kept(exp_avg_sq, n, code)}
         if state == "block8":
-            s["exp_avg_scale"] = kept(exp_avg_scale, "exp_avg_scale", blocks, torch.float32)
-            s["exp_avg_sq_scale"] = kept(exp_avg_sq_scale, "exp_avg_sq_scale", blocks, torch.float32)
+            s["exp_avg_scale"] = kept(exp_avg_scale, blocks, torch.float32)
+            s["exp_avg_sq_scale"] = kept(exp_avg_sq_scale, blocks, torch.float32)
+        tensors = param, copy, *s.values(), *(None,) * (4 - len(s))
+        p, c, *at = self._check_kept(tensors, n, state)
         i = len(self.params)
         self._grow(i + 1)
-        at = [x.data_ptr() for x in s.values()] + [0] * (4 - len(s))
-        _PACK.pack_into(self._table, i * _SIZE, n, param.data_ptr(), 0, 0 if copy is None else copy.data_ptr(), *at,
+        _PACK.pack_into(self._table, i * _SIZE, n, p, 0, c, *at,
                         _TYPES[param.dtype], 0, _STATES[state], i if id is None else id, weight_decay, lr_scale)
         self.params.append(param)
         self.copies.append(copy)
-        self.states.append(s)
+        self.states.append(types.MappingProxyType(s))
+        self._kept.append(tensors)
         return i
 
     def _grow(self, count):
@@ -115,36 +135,64 @@ class AdamWGroup:
         self._all = None
 
     def _chosen(self, ids):
-        """The descriptors of a call, and their address."""
+        """The descriptors of a call, their address, and the tensors behind them."""
         if self._all is None:                       # they and their address are kept
-            self._all = self._table[:len(self.params)], self._table.ctypes.data
+            self._all = self._table[:len(self.params)], self._table.ctypes.data, self._kept
         if ids is None:
             return self._all
-        d = self._all[0][list(ids)]
-        return d, d.ctypes.data
+        rows = np.arange(len(self.params))[list(ids)]
+        d = self._all[0][rows]
+        return d, d.ctypes.data, [self._kept[i] for i in rows.tolist()]
+
+    def _follow(self):
+        """The descriptors of tensors whose storage was replaced (an assignment to .data,
+        module.to): their new places and types.  One that no longer fits is refused."""
+        d, places = self._table[:len(self.params)], []
+        for x, n, state in zip(self._kept, d["n"].tolist(), d["state_dtype"].tolist()):
+            places.append(self._check_kept(x, n, "block8" if state == B.MOARA_DTYPE_BLOCK8 else "f32"))
+            for y in x:
+                if y is not None and y.untyped_storage().nbytes() < (y.storage_offset() + y.numel()) * y.element_size():
+                    raise ValueError("the storage of a registered tensor was freed")
+        fields = "param", "param_bf16", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"
+        for name, column in zip(fields, zip(*places)):
+            d[name] = column
+        d["param_dtype"] = [_TYPES[x[0].dtype] for x in self._kept]
+
+    def _called(self, ids, call):
+        """The code of call(count, descriptors' address, kept tensors), which is made again
+        where it found tensors in other places."""
+        ids = ids if ids is None else list(ids)
+        for _ in range(2):
+            d, at, kept = self._chosen(ids)
+            code = call(len(d), at, kept)
+            if code is not None:
+                return code
+            self._follow()
+        raise RuntimeError("registered tensors change during the call")
 
     def step(self, grads, t, lr, grad_scale=None, ids=None, stream=None):
         """One AdamW step at step t (1-based): grads[i] (fp32 or bf16) of every
         registered tensor, or of those in ids.  grad_scale: a one-element
         float32 device tensor that multiplies every gradient, or None."""
-        d, at = self._chosen(ids)
-        code = _host.adamw_step(_STEP, self.ctx, len(d), at, _listed(grads), ctypes.addressof(self.hp), t, lr, grad_scale,
-                                self.device, stream_handle(stream, self.device))
+        grads = _listed(grads)
+        code = self._called(ids, lambda n, at, kept: _host.adamw_step(
+            _STEP, self.ctx, n, at, grads, ctypes.addressof(self.hp), t, lr, grad_scale, self.device,
+            stream_handle(stream, self.device), kept))
         if code:
             B._check(code, self.ctx, "moara_adamw_step")
 
     def moments(self, exp_avg=None, exp_avg_sq=None, ids=None, stream=None):
         """The moments as fp32 tensors (lists, one per tensor); into the given
         ones, if any."""
-        d, at = self._chosen(ids)
-        n = len(d)
+        ids = ids if ids is None else list(ids)
         if exp_avg is None or exp_avg_sq is None:
-            sizes = d["n"].tolist()
+            sizes = self._chosen(ids)[0]["n"].tolist()
             with allocating_on(stream, self.device):
                 exp_avg, exp_avg_sq = ([torch.empty(k, device=self._dev) for k in sizes] if x is None else x
                                        for x in (exp_avg, exp_avg_sq))
-        code = _host.adamw_moments(_MOMENTS, self.ctx, n, at, _listed(exp_avg), _listed(exp_avg_sq), self.device,
-                                   stream_handle(stream, self.device))
+        m, v = _listed(exp_avg), _listed(exp_avg_sq)
+        code = self._called(ids, lambda n, at, kept: _host.adamw_moments(
+            _MOMENTS, self.ctx, n, at, m, v, self.device, stream_handle(stream, self.device), kept))
         if code:
             B._check(code, self.ctx, "moara_adamw_moments")
         return exp_avg, exp_avg_sq

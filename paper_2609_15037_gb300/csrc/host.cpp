@@ -74,10 +74,45 @@ PyObject* caught(const std::exception& e) {
     return nullptr;
 }
 
-// adamw_step(entry, ctx, count, descriptors, gradients, hparams, t, lr, grad_scale, device, stream)
-// -> error code.  The gradients' addresses and types go into the descriptors.
+// Whether `o` is still what a descriptor was made from: None for no address, or a
+// contiguous tensor of this type and size at it.  A tensor keeps its identity while its
+// storage is replaced (an assignment to .data, module.to).
+bool in_place(PyObject* o, const void* at, at::ScalarType type, int64_t entries) {
+    if (!THPVariable_Check(o)) return o == Py_None && at == nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.scalar_type() == type && t.numel() == entries && t.is_contiguous() && t.const_data_ptr() == at;
+}
+
+// Whether the moments, and with `step` the parameter and its copy, of a tensor are where
+// its descriptor says.  kept: (param, copy, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale)
+bool in_place(PyObject* kept, const moara_adamw_tensor& d, bool step) {
+    PyObject* const* x = &PyTuple_GET_ITEM(kept, 0);
+    const bool block8 = d.state_dtype == MOARA_DTYPE_BLOCK8;
+    const at::ScalarType code = block8 ? at::kByte : at::kFloat;
+    const int64_t blocks = (d.n + MOARA_ADAMW_BLOCK - 1) / MOARA_ADAMW_BLOCK;
+    return (!step || (in_place(x[0], d.param, d.param_dtype == MOARA_DTYPE_BF16 ? at::kBFloat16 : at::kFloat, d.n) &&
+                      in_place(x[1], d.param_bf16, at::kBFloat16, d.n))) &&
+           in_place(x[2], d.exp_avg, code, d.n) && in_place(x[3], d.exp_avg_sq, code, d.n) &&
+           in_place(x[4], d.exp_avg_scale, at::kFloat, blocks) && in_place(x[5], d.exp_avg_sq_scale, at::kFloat, blocks);
+}
+
+// The list of a call's kept tuples, one for each of n descriptors; false with an error set for
+// anything else.
+bool kept_tuples(PyObject* o, Py_ssize_t n) {
+    bool good = PyList_Check(o) && PyList_GET_SIZE(o) == n;
+    for (Py_ssize_t i = 0; good && i < n; ++i) {
+        PyObject* t = PyList_GET_ITEM(o, i);
+        good = PyTuple_Check(t) && PyTuple_GET_SIZE(t) == 6;
+    }
+    if (!good) PyErr_Format(PyExc_TypeError, "a list of %zd tuples of six is needed", n);
+    return good;
+}
+
+// adamw_step(entry, ctx, count, descriptors, gradients, hparams, t, lr, grad_scale, device, stream,
+// kept) -> error code, or None if a kept tensor is not where its descriptor says.  The
+// gradients' addresses and types go into the descriptors.
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
-    if (!arguments(count, 11)) return nullptr;
+    if (!arguments(count, 12)) return nullptr;
     try {
         const auto fn = entry<decltype(&moara_adamw_step)>(a[0]);
         const Py_ssize_t n = PyLong_AsSsize_t(a[2]);
@@ -87,7 +122,9 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
         float* scale = scalar_of(a[8], "grad_scale", device);
         if (PyErr_Occurred()) return nullptr;
         if (grads.n != n) return PyErr_Format(PyExc_ValueError, "%zd gradients for %zd tensors", grads.n, n);
+        if (!kept_tuples(a[11], n)) return nullptr;
         for (Py_ssize_t i = 0; i < n; ++i) {
+            if (!in_place(PyList_GET_ITEM(a[11], i), d[i], true)) Py_RETURN_NONE;
             void* at;
             if (grads.get(i, "gradient", device, d[i].n, at, d[i].grad_dtype) == nullptr) return nullptr;
             d[i].grad = at;
@@ -104,9 +141,10 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
     }
 }
 
-// adamw_moments(entry, ctx, count, descriptors, exp_avg, exp_avg_sq, device, stream) -> error code
+// adamw_moments(entry, ctx, count, descriptors, exp_avg, exp_avg_sq, device, stream, kept)
+// -> error code, or None as adamw_step
 PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t count) {
-    if (!arguments(count, 8)) return nullptr;
+    if (!arguments(count, 9)) return nullptr;
     try {
         const auto fn = entry<decltype(&moara_adamw_moments)>(a[0]);
         const Py_ssize_t n = PyLong_AsSsize_t(a[2]);
@@ -116,6 +154,9 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t count) {
         auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
         void* stream = PyLong_AsVoidPtr(a[7]);
         if (PyErr_Occurred()) return nullptr;
+        if (!kept_tuples(a[8], n)) return nullptr;
+        for (Py_ssize_t i = 0; i < n; ++i)
+            if (!in_place(PyList_GET_ITEM(a[8], i), d[i], false)) Py_RETURN_NONE;
         std::vector<float*> to[2];
         for (int k = 0; k < 2; ++k) {
             if (outs[k].n != n) return PyErr_Format(PyExc_ValueError, "%zd outputs for %zd tensors", outs[k].n, n);
