@@ -17,10 +17,10 @@ _QUANTIZE, _DEQUANTIZE, _PRODUCT, _LINEAR, _LINEAR_BYTES = (
 class Fp4Matrix:
     """A rows x cols matrix in MXFP4 (layouts of moara.h): codes `q`, scales `sf`."""
 
-    __slots__ = "rows", "cols", "_ptrs", "_both", "_q", "_sf"
+    __slots__ = "rows", "cols", "device", "_ptrs", "_both", "_q", "_sf"
 
     def __init__(self, rows, cols, q=None, sf=None, device=0):
-        self.rows, self.cols = rows, cols
+        self.rows, self.cols, self.device = rows, cols, device
         sizes = B.moara_fp4_bytes(rows, cols)
         if q is None and sf is None:
             # one allocation: the codes, and the scales from the next 256 bytes on
@@ -45,10 +45,10 @@ class Fp4Matrix:
         return self._sf if self._both is None else self._both[self._ptrs[1] - self._ptrs[0]:]
 
 
-def _operand(buffer, rows, cols):
+def _operand(buffer, rows, cols, device):
     """The operand in a buffer of the native module: (tensor, address of q, of sf)."""
     a = Fp4Matrix.__new__(Fp4Matrix)
-    a.rows, a.cols, a._both, a._ptrs = rows, cols, buffer[0], buffer[1:]
+    a.rows, a.cols, a.device, a._both, a._ptrs = rows, cols, device, buffer[0], buffer[1:]
     return a
 
 
@@ -79,6 +79,12 @@ class Fp4Group:
                 return Fp4Matrix(rows, cols, device=self.device)
         if (m.rows, m.cols) != (rows, cols):
             raise ValueError(f"out: an operand of {rows} x {cols} is needed")
+        return self._here(m)
+
+    def _here(self, m):
+        """An operand, whose addresses are this group's device's."""
+        if m.device != self.device:
+            raise ValueError(f"an operand on cuda:{m.device}, expected cuda:{self.device}")
         return m
 
     def _bf16(self, out, dtype):
@@ -105,9 +111,9 @@ class Fp4Group:
                 B._check(got, self.ctx, "moara_fp4_quantize")
             r, c, m, k = got
             if not cols:
-                return _operand(r, m, k)
-            b = _operand(c, k, m)
-            return (_operand(r, m, k), b) if rows else b
+                return _operand(r, m, k, self.device)
+            b = _operand(c, k, m, self.device)
+            return (_operand(r, m, k, self.device), b) if rows else b
         ptr, dtype, m, k, ld = _host.matrix(x, self.device)
         a = self._matrix(out, m, k, stream) if rows else None
         b = self._matrix(out_cols, k, m, stream) if cols else None
@@ -118,7 +124,7 @@ class Fp4Group:
 
     def dequantize(self, a, dtype=torch.bfloat16, out=None, stream=None):
         """The values of an operand (bfloat16 holds them exactly)."""
-        args = (_DEQUANTIZE, self.ctx, *a._ptrs, a.rows, a.cols, out, self._bf16(out, dtype), self.device,
+        args = (_DEQUANTIZE, self.ctx, *self._here(a)._ptrs, a.rows, a.cols, out, self._bf16(out, dtype), self.device,
                 stream_handle(stream, self.device))
         if stream is None:
             return self._done(_host.fp4_dequantize(*args), "moara_fp4_dequantize")
@@ -129,8 +135,8 @@ class Fp4Group:
         """a b^T of two operands with the same number of columns."""
         if a.cols != b.cols:
             raise ValueError(f"{a.cols} and {b.cols} columns")
-        args = (_PRODUCT, self.ctx, a.rows, b.rows, a.cols, *a._ptrs, *b._ptrs, out, self._bf16(out, dtype),
-                self.device, stream_handle(stream, self.device))
+        args = (_PRODUCT, self.ctx, a.rows, b.rows, a.cols, *self._here(a)._ptrs, *self._here(b)._ptrs, out,
+                self._bf16(out, dtype), self.device, stream_handle(stream, self.device))
         if stream is None:
             return self._done(_host.fp4_product(*args), "moara_fp4_product")
         with allocating_on(stream, self.device):
@@ -138,7 +144,7 @@ class Fp4Group:
 
     def linear(self, x, b, dtype=torch.bfloat16, out=None, stream=None):
         """x b^T with x (float32 or bfloat16) quantised by rows on the way."""
-        args = (_LINEAR, self.ctx, x, b.rows, b.cols, *b._ptrs, out, self._bf16(out, dtype), self.device,
+        args = (_LINEAR, self.ctx, x, b.rows, b.cols, *self._here(b)._ptrs, out, self._bf16(out, dtype), self.device,
                 stream_handle(stream, self.device), _LINEAR_BYTES)
         if stream is None:
             return self._done(_host.fp4_linear(*args), "moara_fp4_linear")
