@@ -425,7 +425,8 @@ typedef struct moara_adamw_hparams {
 
 /* One tensor of n >= 0 contiguous entries.  Pointers are device pointers,
  * aligned to their type (16-byte alignment of all of them is faster); an n of 0
- * is skipped.
+ * is skipped.  Nothing that a call writes (param, param_bf16, moments, scales) may overlap
+ * anything else that it reads or writes: the tensors of a launch are taken in no order.
  *   param       fp32 or bf16 (param_dtype), updated in place; bf16 is computed in
  *               fp32 and stored rounded to nearest even
  *   grad        fp32 or bf16 (grad_dtype), read

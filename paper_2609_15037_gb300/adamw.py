@@ -4,6 +4,7 @@ moara_grad_norm.  Every computation happens in the library's kernels."""
 
 from __future__ import annotations
 
+import bisect
 import contextlib
 import ctypes
 import struct
@@ -54,11 +55,38 @@ def allocating_on(stream, device):
     return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device))
 
 
+class _Ranges:
+    """Disjoint ranges of addresses."""
+
+    def __init__(self):
+        self._begin, self._end = [], []
+
+    def add(self, tensors, at):
+        """The memory of these contiguous tensors at these addresses (0: of none), all of it or
+        nothing; ValueError where it overlaps a range or itself."""
+        taken = []
+        for x, begin in zip(tensors, at):
+            if begin == 0:
+                continue
+            end = begin + x.nbytes
+            i = bisect.bisect_right(self._begin, begin)
+            if (i and self._end[i - 1] > begin) or (i < len(self._begin) and self._begin[i] < end):
+                for b in taken:
+                    j = bisect.bisect_left(self._begin, b)
+                    del self._begin[j], self._end[j]
+                raise ValueError("the tensor, its copy or its moments overlap registered ones")
+            self._begin.insert(i, begin)
+            self._end.insert(i, end)
+            taken.append(begin)
+
+
 class AdamWGroup:
     """Tensors that take AdamW steps together, with their moments.
 
     A registered tensor whose storage is replaced (an assignment to .data, module.to) is
-    followed to its new place and type, and refused where it no longer fits.
+    followed to its new place and type, and refused where it no longer fits.  What a step
+    writes (parameters, copies, moments) must not overlap: a tensor is registered once, and
+    taken once per call.
     Streams are cudaStream_t handles; None is torch's current stream."""
 
     def __init__(self, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, device=0):
@@ -69,6 +97,7 @@ class AdamWGroup:
         self._dev = torch.device("cuda", device)
         self.params, self.copies, self.states = [], [], []
         self._kept = []         # of each tensor: param, copy, and the four tensors of its moments
+        self._ranges = _Ranges()
         self._table, self._room, self._all = np.zeros(0, _DESC), 0, None
         self._workspace = {}
 
@@ -115,11 +144,16 @@ class AdamWGroup:
             s["exp_avg_scale"] = kept(exp_avg_scale, blocks, torch.float32)
             s["exp_avg_sq_scale"] = kept(exp_avg_sq_scale, blocks, torch.float32)
         tensors = param, copy, *s.values(), *(None,) * (4 - len(s))
-        p, c, *at = self._check_kept(tensors, n, state)
+        at = self._check_kept(tensors, n, state)
         i = len(self.params)
         self._grow(i + 1)
-        _PACK.pack_into(self._table, i * _SIZE, n, p, 0, c, *at,
+        _PACK.pack_into(self._table, i * _SIZE, n, at[0], 0, *at[1:],
                         _TYPES[param.dtype], 0, _STATES[state], i if id is None else id, weight_decay, lr_scale)
+        try:
+            self._ranges.add(tensors, at)
+        except ValueError:      # or they lie where a replaced storage was
+            self._follow()
+            self._ranges.add(tensors, at)
         self.params.append(param)
         self.copies.append(copy)
         self.states.append(types.MappingProxyType(s))
@@ -141,22 +175,27 @@ class AdamWGroup:
         if ids is None:
             return self._all
         rows = np.arange(len(self.params))[list(ids)]
+        at = rows.tolist()
+        if len(set(at)) != len(at):
+            raise ValueError("ids: a tensor is listed twice")
         d = self._all[0][rows]
-        return d, d.ctypes.data, [self._kept[i] for i in rows.tolist()]
+        return d, d.ctypes.data, [self._kept[i] for i in at]
 
     def _follow(self):
         """The descriptors of tensors whose storage was replaced (an assignment to .data,
         module.to): their new places and types.  One that no longer fits is refused."""
-        d, places = self._table[:len(self.params)], []
+        d, places, ranges = self._table[:len(self.params)], [], _Ranges()
         for x, n, state in zip(self._kept, d["n"].tolist(), d["state_dtype"].tolist()):
             places.append(self._check_kept(x, n, "block8" if state == B.MOARA_DTYPE_BLOCK8 else "f32"))
             for y in x:
                 if y is not None and y.untyped_storage().nbytes() < (y.storage_offset() + y.numel()) * y.element_size():
                     raise ValueError("the storage of a registered tensor was freed")
+            ranges.add(x, places[-1])
         fields = "param", "param_bf16", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"
         for name, column in zip(fields, zip(*places)):
             d[name] = column
         d["param_dtype"] = [_TYPES[x[0].dtype] for x in self._kept]
+        self._ranges = ranges
 
     def _called(self, ids, call):
         """The code of call(count, descriptors' address, kept tensors), which is made again

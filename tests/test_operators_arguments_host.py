@@ -41,3 +41,85 @@ def test_operands_of_another_device_are_refused(M, device, monkeypatch):
                  lambda: f.product(a, a, stream=1), lambda: f.quantize(x, out=a, stream=1)):
         with pytest.raises(ValueError):
             call()
+
+
+def adamw_group(M):
+    opt = M.AdamWGroup.__new__(M.AdamWGroup)
+    create, destroy = M.adamw.B.moara_create, M.adamw.B.moara_destroy
+    M.adamw.B.moara_create, M.adamw.B.moara_destroy = lambda *_: None, lambda *_: None
+    try:
+        opt.__init__(device=0)
+    finally:
+        M.adamw.B.moara_create, M.adamw.B.moara_destroy = create, destroy
+    opt.device, opt._dev = -1, torch.device("cpu")
+    return opt
+
+
+def test_overlapping_registrations_are_refused(M):
+    opt = adamw_group(M)
+    flat = torch.zeros(1000)
+    p = flat[100:300]
+    half = torch.zeros(200, dtype=torch.bfloat16)
+    m, v = torch.zeros(200), torch.zeros(200)
+    assert opt.add(p, copy=half, exp_avg=m, exp_avg_sq=v) == 0
+    other = torch.zeros(200)
+    for bad, kw in ((p, {}), (flat[299:400], {}), (flat[:101], {}), (flat, {}), (flat[150:160], {}), (m, {}),
+                    (other, dict(copy=half)), (other, dict(exp_avg=v)), (other, dict(exp_avg_sq=other)),
+                    (other, dict(exp_avg=torch.zeros(200), exp_avg_sq=p))):
+        with pytest.raises(ValueError):
+            opt.add(bad, **kw)
+    # refused ones left nothing behind; neighbours and empty tensors are fine
+    assert opt.add(other) == 1 and opt.add(flat[:100]) == 2 and opt.add(flat[300:]) == 3
+    assert opt.add(flat[:0]) == 4 and opt.add(flat[150:150]) == 5
+    assert len(opt.states) == len(opt.params) == 6
+
+
+def test_eight_bit_scales_are_ranges_too(M):
+    opt = adamw_group(M)
+    scales = torch.zeros(4)
+    kw = dict(state="block8", exp_avg_scale=scales[:2], exp_avg_sq_scale=scales[2:])
+    opt.add(torch.zeros(300), **kw)
+    with pytest.raises(ValueError):
+        opt.add(torch.zeros(300), **kw)
+
+
+def test_a_tensor_is_taken_once_per_call(M, monkeypatch):
+    opt = adamw_group(M)
+    for _ in range(3):
+        opt.add(torch.zeros(8))
+    calls = []
+    monkeypatch.setattr(M.adamw._host, "adamw_step", lambda *a: calls.append(a[2]) or 0)
+    g = torch.zeros(8)
+    for ids in ([0, 0], [2, 1, 2], [0, -3]):
+        with pytest.raises(ValueError):
+            opt.step([g] * len(ids), 1, 0.1, ids=ids, stream=0)
+    with pytest.raises(IndexError):
+        opt.step([g], 1, 0.1, ids=[3], stream=0)
+    opt.step([g, g], 1, 0.1, ids=iter((2, 0)), stream=0)
+    opt.step([], 1, 0.1, ids=[], stream=0)
+    assert calls == [2, 0]
+
+
+def test_replaced_storage_may_not_overlap(M):
+    opt = adamw_group(M)
+    a, b = torch.zeros(100), torch.zeros(100)
+    opt.add(a), opt.add(b)
+    old = b.data
+    b.data = a.data
+    with pytest.raises(ValueError):
+        opt._follow()
+    b.data = old
+    a.data = torch.zeros(100)
+    opt._follow()
+    assert opt._table["param"][:2].tolist() == [a.data_ptr(), b.data_ptr()]
+
+
+def test_memory_of_a_replaced_storage_is_free_again(M):
+    opt = adamw_group(M)
+    a = torch.zeros(100)
+    opt.add(a)
+    old = a.data
+    a.data = torch.zeros(100)
+    assert opt.add(old) == 1
+    with pytest.raises(ValueError):
+        opt.add(a.data)
