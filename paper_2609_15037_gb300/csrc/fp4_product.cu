@@ -178,8 +178,8 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
         int stage = 0;
         uint32_t phase = 0;
         for (int k = k0; k < k1; ++k) {
-            if (!ptx::mbar_wait(ptx::smem_u32(&ctl->full[stage]), phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT,
-                                kWait))
+            if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl->full[stage]), phase, abort_flag, p.status,
+                                     MOARA_ERR_DEVICE_TIMEOUT, kWait))
                 break;
             ptx::tc_fence_after();
             if (leader) {
@@ -230,9 +230,9 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
             int stage = 0;
             uint32_t phase = 0;
             for (int k = k0; k < k1; ++k) {
-                const bool got = ptx::mbar_wait(ptx::smem_u32(&ctl->empty[stage]), phase ^ 1, abort_flag, p.status,
-                                                MOARA_ERR_DEVICE_TIMEOUT, kWait);
-                if (!__all_sync(0xffffffffu, got)) break;
+                if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl->empty[stage]), phase ^ 1, abort_flag, p.status,
+                                         MOARA_ERR_DEVICE_TIMEOUT, kWait))
+                    break;
                 uint8_t* rows = smem + stage * stage_bytes + OPERAND;
                 uint8_t* sf = rows + x_bytes + SF_BYTES;
 #pragma unroll
@@ -258,9 +258,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
             }
         }
-        const bool got = ptx::mbar_wait(ptx::smem_u32(&ctl->accf), 0, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT,
-                                        kWait);
-        if (__all_sync(0xffffffffu, got)) {
+        if (ptx::mbar_wait_warp(ptx::smem_u32(&ctl->accf), 0, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, kWait)) {
             // sums [token][128 rows of the weight] over the stages, which are all consumed
             ptx::tc_fence_after();
             float* part = reinterpret_cast<float*>(smem) + quad * 32 + lane;
@@ -568,7 +566,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
             const uint32_t empty = ptx::smem_u32(&ctl->empty[0]);
             const int tail = (p.K - (steps - 1) * BK + 63) / 64;          // MMAs of a tile's last stage
             auto scales = [&](int stage, uint32_t phase) {
-                if (!ptx::mbar_wait(full + 8 * stage, phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, kWait))
+                if (!ptx::mbar_wait_warp(full + 8 * stage, phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, kWait))
                     return false;
                 ptx::tc_fence_after();
                 if (leader) {
@@ -592,8 +590,8 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
                 const int next = stage + 1 == P_STAGES ? 0 : stage + 1;
                 if (g + 1 < total && !scales(next, next == 0 ? phase ^ 1 : phase)) break;
                 if (k == 0) {
-                    ok = ptx::mbar_wait_cluster(ptx::smem_u32(&ctl->acce), acc ^ 1, abort_flag, p.status,
-                                                MOARA_ERR_DEVICE_TIMEOUT, kWait);
+                    ok = ptx::mbar_wait_cluster_warp(ptx::smem_u32(&ctl->acce), acc ^ 1, abort_flag, p.status,
+                                                     MOARA_ERR_DEVICE_TIMEOUT, kWait);
                     if (!ok) break;
                     ptx::tc_fence_after();
                     acc ^= 1;
@@ -631,9 +629,9 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
         for (int t = first; t < tiles; t += stride, acc ^= 1) {
             int m0, n0;
             tile_of(p, t, m0, n0);
-            const bool got = ptx::mbar_wait(ptx::smem_u32(&ctl->accf), acc, abort_flag, p.status,
-                                            MOARA_ERR_DEVICE_TIMEOUT, kWait);
-            if (!__all_sync(0xffffffffu, got)) break;
+            if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl->accf), acc, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT,
+                                     kWait))
+                break;
             ptx::tc_fence_after();
             const uint32_t from = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * 128;
             const int row = m0 + crank * 128 + quad * 32, col = n0 + half * 128;

@@ -67,6 +67,14 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
 }
 
+// The same by all lanes of a warp, which get one answer: the phase may end just as the limit
+// passes or the flag is raised, and lanes that part there miss one another at the warp's
+// next barrier.
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                               int* status, int code, long long limit) {
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, status, code, limit));
+}
+
 __device__ __forceinline__ void fence_barrier_init() {
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
@@ -121,6 +129,11 @@ __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity,
             return false;
         }
     }
+}
+
+__device__ __forceinline__ bool mbar_wait_cluster_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag,
+                                                       int* status, int code, long long limit) {
+    return __all_sync(0xffffffffu, mbar_wait_cluster(bar, parity, abort_flag, status, code, limit));
 }
 
 // Address of the same shared-memory location in CTA `rank` of the cluster.
