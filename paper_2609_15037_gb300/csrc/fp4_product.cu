@@ -9,6 +9,7 @@
 #include "launch.cuh"
 #include "ops.h"
 #include "tc_ptx.cuh"
+#include "waits.cuh"
 
 namespace moara {
 namespace {
@@ -18,14 +19,6 @@ namespace {
 constexpr int BK = 256;
 constexpr int OPERAND = 128 * BK / 2;              // 16 KB: 128 rows of either operand
 constexpr int SF_BYTES = 1024;                     // the scales of 128 rows
-constexpr long long kWait = 1LL << 32;
-
-__device__ __forceinline__ bool drained(uint32_t bar, uint32_t parity) {
-    const long long t0 = clock64();
-    while (!ptx::mbar_try_wait(bar, parity))
-        if (clock64() - t0 > kWait) return false;
-    return true;
-}
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -162,7 +155,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
             uint32_t phase = 0;
             for (int k = k0 + ahead; k < k1; ++k) {
                 if (!ptx::mbar_wait(ptx::smem_u32(&ctl->empty[stage]), phase, abort_flag, p.status,
-                                    MOARA_ERR_DEVICE_TIMEOUT, kWait))
+                                    MOARA_ERR_DEVICE_TIMEOUT, kWaitLimit))
                     break;
                 load_w(k, stage);
                 load_t(k, stage);
@@ -170,7 +163,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
             }
             for (int s = 0; s < p.stages; ++s)
-                if (issued & (1u << s)) drained(ptx::smem_u32(&ctl->full[s]), (last >> s) & 1);
+                if (issued & (1u << s)) wait_drain(ptx::smem_u32(&ctl->full[s]), (last >> s) & 1);
         }
     } else if (warp == 1) {
         const bool leader = ptx::elect_one();
@@ -179,7 +172,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
         uint32_t phase = 0;
         for (int k = k0; k < k1; ++k) {
             if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl->full[stage]), phase, abort_flag, p.status,
-                                     MOARA_ERR_DEVICE_TIMEOUT, kWait))
+                                     MOARA_ERR_DEVICE_TIMEOUT, kWaitLimit))
                 break;
             ptx::tc_fence_after();
             if (leader) {
@@ -211,7 +204,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
             ptx::mma_commit(ptx::smem_u32(&ctl->drain));
         }
         __syncwarp();
-        drained(ptx::smem_u32(&ctl->drain), 0);
+        wait_drain(ptx::smem_u32(&ctl->drain), 0);
     } else {
         const int quad = warp & 3;
         if (QUANT) {
@@ -231,7 +224,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
             uint32_t phase = 0;
             for (int k = k0; k < k1; ++k) {
                 if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl->empty[stage]), phase ^ 1, abort_flag, p.status,
-                                         MOARA_ERR_DEVICE_TIMEOUT, kWait))
+                                         MOARA_ERR_DEVICE_TIMEOUT, kWaitLimit))
                     break;
                 uint8_t* rows = smem + stage * stage_bytes + OPERAND;
                 uint8_t* sf = rows + x_bytes + SF_BYTES;
@@ -258,7 +251,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
             }
         }
-        if (ptx::mbar_wait_warp(ptx::smem_u32(&ctl->accf), 0, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, kWait)) {
+        if (ptx::mbar_wait_warp(ptx::smem_u32(&ctl->accf), 0, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, kWaitLimit)) {
             // sums [token][128 rows of the weight] over the stages, which are all consumed
             ptx::tc_fence_after();
             float* part = reinterpret_cast<float*>(smem) + quad * 32 + lane;
@@ -375,7 +368,8 @@ constexpr int P_TMEM_STAGE = 24;
 constexpr int P_STAGE = 2 * OPERAND + 3 * SF_BYTES;
 constexpr int P_STAGES = 6;
 constexpr int P_OUT = 32 * 64;                                     // a warp's staging of D: 32 rows of 64 bytes
-constexpr int P_SMEM = P_STAGES * P_STAGE + EPI_WARPS * P_OUT + 256;
+constexpr int P_CTL = 256;
+constexpr int P_SMEM = P_STAGES * P_STAGE + EPI_WARPS * P_OUT + P_CTL;
 static_assert(P_STAGE % 1024 == 0 && P_SMEM <= 227 * 1024, "stages stay on the swizzle's 1024-byte lines");
 static_assert(P_BN + P_STAGES * P_TMEM_STAGE <= 512, "tensor memory");
 
@@ -388,6 +382,7 @@ struct PairParams {
     int bf16;
     int vec;               // rows of D begin on 16-byte lines
     int* status;
+    long long wait_limit;  // clock cycles of a bounded wait before it gives up
 };
 
 struct PairCtl {
@@ -395,7 +390,9 @@ struct PairCtl {
     uint64_t accf, acce, drain;
     uint32_t tmem;
     int abort;
+    uint32_t steps;        // stages that this CTA's producer filled
 };
+static_assert(sizeof(PairCtl) <= P_CTL, "the barriers fit behind the staging of D");
 
 // Tiles in groups of eight row tiles, so that the operands of the tiles in flight stay
 // in L2.
@@ -512,6 +509,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
         ptx::mbar_init(ptx::smem_u32(&ctl->acce), 2 * EPI_WARPS);      // both CTAs' warps, on the even CTA
         ptx::mbar_init(ptx::smem_u32(&ctl->drain), 1);
         ctl->abort = 0;
+        ctl->steps = 0;
         ptx::fence_barrier_init();
     }
     if (warp == 1) {
@@ -528,31 +526,38 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
     const int first = blockIdx.x >> 1, stride = gridDim.x >> 1;
     const int steps = (p.K + BK - 1) / BK;
 
+    // this CTA's copies of step k of a tile into a stage
+    auto fill = [&](int m0, int n0, int k, int stage) {
+        const uint32_t own = ptx::smem_u32(&ctl->full[stage]), fb = ptx::mapa(own, 0);
+        if (crank == 0) ptx::mbar_arrive_expect_tx(own, 2 * P_STAGE);
+        const uint32_t a = ptx::smem_u32(smem + stage * P_STAGE);
+        const uint32_t b = a + OPERAND, sa = b + OPERAND, sb = sa + SF_BYTES;
+        ptx::tma_load_2d_pair(a, &p.amap, fb, k * (BK / 2), m0 + 128 * crank);
+        ptx::tma_load_2d_pair(b, &p.bmap, fb, k * (BK / 2), n0 + 128 * crank);
+        ptx::tma_load_2d_pair(sa, &p.samap, fb, k * 256, (m0 >> 7) + crank);
+        ptx::tma_load_2d_pair(sb, &p.sbmap, fb, k * 256, n0 >> 7);
+    };
+
     if (warp == 0) {
         if (lane == 0) {
             int stage = 0;
-            uint32_t phase = 0;
+            uint32_t phase = 0, filled = 0;
             bool ok = true;
             for (int t = first; t < tiles && ok; t += stride) {
                 int m0, n0;
                 tile_of(p, t, m0, n0);
                 for (int k = 0; k < steps; ++k) {
                     if (!ptx::mbar_wait(ptx::smem_u32(&ctl->empty[stage]), phase ^ 1, abort_flag, p.status,
-                                        MOARA_ERR_DEVICE_TIMEOUT, kWait)) {
+                                        MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit)) {
                         ok = false;
                         break;
                     }
-                    const uint32_t own = ptx::smem_u32(&ctl->full[stage]), fb = ptx::mapa(own, 0);
-                    if (crank == 0) ptx::mbar_arrive_expect_tx(own, 2 * P_STAGE);
-                    const uint32_t a = ptx::smem_u32(smem + stage * P_STAGE);
-                    const uint32_t b = a + OPERAND, sa = b + OPERAND, sb = sa + SF_BYTES;
-                    ptx::tma_load_2d_pair(a, &p.amap, fb, k * (BK / 2), m0 + 128 * crank);
-                    ptx::tma_load_2d_pair(b, &p.bmap, fb, k * (BK / 2), n0 + 128 * crank);
-                    ptx::tma_load_2d_pair(sa, &p.samap, fb, k * 256, (m0 >> 7) + crank);
-                    ptx::tma_load_2d_pair(sb, &p.sbmap, fb, k * 256, n0 >> 7);
+                    fill(m0, n0, k, stage);
+                    ++filled;
                     if (++stage == P_STAGES) { stage = 0; phase ^= 1; }
                 }
             }
+            ctl->steps = filled;
         }
     } else if (warp == 1) {
         if (crank == 0) {
@@ -566,7 +571,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
             const uint32_t empty = ptx::smem_u32(&ctl->empty[0]);
             const int tail = (p.K - (steps - 1) * BK + 63) / 64;          // MMAs of a tile's last stage
             auto scales = [&](int stage, uint32_t phase) {
-                if (!ptx::mbar_wait_warp(full + 8 * stage, phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, kWait))
+                if (!ptx::mbar_wait_warp(full + 8 * stage, phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
                     return false;
                 ptx::tc_fence_after();
                 if (leader) {
@@ -591,7 +596,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
                 if (g + 1 < total && !scales(next, next == 0 ? phase ^ 1 : phase)) break;
                 if (k == 0) {
                     ok = ptx::mbar_wait_cluster_warp(ptx::smem_u32(&ctl->acce), acc ^ 1, abort_flag, p.status,
-                                                     MOARA_ERR_DEVICE_TIMEOUT, kWait);
+                                                     MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
                     if (!ok) break;
                     ptx::tc_fence_after();
                     acc ^= 1;
@@ -618,7 +623,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
             }
             if (leader) ptx::mma2_commit_mc(ptx::smem_u32(&ctl->drain), 0x1);
             __syncwarp();
-            drained(ptx::smem_u32(&ctl->drain), 0);
+            wait_drain(ptx::smem_u32(&ctl->drain), 0);
         }
     } else {
         // lane quadrant warp % 4, column half (warp - 2) / 4
@@ -630,7 +635,7 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
             int m0, n0;
             tile_of(p, t, m0, n0);
             if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl->accf), acc, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT,
-                                     kWait))
+                                     p.wait_limit))
                 break;
             ptx::tc_fence_after();
             const uint32_t from = tmem + (static_cast<uint32_t>(quad * 32) << 16) + half * 128;
@@ -660,7 +665,15 @@ __global__ void __launch_bounds__(P_THREADS, 1) k_fp4_pair(const __grid_constant
     }
     ptx::tc_fence_before();
     __syncwarp();
+    pair_abort(ctl, crank);
+    __syncwarp();
     ptx::cluster_sync();            // no CTA leaves while its peer may still signal or fill it
+    if (*abort_flag) {              // the same in both CTAs
+        // the copies of any step do: every stage takes as many bytes
+        if (threadIdx.x == 0) pair_settle<P_STAGES>(ctl, crank, [&](int, int stage) { fill(0, 0, 0, stage); });
+        __syncwarp();
+        ptx::cluster_sync();
+    }
     if (warp == 1) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc2(tmem, 512);
@@ -734,6 +747,7 @@ cudaError_t launch_pair(const Fp4Product& a, int* status, cudaStream_t s) {
     const uintptr_t d = reinterpret_cast<uintptr_t>(a.D), pitch = static_cast<uintptr_t>(a.ldd) * (p.bf16 ? 2 : 4);
     p.vec = (d | pitch) % 16 == 0;
     p.status = status;
+    p.wait_limit = a.wait_limit;
     const cudaError_t e = allow_shared<1>(k_fp4_pair);
     if (e != cudaSuccess) return e;
     const long long tiles = static_cast<long long>(p.tiles_m) * p.tiles_n;

@@ -129,6 +129,7 @@ struct Fp4Product {
     const void* X;         // A as fp32 or bf16 rows, quantised on the way (aq, asf unused), or null
     int x_dtype;
     int64_t ldx;
+    long long wait_limit;  // clock cycles of a bounded wait before it gives up
 };
 // Whether a product of M rows can quantise A itself.
 bool fp4_quantizes(int M);

@@ -327,7 +327,7 @@ int moara_fp4_product(moara_ctx* ctx, int M, int N, int K, const void* a_q, cons
     if (rc == MOARA_OK) rc = check_operand(ctx, "A", a_q, a_sf);
     if (rc != MOARA_OK) return rc;
     DeviceGuard g(ctx->device);
-    const moara::Fp4Product p{M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, nullptr, 0, 0};
+    const moara::Fp4Product p{M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, nullptr, 0, 0, moara::tc_wait_limit(ctx->tc)};
     const cudaError_t e = moara::launch_fp4_product(p, false, ctx->d_status, static_cast<cudaStream_t>(stream), &ctx->launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "product launch");
     return MOARA_OK;
@@ -353,7 +353,7 @@ int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_d
     if (need > 0 && !aligned16(workspace)) return fail(ctx, MOARA_ERR_ALIGN, "workspace is not 16-byte aligned");
     DeviceGuard g(ctx->device);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    moara::Fp4Product p{M, N, K, nullptr, nullptr, b_q, b_sf, D, d_dtype, ldd, X, x_dtype, ldx};
+    moara::Fp4Product p{M, N, K, nullptr, nullptr, b_q, b_sf, D, d_dtype, ldd, X, x_dtype, ldx, moara::tc_wait_limit(ctx->tc)};
     cudaError_t e = cudaSuccess;
     const bool apart = !moara::fp4_quantizes(M);
     if (apart) {

@@ -33,13 +33,13 @@
 #include "launch.cuh"
 #include "tc.h"
 #include "tc_ptx.cuh"
+#include "waits.cuh"
 
 namespace moara {
 
 namespace {
 
 constexpr int kTcGroup = 224;                 // modules per launch (G maps in params)
-constexpr long long kWaitLimit = 1LL << 32;   // ~2 s of SM clocks
 constexpr int kMaps = 10;                     // tensor maps per module
 
 struct TcMod {
@@ -213,39 +213,6 @@ static_assert(K1_SMEM + 1024 + 1024 <= 228 * 1024 && K2_SMEM + 1024 + 1024 <= 22
 
 __device__ __forceinline__ uint8_t* align1024(uint8_t* p) {
     return reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(p) + 1023) & ~uintptr_t(1023));
-}
-
-__device__ __forceinline__ bool wait_drain(uint32_t bar, uint32_t parity) {
-    const long long t0 = clock64();
-    while (!ptx::mbar_try_wait(bar, parity)) {
-        if (clock64() - t0 > kWaitLimit) return false;
-    }
-    return true;
-}
-
-// A pair whose waits may run out while copies are in flight (a wait limit below
-// a copy's latency).  A copy of either CTA completes on the even CTA's barrier,
-// and a stage's phase ends when both CTAs' copies have landed; the two producers
-// may have given up a different number of stages in.
-//
-// pair_abort, by every warp before the last cluster barrier: if its CTA gave up,
-// the peer knows behind that barrier.  pair_settle, by one thread of each CTA
-// behind it: the CTA that filled fewer stages fills the missing ones (the MMAs
-// are done, what lands there is not used), and the even CTA waits for every
-// stage's last phase.  Another cluster barrier, and no copy is left in flight.
-__device__ __forceinline__ void pair_abort(SmemCtl* ctl, int crank) {
-    if ((threadIdx.x & 31) == 0 && *const_cast<volatile int*>(&ctl->abort) != 0)
-        ptx::st_cluster_u32(ptx::mapa(ptx::smem_u32(&ctl->abort), crank ^ 1), 1);
-}
-
-template <int STAGES, class Fill>
-__device__ __forceinline__ void pair_settle(SmemCtl* ctl, int crank, Fill fill) {
-    const uint32_t own = ctl->steps, peer = ptx::ld_cluster_u32(ptx::mapa(ptx::smem_u32(&ctl->steps), crank ^ 1));
-    const uint32_t all = own > peer ? own : peer;
-    for (uint32_t k = own; k < all; ++k) fill(static_cast<int>(k), static_cast<int>(k % STAGES));
-    if (crank == 0)
-        for (uint32_t q = 0; q < STAGES && q < all; ++q)
-            wait_drain(ptx::smem_u32(&ctl->full[q]), ((all - 1 - q) / STAGES) & 1);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
@@ -2604,6 +2571,8 @@ int tc_step(TcState* st, const moara_hparams& hp, int n_mod, const int* ids, con
 }
 
 const char* tc_last_error(const TcState* st) { return st ? st->err.c_str() : "no tensor-core state"; }
+
+long long tc_wait_limit(const TcState* st) { return st != nullptr ? st->wait_limit : kWaitLimit; }
 
 void tc_set_wait_limit(TcState* st, long long cycles) {
     if (st != nullptr) st->wait_limit = cycles > 0 ? cycles : kWaitLimit;

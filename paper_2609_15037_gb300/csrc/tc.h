@@ -109,5 +109,6 @@ const char* tc_last_error(const TcState* st);
 // spins before it gives up and records MOARA_ERR_DEVICE_TIMEOUT; <= 0 restores
 // the default (~2 s).
 void tc_set_wait_limit(TcState* st, long long cycles);
+long long tc_wait_limit(const TcState* st);
 
 }  // namespace moara
