@@ -327,7 +327,7 @@ int64_t moara_launch_count(const moara_ctx* ctx);
  * work in flight, frees its tensor memory and returns, leaving the context
  * usable.  This call sets the bound, in SM clock cycles, of the waits of the
  * tensor-core products of the projector refresh and of moara_alignment and of the MXFP4
- * products on CTA pairs, for launches enqueued afterwards; cycles <= 0 restores
+ * products, for launches enqueued afterwards; cycles <= 0 restores
  * the default (2^32 cycles, about 2 s).  A bound shorter than the kernels'
  * own latency (a few hundred cycles) makes them give up on purpose, which is
  * how the failure path is tested; their outputs are then undefined until the

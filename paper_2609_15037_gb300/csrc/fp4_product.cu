@@ -6,6 +6,7 @@
 #include <atomic>
 
 #include "fp4.cuh"
+#include "fp4_settle.h"
 #include "launch.cuh"
 #include "ops.h"
 #include "tc_ptx.cuh"
@@ -65,6 +66,7 @@ struct FewParams {
     int vec;               // four entries of a row of D may be written at once
     int ctl;               // offset of the barriers in shared memory
     int* status;
+    long long wait_limit;  // clock cycles of a bounded wait before it gives up
 };
 
 struct FewCtl {
@@ -72,6 +74,7 @@ struct FewCtl {
     uint64_t accf, drain;
     uint32_t tmem;
     int abort;
+    int filled[5];         // stages that the producer and each quantising warp filled
 };
 
 __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
@@ -127,7 +130,6 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
 
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t issued = 0, last = 0;
             // this CTA's copies of step k: the weight's, and the tokens'
             auto load_w = [&](int k, int stage) {
                 const uint32_t fb = ptx::smem_u32(&ctl->full[stage]), w = ptx::smem_u32(smem + stage * stage_bytes);
@@ -147,23 +149,18 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
             const int ahead = min(p.stages, k1 - k0);
             for (int i = 0; i < ahead; ++i) load_w(k0 + i, i);
             if (p.early) asm volatile("griddepcontrol.wait;" ::: "memory");
-            for (int i = 0; i < ahead; ++i) {
-                load_t(k0 + i, i);
-                issued |= 1u << i;
-            }
-            int stage = 0;
+            for (int i = 0; i < ahead; ++i) load_t(k0 + i, i);
+            int stage = 0, k = k0 + ahead;
             uint32_t phase = 0;
-            for (int k = k0 + ahead; k < k1; ++k) {
+            for (; k < k1; ++k) {
                 if (!ptx::mbar_wait(ptx::smem_u32(&ctl->empty[stage]), phase, abort_flag, p.status,
-                                    MOARA_ERR_DEVICE_TIMEOUT, kWaitLimit))
+                                    MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
                     break;
                 load_w(k, stage);
                 load_t(k, stage);
-                last = (last & ~(1u << stage)) | ((phase ^ 1) << stage);
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
             }
-            for (int s = 0; s < p.stages; ++s)
-                if (issued & (1u << s)) wait_drain(ptx::smem_u32(&ctl->full[s]), (last >> s) & 1);
+            ctl->filled[4] = k - k0;
         }
     } else if (warp == 1) {
         const bool leader = ptx::elect_one();
@@ -172,7 +169,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
         uint32_t phase = 0;
         for (int k = k0; k < k1; ++k) {
             if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl->full[stage]), phase, abort_flag, p.status,
-                                     MOARA_ERR_DEVICE_TIMEOUT, kWaitLimit))
+                                     MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
                 break;
             ptx::tc_fence_after();
             if (leader) {
@@ -220,11 +217,11 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
                 }
             };
             fetch(k0);
-            int stage = 0;
+            int stage = 0, k = k0;
             uint32_t phase = 0;
-            for (int k = k0; k < k1; ++k) {
+            for (; k < k1; ++k) {
                 if (!ptx::mbar_wait_warp(ptx::smem_u32(&ctl->empty[stage]), phase ^ 1, abort_flag, p.status,
-                                         MOARA_ERR_DEVICE_TIMEOUT, kWaitLimit))
+                                         MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
                     break;
                 uint8_t* rows = smem + stage * stage_bytes + OPERAND;
                 uint8_t* sf = rows + x_bytes + SF_BYTES;
@@ -250,8 +247,9 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->full[stage]));
                 if (++stage == p.stages) { stage = 0; phase ^= 1; }
             }
+            if (lane == 0) ctl->filled[quad] = k - k0;
         }
-        if (ptx::mbar_wait_warp(ptx::smem_u32(&ctl->accf), 0, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, kWaitLimit)) {
+        if (ptx::mbar_wait_warp(ptx::smem_u32(&ctl->accf), 0, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit)) {
             // sums [token][128 rows of the weight] over the stages, which are all consumed
             ptx::tc_fence_after();
             float* part = reinterpret_cast<float*>(smem) + quad * 32 + lane;
@@ -275,8 +273,16 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, F_TMEM);
     }
+    // a wait that ran out: no copy stays in flight (otherwise the MMAs have waited for all)
+    if (threadIdx.x == 0 && *abort_flag)
+        settle_few<QUANT ? 4 : 0>(
+            ctl->filled[4], ctl->filled, p.stages, [&](int s) { ptx::mbar_arrive(ptx::smem_u32(&ctl->full[s])); },
+            [&](int s, uint32_t parity) { wait_drain(ptx::smem_u32(&ctl->full[s]), parity); });
     __syncwarp();
     ptx::cluster_sync();                                            // every CTA's sums are in its shared memory
+    // whether a CTA of the cluster gave up: its sums are none, and nothing is stored
+    const uint32_t gave_up =
+        lane < p.split ? ptx::ld_cluster_u32(ptx::mapa(ptx::smem_u32(&ctl->abort), static_cast<uint32_t>(lane))) : 0u;
     {
         const int tokens = min(p.nt, p.M - m0), share = (tokens + p.split - 1) / p.split;
         const int t1 = min(tokens, (rank + 1) * share), col = n0 + 4 * lane;
@@ -312,6 +318,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
                     x[i] = ld_cluster_f4(a + t * 512);
                     if (p.split == 2) y[i] = ld_cluster_f4(b + t * 512);
                 }
+                if (__any_sync(0xffffffffu, gave_up != 0)) break;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (t0 + i * WARPS >= t1) break;
@@ -330,6 +337,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
 #pragma unroll
                 for (int r = 0; r < 8; ++r)
                     if (r < p.split) part[r] = ld_cluster_f4(from[r] + t * 512);
+                if (__any_sync(0xffffffffu, gave_up != 0)) break;
                 float4 sum = part[0];
 #pragma unroll
                 for (int r = 1; r < 8; ++r) {
@@ -779,6 +787,7 @@ cudaError_t launch_few(const Fp4Product& a, bool early, int* status, cudaStream_
     p.vec = (reinterpret_cast<uintptr_t>(a.D) | static_cast<uintptr_t>(a.ldd) * size) % (4 * size) == 0;
     p.early = early;
     p.status = status;
+    p.wait_limit = a.wait_limit;
     const int steps = (a.K - 1) / BK + 1;
     const long long tiles = static_cast<long long>(p.tiles_n) * ((a.M - 1) / 128 + 1);
     // K over more CTAs while they are at most 5/4 of the SMs: with N = K = 4096 a token

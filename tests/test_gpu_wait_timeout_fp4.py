@@ -1,7 +1,10 @@
 """Bounded waits that run out in the MXFP4 products, at limits from far below a copy's
 latency (every wait gives up) to above a whole product's: a kernel gives up anywhere in
-between.  Each time the host reads the status, no copy is left in flight, what is not the
-output stays, and the next product with the default bound is the one before."""
+between.  Each time the host reads the status, no copy is left in flight, an entry of the
+output is right or untouched, what is not the output stays, and the next product with the default
+bound is the one before."""
+
+import time
 
 import pytest
 
@@ -33,6 +36,8 @@ def interrupted(M, call, want, m, n, dtype, surely):
         call(f, buf[1:-1, :n])
         torch.cuda.synchronize()
         seen.append(f.status())
+        D = buf[1:-1, :n]
+        assert ((D == want) | (D == 7)).all()
         M.moara_set_wait_limit(f.ctx, 0)
         assert (buf[0] == 7).all() and (buf[-1] == 7).all() and (buf[:, n:] == 7).all()
         if seen[-1] == 0:
@@ -54,4 +59,28 @@ def test_pairs_give_up_and_recover(M, shape, dtype):
     a, b = (f.quantize(torch.randn(x, k, generator=gen, device="cuda")) for x in (m, n))
     want = f.product(a, b, dtype=dtype)
     interrupted(M, lambda g, out: g.product(a, b, out=out), want, m, n, dtype, k >= LONG)
+    f.close()
+
+
+# tokens, N, K; few tiles, so that clusters share K, and several tiles; up to 8 tokens are
+# quantised inside the kernel by linear
+FEW = [(1, 4096, 4096), (5, 300, 160000), (8, 2600, 40000), (12, 300, 160000), (40, 1003, 80000), (128, 300, 160000),
+       (200, 129, 160000), (77, 1003, 2049)]
+
+
+@pytest.mark.parametrize("shape", FEW)
+@pytest.mark.parametrize("form", ["product", "linear"])
+def test_few_tokens_give_up_and_recover(M, shape, form):
+    m, n, k = shape
+    f = M.Fp4Group()
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x, w = (torch.randn(r, k, generator=gen, device="cuda") for r in (m, n))
+    a, b = f.quantize(x), f.quantize(w)
+    want = f.product(a, b)
+    torch.cuda.synchronize()
+    begin = time.time()
+    interrupted(M, lambda g, out: g.product(a, b, out=out) if form == "product" else g.linear(x, b, out=out),
+                want, m, n, torch.bfloat16, k >= 80000)
+    # no wait for a phase that never ends: those take the default bound, 2 s each
+    assert time.time() - begin < 2
     f.close()
