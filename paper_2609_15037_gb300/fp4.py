@@ -44,6 +44,15 @@ class Fp4Matrix:
     def sf(self):
         return self._sf if self._both is None else self._both[self._ptrs[1] - self._ptrs[0]:]
 
+    def record_stream(self, stream):
+        """As torch.Tensor.record_stream: once this operand is released, its memory is taken
+        again only behind what `stream` (a torch.cuda.Stream or a cudaStream_t handle) has been
+        given by then."""
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=self.device)
+        for x in (self._q, self._sf) if self._both is None else (self._both,):
+            x.record_stream(stream)
+
 
 def _operand(buffer, rows, cols, device):
     """The operand in a buffer of the native module: (tensor, address of q, of sf)."""
@@ -64,7 +73,9 @@ class Fp4Group:
         dx = fp4.product(dy_r, w_c)                         # dy W
         dW = fp4.product(dy_c, x_c)                         # dy^T x, G of MoaraGroup.step
 
-    Streams are cudaStream_t handles; None is torch's current stream."""
+    Streams are cudaStream_t handles; None is torch's current stream.  A call orders nothing
+    between streams: an input that was made on another one has to be complete, and has to live
+    until the call's work is done (record_stream of the tensor or operand)."""
 
     def __init__(self, device=0):
         self.device = device
