@@ -33,7 +33,9 @@ class Fp4Matrix:
             if (x is None or x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size
                     or x.get_device() != device):
                 raise ValueError(f"q and sf, contiguous uint8 tensors of {sizes} bytes on cuda:{device}, or neither are needed")
-        self._q, self._sf = q, sf
+        # tensors of its own on the same memory: q and sf keep their identity where their storage is
+        # replaced
+        self._q, self._sf = q.detach(), sf.detach()
         self._ptrs = q.data_ptr(), sf.data_ptr()
 
     @property

@@ -123,3 +123,13 @@ def test_memory_of_a_replaced_storage_is_free_again(M):
     assert opt.add(old) == 1
     with pytest.raises(ValueError):
         opt.add(a.data)
+
+
+def test_an_operand_keeps_the_memory_it_was_made_of(M):
+    nq, nsf = M.moara_fp4_bytes(4, 64)
+    q, sf = torch.ones(nq, dtype=torch.uint8), torch.ones(nsf, dtype=torch.uint8)
+    a = M.Fp4Matrix(4, 64, q, sf, device=-1)
+    places = q.data_ptr(), sf.data_ptr()
+    q.data, sf.data = torch.zeros(nq, dtype=torch.uint8), torch.zeros(nsf, dtype=torch.uint8)
+    assert (a.q.data_ptr(), a.sf.data_ptr()) == places == a._ptrs
+    assert a.q.all() and a.sf.all()
