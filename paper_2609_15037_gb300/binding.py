@@ -340,29 +340,41 @@ def moara_grad_norm(ctx, count, grads, sizes, dtypes, max_norm, extra_sq, out, w
 
 
 # --------------------------------------------------- MXFP4 operands and products
+def _sizes(*sizes):
+    """Sizes that a C int holds; ctypes would pass the lower 32 bits of others."""
+    for x in sizes:
+        if not -2 ** 31 <= x < 2 ** 31:
+            raise ValueError(f"a size of {x}: at most 2^31 - 1")
+
+
 def moara_fp4_bytes(rows, cols):
     """(bytes of q, bytes of sf) of a rows x cols operand."""
+    _sizes(rows, cols)
     q, sf = ctypes.c_size_t(), ctypes.c_size_t()
     _check(_lib.moara_fp4_bytes(rows, cols, ctypes.byref(q), ctypes.byref(sf)), what="moara_fp4_bytes")
     return q.value, sf.value
 
 
 def moara_fp4_quantize(ctx, X, dtype, rows, cols, ld, q=0, sf=0, qt=0, sft=0, stream=0):
+    _sizes(rows, cols)
     _check(_lib.moara_fp4_quantize(ctx, X, dtype, rows, cols, ld, q or None, sf or None, qt or None,
                                    sft or None, stream), ctx, "moara_fp4_quantize")
 
 
 def moara_fp4_dequantize(ctx, q, sf, rows, cols, out, dtype, ldo, stream=0):
+    _sizes(rows, cols)
     _check(_lib.moara_fp4_dequantize(ctx, q, sf, rows, cols, out, dtype, ldo, stream), ctx,
            "moara_fp4_dequantize")
 
 
 def moara_fp4_product(ctx, M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, stream=0):
+    _sizes(M, N, K)
     _check(_lib.moara_fp4_product(ctx, M, N, K, a_q, a_sf, b_q, b_sf, D, d_dtype, ldd, stream), ctx,
            "moara_fp4_product")
 
 
 def moara_fp4_linear_workspace_bytes(M, N, K):
+    _sizes(M, N, K)
     out = ctypes.c_size_t()
     _check(_lib.moara_fp4_linear_workspace_bytes(M, N, K, ctypes.byref(out)),
            what="moara_fp4_linear_workspace_bytes")
@@ -371,6 +383,7 @@ def moara_fp4_linear_workspace_bytes(M, N, K):
 
 def moara_fp4_linear(ctx, M, N, K, X, x_dtype, ldx, b_q, b_sf, D, d_dtype, ldd, workspace=0,
                      workspace_bytes=0, stream=0):
+    _sizes(M, N, K)
     _check(_lib.moara_fp4_linear(ctx, M, N, K, X, x_dtype, ldx, b_q, b_sf, D, d_dtype, ldd, workspace or None,
                                  workspace_bytes, stream), ctx, "moara_fp4_linear")
 

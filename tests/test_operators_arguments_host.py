@@ -133,3 +133,15 @@ def test_an_operand_keeps_the_memory_it_was_made_of(M):
     q.data, sf.data = torch.zeros(nq, dtype=torch.uint8), torch.zeros(nsf, dtype=torch.uint8)
     assert (a.q.data_ptr(), a.sf.data_ptr()) == places == a._ptrs
     assert a.q.all() and a.sf.all()
+
+
+@pytest.mark.parametrize("big", [2 ** 31, 2 ** 32 + 1, -2 ** 32 + 1])
+def test_sizes_beyond_32_bits_are_refused(M, big):
+    """Not taken by their lower half."""
+    for call in (lambda: M.moara_fp4_bytes(big, 32), lambda: M.moara_fp4_bytes(32, big), lambda: M.Fp4Matrix(big, 32),
+                 lambda: M.moara_fp4_linear_workspace_bytes(big, 32, 32), lambda: M.moara_fp4_linear_workspace_bytes(16, 32, big),
+                 lambda: M.moara_fp4_quantize(None, 0, 0, big, 1, 1), lambda: M.moara_fp4_dequantize(None, 0, 0, 1, big, 0, 0, big),
+                 lambda: M.moara_fp4_product(None, 1, big, 1, 0, 0, 0, 0, 0, 0, big),
+                 lambda: M.moara_fp4_linear(None, 1, 1, big, 0, 0, big, 0, 0, 0, 0, 1)):
+        with pytest.raises(ValueError):
+            call()
