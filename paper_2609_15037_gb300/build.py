@@ -66,28 +66,46 @@ def _compile(src, verbose_ptxas=False):
     return obj, p.stderr
 
 
-def _build_host():
-    """_host.so: again when its source, torch or the interpreter is another one."""
+def _identity(path):
+    """Which file is at `path`: the libraries lie beside the sources, where a build on another
+    machine replaces them."""
+    s = os.stat(path)
+    return f"{path} {s.st_size} {s.st_mtime_ns}"
+
+
+def _host_command(out):
     import torch
     root = os.path.dirname(torch.__file__)
-    python = sysconfig.get_paths()["include"]
-    cxx = shutil.which("g++") or "g++"
-    key = "\n".join([HOST, torch.__version__, sys.version, *(str(os.path.getmtime(f)) for f in (HOST_SRC, os.path.join(ROOT, "include", "moara.h")))])
+    return [shutil.which("g++") or "g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall",
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            "-isystem", os.path.join(root, "include"),
+            "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+            "-isystem", sysconfig.get_paths()["include"], "-I", os.path.join(ROOT, "include"), HOST_SRC, "-o", out,
+            "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+
+
+def _host_key():
+    """What _host.so was built from, by what and on which machine, and which file it is."""
+    import torch
+    return "\n".join([platform.machine(), torch.__version__, sys.version, *_host_command(HOST),
+                      *(str(os.stat(f).st_mtime_ns) for f in (HOST_SRC, os.path.join(ROOT, "include", "moara.h"))),
+                      _identity(HOST)])
+
+
+def _build_host():
+    """_host.so: again when its key is another one."""
     stamp = os.path.join(OUT_DIR, "host.stamp")
-    if os.path.exists(HOST) and os.path.exists(stamp) and open(stamp).read() == key:
-        return
+    if os.path.exists(HOST) and os.path.exists(stamp):
+        with open(stamp) as f:
+            if f.read() == _host_key():
+                return
     tmp = HOST + ".tmp"
-    cmd = [cxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall",
-           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-           "-isystem", os.path.join(root, "include"),
-           "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"), "-isystem", python,
-           "-I", os.path.join(ROOT, "include"), HOST_SRC, "-o", tmp, "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
-    p = subprocess.run(cmd, capture_output=True, text=True)
+    p = subprocess.run(_host_command(tmp), capture_output=True, text=True)
     if p.returncode != 0:
         raise RuntimeError(f"g++ failed for host.cpp:\n{p.stdout}\n{p.stderr}")
     os.replace(tmp, HOST)
     with open(stamp, "w") as f:
-        f.write(key)
+        f.write(_host_key())
 
 
 def build(verbose_ptxas=False, jobs=None):
@@ -106,7 +124,7 @@ def build(verbose_ptxas=False, jobs=None):
     newest = max(os.path.getmtime(o) for o in objs)
     stamp = os.path.join(OUT_DIR, "lib.stamp")
     fresh = (os.path.exists(LIB) and os.path.exists(stamp) and
-             os.path.getmtime(LIB) >= newest and open(stamp).read() == LIB)
+             os.path.getmtime(LIB) >= newest and open(stamp).read() == _identity(LIB))
     if not fresh:
         tmp = LIB + ".tmp"
         cmd = [_nvcc()] + ARCH + ["-shared", "-o", tmp] + objs + ["-lcudart"]
@@ -115,7 +133,7 @@ def build(verbose_ptxas=False, jobs=None):
             raise RuntimeError(f"link failed:\n{p.stdout}\n{p.stderr}")
         os.replace(tmp, LIB)
         with open(stamp, "w") as f:
-            f.write(LIB)
+            f.write(_identity(LIB))
     return LIB
 
 
