@@ -28,10 +28,7 @@ namespace {
 // contraction), so that the codes follow from the formulas alone.
 // ---------------------------------------------------------------------------
 constexpr float kCodeTop = 1.875f;
-// 8 / 15 = 1 / 1.875 as a float below it and the rest: a scale takes one rounding, to either
-// side.  The nearest float alone is 5e-8 too large, which every step would add to the moments
-// once more (1e-4 in 2000 steps).
-constexpr float kUnit = 0x1.111110p-1f, kUnitRest = static_cast<float>(8.0 / 15.0 - 0x1.111110p-1);
+constexpr float kCodeUnit = 1.0f / 1.875f;
 
 // Four codes of exp_avg: sign, 4 exponent and 3 mantissa bits are the upper bits of
 // an fp16 number without its top exponent bit, subnormals included.
@@ -389,8 +386,8 @@ __device__ __forceinline__ void adam_tile8(const AdamTensor& t, const AdamCall& 
     else encode_sq<false>(v, vi, r, w);
     store8<FULL>(static_cast<uint8_t*>(t.v), at, n, w);
     if (lane == 0) {
-        t.ms[i0 >> 8] = mf ? __fmaf_rn(mt, kUnit, __fmul_rn(mt, kUnitRest)) : 0.0f;
-        t.vs[i0 >> 8] = vf ? __fmaf_rn(vt, kUnit, __fmul_rn(vt, kUnitRest)) : 0.0f;
+        t.ms[i0 >> 8] = mf ? __fmul_rn(mt, kCodeUnit) : 0.0f;
+        t.vs[i0 >> 8] = vf ? __fmul_rn(vt, kCodeUnit) : 0.0f;
     }
 }
 
