@@ -444,9 +444,12 @@ typedef struct moara_adamw_hparams {
  * MOARA_DTYPE_BLOCK8: entry i of block i / 256 (of the flattened tensor) is
  * scale * y(code) with y in [0, 1.875]: 3 mantissa bits, and a sign and 4 exponent
  * bits for exp_avg (largest exponent 0, subnormal below 2^-14) or 5 exponent bits
- * for exp_avg_sq (subnormal below 2^-30).  scale = the block's largest magnitude
- * / 1.875, in fp32, so that a block whose entries all decay alike decays exactly.
- * Codes are rounded stochastically (unbiased: with beta2 = 0.999 an entry moves by
+ * for exp_avg_sq (subnormal below 2^-30).  scale = the block's largest magnitude times
+ * the float 1 / 1.875, in fp32, so that a block whose entries all decay alike keeps its codes, but
+ * for the roundings of their quotients: one that these put just below its own code takes the
+ * next lower one where its 16 random bits are zero.  The float is 5.2e-8 of itself too
+ * large, by which a block's values grow per step (2^-24 is 6.0e-8).
+ * Codes are rounded stochastically (unbiased to 2^-16 of a code step: with beta2 = 0.999 an entry moves by
  * less than half a code step per step, and rounding to nearest would never move
  * it) with 16 bits of a hash of (seed, id, t, i): the same call gives the same
  * result.  An exp_avg_sq > 0 takes at least the smallest code, so that no

@@ -28,6 +28,9 @@ namespace {
 // contraction), so that the codes follow from the formulas alone.
 // ---------------------------------------------------------------------------
 constexpr float kCodeTop = 1.875f;
+// The nearest float to 1 / 1.875, 5.2e-8 of itself too large: a block's values grow by so much
+// with every step, beside a decay of 1 - beta (1e-4 in 2000 steps without a gradient, 5.2e-8 /
+// (1 - beta) where gradients keep coming).
 constexpr float kCodeUnit = 1.0f / 1.875f;
 
 // Four codes of exp_avg: sign, 4 exponent and 3 mantissa bits are the upper bits of
