@@ -21,6 +21,7 @@ _STATES = {"f32": B.MOARA_DTYPE_F32, "block8": B.MOARA_DTYPE_BLOCK8}
 _DESC = np.dtype(B.moara_adamw_tensor)
 _PACK = struct.Struct("<q7Q3iI2f")          # the same as one record
 _SIZE = _PACK.size
+_PLACES = np.dtype([("storage", np.uint64, 4), ("data", np.uint64, 4)])     # of a tensor's moments: host.cpp
 
 
 def entry_address(name):
@@ -61,14 +62,14 @@ class _Ranges:
     def __init__(self):
         self._begin, self._end = [], []
 
-    def add(self, tensors, at):
-        """The memory of these contiguous tensors at these addresses (0: of none), all of it or
-        nothing; ValueError where it overlaps a range or itself."""
+    def add(self, at, sizes):
+        """The memory at these addresses (0: none), all of it or nothing; ValueError where it
+        overlaps a range or itself."""
         taken = []
-        for x, begin in zip(tensors, at):
+        for begin, size in zip(at, sizes):
             if begin == 0:
                 continue
-            end = begin + x.nbytes
+            end = begin + size
             i = bisect.bisect_right(self._begin, begin)
             if (i and self._end[i - 1] > begin) or (i < len(self._begin) and self._begin[i] < end):
                 for b in taken:
@@ -83,8 +84,9 @@ class _Ranges:
 class AdamWGroup:
     """Tensors that take AdamW steps together, with their moments.
 
-    A registered tensor whose storage is replaced (an assignment to .data, module.to) is
-    followed to its new place and type, and refused where it no longer fits.  What a step
+    A registered parameter or copy whose storage is replaced (an assignment to .data,
+    module.to) is followed to its new place and type, and refused where it no longer fits; the
+    memory of the moments is the group's from add on.  What a step
     writes (parameters, copies, moments) must not overlap: a tensor is registered once, and
     taken once per call.
     Streams are cudaStream_t handles; None is torch's current stream."""
@@ -96,9 +98,10 @@ class AdamWGroup:
         self.ctx = B.moara_create(B.moara_default_hparams(), device)
         self._dev = torch.device("cuda", device)
         self.params, self.copies, self.states = [], [], []
-        self._kept = []         # of each tensor: param, copy, and the four tensors of its moments
+        self._own = []          # of each tensor: four tensors, or None, on its moments' memory
         self._ranges = _Ranges()
-        self._table, self._room, self._all = np.zeros(0, _DESC), 0, None
+        self._table, self._places, self._places_at = np.zeros(0, _DESC), np.zeros(0, _PLACES), 0
+        self._room, self._all = 0, None
         self._workspace = {}
 
     def _check(self, x, what, n=None, dtypes=tuple(_TYPES)):
@@ -124,6 +127,12 @@ class AdamWGroup:
             self._check(moments[3], "exp_avg_sq_scale", blocks, (torch.float32,))
         return [0 if x is None else x.data_ptr() for x in kept]
 
+    @staticmethod
+    def _bytes(n, dtype, state):
+        """Of what _check_kept takes."""
+        code, blocks = 1 if state == "block8" else 4, 4 * -(-n // B.MOARA_ADAMW_BLOCK)
+        return 4 * n if dtype is torch.float32 else 2 * n, 2 * n, code * n, code * n, blocks, blocks
+
     def add(self, param, copy=None, state="f32", weight_decay=0.0, lr_scale=1.0, exp_avg=None, exp_avg_sq=None,
             exp_avg_scale=None, exp_avg_sq_scale=None, id=None):
         """Registers `param` (fp32 or bf16, updated in place) and returns its
@@ -147,17 +156,19 @@ class AdamWGroup:
         at = self._check_kept(tensors, n, state)
         i = len(self.params)
         self._grow(i + 1)
+        own = _host.own(tensors[2:], self._places_at + i * _PLACES.itemsize)
         _PACK.pack_into(self._table, i * _SIZE, n, at[0], 0, *at[1:],
                         _TYPES[param.dtype], 0, _STATES[state], i if id is None else id, weight_decay, lr_scale)
+        sizes = self._bytes(n, param.dtype, state)
         try:
-            self._ranges.add(tensors, at)
+            self._ranges.add(at, sizes)
         except ValueError:      # or they lie where a replaced storage was
             self._follow()
-            self._ranges.add(tensors, at)
+            self._ranges.add(at, sizes)
         self.params.append(param)
         self.copies.append(copy)
         self.states.append(types.MappingProxyType(s))
-        self._kept.append(tensors)
+        self._own.append(own)
         return i
 
     def _grow(self, count):
@@ -165,60 +176,70 @@ class AdamWGroup:
         if count > self._room:
             grown = np.zeros(max(16, 2 * count), _DESC)
             grown[:self._room] = self._table[:self._room]
-            self._table, self._room = grown, len(grown)
+            places = np.zeros(len(grown), _PLACES)
+            places[:self._room] = self._places[:self._room]
+            self._table, self._places, self._room = grown, places, len(grown)
+            self._places_at = places.ctypes.data
         self._all = None
 
     def _chosen(self, ids):
-        """The descriptors of a call, their address, and the tensors behind them."""
+        """The descriptors of a call, their number and address, the address of the moments' places,
+        and the parameters and copies."""
         if self._all is None:                       # they and their address are kept
-            self._all = self._table[:len(self.params)], self._table.ctypes.data, self._kept
+            n = len(self.params)
+            self._all = self._table[:n], n, self._table.ctypes.data, self._places_at, self.params, self.copies
         if ids is None:
             return self._all
-        rows = np.arange(len(self.params))[list(ids)]
+        rows = np.arange(len(self.params))[ids]
         at = rows.tolist()
         if len(set(at)) != len(at):
             raise ValueError("ids: a tensor is listed twice")
-        d = self._all[0][rows]
-        return d, d.ctypes.data, [self._kept[i] for i in at]
+        d, places = self._all[0][rows], self._places[rows]
+        return (d, len(at), d.ctypes.data, places.ctypes.data, [self.params[i] for i in at], [self.copies[i] for i in at],
+                places)
 
     def _follow(self):
         """The descriptors of tensors whose storage was replaced (an assignment to .data,
-        module.to): their new places and types.  One that no longer fits is refused."""
-        d, places, ranges = self._table[:len(self.params)], [], _Ranges()
-        for x, n, state in zip(self._kept, d["n"].tolist(), d["state_dtype"].tolist()):
-            places.append(self._check_kept(x, n, "block8" if state == B.MOARA_DTYPE_BLOCK8 else "f32"))
+        module.to) or taken anew in place: their new places and types.  One that no longer fits is
+        refused."""
+        n = len(self.params)
+        d, places, at, ranges = self._table[:n], self._places[:n], [], _Ranges()
+        for p, c, own, size, state in zip(self.params, self.copies, self._own, d["n"].tolist(), d["state_dtype"].tolist()):
+            x, state = (p, c, *own), "block8" if state == B.MOARA_DTYPE_BLOCK8 else "f32"
+            at.append(self._check_kept(x, size, state))
             for y in x:
                 if y is not None and y.untyped_storage().nbytes() < (y.storage_offset() + y.numel()) * y.element_size():
                     raise ValueError("the storage of a registered tensor was freed")
-            ranges.add(x, places[-1])
+            ranges.add(at[-1], self._bytes(size, p.dtype, state))
         fields = "param", "param_bf16", "exp_avg", "exp_avg_sq", "exp_avg_scale", "exp_avg_sq_scale"
-        for name, column in zip(fields, zip(*places)):
+        for name, column in zip(fields, zip(*at)):
             d[name] = column
-        d["param_dtype"] = [_TYPES[x[0].dtype] for x in self._kept]
+        d["param_dtype"] = [_TYPES[p.dtype] for p in self.params]
+        for i, own in enumerate(self._own):
+            places["data"][i] = [0 if x is None else x.untyped_storage().data_ptr() for x in own]
         self._ranges = ranges
 
-    def _called(self, ids, call):
-        """The code of call(count, descriptors' address, kept tensors), which is made again
-        where it found tensors in other places."""
-        ids = ids if ids is None else list(ids)
-        for _ in range(2):
-            d, at, kept = self._chosen(ids)
-            code = call(len(d), at, kept)
-            if code is not None:
-                return code
-            self._follow()
-        raise RuntimeError("registered tensors change during the call")
+    def _check_code(self, code, name):
+        if code is None:
+            raise RuntimeError("registered tensors change during the call")
+        if code:
+            B._check(code, self.ctx, name)
 
     def step(self, grads, t, lr, grad_scale=None, ids=None, stream=None):
         """One AdamW step at step t (1-based): grads[i] (fp32 or bf16) of every
         registered tensor, or of those in ids.  grad_scale: a one-element
         float32 device tensor that multiplies every gradient, or None."""
-        grads = _listed(grads)
-        code = self._called(ids, lambda n, at, kept: _host.adamw_step(
-            _STEP, self.ctx, n, at, grads, ctypes.addressof(self.hp), t, lr, grad_scale, self.device,
-            stream_handle(stream, self.device), kept))
-        if code:
-            B._check(code, self.ctx, "moara_adamw_step")
+        grads, ids = _listed(grads), ids if ids is None else list(ids)
+        stream = stream_handle(stream, self.device)
+        for _ in range(2):                          # again where tensors were found in other places
+            c = self._chosen(ids)
+            code = _host.adamw_step(_STEP, self.ctx, c[1], c[2], grads, ctypes.addressof(self.hp), t, lr, grad_scale,
+                                    self.device, stream, c[3], c[4], c[5])
+            if code is not None:
+                break
+            self._follow()
+        if code != 0:
+            self._check_code(code, "moara_adamw_step")
 
     def moments(self, exp_avg=None, exp_avg_sq=None, ids=None, stream=None):
         """The moments as fp32 tensors (lists, one per tensor); into the given
@@ -230,10 +251,15 @@ class AdamWGroup:
                 exp_avg, exp_avg_sq = ([torch.empty(k, device=self._dev) for k in sizes] if x is None else x
                                        for x in (exp_avg, exp_avg_sq))
         m, v = _listed(exp_avg), _listed(exp_avg_sq)
-        code = self._called(ids, lambda n, at, kept: _host.adamw_moments(
-            _MOMENTS, self.ctx, n, at, m, v, self.device, stream_handle(stream, self.device), kept))
-        if code:
-            B._check(code, self.ctx, "moara_adamw_moments")
+        stream = stream_handle(stream, self.device)
+        for _ in range(2):
+            c = self._chosen(ids)
+            code = _host.adamw_moments(_MOMENTS, self.ctx, c[1], c[2], m, v, self.device, stream, c[3])
+            if code is not None:
+                break
+            self._follow()
+        if code != 0:
+            self._check_code(code, "moara_adamw_moments")
         return exp_avg, exp_avg_sq
 
     def _norm_workspace(self, count, handle):
@@ -267,15 +293,15 @@ class AdamWGroup:
         return got
 
     def state_dict(self):
-        return [{k: v.detach().clone() for k, v in s.items()} for s in self.states]
+        return [{k: v.clone() for k, v in zip(s, own)} for s, own in zip(self.states, self._own)]
 
     def load_state_dict(self, sd):
         """Into the registered tensors' moments; nothing is taken of one that does not fit."""
         like = [{k: (v.dtype, v.shape) for k, v in s.items()} for s in sd]
-        if like != [{k: (v.dtype, v.shape) for k, v in s.items()} for s in self.states]:
+        if like != [{k: (v.dtype, v.shape) for k, v in zip(s, own)} for s, own in zip(self.states, self._own)]:
             raise ValueError("load_state_dict: the moments of other tensors")
-        for s, new in zip(self.states, sd):
-            for k, v in s.items():
+        for s, own, new in zip(self.states, self._own, sd):
+            for k, v in zip(s, own):
                 v.copy_(new[k])
 
     def close(self):

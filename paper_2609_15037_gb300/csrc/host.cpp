@@ -5,6 +5,7 @@
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/StorageImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -78,41 +79,61 @@ PyObject* caught(const std::exception& e) {
 // contiguous tensor of this type and size at it.  A tensor keeps its identity while its
 // storage is replaced (an assignment to .data, module.to).
 bool in_place(PyObject* o, const void* at, at::ScalarType type, int64_t entries) {
-    if (!THPVariable_Check(o)) return o == Py_None && at == nullptr;
+    if (o == Py_None) return at == nullptr;         // asking torch about None takes 60 ns
+    if (!THPVariable_Check(o)) return false;
     const at::Tensor& t = THPVariable_Unpack(o);
-    return t.scalar_type() == type && t.numel() == entries && t.is_contiguous() && t.const_data_ptr() == at;
+    return t.const_data_ptr() == at && t.scalar_type() == type && t.numel() == entries && t.is_contiguous();
 }
 
-// Whether the moments, and with `step` the parameter and its copy, of a tensor are where
-// its descriptor says.  kept: (param, copy, exp_avg, exp_avg_sq, exp_avg_scale, exp_avg_sq_scale)
-bool in_place(PyObject* kept, const moara_adamw_tensor& d, bool step) {
-    PyObject* const* x = &PyTuple_GET_ITEM(kept, 0);
-    const bool block8 = d.state_dtype == MOARA_DTYPE_BLOCK8;
-    const at::ScalarType code = block8 ? at::kByte : at::kFloat;
-    const int64_t blocks = (d.n + MOARA_ADAMW_BLOCK - 1) / MOARA_ADAMW_BLOCK;
-    return (!step || (in_place(x[0], d.param, d.param_dtype == MOARA_DTYPE_BF16 ? at::kBFloat16 : at::kFloat, d.n) &&
-                      in_place(x[1], d.param_bf16, at::kBFloat16, d.n))) &&
-           in_place(x[2], d.exp_avg, code, d.n) && in_place(x[3], d.exp_avg_sq, code, d.n) &&
-           in_place(x[4], d.exp_avg_scale, at::kFloat, blocks) && in_place(x[5], d.exp_avg_sq_scale, at::kFloat, blocks);
-}
-
-// The list of a call's kept tuples, one for each of n descriptors; false with an error set for
-// anything else.
-bool kept_tuples(PyObject* o, Py_ssize_t n) {
-    bool good = PyList_Check(o) && PyList_GET_SIZE(o) == n;
-    for (Py_ssize_t i = 0; good && i < n; ++i) {
-        PyObject* t = PyList_GET_ITEM(o, i);
-        good = PyTuple_Check(t) && PyTuple_GET_SIZE(t) == 6;
+// Where the storages of a tensor's moments had their memory: adamw.py holds the
+// storages, whose memory can be freed or taken anew in place (resize_).
+struct Places {
+    const c10::StorageImpl* storage[4];
+    const void* data[4];
+    bool hold() const {
+        for (int i = 0; i < 4; ++i)
+            if (storage[i] != nullptr && storage[i]->data() != data[i]) return false;
+        return true;
     }
-    if (!good) PyErr_Format(PyExc_TypeError, "a list of %zd tuples of six is needed", n);
-    return good;
+};
+
+// own(moments, places): tensors of their own on the memory of up to four tensors (or None), whose
+// storages nobody else can replace; writes where they have their memory to the address `places`.
+PyObject* own(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 2)) return nullptr;
+    PyObject* held = nullptr;
+    try {
+        auto* places = static_cast<Places*>(PyLong_AsVoidPtr(a[1]));
+        if (PyErr_Occurred()) return nullptr;
+        if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) > 4) return PyErr_Format(PyExc_TypeError, "a tuple of four is needed");
+        const Py_ssize_t n = PyTuple_GET_SIZE(a[0]);
+        held = PyTuple_New(n);
+        *places = Places{};
+        for (Py_ssize_t i = 0; held != nullptr && i < n; ++i) {
+            PyObject* o = PyTuple_GET_ITEM(a[0], i);
+            if (THPVariable_Check(o)) {
+                at::Tensor t = THPVariable_Unpack(o).detach();
+                places->storage[i] = t.storage().unsafeGetStorageImpl();
+                places->data[i] = places->storage[i]->data();
+                o = THPVariable_Wrap(std::move(t));
+            } else {
+                Py_INCREF(o);
+            }
+            PyTuple_SET_ITEM(held, i, o);
+        }
+        if (PyErr_Occurred()) Py_CLEAR(held);
+        return held;
+    } catch (const std::exception& e) {
+        Py_XDECREF(held);
+        return caught(e);
+    }
 }
 
 // adamw_step(entry, ctx, count, descriptors, gradients, hparams, t, lr, grad_scale, device, stream,
-// kept) -> error code, or None if a kept tensor is not where its descriptor says.  The
-// gradients' addresses and types go into the descriptors.
+// places, params, copies) -> error code, or None if a parameter, a copy (or None) or a moment is not
+// where its descriptor says.  The gradients' addresses and types go into the descriptors.
 PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
-    if (!arguments(count, 12)) return nullptr;
+    if (!arguments(count, 14)) return nullptr;
     try {
         const auto fn = entry<decltype(&moara_adamw_step)>(a[0]);
         const Py_ssize_t n = PyLong_AsSsize_t(a[2]);
@@ -122,9 +143,14 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
         float* scale = scalar_of(a[8], "grad_scale", device);
         if (PyErr_Occurred()) return nullptr;
         if (grads.n != n) return PyErr_Format(PyExc_ValueError, "%zd gradients for %zd tensors", grads.n, n);
-        if (!kept_tuples(a[11], n)) return nullptr;
+        const auto* places = static_cast<const Places*>(PyLong_AsVoidPtr(a[11]));
+        if (!PyList_Check(a[12]) || PyList_GET_SIZE(a[12]) != n || !PyList_Check(a[13]) || PyList_GET_SIZE(a[13]) != n)
+            return PyErr_Format(PyExc_TypeError, "lists of %zd parameters and copies are needed", n);
         for (Py_ssize_t i = 0; i < n; ++i) {
-            if (!in_place(PyList_GET_ITEM(a[11], i), d[i], true)) Py_RETURN_NONE;
+            if (!in_place(PyList_GET_ITEM(a[12], i), d[i].param, d[i].param_dtype == MOARA_DTYPE_BF16 ? at::kBFloat16 : at::kFloat,
+                          d[i].n) ||
+                !in_place(PyList_GET_ITEM(a[13], i), d[i].param_bf16, at::kBFloat16, d[i].n) || !places[i].hold())
+                Py_RETURN_NONE;
             void* at;
             if (grads.get(i, "gradient", device, d[i].n, at, d[i].grad_dtype) == nullptr) return nullptr;
             d[i].grad = at;
@@ -141,7 +167,7 @@ PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t count) {
     }
 }
 
-// adamw_moments(entry, ctx, count, descriptors, exp_avg, exp_avg_sq, device, stream, kept)
+// adamw_moments(entry, ctx, count, descriptors, exp_avg, exp_avg_sq, device, stream, places)
 // -> error code, or None as adamw_step
 PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t count) {
     if (!arguments(count, 9)) return nullptr;
@@ -154,9 +180,10 @@ PyObject* adamw_moments(PyObject*, PyObject* const* a, Py_ssize_t count) {
         auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
         void* stream = PyLong_AsVoidPtr(a[7]);
         if (PyErr_Occurred()) return nullptr;
-        if (!kept_tuples(a[8], n)) return nullptr;
+        const auto* places = static_cast<const Places*>(PyLong_AsVoidPtr(a[8]));
+        if (PyErr_Occurred()) return nullptr;
         for (Py_ssize_t i = 0; i < n; ++i)
-            if (!in_place(PyList_GET_ITEM(a[8], i), d[i], false)) Py_RETURN_NONE;
+            if (!places[i].hold()) Py_RETURN_NONE;
         std::vector<float*> to[2];
         for (int k = 0; k < 2; ++k) {
             if (outs[k].n != n) return PyErr_Format(PyExc_ValueError, "%zd outputs for %zd tensors", outs[k].n, n);
@@ -420,6 +447,7 @@ PyObject* bytes(PyObject*, PyObject* const* a, Py_ssize_t count) {
 #define MOARA_METHOD(name, doc) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, doc}
 
 PyMethodDef methods[] = {
+    MOARA_METHOD(own, "own(moments, places) -> tensors of their own on the same memory"),
     MOARA_METHOD(adamw_step, "moara_adamw_step with a list of gradients -> error code"),
     MOARA_METHOD(adamw_moments, "moara_adamw_moments into two lists of tensors -> error code"),
     MOARA_METHOD(grad_norm, "moara_grad_norm of a list of gradients -> tensor of three, or an error code"),
