@@ -89,7 +89,9 @@ class AdamWGroup:
     memory of the moments is the group's from add on.  What a step
     writes (parameters, copies, moments) must not overlap: a tensor is registered once, and
     taken once per call.
-    Streams are cudaStream_t handles; None is torch's current stream."""
+    Streams are cudaStream_t handles; None is torch's current stream.  A call orders nothing
+    between streams: a tensor that was made on another one has to be complete, and has to live
+    until the call's work is done (torch.Tensor.record_stream)."""
 
     def __init__(self, beta1=0.9, beta2=0.999, eps=1e-8, seed=0, device=0):
         self.device = device

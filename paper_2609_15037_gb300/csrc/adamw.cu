@@ -103,7 +103,7 @@ __device__ __forceinline__ void encode_sq(const float (&x)[8], float inv, const 
     upper_bytes(u, w);
 }
 
-// 32-bit xor-shift-multiply mixing
+// 32-bit xor-shift-multiply mixing: the published finaliser of MurmurHash3 (A. Appleby, public domain)
 __host__ __device__ __forceinline__ uint32_t mix32_rest(uint32_t x) {
     x *= 0x85EBCA6Bu;
     x ^= x >> 13;
