@@ -30,15 +30,16 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // Products with few tiles.  The weight's rows are the MMA's 128 rows, up to 128 rows
 // of A (tokens) its columns, so that a single token costs columns and not rows;
 // a cluster of up to eight CTAs shares K, and each adds the others' sums for its
-// share of the tokens through shared memory.  Bound by latency (launch, one trip
+// share of the tokens through shared memory.  With the weight in L2, bound by latency (launch, one trip
 // to memory, the sums) up to some hundred tokens, then by the operands' way from L2:
-// with N = K = 4096 one token takes 4.7 us, 48 tokens 6.3, 128 8.1, 256 8.9.  (A warp per two rows of
-// the weight without tensor cores takes 4.7 us for a token there and 7.2 against 6.0 with
+// with N = K = 4096 one token takes 4.6 us, 48 tokens 6.2, 128 8.2, 256 8.8 (a weight from
+// DRAM: 5.2, and 8.2 against 6.1 with N = 11008, where its bytes are 3.5).  (A warp per two rows of
+// the weight without tensor cores takes 4.7 us for a token there and 7.2 against 6.1 with
 // N = 11008: the conversions bound it.)
 // With QUANT, A comes as it is (at most 8 rows) and the four epilogue warps
 // quantise a stage's rows into shared memory, so that a token's product is one
-// launch (4.9 us); every CTA of a K range does that again, which pays for few rows: 8 take
-// 6.1 us and 6.8 with a launch of its own for the quantisation, 16 take 8.1 and 6.8.
+// launch (4.6 us); every CTA of a K range does that again, which pays for few rows: 8 take
+// 5.9 us and some 6.4 with a launch of its own for the quantisation, 16 take 8.1 and 6.4.
 // ---------------------------------------------------------------------------
 constexpr int F_THREADS = 6 * 32;                  // TMA, MMA, four epilogue warps
 constexpr int F_STAGES = 4;                        // at most
@@ -306,7 +307,7 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
             }
         };
         // what is read together: a token from each of up to eight CTAs, or four of many tokens
-        // from one or two (128 x 8192 x 600: 7.0 us, token by token 9.2); in one kernel the two
+        // from one or two (128 x 8192 x 600: 7.7 us, token by token 9.6); in one kernel the two
         // take a single token 0.1 us longer
         if constexpr (MANY) {
             const uint32_t a = ptx::mapa(own, 0), b = ptx::mapa(own, p.split - 1);
@@ -361,12 +362,13 @@ __global__ void __launch_bounds__(F_THREADS) k_fp4_few(const __grid_constant__ F
 // tile's MMAs, through 2 KB of shared memory each: rows of 64 bytes whatever their
 // alignment.
 //
-// 16384 x 11008 x 4096 into bf16: 255 us, 5.8 PFLOP/s (three times the bf16 rate), at
-// 2.0 GHz and 1376 of 1400 W; 8192^3 168 us, 6.5 PFLOP/s; 4096^3 31.5 us, 256 tiles in
-// four rounds of 76 pairs.  A stage of 256 entries takes 670 clocks: its four MMAs are
-// 512, and its 35 KB are written to and read from shared memory at 128 bytes a clock in
-// 560.  The drain of a tile costs 0.4 us, the stores of D beside the MMAs another 0.5 of
-// its 7.
+// 16384 x 11008 x 4096 into bf16: 257 us, 5.7 PFLOP/s (three times the bf16 rate), at
+// 2.0 GHz and 1376 of 1400 W; 8192^3 166 us, 6.6 PFLOP/s; 4096^3 28.4 us, 256 tiles in
+// four rounds of 76 pairs.  A stage of 256 entries takes 670 clocks, its four MMAs
+// 512 of them; what they wait for is not known (at 128 bytes a clock its 35 KB would be written
+// to and read from shared memory in 560, but the tensor pipe's reads are counted at 27% of
+// their peak).  The drain of a tile costs 0.4 us, the stores of D beside the MMAs another 0.5 of
+// its 6.9; 0.6 have no account.
 // ---------------------------------------------------------------------------
 constexpr int P_BM = 256, P_BN = 256;
 constexpr int EPI_WARPS = 8;
@@ -820,8 +822,8 @@ cudaError_t launch_few(const Fp4Product& a, bool early, int* status, cudaStream_
 }
 
 // Pairs where their tiles occupy a quarter of the GPU and more, and a sixth where K is
-// short; the other form, which shares K, below that.  20 tiles (512 x 2560 x 4096): 9.7 us against
-// 10.3; 16 (512 x 2048): 9.6 against 8.9, but with K = 2048 7.3 against 7.7; 12 (512 x 1536 x 2048) 7.3
+// short; the other form, which shares K, below that.  20 tiles (512 x 2560 x 4096): 9.4 us against
+// 10.3; 16 (512 x 2048): 9.4 against 8.6, but with K = 2048 7.0 against 7.7; 12 (512 x 1536 x 2048) 7.0
 // against 7.5.
 bool large(const Fp4Product& a) {
     const long long tiles = static_cast<long long>((a.M - 1) / P_BM + 1) * ((a.N - 1) / P_BN + 1);
