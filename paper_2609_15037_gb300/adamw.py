@@ -262,7 +262,7 @@ class AdamWGroup:
             self._follow()
         if code != 0:
             self._check_code(code, "moara_adamw_moments")
-        return exp_avg, exp_avg_sq
+        return m, v
 
     def _norm_workspace(self, count, handle):
         """(tensor, address, bytes, gradients that it serves); zero before its first call."""

@@ -145,3 +145,14 @@ def test_sizes_beyond_32_bits_are_refused(M, big):
                  lambda: M.moara_fp4_linear(None, 1, 1, big, 0, 0, big, 0, 0, 0, 0, 1)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_moments_into_iterables(M, monkeypatch):
+    """Outputs that are no lists come back as lists, not as what was read to its end."""
+    opt = adamw_group(M)
+    opt.add(torch.zeros(8)), opt.add(torch.zeros(3))
+    monkeypatch.setattr(M.adamw._host, "adamw_moments", lambda *a: 0)
+    m, v = ([torch.zeros(8), torch.zeros(3)] for _ in range(2))
+    got = opt.moments(iter(m), (x for x in v), stream=0)
+    assert all(x is y for a, b in zip(got, (m, v)) for x, y in zip(a, b)) and [len(list(x)) for x in got] == [2, 2]
+    assert opt.moments(m, v, stream=0)[0] is m
