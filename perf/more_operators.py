@@ -274,11 +274,13 @@ def _own(s):
     c, layer = s["case"], s["layer"]
     do = c["do"]
     if do.startswith("attention"):
-        out, lse = layer.attention(s["q"], s["k"], s["v"], s["seqs"])
-        got = {"out": out, "lse": lse}
-        if do == "attention_train":
-            got["dq"], got["dk"], got["dv"] = layer.attention_backward(s["do"], s["q"], s["k"], s["v"], out, lse, s["seqs"])
-        return got
+        if do == "attention":
+            out, lse = layer.attention(s["q"], s["k"], s["v"], s["seqs"])
+            return {"out": out, "lse": lse}
+        # rest: what the outputs' rounding dropped, kept for the gradients
+        out, lse, rest = layer.attention(s["q"], s["k"], s["v"], s["seqs"], train=True)
+        dq, dk, dv = layer.attention_backward(s["do"], s["q"], s["k"], s["v"], out, lse, s["seqs"], rest=rest)
+        return {"out": out, "lse": lse, "dq": dq, "dk": dk, "dv": dv}
     if do == "loss":
         ref = s["ref"] if c["kl"] else None
         sums, logp, dz = layer.policy_loss(s["logits"], s["targets"], s["old"], s["adv"], weights=s["weight"], ref=ref,
