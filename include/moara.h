@@ -552,6 +552,95 @@ int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_d
                      const void* b_sf, void* D, int d_dtype, int64_t ldd, void* workspace, size_t workspace_bytes,
                      void* stream);
 
+/* ---- operators of a decoder's layers -------------------------------------
+ *
+ * Root-mean-square norm of rows with the residual's addition:
+ *   H = X + R, rounded to their type;  s = 1 / sqrt(mean H^2 + eps);  Y = (H s) gain
+ * X, R, H: rows x cols of x_dtype (fp32 or bf16), Y of y_dtype, row pitches in entries
+ * (>= cols).  R and H are NULL together: H is X then.  gain: cols floats.  rstd
+ * receives s, one float per row, for the gradients.  Squares are summed in two fp32
+ * numbers, s is the nearest fp32 number but for rare ties, Y is rounded once from fp32; a row's
+ * sum of squares has to lie in fp32's range.  H may be X or R, and Y may be X, R or H, where
+ * type and pitch are the same.  Any alignment of the types; rows that begin on 16-byte lines
+ * are read by lines.  MOARA_ERR_UNSUPPORTED for more than 49152 columns. */
+int moara_rms_norm(moara_ctx* ctx, int rows, int cols, const void* X, int64_t ldx, const void* R, int64_t ldr,
+                   int x_dtype, const float* gain, float eps, void* H, int64_t ldh, void* Y, int y_dtype, int64_t ldy,
+                   float* rstd, void* stream);
+
+/* The same with Y as MXFP4 operands, by rows (q / sf) and by columns (qt / sft) as
+ * moara_fp4_quantize gives them of an fp32 Y; either pair may be NULL. */
+int moara_rms_norm_quantize(moara_ctx* ctx, int rows, int cols, const void* X, int64_t ldx, const void* R, int64_t ldr,
+                            int x_dtype, const float* gain, float eps, void* H, int64_t ldh, void* q, void* sf, void* qt,
+                            void* sft, float* rstd, void* stream);
+
+/* Gradients of the norm from those of Y (dY, fp32 or bf16) and, where it is given, of H
+ * (dH of h_dtype, NULL for none; what flows past the norm):
+ *   dX = dH + s (d - n mean(d n)) with d = dY gain, n = H s     (h_dtype; the gradient of X and of R)
+ *   dgain = sum over rows of dY n                                (floats)
+ * in fp32 with one rounding of dX; the sums over rows in a fixed order.  dX may be dY, H
+ * or dH where type and pitch are the same.  workspace: moara_rms_norm_backward_workspace_bytes
+ * device bytes, 16-byte aligned, in use by one call at a time. */
+int moara_rms_norm_backward_workspace_bytes(int rows, int cols, size_t* out);
+int moara_rms_norm_backward(moara_ctx* ctx, int rows, int cols, const void* dY, int dy_dtype, int64_t lddy,
+                            const void* H, int h_dtype, int64_t ldh, const float* gain, const float* rstd,
+                            const void* dH, int64_t lddh, void* dX, int64_t lddx, float* dgain, void* workspace,
+                            size_t workspace_bytes, void* stream);
+
+/* Packed sequences: token i of the first sequence is row i, the second begins behind
+ * the first, and so on.  moara_sequences_init lists their tiles for the attention kernels
+ * into `tiles` (host memory, moara_sequences_bytes); the caller copies them to the device
+ * and sets out->tiles to the copy, which every later call only reads.  Lengths may
+ * be zero. */
+typedef struct moara_sequences {
+    const void* tiles;      /* device memory, 16-byte aligned                       */
+    int tokens;             /* sum of the lengths                                   */
+    int n_tiles;            /* tiles of 128 tokens                                  */
+    int n_pairs;            /* of 256                                               */
+} moara_sequences;
+int moara_sequences_bytes(int count, const int* lengths, size_t* out);
+int moara_sequences_init(int count, const int* lengths, void* tiles, size_t bytes, moara_sequences* out);
+
+/* Causal attention inside packed sequences: of each query head h, with head h / (heads /
+ * kv_heads) of k and v, and for token i the keys j <= i of its sequence,
+ *   S = scale q k^T, P = softmax S, out = P V, lse = log sum exp S
+ * q, k, v: bf16, entry e of head h of token t at [t * row + h * head + e]; 16-byte aligned,
+ * pitches positive multiples of 8; dim a multiple of 8 up to 128; scale > 0; kv_heads divides
+ * heads; tokens >= seqs->tokens.  out: tokens x heads x dim bf16, lse: heads x tokens
+ * floats.  rest: NULL, or like out: what the rounding of out dropped, for the gradients.  Rows
+ * behind the last sequence are neither read nor written.  Entries of a sequence that are not finite
+ * make rows of that sequence NaN, of no other.  P is rounded to bf16 for its product. */
+int moara_attention(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int heads, int kv_heads, int dim, float scale,
+                    const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row, int64_t k_head,
+                    const void* v, int64_t v_row, int64_t v_head, void* out, void* rest, float* lse, void* stream);
+
+/* Its gradients from dout (strided as q), with what the forward call left in out, rest (or
+ * NULL: the gradient of q is less exact for long sequences) and lse: dq tokens x heads x dim,
+ * dk and dv tokens x kv_heads x dim, bf16; the sums over a group's heads in fp32, every sum in
+ * a fixed order.  delta: workspace of heads x tokens floats, in use by one call at a time. */
+int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int heads, int kv_heads, int dim,
+                             float scale, const void* dout, int64_t do_row, int64_t do_head, const void* q, int64_t q_row,
+                             int64_t q_head, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
+                             int64_t v_head, const void* out, const void* rest, const float* lse, float* delta, void* dq,
+                             void* dk, void* dv, void* stream);
+
+/* Clipped policy loss of `rows` tokens and its gradient, from their logits Z (rows x vocab,
+ * fp32 or bf16, row pitch ldz): with lp = log softmax(z)[target], rho = exp(lp - old_logp),
+ * x = ref_logp - lp,
+ *   loss = sum w (-min(rho adv, clamp(rho, low, high) adv) + kl (exp x - x - 1))
+ *   sums = {loss, sum w (exp x - x - 1), sum w [clipped]}
+ *   dZ   = w (kl (1 - exp x) - [not clipped] rho adv) (1[j = target] - softmax(z)_j)
+ * weight: a float per token, or NULL for 1 / rows.  A token of weight zero, or whose target
+ * is outside 0 .. vocab - 1, counts for nothing, whatever its other inputs hold; the latter's logp is
+ * 0.  ref_logp: NULL without a KL term (kl = 0).  logp receives lp, dZ (of Z's type, row pitch
+ * lddz, may be Z with its pitch, or NULL) the gradient.  The sum over a row is held in fp32, those over rows
+ * in two fp32 numbers, all in a fixed order.  workspace: moara_policy_loss_workspace_bytes(rows)
+ * device bytes, 16-byte aligned, in use by one call at a time. */
+int moara_policy_loss_workspace_bytes(int rows, size_t* out);
+int moara_policy_loss(moara_ctx* ctx, int rows, int vocab, const void* Z, int dtype, int64_t ldz, const int64_t* target,
+                      const float* old_logp, const float* ref_logp, const float* adv, const float* weight, float low,
+                      float high, float kl, float* sums, float* logp, void* dZ, int64_t lddz, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -58,6 +58,10 @@ class moara_hparams(ctypes.Structure):
     ]
 
 
+class moara_sequences(ctypes.Structure):
+    _fields_ = [("tiles", ctypes.c_void_p), ("tokens", ctypes.c_int), ("n_tiles", ctypes.c_int), ("n_pairs", ctypes.c_int)]
+
+
 class moara_module_desc(ctypes.Structure):
     _fields_ = [
         ("m", ctypes.c_int), ("n", ctypes.c_int), ("r", ctypes.c_int),
@@ -132,6 +136,18 @@ def _load():
         "moara_fp4_product": (i32, [vp, i32, i32, i32, vp, vp, vp, vp, vp, i32, i64, vp]),
         "moara_fp4_linear_workspace_bytes": (i32, [i32, i32, i32, P(sz)]),
         "moara_fp4_linear": (i32, [vp, i32, i32, i32, vp, i32, i64, vp, vp, vp, i32, i64, vp, sz, vp]),
+        "moara_rms_norm": (i32, [vp, i32, i32, vp, i64, vp, i64, i32, vp, f32, vp, i64, vp, i32, i64, vp, vp]),
+        "moara_rms_norm_quantize": (i32, [vp, i32, i32, vp, i64, vp, i64, i32, vp, f32, vp, i64, vp, vp, vp, vp, vp, vp]),
+        "moara_rms_norm_backward_workspace_bytes": (i32, [i32, i32, P(sz)]),
+        "moara_rms_norm_backward": (i32, [vp, i32, i32, vp, i32, i64, vp, i32, i64, vp, vp, vp, i64, vp, i64, vp, vp, sz,
+                                          vp]),
+        "moara_sequences_bytes": (i32, [i32, P(i32), P(sz)]),
+        "moara_sequences_init": (i32, [i32, P(i32), vp, sz, P(moara_sequences)]),
+        "moara_attention": (i32, [vp, P(moara_sequences), i32, i32, i32, i32, f32] + 3 * [vp, i64, i64] + 4 * [vp]),
+        "moara_attention_backward": (i32, [vp, P(moara_sequences), i32, i32, i32, i32, f32] + 4 * [vp, i64, i64] + 8 * [vp]),
+        "moara_policy_loss_workspace_bytes": (i32, [i32, P(sz)]),
+        "moara_policy_loss": (i32, [vp, i32, i32, vp, i32, i64, vp, vp, vp, vp, vp, f32, f32, f32, vp, vp, vp, i64, vp, sz,
+                                    vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
@@ -388,6 +404,86 @@ def moara_fp4_linear(ctx, M, N, K, X, x_dtype, ldx, b_q, b_sf, D, d_dtype, ldd, 
                                  workspace_bytes, stream), ctx, "moara_fp4_linear")
 
 
+# ------------------------------------------------- operators of a decoder's layers
+def moara_rms_norm(ctx, rows, cols, X, ldx, R, ldr, x_dtype, gain, eps, H, ldh, Y, y_dtype, ldy, rstd, stream=0):
+    _sizes(rows, cols)
+    _check(_lib.moara_rms_norm(ctx, rows, cols, X, ldx, R or None, ldr, x_dtype, gain, eps, H or None, ldh, Y, y_dtype, ldy,
+                               rstd, stream), ctx, "moara_rms_norm")
+
+
+def moara_rms_norm_quantize(ctx, rows, cols, X, ldx, R, ldr, x_dtype, gain, eps, H, ldh, q, sf, qt, sft, rstd, stream=0):
+    _sizes(rows, cols)
+    _check(_lib.moara_rms_norm_quantize(ctx, rows, cols, X, ldx, R or None, ldr, x_dtype, gain, eps, H or None, ldh,
+                                        q or None, sf or None, qt or None, sft or None, rstd, stream), ctx,
+           "moara_rms_norm_quantize")
+
+
+def moara_rms_norm_backward_workspace_bytes(rows, cols):
+    _sizes(rows, cols)
+    out = ctypes.c_size_t()
+    _check(_lib.moara_rms_norm_backward_workspace_bytes(rows, cols, ctypes.byref(out)),
+           what="moara_rms_norm_backward_workspace_bytes")
+    return out.value
+
+
+def moara_rms_norm_backward(ctx, rows, cols, dY, dy_dtype, lddy, H, h_dtype, ldh, gain, rstd, dH, lddh, dX, lddx, dgain,
+                            workspace, workspace_bytes, stream=0):
+    _sizes(rows, cols)
+    _check(_lib.moara_rms_norm_backward(ctx, rows, cols, dY, dy_dtype, lddy, H, h_dtype, ldh, gain, rstd, dH or None, lddh,
+                                        dX, lddx, dgain, workspace, workspace_bytes, stream), ctx, "moara_rms_norm_backward")
+
+
+def _lengths(lengths):
+    lengths = list(lengths)
+    _sizes(len(lengths), *lengths)
+    return lengths, (ctypes.c_int * max(1, len(lengths)))(*lengths)
+
+
+def moara_sequences_bytes(lengths):
+    lengths, at = _lengths(lengths)
+    out = ctypes.c_size_t()
+    _check(_lib.moara_sequences_bytes(len(lengths), at, ctypes.byref(out)), what="moara_sequences_bytes")
+    return out.value
+
+
+def moara_sequences_init(lengths, tiles, size):
+    """The descriptor of sequences whose tiles go to the host address `tiles`."""
+    lengths, at = _lengths(lengths)
+    out = moara_sequences()
+    _check(_lib.moara_sequences_init(len(lengths), at, tiles or None, size, ctypes.byref(out)), what="moara_sequences_init")
+    return out
+
+
+def moara_attention(ctx, seqs, tokens, heads, kv_heads, dim, scale, q, q_row, q_head, k, k_row, k_head, v, v_row, v_head,
+                    out, rest, lse, stream=0):
+    _sizes(tokens, heads, kv_heads, dim)
+    _check(_lib.moara_attention(ctx, ctypes.byref(seqs), tokens, heads, kv_heads, dim, scale, q, q_row, q_head, k, k_row,
+                                k_head, v, v_row, v_head, out, rest or None, lse, stream), ctx, "moara_attention")
+
+
+def moara_attention_backward(ctx, seqs, tokens, heads, kv_heads, dim, scale, dout, do_row, do_head, q, q_row, q_head, k,
+                             k_row, k_head, v, v_row, v_head, out, rest, lse, delta, dq, dk, dv, stream=0):
+    _sizes(tokens, heads, kv_heads, dim)
+    _check(_lib.moara_attention_backward(ctx, ctypes.byref(seqs), tokens, heads, kv_heads, dim, scale, dout, do_row, do_head,
+                                         q, q_row, q_head, k, k_row, k_head, v, v_row, v_head, out, rest or None, lse, delta,
+                                         dq, dk, dv, stream), ctx, "moara_attention_backward")
+
+
+def moara_policy_loss_workspace_bytes(rows):
+    _sizes(rows)
+    out = ctypes.c_size_t()
+    _check(_lib.moara_policy_loss_workspace_bytes(rows, ctypes.byref(out)), what="moara_policy_loss_workspace_bytes")
+    return out.value
+
+
+def moara_policy_loss(ctx, rows, vocab, Z, dtype, ldz, target, old_logp, ref_logp, adv, weight, low, high, kl, sums, logp,
+                      dZ, lddz, workspace, workspace_bytes, stream=0):
+    _sizes(rows, vocab)
+    _check(_lib.moara_policy_loss(ctx, rows, vocab, Z, dtype, ldz, target, old_logp, ref_logp or None, adv, weight or None,
+                                  low, high, kl, sums, logp, dZ or None, lddz, workspace, workspace_bytes, stream), ctx,
+           "moara_policy_loss")
+
+
 PHASES = ["decompose", "project", "backproject", "refresh", "tc_project",
           "tc_backproject", "tc_decompose", "tc_refresh", "tc_decompose_overlap", "clip_norm"]
 
@@ -416,4 +512,7 @@ EXPORTED = [
     "moara_adamw_step", "moara_adamw_moments", "moara_grad_norm_workspace_bytes", "moara_grad_norm",
     "moara_fp4_bytes", "moara_fp4_quantize", "moara_fp4_dequantize", "moara_fp4_product",
     "moara_fp4_linear_workspace_bytes", "moara_fp4_linear",
+    "moara_rms_norm", "moara_rms_norm_quantize", "moara_rms_norm_backward_workspace_bytes", "moara_rms_norm_backward",
+    "moara_sequences_bytes", "moara_sequences_init", "moara_attention", "moara_attention_backward",
+    "moara_policy_loss_workspace_bytes", "moara_policy_loss",
 ]

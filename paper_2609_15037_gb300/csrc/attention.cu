@@ -1,0 +1,810 @@
+// Causal attention over packed sequences with grouped heads, bf16 on the tensor cores.
+//   S = scale q k^T (keys up to the query's own place in its sequence), P = softmax S,
+//   O = P V, lse = log sum exp S
+// and its gradients from dO, with delta = rowsum(dO O):
+//   P = exp(S - lse), dV = P^T dO, dS = P (dO V^T - delta), dQ = scale dS K, dK = scale dS^T Q
+// Bound by the tensor cores (4 D and 10 D operations a visible pair of query and key).  S
+// and dS are fp32 sums in tensor memory and never leave the SM; P and dS are rounded to bf16
+// for the products that take them, the form in which the tensor cores read them: an error
+// of 2^-9 of each term, which the sums over keys or queries average (outputs 1.7e-3 of their
+// norm from the exact ones, of which their own rounding is 1.66e-3).
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "launch.cuh"
+#include "layers.h"
+#include "tc_ptx.cuh"
+#include "waits.cuh"
+
+namespace moara {
+namespace {
+
+using bf16 = __nv_bfloat16;
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int ROWS = 128;                       // of a tile of queries or keys
+constexpr int PANEL = ROWS * 128;               // 64 columns of a tile: 128 rows of one line of the swizzle
+
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// D = A B^T over DP columns, both tiles in shared memory by rows (K-major): 128 x 128.
+template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b) {
+    constexpr uint32_t idesc = ptx::idesc_bf16(128, ROWS, 0, 0);
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+        const uint32_t at = k / 4 * PANEL + k % 4 * 32;
+        ptx::mma_f16(d, ptx::smem_desc_sw128(a + at, 16, 1024), ptx::smem_desc_sw128(b + at, 16, 1024), idesc, k > 0);
+    }
+}
+
+// The same tile as the operand whose rows are summed over: D (128 x DP) (+)= A B with A in
+// tensor memory, 64 entries of K in columns a .. a + 31 and 64 from a + far on; the first
+// 16 `steps` rows of B.
+template <int DP>
+__device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint32_t far, uint32_t b, int steps, bool add) {
+    constexpr uint32_t idesc = ptx::idesc_bf16(128, DP, 0, 1);
+#pragma unroll
+    for (int k = 0; k < ROWS / 16; ++k)
+        if (k < steps)
+            ptx::mma_f16_ta(d, a + k / 4 * far + k % 4 * 8, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, add || k > 0);
+}
+
+// Rows from `rows` to the next multiple of 16 of a tile become zero, by a warp that
+// issues the products next: what lies there is another sequence's (or nothing), and a
+// factor of zero does not silence its infinities and NaN.
+template <int DP> __device__ __forceinline__ void clear_rows(uint8_t* tile, int rows, int lane) {
+    const int n = ((rows + 15) / 16 * 16 - rows) * 8;              // 16-byte pieces of a panel
+    for (int i = lane; i < n * (DP / 64); i += 32)
+        *reinterpret_cast<uint4*>(tile + i / n * PANEL + rows * 128 + i % n * 16) = make_uint4(0, 0, 0, 0);
+    ptx::fence_proxy_async_smem();
+    __syncwarp();
+}
+
+// ---------------------------------------------------------------------------
+// Outputs.  A CTA takes 256 queries of a head, two tiles of 128, and goes through the
+// keys in tiles of 128 from the sequence's first on.  While the four warps of one tile
+// turn its S into P, the tensor cores work for the other: S (128 columns of tensor memory),
+// over which P is written, and O (DP columns) each.  A row belongs to a thread.  A row's
+// maximum is followed lazily: O is only rescaled once S exceeds the reference by 2^8, so
+// that rows rarely wait for their O.
+// ---------------------------------------------------------------------------
+template <int DP> struct Forward {
+    static constexpr int TILE = DP / 64 * PANEL;
+    static constexpr int SLOTS = DP == 128 ? 4 : 8;                // tiles of K and V in turn
+    static constexpr int CTL = 256;
+    static constexpr int SMEM = (2 + SLOTS) * TILE + CTL + 1024;
+    static constexpr int THREADS = 10 * 32;                        // two tiles' warps, copies, products
+};
+
+struct ForwardParams {
+    CUtensorMap q, k, v;
+    bf16* out;
+    bf16* rest;
+    float* lse;
+    const AttentionTile* pairs;
+    int tokens, heads, group, dim;
+    float scale;
+    int* status;
+    long long wait_limit;
+};
+
+template <int SLOTS> struct ForwardCtl {
+    uint64_t qfull[2], full[SLOTS], empty[SLOTS], sfull[2], pfull[2], ofull[2], drain;
+    uint32_t tmem;
+    int abort;
+    int filled;
+};
+
+template <int DP>
+__global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __grid_constant__ ForwardParams p) {
+    using F = Forward<DP>;
+    using Ctl = ForwardCtl<F::SLOTS>;
+    static_assert(sizeof(Ctl) <= F::CTL, "the barriers fit");
+    extern __shared__ uint8_t raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* ring = smem + 2 * F::TILE;
+    Ctl* ctl = reinterpret_cast<Ctl*>(ring + F::SLOTS * F::TILE);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* abort_flag = &ctl->abort;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctl->qfull[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctl->sfull[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctl->pfull[i]), 4);
+            ptx::mbar_init(ptx::smem_u32(&ctl->ofull[i]), 1);
+        }
+        for (int i = 0; i < F::SLOTS; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctl->full[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctl->empty[i]), 1);
+        }
+        ptx::mbar_init(ptx::smem_u32(&ctl->drain), 1);
+        ctl->abort = 0;
+        ctl->filled = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == 9) {
+        ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = ctl->tmem;
+    pdl_begin();
+    const AttentionTile pair = p.pairs[blockIdx.x / p.heads];
+    const int head = blockIdx.x % p.heads, kv = head / p.group;
+    const int q0 = 2 * pair.tile;                                  // the first of the two tiles
+    const bool two = (q0 + 1) * ROWS < pair.length;
+    const int tiles = q0 + 1 + two;                                // of keys; tile i sees q0 + 1 + i
+    auto wait = [&](uint64_t& bar, uint32_t parity) {
+        return ptx::mbar_wait_warp(ptx::smem_u32(&bar), parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
+    };
+
+    if (warp == 8) {
+        if (lane == 0) {
+            auto fill = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
+                const uint32_t b = ptx::smem_u32(&bar);
+                ptx::mbar_arrive_expect_tx(b, F::TILE);
+                for (int c = 0; c < DP / 64; ++c) ptx::tma_load_3d(ptx::smem_u32(to) + c * PANEL, map, b, c * 64, h, row);
+            };
+            fill(smem, &p.q, ctl->qfull[0], head, pair.begin + q0 * ROWS);
+            int n = 0;
+            for (; n < 2 * tiles; ++n) {
+                const int slot = n % F::SLOTS;
+                if (n >= F::SLOTS && !ptx::mbar_wait(ptx::smem_u32(&ctl->empty[slot]), (n / F::SLOTS - 1) & 1, abort_flag, p.status,
+                                                     MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
+                    break;
+                fill(ring + slot * F::TILE, n & 1 ? &p.v : &p.k, ctl->full[slot], kv, pair.begin + n / 2 * ROWS);
+                if (n == 0 && two) fill(smem + F::TILE, &p.q, ctl->qfull[1], head, pair.begin + (q0 + 1) * ROWS);
+            }
+            ctl->filled = n;
+        }
+    } else if (warp == 9) {
+        const bool leader = ptx::elect_one();
+        const uint32_t base = ptx::smem_u32(smem), slots = ptx::smem_u32(ring);
+        auto score = [&](int i, int slot) {
+            if (leader) {
+                mma_rows<DP>(tmem + i * ROWS, base + i * F::TILE, slots + slot * F::TILE);
+                ptx::mma_commit(ptx::smem_u32(&ctl->sfull[i]));
+            }
+            __syncwarp();
+        };
+        auto release = [&](int slot) {
+            if (leader) ptx::mma_commit(ptx::smem_u32(&ctl->empty[slot]));
+            __syncwarp();
+        };
+        bool ok = wait(ctl->qfull[0], 0) && wait(ctl->full[0], 0);
+        if (ok) {
+            ptx::tc_fence_after();
+            score(0, 0);
+            if (two) {
+                ok = wait(ctl->qfull[1], 0);
+                if (ok) score(1, 0);
+            }
+            if (ok) release(0);
+        }
+        for (int j = 0; j < tiles && ok; ++j) {
+            const int n = 2 * j + 1, vs = n % F::SLOTS, ks = (n + 1) % F::SLOTS;
+            ok = wait(ctl->full[vs], (n / F::SLOTS) & 1);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            const int left = pair.length - j * ROWS;                // keys from this tile on
+            const int steps = left >= ROWS ? ROWS / 16 : (left + 15) / 16;
+            if (left < ROWS && left % 16 != 0) clear_rows<DP>(ring + vs * F::TILE, left, lane);
+            for (int i = 0; i < 2 && ok; ++i) {
+                const int mine = i == 0 ? q0 + 1 : tiles;           // key tiles of this tile of queries
+                if (j >= mine || (i == 1 && !two)) continue;
+                ok = wait(ctl->pfull[i], j & 1);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                if (leader) {
+                    mma_sum<DP>(tmem + 256 + i * DP, tmem + i * ROWS, 32, slots + vs * F::TILE, steps, j > 0);
+                    if (j + 1 == mine) ptx::mma_commit(ptx::smem_u32(&ctl->ofull[i]));
+                }
+                __syncwarp();
+                if (j + 1 < mine) {
+                    // its S over the P that the product in front of it in the queue has read by then
+                    ok = wait(ctl->full[ks], ((n + 1) / F::SLOTS) & 1);
+                    if (ok) score(i, ks);
+                }
+            }
+            if (ok) {
+                release(vs);
+                if (j + 1 < tiles) release(ks);
+            }
+        }
+        if (leader) ptx::mma_commit(ptx::smem_u32(&ctl->drain));
+        __syncwarp();
+        wait_drain(ptx::smem_u32(&ctl->drain), 0);
+    } else {
+        const int i = warp >> 2, quad = warp & 3, r = quad * 32 + lane;     // tile, lane quadrant, row
+        const int mine = i == 0 ? q0 + 1 : two ? tiles : 0;
+        const int row = (q0 + i) * ROWS + r;                        // in the sequence
+        const uint32_t st = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * ROWS;
+        const uint32_t ot = tmem + (static_cast<uint32_t>(quad * 32) << 16) + 256 + i * DP;
+        const float scale = p.scale * kLog2e;
+        float ref = 0.0f, sum = 0.0f;                               // in units of S
+        bool ok = mine > 0;
+        for (int j = 0; j < mine; ++j) {
+            ok = wait(ctl->sfull[i], j & 1);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            uint32_t s[2][64];
+            ptx::tmem_ld64(st, s[0]);
+            ptx::tmem_ld64(st + 64, s[1]);
+            if (j + 1 == mine) {                                    // the diagonal
+#pragma unroll
+                for (int c = 0; c < ROWS; ++c)
+                    if (c > r) s[c / 64][c % 64] = 0xFF800000u;
+            }
+            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int c = 0; c < ROWS; ++c) top[c % 4] = fmaxf(top[c % 4], __uint_as_float(s[c / 64][c % 64]));
+            float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+            if (high == -INFINITY) high = 0.0f;                     // nothing finite
+            if (j == 0) {
+                ref = high;
+            } else if (__any_sync(0xffffffffu, (high - ref) * scale > 8.0f)) {
+                // S of this tile is there, so the products in front of it have added to O
+                const float to = fmaxf(high, ref), f = ex2((ref - to) * scale);
+                ref = to;
+                sum *= f;
+#pragma unroll
+                for (int c = 0; c < DP; c += 32) {
+                    uint32_t o[32];
+                    ptx::tmem_ld32(ot + c, o);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                    ptx::tmem_st32(ot + c, o);
+                }
+            }
+            const float shift = -ref * scale;
+            float part[4] = {};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t w[32];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) {
+                    const float a = ex2(fmaf(__uint_as_float(s[h][2 * c]), scale, shift));
+                    const float b = ex2(fmaf(__uint_as_float(s[h][2 * c + 1]), scale, shift));
+                    part[2 * (c & 1)] += a;
+                    part[2 * (c & 1) + 1] += b;
+                    w[c] = pack2(a, b);
+                }
+                ptx::tmem_st32(st + 32 * h, w);
+            }
+            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull[i]));
+        }
+        if (ok) ok = wait(ctl->ofull[i], 0);
+        if (ok) {
+            ptx::tc_fence_after();
+            const float inv = 1.0f / sum;
+            const bool real = row < pair.length;
+            const long long token = pair.begin + row;
+            if (real) p.lse[static_cast<long long>(head) * p.tokens + token] = fmaf(ref, p.scale, logf(sum));
+            bf16* out = p.out + (token * p.heads + head) * p.dim;
+            bf16* rest = p.rest == nullptr ? nullptr : p.rest + (token * p.heads + head) * p.dim;
+#pragma unroll
+            for (int c = 0; c < DP; c += 32) {
+                uint32_t o[32];
+                ptx::tmem_ld32(ot + c, o);
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    if (!real || c + e >= p.dim) continue;
+                    uint32_t w[4], l[4];
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        const float a = __uint_as_float(o[e + 2 * x]) * inv, b = __uint_as_float(o[e + 2 * x + 1]) * inv;
+                        w[x] = pack2(a, b);
+                        l[x] = pack2(a - __uint_as_float(w[x] << 16), b - __uint_as_float(w[x] & 0xFFFF0000u));
+                    }
+                    *reinterpret_cast<uint4*>(out + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                    if (rest != nullptr) *reinterpret_cast<uint4*>(rest + c + e) = make_uint4(l[0], l[1], l[2], l[3]);
+                }
+            }
+        }
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) {      // a wait that ran out: no copy stays in flight
+        wait_drain(ptx::smem_u32(&ctl->qfull[0]), 0);
+        if (two && ctl->filled > 0) wait_drain(ptx::smem_u32(&ctl->qfull[1]), 0);
+        for (int n = max(0, ctl->filled - F::SLOTS); n < ctl->filled; ++n)
+            wait_drain(ptx::smem_u32(&ctl->full[n % F::SLOTS]), (n / F::SLOTS) & 1);
+    }
+    if (warp == 9) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+    __syncthreads();
+}
+
+// ---------------------------------------------------------------------------
+// Gradients.  Two kernels, so that every sum has one owner and one order (five products a
+// pair of tiles become seven; adding dQ up from one kernel would need atomics, whose order
+// changes the result).  KEYS: a CTA takes 128 keys of a head of k and v and goes through
+// the queries that see them, of every head that shares it; with S^T = K Q^T, P^T and dS^T
+// stay in tensor memory and dV += P^T dO, dK += dS^T Q take them from there.  Otherwise it
+// takes 128 queries of a head and goes through their keys: dQ += dS K.
+//
+// Eight warps turn S into P and dP = dO V^T into dS (64 columns a thread, one row), one
+// issues products, one copies.  The tile that is used twice in a step (first in S, last in a
+// sum) has three slots, the other two.
+// ---------------------------------------------------------------------------
+template <int DP> struct Backward {
+    static constexpr int TILE = DP / 64 * PANEL;
+    static constexpr int SA = 3, SB = 2;
+    static constexpr int STATS = 2 * 2 * ROWS * 4;                 // lse and delta of two steps
+    static constexpr int CTL = 256;
+    static constexpr int SMEM = (2 + SA + SB) * TILE + STATS + CTL;
+    static constexpr int THREADS = 10 * 32;
+    static_assert(SMEM <= 227 * 1024, "shared memory");
+};
+
+struct BackwardParams {
+    CUtensorMap fixed_a, fixed_b, a, b;          // KEYS: k, v, q, dO; otherwise q, dO, k, v
+    const float* lse;
+    const float* delta;
+    bf16* out_a;                                 // KEYS: dk; otherwise dq
+    bf16* out_b;                                 // KEYS: dv
+    const AttentionTile* tiles;
+    int tokens, heads, kv_heads, group, dim;
+    float scale;
+    int* status;
+    long long wait_limit;
+};
+
+struct BackwardCtl {
+    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull, dpfull, dsfull, stats[2], done, drain;
+    uint32_t tmem;
+    int abort;
+    int filled[2];
+};
+
+template <int DP, bool KEYS>
+__global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(const __grid_constant__ BackwardParams p) {
+    using F = Backward<DP>;
+    static_assert(sizeof(BackwardCtl) <= F::CTL, "the barriers fit");
+    extern __shared__ __align__(1024) uint8_t smem[];              // there is no room to align it here
+    uint8_t* const ring_a = smem + 2 * F::TILE;
+    uint8_t* const ring_b = ring_a + F::SA * F::TILE;
+    float* const stats = reinterpret_cast<float*>(ring_b + F::SB * F::TILE);
+    BackwardCtl* ctl = reinterpret_cast<BackwardCtl*>(ring_b + F::SB * F::TILE + F::STATS);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    volatile int* abort_flag = &ctl->abort;
+    if ((ptx::smem_u32(smem) & 1023u) != 0) {                       // the same in every CTA
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, MOARA_ERR_ALIGN);
+        return;
+    }
+    if (threadIdx.x == 0) {
+        for (uint64_t* b : {&ctl->fixed, &ctl->sfull, &ctl->dpfull, &ctl->done, &ctl->drain}) ptx::mbar_init(ptx::smem_u32(b), 1);
+        ptx::mbar_init(ptx::smem_u32(&ctl->pfull), 8);
+        ptx::mbar_init(ptx::smem_u32(&ctl->dsfull), 8);
+        ptx::mbar_init(ptx::smem_u32(&ctl->stats[0]), 8);
+        ptx::mbar_init(ptx::smem_u32(&ctl->stats[1]), 8);
+        for (int i = 0; i < F::SA; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctl->afull[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctl->aempty[i]), 1);
+        }
+        for (int i = 0; i < F::SB; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctl->bfull[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctl->bempty[i]), 1);
+        }
+        ctl->abort = 0;
+        ctl->filled[0] = ctl->filled[1] = 0;
+        ptx::fence_barrier_init();
+    }
+    if (warp == 9) {
+        ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
+        ptx::tmem_relinquish();
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    ptx::tc_fence_after();
+    const uint32_t tmem = ctl->tmem;
+    pdl_begin();
+    const int owners = KEYS ? p.kv_heads : p.heads;
+    const AttentionTile tile = p.tiles[blockIdx.x / owners];
+    const int owner = blockIdx.x % owners, kv = KEYS ? owner : owner / p.group;
+    const int last = (tile.length - 1) / ROWS;                     // tile of the sequence
+    const int per = KEYS ? last - tile.tile + 1 : tile.tile + 1;   // tiles that are gone through, per head
+    const int steps = KEYS ? per * p.group : per;
+    const int tail = tile.length - last * ROWS;                    // rows of the last tile
+    // of step j: head of the streamed operands, their tile
+    auto head_of = [&](int j) { return KEYS ? kv * p.group + j / per : kv; };
+    auto tile_of = [&](int j) { return KEYS ? tile.tile + j % per : j; };
+    auto wait = [&](uint64_t& bar, uint32_t parity) {
+        return ptx::mbar_wait_warp(ptx::smem_u32(&bar), parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
+    };
+    constexpr uint32_t S = 0, DPC = 128;                           // columns of tensor memory
+    constexpr uint32_t SUM_B = 256, SUM_A = 384;                   // KEYS: dV, dK; otherwise dQ is SUM_A
+    auto dp_at = [&](int j) { return KEYS ? DPC : DPC + static_cast<uint32_t>(j & 1) * 128; };
+
+    if (warp == 8) {
+        if (lane == 0) {
+            auto copy = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
+                for (int c = 0; c < DP / 64; ++c)
+                    ptx::tma_load_3d(ptx::smem_u32(to) + c * PANEL, map, ptx::smem_u32(&bar), c * 64, h, row);
+            };
+            ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->fixed), 2 * F::TILE);
+            copy(smem, &p.fixed_a, ctl->fixed, owner, tile.begin + tile.tile * ROWS);
+            copy(smem + F::TILE, &p.fixed_b, ctl->fixed, owner, tile.begin + tile.tile * ROWS);
+            int na = 0, nb = 0;
+            auto room = [&](uint64_t& bar, int n, int slots) {
+                return n < slots || ptx::mbar_wait(ptx::smem_u32(&bar), (n / slots - 1) & 1, abort_flag, p.status,
+                                                   MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
+            };
+            for (int j = 0; j < steps; ++j) {
+                const int row = tile.begin + tile_of(j) * ROWS, h = head_of(j), sa = j % F::SA, sb = j % F::SB;
+                if (!room(ctl->aempty[sa], j, F::SA)) break;
+                ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->afull[sa]), F::TILE);
+                copy(ring_a + sa * F::TILE, &p.a, ctl->afull[sa], h, row);
+                ++na;
+                if (!room(ctl->bempty[sb], j, F::SB)) break;
+                ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->bfull[sb]), F::TILE);
+                copy(ring_b + sb * F::TILE, &p.b, ctl->bfull[sb], h, row);
+                ++nb;
+            }
+            ctl->filled[0] = na;
+            ctl->filled[1] = nb;
+        }
+    } else if (warp == 9) {
+        const bool leader = ptx::elect_one();
+        const uint32_t fixed = ptx::smem_u32(smem), ra = ptx::smem_u32(ring_a), rb = ptx::smem_u32(ring_b);
+        auto commit = [&](uint64_t& bar) {
+            if (leader) ptx::mma_commit(ptx::smem_u32(&bar));
+            __syncwarp();
+        };
+        // rows of a tile that a sum runs over
+        auto rows_of = [&](int j) { return tile_of(j) == last ? tail : ROWS; };
+        auto sum_steps = [&](int j) { return (rows_of(j) + 15) / 16; };
+        auto score = [&](int j) {
+            const int sa = j % F::SA;
+            if (!wait(ctl->afull[sa], (j / F::SA) & 1)) return false;
+            if (rows_of(j) % 16 != 0) clear_rows<DP>(ring_a + sa * F::TILE, rows_of(j), lane);
+            ptx::tc_fence_after();
+            if (leader) mma_rows<DP>(tmem + S, fixed, ra + sa * F::TILE);
+            commit(ctl->sfull);
+            return true;
+        };
+        auto slope = [&](int j) {
+            const int sb = j % F::SB;
+            if (!wait(ctl->bfull[sb], (j / F::SB) & 1)) return false;
+            if (KEYS && rows_of(j) % 16 != 0) clear_rows<DP>(ring_b + sb * F::TILE, rows_of(j), lane);
+            ptx::tc_fence_after();
+            if (leader) mma_rows<DP>(tmem + dp_at(j), fixed + F::TILE, rb + sb * F::TILE);
+            commit(ctl->dpfull);
+            if (!KEYS) commit(ctl->bempty[sb]);
+            return true;
+        };
+        bool ok = wait(ctl->fixed, 0) && score(0) && slope(0);
+        for (int j = 0; j < steps && ok; ++j) {
+            if (KEYS) {
+                ok = wait(ctl->pfull, j & 1);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                if (leader) mma_sum<DP>(tmem + SUM_B, tmem + S, 64, rb + j % F::SB * F::TILE, sum_steps(j), j > 0);
+                commit(ctl->bempty[j % F::SB]);
+                // the next S over the P that the product in front of it has read by then
+                if (j + 1 < steps && !score(j + 1)) break;
+            } else if (j + 1 < steps) {
+                ok = wait(ctl->pfull, j & 1);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                if (!score(j + 1) || !slope(j + 1)) break;
+            }
+            ok = wait(ctl->dsfull, j & 1);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            if (leader) mma_sum<DP>(tmem + SUM_A, tmem + dp_at(j), 64, ra + j % F::SA * F::TILE, sum_steps(j), j > 0);
+            commit(ctl->aempty[j % F::SA]);
+            if (KEYS && j + 1 < steps && !slope(j + 1)) break;
+            if (j + 1 == steps) commit(ctl->done);
+        }
+        commit(ctl->drain);
+        wait_drain(ptx::smem_u32(&ctl->drain), 0);
+    } else {
+        const int half = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
+        const int row = tile.tile * ROWS + r;                       // in the sequence
+        const bool real = row < tile.length;
+        const long long token = tile.begin + row;
+        const float scale = p.scale * kLog2e;
+        float lse = 0.0f, delta = 0.0f;
+        if (!KEYS && real) {
+            lse = p.lse[static_cast<long long>(owner) * p.tokens + token] * kLog2e;
+            delta = p.delta[static_cast<long long>(owner) * p.tokens + token];
+        }
+        // KEYS: lse (first half of the threads) or delta of a query of step j
+        auto stat = [&](int j) {
+            const int q = tile_of(j) * ROWS + r;
+            if (q >= tile.length) return 0.0f;
+            const long long at = static_cast<long long>(head_of(j)) * p.tokens + tile.begin + q;
+            return half == 0 ? p.lse[at] * kLog2e : p.delta[at];
+        };
+        float next = KEYS ? stat(0) : 0.0f;
+        bool ok = true;
+        for (int j = 0; j < steps; ++j) {
+            const float* sl = stats + (j & 1) * 2 * ROWS + half * 64;
+            const float* sd = sl + ROWS;
+            if (KEYS) {
+                stats[(j & 1) * 2 * ROWS + half * ROWS + r] = next;
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->stats[j & 1]));
+                if (j + 1 < steps) next = stat(j + 1);
+                // all eight warps' (a barrier whose wait is bounded); they have left step j - 1 by then
+                ok = wait(ctl->stats[j & 1], (j >> 1) & 1);
+                if (!ok) break;
+            }
+            // which columns of this thread count: from `from` on (KEYS) up to `to`
+            int from = 0, to = 64;
+            if (KEYS) {
+                if (tile_of(j) == tile.tile) from = r - half * 64;
+                if (tile_of(j) == last) to = tail - half * 64;
+            } else if (j == tile.tile) {
+                to = r + 1 - half * 64;
+            }
+            const bool all = from <= 0 && to >= 64;
+            ok = wait(ctl->sfull, j & 1);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            uint32_t s[64];
+            ptx::tmem_ld64(lanes + S + half * 64, s);
+            if (!KEYS) {
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull));
+            }
+            float x[64];
+#pragma unroll
+            for (int c = 0; c < 64; ++c) x[c] = ex2(fmaf(__uint_as_float(s[c]), scale, KEYS ? -sl[c] : -lse));
+            if (__any_sync(0xffffffffu, !all)) {
+#pragma unroll
+                for (int c = 0; c < 64; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
+            }
+            if (KEYS) {
+                uint32_t w[32];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
+                ptx::tmem_st32(lanes + S + half * 64, w);
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull));
+            }
+            ok = wait(ctl->dpfull, j & 1);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            ptx::tmem_ld64(lanes + dp_at(j) + half * 64, s);
+#pragma unroll
+            for (int c = 0; c < 64; ++c) x[c] *= __uint_as_float(s[c]) - (KEYS ? sd[c] : delta);
+            if (__any_sync(0xffffffffu, !all)) {                    // what is not counted may be infinite or NaN
+#pragma unroll
+                for (int c = 0; c < 64; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
+            }
+            uint32_t w[32];
+#pragma unroll
+            for (int c = 0; c < 32; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
+            ptx::tmem_st32(lanes + dp_at(j) + half * 64, w);
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->dsfull));
+        }
+        if (ok) ok = wait(ctl->done, 0);
+        if (ok) {
+            ptx::tc_fence_after();
+            // KEYS: the first half of the threads has dV, the second dK; otherwise half of dQ's columns each
+            const long long at = (token * owners + owner) * p.dim;
+            bf16* out = (KEYS && half == 0 ? p.out_b : p.out_a) + at;
+            const uint32_t src = lanes + (KEYS && half == 0 ? SUM_B : SUM_A);
+            const float factor = KEYS && half == 0 ? 1.0f : p.scale;
+            constexpr int COLS = KEYS ? DP : DP / 2;
+            const int c0 = KEYS ? 0 : half * COLS;
+#pragma unroll
+            for (int c = 0; c < COLS; c += 32) {
+                uint32_t o[32];
+                ptx::tmem_ld32(src + c0 + c, o);
+#pragma unroll
+                for (int e = 0; e < 32; e += 8) {
+                    if (!real || c0 + c + e >= p.dim) continue;
+                    uint32_t w[4];
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        w[y] = pack2(__uint_as_float(o[e + 2 * y]) * factor, __uint_as_float(o[e + 2 * y + 1]) * factor);
+                    *reinterpret_cast<uint4*>(out + c0 + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                }
+            }
+        }
+    }
+    ptx::tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && *abort_flag) {      // a wait that ran out: no copy stays in flight
+        wait_drain(ptx::smem_u32(&ctl->fixed), 0);
+        for (int n = max(0, ctl->filled[0] - F::SA); n < ctl->filled[0]; ++n)
+            wait_drain(ptx::smem_u32(&ctl->afull[n % F::SA]), (n / F::SA) & 1);
+        for (int n = max(0, ctl->filled[1] - F::SB); n < ctl->filled[1]; ++n)
+            wait_drain(ptx::smem_u32(&ctl->bfull[n % F::SB]), (n / F::SB) & 1);
+    }
+    if (warp == 9) {
+        ptx::tc_fence_after();
+        ptx::tmem_dealloc(tmem, 512);
+    }
+    __syncthreads();
+}
+
+struct DeltaParams {
+    const bf16* dout;
+    const bf16* out;
+    const bf16* rest;
+    float* delta;
+    long long row, head;                         // pitches of dO
+    int tokens, heads, dim;
+};
+
+// delta = rowsum(dO O), with what the rounding of O dropped where it was kept: an error of
+// delta is the same for all keys of a row, and where keys share a direction dQ's error would
+// grow with their number (1024 keys: 0.45% of dQ's norm with O alone, 0.25% so).  16 lanes a
+// row, heads of a token beside one another.
+__global__ void __launch_bounds__(256) k_attention_delta(const DeltaParams p) {
+    pdl_begin();
+    const long long n = static_cast<long long>(blockIdx.x) * 16 + (threadIdx.x >> 4);
+    const int c = (threadIdx.x & 15) * 8;
+    const long long token = n / p.heads;
+    const int head = static_cast<int>(n % p.heads);
+    float sum = 0.0f;
+    if (token < p.tokens && c < p.dim) {
+        const long long at = n * p.dim + c;
+        const uint4 a = *reinterpret_cast<const uint4*>(p.dout + token * p.row + head * p.head + c);
+        const uint4 b = *reinterpret_cast<const uint4*>(p.out + at);
+        const uint4 l = p.rest == nullptr ? make_uint4(0, 0, 0, 0) : *reinterpret_cast<const uint4*>(p.rest + at);
+        const uint32_t x[4] = {a.x, a.y, a.z, a.w}, y[4] = {b.x, b.y, b.z, b.w}, z[4] = {l.x, l.y, l.z, l.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sum = fmaf(__uint_as_float(x[e] << 16), __uint_as_float(y[e] << 16) + __uint_as_float(z[e] << 16), sum);
+            sum = fmaf(__uint_as_float(x[e] & 0xFFFF0000u),
+                       __uint_as_float(y[e] & 0xFFFF0000u) + __uint_as_float(z[e] & 0xFFFF0000u), sum);
+        }
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (token < p.tokens && (threadIdx.x & 15) == 0) p.delta[static_cast<long long>(head) * p.tokens + token] = sum;
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encoder() {
+    static const EncodeTiledFn fn = [] {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult q{};
+        if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            f = nullptr;
+        return reinterpret_cast<EncodeTiledFn>(f);
+    }();
+    return fn;
+}
+
+// 128 tokens of a head, 64 entries at a time; entries behind the head's last and tokens
+// behind the tensor's last are zeros.
+bool encode(CUtensorMap* map, const void* x, int tokens, int heads, int dim, int64_t row, int64_t head) {
+    EncodeTiledFn fn = encoder();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(tokens)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(head) * 2, static_cast<cuuint64_t>(row) * 2};
+    const cuuint32_t box[3] = {64, 1, ROWS}, estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(x), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Lets a kernel take `bytes` of shared memory: once per device.
+template <int ID, class... P> cudaError_t allow_shared(void (*fn)(P...), int bytes) {
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess || (device < 64 && (done.load() >> device & 1))) return e;
+    e = cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && device < 64) done.fetch_or(1ull << device);
+    return e;
+}
+
+template <int DP> cudaError_t forward_as(const ForwardParams& p, int ctas, cudaStream_t s) {
+    const cudaError_t e = allow_shared<DP>(k_attention<DP>, Forward<DP>::SMEM);
+    if (e != cudaSuccess) return e;
+    return launch(k_attention<DP>, dim3(ctas), dim3(Forward<DP>::THREADS), Forward<DP>::SMEM, s, 1, p);
+}
+
+template <int DP, bool KEYS> cudaError_t backward_as(const BackwardParams& p, int ctas, cudaStream_t s) {
+    const cudaError_t e = allow_shared<DP + KEYS>(k_attention_grad<DP, KEYS>, Backward<DP>::SMEM);
+    if (e != cudaSuccess) return e;
+    return launch(k_attention_grad<DP, KEYS>, dim3(ctas), dim3(Backward<DP>::THREADS), Backward<DP>::SMEM, s, 1, p);
+}
+
+}  // namespace
+
+cudaError_t launch_attention(const Attention& a, cudaStream_t s, int64_t* launches) {
+    ForwardParams p{};
+    if (!encode(&p.q, a.q, a.tokens, a.heads, a.dim, a.q_row, a.q_head) ||
+        !encode(&p.k, a.k, a.tokens, a.kv_heads, a.dim, a.k_row, a.k_head) ||
+        !encode(&p.v, a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head))
+        return cudaErrorInvalidValue;
+    p.out = static_cast<bf16*>(a.out);
+    p.rest = static_cast<bf16*>(a.rest);
+    p.lse = a.lse;
+    p.pairs = a.pairs;
+    p.tokens = a.tokens;
+    p.heads = a.heads;
+    p.group = a.heads / a.kv_heads;
+    p.dim = a.dim;
+    p.scale = a.scale;
+    p.status = a.status;
+    p.wait_limit = a.wait_limit;
+    ++*launches;
+    return a.dim <= 64 ? forward_as<64>(p, a.n_pairs * a.heads, s) : forward_as<128>(p, a.n_pairs * a.heads, s);
+}
+
+cudaError_t launch_attention_backward(const AttentionGrad& a, cudaStream_t s, int64_t* launches) {
+    CUtensorMap q, k, v, dout;
+    if (!encode(&q, a.q, a.tokens, a.heads, a.dim, a.q_row, a.q_head) ||
+        !encode(&k, a.k, a.tokens, a.kv_heads, a.dim, a.k_row, a.k_head) ||
+        !encode(&v, a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head) ||
+        !encode(&dout, a.dout, a.tokens, a.heads, a.dim, a.do_row, a.do_head))
+        return cudaErrorInvalidValue;
+    const DeltaParams d{static_cast<const bf16*>(a.dout), static_cast<const bf16*>(a.out), static_cast<const bf16*>(a.rest),
+                        a.delta, a.do_row, a.do_head, a.tokens, a.heads, a.dim};
+    const long long rows = static_cast<long long>(a.tokens) * a.heads;
+    ++*launches;
+    cudaError_t e = launch(k_attention_delta, dim3(static_cast<unsigned int>((rows - 1) / 16 + 1)), dim3(256), 0, s, 1, d);
+    if (e != cudaSuccess) return e;
+    BackwardParams p{};
+    p.lse = a.lse;
+    p.delta = a.delta;
+    p.tokens = a.tokens;
+    p.heads = a.heads;
+    p.kv_heads = a.kv_heads;
+    p.group = a.heads / a.kv_heads;
+    p.dim = a.dim;
+    p.scale = a.scale;
+    p.status = a.status;
+    p.wait_limit = a.wait_limit;
+    const bool narrow = a.dim <= 64;
+    p.fixed_a = k;
+    p.fixed_b = v;
+    p.a = q;
+    p.b = dout;
+    p.out_a = static_cast<bf16*>(a.dk);
+    p.out_b = static_cast<bf16*>(a.dv);
+    p.tiles = a.k_tiles;
+    ++*launches;
+    e = narrow ? backward_as<64, true>(p, a.n_tiles * a.kv_heads, s) : backward_as<128, true>(p, a.n_tiles * a.kv_heads, s);
+    if (e != cudaSuccess) return e;
+    p.fixed_a = q;
+    p.fixed_b = dout;
+    p.a = k;
+    p.b = v;
+    p.out_a = static_cast<bf16*>(a.dq);
+    p.out_b = nullptr;
+    p.tiles = a.q_tiles;
+    ++*launches;
+    return narrow ? backward_as<64, false>(p, a.n_tiles * a.heads, s) : backward_as<128, false>(p, a.n_tiles * a.heads, s);
+}
+
+}  // namespace moara

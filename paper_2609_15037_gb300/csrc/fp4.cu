@@ -3,8 +3,11 @@
 // and 17/32 of a byte out per orientation.
 #include <cuda_bf16.h>
 
+#include <type_traits>
+
 #include "fp4.cuh"
 #include "launch.cuh"
+#include "layers.h"
 #include "ops.h"
 
 namespace moara {
@@ -21,6 +24,8 @@ struct QuantParams {
     uint32_t* sf;          // words of four scales
     uint8_t* qt;
     uint32_t* sft;
+    const float* rstd;     // NORM: of the rows
+    const float* gain;     // of the columns
 };
 
 // One CTA takes a 128 x 128 tile, which is one 512-byte scale tile of either
@@ -56,8 +61,10 @@ template <int V, int L, int STEP> __device__ __forceinline__ void scatter_max(ui
     }
 }
 
-template <class T, bool ROWS, bool COLS>
-__global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 ? 2 : ROWS && COLS ? 3 : 4) k_fp4_quantize(const QuantParams p) {
+// With NORM the entries are those of a norm's output, x rstd gain in fp32, which is never
+// stored: the norm's kernel leaves h, which is still in L2, and rstd.
+template <class T, bool ROWS, bool COLS, bool NORM>
+__global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 || NORM ? 2 : ROWS && COLS ? 3 : 4) k_fp4_quantize(const QuantParams p) {
     constexpr int N = Quant<T>::N, BLOCK = Quant<T>::BLOCK, THREADS = Quant<T>::THREADS;
     __shared__ __align__(16) uint8_t sfr[512];
     __shared__ __align__(16) uint8_t sfc[512];
@@ -71,7 +78,7 @@ __global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 ? 2 : ROWS &
     const int lr = wr * 32 + (lane >> 3) * 8, lc = sub * N;          // the lane's entries inside the tile
     const int row0 = tr * 128 + lr, col0 = tc * 128 + lc;
     const T* X = static_cast<const T*>(p.X) + row0 * p.ld + col0;
-    Row<T, N> x[8];
+    Row<T, N> from[8];
     const bool whole = col0 + N <= p.cols && row0 + 8 <= p.rows;
     // rows on other boundaries: by lines of 8 bytes, while they lie inside the matrix.  Eight
     // rows further a row begins on the same byte of its line.
@@ -80,14 +87,31 @@ __global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 ? 2 : ROWS &
     const uintptr_t end = reinterpret_cast<uintptr_t>(static_cast<const T*>(p.X) + (p.rows - 1) * p.ld + p.cols);
     if (whole && p.vec) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i].load(X + i * p.ld);
+        for (int i = 0; i < 8; ++i) from[i].load(X + i * p.ld);
     } else if (whole && (reinterpret_cast<uintptr_t>(X) & ~LINE) >= begin &&
                (reinterpret_cast<uintptr_t>(X + 7 * p.ld) & ~LINE) + 24 <= end) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i].load_any(X + i * p.ld, static_cast<int>((begin + i * p.ld * sizeof(T)) & LINE));
+        for (int i = 0; i < 8; ++i) from[i].load_any(X + i * p.ld, static_cast<int>((begin + i * p.ld * sizeof(T)) & LINE));
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i].load_some(X + i * p.ld, row0 + i < p.rows ? p.cols - col0 : 0);
+        for (int i = 0; i < 8; ++i) from[i].load_some(X + i * p.ld, row0 + i < p.rows ? p.cols - col0 : 0);
+    }
+    using Value = typename std::conditional<NORM, Row<float, N>, Row<T, N>>::type;
+    Value x[8];
+    if constexpr (NORM) {
+        float g[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) g[e] = col0 + e < p.cols ? p.gain[col0 + e] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float s = row0 + i < p.rows ? p.rstd[row0 + i] : 0.0f;
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                x[i].w[e] = row0 + i < p.rows && col0 + e < p.cols ? __float_as_uint(from[i].get(e) * s * g[e]) : 0u;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = from[i];
     }
     if (ROWS) {
         const int block = (tc * 128 + lc) >> 5;
@@ -128,7 +152,7 @@ __global__ void __launch_bounds__(Quant<T>::THREADS, sizeof(T) == 4 ? 2 : ROWS &
     if (COLS) {
         const bool rows_real = tr * 4 + wr < p.kbt;
         uint32_t tops[N];
-        Row<T, N>::tops(x, tops);
+        Value::tops(x, tops);
         scatter_max<N, 4, 8>(tops, lane);
         constexpr int OWN = N / 4;                                   // columns whose scale this lane works out
         float factor[OWN];
@@ -301,19 +325,16 @@ template <class T, bool ANY> __global__ void __launch_bounds__(256) k_fp4_values
     }
 }
 
-template <class T>
+template <class T, bool NORM>
 cudaError_t quantize_as(const QuantParams& p, cudaStream_t s) {
     const unsigned int grid = static_cast<unsigned int>(p.tiles_r) * p.tiles_c;
-    const auto fn = p.qt == nullptr  ? k_fp4_quantize<T, true, false>
-                    : p.q == nullptr ? k_fp4_quantize<T, false, true>
-                                     : k_fp4_quantize<T, true, true>;
+    const auto fn = p.qt == nullptr  ? k_fp4_quantize<T, true, false, NORM>
+                    : p.q == nullptr ? k_fp4_quantize<T, false, true, NORM>
+                                     : k_fp4_quantize<T, true, true, NORM>;
     return launch(fn, dim3(grid), dim3(Quant<T>::THREADS), 0, s, 1, p);
 }
 
-}  // namespace
-
-cudaError_t launch_fp4_quantize(const void* X, int dtype, int rows, int cols, int64_t ld, void* q, void* sf, void* qt,
-                                void* sft, cudaStream_t s, int64_t* launches) {
+QuantParams quant_params(const void* X, int dtype, int rows, int cols, int64_t ld, void* q, void* sf, void* qt, void* sft) {
     QuantParams p{};
     p.X = X;
     p.ld = ld;
@@ -328,8 +349,26 @@ cudaError_t launch_fp4_quantize(const void* X, int dtype, int rows, int cols, in
     p.sf = static_cast<uint32_t*>(sf);
     p.qt = static_cast<uint8_t*>(qt);
     p.sft = static_cast<uint32_t*>(sft);
+    return p;
+}
+
+}  // namespace
+
+cudaError_t launch_fp4_quantize(const void* X, int dtype, int rows, int cols, int64_t ld, void* q, void* sf, void* qt,
+                                void* sft, cudaStream_t s, int64_t* launches) {
+    const QuantParams p = quant_params(X, dtype, rows, cols, ld, q, sf, qt, sft);
     ++*launches;
-    return dtype == MOARA_DTYPE_BF16 ? quantize_as<__nv_bfloat16>(p, s) : quantize_as<float>(p, s);
+    return dtype == MOARA_DTYPE_BF16 ? quantize_as<__nv_bfloat16, false>(p, s) : quantize_as<float, false>(p, s);
+}
+
+cudaError_t launch_norm_quantize(const void* h, int dtype, int rows, int cols, int64_t ld, const float* rstd,
+                                 const float* gain, void* q, void* sf, void* qt, void* sft, cudaStream_t s,
+                                 int64_t* launches) {
+    QuantParams p = quant_params(h, dtype, rows, cols, ld, q, sf, qt, sft);
+    p.rstd = rstd;
+    p.gain = gain;
+    ++*launches;
+    return dtype == MOARA_DTYPE_BF16 ? quantize_as<__nv_bfloat16, true>(p, s) : quantize_as<float, true>(p, s);
 }
 
 cudaError_t launch_fp4_dequantize(const void* q, const void* sf, int rows, int cols, void* out, int dtype, int64_t ldo,

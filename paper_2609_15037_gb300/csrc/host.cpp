@@ -5,6 +5,7 @@
 #include <Python.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/zeros.h>
 #include <c10/core/StorageImpl.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -444,6 +445,332 @@ PyObject* bytes(PyObject*, PyObject* const* a, Py_ssize_t count) {
     }
 }
 
+// ------------------------------------------------------- operators of a decoder's layers
+at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type, long device, bool zero = false) {
+    const auto o = at::TensorOptions().dtype(type).device(at::kCUDA, static_cast<at::DeviceIndex>(device));
+    return zero ? at::zeros(shape, o) : at::empty(shape, o);
+}
+
+// The entries of a contiguous tensor of this type and size (null for None where it may be),
+// or an error that names `what`.
+const void* entries_of(PyObject* o, const char* what, at::ScalarType type, int64_t n, long device, bool optional = false) {
+    if (optional && o == Py_None) return nullptr;
+    if (THPVariable_Check(o)) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (t.layout() == at::kStrided && t.is_cuda() && t.get_device() == device && t.is_contiguous() && t.scalar_type() == type &&
+            t.numel() == n)
+            return t.const_data_ptr();
+    }
+    PyErr_Format(PyExc_ValueError, "%s: a contiguous %s tensor of %lld entries on cuda:%ld is needed", what,
+                 type == at::kLong ? "int64" : type == at::kFloat ? "float32" : "bfloat16", static_cast<long long>(n), device);
+    return nullptr;
+}
+
+// Errors of a matrix argument by its name.
+bool matrix_arg(PyObject* o, const char* what, long device, Matrix& m) {
+    const char* wrong = matrix_of(o, device, m);
+    if (wrong != nullptr && !PyErr_Occurred()) PyErr_Format(PyExc_ValueError, "%s: %s", what, wrong);
+    return !PyErr_Occurred();
+}
+
+bool like_arg(PyObject* o, const char* what, long device, const Matrix& like, Matrix& m) {
+    if (!matrix_arg(o, what, device, m)) return false;
+    if (m.rows != like.rows || m.cols != like.cols || (like.dtype >= 0 && m.dtype != like.dtype))
+        PyErr_Format(PyExc_ValueError, "%s: a %s matrix of %d x %d is needed", what,
+                     like.dtype < 0 ? "float32 or bfloat16" : like.dtype ? "bfloat16" : "float32", like.rows, like.cols);
+    return !PyErr_Occurred();
+}
+
+// `o`, or a new matrix for None; of like's type, or of the given one's own for -1.
+PyObject* output_arg(PyObject* o, const char* what, long device, const Matrix& like, int dtype, Matrix& m) {
+    if (o == Py_None) {
+        const at::Tensor t = fresh({like.rows, like.cols}, dtype ? at::kBFloat16 : at::kFloat, device);
+        m = Matrix{t.data_ptr(), dtype, like.rows, like.cols, like.cols > 0 ? like.cols : 1};
+        return THPVariable_Wrap(t);
+    }
+    if (!like_arg(o, what, device, like, m)) return nullptr;
+    return Py_NewRef(o);
+}
+
+// References that are given up unless they are handed on.
+struct Held {
+    PyObject* at[5] = {};
+    ~Held() {
+        for (PyObject* o : at) Py_XDECREF(o);
+    }
+    PyObject* take(int i) {
+        PyObject* o = at[i];
+        at[i] = nullptr;
+        return o;
+    }
+};
+
+struct NormArgs {
+    Matrix x{}, r{}, h{};
+    const float* gain = nullptr;
+    float* rstd = nullptr;
+    float eps = 0;
+    long device = 0;
+    bool res = false;
+};
+
+// x, gain, residual (or None), eps and h (or None) of a norm's call; held.at[0]: h, held.at[1]: rstd
+bool norm_args(PyObject* x, PyObject* gain, PyObject* res, PyObject* eps, PyObject* h, NormArgs& n, Held& held) {
+    n.eps = static_cast<float>(PyFloat_AsDouble(eps));
+    if (PyErr_Occurred() || !matrix_arg(x, "x", n.device, n.x)) return false;
+    n.res = res != Py_None;
+    if (n.res && !like_arg(res, "residual", n.device, n.x, n.r)) return false;
+    n.gain = static_cast<const float*>(entries_of(gain, "gain", at::kFloat, n.x.cols, n.device));
+    if (PyErr_Occurred()) return false;
+    if (n.res) {
+        held.at[0] = output_arg(h, "h", n.device, n.x, n.x.dtype, n.h);
+    } else if (h != Py_None) {
+        PyErr_SetString(PyExc_ValueError, "h: without a residual h is x");
+    } else {
+        held.at[0] = Py_NewRef(x);
+    }
+    if (PyErr_Occurred()) return false;
+    const at::Tensor rstd = fresh({n.x.rows}, at::kFloat, n.device);
+    n.rstd = rstd.data_ptr<float>();
+    held.at[1] = THPVariable_Wrap(rstd);
+    return held.at[1] != nullptr;
+}
+
+// rms_norm(entry, ctx, x, gain, residual, eps, bf16, h, y, device, stream) -> (h, y, rstd) or an error code
+PyObject* rms_norm(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 11)) return nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_rms_norm)>(a[0]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        const int bf16 = PyObject_IsTrue(a[6]);
+        NormArgs n;
+        Held held;
+        n.device = PyLong_AsLong(a[9]);
+        void* stream = PyLong_AsVoidPtr(a[10]);
+        if (PyErr_Occurred() || !norm_args(a[2], a[3], a[4], a[5], a[7], n, held)) return nullptr;
+        Matrix y{}, any = n.x;
+        any.dtype = -1;
+        held.at[2] = output_arg(a[8], "out", n.device, any, bf16, y);
+        if (held.at[2] == nullptr) return nullptr;
+        const int code = fn(ctx, n.x.rows, n.x.cols, n.x.p, n.x.ld, n.r.p, n.r.ld, n.x.dtype, n.gain, n.eps, n.h.p, n.h.ld, y.p,
+                            y.dtype, y.ld, n.rstd, stream);
+        if (code != MOARA_OK) return PyLong_FromLong(code);
+        PyObject *h = held.take(0), *rstd = held.take(1);
+        return Py_BuildValue("(NNN)", h, held.take(2), rstd);
+    } catch (const std::exception& e) {
+        return caught(e);
+    }
+}
+
+// rms_norm_quantize(entry, ctx, x, gain, residual, eps, rows, cols, h, device, stream)
+// -> (h, (buffer, q, sf) or None, the same, rstd, rows, columns), or an error code
+PyObject* rms_norm_quantize(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 11)) return nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_rms_norm_quantize)>(a[0]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        const int rows = PyObject_IsTrue(a[6]), cols = PyObject_IsTrue(a[7]);
+        NormArgs n;
+        Held held;
+        n.device = PyLong_AsLong(a[9]);
+        void* stream = PyLong_AsVoidPtr(a[10]);
+        if (PyErr_Occurred() || !norm_args(a[2], a[3], a[4], a[5], a[8], n, held)) return nullptr;
+        std::optional<Operand> r, c;
+        if (rows) r.emplace(n.x.rows, n.x.cols, n.device);
+        if (cols) c.emplace(n.x.cols, n.x.rows, n.device);
+        const int code = fn(ctx, n.x.rows, n.x.cols, n.x.p, n.x.ld, n.r.p, n.r.ld, n.x.dtype, n.gain, n.eps, n.h.p, n.h.ld,
+                            rows ? r->q : nullptr, rows ? r->sf : nullptr, cols ? c->q : nullptr, cols ? c->sf : nullptr, n.rstd,
+                            stream);
+        if (code != MOARA_OK) return PyLong_FromLong(code);
+        PyObject *h = held.take(0), *rstd = held.take(1);
+        return Py_BuildValue("(NNNNii)", h, rows ? r->tuple() : Py_NewRef(Py_None), cols ? c->tuple() : Py_NewRef(Py_None), rstd,
+                             n.x.rows, n.x.cols);
+    } catch (const std::exception& e) {
+        return caught(e);
+    }
+}
+
+// rms_norm_backward(entry, ctx, dy, h, gain, rstd, dh, dx, device, stream, workspace_entry) -> (dx, dgain) or an error code
+PyObject* rms_norm_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 11)) return nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_rms_norm_backward)>(a[0]);
+        const auto bytes = entry<decltype(&moara_rms_norm_backward_workspace_bytes)>(a[10]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        const long device = PyLong_AsLong(a[8]);
+        void* stream = PyLong_AsVoidPtr(a[9]);
+        Matrix dy{}, h{}, dh{}, dx{};
+        Held held;
+        if (PyErr_Occurred() || !matrix_arg(a[3], "h", device, h)) return nullptr;
+        Matrix any = h;
+        any.dtype = -1;
+        if (!like_arg(a[2], "dy", device, any, dy)) return nullptr;
+        if (a[6] != Py_None && !like_arg(a[6], "dh", device, h, dh)) return nullptr;
+        const auto* gain = static_cast<const float*>(entries_of(a[4], "gain", at::kFloat, h.cols, device));
+        if (PyErr_Occurred()) return nullptr;
+        const auto* rstd = static_cast<const float*>(entries_of(a[5], "rstd", at::kFloat, h.rows, device));
+        if (PyErr_Occurred()) return nullptr;
+        held.at[0] = output_arg(a[7], "out", device, h, h.dtype, dx);
+        if (held.at[0] == nullptr) return nullptr;
+        const at::Tensor dgain = fresh({h.cols}, at::kFloat, device);
+        held.at[1] = THPVariable_Wrap(dgain);
+        size_t size = 0;
+        at::Tensor ws;
+        // a shape that has no workspace is refused by the entry itself
+        if (bytes(h.rows, h.cols, &size) == MOARA_OK && size > 0) ws = fresh({static_cast<int64_t>(size)}, at::kByte, device);
+        const int code = fn(ctx, h.rows, h.cols, dy.p, dy.dtype, dy.ld, h.p, h.dtype, h.ld, gain, rstd, dh.p, dh.ld, dx.p, dx.ld,
+                            dgain.data_ptr<float>(), size > 0 ? ws.data_ptr() : nullptr, size, stream);
+        if (code != MOARA_OK) return PyLong_FromLong(code);
+        PyObject* first = held.take(0);
+        return Py_BuildValue("(NN)", first, held.take(1));
+    } catch (const std::exception& e) {
+        return caught(e);
+    }
+}
+
+// policy_loss(entry, ctx, logits, targets, old, adv, weights, ref, low, high, kl, grad, out, device, stream,
+// workspace_entry) -> (sums, logp, gradient or None) or an error code
+PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 16)) return nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_policy_loss)>(a[0]);
+        const auto bytes = entry<decltype(&moara_policy_loss_workspace_bytes)>(a[15]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        const long device = PyLong_AsLong(a[13]);
+        void* stream = PyLong_AsVoidPtr(a[14]);
+        const double low = PyFloat_AsDouble(a[8]), high = PyFloat_AsDouble(a[9]), kl = PyFloat_AsDouble(a[10]);
+        const int grad = PyObject_IsTrue(a[11]);
+        Matrix z{}, dz{};
+        Held held;
+        if (PyErr_Occurred() || !matrix_arg(a[2], "logits", device, z)) return nullptr;
+        const auto* target = static_cast<const int64_t*>(entries_of(a[3], "targets", at::kLong, z.rows, device));
+        if (PyErr_Occurred()) return nullptr;
+        const char* const names[4] = {"old", "adv", "weights", "ref"};
+        const float* v[4];
+        for (int i = 0; i < 4; ++i) {
+            v[i] = static_cast<const float*>(entries_of(a[4 + i], names[i], at::kFloat, z.rows, device, i >= 2));
+            if (PyErr_Occurred()) return nullptr;
+        }
+        if (grad) {
+            held.at[2] = output_arg(a[12], "out", device, z, z.dtype, dz);
+        } else if (a[12] != Py_None) {
+            PyErr_SetString(PyExc_ValueError, "out: no gradient is asked for");
+        } else {
+            held.at[2] = Py_NewRef(Py_None);
+        }
+        if (PyErr_Occurred()) return nullptr;
+        const at::Tensor sums = fresh({3}, at::kFloat, device), logp = fresh({z.rows}, at::kFloat, device);
+        held.at[0] = THPVariable_Wrap(sums);
+        held.at[1] = THPVariable_Wrap(logp);
+        size_t size = 0;
+        at::Tensor ws;
+        if (bytes(z.rows, &size) == MOARA_OK) ws = fresh({static_cast<int64_t>(size)}, at::kByte, device);
+        const int code = fn(ctx, z.rows, z.cols, z.p, z.dtype, z.ld, target, v[0], v[3], v[1], v[2], static_cast<float>(low),
+                            static_cast<float>(high), static_cast<float>(kl), sums.data_ptr<float>(), logp.data_ptr<float>(), dz.p,
+                            dz.ld, size > 0 ? ws.data_ptr() : nullptr, size, stream);
+        if (code != MOARA_OK) return PyLong_FromLong(code);
+        PyObject *s = held.take(0), *l = held.take(1);
+        return Py_BuildValue("(NNN)", s, l, held.take(2));
+    } catch (const std::exception& e) {
+        return caught(e);
+    }
+}
+
+// A bf16 tensor of tokens x heads x entries whose entries are contiguous.
+struct Heads {
+    void* p;
+    int tokens, heads, dim;
+    int64_t row, head;
+};
+
+bool heads_arg(PyObject* o, const char* what, long device, Heads& h) {
+    if (THPVariable_Check(o)) {
+        const at::Tensor& t = THPVariable_Unpack(o);
+        if (t.layout() == at::kStrided && t.dim() == 3 && t.is_cuda() && t.get_device() == device && t.scalar_type() == at::kBFloat16 &&
+            t.size(0) <= INT32_MAX && t.size(1) <= INT32_MAX && t.size(2) <= INT32_MAX && (t.size(2) == 1 || t.stride(2) == 1)) {
+            h = Heads{const_cast<void*>(t.const_data_ptr()), static_cast<int>(t.size(0)), static_cast<int>(t.size(1)),
+                      static_cast<int>(t.size(2)), t.stride(0), t.stride(1)};
+            return true;
+        }
+    }
+    PyErr_Format(PyExc_ValueError, "%s: a bfloat16 tensor of tokens x heads x contiguous entries on cuda:%ld is needed", what, device);
+    return false;
+}
+
+bool attention_args(PyObject* const* a, long device, Heads& q, Heads& k, Heads& v) {
+    if (!heads_arg(a[0], "q", device, q) || !heads_arg(a[1], "k", device, k) || !heads_arg(a[2], "v", device, v)) return false;
+    if (k.tokens != q.tokens || v.tokens != q.tokens || k.dim != q.dim || v.dim != q.dim || k.heads != v.heads) {
+        PyErr_SetString(PyExc_ValueError, "q, k and v need the same tokens and entries, k and v the same heads");
+        return false;
+    }
+    return true;
+}
+
+// attention(entry, ctx, sequences, q, k, v, scale, train, device, stream) -> (out, lse, rest or None) or an error code
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 10)) return nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_attention)>(a[0]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        const auto* seqs = static_cast<const moara_sequences*>(PyLong_AsVoidPtr(a[2]));
+        const double scale = PyFloat_AsDouble(a[6]);
+        const int train = PyObject_IsTrue(a[7]);
+        const long device = PyLong_AsLong(a[8]);
+        void* stream = PyLong_AsVoidPtr(a[9]);
+        Heads q, k, v;
+        if (PyErr_Occurred() || !attention_args(a + 3, device, q, k, v)) return nullptr;
+        // rows that belong to no sequence are not written
+        const bool zero = q.tokens > seqs->tokens;
+        const at::Tensor out = fresh({q.tokens, q.heads, q.dim}, at::kBFloat16, device, zero);
+        const at::Tensor lse = fresh({q.heads, q.tokens}, at::kFloat, device, zero);
+        at::Tensor rest;
+        if (train) rest = fresh({q.tokens, q.heads, q.dim}, at::kBFloat16, device, zero);
+        const int code = fn(ctx, seqs, q.tokens, q.heads, k.heads, q.dim, static_cast<float>(scale), q.p, q.row, q.head, k.p, k.row,
+                            k.head, v.p, v.row, v.head, out.data_ptr(), train ? rest.data_ptr() : nullptr, lse.data_ptr<float>(), stream);
+        if (code != MOARA_OK) return PyLong_FromLong(code);
+        return Py_BuildValue("(NNN)", THPVariable_Wrap(out), THPVariable_Wrap(lse), train ? THPVariable_Wrap(rest) : Py_NewRef(Py_None));
+    } catch (const std::exception& e) {
+        return caught(e);
+    }
+}
+
+// attention_backward(entry, ctx, sequences, dout, q, k, v, out, lse, rest, scale, device, stream)
+// -> (dq, dk, dv) or an error code
+PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
+    if (!arguments(count, 13)) return nullptr;
+    try {
+        const auto fn = entry<decltype(&moara_attention_backward)>(a[0]);
+        auto* ctx = static_cast<moara_ctx*>(PyLong_AsVoidPtr(a[1]));
+        const auto* seqs = static_cast<const moara_sequences*>(PyLong_AsVoidPtr(a[2]));
+        const double scale = PyFloat_AsDouble(a[10]);
+        const long device = PyLong_AsLong(a[11]);
+        void* stream = PyLong_AsVoidPtr(a[12]);
+        Heads q, k, v, d;
+        if (PyErr_Occurred() || !heads_arg(a[3], "dout", device, d) || !attention_args(a + 4, device, q, k, v)) return nullptr;
+        if (d.tokens != q.tokens || d.heads != q.heads || d.dim != q.dim)
+            return PyErr_Format(PyExc_ValueError, "dout needs q's shape");
+        const int64_t rows = static_cast<int64_t>(q.tokens) * q.heads, entries = rows * q.dim;
+        const void* out = entries_of(a[7], "out", at::kBFloat16, entries, device);
+        if (PyErr_Occurred()) return nullptr;
+        const void* lse = entries_of(a[8], "lse", at::kFloat, rows, device);
+        if (PyErr_Occurred()) return nullptr;
+        const void* rest = entries_of(a[9], "rest", at::kBFloat16, entries, device, true);
+        if (PyErr_Occurred()) return nullptr;
+        const bool zero = q.tokens > seqs->tokens;
+        const at::Tensor dq = fresh({q.tokens, q.heads, q.dim}, at::kBFloat16, device, zero);
+        const at::Tensor dk = fresh({q.tokens, k.heads, q.dim}, at::kBFloat16, device, zero);
+        const at::Tensor dv = fresh({q.tokens, k.heads, q.dim}, at::kBFloat16, device, zero);
+        const at::Tensor delta = fresh({rows}, at::kFloat, device);
+        const int code = fn(ctx, seqs, q.tokens, q.heads, k.heads, q.dim, static_cast<float>(scale), d.p, d.row, d.head, q.p, q.row,
+                            q.head, k.p, k.row, k.head, v.p, v.row, v.head, out, rest, static_cast<const float*>(lse),
+                            delta.data_ptr<float>(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), stream);
+        if (code != MOARA_OK) return PyLong_FromLong(code);
+        return Py_BuildValue("(NNN)", THPVariable_Wrap(dq), THPVariable_Wrap(dk), THPVariable_Wrap(dv));
+    } catch (const std::exception& e) {
+        return caught(e);
+    }
+}
+
 #define MOARA_METHOD(name, doc) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, doc}
 
 PyMethodDef methods[] = {
@@ -455,6 +782,12 @@ PyMethodDef methods[] = {
     MOARA_METHOD(fp4_product, "moara_fp4_product into a matrix or a new one -> the matrix, or an error code"),
     MOARA_METHOD(fp4_linear, "moara_fp4_linear into a matrix or a new one -> the matrix, or an error code"),
     MOARA_METHOD(fp4_dequantize, "moara_fp4_dequantize into a matrix or a new one -> the matrix, or an error code"),
+    MOARA_METHOD(rms_norm, "moara_rms_norm -> (h, y, rstd), or an error code"),
+    MOARA_METHOD(rms_norm_quantize, "moara_rms_norm_quantize into new operands -> their buffers, or an error code"),
+    MOARA_METHOD(rms_norm_backward, "moara_rms_norm_backward -> (dx, dgain), or an error code"),
+    MOARA_METHOD(policy_loss, "moara_policy_loss -> (sums, logp, gradient), or an error code"),
+    MOARA_METHOD(attention, "moara_attention -> (out, lse, rest), or an error code"),
+    MOARA_METHOD(attention_backward, "moara_attention_backward -> (dq, dk, dv), or an error code"),
     MOARA_METHOD(matrix, "matrix(x, device) -> (address, type, rows, columns, row pitch)"),
     MOARA_METHOD(bytes, "bytes(count, device) -> (uint8 tensor, its address)"),
     {nullptr, nullptr, 0, nullptr}};
