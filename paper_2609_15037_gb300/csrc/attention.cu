@@ -38,6 +38,29 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t f32x2(float a, float b) {
+    uint64_t y;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+    return y;
+}
+__device__ __forceinline__ void split(uint64_t x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t y;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+    return y;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t y;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+    return y;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t y;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+    return y;
+}
+
 // D = A B^T over DP columns, both tiles in shared memory by rows (K-major): 128 x 128.
 template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b) {
     constexpr uint32_t idesc = ptx::idesc_bf16(128, ROWS, 0, 0);
@@ -49,15 +72,15 @@ template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t 
 }
 
 // The same tile as the operand whose rows are summed over: D (128 x DP) (+)= A B with A in
-// tensor memory, 64 entries of K in columns a .. a + 31 and 64 from a + far on; the first
-// 16 `steps` rows of B.
-template <int DP>
-__device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint32_t far, uint32_t b, int steps, bool add) {
+// tensor memory, RUN entries of K in columns a .. a + RUN / 2 - 1, RUN more from a + PITCH on
+// and so on; the first 16 `steps` rows of B.
+template <int DP, int RUN, int PITCH>
+__device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint32_t b, int steps, bool add) {
     constexpr uint32_t idesc = ptx::idesc_bf16(128, DP, 0, 1);
 #pragma unroll
     for (int k = 0; k < ROWS / 16; ++k)
         if (k < steps)
-            ptx::mma_f16_ta(d, a + k / 4 * far + k % 4 * 8, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, add || k > 0);
+            ptx::mma_f16_ta(d, a + k * 16 / RUN * PITCH + k * 16 % RUN / 2, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, add || k > 0);
 }
 
 // Rows from `rows` to the next multiple of 16 of a tile become zero, by a warp that
@@ -209,7 +232,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
                 if (!ok) break;
                 ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP>(tmem + 256 + i * DP, tmem + i * ROWS, 32, slots + vs * F::TILE, steps, j > 0);
+                    mma_sum<DP, ROWS, 0>(tmem + 256 + i * DP, tmem + i * ROWS, slots + vs * F::TILE, steps, j > 0);
                     if (j + 1 == mine) ptx::mma_commit(ptx::smem_u32(&ctl->ofull[i]));
                 }
                 __syncwarp();
@@ -269,22 +292,25 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
                     ptx::tmem_st32(ot + c, o);
                 }
             }
-            const float shift = -ref * scale;
-            float part[4] = {};
+            const uint64_t by = f32x2(scale, scale), shift = f32x2(-ref * scale, -ref * scale);
+            uint64_t part[2] = {};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 uint32_t w[32];
 #pragma unroll
                 for (int c = 0; c < 32; ++c) {
-                    const float a = ex2(fmaf(__uint_as_float(s[h][2 * c]), scale, shift));
-                    const float b = ex2(fmaf(__uint_as_float(s[h][2 * c + 1]), scale, shift));
-                    part[2 * (c & 1)] += a;
-                    part[2 * (c & 1) + 1] += b;
+                    float a, b;
+                    split(fma2(f32x2(__uint_as_float(s[h][2 * c]), __uint_as_float(s[h][2 * c + 1])), by, shift), a, b);
+                    a = ex2(a);
+                    b = ex2(b);
+                    part[c & 1] = add2(part[c & 1], f32x2(a, b));
                     w[c] = pack2(a, b);
                 }
                 ptx::tmem_st32(st + 32 * h, w);
             }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            float a, b;
+            split(add2(part[0], part[1]), a, b);
+            sum += a + b;
             ptx::tmem_st_wait();
             ptx::tc_fence_before();
             __syncwarp();
@@ -342,7 +368,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
 // stay in tensor memory and dV += P^T dO, dK += dS^T Q take them from there.  Otherwise it
 // takes 128 queries of a head and goes through their keys: dQ += dS K.
 //
-// Eight warps turn S into P and dP = dO V^T into dS (64 columns a thread, one row), one
+// Sixteen warps turn S into P and dP = dO V^T into dS (32 columns of a row a thread), one
 // issues products, one copies.  The tile that is used twice in a step (first in S, last in a
 // sum) has three slots, the other two.
 // ---------------------------------------------------------------------------
@@ -352,7 +378,8 @@ template <int DP> struct Backward {
     static constexpr int STATS = 2 * 2 * ROWS * 4;                 // lse and delta of two steps
     static constexpr int CTL = 256;
     static constexpr int SMEM = (2 + SA + SB) * TILE + STATS + CTL;
-    static constexpr int THREADS = 10 * 32;
+    static constexpr int WARPS = 16, COLS = ROWS * 4 / WARPS;      // that turn S into dS; columns of a thread
+    static constexpr int THREADS = (WARPS + 2) * 32;
     static_assert(SMEM <= 227 * 1024, "shared memory");
 };
 
@@ -379,6 +406,7 @@ struct BackwardCtl {
 template <int DP, bool KEYS>
 __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(const __grid_constant__ BackwardParams p) {
     using F = Backward<DP>;
+    constexpr int WARPS = F::WARPS, COLS = F::COLS;
     static_assert(sizeof(BackwardCtl) <= F::CTL, "the barriers fit");
     extern __shared__ __align__(1024) uint8_t smem[];              // there is no room to align it here
     uint8_t* const ring_a = smem + 2 * F::TILE;
@@ -393,10 +421,10 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
     }
     if (threadIdx.x == 0) {
         for (uint64_t* b : {&ctl->fixed, &ctl->sfull, &ctl->dpfull, &ctl->done, &ctl->drain}) ptx::mbar_init(ptx::smem_u32(b), 1);
-        ptx::mbar_init(ptx::smem_u32(&ctl->pfull), 8);
-        ptx::mbar_init(ptx::smem_u32(&ctl->dsfull), 8);
-        ptx::mbar_init(ptx::smem_u32(&ctl->stats[0]), 8);
-        ptx::mbar_init(ptx::smem_u32(&ctl->stats[1]), 8);
+        ptx::mbar_init(ptx::smem_u32(&ctl->pfull), WARPS);
+        ptx::mbar_init(ptx::smem_u32(&ctl->dsfull), WARPS);
+        ptx::mbar_init(ptx::smem_u32(&ctl->stats[0]), WARPS);
+        ptx::mbar_init(ptx::smem_u32(&ctl->stats[1]), WARPS);
         for (int i = 0; i < F::SA; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl->afull[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl->aempty[i]), 1);
@@ -409,7 +437,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         ctl->filled[0] = ctl->filled[1] = 0;
         ptx::fence_barrier_init();
     }
-    if (warp == 9) {
+    if (warp == WARPS + 1) {
         ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
         ptx::tmem_relinquish();
     }
@@ -435,7 +463,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
     constexpr uint32_t SUM_B = 256, SUM_A = 384;                   // KEYS: dV, dK; otherwise dQ is SUM_A
     auto dp_at = [&](int j) { return KEYS ? DPC : DPC + static_cast<uint32_t>(j & 1) * 128; };
 
-    if (warp == 8) {
+    if (warp == WARPS) {
         if (lane == 0) {
             auto copy = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
                 for (int c = 0; c < DP / 64; ++c)
@@ -463,7 +491,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             ctl->filled[0] = na;
             ctl->filled[1] = nb;
         }
-    } else if (warp == 9) {
+    } else if (warp == WARPS + 1) {
         const bool leader = ptx::elect_one();
         const uint32_t fixed = ptx::smem_u32(smem), ra = ptx::smem_u32(ring_a), rb = ptx::smem_u32(ring_b);
         auto commit = [&](uint64_t& bar) {
@@ -498,7 +526,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
                 ok = wait(ctl->pfull, j & 1);
                 if (!ok) break;
                 ptx::tc_fence_after();
-                if (leader) mma_sum<DP>(tmem + SUM_B, tmem + S, 64, rb + j % F::SB * F::TILE, sum_steps(j), j > 0);
+                if (leader) mma_sum<DP, COLS, COLS>(tmem + SUM_B, tmem + S, rb + j % F::SB * F::TILE, sum_steps(j), j > 0);
                 commit(ctl->bempty[j % F::SB]);
                 // the next S over the P that the product in front of it has read by then
                 if (j + 1 < steps && !score(j + 1)) break;
@@ -511,7 +539,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             ok = wait(ctl->dsfull, j & 1);
             if (!ok) break;
             ptx::tc_fence_after();
-            if (leader) mma_sum<DP>(tmem + SUM_A, tmem + dp_at(j), 64, ra + j % F::SA * F::TILE, sum_steps(j), j > 0);
+            if (leader) mma_sum<DP, COLS, COLS>(tmem + SUM_A, tmem + dp_at(j), ra + j % F::SA * F::TILE, sum_steps(j), j > 0);
             commit(ctl->aempty[j % F::SA]);
             if (KEYS && j + 1 < steps && !slope(j + 1)) break;
             if (j + 1 == steps) commit(ctl->done);
@@ -519,69 +547,80 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         commit(ctl->drain);
         wait_drain(ptx::smem_u32(&ctl->drain), 0);
     } else {
-        const int half = warp >> 2, quad = warp & 3, r = quad * 32 + lane;
+        const int part = warp >> 2, quad = warp & 3, r = quad * 32 + lane, c0 = part * COLS;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const int row = tile.tile * ROWS + r;                       // in the sequence
         const bool real = row < tile.length;
         const long long token = tile.begin + row;
-        const float scale = p.scale * kLog2e;
-        float lse = 0.0f, delta = 0.0f;
+        const uint64_t scale = f32x2(p.scale * kLog2e, p.scale * kLog2e);
+        uint64_t lse = 0, delta = 0;                                // negative, of the row
         if (!KEYS && real) {
-            lse = p.lse[static_cast<long long>(owner) * p.tokens + token] * kLog2e;
-            delta = p.delta[static_cast<long long>(owner) * p.tokens + token];
+            const float l = -p.lse[static_cast<long long>(owner) * p.tokens + token] * kLog2e;
+            const float d = -p.delta[static_cast<long long>(owner) * p.tokens + token];
+            lse = f32x2(l, l);
+            delta = f32x2(d, d);
         }
-        // KEYS: lse (first half of the threads) or delta of a query of step j
+        // KEYS: negative lse (first 128 threads) or delta (the next) of a query of step j
         auto stat = [&](int j) {
             const int q = tile_of(j) * ROWS + r;
-            if (q >= tile.length) return 0.0f;
+            if (q >= tile.length || part >= 2) return 0.0f;
             const long long at = static_cast<long long>(head_of(j)) * p.tokens + tile.begin + q;
-            return half == 0 ? p.lse[at] * kLog2e : p.delta[at];
+            return part == 0 ? -p.lse[at] * kLog2e : -p.delta[at];
         };
         float next = KEYS ? stat(0) : 0.0f;
         bool ok = true;
         for (int j = 0; j < steps; ++j) {
-            const float* sl = stats + (j & 1) * 2 * ROWS + half * 64;
-            const float* sd = sl + ROWS;
+            const ulonglong2* sl = reinterpret_cast<const ulonglong2*>(stats + (j & 1) * 2 * ROWS + c0);
+            const ulonglong2* sd = sl + ROWS / 4;
             if (KEYS) {
-                stats[(j & 1) * 2 * ROWS + half * ROWS + r] = next;
+                if (part < 2) stats[(j & 1) * 2 * ROWS + part * ROWS + r] = next;
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->stats[j & 1]));
                 if (j + 1 < steps) next = stat(j + 1);
-                // all eight warps' (a barrier whose wait is bounded); they have left step j - 1 by then
+                // all warps' (a barrier whose wait is bounded); they have left step j - 1 by then
                 ok = wait(ctl->stats[j & 1], (j >> 1) & 1);
                 if (!ok) break;
             }
             // which columns of this thread count: from `from` on (KEYS) up to `to`
-            int from = 0, to = 64;
+            int from = 0, to = COLS;
             if (KEYS) {
-                if (tile_of(j) == tile.tile) from = r - half * 64;
-                if (tile_of(j) == last) to = tail - half * 64;
+                if (tile_of(j) == tile.tile) from = r - c0;
+                if (tile_of(j) == last) to = tail - c0;
             } else if (j == tile.tile) {
-                to = r + 1 - half * 64;
+                to = r + 1 - c0;
             }
-            const bool all = from <= 0 && to >= 64;
+            const bool all = __all_sync(0xffffffffu, from <= 0 && to >= COLS);
             ok = wait(ctl->sfull, j & 1);
             if (!ok) break;
             ptx::tc_fence_after();
-            uint32_t s[64];
-            ptx::tmem_ld64(lanes + S + half * 64, s);
+            uint32_t s[COLS];
+            ptx::tmem_ld32(lanes + S + c0, s);
             if (!KEYS) {
                 ptx::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull));
             }
-            float x[64];
+            float x[COLS];
 #pragma unroll
-            for (int c = 0; c < 64; ++c) x[c] = ex2(fmaf(__uint_as_float(s[c]), scale, KEYS ? -sl[c] : -lse));
-            if (__any_sync(0xffffffffu, !all)) {
+            for (int c = 0; c < COLS; c += 4) {
+                const ulonglong2 l = KEYS ? sl[c / 4] : make_ulonglong2(lse, lse);
 #pragma unroll
-                for (int c = 0; c < 64; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
+                for (int e = 0; e < 4; e += 2) {
+                    split(fma2(f32x2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale, e == 0 ? l.x : l.y), x[c + e],
+                          x[c + e + 1]);
+                    x[c + e] = ex2(x[c + e]);
+                    x[c + e + 1] = ex2(x[c + e + 1]);
+                }
             }
-            if (KEYS) {
-                uint32_t w[32];
+            if (!all) {
 #pragma unroll
-                for (int c = 0; c < 32; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
-                ptx::tmem_st32(lanes + S + half * 64, w);
+                for (int c = 0; c < COLS; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
+            }
+            uint32_t w[COLS / 2];
+            if (KEYS) {
+#pragma unroll
+                for (int c = 0; c < COLS / 2; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
+                ptx::tmem_st16(lanes + S + c0, w);
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -590,17 +629,23 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             ok = wait(ctl->dpfull, j & 1);
             if (!ok) break;
             ptx::tc_fence_after();
-            ptx::tmem_ld64(lanes + dp_at(j) + half * 64, s);
+            ptx::tmem_ld32(lanes + dp_at(j) + c0, s);
 #pragma unroll
-            for (int c = 0; c < 64; ++c) x[c] *= __uint_as_float(s[c]) - (KEYS ? sd[c] : delta);
-            if (__any_sync(0xffffffffu, !all)) {                    // what is not counted may be infinite or NaN
+            for (int c = 0; c < COLS; c += 4) {
+                const ulonglong2 d = KEYS ? sd[c / 4] : make_ulonglong2(delta, delta);
 #pragma unroll
-                for (int c = 0; c < 64; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
+                for (int e = 0; e < 4; e += 2)
+                    split(mul2(f32x2(x[c + e], x[c + e + 1]),
+                               add2(f32x2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), e == 0 ? d.x : d.y)),
+                          x[c + e], x[c + e + 1]);
             }
-            uint32_t w[32];
+            if (!all) {                                             // what is not counted may be infinite or NaN
 #pragma unroll
-            for (int c = 0; c < 32; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
-            ptx::tmem_st32(lanes + dp_at(j) + half * 64, w);
+                for (int c = 0; c < COLS; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
+            }
+#pragma unroll
+            for (int c = 0; c < COLS / 2; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
+            ptx::tmem_st16(lanes + dp_at(j) + c0, w);
             ptx::tmem_st_wait();
             ptx::tc_fence_before();
             __syncwarp();
@@ -609,25 +654,25 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         if (ok) ok = wait(ctl->done, 0);
         if (ok) {
             ptx::tc_fence_after();
-            // KEYS: the first half of the threads has dV, the second dK; otherwise half of dQ's columns each
+            // KEYS: the first half of the threads has dV, the second dK; otherwise all have dQ
+            constexpr int PARTS = KEYS ? WARPS / 8 : WARPS / 4, WIDTH = DP / PARTS;
+            const bool first = KEYS && part < PARTS;
             const long long at = (token * owners + owner) * p.dim;
-            bf16* out = (KEYS && half == 0 ? p.out_b : p.out_a) + at;
-            const uint32_t src = lanes + (KEYS && half == 0 ? SUM_B : SUM_A);
-            const float factor = KEYS && half == 0 ? 1.0f : p.scale;
-            constexpr int COLS = KEYS ? DP : DP / 2;
-            const int c0 = KEYS ? 0 : half * COLS;
+            bf16* out = (first ? p.out_b : p.out_a) + at;
+            const uint32_t src = lanes + (first ? SUM_B : SUM_A);
+            const float factor = first ? 1.0f : p.scale;
+            const int o0 = part % PARTS * WIDTH;
 #pragma unroll
-            for (int c = 0; c < COLS; c += 32) {
-                uint32_t o[32];
-                ptx::tmem_ld32(src + c0 + c, o);
+            for (int c = 0; c < WIDTH; c += 16) {
+                float o[16];
+                ptx::tmem_ld16(src + o0 + c, o);
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    if (!real || c0 + c + e >= p.dim) continue;
+                for (int e = 0; e < 16; e += 8) {
+                    if (!real || o0 + c + e >= p.dim) continue;
                     uint32_t w[4];
 #pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        w[y] = pack2(__uint_as_float(o[e + 2 * y]) * factor, __uint_as_float(o[e + 2 * y + 1]) * factor);
-                    *reinterpret_cast<uint4*>(out + c0 + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
+                    for (int y = 0; y < 4; ++y) w[y] = pack2(o[e + 2 * y] * factor, o[e + 2 * y + 1] * factor);
+                    *reinterpret_cast<uint4*>(out + o0 + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
                 }
             }
         }
@@ -641,7 +686,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         for (int n = max(0, ctl->filled[1] - F::SB); n < ctl->filled[1]; ++n)
             wait_drain(ptx::smem_u32(&ctl->bfull[n % F::SB]), (n / F::SB) & 1);
     }
-    if (warp == 9) {
+    if (warp == WARPS + 1) {
         ptx::tc_fence_after();
         ptx::tmem_dealloc(tmem, 512);
     }
