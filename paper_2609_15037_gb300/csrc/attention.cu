@@ -77,10 +77,16 @@ template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t 
 template <int DP, int RUN, int PITCH>
 __device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint32_t b, int steps, bool add) {
     constexpr uint32_t idesc = ptx::idesc_bf16(128, DP, 0, 1);
+    const auto one = [&](int k, uint32_t acc) {
+        ptx::mma_f16_ta(d, a + k * 16 / RUN * PITCH + k * 16 % RUN / 2, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, acc);
+    };
+    one(0, add);
+    if (steps == ROWS / 16) {                                      // a test for each would take as long as a product
 #pragma unroll
-    for (int k = 0; k < ROWS / 16; ++k)
-        if (k < steps)
-            ptx::mma_f16_ta(d, a + k * 16 / RUN * PITCH + k * 16 % RUN / 2, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, add || k > 0);
+        for (int k = 1; k < ROWS / 16; ++k) one(k, 1);
+    } else {
+        for (int k = 1; k < steps; ++k) one(k, 1);
+    }
 }
 
 // Rows from `rows` to the next multiple of 16 of a tile become zero, by a warp that
@@ -168,8 +174,8 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     const AttentionTile pair = p.pairs[blockIdx.x / p.heads];
     const int head = blockIdx.x % p.heads, kv = head / p.group;
     const int q0 = 2 * pair.tile;                                  // the first of the two tiles
-    const bool two = (q0 + 1) * ROWS < pair.length;
-    const int tiles = q0 + 1 + two;                                // of keys; tile i sees q0 + 1 + i
+    const bool second = (q0 + 1) * ROWS < pair.length;
+    const int tiles = q0 + 1 + second;                                // of keys; tile i sees q0 + 1 + i
     auto wait = [&](uint64_t& bar, uint32_t parity) {
         return ptx::mbar_wait_warp(ptx::smem_u32(&bar), parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
     };
@@ -189,7 +195,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
                                                      MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
                     break;
                 fill(ring + slot * F::TILE, n & 1 ? &p.v : &p.k, ctl->full[slot], kv, pair.begin + n / 2 * ROWS);
-                if (n == 0 && two) fill(smem + F::TILE, &p.q, ctl->qfull[1], head, pair.begin + (q0 + 1) * ROWS);
+                if (n == 0 && second) fill(smem + F::TILE, &p.q, ctl->qfull[1], head, pair.begin + (q0 + 1) * ROWS);
             }
             ctl->filled = n;
         }
@@ -211,40 +217,44 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
         if (ok) {
             ptx::tc_fence_after();
             score(0, 0);
-            if (two) {
+            if (second) {
                 ok = wait(ctl->qfull[1], 0);
                 if (ok) score(1, 0);
             }
             if (ok) release(0);
         }
+        // what a product needs but P is waited for ahead, so that the products of a step follow
+        // one another
         for (int j = 0; j < tiles && ok; ++j) {
             const int n = 2 * j + 1, vs = n % F::SLOTS, ks = (n + 1) % F::SLOTS;
-            ok = wait(ctl->full[vs], (n / F::SLOTS) & 1);
-            if (!ok) break;
-            ptx::tc_fence_after();
+            const bool more = j + 1 < tiles;
             const int left = pair.length - j * ROWS;                // keys from this tile on
             const int steps = left >= ROWS ? ROWS / 16 : (left + 15) / 16;
+            const uint32_t v = slots + vs * F::TILE, k = slots + ks * F::TILE;
+            ok = wait(ctl->full[vs], (n / F::SLOTS) & 1) && (!more || wait(ctl->full[ks], ((n + 1) / F::SLOTS) & 1));
+            if (!ok) break;
             if (left < ROWS && left % 16 != 0) clear_rows<DP>(ring + vs * F::TILE, left, lane);
-            for (int i = 0; i < 2 && ok; ++i) {
+            for (int i = 0; i < 2; ++i) {
                 const int mine = i == 0 ? q0 + 1 : tiles;           // key tiles of this tile of queries
-                if (j >= mine || (i == 1 && !two)) continue;
+                if (j >= mine || (i == 1 && !second)) continue;
                 ok = wait(ctl->pfull[i], j & 1);
                 if (!ok) break;
                 ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, ROWS, 0>(tmem + 256 + i * DP, tmem + i * ROWS, slots + vs * F::TILE, steps, j > 0);
-                    if (j + 1 == mine) ptx::mma_commit(ptx::smem_u32(&ctl->ofull[i]));
+                    mma_sum<DP, ROWS, 0>(tmem + 256 + i * DP, tmem + i * ROWS, v, steps, j > 0);
+                    if (j + 1 == mine) {
+                        ptx::mma_commit(ptx::smem_u32(&ctl->ofull[i]));
+                    } else {
+                        // S over the P that the product in front of it has read by then
+                        mma_rows<DP>(tmem + i * ROWS, base + i * F::TILE, k);
+                        ptx::mma_commit(ptx::smem_u32(&ctl->sfull[i]));
+                    }
                 }
                 __syncwarp();
-                if (j + 1 < mine) {
-                    // its S over the P that the product in front of it in the queue has read by then
-                    ok = wait(ctl->full[ks], ((n + 1) / F::SLOTS) & 1);
-                    if (ok) score(i, ks);
-                }
             }
             if (ok) {
                 release(vs);
-                if (j + 1 < tiles) release(ks);
+                if (more) release(ks);
             }
         }
         if (leader) ptx::mma_commit(ptx::smem_u32(&ctl->drain));
@@ -252,7 +262,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
         wait_drain(ptx::smem_u32(&ctl->drain), 0);
     } else {
         const int i = warp >> 2, quad = warp & 3, r = quad * 32 + lane;     // tile, lane quadrant, row
-        const int mine = i == 0 ? q0 + 1 : two ? tiles : 0;
+        const int mine = i == 0 ? q0 + 1 : second ? tiles : 0;
         const int row = (q0 + i) * ROWS + r;                        // in the sequence
         const uint32_t st = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * ROWS;
         const uint32_t ot = tmem + (static_cast<uint32_t>(quad * 32) << 16) + 256 + i * DP;
@@ -349,7 +359,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) {      // a wait that ran out: no copy stays in flight
         wait_drain(ptx::smem_u32(&ctl->qfull[0]), 0);
-        if (two && ctl->filled > 0) wait_drain(ptx::smem_u32(&ctl->qfull[1]), 0);
+        if (second && ctl->filled > 0) wait_drain(ptx::smem_u32(&ctl->qfull[1]), 0);
         for (int n = max(0, ctl->filled - F::SLOTS); n < ctl->filled; ++n)
             wait_drain(ptx::smem_u32(&ctl->full[n % F::SLOTS]), (n / F::SLOTS) & 1);
     }
@@ -498,51 +508,83 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             if (leader) ptx::mma_commit(ptx::smem_u32(&bar));
             __syncwarp();
         };
-        // rows of a tile that a sum runs over
-        auto rows_of = [&](int j) { return tile_of(j) == last ? tail : ROWS; };
-        auto sum_steps = [&](int j) { return (rows_of(j) + 15) / 16; };
-        auto score = [&](int j) {
-            const int sa = j % F::SA;
-            if (!wait(ctl->afull[sa], (j / F::SA) & 1)) return false;
-            if (rows_of(j) % 16 != 0) clear_rows<DP>(ring_a + sa * F::TILE, rows_of(j), lane);
-            ptx::tc_fence_after();
-            if (leader) mma_rows<DP>(tmem + S, fixed, ra + sa * F::TILE);
-            commit(ctl->sfull);
+        // The operands of step j: slots of both rings, whose phases end with theirs, and the rows
+        // of the tile that a sum runs over.  They are waited for ahead, so that the products of
+        // a step follow one another.
+        int sa = 0, sb = 0, at = KEYS ? tile.tile : 0;
+        uint32_t pa = 0, pb = 0;
+        auto rows = [&] { return at == last ? tail : ROWS; };
+        auto have_a = [&] {
+            if (!wait(ctl->afull[sa], pa)) return false;
+            if (rows() % 16 != 0) clear_rows<DP>(ring_a + sa * F::TILE, rows(), lane);
             return true;
+        };
+        auto have_b = [&] {
+            if (!wait(ctl->bfull[sb], pb)) return false;
+            if (KEYS && rows() % 16 != 0) clear_rows<DP>(ring_b + sb * F::TILE, rows(), lane);
+            return true;
+        };
+        auto next = [&] {
+            at = at == last ? tile.tile : at + 1;
+            if (++sa == F::SA) { sa = 0; pa ^= 1; }
+            if (++sb == F::SB) { sb = 0; pb ^= 1; }
+        };
+        auto score = [&] {
+            mma_rows<DP>(tmem + S, fixed, ra + sa * F::TILE);
+            ptx::mma_commit(ptx::smem_u32(&ctl->sfull));
         };
         auto slope = [&](int j) {
-            const int sb = j % F::SB;
-            if (!wait(ctl->bfull[sb], (j / F::SB) & 1)) return false;
-            if (KEYS && rows_of(j) % 16 != 0) clear_rows<DP>(ring_b + sb * F::TILE, rows_of(j), lane);
-            ptx::tc_fence_after();
-            if (leader) mma_rows<DP>(tmem + dp_at(j), fixed + F::TILE, rb + sb * F::TILE);
-            commit(ctl->dpfull);
-            if (!KEYS) commit(ctl->bempty[sb]);
-            return true;
+            mma_rows<DP>(tmem + dp_at(j), fixed + F::TILE, rb + sb * F::TILE);
+            ptx::mma_commit(ptx::smem_u32(&ctl->dpfull));
+            if (!KEYS) ptx::mma_commit(ptx::smem_u32(&ctl->bempty[sb]));
         };
-        bool ok = wait(ctl->fixed, 0) && score(0) && slope(0);
+        bool ok = wait(ctl->fixed, 0) && have_a() && have_b();
+        if (ok) {
+            ptx::tc_fence_after();
+            if (leader) {
+                score();
+                slope(0);
+            }
+            __syncwarp();
+        }
         for (int j = 0; j < steps && ok; ++j) {
+            const bool more = j + 1 < steps;
+            const uint32_t a = ra + sa * F::TILE, b = rb + sb * F::TILE;
+            const int oa = sa, ob = sb, sums = (rows() + 15) / 16;
+            next();
+            if (more && !have_a()) break;
             if (KEYS) {
                 ok = wait(ctl->pfull, j & 1);
                 if (!ok) break;
                 ptx::tc_fence_after();
-                if (leader) mma_sum<DP, COLS, COLS>(tmem + SUM_B, tmem + S, rb + j % F::SB * F::TILE, sum_steps(j), j > 0);
-                commit(ctl->bempty[j % F::SB]);
-                // the next S over the P that the product in front of it has read by then
-                if (j + 1 < steps && !score(j + 1)) break;
-            } else if (j + 1 < steps) {
+                if (leader) {
+                    mma_sum<DP, COLS, COLS>(tmem + SUM_B, tmem + S, b, sums, j > 0);
+                    ptx::mma_commit(ptx::smem_u32(&ctl->bempty[ob]));
+                    if (more) score();                              // over the P that the product in front of it has read by then
+                }
+                __syncwarp();
+                if (more && !have_b()) break;
+            } else if (more) {
+                if (!have_b()) break;
                 ok = wait(ctl->pfull, j & 1);
                 if (!ok) break;
                 ptx::tc_fence_after();
-                if (!score(j + 1) || !slope(j + 1)) break;
+                if (leader) {
+                    score();
+                    slope(j + 1);
+                }
+                __syncwarp();
             }
             ok = wait(ctl->dsfull, j & 1);
             if (!ok) break;
             ptx::tc_fence_after();
-            if (leader) mma_sum<DP, COLS, COLS>(tmem + SUM_A, tmem + dp_at(j), ra + j % F::SA * F::TILE, sum_steps(j), j > 0);
-            commit(ctl->aempty[j % F::SA]);
-            if (KEYS && j + 1 < steps && !slope(j + 1)) break;
-            if (j + 1 == steps) commit(ctl->done);
+            if (leader) {
+                mma_sum<DP, COLS, COLS>(tmem + SUM_A, tmem + dp_at(j), a, sums, j > 0);
+                ptx::mma_commit(ptx::smem_u32(&ctl->aempty[oa]));
+                if (KEYS && more) slope(j + 1);
+                if (!more) ptx::mma_commit(ptx::smem_u32(&ctl->done));
+            }
+            __syncwarp();
         }
         commit(ctl->drain);
         wait_drain(ptx::smem_u32(&ctl->drain), 0);
@@ -560,23 +602,30 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             lse = f32x2(l, l);
             delta = f32x2(d, d);
         }
-        // KEYS: negative lse (first 128 threads) or delta (the next) of a query of step j
-        auto stat = [&](int j) {
-            const int q = tile_of(j) * ROWS + r;
-            if (q >= tile.length || part >= 2) return 0.0f;
-            const long long at = static_cast<long long>(head_of(j)) * p.tokens + tile.begin + q;
-            return part == 0 ? -p.lse[at] * kLog2e : -p.delta[at];
+        // KEYS: negative lse (first 128 threads) or delta (the next) of a query of a step
+        int at = KEYS ? tile.tile : 0, head = kv * p.group;         // of the step: tile, head
+        auto follow = [&](int& t, int& h) {
+            h += t == last;
+            t = t == last ? tile.tile : t + 1;
         };
-        float next = KEYS ? stat(0) : 0.0f;
+        auto stat = [&](int t, int h) {
+            const int q = t * ROWS + r;
+            if (q >= tile.length || part >= 2) return 0.0f;
+            const long long from = static_cast<long long>(h) * p.tokens + tile.begin + q;
+            return part == 0 ? -p.lse[from] * kLog2e : -p.delta[from];
+        };
+        float stat_ahead = KEYS ? stat(at, head) : 0.0f;
         bool ok = true;
         for (int j = 0; j < steps; ++j) {
             const ulonglong2* sl = reinterpret_cast<const ulonglong2*>(stats + (j & 1) * 2 * ROWS + c0);
             const ulonglong2* sd = sl + ROWS / 4;
             if (KEYS) {
-                if (part < 2) stats[(j & 1) * 2 * ROWS + part * ROWS + r] = next;
+                if (part < 2) stats[(j & 1) * 2 * ROWS + part * ROWS + r] = stat_ahead;
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->stats[j & 1]));
-                if (j + 1 < steps) next = stat(j + 1);
+                int t = at, h = head;
+                follow(t, h);
+                if (j + 1 < steps) stat_ahead = stat(t, h);
                 // all warps' (a barrier whose wait is bounded); they have left step j - 1 by then
                 ok = wait(ctl->stats[j & 1], (j >> 1) & 1);
                 if (!ok) break;
@@ -584,8 +633,8 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             // which columns of this thread count: from `from` on (KEYS) up to `to`
             int from = 0, to = COLS;
             if (KEYS) {
-                if (tile_of(j) == tile.tile) from = r - c0;
-                if (tile_of(j) == last) to = tail - c0;
+                if (at == tile.tile) from = r - c0;
+                if (at == last) to = tail - c0;
             } else if (j == tile.tile) {
                 to = r + 1 - c0;
             }
@@ -650,6 +699,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             ptx::tc_fence_before();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->dsfull));
+            if (KEYS) follow(at, head);
         }
         if (ok) ok = wait(ctl->done, 0);
         if (ok) {
