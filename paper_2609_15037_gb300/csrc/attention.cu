@@ -128,6 +128,25 @@ struct ForwardParams {
     long long wait_limit;
 };
 
+// Waits of the warp that issues products.  Several at once: each costs some 100 clocks, and
+// the queue of products holds about 200 clocks of them.
+struct Waits {
+    volatile int* abort;
+    int* status;
+    long long limit;
+    __device__ __forceinline__ bool one(uint32_t bar, uint32_t parity) const {
+        return ptx::mbar_wait_warp(bar, parity, abort, status, MOARA_ERR_DEVICE_TIMEOUT, limit);
+    }
+    __device__ __forceinline__ bool two(uint32_t a, uint32_t pa, uint32_t b, uint32_t pb) const {
+        const bool x = ptx::mbar_try_wait(a, pa), y = ptx::mbar_try_wait(b, pb);
+        return __all_sync(0xffffffffu, x && y) || (one(a, pa) && one(b, pb));
+    }
+    __device__ __forceinline__ bool three(uint32_t a, uint32_t pa, uint32_t b, uint32_t pb, uint32_t c, uint32_t pc) const {
+        const bool x = ptx::mbar_try_wait(a, pa), y = ptx::mbar_try_wait(b, pb), z = ptx::mbar_try_wait(c, pc);
+        return __all_sync(0xffffffffu, x && y && z) || (one(a, pa) && one(b, pb) && one(c, pc));
+    }
+};
+
 template <int SLOTS> struct ForwardCtl {
     uint64_t qfull[2], full[SLOTS], empty[SLOTS], sfull[2], pfull[2], ofull[2], drain;
     uint32_t tmem;
@@ -223,39 +242,54 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             }
             if (ok) release(0);
         }
-        // what a product needs but P is waited for ahead, so that the products of a step follow
-        // one another
+        const Waits waits{abort_flag, p.status, p.wait_limit};
+        const uint32_t full = ptx::smem_u32(&ctl->full[0]), pfull = ptx::smem_u32(&ctl->pfull[0]);
         for (int j = 0; j < tiles && ok; ++j) {
             const int n = 2 * j + 1, vs = n % F::SLOTS, ks = (n + 1) % F::SLOTS;
             const bool more = j + 1 < tiles;
             const int left = pair.length - j * ROWS;                // keys from this tile on
             const int steps = left >= ROWS ? ROWS / 16 : (left + 15) / 16;
             const uint32_t v = slots + vs * F::TILE, k = slots + ks * F::TILE;
-            ok = wait(ctl->full[vs], (n / F::SLOTS) & 1) && (!more || wait(ctl->full[ks], ((n + 1) / F::SLOTS) & 1));
+            const uint32_t vp = (n / F::SLOTS) & 1, kp = ((n + 1) / F::SLOTS) & 1;
+            const bool one = j <= q0;                               // the first tile of queries sees these keys
+            const uint32_t first = pfull + (one ? 0 : 8);           // whose P comes first
+            ok = more ? waits.three(full + 8 * vs, vp, full + 8 * ks, kp, first, j & 1)
+                      : waits.two(full + 8 * vs, vp, first, j & 1);
             if (!ok) break;
             if (left < ROWS && left % 16 != 0) clear_rows<DP>(ring + vs * F::TILE, left, lane);
-            for (int i = 0; i < 2; ++i) {
-                const int mine = i == 0 ? q0 + 1 : tiles;           // key tiles of this tile of queries
-                if (j >= mine || (i == 1 && !second)) continue;
-                ok = wait(ctl->pfull[i], j & 1);
-                if (!ok) break;
+            if (one) {
                 ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, ROWS, 0>(tmem + 256 + i * DP, tmem + i * ROWS, v, steps, j > 0);
-                    if (j + 1 == mine) {
-                        ptx::mma_commit(ptx::smem_u32(&ctl->ofull[i]));
+                    mma_sum<DP, ROWS, 0>(tmem + 256, tmem, v, steps, j > 0);
+                    if (j == q0) {
+                        ptx::mma_commit(ptx::smem_u32(&ctl->ofull[0]));
                     } else {
                         // S over the P that the product in front of it has read by then
-                        mma_rows<DP>(tmem + i * ROWS, base + i * F::TILE, k);
-                        ptx::mma_commit(ptx::smem_u32(&ctl->sfull[i]));
+                        mma_rows<DP>(tmem, base, k);
+                        ptx::mma_commit(ptx::smem_u32(&ctl->sfull[0]));
+                    }
+                }
+                __syncwarp();
+                if (second && !(ok = waits.one(pfull + 8, j & 1))) break;
+            }
+            if (second) {
+                ptx::tc_fence_after();
+                if (leader) {
+                    mma_sum<DP, ROWS, 0>(tmem + 256 + DP, tmem + ROWS, v, steps, j > 0);
+                    if (!more) {
+                        ptx::mma_commit(ptx::smem_u32(&ctl->ofull[1]));
+                    } else {
+                        mma_rows<DP>(tmem + ROWS, base + F::TILE, k);
+                        ptx::mma_commit(ptx::smem_u32(&ctl->sfull[1]));
                     }
                 }
                 __syncwarp();
             }
-            if (ok) {
-                release(vs);
-                if (more) release(ks);
+            if (leader) {
+                ptx::mma_commit(ptx::smem_u32(&ctl->empty[vs]));
+                if (more) ptx::mma_commit(ptx::smem_u32(&ctl->empty[ks]));
             }
+            __syncwarp();
         }
         if (leader) ptx::mma_commit(ptx::smem_u32(&ctl->drain));
         __syncwarp();
@@ -508,80 +542,88 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             if (leader) ptx::mma_commit(ptx::smem_u32(&bar));
             __syncwarp();
         };
-        // The operands of step j: slots of both rings, whose phases end with theirs, and the rows
-        // of the tile that a sum runs over.  They are waited for ahead, so that the products of
-        // a step follow one another.
+        // The operands of a step: slots of both rings, whose phases end with theirs, and the rows
+        // of the tile that a sum runs over
+        const Waits waits{abort_flag, p.status, p.wait_limit};
+        const uint32_t afull = ptx::smem_u32(&ctl->afull[0]), bfull = ptx::smem_u32(&ctl->bfull[0]);
+        const uint32_t aempty = ptx::smem_u32(&ctl->aempty[0]), bempty = ptx::smem_u32(&ctl->bempty[0]);
+        const uint32_t pfull = ptx::smem_u32(&ctl->pfull), dsfull = ptx::smem_u32(&ctl->dsfull);
+        const uint32_t sfull = ptx::smem_u32(&ctl->sfull), dpfull = ptx::smem_u32(&ctl->dpfull);
         int sa = 0, sb = 0, at = KEYS ? tile.tile : 0;
         uint32_t pa = 0, pb = 0;
-        auto rows = [&] { return at == last ? tail : ROWS; };
-        auto have_a = [&] {
-            if (!wait(ctl->afull[sa], pa)) return false;
-            if (rows() % 16 != 0) clear_rows<DP>(ring_a + sa * F::TILE, rows(), lane);
-            return true;
+        int rows = at == last ? tail : ROWS;
+        auto clean_a = [&] {
+            if (rows % 16 != 0) clear_rows<DP>(ring_a + sa * F::TILE, rows, lane);
         };
-        auto have_b = [&] {
-            if (!wait(ctl->bfull[sb], pb)) return false;
-            if (KEYS && rows() % 16 != 0) clear_rows<DP>(ring_b + sb * F::TILE, rows(), lane);
-            return true;
+        auto clean_b = [&] {
+            if (KEYS && rows % 16 != 0) clear_rows<DP>(ring_b + sb * F::TILE, rows, lane);
         };
-        auto next = [&] {
-            at = at == last ? tile.tile : at + 1;
-            if (++sa == F::SA) { sa = 0; pa ^= 1; }
-            if (++sb == F::SB) { sb = 0; pb ^= 1; }
-        };
-        auto score = [&] {
-            mma_rows<DP>(tmem + S, fixed, ra + sa * F::TILE);
-            ptx::mma_commit(ptx::smem_u32(&ctl->sfull));
-        };
-        auto slope = [&](int j) {
-            mma_rows<DP>(tmem + dp_at(j), fixed + F::TILE, rb + sb * F::TILE);
-            ptx::mma_commit(ptx::smem_u32(&ctl->dpfull));
-            if (!KEYS) ptx::mma_commit(ptx::smem_u32(&ctl->bempty[sb]));
-        };
-        bool ok = wait(ctl->fixed, 0) && have_a() && have_b();
+        bool ok = wait(ctl->fixed, 0) && waits.two(afull, 0, bfull, 0);
         if (ok) {
+            clean_a();
+            clean_b();
             ptx::tc_fence_after();
             if (leader) {
-                score();
-                slope(0);
+                mma_rows<DP>(tmem + S, fixed, ra);
+                ptx::mma_commit(sfull);
+                mma_rows<DP>(tmem + DPC, fixed + F::TILE, rb);
+                ptx::mma_commit(dpfull);
+                if (!KEYS) ptx::mma_commit(bempty);
             }
             __syncwarp();
         }
         for (int j = 0; j < steps && ok; ++j) {
             const bool more = j + 1 < steps;
-            const uint32_t a = ra + sa * F::TILE, b = rb + sb * F::TILE;
-            const int oa = sa, ob = sb, sums = (rows() + 15) / 16;
-            next();
-            if (more && !have_a()) break;
+            const int oa = sa, ob = sb, sums = (rows + 15) / 16;
+            const uint32_t a = ra + oa * F::TILE, b = rb + ob * F::TILE;
+            at = at == last ? tile.tile : at + 1;
+            rows = at == last ? tail : ROWS;
+            if (++sa == F::SA) { sa = 0; pa ^= 1; }
+            if (++sb == F::SB) { sb = 0; pb ^= 1; }
+            const uint32_t a1 = ra + sa * F::TILE, b1 = rb + sb * F::TILE;
             if (KEYS) {
-                ok = wait(ctl->pfull, j & 1);
+                ok = more ? waits.two(pfull, j & 1, afull + 8 * sa, pa) : waits.one(pfull, j & 1);
                 if (!ok) break;
+                if (more) clean_a();
                 ptx::tc_fence_after();
                 if (leader) {
                     mma_sum<DP, COLS, COLS>(tmem + SUM_B, tmem + S, b, sums, j > 0);
-                    ptx::mma_commit(ptx::smem_u32(&ctl->bempty[ob]));
-                    if (more) score();                              // over the P that the product in front of it has read by then
+                    ptx::mma_commit(bempty + 8 * ob);
+                    if (more) {                                     // over the P that the product in front of it has read by then
+                        mma_rows<DP>(tmem + S, fixed, a1);
+                        ptx::mma_commit(sfull);
+                    }
                 }
                 __syncwarp();
-                if (more && !have_b()) break;
-            } else if (more) {
-                if (!have_b()) break;
-                ok = wait(ctl->pfull, j & 1);
+                ok = more ? waits.two(dsfull, j & 1, bfull + 8 * sb, pb) : waits.one(dsfull, j & 1);
                 if (!ok) break;
-                ptx::tc_fence_after();
-                if (leader) {
-                    score();
-                    slope(j + 1);
+                if (more) clean_b();
+            } else {
+                if (more) {
+                    ok = waits.three(pfull, j & 1, afull + 8 * sa, pa, bfull + 8 * sb, pb);
+                    if (!ok) break;
+                    clean_a();
+                    ptx::tc_fence_after();
+                    if (leader) {
+                        mma_rows<DP>(tmem + S, fixed, a1);
+                        ptx::mma_commit(sfull);
+                        mma_rows<DP>(tmem + dp_at(j + 1), fixed + F::TILE, b1);
+                        ptx::mma_commit(dpfull);
+                        ptx::mma_commit(bempty + 8 * sb);
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
+                ok = waits.one(dsfull, j & 1);
+                if (!ok) break;
             }
-            ok = wait(ctl->dsfull, j & 1);
-            if (!ok) break;
             ptx::tc_fence_after();
             if (leader) {
                 mma_sum<DP, COLS, COLS>(tmem + SUM_A, tmem + dp_at(j), a, sums, j > 0);
-                ptx::mma_commit(ptx::smem_u32(&ctl->aempty[oa]));
-                if (KEYS && more) slope(j + 1);
+                ptx::mma_commit(aempty + 8 * oa);
+                if (KEYS && more) {
+                    mma_rows<DP>(tmem + DPC, fixed + F::TILE, b1);
+                    ptx::mma_commit(dpfull);
+                }
                 if (!more) ptx::mma_commit(ptx::smem_u32(&ctl->done));
             }
             __syncwarp();
