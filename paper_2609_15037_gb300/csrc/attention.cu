@@ -72,20 +72,20 @@ template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t 
 }
 
 // The same tile as the operand whose rows are summed over: D (128 x DP) (+)= A B with A in
-// tensor memory, RUN entries of K in columns a .. a + RUN / 2 - 1, RUN more from a + PITCH on
-// and so on; the first 16 `steps` rows of B.
-template <int DP, int RUN, int PITCH>
+// tensor memory, 16 entries of K in columns a .. a + 7, 16 more from a + PITCH on and so on; the
+// 16 rows of B from FROM on, up to 16 `steps` and 16 TO of all.
+template <int DP, int PITCH, int FROM = 0, int TO = ROWS / 16>
 __device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint32_t b, int steps, bool add) {
     constexpr uint32_t idesc = ptx::idesc_bf16(128, DP, 0, 1);
     const auto one = [&](int k, uint32_t acc) {
-        ptx::mma_f16_ta(d, a + k * 16 / RUN * PITCH + k * 16 % RUN / 2, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, acc);
+        ptx::mma_f16_ta(d, a + k * PITCH, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, acc);
     };
-    one(0, add);
-    if (steps == ROWS / 16) {                                      // a test for each would take as long as a product
+    if (steps >= TO) {                                             // a test for each would take as long as a product
+        one(FROM, add);
 #pragma unroll
-        for (int k = 1; k < ROWS / 16; ++k) one(k, 1);
+        for (int k = FROM + 1; k < TO; ++k) one(k, 1);
     } else {
-        for (int k = 1; k < steps; ++k) one(k, 1);
+        for (int k = FROM; k < steps; ++k) one(k, add || k > FROM);
     }
 }
 
@@ -128,6 +128,27 @@ struct ForwardParams {
     long long wait_limit;
 };
 
+// 32 rows of a warp (one a lane) of CHUNKS 16-byte pieces from registers to rows of the
+// output `pitch` bytes apart, through shared memory of the warp's own, so that a row's pieces leave
+// beside one another; `rows` of them exist, and `bytes` of each.
+template <int CHUNKS>
+__device__ __forceinline__ void store_rows(uint8_t* stage, const uint4 (&w)[CHUNKS], uint8_t* to, long long pitch, int rows, int bytes,
+                                           int lane) {
+    constexpr int MASK = CHUNKS < 8 ? CHUNKS - 1 : 7, PER = 32 / CHUNKS;
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
+        *reinterpret_cast<uint4*>(stage + (lane * CHUNKS + (c ^ (lane * CHUNKS / 8 & MASK))) * 16) = w[c];
+    __syncwarp();
+    const int c = lane % CHUNKS;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) {
+        const int r = i * PER + lane / CHUNKS;
+        const uint4 v = *reinterpret_cast<const uint4*>(stage + (r * CHUNKS + (c ^ (r * CHUNKS / 8 & MASK))) * 16);
+        if (r < rows && c * 16 < bytes) *reinterpret_cast<uint4*>(to + r * pitch + c * 16) = v;
+    }
+    __syncwarp();
+}
+
 // Waits of the warp that issues products.  Several at once: each costs some 100 clocks, and
 // the queue of products holds about 200 clocks of them.
 struct Waits {
@@ -165,7 +186,14 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     Ctl* ctl = reinterpret_cast<Ctl*>(ring + F::SLOTS * F::TILE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort_flag = &ctl->abort;
-    if (threadIdx.x == 0) {
+    const int head = blockIdx.x % p.heads, kv = head / p.group;
+    auto fill = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
+        const uint32_t b = ptx::smem_u32(&bar);
+        ptx::mbar_arrive_expect_tx(b, F::TILE);
+        for (int c = 0; c < DP / 64; ++c) ptx::tma_load_3d(ptx::smem_u32(to) + c * PANEL, map, b, c * 64, h, row);
+    };
+    if (threadIdx.x == 8 * 32) {
+        // the thread that copies starts what the first products need beside the others' set-up
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl->qfull[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl->sfull[i]), 1);
@@ -178,8 +206,15 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
         }
         ptx::mbar_init(ptx::smem_u32(&ctl->drain), 1);
         ctl->abort = 0;
-        ctl->filled = 0;
+        ctl->filled = 2;
         ptx::fence_barrier_init();
+        ptx::fence_proxy_async_smem();
+        pdl_begin();
+        const AttentionTile t = p.pairs[blockIdx.x / p.heads];
+        fill(smem, &p.q, ctl->qfull[0], head, t.begin + 2 * t.tile * ROWS);
+        fill(ring, &p.k, ctl->full[0], kv, t.begin);
+        if ((2 * t.tile + 1) * ROWS < t.length) fill(smem + F::TILE, &p.q, ctl->qfull[1], head, t.begin + (2 * t.tile + 1) * ROWS);
+        fill(ring + F::TILE, &p.v, ctl->full[1], kv, t.begin);
     }
     if (warp == 9) {
         ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
@@ -191,30 +226,22 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     const uint32_t tmem = ctl->tmem;
     pdl_begin();
     const AttentionTile pair = p.pairs[blockIdx.x / p.heads];
-    const int head = blockIdx.x % p.heads, kv = head / p.group;
     const int q0 = 2 * pair.tile;                                  // the first of the two tiles
     const bool second = (q0 + 1) * ROWS < pair.length;
-    const int tiles = q0 + 1 + second;                                // of keys; tile i sees q0 + 1 + i
+    const int tiles = q0 + 1 + second;                             // of keys; tile i sees q0 + 1 + i
     auto wait = [&](uint64_t& bar, uint32_t parity) {
         return ptx::mbar_wait_warp(ptx::smem_u32(&bar), parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
     };
 
     if (warp == 8) {
         if (lane == 0) {
-            auto fill = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
-                const uint32_t b = ptx::smem_u32(&bar);
-                ptx::mbar_arrive_expect_tx(b, F::TILE);
-                for (int c = 0; c < DP / 64; ++c) ptx::tma_load_3d(ptx::smem_u32(to) + c * PANEL, map, b, c * 64, h, row);
-            };
-            fill(smem, &p.q, ctl->qfull[0], head, pair.begin + q0 * ROWS);
-            int n = 0;
+            int n = 2;
             for (; n < 2 * tiles; ++n) {
                 const int slot = n % F::SLOTS;
                 if (n >= F::SLOTS && !ptx::mbar_wait(ptx::smem_u32(&ctl->empty[slot]), (n / F::SLOTS - 1) & 1, abort_flag, p.status,
                                                      MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
                     break;
                 fill(ring + slot * F::TILE, n & 1 ? &p.v : &p.k, ctl->full[slot], kv, pair.begin + n / 2 * ROWS);
-                if (n == 0 && second) fill(smem + F::TILE, &p.q, ctl->qfull[1], head, pair.begin + (q0 + 1) * ROWS);
             }
             ctl->filled = n;
         }
@@ -260,7 +287,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             if (one) {
                 ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, ROWS, 0>(tmem + 256, tmem, v, steps, j > 0);
+                    mma_sum<DP, 8>(tmem + 256, tmem, v, steps, j > 0);
                     if (j == q0) {
                         ptx::mma_commit(ptx::smem_u32(&ctl->ofull[0]));
                     } else {
@@ -275,7 +302,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             if (second) {
                 ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, ROWS, 0>(tmem + 256 + DP, tmem + ROWS, v, steps, j > 0);
+                    mma_sum<DP, 8>(tmem + 256 + DP, tmem + ROWS, v, steps, j > 0);
                     if (!more) {
                         ptx::mma_commit(ptx::smem_u32(&ctl->ofull[1]));
                     } else {
@@ -364,28 +391,32 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
         if (ok) {
             ptx::tc_fence_after();
             const float inv = 1.0f / sum;
-            const bool real = row < pair.length;
             const long long token = pair.begin + row;
-            if (real) p.lse[static_cast<long long>(head) * p.tokens + token] = fmaf(ref, p.scale, logf(sum));
-            bf16* out = p.out + (token * p.heads + head) * p.dim;
-            bf16* rest = p.rest == nullptr ? nullptr : p.rest + (token * p.heads + head) * p.dim;
+            if (row < pair.length) p.lse[static_cast<long long>(head) * p.tokens + token] = fmaf(ref, p.scale, logf(sum));
+            // Q's tile is no longer read
+            uint8_t* const stage = smem + i * F::TILE + quad * (F::TILE / 4);
+            const long long pitch = static_cast<long long>(p.heads) * p.dim * 2, first = ((token - lane) * p.heads + head) * p.dim;
+            const int rows = pair.length - (row - lane);
 #pragma unroll
             for (int c = 0; c < DP; c += 32) {
                 uint32_t o[32];
                 ptx::tmem_ld32(ot + c, o);
+                uint4 w[4], l[4];
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    if (!real || c + e >= p.dim) continue;
-                    uint32_t w[4], l[4];
+                for (int e = 0; e < 4; ++e) {
+                    uint32_t a[4], b[4];
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        const float a = __uint_as_float(o[e + 2 * x]) * inv, b = __uint_as_float(o[e + 2 * x + 1]) * inv;
-                        w[x] = pack2(a, b);
-                        l[x] = pack2(a - __uint_as_float(w[x] << 16), b - __uint_as_float(w[x] & 0xFFFF0000u));
+                        const float y = __uint_as_float(o[8 * e + 2 * x]) * inv, z = __uint_as_float(o[8 * e + 2 * x + 1]) * inv;
+                        a[x] = pack2(y, z);
+                        b[x] = pack2(y - __uint_as_float(a[x] << 16), z - __uint_as_float(a[x] & 0xFFFF0000u));
                     }
-                    *reinterpret_cast<uint4*>(out + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
-                    if (rest != nullptr) *reinterpret_cast<uint4*>(rest + c + e) = make_uint4(l[0], l[1], l[2], l[3]);
+                    w[e] = make_uint4(a[0], a[1], a[2], a[3]);
+                    l[e] = make_uint4(b[0], b[1], b[2], b[3]);
                 }
+                const int bytes = (p.dim - c) * 2;
+                store_rows(stage, w, reinterpret_cast<uint8_t*>(p.out + first + c), pitch, rows, bytes, lane);
+                if (p.rest != nullptr) store_rows(stage, l, reinterpret_cast<uint8_t*>(p.rest + first + c), pitch, rows, bytes, lane);
             }
         }
     }
@@ -393,7 +424,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) {      // a wait that ran out: no copy stays in flight
         wait_drain(ptx::smem_u32(&ctl->qfull[0]), 0);
-        if (second && ctl->filled > 0) wait_drain(ptx::smem_u32(&ctl->qfull[1]), 0);
+        if (second) wait_drain(ptx::smem_u32(&ctl->qfull[1]), 0);
         for (int n = max(0, ctl->filled - F::SLOTS); n < ctl->filled; ++n)
             wait_drain(ptx::smem_u32(&ctl->full[n % F::SLOTS]), (n / F::SLOTS) & 1);
     }
@@ -412,8 +443,9 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
 // stay in tensor memory and dV += P^T dO, dK += dS^T Q take them from there.  Otherwise it
 // takes 128 queries of a head and goes through their keys: dQ += dS K.
 //
-// Sixteen warps turn S into P and dP = dO V^T into dS (32 columns of a row a thread), one
-// issues products, one copies.  The tile that is used twice in a step (first in S, last in a
+// Sixteen warps turn S into P and dP = dO V^T into dS (a thread has 16 columns of either half
+// of a row, and the sums take the first halves while the second are worked out), one issues
+// products, one copies.  The tile that is used twice in a step (first in S, last in a
 // sum) has three slots, the other two.
 // ---------------------------------------------------------------------------
 template <int DP> struct Backward {
@@ -422,7 +454,7 @@ template <int DP> struct Backward {
     static constexpr int STATS = 2 * 2 * ROWS * 4;                 // lse and delta of two steps
     static constexpr int CTL = 256;
     static constexpr int SMEM = (2 + SA + SB) * TILE + STATS + CTL;
-    static constexpr int WARPS = 16, COLS = ROWS * 4 / WARPS;      // that turn S into dS; columns of a thread
+    static constexpr int WARPS = 16;                               // that turn S into dS
     static constexpr int THREADS = (WARPS + 2) * 32;
     static_assert(SMEM <= 227 * 1024, "shared memory");
 };
@@ -441,7 +473,7 @@ struct BackwardParams {
 };
 
 struct BackwardCtl {
-    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull, dpfull, dsfull, stats[2], done, drain;
+    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull[2], dpfull, dsfull[2], stats[2], done, drain;
     uint32_t tmem;
     int abort;
     int filled[2];
@@ -450,7 +482,7 @@ struct BackwardCtl {
 template <int DP, bool KEYS>
 __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(const __grid_constant__ BackwardParams p) {
     using F = Backward<DP>;
-    constexpr int WARPS = F::WARPS, COLS = F::COLS;
+    constexpr int WARPS = F::WARPS;
     static_assert(sizeof(BackwardCtl) <= F::CTL, "the barriers fit");
     extern __shared__ __align__(1024) uint8_t smem[];              // there is no room to align it here
     uint8_t* const ring_a = smem + 2 * F::TILE;
@@ -463,12 +495,30 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         if (threadIdx.x == 0) atomicCAS(p.status, 0, MOARA_ERR_ALIGN);
         return;
     }
-    if (threadIdx.x == 0) {
+    const int owners = KEYS ? p.kv_heads : p.heads, owner = blockIdx.x % owners, kv = KEYS ? owner : owner / p.group;
+    // copies of step j, whose tile is `at` of head `h`
+    auto copy = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
+        for (int c = 0; c < DP / 64; ++c)
+            ptx::tma_load_3d(ptx::smem_u32(to) + c * PANEL, map, ptx::smem_u32(&bar), c * 64, h, row);
+    };
+    auto copy_a = [&](const AttentionTile& t, int j, int h, int at) {
+        const int slot = j % F::SA;
+        ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->afull[slot]), F::TILE);
+        copy(ring_a + slot * F::TILE, &p.a, ctl->afull[slot], h, t.begin + at * ROWS);
+    };
+    auto copy_b = [&](const AttentionTile& t, int j, int h, int at) {
+        const int slot = j % F::SB;
+        ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->bfull[slot]), F::TILE);
+        copy(ring_b + slot * F::TILE, &p.b, ctl->bfull[slot], h, t.begin + at * ROWS);
+    };
+    if (threadIdx.x == WARPS * 32) {
+        // the thread that copies starts what the first step needs beside the others' set-up
         for (uint64_t* b : {&ctl->fixed, &ctl->sfull, &ctl->dpfull, &ctl->done, &ctl->drain}) ptx::mbar_init(ptx::smem_u32(b), 1);
-        ptx::mbar_init(ptx::smem_u32(&ctl->pfull), WARPS);
-        ptx::mbar_init(ptx::smem_u32(&ctl->dsfull), WARPS);
-        ptx::mbar_init(ptx::smem_u32(&ctl->stats[0]), WARPS);
-        ptx::mbar_init(ptx::smem_u32(&ctl->stats[1]), WARPS);
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctl->pfull[i]), WARPS);
+            ptx::mbar_init(ptx::smem_u32(&ctl->dsfull[i]), WARPS);
+            ptx::mbar_init(ptx::smem_u32(&ctl->stats[i]), WARPS);
+        }
         for (int i = 0; i < F::SA; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl->afull[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl->aempty[i]), 1);
@@ -478,8 +528,16 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             ptx::mbar_init(ptx::smem_u32(&ctl->bempty[i]), 1);
         }
         ctl->abort = 0;
-        ctl->filled[0] = ctl->filled[1] = 0;
+        ctl->filled[0] = ctl->filled[1] = 1;
         ptx::fence_barrier_init();
+        ptx::fence_proxy_async_smem();
+        pdl_begin();
+        const AttentionTile t = p.tiles[blockIdx.x / owners];
+        ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->fixed), 2 * F::TILE);
+        copy(smem, &p.fixed_a, ctl->fixed, owner, t.begin + t.tile * ROWS);
+        copy_a(t, 0, KEYS ? kv * p.group : kv, KEYS ? t.tile : 0);
+        copy(smem + F::TILE, &p.fixed_b, ctl->fixed, owner, t.begin + t.tile * ROWS);
+        copy_b(t, 0, KEYS ? kv * p.group : kv, KEYS ? t.tile : 0);
     }
     if (warp == WARPS + 1) {
         ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
@@ -490,16 +548,11 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
     ptx::tc_fence_after();
     const uint32_t tmem = ctl->tmem;
     pdl_begin();
-    const int owners = KEYS ? p.kv_heads : p.heads;
     const AttentionTile tile = p.tiles[blockIdx.x / owners];
-    const int owner = blockIdx.x % owners, kv = KEYS ? owner : owner / p.group;
     const int last = (tile.length - 1) / ROWS;                     // tile of the sequence
     const int per = KEYS ? last - tile.tile + 1 : tile.tile + 1;   // tiles that are gone through, per head
     const int steps = KEYS ? per * p.group : per;
     const int tail = tile.length - last * ROWS;                    // rows of the last tile
-    // of step j: head of the streamed operands, their tile
-    auto head_of = [&](int j) { return KEYS ? kv * p.group + j / per : kv; };
-    auto tile_of = [&](int j) { return KEYS ? tile.tile + j % per : j; };
     auto wait = [&](uint64_t& bar, uint32_t parity) {
         return ptx::mbar_wait_warp(ptx::smem_u32(&bar), parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
     };
@@ -509,27 +562,19 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
 
     if (warp == WARPS) {
         if (lane == 0) {
-            auto copy = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
-                for (int c = 0; c < DP / 64; ++c)
-                    ptx::tma_load_3d(ptx::smem_u32(to) + c * PANEL, map, ptx::smem_u32(&bar), c * 64, h, row);
-            };
-            ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->fixed), 2 * F::TILE);
-            copy(smem, &p.fixed_a, ctl->fixed, owner, tile.begin + tile.tile * ROWS);
-            copy(smem + F::TILE, &p.fixed_b, ctl->fixed, owner, tile.begin + tile.tile * ROWS);
-            int na = 0, nb = 0;
+            int na = 1, nb = 1, at = KEYS ? tile.tile : 0, h = KEYS ? kv * p.group : kv;
             auto room = [&](uint64_t& bar, int n, int slots) {
                 return n < slots || ptx::mbar_wait(ptx::smem_u32(&bar), (n / slots - 1) & 1, abort_flag, p.status,
                                                    MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
             };
-            for (int j = 0; j < steps; ++j) {
-                const int row = tile.begin + tile_of(j) * ROWS, h = head_of(j), sa = j % F::SA, sb = j % F::SB;
-                if (!room(ctl->aempty[sa], j, F::SA)) break;
-                ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->afull[sa]), F::TILE);
-                copy(ring_a + sa * F::TILE, &p.a, ctl->afull[sa], h, row);
+            for (int j = 1; j < steps; ++j) {
+                h += KEYS && at == last;
+                at = at == last ? tile.tile : at + 1;
+                if (!room(ctl->aempty[j % F::SA], j, F::SA)) break;
+                copy_a(tile, j, h, at);
                 ++na;
-                if (!room(ctl->bempty[sb], j, F::SB)) break;
-                ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->bfull[sb]), F::TILE);
-                copy(ring_b + sb * F::TILE, &p.b, ctl->bfull[sb], h, row);
+                if (!room(ctl->bempty[j % F::SB], j, F::SB)) break;
+                copy_b(tile, j, h, at);
                 ++nb;
             }
             ctl->filled[0] = na;
@@ -547,7 +592,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         const Waits waits{abort_flag, p.status, p.wait_limit};
         const uint32_t afull = ptx::smem_u32(&ctl->afull[0]), bfull = ptx::smem_u32(&ctl->bfull[0]);
         const uint32_t aempty = ptx::smem_u32(&ctl->aempty[0]), bempty = ptx::smem_u32(&ctl->bempty[0]);
-        const uint32_t pfull = ptx::smem_u32(&ctl->pfull), dsfull = ptx::smem_u32(&ctl->dsfull);
+        const uint32_t pfull = ptx::smem_u32(&ctl->pfull[0]), dsfull = ptx::smem_u32(&ctl->dsfull[0]);
         const uint32_t sfull = ptx::smem_u32(&ctl->sfull), dpfull = ptx::smem_u32(&ctl->dpfull);
         int sa = 0, sb = 0, at = KEYS ? tile.tile : 0;
         uint32_t pa = 0, pb = 0;
@@ -586,8 +631,13 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
                 if (!ok) break;
                 if (more) clean_a();
                 ptx::tc_fence_after();
+                if (leader) mma_sum<DP, 16, 0, 4>(tmem + SUM_B, tmem + S, b, sums, j > 0);
+                __syncwarp();
+                ok = waits.one(pfull + 8, j & 1);
+                if (!ok) break;
+                ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, COLS, COLS>(tmem + SUM_B, tmem + S, b, sums, j > 0);
+                    mma_sum<DP, 16, 4, 8>(tmem + SUM_B, tmem + S, b, sums, true);
                     ptx::mma_commit(bempty + 8 * ob);
                     if (more) {                                     // over the P that the product in front of it has read by then
                         mma_rows<DP>(tmem + S, fixed, a1);
@@ -617,8 +667,13 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
                 if (!ok) break;
             }
             ptx::tc_fence_after();
+            if (leader) mma_sum<DP, 16, 0, 4>(tmem + SUM_A, tmem + dp_at(j), a, sums, j > 0);
+            __syncwarp();
+            ok = waits.one(dsfull + 8, j & 1);
+            if (!ok) break;
+            ptx::tc_fence_after();
             if (leader) {
-                mma_sum<DP, COLS, COLS>(tmem + SUM_A, tmem + dp_at(j), a, sums, j > 0);
+                mma_sum<DP, 16, 4, 8>(tmem + SUM_A, tmem + dp_at(j), a, sums, true);
                 ptx::mma_commit(aempty + 8 * oa);
                 if (KEYS && more) {
                     mma_rows<DP>(tmem + DPC, fixed + F::TILE, b1);
@@ -631,7 +686,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         commit(ctl->drain);
         wait_drain(ptx::smem_u32(&ctl->drain), 0);
     } else {
-        const int part = warp >> 2, quad = warp & 3, r = quad * 32 + lane, c0 = part * COLS;
+        const int part = warp >> 2, quad = warp & 3, r = quad * 32 + lane, c0 = part * 16;    // columns c0 .. + 15 and 64 more
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const int row = tile.tile * ROWS + r;                       // in the sequence
         const bool real = row < tile.length;
@@ -672,75 +727,74 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
                 ok = wait(ctl->stats[j & 1], (j >> 1) & 1);
                 if (!ok) break;
             }
-            // which columns of this thread count: from `from` on (KEYS) up to `to`
-            int from = 0, to = COLS;
+            // which columns of the row count: from `from` on (KEYS) up to `to`
+            int from = 0, to = ROWS;
             if (KEYS) {
-                if (at == tile.tile) from = r - c0;
-                if (at == last) to = tail - c0;
+                if (at == tile.tile) from = r;
+                if (at == last) to = tail;
             } else if (j == tile.tile) {
-                to = r + 1 - c0;
+                to = r + 1;
             }
-            const bool all = __all_sync(0xffffffffu, from <= 0 && to >= COLS);
-            ok = wait(ctl->sfull, j & 1);
-            if (!ok) break;
-            ptx::tc_fence_after();
-            uint32_t s[COLS];
-            ptx::tmem_ld32(lanes + S + c0, s);
-            if (!KEYS) {
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull));
-            }
-            float x[COLS];
+            const bool all = __all_sync(0xffffffffu, from == 0 && to == ROWS);
+            auto mask = [&](float (&x)[16], int c) {
 #pragma unroll
-            for (int c = 0; c < COLS; c += 4) {
-                const ulonglong2 l = KEYS ? sl[c / 4] : make_ulonglong2(lse, lse);
+                for (int e = 0; e < 16; ++e) x[e] = c + e >= from && c + e < to ? x[e] : 0.0f;
+            };
+            auto put = [&](uint32_t column, const float (&x)[16], uint64_t& bar) {
+                uint32_t w[8];
 #pragma unroll
-                for (int e = 0; e < 4; e += 2) {
-                    split(fma2(f32x2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), scale, e == 0 ? l.x : l.y), x[c + e],
-                          x[c + e + 1]);
-                    x[c + e] = ex2(x[c + e]);
-                    x[c + e + 1] = ex2(x[c + e + 1]);
-                }
-            }
-            if (!all) {
-#pragma unroll
-                for (int c = 0; c < COLS; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
-            }
-            uint32_t w[COLS / 2];
-            if (KEYS) {
-#pragma unroll
-                for (int c = 0; c < COLS / 2; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
-                ptx::tmem_st16(lanes + S + c0, w);
+                for (int e = 0; e < 8; ++e) w[e] = pack2(x[2 * e], x[2 * e + 1]);
+                ptx::tmem_st8(lanes + column, w);
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull));
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar));
+            };
+            ok = wait(ctl->sfull, j & 1);
+            if (!ok) break;
+            ptx::tc_fence_after();
+            uint32_t s[32];
+            ptx::tmem_ld16x2(lanes + S + c0, lanes + S + 64 + c0, s);
+            if (!KEYS) {
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull[0]));
+            }
+            float x[2][16];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int c = 0; c < 16; c += 4) {
+                    const ulonglong2 l = KEYS ? sl[16 * h + c / 4] : make_ulonglong2(lse, lse);
+#pragma unroll
+                    for (int e = c; e < c + 4; e += 2) {
+                        split(fma2(f32x2(__uint_as_float(s[16 * h + e]), __uint_as_float(s[16 * h + e + 1])), scale, e == c ? l.x : l.y),
+                              x[h][e], x[h][e + 1]);
+                        x[h][e] = ex2(x[h][e]);
+                        x[h][e + 1] = ex2(x[h][e + 1]);
+                    }
+                }
+                if (!all) mask(x[h], 64 * h + c0);
+                if (KEYS) put(S + 64 * h + c0, x[h], ctl->pfull[h]);
             }
             ok = wait(ctl->dpfull, j & 1);
             if (!ok) break;
             ptx::tc_fence_after();
-            ptx::tmem_ld32(lanes + dp_at(j) + c0, s);
+            ptx::tmem_ld16x2(lanes + dp_at(j) + c0, lanes + dp_at(j) + 64 + c0, s);
 #pragma unroll
-            for (int c = 0; c < COLS; c += 4) {
-                const ulonglong2 d = KEYS ? sd[c / 4] : make_ulonglong2(delta, delta);
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int e = 0; e < 4; e += 2)
-                    split(mul2(f32x2(x[c + e], x[c + e + 1]),
-                               add2(f32x2(__uint_as_float(s[c + e]), __uint_as_float(s[c + e + 1])), e == 0 ? d.x : d.y)),
-                          x[c + e], x[c + e + 1]);
+                for (int c = 0; c < 16; c += 4) {
+                    const ulonglong2 d = KEYS ? sd[16 * h + c / 4] : make_ulonglong2(delta, delta);
+#pragma unroll
+                    for (int e = c; e < c + 4; e += 2)
+                        split(mul2(f32x2(x[h][e], x[h][e + 1]),
+                                   add2(f32x2(__uint_as_float(s[16 * h + e]), __uint_as_float(s[16 * h + e + 1])), e == c ? d.x : d.y)),
+                              x[h][e], x[h][e + 1]);
+                }
+                if (!all) mask(x[h], 64 * h + c0);                  // what is not counted may be infinite or NaN
+                put(dp_at(j) + 64 * h + c0, x[h], ctl->dsfull[h]);
             }
-            if (!all) {                                             // what is not counted may be infinite or NaN
-#pragma unroll
-                for (int c = 0; c < COLS; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
-            }
-#pragma unroll
-            for (int c = 0; c < COLS / 2; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
-            ptx::tmem_st16(lanes + dp_at(j) + c0, w);
-            ptx::tmem_st_wait();
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->dsfull));
             if (KEYS) follow(at, head);
         }
         if (ok) ok = wait(ctl->done, 0);
@@ -749,24 +803,26 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             // KEYS: the first half of the threads has dV, the second dK; otherwise all have dQ
             constexpr int PARTS = KEYS ? WARPS / 8 : WARPS / 4, WIDTH = DP / PARTS;
             const bool first = KEYS && part < PARTS;
-            const long long at = (token * owners + owner) * p.dim;
-            bf16* out = (first ? p.out_b : p.out_a) + at;
             const uint32_t src = lanes + (first ? SUM_B : SUM_A);
             const float factor = first ? 1.0f : p.scale;
             const int o0 = part % PARTS * WIDTH;
+            const long long pitch = static_cast<long long>(owners) * p.dim * 2;
+            bf16* const out = (first ? p.out_b : p.out_a) + ((token - lane) * owners + owner) * p.dim + o0;
+            // the fixed tiles are no longer read
+            uint8_t* const stage = smem + warp * (2 * F::TILE / WARPS);
+            uint4 w[WIDTH / 8];
 #pragma unroll
             for (int c = 0; c < WIDTH; c += 16) {
                 float o[16];
                 ptx::tmem_ld16(src + o0 + c, o);
 #pragma unroll
-                for (int e = 0; e < 16; e += 8) {
-                    if (!real || o0 + c + e >= p.dim) continue;
-                    uint32_t w[4];
-#pragma unroll
-                    for (int y = 0; y < 4; ++y) w[y] = pack2(o[e + 2 * y] * factor, o[e + 2 * y + 1] * factor);
-                    *reinterpret_cast<uint4*>(out + o0 + c + e) = make_uint4(w[0], w[1], w[2], w[3]);
-                }
+                for (int e = 0; e < 2; ++e)
+                    w[c / 8 + e] = make_uint4(pack2(o[8 * e] * factor, o[8 * e + 1] * factor),
+                                              pack2(o[8 * e + 2] * factor, o[8 * e + 3] * factor),
+                                              pack2(o[8 * e + 4] * factor, o[8 * e + 5] * factor),
+                                              pack2(o[8 * e + 6] * factor, o[8 * e + 7] * factor));
             }
+            store_rows(stage, w, reinterpret_cast<uint8_t*>(out), pitch, tile.length - (row - lane), (p.dim - o0) * 2, lane);
         }
     }
     ptx::tc_fence_before();
