@@ -596,6 +596,8 @@ typedef struct moara_sequences {
     int tokens;             /* sum of the lengths                                   */
     int n_tiles;            /* tiles of 128 tokens                                  */
     int n_pairs;            /* of 256                                               */
+    int longest;            /* tiles of the longest sequence                        */
+    int64_t work;           /* pairs of a query tile and a key tile that it sees    */
 } moara_sequences;
 int moara_sequences_bytes(int count, const int* lengths, size_t* out);
 int moara_sequences_init(int count, const int* lengths, void* tiles, size_t bytes, moara_sequences* out);

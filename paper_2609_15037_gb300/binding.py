@@ -59,7 +59,8 @@ class moara_hparams(ctypes.Structure):
 
 
 class moara_sequences(ctypes.Structure):
-    _fields_ = [("tiles", ctypes.c_void_p), ("tokens", ctypes.c_int), ("n_tiles", ctypes.c_int), ("n_pairs", ctypes.c_int)]
+    _fields_ = [("tiles", ctypes.c_void_p), ("tokens", ctypes.c_int), ("n_tiles", ctypes.c_int), ("n_pairs", ctypes.c_int),
+                ("longest", ctypes.c_int), ("work", ctypes.c_int64)]
 
 
 class moara_module_desc(ctypes.Structure):

@@ -72,20 +72,20 @@ template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t 
 }
 
 // The same tile as the operand whose rows are summed over: D (128 x DP) (+)= A B with A in
-// tensor memory, 16 entries of K in columns a .. a + 7, 16 more from a + PITCH on and so on; the
-// 16 rows of B from FROM on, up to 16 `steps` and 16 TO of all.
-template <int DP, int PITCH, int FROM = 0, int TO = ROWS / 16>
+// tensor memory, RUN entries of K in columns a .. a + RUN / 2 - 1, RUN more from a + PITCH on
+// and so on; the first 16 `steps` rows of B.
+template <int DP, int RUN, int PITCH>
 __device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint32_t b, int steps, bool add) {
     constexpr uint32_t idesc = ptx::idesc_bf16(128, DP, 0, 1);
     const auto one = [&](int k, uint32_t acc) {
-        ptx::mma_f16_ta(d, a + k * PITCH, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, acc);
+        ptx::mma_f16_ta(d, a + k * 16 / RUN * PITCH + k * 16 % RUN / 2, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, acc);
     };
-    if (steps >= TO) {                                             // a test for each would take as long as a product
-        one(FROM, add);
+    one(0, add);
+    if (steps == ROWS / 16) {                                      // a test for each would take as long as a product
 #pragma unroll
-        for (int k = FROM + 1; k < TO; ++k) one(k, 1);
+        for (int k = 1; k < ROWS / 16; ++k) one(k, 1);
     } else {
-        for (int k = FROM; k < steps; ++k) one(k, add || k > FROM);
+        for (int k = 1; k < steps; ++k) one(k, 1);
     }
 }
 
@@ -287,7 +287,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             if (one) {
                 ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, 8>(tmem + 256, tmem, v, steps, j > 0);
+                    mma_sum<DP, ROWS, 0>(tmem + 256, tmem, v, steps, j > 0);
                     if (j == q0) {
                         ptx::mma_commit(ptx::smem_u32(&ctl->ofull[0]));
                     } else {
@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             if (second) {
                 ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, 8>(tmem + 256 + DP, tmem + ROWS, v, steps, j > 0);
+                    mma_sum<DP, ROWS, 0>(tmem + 256 + DP, tmem + ROWS, v, steps, j > 0);
                     if (!more) {
                         ptx::mma_commit(ptx::smem_u32(&ctl->ofull[1]));
                     } else {
@@ -436,16 +436,17 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
 }
 
 // ---------------------------------------------------------------------------
-// Gradients.  Two kernels, so that every sum has one owner and one order (five products a
-// pair of tiles become seven; adding dQ up from one kernel would need atomics, whose order
+// Gradients.  Two kinds of CTAs, so that every sum has one owner and one order (five products a
+// pair of tiles become seven; adding dQ up where dK and dV are would need atomics, whose order
 // changes the result).  KEYS: a CTA takes 128 keys of a head of k and v and goes through
 // the queries that see them, of every head that shares it; with S^T = K Q^T, P^T and dS^T
 // stay in tensor memory and dV += P^T dO, dK += dS^T Q take them from there.  Otherwise it
 // takes 128 queries of a head and goes through their keys: dQ += dS K.
 //
-// Sixteen warps turn S into P and dP = dO V^T into dS (a thread has 16 columns of either half
-// of a row, and the sums take the first halves while the second are worked out), one issues
-// products, one copies.  The tile that is used twice in a step (first in S, last in a
+// Sixteen warps turn S into P and dP = dO V^T into dS (32 columns of a row a thread), one
+// issues products, one copies.  Where the longest tiles would outlast the rest, a cluster
+// shares a tile's steps, and its CTAs add one another's sums, in order, through shared memory
+//.  The tile that is used twice in a step (first in S, last in a
 // sum) has three slots, the other two.
 // ---------------------------------------------------------------------------
 template <int DP> struct Backward {
@@ -460,27 +461,70 @@ template <int DP> struct Backward {
 };
 
 struct BackwardParams {
-    CUtensorMap fixed_a, fixed_b, a, b;          // KEYS: k, v, q, dO; otherwise q, dO, k, v
+    CUtensorMap q, k, v, dout;
     const float* lse;
     const float* delta;
-    bf16* out_a;                                 // KEYS: dk; otherwise dq
-    bf16* out_b;                                 // KEYS: dv
-    const AttentionTile* tiles;
+    bf16* dq;
+    bf16* dk;
+    bf16* dv;
+    const AttentionTile* q_tiles;
+    const AttentionTile* k_tiles;
+    int n_tiles;
     int tokens, heads, kv_heads, group, dim;
+    int split;                                   // CTAs of a cluster, which share a tile's steps
     float scale;
     int* status;
     long long wait_limit;
 };
 
 struct BackwardCtl {
-    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull[2], dpfull, dsfull[2], stats[2], done, drain;
+    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull, dpfull, dsfull, stats[2], done, drain;
     uint32_t tmem;
     int abort;
     int filled[2];
 };
 
-template <int DP, bool KEYS>
-__global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(const __grid_constant__ BackwardParams p) {
+// The steps of a CTA: every `split`-th of (head, tile) in order.  KEYS: tiles of queries from
+// the keys' own to the sequence's last, for each head of the group; otherwise tiles of keys up to the
+// queries' own.
+struct Steps {
+    int at, head, count;
+    int first, last, stride;
+    __device__ __forceinline__ Steps(const AttentionTile& t, int rank, int split, int kv, int group, bool keys) {
+        last = (t.length - 1) / ROWS;
+        first = keys ? t.tile : 0;
+        stride = split;
+        const int all = keys ? (last - first + 1) * group : t.tile + 1;
+        count = all > rank ? (all - rank - 1) / split + 1 : 0;
+        at = first + rank;
+        head = keys ? kv * group : kv;
+        wrap();
+    }
+    __device__ __forceinline__ void wrap() {
+        while (at > last) {
+            at -= last - first + 1;
+            ++head;
+        }
+    }
+    __device__ __forceinline__ void next() {
+        at += stride;
+        wrap();
+    }
+};
+
+// Where a CTA of a cluster leaves four columns of a row of its first or second sum.
+template <int DP> __device__ __forceinline__ uint32_t sum_at(int which, int row, int c) {
+    return (which * ROWS + row) * DP * 4 + (c ^ (row & 7)) * 16;
+}
+
+__device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a));
+    return v;
+}
+
+// block: among the CTAs of its kind
+template <int DP, bool KEYS> __device__ __forceinline__ void gradient_tile(const BackwardParams& p, int block) {
     using F = Backward<DP>;
     constexpr int WARPS = F::WARPS;
     static_assert(sizeof(BackwardCtl) <= F::CTL, "the barriers fit");
@@ -495,7 +539,12 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         if (threadIdx.x == 0) atomicCAS(p.status, 0, MOARA_ERR_ALIGN);
         return;
     }
-    const int owners = KEYS ? p.kv_heads : p.heads, owner = blockIdx.x % owners, kv = KEYS ? owner : owner / p.group;
+    const int rank = block % p.split, item = block / p.split;
+    const AttentionTile* const tiles = KEYS ? p.k_tiles : p.q_tiles;
+    const CUtensorMap *const fixed_a = KEYS ? &p.k : &p.q, *const fixed_b = KEYS ? &p.v : &p.dout;
+    const CUtensorMap *const map_a = KEYS ? &p.q : &p.k, *const map_b = KEYS ? &p.dout : &p.v;
+    bf16 *const out_a = KEYS ? p.dk : p.dq, *const out_b = p.dv;
+    const int owners = KEYS ? p.kv_heads : p.heads, owner = item % owners, kv = KEYS ? owner : owner / p.group;
     // copies of step j, whose tile is `at` of head `h`
     auto copy = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
         for (int c = 0; c < DP / 64; ++c)
@@ -504,21 +553,19 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
     auto copy_a = [&](const AttentionTile& t, int j, int h, int at) {
         const int slot = j % F::SA;
         ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->afull[slot]), F::TILE);
-        copy(ring_a + slot * F::TILE, &p.a, ctl->afull[slot], h, t.begin + at * ROWS);
+        copy(ring_a + slot * F::TILE, map_a, ctl->afull[slot], h, t.begin + at * ROWS);
     };
     auto copy_b = [&](const AttentionTile& t, int j, int h, int at) {
         const int slot = j % F::SB;
         ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->bfull[slot]), F::TILE);
-        copy(ring_b + slot * F::TILE, &p.b, ctl->bfull[slot], h, t.begin + at * ROWS);
+        copy(ring_b + slot * F::TILE, map_b, ctl->bfull[slot], h, t.begin + at * ROWS);
     };
     if (threadIdx.x == WARPS * 32) {
         // the thread that copies starts what the first step needs beside the others' set-up
         for (uint64_t* b : {&ctl->fixed, &ctl->sfull, &ctl->dpfull, &ctl->done, &ctl->drain}) ptx::mbar_init(ptx::smem_u32(b), 1);
-        for (int i = 0; i < 2; ++i) {
-            ptx::mbar_init(ptx::smem_u32(&ctl->pfull[i]), WARPS);
-            ptx::mbar_init(ptx::smem_u32(&ctl->dsfull[i]), WARPS);
-            ptx::mbar_init(ptx::smem_u32(&ctl->stats[i]), WARPS);
-        }
+        for (int i = 0; i < 2; ++i) ptx::mbar_init(ptx::smem_u32(&ctl->stats[i]), WARPS);
+        ptx::mbar_init(ptx::smem_u32(&ctl->pfull), WARPS);
+        ptx::mbar_init(ptx::smem_u32(&ctl->dsfull), WARPS);
         for (int i = 0; i < F::SA; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl->afull[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl->aempty[i]), 1);
@@ -528,16 +575,17 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             ptx::mbar_init(ptx::smem_u32(&ctl->bempty[i]), 1);
         }
         ctl->abort = 0;
-        ctl->filled[0] = ctl->filled[1] = 1;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
         pdl_begin();
-        const AttentionTile t = p.tiles[blockIdx.x / owners];
+        const AttentionTile t = tiles[item / owners];
+        const Steps s(t, rank, p.split, kv, p.group, KEYS);
         ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->fixed), 2 * F::TILE);
-        copy(smem, &p.fixed_a, ctl->fixed, owner, t.begin + t.tile * ROWS);
-        copy_a(t, 0, KEYS ? kv * p.group : kv, KEYS ? t.tile : 0);
-        copy(smem + F::TILE, &p.fixed_b, ctl->fixed, owner, t.begin + t.tile * ROWS);
-        copy_b(t, 0, KEYS ? kv * p.group : kv, KEYS ? t.tile : 0);
+        copy(smem, fixed_a, ctl->fixed, owner, t.begin + t.tile * ROWS);
+        if (s.count > 0) copy_a(t, 0, s.head, s.at);
+        copy(smem + F::TILE, fixed_b, ctl->fixed, owner, t.begin + t.tile * ROWS);
+        if (s.count > 0) copy_b(t, 0, s.head, s.at);
+        ctl->filled[0] = ctl->filled[1] = s.count > 0;
     }
     if (warp == WARPS + 1) {
         ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
@@ -548,10 +596,9 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
     ptx::tc_fence_after();
     const uint32_t tmem = ctl->tmem;
     pdl_begin();
-    const AttentionTile tile = p.tiles[blockIdx.x / owners];
-    const int last = (tile.length - 1) / ROWS;                     // tile of the sequence
-    const int per = KEYS ? last - tile.tile + 1 : tile.tile + 1;   // tiles that are gone through, per head
-    const int steps = KEYS ? per * p.group : per;
+    const AttentionTile tile = tiles[item / owners];
+    const Steps begin(tile, rank, p.split, kv, p.group, KEYS);
+    const int steps = begin.count, last = begin.last;              // this CTA's; tile of the sequence
     const int tail = tile.length - last * ROWS;                    // rows of the last tile
     auto wait = [&](uint64_t& bar, uint32_t parity) {
         return ptx::mbar_wait_warp(ptx::smem_u32(&bar), parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
@@ -562,19 +609,19 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
 
     if (warp == WARPS) {
         if (lane == 0) {
-            int na = 1, nb = 1, at = KEYS ? tile.tile : 0, h = KEYS ? kv * p.group : kv;
+            int na = steps > 0, nb = na;
+            Steps s = begin;
             auto room = [&](uint64_t& bar, int n, int slots) {
                 return n < slots || ptx::mbar_wait(ptx::smem_u32(&bar), (n / slots - 1) & 1, abort_flag, p.status,
                                                    MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
             };
             for (int j = 1; j < steps; ++j) {
-                h += KEYS && at == last;
-                at = at == last ? tile.tile : at + 1;
+                s.next();
                 if (!room(ctl->aempty[j % F::SA], j, F::SA)) break;
-                copy_a(tile, j, h, at);
+                copy_a(tile, j, s.head, s.at);
                 ++na;
                 if (!room(ctl->bempty[j % F::SB], j, F::SB)) break;
-                copy_b(tile, j, h, at);
+                copy_b(tile, j, s.head, s.at);
                 ++nb;
             }
             ctl->filled[0] = na;
@@ -592,18 +639,19 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         const Waits waits{abort_flag, p.status, p.wait_limit};
         const uint32_t afull = ptx::smem_u32(&ctl->afull[0]), bfull = ptx::smem_u32(&ctl->bfull[0]);
         const uint32_t aempty = ptx::smem_u32(&ctl->aempty[0]), bempty = ptx::smem_u32(&ctl->bempty[0]);
-        const uint32_t pfull = ptx::smem_u32(&ctl->pfull[0]), dsfull = ptx::smem_u32(&ctl->dsfull[0]);
+        const uint32_t pfull = ptx::smem_u32(&ctl->pfull), dsfull = ptx::smem_u32(&ctl->dsfull);
         const uint32_t sfull = ptx::smem_u32(&ctl->sfull), dpfull = ptx::smem_u32(&ctl->dpfull);
-        int sa = 0, sb = 0, at = KEYS ? tile.tile : 0;
+        int sa = 0, sb = 0;
         uint32_t pa = 0, pb = 0;
-        int rows = at == last ? tail : ROWS;
+        Steps step = begin;
+        int rows = step.at == last ? tail : ROWS;
         auto clean_a = [&] {
             if (rows % 16 != 0) clear_rows<DP>(ring_a + sa * F::TILE, rows, lane);
         };
         auto clean_b = [&] {
             if (KEYS && rows % 16 != 0) clear_rows<DP>(ring_b + sb * F::TILE, rows, lane);
         };
-        bool ok = wait(ctl->fixed, 0) && waits.two(afull, 0, bfull, 0);
+        bool ok = wait(ctl->fixed, 0) && steps > 0 && waits.two(afull, 0, bfull, 0);
         if (ok) {
             clean_a();
             clean_b();
@@ -621,8 +669,8 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             const bool more = j + 1 < steps;
             const int oa = sa, ob = sb, sums = (rows + 15) / 16;
             const uint32_t a = ra + oa * F::TILE, b = rb + ob * F::TILE;
-            at = at == last ? tile.tile : at + 1;
-            rows = at == last ? tail : ROWS;
+            step.next();
+            rows = step.at == last ? tail : ROWS;
             if (++sa == F::SA) { sa = 0; pa ^= 1; }
             if (++sb == F::SB) { sb = 0; pb ^= 1; }
             const uint32_t a1 = ra + sa * F::TILE, b1 = rb + sb * F::TILE;
@@ -631,13 +679,8 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
                 if (!ok) break;
                 if (more) clean_a();
                 ptx::tc_fence_after();
-                if (leader) mma_sum<DP, 16, 0, 4>(tmem + SUM_B, tmem + S, b, sums, j > 0);
-                __syncwarp();
-                ok = waits.one(pfull + 8, j & 1);
-                if (!ok) break;
-                ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, 16, 4, 8>(tmem + SUM_B, tmem + S, b, sums, true);
+                    mma_sum<DP, 32, 32>(tmem + SUM_B, tmem + S, b, sums, j > 0);
                     ptx::mma_commit(bempty + 8 * ob);
                     if (more) {                                     // over the P that the product in front of it has read by then
                         mma_rows<DP>(tmem + S, fixed, a1);
@@ -667,13 +710,8 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
                 if (!ok) break;
             }
             ptx::tc_fence_after();
-            if (leader) mma_sum<DP, 16, 0, 4>(tmem + SUM_A, tmem + dp_at(j), a, sums, j > 0);
-            __syncwarp();
-            ok = waits.one(dsfull + 8, j & 1);
-            if (!ok) break;
-            ptx::tc_fence_after();
             if (leader) {
-                mma_sum<DP, 16, 4, 8>(tmem + SUM_A, tmem + dp_at(j), a, sums, true);
+                mma_sum<DP, 32, 32>(tmem + SUM_A, tmem + dp_at(j), a, sums, j > 0);
                 ptx::mma_commit(aempty + 8 * oa);
                 if (KEYS && more) {
                     mma_rows<DP>(tmem + DPC, fixed + F::TILE, b1);
@@ -686,7 +724,7 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         commit(ctl->drain);
         wait_drain(ptx::smem_u32(&ctl->drain), 0);
     } else {
-        const int part = warp >> 2, quad = warp & 3, r = quad * 32 + lane, c0 = part * 16;    // columns c0 .. + 15 and 64 more
+        const int part = warp >> 2, quad = warp & 3, r = quad * 32 + lane, c0 = part * 32;
         const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
         const int row = tile.tile * ROWS + r;                       // in the sequence
         const bool real = row < tile.length;
@@ -700,51 +738,47 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             delta = f32x2(d, d);
         }
         // KEYS: negative lse (first 128 threads) or delta (the next) of a query of a step
-        int at = KEYS ? tile.tile : 0, head = kv * p.group;         // of the step: tile, head
-        auto follow = [&](int& t, int& h) {
-            h += t == last;
-            t = t == last ? tile.tile : t + 1;
-        };
-        auto stat = [&](int t, int h) {
-            const int q = t * ROWS + r;
+        Steps step = begin;
+        auto stat = [&](const Steps& s) {
+            const int q = s.at * ROWS + r;
             if (q >= tile.length || part >= 2) return 0.0f;
-            const long long from = static_cast<long long>(h) * p.tokens + tile.begin + q;
+            const long long from = static_cast<long long>(s.head) * p.tokens + tile.begin + q;
             return part == 0 ? -p.lse[from] * kLog2e : -p.delta[from];
         };
-        float stat_ahead = KEYS ? stat(at, head) : 0.0f;
-        bool ok = true;
+        float stat_ahead = KEYS && steps > 0 ? stat(step) : 0.0f;
+        bool ok = steps > 0;
         for (int j = 0; j < steps; ++j) {
             const ulonglong2* sl = reinterpret_cast<const ulonglong2*>(stats + (j & 1) * 2 * ROWS + c0);
             const ulonglong2* sd = sl + ROWS / 4;
+            const int at = step.at;
+            step.next();
             if (KEYS) {
                 if (part < 2) stats[(j & 1) * 2 * ROWS + part * ROWS + r] = stat_ahead;
                 __syncwarp();
                 if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->stats[j & 1]));
-                int t = at, h = head;
-                follow(t, h);
-                if (j + 1 < steps) stat_ahead = stat(t, h);
+                if (j + 1 < steps) stat_ahead = stat(step);
                 // all warps' (a barrier whose wait is bounded); they have left step j - 1 by then
                 ok = wait(ctl->stats[j & 1], (j >> 1) & 1);
                 if (!ok) break;
             }
-            // which columns of the row count: from `from` on (KEYS) up to `to`
-            int from = 0, to = ROWS;
+            // which columns of this thread count: from `from` on (KEYS) up to `to`
+            int from = 0, to = 32;
             if (KEYS) {
-                if (at == tile.tile) from = r;
-                if (at == last) to = tail;
-            } else if (j == tile.tile) {
-                to = r + 1;
+                if (at == tile.tile) from = r - c0;
+                if (at == last) to = tail - c0;
+            } else if (at == tile.tile) {
+                to = r + 1 - c0;
             }
-            const bool all = __all_sync(0xffffffffu, from == 0 && to == ROWS);
-            auto mask = [&](float (&x)[16], int c) {
+            const bool all = __all_sync(0xffffffffu, from <= 0 && to >= 32);
+            auto put = [&](uint32_t column, float (&x)[32], uint64_t& bar) {
+                if (!all) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = c + e >= from && c + e < to ? x[e] : 0.0f;
-            };
-            auto put = [&](uint32_t column, const float (&x)[16], uint64_t& bar) {
-                uint32_t w[8];
+                    for (int c = 0; c < 32; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
+                }
+                uint32_t w[16];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) w[e] = pack2(x[2 * e], x[2 * e + 1]);
-                ptx::tmem_st8(lanes + column, w);
+                for (int c = 0; c < 16; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
+                ptx::tmem_st16(lanes + column + c0, w);
                 ptx::tmem_st_wait();
                 ptx::tc_fence_before();
                 __syncwarp();
@@ -754,48 +788,37 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             if (!ok) break;
             ptx::tc_fence_after();
             uint32_t s[32];
-            ptx::tmem_ld16x2(lanes + S + c0, lanes + S + 64 + c0, s);
+            ptx::tmem_ld32(lanes + S + c0, s);
             if (!KEYS) {
                 ptx::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull[0]));
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull));
             }
-            float x[2][16];
+            float x[32];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int c = 0; c < 32; c += 4) {
+                const ulonglong2 l = KEYS ? sl[c / 4] : make_ulonglong2(lse, lse);
 #pragma unroll
-                for (int c = 0; c < 16; c += 4) {
-                    const ulonglong2 l = KEYS ? sl[16 * h + c / 4] : make_ulonglong2(lse, lse);
-#pragma unroll
-                    for (int e = c; e < c + 4; e += 2) {
-                        split(fma2(f32x2(__uint_as_float(s[16 * h + e]), __uint_as_float(s[16 * h + e + 1])), scale, e == c ? l.x : l.y),
-                              x[h][e], x[h][e + 1]);
-                        x[h][e] = ex2(x[h][e]);
-                        x[h][e + 1] = ex2(x[h][e + 1]);
-                    }
+                for (int e = c; e < c + 4; e += 2) {
+                    split(fma2(f32x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale, e == c ? l.x : l.y), x[e], x[e + 1]);
+                    x[e] = ex2(x[e]);
+                    x[e + 1] = ex2(x[e + 1]);
                 }
-                if (!all) mask(x[h], 64 * h + c0);
-                if (KEYS) put(S + 64 * h + c0, x[h], ctl->pfull[h]);
             }
+            if (KEYS) put(S, x, ctl->pfull);
             ok = wait(ctl->dpfull, j & 1);
             if (!ok) break;
             ptx::tc_fence_after();
-            ptx::tmem_ld16x2(lanes + dp_at(j) + c0, lanes + dp_at(j) + 64 + c0, s);
+            ptx::tmem_ld32(lanes + dp_at(j) + c0, s);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int c = 0; c < 32; c += 4) {
+                const ulonglong2 d = KEYS ? sd[c / 4] : make_ulonglong2(delta, delta);
 #pragma unroll
-                for (int c = 0; c < 16; c += 4) {
-                    const ulonglong2 d = KEYS ? sd[16 * h + c / 4] : make_ulonglong2(delta, delta);
-#pragma unroll
-                    for (int e = c; e < c + 4; e += 2)
-                        split(mul2(f32x2(x[h][e], x[h][e + 1]),
-                                   add2(f32x2(__uint_as_float(s[16 * h + e]), __uint_as_float(s[16 * h + e + 1])), e == c ? d.x : d.y)),
-                              x[h][e], x[h][e + 1]);
-                }
-                if (!all) mask(x[h], 64 * h + c0);                  // what is not counted may be infinite or NaN
-                put(dp_at(j) + 64 * h + c0, x[h], ctl->dsfull[h]);
+                for (int e = c; e < c + 4; e += 2)
+                    split(mul2(f32x2(x[e], x[e + 1]), add2(f32x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), e == c ? d.x : d.y)),
+                          x[e], x[e + 1]);
             }
-            if (KEYS) follow(at, head);
+            put(dp_at(j), x, ctl->dsfull);                          // what does not count may be infinite or NaN
         }
         if (ok) ok = wait(ctl->done, 0);
         if (ok) {
@@ -807,14 +830,20 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
             const float factor = first ? 1.0f : p.scale;
             const int o0 = part % PARTS * WIDTH;
             const long long pitch = static_cast<long long>(owners) * p.dim * 2;
-            bf16* const out = (first ? p.out_b : p.out_a) + ((token - lane) * owners + owner) * p.dim + o0;
-            // the fixed tiles are no longer read
+            bf16* const out = (first ? out_b : out_a) + ((token - lane) * owners + owner) * p.dim + o0;
+            // the tiles are no longer read
             uint8_t* const stage = smem + warp * (2 * F::TILE / WARPS);
             uint4 w[WIDTH / 8];
 #pragma unroll
             for (int c = 0; c < WIDTH; c += 16) {
                 float o[16];
                 ptx::tmem_ld16(src + o0 + c, o);
+                if (p.split > 1) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        *reinterpret_cast<float4*>(smem + sum_at<DP>(first, r, (o0 + c) / 4 + e)) =
+                            make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                }
 #pragma unroll
                 for (int e = 0; e < 2; ++e)
                     w[c / 8 + e] = make_uint4(pack2(o[8 * e] * factor, o[8 * e + 1] * factor),
@@ -822,7 +851,8 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
                                               pack2(o[8 * e + 4] * factor, o[8 * e + 5] * factor),
                                               pack2(o[8 * e + 6] * factor, o[8 * e + 7] * factor));
             }
-            store_rows(stage, w, reinterpret_cast<uint8_t*>(out), pitch, tile.length - (row - lane), (p.dim - o0) * 2, lane);
+            if (p.split == 1)
+                store_rows(stage, w, reinterpret_cast<uint8_t*>(out), pitch, tile.length - (row - lane), (p.dim - o0) * 2, lane);
         }
     }
     ptx::tc_fence_before();
@@ -839,6 +869,41 @@ __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(con
         ptx::tmem_dealloc(tmem, 512);
     }
     __syncthreads();
+    if (p.split == 1) return;
+    ptx::cluster_sync();                         // every CTA's sums are in its shared memory
+    const bool gave_up =
+        lane < p.split && ptx::ld_cluster_u32(ptx::mapa(ptx::smem_u32(&ctl->abort), static_cast<uint32_t>(lane))) != 0;
+    if (!__any_sync(0xffffffffu, gave_up)) {
+        // a share of the rows each; ranks behind the last step have none
+        const int all = KEYS ? (last - begin.first + 1) * p.group : tile.tile + 1, ranks = min(p.split, all);
+        const int share = ROWS / p.split, chunks = DP / 8;
+        for (int n = threadIdx.x; n < (KEYS ? 2 : 1) * share * chunks; n += blockDim.x) {
+            const int c = n % chunks, row = rank * share + n / chunks % share, which = n / (chunks * share);
+            float o[8] = {};
+            for (int k = 0; k < ranks; ++k)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float4 v = ld_cluster_f4(ptx::mapa(ptx::smem_u32(smem + sum_at<DP>(which, row, 2 * c + e)), k));
+                    o[4 * e] += v.x; o[4 * e + 1] += v.y; o[4 * e + 2] += v.z; o[4 * e + 3] += v.w;
+                }
+            if (tile.tile * ROWS + row >= tile.length || 8 * c >= p.dim) continue;
+            const float factor = which != 0 ? 1.0f : p.scale;
+            bf16* out = (which != 0 ? out_b : out_a) +
+                        (static_cast<long long>(tile.begin + tile.tile * ROWS + row) * owners + owner) * p.dim + 8 * c;
+            *reinterpret_cast<uint4*>(out) = make_uint4(pack2(o[0] * factor, o[1] * factor), pack2(o[2] * factor, o[3] * factor),
+                                                        pack2(o[4] * factor, o[5] * factor), pack2(o[6] * factor, o[7] * factor));
+        }
+    }
+    __syncwarp();
+    ptx::cluster_sync();                         // no CTA leaves while another reads its sums
+}
+
+// The keys' tiles first, of which a group of heads makes the longest; the queries' fill the GPU
+// behind them.  (Apart, 8192 packed tokens with 28 heads on 4 took 324 + 207 us.)
+template <int DP> __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(const __grid_constant__ BackwardParams p) {
+    const int keys = p.n_tiles * p.kv_heads * p.split, block = static_cast<int>(blockIdx.x);
+    if (block < keys) gradient_tile<DP, true>(p, block);
+    else gradient_tile<DP, false>(p, block - keys);
 }
 
 struct DeltaParams {
@@ -925,10 +990,11 @@ template <int DP> cudaError_t forward_as(const ForwardParams& p, int ctas, cudaS
     return launch(k_attention<DP>, dim3(ctas), dim3(Forward<DP>::THREADS), Forward<DP>::SMEM, s, 1, p);
 }
 
-template <int DP, bool KEYS> cudaError_t backward_as(const BackwardParams& p, int ctas, cudaStream_t s) {
-    const cudaError_t e = allow_shared<DP + KEYS>(k_attention_grad<DP, KEYS>, Backward<DP>::SMEM);
+template <int DP> cudaError_t backward_as(const BackwardParams& p, cudaStream_t s) {
+    const cudaError_t e = allow_shared<DP>(k_attention_grad<DP>, Backward<DP>::SMEM);
     if (e != cudaSuccess) return e;
-    return launch(k_attention_grad<DP, KEYS>, dim3(ctas), dim3(Backward<DP>::THREADS), Backward<DP>::SMEM, s, 1, p);
+    const unsigned int ctas = static_cast<unsigned int>(p.n_tiles) * (p.kv_heads + p.heads) * p.split;
+    return launch(k_attention_grad<DP>, dim3(ctas), dim3(Backward<DP>::THREADS), Backward<DP>::SMEM, s, p.split, p);
 }
 
 }  // namespace
@@ -955,11 +1021,11 @@ cudaError_t launch_attention(const Attention& a, cudaStream_t s, int64_t* launch
 }
 
 cudaError_t launch_attention_backward(const AttentionGrad& a, cudaStream_t s, int64_t* launches) {
-    CUtensorMap q, k, v, dout;
-    if (!encode(&q, a.q, a.tokens, a.heads, a.dim, a.q_row, a.q_head) ||
-        !encode(&k, a.k, a.tokens, a.kv_heads, a.dim, a.k_row, a.k_head) ||
-        !encode(&v, a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head) ||
-        !encode(&dout, a.dout, a.tokens, a.heads, a.dim, a.do_row, a.do_head))
+    BackwardParams p{};
+    if (!encode(&p.q, a.q, a.tokens, a.heads, a.dim, a.q_row, a.q_head) ||
+        !encode(&p.k, a.k, a.tokens, a.kv_heads, a.dim, a.k_row, a.k_head) ||
+        !encode(&p.v, a.v, a.tokens, a.kv_heads, a.dim, a.v_row, a.v_head) ||
+        !encode(&p.dout, a.dout, a.tokens, a.heads, a.dim, a.do_row, a.do_head))
         return cudaErrorInvalidValue;
     const DeltaParams d{static_cast<const bf16*>(a.dout), static_cast<const bf16*>(a.out), static_cast<const bf16*>(a.rest),
                         a.delta, a.do_row, a.do_head, a.tokens, a.heads, a.dim};
@@ -967,9 +1033,14 @@ cudaError_t launch_attention_backward(const AttentionGrad& a, cudaStream_t s, in
     ++*launches;
     cudaError_t e = launch(k_attention_delta, dim3(static_cast<unsigned int>((rows - 1) / 16 + 1)), dim3(256), 0, s, 1, d);
     if (e != cudaSuccess) return e;
-    BackwardParams p{};
     p.lse = a.lse;
     p.delta = a.delta;
+    p.dq = static_cast<bf16*>(a.dq);
+    p.dk = static_cast<bf16*>(a.dk);
+    p.dv = static_cast<bf16*>(a.dv);
+    p.q_tiles = a.q_tiles;
+    p.k_tiles = a.k_tiles;
+    p.n_tiles = a.n_tiles;
     p.tokens = a.tokens;
     p.heads = a.heads;
     p.kv_heads = a.kv_heads;
@@ -978,26 +1049,13 @@ cudaError_t launch_attention_backward(const AttentionGrad& a, cudaStream_t s, in
     p.scale = a.scale;
     p.status = a.status;
     p.wait_limit = a.wait_limit;
-    const bool narrow = a.dim <= 64;
-    p.fixed_a = k;
-    p.fixed_b = v;
-    p.a = q;
-    p.b = dout;
-    p.out_a = static_cast<bf16*>(a.dk);
-    p.out_b = static_cast<bf16*>(a.dv);
-    p.tiles = a.k_tiles;
+    // clusters share a tile while the longest would outlast an SM's share of all steps, and has
+    // more than eight
+    const long long longest = static_cast<long long>(a.longest) * p.group, most = std::max<long long>(8, 2 * a.work * a.heads / 152);
+    p.split = 1;
+    while (p.split < 8 && longest > most * p.split) p.split *= 2;
     ++*launches;
-    e = narrow ? backward_as<64, true>(p, a.n_tiles * a.kv_heads, s) : backward_as<128, true>(p, a.n_tiles * a.kv_heads, s);
-    if (e != cudaSuccess) return e;
-    p.fixed_a = q;
-    p.fixed_b = dout;
-    p.a = k;
-    p.b = v;
-    p.out_a = static_cast<bf16*>(a.dq);
-    p.out_b = nullptr;
-    p.tiles = a.q_tiles;
-    ++*launches;
-    return narrow ? backward_as<64, false>(p, a.n_tiles * a.heads, s) : backward_as<128, false>(p, a.n_tiles * a.heads, s);
+    return a.dim <= 64 ? backward_as<64>(p, s) : backward_as<128>(p, s);
 }
 
 }  // namespace moara

@@ -114,6 +114,8 @@ struct AttentionGrad {
     const AttentionTile* q_tiles;  // by falling work of a query tile
     const AttentionTile* k_tiles;  // by falling work of a key tile
     int n_tiles;
+    int longest;           // tiles of the longest sequence
+    long long work;        // pairs of a query tile and a key tile that it sees
     int* status;
     long long wait_limit;
 };

@@ -86,7 +86,7 @@ int check_attention(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int
         return fail(ctx, MOARA_ERR_UNSUPPORTED, "heads of 8, 16, .. 128 entries are needed, not %d", dim);
     if (!(scale > 0.0f && scale < INFINITY)) return fail(ctx, MOARA_ERR_INVALID_ARG, "scale must be positive");
     const long long rows = static_cast<long long>(tokens) * heads;
-    if (static_cast<long long>(seqs->n_tiles) * heads > INT_MAX || rows / 16 > INT_MAX - 1)
+    if (static_cast<long long>(seqs->n_tiles) * heads > INT_MAX / 16 || seqs->work < 0 || rows / 16 > INT_MAX - 1)
         return fail(ctx, MOARA_ERR_SHAPE, "too many tokens and heads");
     if (seqs->n_tiles > 0) return check_out(ctx, "seqs->tiles", seqs->tiles);
     return MOARA_OK;
@@ -200,7 +200,7 @@ int moara_sequences_init(int count, const int* lengths, void* to, size_t bytes, 
     if (rc != MOARA_OK) return rc;
     const size_t need = static_cast<size_t>(2 * tiles + pairs) * sizeof(AttentionTile);
     if (bytes < need || (need > 0 && to == nullptr)) return MOARA_ERR_WORKSPACE;
-    *out = moara_sequences{nullptr, static_cast<int>(tokens), static_cast<int>(tiles), static_cast<int>(pairs)};
+    *out = moara_sequences{nullptr, static_cast<int>(tokens), static_cast<int>(tiles), static_cast<int>(pairs), 0, 0};
     AttentionTile* pair = static_cast<AttentionTile*>(to);
     AttentionTile* query = pair + pairs;
     AttentionTile* key = query + tiles;
@@ -212,6 +212,9 @@ int moara_sequences_init(int count, const int* lengths, void* to, size_t bytes, 
             if (t % 2 == 0) pair[p++] = AttentionTile{begin, lengths[i], t / 2, 0};
         }
         begin += lengths[i];
+        const long long n_seq = (static_cast<long long>(lengths[i]) + 127) / 128;
+        out->longest = std::max(out->longest, static_cast<int>(n_seq));
+        out->work += n_seq * (n_seq + 1) / 2;
     }
     const auto later = [](const AttentionTile& a, const AttentionTile& b) { return a.tile > b.tile; };
     std::stable_sort(pair, pair + pairs, later);
@@ -268,7 +271,7 @@ int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int to
     const AttentionTile* tiles = static_cast<const AttentionTile*>(seqs->tiles) + seqs->n_pairs;
     const moara::AttentionGrad a{dout, q, k, v, out, rest, lse, delta, dq, dk, dv, do_row, do_head, q_row, q_head, k_row, k_head,
                                  v_row, v_head, tokens, heads, kv_heads, dim, scale, tiles, tiles + seqs->n_tiles, seqs->n_tiles,
-                                 ctx->d_status, moara::tc_wait_limit(ctx->tc)};
+                                 seqs->longest, seqs->work, ctx->d_status, moara::tc_wait_limit(ctx->tc)};
     const cudaError_t e = moara::launch_attention_backward(a, static_cast<cudaStream_t>(stream), &ctx->launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "attention gradient launch");
     return MOARA_OK;
