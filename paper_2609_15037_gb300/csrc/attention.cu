@@ -14,6 +14,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "f32x2.cuh"
 #include "launch.cuh"
 #include "layers.h"
 #include "tc_ptx.cuh"
@@ -36,29 +37,6 @@ __device__ __forceinline__ float ex2(float x) {
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
-}
-
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ uint64_t f32x2(float a, float b) {
-    uint64_t y;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
-    return y;
-}
-__device__ __forceinline__ void split(uint64_t x, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-    uint64_t y;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
-    return y;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-    uint64_t y;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
-    return y;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-    uint64_t y;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
-    return y;
 }
 
 // D = A B^T over DP columns, both tiles in shared memory by rows (K-major): 128 x 128.

@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <atomic>
 
+#include "f32x2.cuh"
 #include "launch.cuh"
 #include "layers.h"
 #include "tc_ptx.cuh"
@@ -57,43 +58,46 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// 16 bytes of a row as fp32, their largest (NaN left out: it returns in the sum), and
-// exponentials relative to a reference: bf16 logits in powers of two, where the argument
-// is one fused operation and the result's error of 2^-22 far below the gradient's rounding;
-// fp32 logits with expf.
+// 16 bytes of a row as pairs of fp32 numbers, their largest (NaN left out: it returns in the
+// sum), and exponentials relative to a reference: powers of two, whose argument is one fused
+// operation for bf16 logits, an error far below the gradient's rounding; fp32 logits take z - ref
+// exactly as far as fp32 holds it, and what the product with log2 e rounds off as a factor
+// (1 + its natural power).
 template <class T> struct Line;
 
 template <> struct Line<float> {
     static constexpr int N = 4;
-    static __device__ __forceinline__ void values(const uint4& w, float (&v)[4]) {
-        v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y);
-        v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+    static __device__ __forceinline__ uint64_t pair(const uint4& w, int e) {
+        return e == 0 ? f32x2(__uint_as_float(w.x), __uint_as_float(w.y)) : f32x2(__uint_as_float(w.z), __uint_as_float(w.w));
     }
     static __device__ __forceinline__ float top(const uint4& w) {
-        float v[4];
-        values(w, v);
-        return fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3]));
+        return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
     }
     static __device__ __forceinline__ float reference(float top) { return top; }
-    static __device__ __forceinline__ float exponential(float z, float ref) { return expf(z - ref); }
+    static __device__ __forceinline__ uint64_t exponentials(uint64_t z, float ref) {
+        const uint64_t t = add2(z, both(-ref)), l = both(kLog2e), x = mul2(t, l);
+        float a, b, c, d;
+        split(x, a, b);
+        // of minus infinity the rest is NaN: its exponential is 0 whatever it is
+        split(fma2(t, l, mul2(x, both(-1.0f))), c, d);
+        const uint64_t y = f32x2(ex2(a), ex2(b));
+        return fma2(y, mul2(f32x2(a == -INFINITY ? 0.0f : c, b == -INFINITY ? 0.0f : d), both(0.69314718f)), y);
+    }
     static __device__ __forceinline__ float apart(float x) { return expf(x); }      // of a difference of references
     static __device__ __forceinline__ double natural(float ref) { return ref; }
-    static __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
-        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    static __device__ __forceinline__ uint4 pack(const uint64_t (&v)[2]) {
+        float a, b, c, d;
+        split(v[0], a, b);
+        split(v[1], c, d);
+        return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
     }
-    static __device__ __forceinline__ uint32_t lowest() { return 0xFF800000u; }
     static __device__ __forceinline__ float rounded(float x) { return x; }
 };
 
 template <> struct Line<__nv_bfloat16> {
     static constexpr int N = 8;
-    static __device__ __forceinline__ void values(const uint4& w, float (&v)[8]) {
-        const uint32_t a[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[2 * e] = __uint_as_float(a[e] << 16);
-            v[2 * e + 1] = __uint_as_float(a[e] & 0xFFFF0000u);
-        }
+    static __device__ __forceinline__ uint64_t pair(const uint4& w, int e) {
+        return widen2(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w);
     }
     static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
         uint32_t y;
@@ -105,15 +109,21 @@ template <> struct Line<__nv_bfloat16> {
         return fmaxf(__uint_as_float(t << 16), __uint_as_float(t & 0xFFFF0000u));
     }
     static __device__ __forceinline__ float reference(float top) { return top * kLog2e; }
-    static __device__ __forceinline__ float exponential(float z, float ref) { return ex2(fmaf(z, kLog2e, -ref)); }
+    static __device__ __forceinline__ uint64_t exponentials(uint64_t z, float ref) {
+        float a, b;
+        split(fma2(z, both(kLog2e), both(-ref)), a, b);
+        return f32x2(ex2(a), ex2(b));
+    }
     static __device__ __forceinline__ float apart(float x) { return ex2(x); }
     static __device__ __forceinline__ double natural(float ref) { return ref * kLn2; }
-    static __device__ __forceinline__ uint32_t pack2(float a, float b) {
+    static __device__ __forceinline__ uint32_t pack2(uint64_t v) {
+        float a, b;
+        split(v, a, b);
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
-    static __device__ __forceinline__ uint4 pack(const float (&v)[8]) {
-        return make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
+    static __device__ __forceinline__ uint4 pack(const uint64_t (&v)[4]) {
+        return make_uint4(pack2(v[0]), pack2(v[1]), pack2(v[2]), pack2(v[3]));
     }
     static __device__ __forceinline__ __nv_bfloat16 rounded(float x) { return __float2bfloat16_rn(x); }
 };
@@ -218,14 +228,15 @@ __global__ void __launch_bounds__(1024) k_policy_loss(const __grid_constant__ Lo
     top = all(top, true);
     // a part without a finite logit: its exponentials are 0 (or NaN, or infinity's)
     const float ref = top == -INFINITY ? 0.0f : L::reference(top);
-    float sum = 0.0f;
+    uint64_t sums2 = 0;
     for (int i = threadIdx.x; i < lines; i += blockDim.x) {
-        float v[N];
-        L::values(fetch(i), v);
+        const uint4 w = fetch(i);
 #pragma unroll
-        for (int e = 0; e < N; ++e) sum += L::exponential(v[e], ref);
+        for (int e = 0; e < N / 2; ++e) sums2 = add2(sums2, L::exponentials(L::pair(w, e), ref));
     }
-    sum = all(sum, false);
+    float sum, odd;
+    split(sums2, sum, odd);
+    sum = all(sum + odd, false);
     if (threadIdx.x == 0) {
         ctl.top = top == -INFINITY ? -INFINITY : ref;
         ctl.sum = ok ? sum : NAN;
@@ -303,16 +314,16 @@ __global__ void __launch_bounds__(1024) k_policy_loss(const __grid_constant__ Lo
     T* dz = static_cast<T*>(p.dz) + row * p.lddz + first;
     const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == off * sizeof(T);
     T* out0 = dz - off;
-    const int hit = counts && owner == rank ? static_cast<int>(target - first) + off : -1;
+    const int hit = counts && owner == rank ? static_cast<int>(target - first) + off : -1, hit_line = hit < 0 ? -1 : hit / N;
     for (int i = threadIdx.x; i < lines; i += blockDim.x) {
-        float v[N];
-        L::values(fetch(i), v);
+        const uint4 w = fetch(i);
+        uint64_t v[N / 2];
 #pragma unroll
-        for (int e = 0; e < N; ++e) v[e] = zero ? 0.0f : L::exponential(v[e], ref) * factor;
-        if (!zero && hit / N == i && hit >= 0) {
+        for (int e = 0; e < N / 2; ++e) v[e] = zero ? 0 : mul2(L::exponentials(L::pair(w, e), ref), both(factor));
+        if (i == hit_line && !zero) {
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (hit % N == e) v[e] += gain;
+            for (int e = 0; e < N / 2; ++e)
+                if (hit % N / 2 == e) v[e] = add2(v[e], hit & 1 ? f32x2(0.0f, gain) : f32x2(gain, 0.0f));
         }
         if (same && i >= inner0 && i < inner1) {
             reinterpret_cast<uint4*>(out0)[i] = L::pack(v);
@@ -320,7 +331,9 @@ __global__ void __launch_bounds__(1024) k_policy_loss(const __grid_constant__ Lo
 #pragma unroll
             for (int e = 0; e < N; ++e) {
                 const int c = i * N + e - off;
-                if (c >= 0 && c < len) dz[c] = L::rounded(v[e]);
+                float x[2];
+                split(v[e / 2], x[0], x[1]);
+                if (c >= 0 && c < len) dz[c] = L::rounded(x[e & 1]);
             }
         }
     }

@@ -6,6 +6,7 @@
 
 #include <algorithm>
 
+#include "f32x2.cuh"
 #include "launch.cuh"
 #include "layers.h"
 
@@ -13,30 +14,6 @@ namespace moara {
 namespace {
 
 using bf16 = __nv_bfloat16;
-
-// V entries in one access, as fp32.
-template <class T, int V> __device__ __forceinline__ void load(const T* p, float (&v)[V]) {
-    if constexpr (V == 1) {
-        v[0] = static_cast<float>(p[0]);
-    } else if constexpr (sizeof(T) == 4) {
-#pragma unroll
-        for (int e = 0; e < V; e += 4) {
-            const float4 a = *reinterpret_cast<const float4*>(p + e);
-            v[e] = a.x; v[e + 1] = a.y; v[e + 2] = a.z; v[e + 3] = a.w;
-        }
-    } else {
-        uint32_t w[V / 2];
-        if constexpr (V == 8) {
-            const uint4 a = *reinterpret_cast<const uint4*>(p);
-            w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w;
-        } else {
-            const uint2 a = *reinterpret_cast<const uint2*>(p);
-            w[0] = a.x; w[1] = a.y;
-        }
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
-    }
-}
 
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
@@ -78,47 +55,56 @@ template <class T, int V> struct Raw {
             }
         }
     }
-    __device__ __forceinline__ float get(int e) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(w[e]);
-        else return __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
+    // entries 2e and 2e + 1; of a single one, it and a zero
+    __device__ __forceinline__ uint64_t pair(int e) const {
+        if constexpr (V == 1) return f32x2(__uint_as_float(sizeof(T) == 4 ? w[0] : w[0] << 16), 0.0f);
+        else if constexpr (sizeof(T) == 4) return f32x2(__uint_as_float(w[2 * e]), __uint_as_float(w[2 * e + 1]));
+        else return widen2(w[e]);
+    }
+    __device__ __forceinline__ void set(int e, uint64_t x) {
+        float a, b;
+        split(x, a, b);
+        if constexpr (sizeof(T) == 4) {
+            w[V == 1 ? 0 : 2 * e] = __float_as_uint(a);
+            if constexpr (V > 1) w[2 * e + 1] = __float_as_uint(b);
+        } else {
+            w[e] = pack2(a, b);
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const {
+        if constexpr (BYTES == 2) {
+            *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>(w[0]);
+        } else if constexpr (BYTES == 4) {
+            *reinterpret_cast<uint32_t*>(p) = w[0];
+        } else if constexpr (BYTES == 8) {
+            *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < WORDS; e += 4)
+                *reinterpret_cast<uint4*>(p + e * 4 / static_cast<int>(sizeof(T))) = make_uint4(w[e], w[e + 1], w[e + 2], w[e + 3]);
+        }
+    }
+    __device__ __forceinline__ void store_at(T* row, int c, int n) const {
+        if (c >= 0 && c + V <= n) {
+            store(row + c);
+        } else {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                if (c + e < 0 || c + e >= n) continue;
+                if constexpr (sizeof(T) == 4) reinterpret_cast<uint32_t*>(row)[c + e] = w[e];
+                else reinterpret_cast<uint16_t*>(row)[c + e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+            }
+        }
     }
 };
 
-template <class T> __device__ __forceinline__ T rounded(float x) {
-    if constexpr (sizeof(T) == 4) return x;
-    else return __float2bfloat16_rn(x);
-}
-
-template <class T, int V> __device__ __forceinline__ void store(T* p, const float (&v)[V]) {
-    if constexpr (V == 1) {
-        p[0] = rounded<T>(v[0]);
-    } else if constexpr (sizeof(T) == 4) {
+// x + r, rounded once (two bf16 numbers at a time; what fp32 would round off first is never
+// more than a trace below the larger one's last bit)
+template <class T, int V> __device__ __forceinline__ void add_raw(Raw<T, V>& x, const Raw<T, V>& r) {
 #pragma unroll
-        for (int e = 0; e < V; e += 4) *reinterpret_cast<float4*>(p + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-    } else if constexpr (V == 8) {
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
-    } else {
-        *reinterpret_cast<uint2*>(p) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
-    }
-}
-
-// The same at column c of a row with n columns (c may lie in front of it), zeros outside.
-template <class T, int V> __device__ __forceinline__ void load_at(const T* row, int c, int n, float (&v)[V]) {
-    if (c >= 0 && c + V <= n) {
-        load<T, V>(row + c, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e) v[e] = c + e >= 0 && c + e < n ? static_cast<float>(row[c + e]) : 0.0f;
-    }
-}
-
-template <class T, int V> __device__ __forceinline__ void store_at(T* row, int c, int n, const float (&v)[V]) {
-    if (c >= 0 && c + V <= n) {
-        store<T, V>(row + c, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < V; ++e)
-            if (c + e >= 0 && c + e < n) row[c + e] = rounded<T>(v[e]);
+    for (int e = 0; e < Raw<T, V>::WORDS; ++e) {
+        if constexpr (sizeof(T) == 4) x.w[e] = __float_as_uint(__uint_as_float(x.w[e]) + __uint_as_float(r.w[e]));
+        else asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(x.w[e]) : "r"(x.w[e]), "r"(r.w[e]));
     }
 }
 
@@ -135,6 +121,23 @@ struct Sum {
     __device__ __forceinline__ void add(const Sum& o) {
         add(o.hi);
         lo += o.lo;
+    }
+};
+
+// Two of them beside one another.
+struct Sums {
+    uint64_t hi = 0, lo = 0;
+    __device__ __forceinline__ void add(uint64_t x) {
+        const uint64_t s = add2(hi, x), b = sub2(s, hi);
+        lo = add2(lo, add2(sub2(hi, sub2(s, b)), sub2(x, b)));
+        hi = s;
+    }
+    __device__ __forceinline__ Sum both() const {
+        Sum a, b;
+        split(hi, a.hi, b.hi);
+        split(lo, a.lo, b.lo);
+        a.add(b);
+        return a;
     }
 };
 
@@ -210,18 +213,19 @@ template <int V> __device__ __forceinline__ void stage_gain(float* to, const flo
 }
 
 template <bool SHIFT, int V>
-__device__ __forceinline__ void gain_at(const float* gain, const float* staged, int c, int n, float (&g)[V]) {
+__device__ __forceinline__ void gain_at(const float* gain, const float* staged, int c, int n, Raw<float, V>& g) {
     if constexpr (SHIFT) {
 #pragma unroll
-        for (int e = 0; e < V; ++e) g[e] = c + e >= 0 && c + e < n ? staged[column<V>(c + e, n)] : 0.0f;
+        for (int e = 0; e < V; ++e) g.w[e] = c + e >= 0 && c + e < n ? __float_as_uint(staged[column<V>(c + e, n)]) : 0u;
     } else {
-        load_at<float, V>(gain, c, n, g);
+        g.load_at(gain, c, n);
     }
 }
 
-// A group of threads takes a row and keeps it in registers, E entries a thread: 32, so that
-// the sum over the group costs little beside them, or 8 where rows are too few to fill the GPU.
-// E = 0: a row of more than 32768 entries is read again, from L2, once its sum is known.
+// A group of threads takes a row and keeps it in registers, E entries a thread: 32 of bf16 or
+// 16 of fp32, so that the sum over the group costs little beside them, or 8 where rows are too
+// few to fill the GPU.  E = 0: a row of more than 1024 threads' entries is read again, from L2, once
+// its sum is known.
 template <class T, class TY, int V, int E, bool SHIFT>
 __global__ void __launch_bounds__(1024) k_norm(const ForwardParams p) {
     extern __shared__ float staged[];
@@ -241,31 +245,33 @@ __global__ void __launch_bounds__(1024) k_norm(const ForwardParams p) {
         T* h = p.r == nullptr ? nullptr : static_cast<T*>(p.h) + row * p.ldh;
         TY* y = p.y == nullptr ? nullptr : static_cast<TY*>(p.y) + row * p.ldy;
         const int off = SHIFT ? static_cast<int>((p.phase + row % V * p.pitch) % V) : 0;
-        float f[NV][V];
-        Sum s;
-        auto take = [&](int c, float (&v)[V]) {
-            load_at<T, V>(x, c, n, v);
+        constexpr int P = (V + 1) / 2;                       // pairs of an access
+        Raw<T, V> f[NV];                                     // h
+        Sums sums;
+        auto take = [&](int c, Raw<T, V>& v) {
+            v.load_at(x, c, n);
             if (r != nullptr) {
-                float w[V];
-                load_at<T, V>(r, c, n, w);
-#pragma unroll
-                for (int e = 0; e < V; ++e) v[e] = static_cast<float>(rounded<T>(v[e] + w[e]));
+                Raw<T, V> w;
+                w.load_at(r, c, n);
+                add_raw(v, w);
             }
         };
-        auto square = [&](const float (&v)[V]) {
+        auto square = [&](const Raw<T, V>& v) {
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float q = v[e] * v[e];
-                s.add(q);
-                if (sizeof(T) == 4) s.lo += fmaf(v[e], v[e], -q);   // of bf16 entries it is exact
+            for (int e = 0; e < P; ++e) {
+                const uint64_t a = v.pair(e), q = mul2(a, a);
+                sums.add(q);
+                // of bf16 entries the square is exact
+                if (sizeof(T) == 4) sums.lo = add2(sums.lo, fma2(a, a, mul2(q, both(-1.0f))));
             }
         };
-        auto put = [&](int c, const float (&v)[V], float rstd) {
-            float g[V], o[V];
+        auto put = [&](int c, const Raw<T, V>& v, float rstd) {
+            Raw<float, V> g;
+            Raw<TY, V> o;
             gain_at<SHIFT, V>(p.gain, staged, c, n, g);
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = v[e] * rstd * g[e];
-            store_at<TY, V>(y, c, n, o);
+            for (int e = 0; e < P; ++e) o.set(e, mul2(mul2(v.pair(e), both(rstd)), g.pair(e)));
+            o.store_at(y, c, n);
         };
         if constexpr (E > 0) {
             if (real) {
@@ -279,17 +285,17 @@ __global__ void __launch_bounds__(1024) k_norm(const ForwardParams p) {
                     const int c = (j * group + i) * V - off;
                     if (c >= n) continue;
                     square(f[j]);
-                    if (h != nullptr) store_at<T, V>(h, c, n, f[j]);
+                    if (h != nullptr) f[j].store_at(h, c, n);
                 }
             }
         } else if (real) {
             for (int c = i * V; c < n; c += group * V) {
                 take(c, f[0]);
                 square(f[0]);
-                if (h != nullptr) store_at<T, V>(h, c, n, f[0]);
+                if (h != nullptr) f[0].store_at(h, c, n);
             }
         }
-        s = group_sum(s, group, parts[turn] + mine * (group >> 5));
+        const Sum s = group_sum(sums.both(), group, parts[turn] + mine * (group >> 5));
         if (!real) continue;
         const float rstd = inverse_rms(s, n, p.eps);
         if (i == 0) p.rstd[row] = rstd;
@@ -303,7 +309,7 @@ __global__ void __launch_bounds__(1024) k_norm(const ForwardParams p) {
         } else {
             const T* from = h != nullptr ? h : x;            // a thread's own entries
             for (int c = i * V; c < n; c += group * V) {
-                load_at<T, V>(from, c, n, f[0]);
+                f[0].load_at(from, c, n);
                 put(c, f[0], rstd);
             }
         }
@@ -323,8 +329,18 @@ struct BackwardParams {
     int phase, pitch;
 };
 
+// Columns c and c + 1 (V = 1: c alone) of the sums, where they exist.
+template <int V, class At> __device__ __forceinline__ void add_column(float* columns, int c, int n, uint64_t u, uint64_t v, At at) {
+    float a[2], b[2];
+    split(u, a[0], a[1]);
+    split(v, b[0], b[1]);
+#pragma unroll
+    for (int e = 0; e < (V == 1 ? 1 : 2); ++e)
+        if (c + e >= 0 && c + e < n) columns[at(c + e)] = fmaf(a[e], b[e], columns[at(c + e)]);
+}
+
 // CTAs take rows a grid apart and leave their columns' sums of dy n.  E entries a thread
-// stay in registers as they came, with the columns' sums; E = 0: rows of more than 16384
+// stay in registers as they came, with the columns' sums; E = 0: rows of more than 512 threads'
 // entries are read again, the sums are in shared memory.  SHIFT: there too; a column's sum has
 // another thread from row to row, behind the barrier of the row's mean.
 template <class T, class TY, int V, int E, bool SHIFT>
@@ -335,7 +351,7 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
     const int group = p.group, per = blockDim.x / group, mine = threadIdx.x / group, i = threadIdx.x % group;
     const int n = p.cols;
     constexpr int NV = E == 0 ? 1 : E / V;
-    float acc[NV][V] = {};
+    uint64_t acc[NV][(V + 1) / 2] = {};
     if (E == 0 || SHIFT) {
         for (int c = threadIdx.x; c < n; c += blockDim.x) columns[SHIFT ? column<V>(c, n) : c] = 0.0f;
         __syncthreads();
@@ -355,32 +371,30 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
         const int off = SHIFT ? static_cast<int>((p.phase + row % V * p.pitch) % V) : 0;
         Raw<TY, V> a[NV];
         Raw<T, V> b[NV], w[NV];
+        constexpr int P = (V + 1) / 2;
         float rstd = 0.0f;
-        Sum dot;
+        Sums dots;
         auto product = [&](int c, int j) {
-            float g[V], q = 0.0f;
+            Raw<float, V> g;
             gain_at<SHIFT, V>(p.gain, staged, c, n, g);
+            uint64_t q = 0;
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                q = fmaf(a[j].get(e) * g[e], b[j].get(e) * rstd, q);
-                if (e % 4 == 3 || e == V - 1) {
-                    dot.add(q);
-                    q = 0.0f;
-                }
-            }
+            for (int e = 0; e < P; ++e) q = fma2(mul2(a[j].pair(e), g.pair(e)), mul2(b[j].pair(e), both(rstd)), q);
+            dots.add(q);
         };
         // dx, and the columns' sums by `add`
         auto put = [&](int c, int j, float mean, auto add) {
-            float g[V], o[V];
+            Raw<float, V> g;
             gain_at<SHIFT, V>(p.gain, staged, c, n, g);
+            Raw<T, V> o;
 #pragma unroll
-            for (int e = 0; e < V; ++e) {
-                const float u = a[j].get(e), v = b[j].get(e) * rstd;
+            for (int e = 0; e < P; ++e) {
+                const uint64_t u = a[j].pair(e), v = mul2(b[j].pair(e), both(rstd));
                 add(e, u, v);
-                o[e] = rstd * fmaf(-v, mean, u * g[e]);
-                if (dh != nullptr) o[e] += w[j].get(e);
+                const uint64_t d = fma2(v, both(-mean), mul2(u, g.pair(e)));
+                o.set(e, dh != nullptr ? fma2(both(rstd), d, w[j].pair(e)) : mul2(both(rstd), d));
             }
-            store_at<T, V>(dx, c, n, o);
+            o.store_at(dx, c, n);
         };
         if (real) {
             rstd = p.rstd[row];
@@ -410,7 +424,7 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
                 }
             }
         }
-        dot = group_sum(dot, group, parts[turn] + mine * (group >> 5));
+        const Sum dot = group_sum(dots.both(), group, parts[turn] + mine * (group >> 5));
         if (SHIFT) __syncwarp();                 // a group of one warp has no other barrier
         if (!real) continue;
         const float mean = (dot.hi + dot.lo) * inv;
@@ -419,14 +433,9 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
             for (int j = 0; j < NV; ++j) {
                 const int c = (j * group + i) * V - off;
                 if (c >= n) continue;
-                put(c, j, mean, [&](int e, float u, float v) {
-                    if constexpr (SHIFT) {
-                        if (c + e < 0 || c + e >= n) return;
-                        float& sum = columns[column<V>(c + e, n)];
-                        sum = fmaf(u, v, sum);
-                    } else {
-                        acc[j][e] = fmaf(u, v, acc[j][e]);
-                    }
+                put(c, j, mean, [&](int e, uint64_t u, uint64_t v) {
+                    if constexpr (SHIFT) add_column<V>(columns, c + 2 * e, n, u, v, [&](int k) { return column<V>(k, n); });
+                    else acc[j][e] = fma2(u, v, acc[j][e]);
                 });
             }
         } else {
@@ -434,8 +443,8 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
                 a[0].load_at(dy, c, n);
                 b[0].load_at(h, c, n);
                 if (dh != nullptr) w[0].load_at(dh, c, n);
-                put(c, 0, mean, [&](int e, float u, float v) {
-                    if (c + e < n) columns[c + e] = fmaf(u, v, columns[c + e]);
+                put(c, 0, mean, [&](int e, uint64_t u, uint64_t v) {
+                    add_column<V>(columns, c + 2 * e, n, u, v, [](int k) { return k; });
                 });
             }
         }
@@ -452,7 +461,9 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
                 for (int e = 0; e < V; ++e) {
                     const int c = (j * group + i) * V + e;
                     if (c >= n) continue;
-                    const float sum = k == 0 ? acc[j][e] : columns[c] + acc[j][e];
+                    float x, y;
+                    split(acc[j][e / 2], x, y);
+                    const float mine_sum = e & 1 ? y : x, sum = k == 0 ? mine_sum : columns[c] + mine_sum;
                     if (k + 1 < per) columns[c] = sum;
                     else out[c] = sum;
                 }
@@ -463,24 +474,52 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
     }
 }
 
-// Column sums of the partial rows, in their order: 32 columns a CTA, 16 warps share the rows.
+// Column sums of the partial rows, in their order: 32 columns a CTA, 16 warps with four rows at a
+// time share the rows; a lane has four columns.
 __global__ void __launch_bounds__(512) k_norm_gain(const float* partials, int count, int n, float* dgain) {
-    __shared__ float2 sums[16][32];
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    __shared__ float2 sums[64][33];
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, c = blockIdx.x * 32 + lane % 8 * 4, r0 = w * 4 + lane / 8;
     pdl_begin();
-    Sum s;
-    if (c < n)
-        for (int r = w; r < count; r += 16) s.add(partials[static_cast<long long>(r) * n + c]);
-    sums[w][lane] = make_float2(s.hi, s.lo);
-    __syncthreads();
-    if (w > 0 || c >= n) return;
-    for (int k = 1; k < 16; ++k) {
-        Sum t;
-        t.hi = sums[k][lane].x;
-        t.lo = sums[k][lane].y;
-        s.add(t);
+    Sum s[4];
+    const bool whole = n % 4 == 0;                           // rows begin on 16-byte lines
+#pragma unroll 4
+    for (int r = r0; r < count; r += 64) {
+        const float* row = partials + static_cast<long long>(r) * n;
+        float4 x = make_float4(0, 0, 0, 0);
+        if (whole && c < n) {
+            x = *reinterpret_cast<const float4*>(row + c);
+        } else {
+            if (c < n) x.x = row[c];
+            if (c + 1 < n) x.y = row[c + 1];
+            if (c + 2 < n) x.z = row[c + 2];
+            if (c + 3 < n) x.w = row[c + 3];
+        }
+        s[0].add(x.x);
+        s[1].add(x.y);
+        s[2].add(x.z);
+        s[3].add(x.w);
     }
-    dgain[c] = s.hi + s.lo;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) sums[r0][lane % 8 * 4 + e] = make_float2(s[e].hi, s[e].lo);
+    __syncthreads();
+    // two columns a warp, 16 lanes each with four of the 64 sums
+    const int k = w * 2 + lane / 16;
+    Sum t;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        Sum u;
+        u.hi = sums[lane % 16 * 4 + e][k].x;
+        u.lo = sums[lane % 16 * 4 + e][k].y;
+        t.add(u);
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o /= 2) {
+        Sum u;
+        u.hi = __shfl_down_sync(0xffffffffu, t.hi, o);
+        u.lo = __shfl_down_sync(0xffffffffu, t.lo, o);
+        t.add(u);
+    }
+    if (lane % 16 == 0 && blockIdx.x * 32 + k < n) dgain[blockIdx.x * 32 + k] = t.hi + t.lo;
 }
 
 // Whether the rows of all arrays lie alike in their 16-byte lines: `phase` entries into one
@@ -507,6 +546,7 @@ struct Lines {
 };
 
 constexpr long long kFull = 152 * 2048;          // threads that the GPU holds
+template <class T> constexpr int many = sizeof(T) == 2 ? 32 : 16;
 
 // Threads of a row of n entries, e of them each.
 int group_of(int n, int e) { return (n + 32 * e - 1) / (32 * e) * 32; }
@@ -520,8 +560,9 @@ template <class T, class TY, int V, bool SHIFT> cudaError_t forward_as(const For
     ForwardParams p = q;
     const int n = p.cols, reach = n + (SHIFT ? V - 1 : 0);
     // entry by entry there are no registers for 32
-    const bool wide = reach > (V == 1 ? 8192 : 32768);
-    const int e = V == 1 || (reach <= 8192 && static_cast<long long>(p.rows) * group_of(n, 8) < kFull) ? 8 : 32;
+    constexpr int MANY = V == 1 ? 8 : many<T>;
+    const bool wide = reach > 1024 * MANY;
+    const int e = reach <= 8192 && static_cast<long long>(p.rows) * group_of(n, 8) < kFull ? 8 : MANY;
     p.group = wide ? 1024 : group_of(reach, e);
     const int per = std::max(1, 256 / p.group);
     int ctas = (p.rows - 1) / per + 1;
@@ -530,7 +571,7 @@ template <class T, class TY, int V, bool SHIFT> cudaError_t forward_as(const For
         smem = static_cast<size_t>(n / V + 1) * V * 4;
         ctas = std::min<int>(ctas, 152 * std::max<int>(1, std::min<size_t>(2048 / (p.group * per), (200 << 10) / smem)));
     }
-    const auto fn = wide ? k_norm<T, TY, V, 0, false> : e == 8 ? k_norm<T, TY, V, 8, SHIFT> : k_norm<T, TY, V, V == 1 ? 8 : 32, SHIFT>;
+    const auto fn = wide ? k_norm<T, TY, V, 0, false> : e == 8 ? k_norm<T, TY, V, 8, SHIFT> : k_norm<T, TY, V, MANY, SHIFT>;
     const cudaError_t err = allow_shared(fn, smem);
     if (err != cudaSuccess) return err;
     return launch(fn, dim3(ctas), dim3(p.group * per), smem, s, 1, p);
@@ -543,22 +584,23 @@ template <class T, class TY> cudaError_t forward_of(ForwardParams p, cudaStream_
     if (l.aligned() && reinterpret_cast<uintptr_t>(p.gain) % 16 == 0) return forward_as<T, TY, V, false>(p, s);
     p.phase = l.phase;
     p.pitch = l.pitch;
-    return l.ok && p.cols <= 32000 ? forward_as<T, TY, V, true>(p, s) : forward_as<T, TY, 1, false>(p, s);
+    return l.ok && p.cols + V <= 1024 * many<T> ? forward_as<T, TY, V, true>(p, s) : forward_as<T, TY, 1, false>(p, s);
 }
 
 struct BackwardShape {
     int entries, group, per, ctas;
 };
 
-// v: entries of an access (1: of rows whose lines differ); shift: rows in their own lines
-BackwardShape backward_shape(int rows, int n, int v, bool shift) {
+// v: entries of an access (1: of rows whose lines differ); shift: rows in their own lines;
+// most: entries of a thread
+BackwardShape backward_shape(int rows, int n, int v, bool shift, int most) {
     BackwardShape b;
     const int reach = n + (shift ? v - 1 : 0);
     const bool few = reach <= 4096 && (v == 1 || static_cast<long long>(rows) * group_of(n, 8) < kFull / 2);
-    b.entries = few ? 8 : v == 1 || reach > 16384 ? 0 : 32;
+    b.entries = few ? 8 : v == 1 || reach > 512 * most ? 0 : most;
     b.group = b.entries == 0 ? 1024 : group_of(reach, b.entries);
     b.per = shift ? 1 : std::max(1, 128 / b.group);
-    int resident = b.entries == 0 ? 1 : std::max(1, (b.entries == 32 ? 512 : 1536) / (b.group * b.per));
+    int resident = b.entries == 0 ? 1 : std::max(1, (b.entries == 8 ? 1536 : 512) / (b.group * b.per));
     if (shift) resident = std::max(1, std::min(std::min(16, resident), (200 << 10) / (8 * (n + v))));
     const long long need = (static_cast<long long>(rows) - 1) / b.per + 1;
     b.ctas = static_cast<int>(std::min<long long>(need, 152LL * resident));
@@ -567,7 +609,8 @@ BackwardShape backward_shape(int rows, int n, int v, bool shift) {
 
 template <class T, class TY, int V, bool SHIFT> cudaError_t backward_as(const BackwardParams& q, int& ctas, cudaStream_t s) {
     BackwardParams p = q;
-    const BackwardShape b = backward_shape(p.rows, p.cols, V, SHIFT);
+    constexpr int MANY = V == 1 ? 8 : many<T>;
+    const BackwardShape b = backward_shape(p.rows, p.cols, V, SHIFT, MANY);
     const bool wide = b.entries == 0;
     p.group = b.group;
     ctas = b.ctas;
@@ -576,7 +619,7 @@ template <class T, class TY, int V, bool SHIFT> cudaError_t backward_as(const Ba
     const size_t smem = shift ? 2 * one : wide || b.per > 1 ? static_cast<size_t>(p.cols) * 4 : 0;
     const auto fn = wide             ? k_norm_backward<T, TY, V, 0, false>
                     : b.entries == 8 ? k_norm_backward<T, TY, V, 8, SHIFT>
-                                     : k_norm_backward<T, TY, V, V == 1 ? 8 : 32, SHIFT>;
+                                     : k_norm_backward<T, TY, V, MANY, SHIFT>;
     const cudaError_t e = allow_shared(fn, smem);
     if (e != cudaSuccess) return e;
     return launch(fn, dim3(b.ctas), dim3(b.group * b.per), smem, s, 1, p);
@@ -589,7 +632,7 @@ template <class T, class TY> cudaError_t backward_of(BackwardParams p, int& ctas
     if (l.aligned() && reinterpret_cast<uintptr_t>(p.gain) % 16 == 0) return backward_as<T, TY, V, false>(p, ctas, s);
     p.phase = l.phase;
     p.pitch = l.pitch;
-    return l.ok && p.cols + V <= 16384 ? backward_as<T, TY, V, true>(p, ctas, s) : backward_as<T, TY, 1, false>(p, ctas, s);
+    return l.ok && p.cols + V <= 512 * many<T> ? backward_as<T, TY, V, true>(p, ctas, s) : backward_as<T, TY, 1, false>(p, ctas, s);
 }
 
 }  // namespace
@@ -607,7 +650,7 @@ int norm_partials(int rows, int cols) {
     int most = 0;
     for (int v : {1, 4, 8})
         for (bool shift : {false, true})
-            if (!(shift && v == 1)) most = std::max(most, backward_shape(rows, cols, v, shift).ctas);
+            if (!(shift && v == 1)) most = std::max(most, backward_shape(rows, cols, v, shift, v == 1 ? 8 : 4 * v).ctas);
     return most;
 }
 
