@@ -558,9 +558,10 @@ int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_d
  *   H = X + R, rounded to their type;  s = 1 / sqrt(mean H^2 + eps);  Y = (H s) gain
  * X, R, H: rows x cols of x_dtype (fp32 or bf16), Y of y_dtype, row pitches in entries
  * (>= cols).  R and H are NULL together: H is X then.  gain: cols floats.  rstd
- * receives s, one float per row, for the gradients.  Squares are summed in two fp32
- * numbers, s is the nearest fp32 number but for rare ties, Y is rounded once from fp32; a row's
- * sum of squares has to lie in fp32's range.  H may be X or R, and Y may be X, R or H, where
+ * receives s, one float per row, for the gradients.  Squares are summed four at a time in fp32 and
+ * those sums in two fp32 numbers, s is off by 3 2^-24 of its value at most (for long rows it is mostly the
+ * nearest fp32 number), Y is rounded once from fp32; a row's sum of squares has to lie in fp32's
+ * range.  H may be X or R, and Y may be X, R or H, where
  * type and pitch are the same.  Any alignment of the types; rows that begin on 16-byte lines
  * are read by lines.  MOARA_ERR_UNSUPPORTED for more than 49152 columns. */
 int moara_rms_norm(moara_ctx* ctx, int rows, int cols, const void* X, int64_t ldx, const void* R, int64_t ldr,

@@ -67,10 +67,11 @@ struct PolicyLoss {
     float* logp;
     void* dz;              // null: no gradient
     int64_t lddz;
-    float* terms;          // three per row
+    void* terms;           // policy_loss_workspace(rows) bytes
     int* status;
     long long wait_limit;
 };
+size_t policy_loss_workspace(int rows);
 cudaError_t launch_policy_loss(const PolicyLoss& a, cudaStream_t s, int64_t* launches);
 
 // ------------------------------------------------------------------ attention

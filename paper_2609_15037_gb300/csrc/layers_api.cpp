@@ -280,7 +280,7 @@ int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int to
 int moara_policy_loss_workspace_bytes(int rows, size_t* out) {
     if (out == nullptr) return MOARA_ERR_INVALID_ARG;
     if (rows < 1) return MOARA_ERR_SHAPE;
-    *out = static_cast<size_t>(rows) * 3 * sizeof(float);
+    *out = moara::policy_loss_workspace(rows);
     return MOARA_OK;
 }
 
@@ -314,7 +314,7 @@ int moara_policy_loss(moara_ctx* ctx, int rows, int vocab, const void* Z, int dt
     if (!aligned16(workspace)) return fail(ctx, MOARA_ERR_ALIGN, "workspace is not 16-byte aligned");
     DeviceGuard g(ctx->device);
     const moara::PolicyLoss a{rows, vocab, Z, dtype, ldz, target, old_logp, ref_logp, adv, weight, low, high, kl, sums, logp,
-                              dZ, lddz, static_cast<float*>(workspace), ctx->d_status, moara::tc_wait_limit(ctx->tc)};
+                              dZ, lddz, workspace, ctx->d_status, moara::tc_wait_limit(ctx->tc)};
     const cudaError_t e = moara::launch_policy_loss(a, static_cast<cudaStream_t>(stream), &ctx->launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "policy loss launch");
     return MOARA_OK;

@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cstddef>
 
 #include "f32x2.cuh"
 #include "launch.cuh"
@@ -29,7 +30,7 @@ struct LossParams {
     const float* adv;
     const float* weight;
     float* logp;
-    float* terms;
+    float2* terms;
     long long ldz, lddz;
     int rows, vocab, part, split;
     float low, high, kl, mean;     // mean: weight of a token where none are given
@@ -128,259 +129,298 @@ template <> struct Line<__nv_bfloat16> {
     static __device__ __forceinline__ __nv_bfloat16 rounded(float x) { return __float2bfloat16_rn(x); }
 };
 
+// A sum held in two fp32 numbers: what an addition rounds off goes to the second.
+struct Sum {
+    float hi = 0.0f, lo = 0.0f;
+    __device__ __forceinline__ void add(float x) {
+        const float s = hi + x, b = s - hi;
+        lo += (hi - (s - b)) + (x - b);
+        hi = s;
+    }
+};
+
 struct LossCtl {
     uint64_t full;
     int abort;
     float top, sum, at;            // of this CTA's part: reference, sum, the target's logit if it is here
     float factor, gain;            // of the gradient
-    float part[32];
+    int hit;
+    float part[2][32];
 };
 
 __device__ __forceinline__ float ld_cluster_f32(uint32_t a) { return __uint_as_float(ptx::ld_cluster_u32(a)); }
 
-// A cluster of `split` CTAs takes a row, each a part of its columns, which a bulk copy
-// puts into shared memory in the 16-byte lines of the row's own alignment; what lies in
-// the first and last line beside the part is -infinity there.  !STAGED: a part that is
-// too large for that is read again from L2.
+// A cluster of `split` CTAs takes rows a grid apart, each CTA a part of their columns, whose
+// whole 16-byte lines a bulk copy puts into shared memory, in the row's own alignment; the next
+// row's copy begins as soon as this one has been read.  The first and the last line are read where
+// they lie if they are not whole, with -infinity beside the part.  !STAGED: a part that is too
+// large for shared memory is read again from L2.
 template <class T, bool STAGED>
-__global__ void __launch_bounds__(1024) k_policy_loss(const __grid_constant__ LossParams p) {
+__global__ void __launch_bounds__(512, 3) k_policy_loss(const __grid_constant__ LossParams p) {
     extern __shared__ __align__(16) uint8_t raw[];
     using L = Line<T>;
     constexpr int N = L::N;
     __shared__ LossCtl ctl;
-    const int rank = blockIdx.x % p.split, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long row = blockIdx.x / p.split;
+    const int rank = blockIdx.x % p.split, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     const int first = rank * p.part, len = max(0, min(p.vocab - first, p.part));
-    const T* z = static_cast<const T*>(p.z) + row * p.ldz + first;
-    const int off = static_cast<int>(reinterpret_cast<uintptr_t>(z) & 15) / static_cast<int>(sizeof(T));
-    const T* line0 = z - off;                                   // of the part's first line
-    const int lines = (off + len + N - 1) / N;
-    const int inner0 = off != 0, inner1 = (off + len) / N;      // whole lines
+    volatile int* abort_flag = &ctl.abort;
     if (threadIdx.x == 0) {
         ctl.abort = 0;
         if (STAGED) {
             ptx::mbar_init(ptx::smem_u32(&ctl.full), 1);
             ptx::fence_barrier_init();
+            ptx::fence_proxy_async_smem();
         }
     }
     __syncthreads();
     pdl_begin();
-    T* const stage = reinterpret_cast<T*>(raw);
-    // an element of the part's lines, -infinity outside the part
-    auto edge = [&](int i) -> T {
-        const int c = i - off;
-        return c >= 0 && c < len ? line0[i] : L::rounded(-INFINITY);
+    const uint32_t bar = ptx::smem_u32(&ctl.full), own = ptx::smem_u32(&ctl);
+    const long long step = gridDim.x / p.split;
+    // a row's part in lines: entries in front of it in its first line, lines, whole ones among them
+    struct Place {
+        const T* line0;
+        int off, lines, inner0, inner1;
     };
-    auto gather = [&](int line) {
-        uint4 w;
-        T* t = reinterpret_cast<T*>(&w);
-#pragma unroll
-        for (int e = 0; e < N; ++e) t[e] = edge(line * N + e);
-        return w;
+    auto place = [&](long long row) {
+        const T* z = static_cast<const T*>(p.z) + row * p.ldz + first;
+        Place x;
+        x.off = static_cast<int>(reinterpret_cast<uintptr_t>(z) & 15) / static_cast<int>(sizeof(T));
+        x.line0 = z - x.off;
+        x.lines = (x.off + len + N - 1) / N;
+        x.inner0 = x.off != 0;
+        x.inner1 = max(x.inner0, (x.off + len) / N);
+        return x;
     };
-    auto fetch = [&](int line) -> uint4 {
-        if (STAGED) return reinterpret_cast<const uint4*>(raw)[line];
-        return line >= inner0 && line < inner1 ? reinterpret_cast<const uint4*>(line0)[line] : gather(line);
+    auto copy = [&](const Place& x) {
+        const uint32_t bytes = (x.inner1 - x.inner0) * 16u;
+        if (bytes == 0) return;
+        ptx::mbar_arrive_expect_tx(bar, bytes);
+        for (uint32_t at = 0; at < bytes; at += 16384)
+            ptx::bulk_load(ptx::smem_u32(raw) + x.inner0 * 16 + at, reinterpret_cast<const uint8_t*>(x.line0) + x.inner0 * 16 + at,
+                           min(16384u, bytes - at), bar);
     };
-    const int64_t target = p.target[row];
-    const bool counts = target >= 0 && target < p.vocab;
-    const int owner = counts ? static_cast<int>(target / p.part) : 0;
-    bool ok = true;
-    if (STAGED) {
-        if (threadIdx.x == 0 && inner1 > inner0) {
-            const uint32_t bar = ptx::smem_u32(&ctl.full), bytes = (inner1 - inner0) * 16u;
-            ptx::mbar_arrive_expect_tx(bar, bytes);
-            for (uint32_t at = 0; at < bytes; at += 16384)
-                ptx::bulk_load(ptx::smem_u32(raw) + inner0 * 16 + at, reinterpret_cast<const uint8_t*>(line0) + inner0 * 16 + at,
-                               min(16384u, bytes - at), bar);
-        }
-        // the first and the last line, where they are not whole
-        if (threadIdx.x >= 32 && threadIdx.x < 32 + 2 * N) {
-            const int e = threadIdx.x - 32, line = e < N ? 0 : lines - 1;
-            const bool whole = line >= inner0 && line < inner1;
-            if (lines > 0 && !whole) stage[line * N + e % N] = edge(line * N + e % N);
-        }
-        if (inner1 > inner0)
-            ok = ptx::mbar_wait(ptx::smem_u32(&ctl.full), 0, &ctl.abort, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
-        if (!ok) wait_drain(ptx::smem_u32(&ctl.full), 0);
-        ok = __syncthreads_and(ok);
-    }
-    auto all = [&](float v, bool largest) {
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) {
-            const float w = __shfl_xor_sync(0xffffffffu, v, o);
-            v = largest ? fmaxf(v, w) : v + w;
-        }
-        if (lane == 0) ctl.part[warp] = v;
-        __syncthreads();
-        const int warps = blockDim.x >> 5;
-        v = lane < warps ? ctl.part[lane] : largest ? -INFINITY : 0.0f;
-#pragma unroll
-        for (int o = 16; o > 0; o /= 2) {
-            const float w = __shfl_xor_sync(0xffffffffu, v, o);
-            v = largest ? fmaxf(v, w) : v + w;
-        }
-        __syncthreads();
-        return v;
-    };
-    float top = -INFINITY;
-    for (int i = threadIdx.x; i < lines; i += blockDim.x) top = fmaxf(top, L::top(fetch(i)));
-    top = all(top, true);
-    // a part without a finite logit: its exponentials are 0 (or NaN, or infinity's)
-    const float ref = top == -INFINITY ? 0.0f : L::reference(top);
-    uint64_t sums2 = 0;
-    for (int i = threadIdx.x; i < lines; i += blockDim.x) {
-        const uint4 w = fetch(i);
-#pragma unroll
-        for (int e = 0; e < N / 2; ++e) sums2 = add2(sums2, L::exponentials(L::pair(w, e), ref));
-    }
-    float sum, odd;
-    split(sums2, sum, odd);
-    sum = all(sum + odd, false);
-    if (threadIdx.x == 0) {
-        ctl.top = top == -INFINITY ? -INFINITY : ref;
-        ctl.sum = ok ? sum : NAN;
-        if (counts && owner == rank) {
-            const int i = static_cast<int>(target - first) + off;
-            ctl.at = static_cast<float>(STAGED ? stage[i] : line0[i]);
-        }
-    }
-    if (p.split > 1) ptx::cluster_sync();
-    else __syncthreads();
-    if (threadIdx.x == 0) {
-        float base = -INFINITY, total = 0.0f, at = 0.0f;
-        float tops[8], sums[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            if (r >= p.split) break;
-            tops[r] = p.split == 1 ? ctl.top : ld_cluster_f32(ptx::mapa(ptx::smem_u32(&ctl.top), r));
-            sums[r] = p.split == 1 ? ctl.sum : ld_cluster_f32(ptx::mapa(ptx::smem_u32(&ctl.sum), r));
-            base = fmaxf(base, tops[r]);
-        }
-        if (counts) at = p.split == 1 ? ctl.at : ld_cluster_f32(ptx::mapa(ptx::smem_u32(&ctl.at), owner));
-        const float base0 = base == -INFINITY ? 0.0f : base;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            if (r >= p.split) break;
-            total += tops[r] == -INFINITY ? sums[r] : sums[r] * L::apart(tops[r] - base0);
-        }
-        // log(total) from its exponent and the rest, which lies in [1, 2)
-        int e = 0;
-        float log_total;
-        double lp;
-        if (total > 0.0f && total < INFINITY) {
-            e = static_cast<int>(__float_as_uint(total) >> 23) - 127;
-            log_total = logf(__uint_as_float((__float_as_uint(total) & 0x7FFFFFu) | 0x3F800000u));
-            lp = static_cast<double>(at) - (L::natural(base0) + (e * kLn2 + log_total));
-        } else {
-            lp = static_cast<double>(at) - (L::natural(base0) + logf(total));
-        }
-        const float w = p.weight != nullptr ? p.weight[row] : p.mean;
-        float gain = 0.0f, loss = 0.0f, kl = 0.0f, cut = 0.0f;
-        const bool taken = counts && w != 0.0f;
-        if (taken) {
-            const float a = p.adv[row], rho = expf(static_cast<float>(lp - p.old_logp[row]));
-            // NaN advantages and ratios stay NaN
-            const float bound = rho < p.low ? p.low : rho > p.high ? p.high : rho;
-            const bool clipped = bound * a < rho * a;
-            loss = clipped ? -bound * a : -rho * a;
-            float d = clipped ? 0.0f : -rho * a;
-            if (p.ref_logp != nullptr) {
-                const float x = static_cast<float>(p.ref_logp[row] - lp);
-                kl = exp_beyond_linear(x);
-                loss = fmaf(p.kl, kl, loss);
-                d = fmaf(-p.kl, expm1f(x), d);
-            }
-            cut = clipped ? w : 0.0f;
-            kl *= w;
-            loss *= w;
-            gain = w * d;
-        }
-        if (rank == 0) {
-            p.logp[row] = counts ? static_cast<float>(lp) : 0.0f;
-            p.terms[3 * row] = loss;
-            p.terms[3 * row + 1] = kl;
-            p.terms[3 * row + 2] = cut;
-        }
-        ctl.gain = gain;
-        // relative to this part's reference; infinite where nothing of it is to be multiplied
-        ctl.factor = taken ? -gain * ((ctl.top == -INFINITY ? 1.0f : L::apart(ref - base0)) / total) : INFINITY;
-    }
-    if (p.split > 1) ptx::cluster_sync();       // no CTA leaves while another reads its sums
-    else __syncthreads();
-    if (p.dz == nullptr || !ok) return;
-    const float factor = ctl.factor, gain = ctl.gain;
-    const bool zero = factor == INFINITY;
-    T* dz = static_cast<T*>(p.dz) + row * p.lddz + first;
-    const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == off * sizeof(T);
-    T* out0 = dz - off;
-    const int hit = counts && owner == rank ? static_cast<int>(target - first) + off : -1, hit_line = hit < 0 ? -1 : hit / N;
-    for (int i = threadIdx.x; i < lines; i += blockDim.x) {
-        const uint4 w = fetch(i);
-        uint64_t v[N / 2];
-#pragma unroll
-        for (int e = 0; e < N / 2; ++e) v[e] = zero ? 0 : mul2(L::exponentials(L::pair(w, e), ref), both(factor));
-        if (i == hit_line && !zero) {
-#pragma unroll
-            for (int e = 0; e < N / 2; ++e)
-                if (hit % N / 2 == e) v[e] = add2(v[e], hit & 1 ? f32x2(0.0f, gain) : f32x2(gain, 0.0f));
-        }
-        if (same && i >= inner0 && i < inner1) {
-            reinterpret_cast<uint4*>(out0)[i] = L::pack(v);
-        } else {
+    long long row = blockIdx.x / p.split;
+    Place x = place(row);
+    if (STAGED && threadIdx.x == 0) copy(x);
+    uint32_t phase = 0;
+    Sum sums[3];                                 // of the first thread: loss, KL term, clipped
+    for (; row < p.rows; row += step) {
+        auto fetch = [&](int line) {
+            if (line >= x.inner0 && line < x.inner1)
+                return STAGED ? reinterpret_cast<const uint4*>(raw)[line] : reinterpret_cast<const uint4*>(x.line0)[line];
+            uint4 w;
+            T* t = reinterpret_cast<T*>(&w);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const int c = i * N + e - off;
-                float x[2];
-                split(v[e / 2], x[0], x[1]);
-                if (c >= 0 && c < len) dz[c] = L::rounded(x[e & 1]);
+                const int c = line * N + e - x.off;
+                t[e] = c >= 0 && c < len ? x.line0[line * N + e] : L::rounded(-INFINITY);
+            }
+            return w;
+        };
+        // what the first thread needs of the token, fetched beside the row
+        int64_t target = 0;
+        float w = 0.0f, a = 0.0f, old = 0.0f, other = 0.0f;
+        if (threadIdx.x == 0) {
+            target = p.target[row];
+            w = p.weight != nullptr ? p.weight[row] : p.mean;
+            a = p.adv[row];
+            old = p.old_logp[row];
+            if (p.ref_logp != nullptr) other = p.ref_logp[row];
+        }
+        if (STAGED && x.inner1 > x.inner0) {
+            if (!ptx::mbar_wait(bar, phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit)) wait_drain(bar, phase);
+            phase ^= 1;
+        }
+        auto all = [&](float v, bool largest, float* part) {
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) {
+                const float y = __shfl_xor_sync(0xffffffffu, v, o);
+                v = largest ? fmaxf(v, y) : v + y;
+            }
+            if (lane == 0) part[warp] = v;
+            __syncthreads();
+            v = lane < warps ? part[lane] : largest ? -INFINITY : 0.0f;
+#pragma unroll
+            for (int o = 16; o > 0; o /= 2) {
+                const float y = __shfl_xor_sync(0xffffffffu, v, o);
+                v = largest ? fmaxf(v, y) : v + y;
+            }
+            return v;
+        };
+        float top = -INFINITY;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < x.lines; i += blockDim.x) top = fmaxf(top, L::top(fetch(i)));
+        top = all(top, true, ctl.part[0]);
+        // a part without a finite logit: its exponentials are 0 (or NaN, or infinity's)
+        const float ref = top == -INFINITY ? 0.0f : L::reference(top);
+        uint64_t pairs = 0;
+#pragma unroll 4
+        for (int i = threadIdx.x; i < x.lines; i += blockDim.x) {
+            const uint4 v = fetch(i);
+#pragma unroll
+            for (int e = 0; e < N / 2; ++e) pairs = add2(pairs, L::exponentials(L::pair(v, e), ref));
+        }
+        float sum, odd;
+        split(pairs, sum, odd);
+        sum = all(sum + odd, false, ctl.part[1]);
+        const bool ok = *abort_flag == 0;        // the same in every thread: a wait ran out before the barriers above
+        if (threadIdx.x == 0) {
+            const bool counts = target >= 0 && target < p.vocab;
+            const int column = counts ? static_cast<int>(target) : 0, owner = column / p.part;
+            ctl.top = top == -INFINITY ? -INFINITY : ref;
+            ctl.sum = ok ? sum : NAN;
+            if (counts && owner == rank) ctl.at = static_cast<float>(x.line0[column - first + x.off]);
+        }
+        if (p.split > 1) {
+            __syncwarp();
+            ptx::cluster_sync();
+        }
+        if (threadIdx.x == 0) {
+            const bool counts = target >= 0 && target < p.vocab;
+            const int column = counts ? static_cast<int>(target) : 0, owner = column / p.part;
+            float tops[8], parts[8], base = -INFINITY, total = 0.0f, at = 0.0f;
+            if (p.split == 1) {
+                base = ctl.top;
+                total = ctl.sum;
+                at = ctl.at;
+            } else {
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    if (r >= p.split) break;
+                    const uint32_t peer = ptx::mapa(own, r);
+                    tops[r] = ld_cluster_f32(peer + static_cast<uint32_t>(offsetof(LossCtl, top)));
+                    parts[r] = ld_cluster_f32(peer + static_cast<uint32_t>(offsetof(LossCtl, sum)));
+                    base = fmaxf(base, tops[r]);
+                }
+                at = ld_cluster_f32(ptx::mapa(own, owner) + static_cast<uint32_t>(offsetof(LossCtl, at)));
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    if (r >= p.split) break;
+                    total += tops[r] == -INFINITY ? parts[r] : parts[r] * L::apart(tops[r] - base);
+                }
+            }
+            const float base0 = base == -INFINITY ? 0.0f : base;
+            // log(total) from its exponent and the rest, which lies in [1, 2)
+            double lp;
+            if (total > 0.0f && total < INFINITY) {
+                const int e = static_cast<int>(__float_as_uint(total) >> 23) - 127;
+                const float rest = logf(__uint_as_float((__float_as_uint(total) & 0x7FFFFFu) | 0x3F800000u));
+                lp = static_cast<double>(at) - (L::natural(base0) + (e * kLn2 + rest));
+            } else {
+                lp = static_cast<double>(at) - (L::natural(base0) + logf(total));
+            }
+            float gain = 0.0f;
+            const bool taken = counts && w != 0.0f;
+            if (taken) {
+                const float rho = expf(static_cast<float>(lp - old));
+                // NaN advantages and ratios stay NaN
+                const float bound = rho < p.low ? p.low : rho > p.high ? p.high : rho;
+                const bool clipped = bound * a < rho * a;
+                float loss = clipped ? -bound * a : -rho * a, d = clipped ? 0.0f : -rho * a;
+                if (p.ref_logp != nullptr) {
+                    const float y = static_cast<float>(other - lp), k = exp_beyond_linear(y);
+                    loss = fmaf(p.kl, k, loss);
+                    d = fmaf(-p.kl, expm1f(y), d);
+                    sums[1].add(k * w);
+                }
+                sums[0].add(loss * w);
+                if (clipped) sums[2].add(w);
+                gain = w * d;
+            }
+            if (rank == 0) p.logp[row] = counts ? static_cast<float>(lp) : 0.0f;
+            ctl.gain = gain;
+            // relative to this part's reference; infinite where nothing of it is to be multiplied
+            ctl.factor = taken ? -gain * ((ctl.top == -INFINITY ? 1.0f : L::apart(ref - base0)) / total) : INFINITY;
+            // the target's place among the part's lines, none for -1
+            ctl.hit = counts && owner == rank ? column - first + x.off : -1;
+        }
+        if (p.split > 1) {
+            __syncwarp();
+            ptx::cluster_sync();                 // no CTA goes on while another reads its sums
+        } else {
+            __syncthreads();
+        }
+        const Place mine = x;
+        if (p.dz != nullptr && ok) {
+            const float factor = ctl.factor, gain = ctl.gain;
+            const int hit = ctl.hit, hit_line = hit < 0 ? -1 : hit / N;
+            const bool zero = factor == INFINITY;
+            T* dz = static_cast<T*>(p.dz) + row * p.lddz + first;
+            const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == mine.off * sizeof(T);
+            T* out0 = dz - mine.off;
+#pragma unroll 4
+            for (int i = threadIdx.x; i < mine.lines; i += blockDim.x) {
+                const uint4 z = fetch(i);
+                uint64_t v[N / 2];
+#pragma unroll
+                for (int e = 0; e < N / 2; ++e) v[e] = zero ? 0 : mul2(L::exponentials(L::pair(z, e), ref), both(factor));
+                if (i == hit_line && !zero) {
+#pragma unroll
+                    for (int e = 0; e < N / 2; ++e)
+                        if (hit % N / 2 == e) v[e] = add2(v[e], hit & 1 ? f32x2(0.0f, gain) : f32x2(gain, 0.0f));
+                }
+                if (same && i >= mine.inner0 && i < mine.inner1) {
+                    reinterpret_cast<uint4*>(out0)[i] = L::pack(v);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const int c = i * N + e - mine.off;
+                        float y[2];
+                        split(v[e / 2], y[0], y[1]);
+                        if (c >= 0 && c < len) dz[c] = L::rounded(y[e & 1]);
+                    }
+                }
             }
         }
+        if (row + step < p.rows) {
+            x = place(row + step);
+            __syncthreads();                     // the row has been read
+            if (STAGED && threadIdx.x == 0) copy(x);
+        }
     }
+    if (threadIdx.x == 0 && rank == 0)
+        for (int k = 0; k < 3; ++k) p.terms[3 * (blockIdx.x / p.split) + k] = make_float2(sums[k].hi, sums[k].lo);
 }
 
-// The three sums over the rows, in their order by thread; what an addition rounds off is kept.
-__global__ void __launch_bounds__(1024) k_loss_sums(const float* terms, int rows, float* sums) {
-    __shared__ float2 part[3][32];
+// The clusters' sums, added up in a fixed order: at most kLossClusters of them.
+constexpr int kLossClusters = 152 * 8;
+__global__ void __launch_bounds__(128) k_loss_sums(const float2* terms, int count, float* out) {
+    __shared__ float2 part[3][4];
     pdl_begin();
-    float hi[3] = {}, lo[3] = {};
-    auto add = [&](int k, float x) {
-        const float s = hi[k] + x, b = s - hi[k];
-        lo[k] += (hi[k] - (s - b)) + (x - b);
-        hi[k] = s;
-    };
-    for (int r = threadIdx.x; r < rows; r += blockDim.x)
+    Sum s[3];
+#pragma unroll 4
+    for (int r = threadIdx.x; r < count; r += 128)
 #pragma unroll
-        for (int k = 0; k < 3; ++k) add(k, terms[3LL * r + k]);
+        for (int k = 0; k < 3; ++k) {
+            const float2 t = terms[3 * r + k];
+            s[k].add(t.x);
+            s[k].lo += t.y;
+        }
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    auto across = [&](int k) {
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
 #pragma unroll
         for (int o = 16; o > 0; o /= 2) {
-            const float h = __shfl_down_sync(0xffffffffu, hi[k], o), l = __shfl_down_sync(0xffffffffu, lo[k], o);
-            add(k, h);
-            lo[k] += l;
+            const float h = __shfl_down_sync(0xffffffffu, s[k].hi, o), l = __shfl_down_sync(0xffffffffu, s[k].lo, o);
+            s[k].add(h);
+            s[k].lo += l;
         }
-    };
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        across(k);
-        if (lane == 0) part[k][warp] = make_float2(hi[k], lo[k]);
+        if (lane == 0) part[k][warp] = make_float2(s[k].hi, s[k].lo);
     }
     __syncthreads();
-    if (warp > 0) return;
-#pragma unroll
-    for (int k = 0; k < 3; ++k) {
-        const bool has = lane < static_cast<int>(blockDim.x >> 5);
-        hi[k] = has ? part[k][lane].x : 0.0f;
-        lo[k] = has ? part[k][lane].y : 0.0f;
-        across(k);
-        if (lane == 0) sums[k] = hi[k] + lo[k];
+    if (threadIdx.x >= 3) return;
+    Sum all;
+    for (int w = 0; w < 4; ++w) {
+        all.add(part[threadIdx.x][w].x);
+        all.lo += part[threadIdx.x][w].y;
     }
+    // an infinite sum has NaN beside it
+    out[threadIdx.x] = fabsf(all.hi) < INFINITY ? all.hi + all.lo : all.hi;
 }
 
 constexpr int kStage = 200 * 1024;     // most bytes of a part in shared memory
 
-template <class T, bool STAGED> cudaError_t launch_loss(const LossParams& p, cudaStream_t s) {
+template <class T, bool STAGED> cudaError_t launch_loss(const LossParams& p, int& clusters, cudaStream_t s) {
     const auto fn = k_policy_loss<T, STAGED>;
     const int bytes = STAGED ? (p.part * static_cast<int>(sizeof(T)) + 15) / 16 * 16 + 16 : 0;
     if (bytes > 40 * 1024) {
@@ -395,11 +435,14 @@ template <class T, bool STAGED> cudaError_t launch_loss(const LossParams& p, cud
         }
     }
     const int lines = p.part / Line<T>::N + 2;
-    const int threads = std::min(STAGED ? 512 : 1024, std::max(64, (lines + 31) / 32 * 32));
-    return launch(fn, dim3(static_cast<unsigned int>(p.rows) * p.split), dim3(threads), bytes, s, p.split, p);
+    const int threads = std::min(512, std::max(64, (lines + 31) / 32 * 32));
+    // CTAs that an SM holds, by registers and shared memory (1.5 KB beside the part)
+    const int resident = std::max(1, std::min({8, 1536 / threads, (226 << 10) / (bytes + 1536)}));
+    clusters = std::min(p.rows, 152 * resident / p.split);
+    return launch(fn, dim3(static_cast<unsigned int>(clusters) * p.split), dim3(threads), bytes, s, p.split, p);
 }
 
-template <class T> cudaError_t loss_as(LossParams& p, cudaStream_t s) {
+template <class T> cudaError_t loss_as(LossParams& p, int& clusters, cudaStream_t s) {
     constexpr int N = Line<T>::N;
     // a row over more CTAs while they are few, each with some 4 KB and more, and where its part
     // would fill an SM's shared memory alone
@@ -409,7 +452,8 @@ template <class T> cudaError_t loss_as(LossParams& p, cudaStream_t s) {
                            (2LL * p.split * p.rows <= 304 && part(2 * p.split) * sizeof(T) >= 4096)))
         p.split *= 2;
     p.part = part(p.split);
-    return p.part * static_cast<long long>(sizeof(T)) <= kStage ? launch_loss<T, true>(p, s) : launch_loss<T, false>(p, s);
+    return p.part * static_cast<long long>(sizeof(T)) <= kStage ? launch_loss<T, true>(p, clusters, s)
+                                                                : launch_loss<T, false>(p, clusters, s);
 }
 
 }  // namespace
@@ -424,7 +468,7 @@ cudaError_t launch_policy_loss(const PolicyLoss& a, cudaStream_t s, int64_t* lau
     p.adv = a.adv;
     p.weight = a.weight;
     p.logp = a.logp;
-    p.terms = a.terms;
+    p.terms = static_cast<float2*>(a.terms);
     p.ldz = a.ldz;
     p.lddz = a.lddz;
     p.rows = a.rows;
@@ -435,12 +479,14 @@ cudaError_t launch_policy_loss(const PolicyLoss& a, cudaStream_t s, int64_t* lau
     p.mean = 1.0f / static_cast<float>(a.rows);
     p.status = a.status;
     p.wait_limit = a.wait_limit;
+    int clusters = 0;
     ++*launches;
-    cudaError_t e = a.dtype == MOARA_DTYPE_BF16 ? loss_as<__nv_bfloat16>(p, s) : loss_as<float>(p, s);
+    cudaError_t e = a.dtype == MOARA_DTYPE_BF16 ? loss_as<__nv_bfloat16>(p, clusters, s) : loss_as<float>(p, clusters, s);
     if (e != cudaSuccess) return e;
     ++*launches;
-    return launch(k_loss_sums, dim3(1), dim3(std::min(1024, (a.rows + 31) / 32 * 32)), 0, s, 1, static_cast<const float*>(a.terms),
-                  a.rows, a.sums);
+    return launch(k_loss_sums, dim3(1), dim3(128), 0, s, 1, static_cast<const float2*>(p.terms), clusters, a.sums);
 }
+
+size_t policy_loss_workspace(int rows) { return static_cast<size_t>(std::min(rows, kLossClusters)) * 3 * sizeof(float2); }
 
 }  // namespace moara

@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "f32x2.cuh"
 #include "launch.cuh"
@@ -141,8 +142,20 @@ struct Sums {
     }
 };
 
+// Squares of an access: each lane of a pair adds up its own in fp32 (three roundings at most),
+// and the group's total goes to the sums.
+template <class T, int V> __device__ __forceinline__ void add_squares(Sums& sums, const Raw<T, V>& v) {
+    uint64_t q = 0;
+#pragma unroll
+    for (int e = 0; e < (V + 1) / 2; ++e) {
+        const uint64_t a = v.pair(e);
+        q = e == 0 ? mul2(a, a) : fma2(a, a, q);
+    }
+    sums.add(q);
+}
+
 // 1 / sqrt(sum / n + eps): a Newton step on the residual of rsqrtf, in two numbers
-// throughout, so that the result is the nearest fp32 number but for rare ties.
+// throughout, so that it adds one rounding to the sum's error.
 __device__ __forceinline__ float inverse_rms(const Sum& s, int n, float eps) {
     if (!(s.hi < INFINITY)) return rsqrtf(s.hi);             // lo is NaN beside it
     const float f = static_cast<float>(n), total = s.hi + s.lo, rest = (s.hi - total) + s.lo;
@@ -222,10 +235,45 @@ __device__ __forceinline__ void gain_at(const float* gain, const float* staged, 
     }
 }
 
-// A group of threads takes a row and keeps it in registers, E entries a thread: 32 of bf16 or
-// 16 of fp32, so that the sum over the group costs little beside them, or 8 where rows are too
-// few to fill the GPU.  E = 0: a row of more than 1024 threads' entries is read again, from L2, once
-// its sum is known.
+// The same where columns c .. c + V - 1 all exist: from the first one's class on, entry e is e
+// classes further, and a place further where the classes end.
+template <int V> struct Classes {
+    int at, pitch, wrap, back;
+    __device__ __forceinline__ Classes(int c, int n) {
+        pitch = n / V + 1;
+        at = c % V * pitch + c / V;
+        wrap = V - c % V;
+        back = V * pitch - 1;
+    }
+    __device__ __forceinline__ int of(int e) const { return at + e * pitch - (e >= wrap ? back : 0); }
+};
+
+template <bool SHIFT, int V>
+__device__ __forceinline__ void gain_whole(const float* gain, const float* staged, int c, int n, Raw<float, V>& g) {
+    if constexpr (SHIFT) {
+        const Classes<V> k(c, n);
+#pragma unroll
+        for (int e = 0; e < V; ++e) g.w[e] = __float_as_uint(staged[k.of(e)]);
+    } else {
+        g.load(gain + c);
+    }
+}
+
+template <int V> __device__ __forceinline__ void add_whole(float* columns, int c, int n, int e, uint64_t u, uint64_t v) {
+    const Classes<V> k(c, n);
+    float a[2], b[2];
+    split(u, a[0], a[1]);
+    split(v, b[0], b[1]);
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+        float& sum = columns[k.of(2 * e + y)];
+        sum = fmaf(a[y], b[y], sum);
+    }
+}
+
+// Few rows: a group of threads takes a row and keeps it in registers, E = 8 entries a thread.
+// E = 0: rows of more than 1024 threads' entries, or whose arrays lie differently in their lines,
+// are read again, from L2, once their sum is known.
 template <class T, class TY, int V, int E, bool SHIFT>
 __global__ void __launch_bounds__(1024) k_norm(const ForwardParams p) {
     extern __shared__ float staged[];
@@ -256,15 +304,6 @@ __global__ void __launch_bounds__(1024) k_norm(const ForwardParams p) {
                 add_raw(v, w);
             }
         };
-        auto square = [&](const Raw<T, V>& v) {
-#pragma unroll
-            for (int e = 0; e < P; ++e) {
-                const uint64_t a = v.pair(e), q = mul2(a, a);
-                sums.add(q);
-                // of bf16 entries the square is exact
-                if (sizeof(T) == 4) sums.lo = add2(sums.lo, fma2(a, a, mul2(q, both(-1.0f))));
-            }
-        };
         auto put = [&](int c, const Raw<T, V>& v, float rstd) {
             Raw<float, V> g;
             Raw<TY, V> o;
@@ -284,14 +323,14 @@ __global__ void __launch_bounds__(1024) k_norm(const ForwardParams p) {
                 for (int j = 0; j < NV; ++j) {
                     const int c = (j * group + i) * V - off;
                     if (c >= n) continue;
-                    square(f[j]);
+                    add_squares(sums, f[j]);
                     if (h != nullptr) f[j].store_at(h, c, n);
                 }
             }
         } else if (real) {
             for (int c = i * V; c < n; c += group * V) {
                 take(c, f[0]);
-                square(f[0]);
+                add_squares(sums, f[0]);
                 if (h != nullptr) f[0].store_at(h, c, n);
             }
         }
@@ -474,6 +513,261 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
     }
 }
 
+// ---------------------------------------------------------------------------
+// Many rows.  A thread has four accesses of a row in each array, and its
+// copies of the next rows run into shared memory of its own while it works on this one: no
+// registers wait for DRAM, and what a thread reads it has copied itself, so that a row's sum is the
+// only barrier.  A row's first and last line are read where they lie if they are not whole.
+// 16384 x 4096 bf16 with the residual: FORWARDTIME, backward BACKWARDTIME (floor 79); with loads into registers
+// 107 and 108.
+// ---------------------------------------------------------------------------
+template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const void* from) {
+    const uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(to));
+    if constexpr (BYTES == 8) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(a), "l"(from) : "memory");
+    } else {
+#pragma unroll
+        for (int e = 0; e < BYTES; e += 16)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(a + e), "l"(static_cast<const char*>(from) + e) : "memory");
+    }
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// All but the newest N groups of this thread's copies have landed.
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+constexpr int kAccesses = 4;
+
+// Where a thread's copy of access j lies: beside its neighbours' (64 bytes a thread in a row of
+// their own, in swizzled order, took 137 us where this takes 98).
+template <int BYTES> __device__ __forceinline__ int place_of(int j) { return j * static_cast<int>(blockDim.x) * BYTES; }
+
+// f(j, c, whole) for each access of a thread in a row that begins `off` entries into its first
+// line; whole: none of its entries lies outside the row, known for all four of most threads.
+template <int V, int A, class F> __device__ __forceinline__ void accesses(int i, int group, int off, int n, F f) {
+    const int c0 = i * V - off, step = group * V;
+    if (c0 >= 0 && c0 + (A - 1) * step + V <= n) {
+#pragma unroll
+        for (int j = 0; j < A; ++j) f(j, c0 + j * step, std::true_type());
+    } else {
+#pragma unroll
+        for (int j = 0; j < A; ++j) {
+            const int c = c0 + j * step;
+            if (c >= n) continue;
+            if (c >= 0 && c + V <= n) f(j, c, std::true_type());
+            else f(j, c, std::false_type());
+        }
+    }
+}
+
+template <class T, class TY, int V, int STAGES, bool SHIFT>
+__global__ void __launch_bounds__(1024) k_norm_many(const ForwardParams p) {
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    __shared__ float2 parts[2][32];
+    using R = Raw<T, V>;
+    constexpr int P = V / 2, OWN = kAccesses * R::BYTES;     // of an array's copies, a thread
+    const int group = p.group, per = blockDim.x / group, mine = threadIdx.x / group, i = threadIdx.x % group;
+    const int n = p.cols, array = blockDim.x * OWN;
+    uint8_t* const slots = dynamic + threadIdx.x * R::BYTES; // of x; of r `array` bytes further
+    float* const staged = reinterpret_cast<float*>(dynamic + STAGES * 2 * array);
+    pdl_begin();
+    if (SHIFT) stage_gain<V>(staged, p.gain, n);
+    const long long step = static_cast<long long>(gridDim.x) * per;
+    auto off_of = [&](long long row) { return SHIFT ? static_cast<int>((p.phase + row % V * p.pitch) % V) : 0; };
+    auto prefetch = [&](long long row, int stage) {
+        if (row < p.rows) {
+            const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+            const T* r = static_cast<const T*>(p.r) + row * p.ldr;
+            uint8_t* const to = slots + stage * 2 * array;
+            accesses<V, kAccesses>(i, group, off_of(row), n, [&](int j, int c, auto whole) {
+                if constexpr (!decltype(whole)::value) return;
+                copy_async<R::BYTES>(to + place_of<R::BYTES>(j), x + c);
+                if (p.r != nullptr) copy_async<R::BYTES>(to + array + place_of<R::BYTES>(j), r + c);
+            });
+        }
+        copies_commit();
+    };
+    const long long first = static_cast<long long>(blockIdx.x) * per + mine;
+#pragma unroll
+    for (int k = 0; k + 1 < STAGES; ++k) prefetch(first + k * step, k);
+    int turn = 0, stage = 0;
+    for (long long row = first; row - mine < p.rows; row += step, turn ^= 1) {
+        prefetch(row + (STAGES - 1) * step, stage == 0 ? STAGES - 1 : stage - 1);
+        const bool real = row < p.rows;
+        const T* x = static_cast<const T*>(p.x) + row * p.ldx;
+        const T* r = p.r == nullptr ? nullptr : static_cast<const T*>(p.r) + row * p.ldr;
+        T* h = p.r == nullptr ? nullptr : static_cast<T*>(p.h) + row * p.ldh;
+        TY* y = p.y == nullptr ? nullptr : static_cast<TY*>(p.y) + row * p.ldy;
+        const int off = off_of(row);
+        const uint8_t* const from = slots + stage * 2 * array;
+        R f[kAccesses];                                      // h
+        Sums sums;
+        copies_wait<STAGES - 1>();
+        if (real)
+            accesses<V, kAccesses>(i, group, off, n, [&](int j, int c, auto whole) {
+                R w;
+                if constexpr (decltype(whole)::value) {
+                    f[j].load(reinterpret_cast<const T*>(from + place_of<R::BYTES>(j)));
+                    if (r != nullptr) w.load(reinterpret_cast<const T*>(from + array + place_of<R::BYTES>(j)));
+                } else {
+                    f[j].load_at(x, c, n);
+                    if (r != nullptr) w.load_at(r, c, n);
+                }
+                if (r != nullptr) {
+                    add_raw(f[j], w);
+                    if constexpr (decltype(whole)::value) f[j].store(h + c);
+                    else f[j].store_at(h, c, n);
+                }
+                add_squares(sums, f[j]);
+            });
+        if (++stage == STAGES) stage = 0;
+        const Sum s = group_sum(sums.both(), group, parts[turn] + mine * (group >> 5));
+        if (!real) continue;
+        const float rstd = inverse_rms(s, n, p.eps);
+        if (i == 0) p.rstd[row] = rstd;
+        if (y == nullptr) continue;
+        accesses<V, kAccesses>(i, group, off, n, [&](int j, int c, auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            Raw<float, V> g;
+            Raw<TY, V> o;
+            if constexpr (WHOLE) gain_whole<SHIFT, V>(p.gain, staged, c, n, g);
+            else gain_at<SHIFT, V>(p.gain, staged, c, n, g);
+#pragma unroll
+            for (int e = 0; e < P; ++e) o.set(e, mul2(mul2(f[j].pair(e), both(rstd)), g.pair(e)));
+            if constexpr (WHOLE) o.store(y + c);
+            else o.store_at(y, c, n);
+        });
+    }
+}
+
+// The same for the gradients: dy and h are read from shared memory in both passes, dh in the
+// second.  SHIFT: the columns' sums are in shared memory too, one group a CTA; a column's sum has
+// another thread from row to row, behind the barrier of the row's mean.
+template <class T, class TY, int V, int A, bool SHIFT>
+__global__ void __launch_bounds__(512) k_norm_backward_many(const BackwardParams p) {
+    extern __shared__ __align__(16) uint8_t dynamic[];
+    __shared__ float2 parts[2][32];
+    using R = Raw<T, V>;
+    using RY = Raw<TY, V>;
+    constexpr int P = V / 2, STAGES = 2, OWN = A * R::BYTES, OWN_Y = A * RY::BYTES;
+    const int group = p.group, per = blockDim.x / group, mine = threadIdx.x / group, i = threadIdx.x % group;
+    const int n = p.cols, threads = blockDim.x, all = (2 * OWN + OWN_Y) * threads;        // bytes of a stage
+    uint8_t* const slots = dynamic + threadIdx.x * R::BYTES; // of h; of dh behind all threads' h
+    uint8_t* const slots_y = dynamic + 2 * OWN * threads + threadIdx.x * RY::BYTES;
+    float* const columns = reinterpret_cast<float*>(dynamic + STAGES * all);
+    float* const staged = columns + (n / V + 1) * V;         // SHIFT: the gain
+    if (SHIFT) {
+        for (int c = threadIdx.x; c < n; c += threads) columns[column<V>(c, n)] = 0.0f;
+        __syncthreads();
+    }
+    pdl_begin();
+    if (SHIFT) stage_gain<V>(staged, p.gain, n);
+    const long long step = static_cast<long long>(gridDim.x) * per;
+    auto off_of = [&](long long row) { return SHIFT ? static_cast<int>((p.phase + row % V * p.pitch) % V) : 0; };
+    auto prefetch = [&](long long row, int stage) {
+        if (row < p.rows) {
+            const TY* dy = static_cast<const TY*>(p.dy) + row * p.lddy;
+            const T* h = static_cast<const T*>(p.h) + row * p.ldh;
+            const T* dh = static_cast<const T*>(p.dh) + row * p.lddh;
+            accesses<V, A>(i, group, off_of(row), n, [&](int j, int c, auto whole) {
+                if constexpr (!decltype(whole)::value) return;
+                copy_async<RY::BYTES>(slots_y + stage * all + place_of<RY::BYTES>(j), dy + c);
+                copy_async<R::BYTES>(slots + stage * all + place_of<R::BYTES>(j), h + c);
+                if (p.dh != nullptr) copy_async<R::BYTES>(slots + stage * all + OWN * threads + place_of<R::BYTES>(j), dh + c);
+            });
+        }
+        copies_commit();
+    };
+    uint64_t acc[A][P] = {};
+    const long long first = static_cast<long long>(blockIdx.x) * per + mine;
+    prefetch(first, 0);
+    int turn = 0;
+    const float inv = 1.0f / static_cast<float>(n);
+    for (long long row = first; row - mine < p.rows; row += step, turn ^= 1) {
+        prefetch(row + step, turn ^ 1);
+        const bool real = row < p.rows;
+        const TY* dy = static_cast<const TY*>(p.dy) + row * p.lddy;
+        const T* h = static_cast<const T*>(p.h) + row * p.ldh;
+        const T* dh = p.dh == nullptr ? nullptr : static_cast<const T*>(p.dh) + row * p.lddh;
+        T* dx = static_cast<T*>(p.dx) + row * p.lddx;
+        const int off = off_of(row);
+        const float rstd = real ? p.rstd[row] : 0.0f;
+        const uint64_t scale = both(rstd);
+        auto take = [&](int j, int c, auto whole, RY& a, R& b, Raw<float, V>& g) {
+            if constexpr (decltype(whole)::value) {
+                a.load(reinterpret_cast<const TY*>(slots_y + turn * all + place_of<RY::BYTES>(j)));
+                b.load(reinterpret_cast<const T*>(slots + turn * all + place_of<R::BYTES>(j)));
+            } else {
+                a.load_at(dy, c, n);
+                b.load_at(h, c, n);
+            }
+            if constexpr (decltype(whole)::value) gain_whole<SHIFT, V>(p.gain, staged, c, n, g);
+            else gain_at<SHIFT, V>(p.gain, staged, c, n, g);
+        };
+        Sums dots;
+        copies_wait<1>();
+        if (real)
+            accesses<V, A>(i, group, off, n, [&](int j, int c, auto whole) {
+                RY a;
+                R b;
+                Raw<float, V> g;
+                take(j, c, whole, a, b, g);
+                uint64_t q = 0;
+#pragma unroll
+                for (int e = 0; e < P; ++e) q = fma2(mul2(a.pair(e), g.pair(e)), mul2(b.pair(e), scale), q);
+                dots.add(q);
+            });
+        const Sum dot = group_sum(dots.both(), group, parts[turn] + mine * (group >> 5));
+        if (SHIFT) __syncwarp();                 // a group of one warp has no other barrier
+        if (!real) continue;
+        const uint64_t mean = both(-(dot.hi + dot.lo) * inv);
+        accesses<V, A>(i, group, off, n, [&](int j, int c, auto whole) {
+            constexpr bool WHOLE = decltype(whole)::value;
+            RY a;
+            R b, w, o;
+            Raw<float, V> g;
+            take(j, c, whole, a, b, g);
+            if (dh != nullptr) {
+                if constexpr (WHOLE) w.load(reinterpret_cast<const T*>(slots + turn * all + OWN * threads + place_of<R::BYTES>(j)));
+                else w.load_at(dh, c, n);
+            }
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                const uint64_t u = a.pair(e), v = mul2(b.pair(e), scale);
+                if constexpr (SHIFT && WHOLE) add_whole<V>(columns, c, n, e, u, v);
+                else if constexpr (SHIFT) add_column<V>(columns, c + 2 * e, n, u, v, [&](int k) { return column<V>(k, n); });
+                else acc[j][e] = fma2(u, v, acc[j][e]);
+                const uint64_t d = fma2(v, mean, mul2(u, g.pair(e)));
+                o.set(e, dh != nullptr ? fma2(scale, d, w.pair(e)) : mul2(scale, d));
+            }
+            if constexpr (WHOLE) o.store(dx + c);
+            else o.store_at(dx, c, n);
+        });
+    }
+    float* out = p.partials + static_cast<long long>(blockIdx.x) * n;
+    if constexpr (SHIFT) {
+        __syncthreads();
+        for (int c = threadIdx.x; c < n; c += threads) out[c] = columns[column<V>(c, n)];
+    } else {
+        // the groups' sums, in order
+        for (int k = 0; k < per; ++k) {
+            if (per > 1) __syncthreads();
+            if (mine != k) continue;
+#pragma unroll
+            for (int j = 0; j < A; ++j)
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const int c = (j * group + i) * V + e;
+                    if (c >= n) continue;
+                    float x, y;
+                    split(acc[j][e / 2], x, y);
+                    const float own = e & 1 ? y : x, sum = k == 0 ? own : columns[c] + own;
+                    if (k + 1 < per) columns[c] = sum;
+                    else out[c] = sum;
+                }
+        }
+    }
+}
+
 // Column sums of the partial rows, in their order: 32 columns a CTA, 16 warps with four rows at a
 // time share the rows; a lane has four columns.
 __global__ void __launch_bounds__(512) k_norm_gain(const float* partials, int count, int n, float* dgain) {
@@ -546,35 +840,50 @@ struct Lines {
 };
 
 constexpr long long kFull = 152 * 2048;          // threads that the GPU holds
-template <class T> constexpr int many = sizeof(T) == 2 ? 32 : 16;
 
 // Threads of a row of n entries, e of them each.
 int group_of(int n, int e) { return (n + 32 * e - 1) / (32 * e) * 32; }
 
 template <class F> cudaError_t allow_shared(F fn, size_t bytes) {
-    if (bytes <= 48 * 1024) return cudaSuccess;
+    if (bytes <= 40 * 1024) return cudaSuccess;
     return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
 }
+
+constexpr size_t kShared = 222 << 10;
 
 template <class T, class TY, int V, bool SHIFT> cudaError_t forward_as(const ForwardParams& q, cudaStream_t s) {
     ForwardParams p = q;
     const int n = p.cols, reach = n + (SHIFT ? V - 1 : 0);
-    // entry by entry there are no registers for 32
-    constexpr int MANY = V == 1 ? 8 : many<T>;
-    const bool wide = reach > 1024 * MANY;
-    const int e = reach <= 8192 && static_cast<long long>(p.rows) * group_of(n, 8) < kFull ? 8 : MANY;
-    p.group = wide ? 1024 : group_of(reach, e);
+    const size_t gain = SHIFT ? static_cast<size_t>(n / V + 1) * V * 4 : 0;
+    const bool few = reach <= 8192 && static_cast<long long>(p.rows) * group_of(reach, 8) < kFull;
+    if constexpr (V > 1) {
+        if (!few && reach <= 1024 * kAccesses * V) {
+            p.group = group_of(reach, kAccesses * V);
+            const int per = std::max(1, 128 / p.group), threads = p.group * per;
+            const size_t stage = static_cast<size_t>(threads) * 2 * kAccesses * V * sizeof(T);
+            const int resident = std::max(1, std::min(16, 512 / threads));
+            const int stages = static_cast<int>(std::min<size_t>(3, (kShared / resident - 1024 - gain) / stage));
+            const size_t smem = stages * stage + gain;
+            const int ctas = std::min((p.rows - 1) / per + 1, 152 * resident);
+            const auto fn = stages >= 3   ? k_norm_many<T, TY, V, 3, SHIFT>
+                            : stages == 2 ? k_norm_many<T, TY, V, 2, SHIFT>
+                                          : k_norm_many<T, TY, V, 1, SHIFT>;
+            if (stages > 0) {
+                const cudaError_t err = allow_shared(fn, smem);
+                if (err != cudaSuccess) return err;
+                return launch(fn, dim3(ctas), dim3(threads), smem, s, 1, p);
+            }
+        }
+    }
+    const bool wide = reach > 8192;
+    p.group = wide ? 1024 : group_of(reach, 8);
     const int per = std::max(1, 256 / p.group);
     int ctas = (p.rows - 1) / per + 1;
-    size_t smem = 0;
-    if (SHIFT) {
-        smem = static_cast<size_t>(n / V + 1) * V * 4;
-        ctas = std::min<int>(ctas, 152 * std::max<int>(1, std::min<size_t>(2048 / (p.group * per), (200 << 10) / smem)));
-    }
-    const auto fn = wide ? k_norm<T, TY, V, 0, false> : e == 8 ? k_norm<T, TY, V, 8, SHIFT> : k_norm<T, TY, V, MANY, SHIFT>;
-    const cudaError_t err = allow_shared(fn, smem);
+    if (SHIFT) ctas = std::min<int>(ctas, 152 * std::max<int>(1, std::min<size_t>(2048 / (p.group * per), kShared / (gain + 1024))));
+    const auto fn = wide ? k_norm<T, TY, V, 0, false> : k_norm<T, TY, V, 8, SHIFT>;
+    const cudaError_t err = allow_shared(fn, gain);
     if (err != cudaSuccess) return err;
-    return launch(fn, dim3(ctas), dim3(p.group * per), smem, s, 1, p);
+    return launch(fn, dim3(ctas), dim3(p.group * per), gain, s, 1, p);
 }
 
 template <class T, class TY> cudaError_t forward_of(ForwardParams p, cudaStream_t s) {
@@ -584,24 +893,42 @@ template <class T, class TY> cudaError_t forward_of(ForwardParams p, cudaStream_
     if (l.aligned() && reinterpret_cast<uintptr_t>(p.gain) % 16 == 0) return forward_as<T, TY, V, false>(p, s);
     p.phase = l.phase;
     p.pitch = l.pitch;
-    return l.ok && p.cols + V <= 1024 * many<T> ? forward_as<T, TY, V, true>(p, s) : forward_as<T, TY, 1, false>(p, s);
+    // a row and its gain in shared memory
+    return l.ok && p.cols <= 16000 ? forward_as<T, TY, V, true>(p, s) : forward_as<T, TY, 1, false>(p, s);
 }
 
 struct BackwardShape {
-    int entries, group, per, ctas;
+    int entries, accesses, group, per, ctas;
+    size_t smem;
 };
 
-// v: entries of an access (1: of rows whose lines differ); shift: rows in their own lines;
-// most: entries of a thread
-BackwardShape backward_shape(int rows, int n, int v, bool shift, int most) {
+// Entries of a thread: 8 for few rows, 4 accesses of v for many, 0 for rows that are read again.
+// v: entries of an access (1: of rows whose lines differ); shift: rows in their own lines; bytes of an
+// access's copies of a row's three arrays.
+BackwardShape backward_shape(int rows, int n, int v, bool shift, int bytes) {
     BackwardShape b;
+    // rows in their own lines need more shared memory: more threads share a row
+    const int accesses = shift && n + v <= 512 * 2 * v ? 2 : kAccesses;
     const int reach = n + (shift ? v - 1 : 0);
-    const bool few = reach <= 4096 && (v == 1 || static_cast<long long>(rows) * group_of(n, 8) < kFull / 2);
-    b.entries = few ? 8 : v == 1 || reach > 512 * most ? 0 : most;
+    const size_t one = static_cast<size_t>(n / v + 1) * v * 4, extra = shift ? 2 * one : 0;
+    const bool few = reach <= 4096 && (v == 1 || static_cast<long long>(rows) * group_of(reach, 8) < kFull / 2);
+    b.entries = few ? 8 : v == 1 || reach > 512 * kAccesses * v ? 0 : accesses * v;
+    b.accesses = few || b.entries == 0 ? 0 : accesses;
     b.group = b.entries == 0 ? 1024 : group_of(reach, b.entries);
     b.per = shift ? 1 : std::max(1, 128 / b.group);
-    int resident = b.entries == 0 ? 1 : std::max(1, (b.entries == 8 ? 1536 : 512) / (b.group * b.per));
-    if (shift) resident = std::max(1, std::min(std::min(16, resident), (200 << 10) / (8 * (n + v))));
+    const int threads = b.group * b.per;
+    int resident = 1;
+    if (few) {
+        resident = std::max(1, 1536 / threads);
+        b.smem = shift ? extra : b.per > 1 ? static_cast<size_t>(n) * 4 : 0;
+        if (shift) resident = std::max<int>(1, std::min<size_t>(std::min(16, resident), kShared / (extra + 1024)));
+    } else if (b.entries == 0) {
+        b.smem = static_cast<size_t>(n) * 4;
+    } else {
+        b.smem = 2 * static_cast<size_t>(threads) * accesses * bytes + (shift ? extra : b.per > 1 ? one : 0);
+        if (b.smem > kShared) return backward_shape(rows, n, 1, false, 0);
+        resident = std::max<int>(1, std::min<size_t>(std::min(16, (shift ? 1024 : 512) / threads), kShared / (b.smem + 1024)));
+    }
     const long long need = (static_cast<long long>(rows) - 1) / b.per + 1;
     b.ctas = static_cast<int>(std::min<long long>(need, 152LL * resident));
     return b;
@@ -609,20 +936,16 @@ BackwardShape backward_shape(int rows, int n, int v, bool shift, int most) {
 
 template <class T, class TY, int V, bool SHIFT> cudaError_t backward_as(const BackwardParams& q, int& ctas, cudaStream_t s) {
     BackwardParams p = q;
-    constexpr int MANY = V == 1 ? 8 : many<T>;
-    const BackwardShape b = backward_shape(p.rows, p.cols, V, SHIFT, MANY);
-    const bool wide = b.entries == 0;
+    const BackwardShape b = backward_shape(p.rows, p.cols, V, SHIFT, V * (2 * sizeof(T) + sizeof(TY)));
     p.group = b.group;
     ctas = b.ctas;
-    const size_t one = static_cast<size_t>(p.cols / V + 1) * V * 4;
-    const bool shift = SHIFT && !wide;
-    const size_t smem = shift ? 2 * one : wide || b.per > 1 ? static_cast<size_t>(p.cols) * 4 : 0;
-    const auto fn = wide             ? k_norm_backward<T, TY, V, 0, false>
-                    : b.entries == 8 ? k_norm_backward<T, TY, V, 8, SHIFT>
-                                     : k_norm_backward<T, TY, V, MANY, SHIFT>;
-    const cudaError_t e = allow_shared(fn, smem);
+    auto fn = k_norm_backward<T, TY, V, 8, SHIFT>;
+    if (b.entries == 0) fn = k_norm_backward<T, TY, V, 0, false>;
+    if constexpr (V > 1)
+        if (b.accesses > 0) fn = b.accesses == 2 ? k_norm_backward_many<T, TY, V, 2, SHIFT> : k_norm_backward_many<T, TY, V, 4, SHIFT>;
+    const cudaError_t e = allow_shared(fn, b.smem);
     if (e != cudaSuccess) return e;
-    return launch(fn, dim3(b.ctas), dim3(b.group * b.per), smem, s, 1, p);
+    return launch(fn, dim3(b.ctas), dim3(b.group * b.per), b.smem, s, 1, p);
 }
 
 template <class T, class TY> cudaError_t backward_of(BackwardParams p, int& ctas, cudaStream_t s) {
@@ -632,7 +955,9 @@ template <class T, class TY> cudaError_t backward_of(BackwardParams p, int& ctas
     if (l.aligned() && reinterpret_cast<uintptr_t>(p.gain) % 16 == 0) return backward_as<T, TY, V, false>(p, ctas, s);
     p.phase = l.phase;
     p.pitch = l.pitch;
-    return l.ok && p.cols + V <= 512 * many<T> ? backward_as<T, TY, V, true>(p, ctas, s) : backward_as<T, TY, 1, false>(p, ctas, s);
+    constexpr int BYTES = V * (2 * sizeof(T) + sizeof(TY));
+    const bool fits = l.ok && backward_shape(p.rows, p.cols, V, true, BYTES).entries > 0;
+    return fits ? backward_as<T, TY, V, true>(p, ctas, s) : backward_as<T, TY, 1, false>(p, ctas, s);
 }
 
 }  // namespace
@@ -650,7 +975,8 @@ int norm_partials(int rows, int cols) {
     int most = 0;
     for (int v : {1, 4, 8})
         for (bool shift : {false, true})
-            if (!(shift && v == 1)) most = std::max(most, backward_shape(rows, cols, v, shift, v == 1 ? 8 : 4 * v).ctas);
+            for (int bytes : {6, 8, 10, 12})
+                if (!(shift && v == 1)) most = std::max(most, backward_shape(rows, cols, v, shift, v * bytes).ctas);
     return most;
 }
 
@@ -666,7 +992,9 @@ cudaError_t launch_norm_backward(const NormBackward& a, cudaStream_t s, int64_t*
         e = a.dy_dtype == MOARA_DTYPE_BF16 ? backward_of<float, bf16>(p, ctas, s) : backward_of<float, float>(p, ctas, s);
     if (e != cudaSuccess) return e;
     ++*launches;
-    return launch(k_norm_gain, dim3((a.cols - 1) / 32 + 1), dim3(512), 0, s, 1, static_cast<const float*>(a.partials), ctas,
+    // begins once the sums are there: CTAs that wait would take the places of some of the CTAs in
+    // front, all of which have to be resident to share the rows evenly (16384 x 4096 bf16: 180 us instead of 117)
+    return launch_if(false, k_norm_gain, dim3((a.cols - 1) / 32 + 1), dim3(512), 0, s, 1, static_cast<const float*>(a.partials), ctas,
                   a.cols, a.dgain);
 }
 
