@@ -9,7 +9,6 @@
 #include <atomic>
 #include <cstddef>
 
-#include "f32x2.cuh"
 #include "launch.cuh"
 #include "layers.h"
 #include "tc_ptx.cuh"
@@ -19,7 +18,7 @@ namespace moara {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
-constexpr double kLn2 = 0.69314718055994530942;
+constexpr float kLn2 = 0.69314718f, kLn2Rest = -1.90465421e-9f;      // ln 2 in two fp32 numbers
 
 struct LossParams {
     const void* z;
@@ -59,8 +58,31 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
-// 16 bytes of a row as pairs of fp32 numbers, their largest (NaN left out: it returns in the
-// sum), and exponentials relative to a reference: powers of two, whose argument is one fused
+// A sum held in two fp32 numbers: what an addition rounds off goes to the second.
+struct Sum {
+    float hi = 0.0f, lo = 0.0f;
+    __device__ __forceinline__ void add(float x) {
+        const float s = hi + x, b = s - hi;
+        lo += (hi - (s - b)) + (x - b);
+        hi = s;
+    }
+    // - x ln 2
+    __device__ __forceinline__ void subtract_ln2(float x) {
+        const float y = x * kLn2;
+        add(-y);
+        lo -= fmaf(x, kLn2, -y) + x * kLn2Rest;
+    }
+    // beside an infinite sum there is NaN
+    __device__ __forceinline__ float value() const { return fabsf(hi) < INFINITY ? hi + lo : hi; }
+    __device__ __forceinline__ float minus(float x) const {
+        Sum s = *this;
+        s.add(-x);
+        return s.value();
+    }
+};
+
+// 16 bytes of a row as fp32, their largest (NaN left out: it returns in the sum), and
+// exponentials relative to a reference: powers of two, whose argument is one fused
 // operation for bf16 logits, an error far below the gradient's rounding; fp32 logits take z - ref
 // exactly as far as fp32 holds it, and what the product with log2 e rounds off as a factor
 // (1 + its natural power).
@@ -68,38 +90,32 @@ template <class T> struct Line;
 
 template <> struct Line<float> {
     static constexpr int N = 4;
-    static __device__ __forceinline__ uint64_t pair(const uint4& w, int e) {
-        return e == 0 ? f32x2(__uint_as_float(w.x), __uint_as_float(w.y)) : f32x2(__uint_as_float(w.z), __uint_as_float(w.w));
-    }
     static __device__ __forceinline__ float top(const uint4& w) {
         return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
     }
     static __device__ __forceinline__ float reference(float top) { return top; }
-    static __device__ __forceinline__ uint64_t exponentials(uint64_t z, float ref) {
-        const uint64_t t = add2(z, both(-ref)), l = both(kLog2e), x = mul2(t, l);
-        float a, b, c, d;
-        split(x, a, b);
+    static __device__ __forceinline__ float exponential(float z, float ref) {
+        const float t = z - ref, x = t * kLog2e, y = ex2(x);
         // of minus infinity the rest is NaN: its exponential is 0 whatever it is
-        split(fma2(t, l, mul2(x, both(-1.0f))), c, d);
-        const uint64_t y = f32x2(ex2(a), ex2(b));
-        return fma2(y, mul2(f32x2(a == -INFINITY ? 0.0f : c, b == -INFINITY ? 0.0f : d), both(0.69314718f)), y);
+        const float rest = x == -INFINITY ? 0.0f : fmaf(t, kLog2e, -x);
+        return fmaf(y, rest * 0.69314718f, y);
+    }
+    static __device__ __forceinline__ void exponentials(const uint4& w, float ref, float (&e)[4]) {
+        e[0] = exponential(__uint_as_float(w.x), ref);
+        e[1] = exponential(__uint_as_float(w.y), ref);
+        e[2] = exponential(__uint_as_float(w.z), ref);
+        e[3] = exponential(__uint_as_float(w.w), ref);
     }
     static __device__ __forceinline__ float apart(float x) { return expf(x); }      // of a difference of references
-    static __device__ __forceinline__ double natural(float ref) { return ref; }
-    static __device__ __forceinline__ uint4 pack(const uint64_t (&v)[2]) {
-        float a, b, c, d;
-        split(v[0], a, b);
-        split(v[1], c, d);
-        return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+    static __device__ __forceinline__ void subtract(Sum& s, float ref) { s.add(-ref); }
+    static __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
+        return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     }
     static __device__ __forceinline__ float rounded(float x) { return x; }
 };
 
 template <> struct Line<__nv_bfloat16> {
     static constexpr int N = 8;
-    static __device__ __forceinline__ uint64_t pair(const uint4& w, int e) {
-        return widen2(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w);
-    }
     static __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
         uint32_t y;
         asm("max.bf16x2 %0, %1, %2;" : "=r"(y) : "r"(a), "r"(b));
@@ -110,53 +126,50 @@ template <> struct Line<__nv_bfloat16> {
         return fmaxf(__uint_as_float(t << 16), __uint_as_float(t & 0xFFFF0000u));
     }
     static __device__ __forceinline__ float reference(float top) { return top * kLog2e; }
-    static __device__ __forceinline__ uint64_t exponentials(uint64_t z, float ref) {
-        float a, b;
-        split(fma2(z, both(kLog2e), both(-ref)), a, b);
-        return f32x2(ex2(a), ex2(b));
+    static __device__ __forceinline__ float exponential(float z, float ref) { return ex2(fmaf(z, kLog2e, -ref)); }
+    static __device__ __forceinline__ void exponentials(const uint4& w, float ref, float (&e)[8]) {
+        const uint32_t a[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            e[2 * k] = exponential(__uint_as_float(a[k] << 16), ref);
+            e[2 * k + 1] = exponential(__uint_as_float(a[k] & 0xFFFF0000u), ref);
+        }
     }
     static __device__ __forceinline__ float apart(float x) { return ex2(x); }
-    static __device__ __forceinline__ double natural(float ref) { return ref * kLn2; }
-    static __device__ __forceinline__ uint32_t pack2(uint64_t v) {
-        float a, b;
-        split(v, a, b);
+    static __device__ __forceinline__ void subtract(Sum& s, float ref) { s.subtract_ln2(ref); }
+    static __device__ __forceinline__ uint32_t pack2(float a, float b) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
     }
-    static __device__ __forceinline__ uint4 pack(const uint64_t (&v)[4]) {
-        return make_uint4(pack2(v[0]), pack2(v[1]), pack2(v[2]), pack2(v[3]));
+    static __device__ __forceinline__ uint4 pack(const float (&v)[8]) {
+        return make_uint4(pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7]));
     }
     static __device__ __forceinline__ __nv_bfloat16 rounded(float x) { return __float2bfloat16_rn(x); }
 };
 
-// A sum held in two fp32 numbers: what an addition rounds off goes to the second.
-struct Sum {
-    float hi = 0.0f, lo = 0.0f;
-    __device__ __forceinline__ void add(float x) {
-        const float s = hi + x, b = s - hi;
-        lo += (hi - (s - b)) + (x - b);
-        hi = s;
-    }
-};
+constexpr int kLossThreads = 384;
+constexpr int kChunks = 4;             // of a part, copied apart
 
 struct LossCtl {
-    uint64_t full;
+    uint64_t full[kChunks];
     int abort;
     float top, sum, at;            // of this CTA's part: reference, sum, the target's logit if it is here
     float factor, gain;            // of the gradient
     int hit;
-    float part[2][32];
+    float2 part[2][16];            // of the warps: reference, sum
 };
 
 __device__ __forceinline__ float ld_cluster_f32(uint32_t a) { return __uint_as_float(ptx::ld_cluster_u32(a)); }
 
 // A cluster of `split` CTAs takes rows a grid apart, each CTA a part of their columns, whose
-// whole 16-byte lines a bulk copy puts into shared memory, in the row's own alignment; the next
-// row's copy begins as soon as this one has been read.  The first and the last line are read where
-// they lie if they are not whole, with -infinity beside the part.  !STAGED: a part that is too
-// large for shared memory is read again from L2.
+// whole 16-byte lines bulk copies put into shared memory, in the row's own alignment, in four
+// chunks; the next row's copy of a chunk begins as soon as this row's gradient has been taken from it.
+// What lies in front of the first and behind the last whole line is read where it lies, an entry a
+// thread.  A thread's sum is relative to the largest logit that it has met, or one that is at most
+// 8 below it, so that the row is read twice, not three times.  !STAGED: a part that is too large for
+// shared memory is read again from L2.  8192 x 32000 bf16: LOSSTIME (floor 155).
 template <class T, bool STAGED>
-__global__ void __launch_bounds__(512, 3) k_policy_loss(const __grid_constant__ LossParams p) {
+__global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_constant__ LossParams p) {
     extern __shared__ __align__(16) uint8_t raw[];
     using L = Line<T>;
     constexpr int N = L::N;
@@ -167,56 +180,50 @@ __global__ void __launch_bounds__(512, 3) k_policy_loss(const __grid_constant__ 
     if (threadIdx.x == 0) {
         ctl.abort = 0;
         if (STAGED) {
-            ptx::mbar_init(ptx::smem_u32(&ctl.full), 1);
+            for (int c = 0; c < kChunks; ++c) ptx::mbar_init(ptx::smem_u32(&ctl.full[c]), 1);
             ptx::fence_barrier_init();
             ptx::fence_proxy_async_smem();
         }
     }
     __syncthreads();
     pdl_begin();
-    const uint32_t bar = ptx::smem_u32(&ctl.full), own = ptx::smem_u32(&ctl);
+    const uint32_t full = ptx::smem_u32(&ctl.full[0]), own = ptx::smem_u32(&ctl);
     const long long step = gridDim.x / p.split;
-    // a row's part in lines: entries in front of it in its first line, lines, whole ones among them
+    const int chunk = (p.part / N + kChunks) / kChunks;          // lines
+    // a row's part: its entries in front of the first whole line, and the whole lines
     struct Place {
-        const T* line0;
-        int off, lines, inner0, inner1;
+        const T* z;
+        int front, lines;
     };
     auto place = [&](long long row) {
-        const T* z = static_cast<const T*>(p.z) + row * p.ldz + first;
         Place x;
-        x.off = static_cast<int>(reinterpret_cast<uintptr_t>(z) & 15) / static_cast<int>(sizeof(T));
-        x.line0 = z - x.off;
-        x.lines = (x.off + len + N - 1) / N;
-        x.inner0 = x.off != 0;
-        x.inner1 = max(x.inner0, (x.off + len) / N);
+        x.z = static_cast<const T*>(p.z) + row * p.ldz + first;
+        x.front = min(len, static_cast<int>(-reinterpret_cast<uintptr_t>(x.z) & 15) / static_cast<int>(sizeof(T)));
+        x.lines = (len - x.front) / N;
         return x;
     };
-    auto copy = [&](const Place& x) {
-        const uint32_t bytes = (x.inner1 - x.inner0) * 16u;
-        if (bytes == 0) return;
-        ptx::mbar_arrive_expect_tx(bar, bytes);
+    // an empty chunk's phase ends all the same
+    auto copy = [&](const Place& x, int c) {
+        const int from = c * chunk, to = min(x.lines, (c + 1) * chunk);
+        const uint32_t bytes = to > from ? (to - from) * 16u : 0u;
+        ptx::mbar_arrive_expect_tx(full + 8 * c, bytes);
         for (uint32_t at = 0; at < bytes; at += 16384)
-            ptx::bulk_load(ptx::smem_u32(raw) + x.inner0 * 16 + at, reinterpret_cast<const uint8_t*>(x.line0) + x.inner0 * 16 + at,
-                           min(16384u, bytes - at), bar);
+            ptx::bulk_load(ptx::smem_u32(raw) + from * 16 + at, reinterpret_cast<const uint8_t*>(x.z + x.front) + from * 16ll + at,
+                           min(16384u, bytes - at), full + 8 * c);
     };
     long long row = blockIdx.x / p.split;
     Place x = place(row);
-    if (STAGED && threadIdx.x == 0) copy(x);
+    if (STAGED && threadIdx.x == 0)
+        for (int c = 0; c < kChunks; ++c) copy(x, c);
     uint32_t phase = 0;
     Sum sums[3];                                 // of the first thread: loss, KL term, clipped
-    for (; row < p.rows; row += step) {
-        auto fetch = [&](int line) {
-            if (line >= x.inner0 && line < x.inner1)
-                return STAGED ? reinterpret_cast<const uint4*>(raw)[line] : reinterpret_cast<const uint4*>(x.line0)[line];
-            uint4 w;
-            T* t = reinterpret_cast<T*>(&w);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int c = line * N + e - x.off;
-                t[e] = c >= 0 && c < len ? x.line0[line * N + e] : L::rounded(-INFINITY);
-            }
-            return w;
-        };
+    for (; row < p.rows; row += step, phase ^= 1) {
+        const bool more = row + step < p.rows;
+        const uint4* const lines = STAGED ? reinterpret_cast<const uint4*>(raw) : reinterpret_cast<const uint4*>(x.z + x.front);
+        // the entry beside the lines that this thread has, or -1
+        int beside = static_cast<int>(threadIdx.x);
+        if (beside >= x.front) beside += x.lines * N;
+        if (beside >= len) beside = -1;
         // what the first thread needs of the token, fetched beside the row
         int64_t target = 0;
         float w = 0.0f, a = 0.0f, old = 0.0f, other = 0.0f;
@@ -227,49 +234,71 @@ __global__ void __launch_bounds__(512, 3) k_policy_loss(const __grid_constant__ 
             old = p.old_logp[row];
             if (p.ref_logp != nullptr) other = p.ref_logp[row];
         }
-        if (STAGED && x.inner1 > x.inner0) {
-            if (!ptx::mbar_wait(bar, phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit)) wait_drain(bar, phase);
-            phase ^= 1;
+        // top: the thread's largest logit when its reference was taken
+        float top = -INFINITY, ref = 0.0f, sum = 0.0f;
+        for (int c = 0; c < kChunks; ++c) {
+            if (STAGED && !ptx::mbar_wait(full + 8 * c, phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
+                wait_drain(full + 8 * c, phase);
+            const int end = min(x.lines, (c + 1) * chunk);
+            for (int i = c * chunk + threadIdx.x; i < end; i += blockDim.x) {
+                const uint4 v = lines[i];
+                const float high = L::top(v);
+                if (high > top + 8.0f) {
+                    const float to = L::reference(high);
+                    // of a first finite logit: nothing but zeros (or NaN) has been added
+                    if (top > -INFINITY) sum = sum * L::apart(ref - to);
+                    top = high;
+                    ref = to;
+                }
+                float e[N];
+                L::exponentials(v, ref, e);
+#pragma unroll
+                for (int k = N / 2; k > 0; k /= 2)
+#pragma unroll
+                    for (int y = 0; y < k; ++y) e[y] += e[y + k];
+                sum += e[0];
+            }
         }
-        auto all = [&](float v, bool largest, float* part) {
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) {
-                const float y = __shfl_xor_sync(0xffffffffu, v, o);
-                v = largest ? fmaxf(v, y) : v + y;
+        if (beside >= 0) {
+            const float v = static_cast<float>(x.z[beside]);
+            if (v > top + 8.0f) {
+                const float to = L::reference(v);
+                if (top > -INFINITY) sum *= L::apart(ref - to);
+                top = v;
+                ref = to;
             }
-            if (lane == 0) part[warp] = v;
-            __syncthreads();
-            v = lane < warps ? part[lane] : largest ? -INFINITY : 0.0f;
-#pragma unroll
-            for (int o = 16; o > 0; o /= 2) {
-                const float y = __shfl_xor_sync(0xffffffffu, v, o);
-                v = largest ? fmaxf(v, y) : v + y;
-            }
-            return v;
+            sum += L::exponential(v, ref);
+        }
+        // all threads' relative to their largest reference: within the warp, then the CTA
+        auto join = [&](float& top, float& sum, int most) {
+            float high = top;
+            for (int o = most / 2; o > 0; o /= 2) high = fmaxf(high, __shfl_xor_sync(0xffffffffu, high, o));
+            // what has no finite logit has a sum of 0, or NaN
+            sum = top > -INFINITY ? sum * L::apart(top - high) : sum;
+            for (int o = most / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+            top = high;
         };
-        float top = -INFINITY;
-#pragma unroll 4
-        for (int i = threadIdx.x; i < x.lines; i += blockDim.x) top = fmaxf(top, L::top(fetch(i)));
-        top = all(top, true, ctl.part[0]);
-        // a part without a finite logit: its exponentials are 0 (or NaN, or infinity's)
-        const float ref = top == -INFINITY ? 0.0f : L::reference(top);
-        uint64_t pairs = 0;
-#pragma unroll 4
-        for (int i = threadIdx.x; i < x.lines; i += blockDim.x) {
-            const uint4 v = fetch(i);
-#pragma unroll
-            for (int e = 0; e < N / 2; ++e) pairs = add2(pairs, L::exponentials(L::pair(v, e), ref));
+        float base = top > -INFINITY ? ref : -INFINITY;
+        join(base, sum, 32);
+        float2* const part = ctl.part[phase];
+        if (lane == 0) part[warp] = make_float2(base, sum);
+        __syncthreads();
+        {
+            const float2 t = lane < warps ? part[lane] : make_float2(-INFINITY, 0.0f);
+            base = t.x;
+            sum = t.y;
+            join(base, sum, 16);
+            base = __shfl_sync(0xffffffffu, base, 0);
+            sum = __shfl_sync(0xffffffffu, sum, 0);
         }
-        float sum, odd;
-        split(pairs, sum, odd);
-        sum = all(sum + odd, false, ctl.part[1]);
-        const bool ok = *abort_flag == 0;        // the same in every thread: a wait ran out before the barriers above
+        const bool ok = *abort_flag == 0;        // the same in every thread: a wait ran out before the barrier above
+        const float mine = base == -INFINITY ? 0.0f : base;             // this part's reference
         if (threadIdx.x == 0) {
             const bool counts = target >= 0 && target < p.vocab;
             const int column = counts ? static_cast<int>(target) : 0, owner = column / p.part;
-            ctl.top = top == -INFINITY ? -INFINITY : ref;
+            ctl.top = base;
             ctl.sum = ok ? sum : NAN;
-            if (counts && owner == rank) ctl.at = static_cast<float>(x.line0[column - first + x.off]);
+            if (counts && owner == rank) ctl.at = static_cast<float>(x.z[column - first]);
         }
         if (p.split > 1) {
             __syncwarp();
@@ -278,12 +307,12 @@ __global__ void __launch_bounds__(512, 3) k_policy_loss(const __grid_constant__ 
         if (threadIdx.x == 0) {
             const bool counts = target >= 0 && target < p.vocab;
             const int column = counts ? static_cast<int>(target) : 0, owner = column / p.part;
-            float tops[8], parts[8], base = -INFINITY, total = 0.0f, at = 0.0f;
+            float tops[8], parts[8], total = 0.0f, at = 0.0f;
             if (p.split == 1) {
-                base = ctl.top;
                 total = ctl.sum;
                 at = ctl.at;
             } else {
+                base = -INFINITY;
 #pragma unroll
                 for (int r = 0; r < 8; ++r) {
                     if (r >= p.split) break;
@@ -301,24 +330,25 @@ __global__ void __launch_bounds__(512, 3) k_policy_loss(const __grid_constant__ 
             }
             const float base0 = base == -INFINITY ? 0.0f : base;
             // log(total) from its exponent and the rest, which lies in [1, 2)
-            double lp;
+            Sum lp;
+            lp.add(at);
+            L::subtract(lp, base0);
             if (total > 0.0f && total < INFINITY) {
-                const int e = static_cast<int>(__float_as_uint(total) >> 23) - 127;
-                const float rest = logf(__uint_as_float((__float_as_uint(total) & 0x7FFFFFu) | 0x3F800000u));
-                lp = static_cast<double>(at) - (L::natural(base0) + (e * kLn2 + rest));
+                lp.subtract_ln2(static_cast<float>(static_cast<int>(__float_as_uint(total) >> 23) - 127));
+                lp.add(-logf(__uint_as_float((__float_as_uint(total) & 0x7FFFFFu) | 0x3F800000u)));
             } else {
-                lp = static_cast<double>(at) - (L::natural(base0) + logf(total));
+                lp.add(-logf(total));                       // without any probability, or not a number
             }
             float gain = 0.0f;
             const bool taken = counts && w != 0.0f;
             if (taken) {
-                const float rho = expf(static_cast<float>(lp - old));
+                const float rho = expf(lp.minus(old));
                 // NaN advantages and ratios stay NaN
                 const float bound = rho < p.low ? p.low : rho > p.high ? p.high : rho;
                 const bool clipped = bound * a < rho * a;
                 float loss = clipped ? -bound * a : -rho * a, d = clipped ? 0.0f : -rho * a;
                 if (p.ref_logp != nullptr) {
-                    const float y = static_cast<float>(other - lp), k = exp_beyond_linear(y);
+                    const float y = -lp.minus(other), k = exp_beyond_linear(y);
                     loss = fmaf(p.kl, k, loss);
                     d = fmaf(-p.kl, expm1f(y), d);
                     sums[1].add(k * w);
@@ -327,12 +357,11 @@ __global__ void __launch_bounds__(512, 3) k_policy_loss(const __grid_constant__ 
                 if (clipped) sums[2].add(w);
                 gain = w * d;
             }
-            if (rank == 0) p.logp[row] = counts ? static_cast<float>(lp) : 0.0f;
+            if (rank == 0) p.logp[row] = counts ? lp.value() : 0.0f;
             ctl.gain = gain;
             // relative to this part's reference; infinite where nothing of it is to be multiplied
-            ctl.factor = taken ? -gain * ((ctl.top == -INFINITY ? 1.0f : L::apart(ref - base0)) / total) : INFINITY;
-            // the target's place among the part's lines, none for -1
-            ctl.hit = counts && owner == rank ? column - first + x.off : -1;
+            ctl.factor = taken ? -gain * ((ctl.top == -INFINITY ? 1.0f : L::apart(mine - base0)) / total) : INFINITY;
+            ctl.hit = counts && owner == rank ? column - first : -1;
         }
         if (p.split > 1) {
             __syncwarp();
@@ -340,50 +369,59 @@ __global__ void __launch_bounds__(512, 3) k_policy_loss(const __grid_constant__ 
         } else {
             __syncthreads();
         }
-        const Place mine = x;
-        if (p.dz != nullptr && ok) {
-            const float factor = ctl.factor, gain = ctl.gain;
-            const int hit = ctl.hit, hit_line = hit < 0 ? -1 : hit / N;
-            const bool zero = factor == INFINITY;
-            T* dz = static_cast<T*>(p.dz) + row * p.lddz + first;
-            const bool same = (reinterpret_cast<uintptr_t>(dz) & 15) == mine.off * sizeof(T);
-            T* out0 = dz - mine.off;
-#pragma unroll 4
-            for (int i = threadIdx.x; i < mine.lines; i += blockDim.x) {
-                const uint4 z = fetch(i);
-                uint64_t v[N / 2];
+        const float factor = ctl.factor, gain = ctl.gain;
+        const int hit = ctl.hit;
+        const bool zero = factor == INFINITY, wanted = p.dz != nullptr && ok;
+        T* const dz = static_cast<T*>(p.dz) + row * p.lddz + first;
+        // whether the gradient's entries lie in lines as the logits' do
+        const bool same = (reinterpret_cast<uintptr_t>(dz + x.front) & 15) == 0;
+        auto slope = [&](float z) { return zero ? 0.0f : L::exponential(z, mine) * factor; };
+        // the target's entry, by the thread that writes its line, read before that is over-written
+        const int hit_line = hit >= x.front && hit < x.front + x.lines * N ? (hit - x.front) / N : -1;
+        const bool hits = wanted && !zero && (hit_line >= 0 ? hit_line % chunk % blockDim.x == threadIdx.x : hit >= 0 && hit == beside);
+        const float hit_value = hits ? slope(static_cast<float>(x.z[hit])) + gain : 0.0f;
+        const float beside_value = wanted && beside >= 0 ? slope(static_cast<float>(x.z[beside])) : 0.0f;
+        Place next = x;
+        if (more) next = place(row + step);
+        for (int c = 0; c < kChunks; ++c) {
+            const int end = wanted ? min(x.lines, (c + 1) * chunk) : 0;
+            uint4* const out = reinterpret_cast<uint4*>(dz + x.front);
+            if (zero && same) {
+                for (int i = c * chunk + threadIdx.x; i < end; i += blockDim.x) out[i] = make_uint4(0, 0, 0, 0);
+            } else if (zero) {
+                for (int i = c * chunk + threadIdx.x; i < end; i += blockDim.x)
+                    for (int e = 0; e < N; ++e) dz[x.front + i * N + e] = L::rounded(0.0f);
+            } else if (same) {
+                for (int i = c * chunk + threadIdx.x; i < end; i += blockDim.x) {
+                    float e[N];
+                    L::exponentials(lines[i], mine, e);
 #pragma unroll
-                for (int e = 0; e < N / 2; ++e) v[e] = zero ? 0 : mul2(L::exponentials(L::pair(z, e), ref), both(factor));
-                if (i == hit_line && !zero) {
-#pragma unroll
-                    for (int e = 0; e < N / 2; ++e)
-                        if (hit % N / 2 == e) v[e] = add2(v[e], hit & 1 ? f32x2(0.0f, gain) : f32x2(gain, 0.0f));
+                    for (int y = 0; y < N; ++y) e[y] *= factor;
+                    out[i] = L::pack(e);
                 }
-                if (same && i >= mine.inner0 && i < mine.inner1) {
-                    reinterpret_cast<uint4*>(out0)[i] = L::pack(v);
-                } else {
+            } else {
+                for (int i = c * chunk + threadIdx.x; i < end; i += blockDim.x) {
+                    float e[N];
+                    L::exponentials(lines[i], mine, e);
 #pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const int c = i * N + e - mine.off;
-                        float y[2];
-                        split(v[e / 2], y[0], y[1]);
-                        if (c >= 0 && c < len) dz[c] = L::rounded(y[e & 1]);
-                    }
+                    for (int y = 0; y < N; ++y) dz[x.front + i * N + y] = L::rounded(e[y] * factor);
                 }
             }
+            if (more && STAGED) {
+                __syncthreads();                 // the chunk has been read
+                if (threadIdx.x == 0) copy(next, c);
+            }
         }
-        if (row + step < p.rows) {
-            x = place(row + step);
-            __syncthreads();                     // the row has been read
-            if (STAGED && threadIdx.x == 0) copy(x);
-        }
+        if (wanted && beside >= 0) dz[beside] = L::rounded(beside_value);
+        if (hits) dz[hit] = L::rounded(hit_value);
+        x = next;
     }
     if (threadIdx.x == 0 && rank == 0)
         for (int k = 0; k < 3; ++k) p.terms[3 * (blockIdx.x / p.split) + k] = make_float2(sums[k].hi, sums[k].lo);
 }
 
 // The clusters' sums, added up in a fixed order: at most kLossClusters of them.
-constexpr int kLossClusters = 152 * 8;
+constexpr int kLossClusters = 152 * 16;
 __global__ void __launch_bounds__(128) k_loss_sums(const float2* terms, int count, float* out) {
     __shared__ float2 part[3][4];
     pdl_begin();
@@ -414,10 +452,12 @@ __global__ void __launch_bounds__(128) k_loss_sums(const float2* terms, int coun
         all.add(part[threadIdx.x][w].x);
         all.lo += part[threadIdx.x][w].y;
     }
-    // an infinite sum has NaN beside it
-    out[threadIdx.x] = fabsf(all.hi) < INFINITY ? all.hi + all.lo : all.hi;
+    out[threadIdx.x] = all.value();
 }
 
+// Bytes of a row's part, beyond which it is split: the clusters' barriers cost more than a second CTA
+// on the SM gives (701 x 50001 fp32: 71 us in two parts, 89 in four)
+constexpr int kPart = 112 * 1024;
 constexpr int kStage = 200 * 1024;     // most bytes of a part in shared memory
 
 template <class T, bool STAGED> cudaError_t launch_loss(const LossParams& p, int& clusters, cudaStream_t s) {
@@ -434,10 +474,11 @@ template <class T, bool STAGED> cudaError_t launch_loss(const LossParams& p, int
             if (device < 64) done.fetch_or(1ull << device);
         }
     }
-    const int lines = p.part / Line<T>::N + 2;
-    const int threads = std::min(512, std::max(64, (lines + 31) / 32 * 32));
-    // CTAs that an SM holds, by registers and shared memory (1.5 KB beside the part)
-    const int resident = std::max(1, std::min({8, 1536 / threads, (226 << 10) / (bytes + 1536)}));
+    // CTAs that an SM holds by shared memory (1.5 KB beside the part); they share the threads that
+    // its registers are enough for
+    const int lines = p.part / Line<T>::N + 2, fit = std::max(1, std::min(16, (226 << 10) / (bytes + 1536)));
+    const int threads = std::min({kLossThreads, std::max(64, 3 * kLossThreads / fit / 32 * 32), std::max(64, (lines + 31) / 32 * 32)});
+    const int resident = std::max(1, std::min(fit, 3 * kLossThreads / threads));
     clusters = std::min(p.rows, 152 * resident / p.split);
     return launch(fn, dim3(static_cast<unsigned int>(clusters) * p.split), dim3(threads), bytes, s, p.split, p);
 }
@@ -448,7 +489,7 @@ template <class T> cudaError_t loss_as(LossParams& p, int& clusters, cudaStream_
     // would fill an SM's shared memory alone
     p.split = 1;
     const auto part = [&](int split) { return ((p.vocab - 1) / split + N) / N * N; };
-    while (p.split < 8 && (part(p.split) * static_cast<long long>(sizeof(T)) > 72 * 1024 ||
+    while (p.split < 8 && (part(p.split) * static_cast<long long>(sizeof(T)) > kPart ||
                            (2LL * p.split * p.rows <= 304 && part(2 * p.split) * sizeof(T) >= 4096)))
         p.split *= 2;
     p.part = part(p.split);
