@@ -619,7 +619,7 @@ int moara_attention(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int
 /* Its gradients from dout (strided as q), with what the forward call left in out, rest (or
  * NULL: the gradient of q is less exact for long sequences) and lse: dq tokens x heads x dim,
  * dk and dv tokens x kv_heads x dim, bf16; the sums over a group's heads in fp32, every sum in
- * a fixed order.  delta: workspace of heads x tokens floats, in use by one call at a time. */
+ * a fixed order.  delta: workspace of heads x tokens + 1 floats, in use by one call at a time. */
 int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int heads, int kv_heads, int dim,
                              float scale, const void* dout, int64_t do_row, int64_t do_head, const void* q, int64_t q_row,
                              int64_t q_head, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,

@@ -13,6 +13,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <climits>
 
 #include "f32x2.cuh"
 #include "launch.cuh"
@@ -106,9 +107,34 @@ struct ForwardParams {
     long long wait_limit;
 };
 
-// 32 rows of a warp (one a lane) of CHUNKS 16-byte pieces from registers to rows of the
-// output `pitch` bytes apart, through shared memory of the warp's own, so that a row's pieces leave
-// beside one another; `rows` of them exist, and `bytes` of each.
+// 32 rows of a warp (one a lane) of CHUNKS 16-byte pieces from registers to rows of the output
+// `pitch` bytes apart; `rows` of them exist, and `bytes` of each.  CHUNKS lanes exchange pieces
+// until each has the same one of all their rows, so that a row's leave beside one another.
+template <int CHUNKS>
+__device__ __forceinline__ void store_rows(uint4 (&w)[CHUNKS], uint8_t* to, long long pitch, int rows, int bytes, int lane) {
+#pragma unroll
+    for (int s = CHUNKS / 2; s > 0; s /= 2) {
+        const bool upper = (lane & s) != 0;
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            if (i & s) continue;
+            uint4 send = upper ? w[i] : w[i + s];
+            send.x = __shfl_xor_sync(0xffffffffu, send.x, s);
+            send.y = __shfl_xor_sync(0xffffffffu, send.y, s);
+            send.z = __shfl_xor_sync(0xffffffffu, send.z, s);
+            send.w = __shfl_xor_sync(0xffffffffu, send.w, s);
+            if (upper) w[i] = send;
+            else w[i + s] = send;
+        }
+    }
+    const int c = lane % CHUNKS, r0 = lane - c;
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i)
+        if (r0 + i < rows && c * 16 < bytes) *reinterpret_cast<uint4*>(to + (r0 + i) * pitch + c * 16) = w[i];
+}
+
+// The same through shared memory of the warp's own, 32 CHUNKS 16 bytes: where registers are few, and
+// the memory is free.
 template <int CHUNKS>
 __device__ __forceinline__ void store_rows(uint8_t* stage, const uint4 (&w)[CHUNKS], uint8_t* to, long long pitch, int rows, int bytes,
                                            int lane) {
@@ -414,24 +440,26 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
 }
 
 // ---------------------------------------------------------------------------
-// Gradients.  Two kinds of CTAs, so that every sum has one owner and one order (five products a
+// Gradients.  Two kinds of tiles, so that every sum has one owner and one order (five products a
 // pair of tiles become seven; adding dQ up where dK and dV are would need atomics, whose order
-// changes the result).  KEYS: a CTA takes 128 keys of a head of k and v and goes through
-// the queries that see them, of every head that shares it; with S^T = K Q^T, P^T and dS^T
-// stay in tensor memory and dV += P^T dO, dK += dS^T Q take them from there.  Otherwise it
-// takes 128 queries of a head and goes through their keys: dQ += dS K.
+// changes the result).  KEYS: 128 keys of a head of k and v, against the queries that see them, of
+// every head that shares it; with S^T = K Q^T, P^T and dS^T stay in tensor memory and
+// dV += P^T dO, dK += dS^T Q take them from there.  Otherwise 128 queries of a head against their
+// keys: dQ += dS K.
 //
 // Sixteen warps turn S into P and dP = dO V^T into dS (32 columns of a row a thread), one
-// issues products, one copies.  Where the longest tiles would outlast the rest, a cluster
-// shares a tile's steps, and its CTAs add one another's sums, in order, through shared memory
-//.  The tile that is used twice in a step (first in S, last in a
-// sum) has three slots, the other two.
+// issues products, one copies.  A CTA takes tile after tile, the longest first, from a counter, each
+// warp goes from one to the next on its own, and the next tile's first copies and products run
+// beside this one's last sums and stores.  The operand that
+// is used twice in a step (first in S, last in a sum) has three slots, the other two.  Where the
+// longest tiles would outlast the rest, a cluster shares a tile's steps, and its CTAs add one
+// another's sums, in order, through shared memory.
 // ---------------------------------------------------------------------------
 template <int DP> struct Backward {
     static constexpr int TILE = DP / 64 * PANEL;
     static constexpr int SA = 3, SB = 2;
     static constexpr int STATS = 2 * 2 * ROWS * 4;                 // lse and delta of two steps
-    static constexpr int CTL = 256;
+    static constexpr int CTL = 512;
     static constexpr int SMEM = (2 + SA + SB) * TILE + STATS + CTL;
     static constexpr int WARPS = 16;                               // that turn S into dS
     static constexpr int THREADS = (WARPS + 2) * 32;
@@ -447,6 +475,7 @@ struct BackwardParams {
     bf16* dv;
     const AttentionTile* q_tiles;
     const AttentionTile* k_tiles;
+    unsigned int* counter;                       // of the tiles that have been taken, beyond one a CTA
     int n_tiles;
     int tokens, heads, kv_heads, group, dim;
     int split;                                   // CTAs of a cluster, which share a tile's steps
@@ -456,27 +485,40 @@ struct BackwardParams {
 };
 
 struct BackwardCtl {
-    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull, dpfull, dsfull, stats[2], done, drain;
+    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull, dpfull, dsfull, stats[2], done, read, drain, listed[2], taken[2];
     uint32_t tmem;
     int abort;
-    int filled[2];
+    int filled[3];
+    int tiles[2];                                // the CTA's next tiles, of which the warps learn here
 };
 
-// The steps of a CTA: every `split`-th of (head, tile) in order.  KEYS: tiles of queries from
-// the keys' own to the sequence's last, for each head of the group; otherwise tiles of keys up to the
-// queries' own.
-struct Steps {
-    int at, head, count;
-    int first, last, stride;
-    __device__ __forceinline__ Steps(const AttentionTile& t, int rank, int split, int kv, int group, bool keys) {
-        last = (t.length - 1) / ROWS;
-        first = keys ? t.tile : 0;
-        stride = split;
-        const int all = keys ? (last - first + 1) * group : t.tile + 1;
-        count = all > rank ? (all - rank - 1) / split + 1 : 0;
+// Tile n: those of the keys first, of which a group of heads makes the longest, by falling work.
+// Its steps are every `split`-th of (head, tile) in order.  KEYS: tiles of queries from the keys' own
+// to the sequence's last, for each head of the group; otherwise tiles of keys up to the queries' own.
+struct Work {
+    AttentionTile tile;
+    int owner, kv;                               // head that the tile is of, its head of k and v
+    bool keys;
+    int at, head, count;                         // of the next step; steps
+    int first, last, stride, all;
+    __device__ __forceinline__ bool get(const BackwardParams& p, int n) {
+        const int rank = blockIdx.x % p.split, of_keys = p.n_tiles * p.kv_heads;
+        if (n >= of_keys + p.n_tiles * p.heads) return false;
+        keys = n < of_keys;
+        if (!keys) n -= of_keys;
+        const int owners = keys ? p.kv_heads : p.heads;
+        tile = (keys ? p.k_tiles : p.q_tiles)[n / owners];
+        owner = n % owners;
+        kv = keys ? owner : owner / p.group;
+        last = (tile.length - 1) / ROWS;
+        first = keys ? tile.tile : 0;
+        stride = p.split;
+        all = keys ? (last - first + 1) * p.group : tile.tile + 1;
+        count = all > rank ? (all - rank - 1) / p.split + 1 : 0;
         at = first + rank;
-        head = keys ? kv * group : kv;
+        head = keys ? kv * p.group : kv;
         wrap();
+        return true;
     }
     __device__ __forceinline__ void wrap() {
         while (at > last) {
@@ -488,6 +530,10 @@ struct Steps {
         at += stride;
         wrap();
     }
+    // rows of the step's tile that exist
+    __device__ __forceinline__ int rows() const { return at == last ? tile.length - last * ROWS : ROWS; }
+    // first token of the tile
+    __device__ __forceinline__ int token() const { return tile.begin + tile.tile * ROWS; }
 };
 
 // Where a CTA of a cluster leaves four columns of a row of its first or second sum.
@@ -501,49 +547,308 @@ __device__ __forceinline__ float4 ld_cluster_f4(uint32_t a) {
     return v;
 }
 
-// block: among the CTAs of its kind
-template <int DP, bool KEYS> __device__ __forceinline__ void gradient_tile(const BackwardParams& p, int block) {
+// Columns of tensor memory.  KEYS: S, dP, dV, dK; otherwise S, dP of even and odd steps, dQ.
+constexpr uint32_t COL_S = 0, COL_DP = 128, COL_SUM_B = 256, COL_SUM_A = 384;
+template <bool KEYS> __device__ __forceinline__ uint32_t dp_column(int j) {
+    return KEYS ? COL_DP : COL_DP + static_cast<uint32_t>(j & 1) * 128;
+}
+
+template <int DP> struct Shared {
+    uint8_t* smem;
+    uint8_t* ring_a;
+    uint8_t* ring_b;
+    float* stats;
+    BackwardCtl* ctl;
+    __device__ __forceinline__ explicit Shared(uint8_t* base) {
+        using F = Backward<DP>;
+        smem = base;
+        ring_a = smem + 2 * F::TILE;
+        ring_b = ring_a + F::SA * F::TILE;
+        stats = reinterpret_cast<float*>(ring_b + F::SB * F::TILE);
+        ctl = reinterpret_cast<BackwardCtl*>(ring_b + F::SB * F::TILE + F::STATS);
+    }
+};
+
+// What the warp that issues products carries from tile to tile.
+struct Products {
+    uint32_t tmem;
+    int sa = 0, sb = 0;                          // slots of both rings, whose phases end with theirs
+    uint32_t pa = 0, pb = 0, step = 0, tile = 0;
+};
+
+template <int DP, bool KEYS>
+__device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits, Products& st, Work& work, bool leader, int lane) {
+    using F = Backward<DP>;
+    BackwardCtl* const ctl = x.ctl;
+    const uint32_t fixed = ptx::smem_u32(x.smem), ra = ptx::smem_u32(x.ring_a), rb = ptx::smem_u32(x.ring_b);
+    const uint32_t afull = ptx::smem_u32(&ctl->afull[0]), bfull = ptx::smem_u32(&ctl->bfull[0]);
+    const uint32_t aempty = ptx::smem_u32(&ctl->aempty[0]), bempty = ptx::smem_u32(&ctl->bempty[0]);
+    const uint32_t pfull = ptx::smem_u32(&ctl->pfull), dsfull = ptx::smem_u32(&ctl->dsfull);
+    const uint32_t sfull = ptx::smem_u32(&ctl->sfull), dpfull = ptx::smem_u32(&ctl->dpfull);
+    const uint32_t tmem = st.tmem;
+    const int steps = work.count;
+    // rows of the tile that a sum runs over
+    int rows = work.rows();
+    auto clean_a = [&] {
+        if (rows % 16 != 0) clear_rows<DP>(x.ring_a + st.sa * F::TILE, rows, lane);
+    };
+    auto clean_b = [&] {
+        if (KEYS && rows % 16 != 0) clear_rows<DP>(x.ring_b + st.sb * F::TILE, rows, lane);
+    };
+    if (steps == 0) return true;
+    if (!waits.three(ptx::smem_u32(&ctl->fixed), st.tile & 1, afull + 8 * st.sa, st.pa, bfull + 8 * st.sb, st.pb)) return false;
+    clean_a();
+    clean_b();
+    ptx::tc_fence_after();
+    if (leader) {
+        mma_rows<DP>(tmem + COL_S, fixed, ra + st.sa * F::TILE);
+        ptx::mma_commit(sfull);
+        mma_rows<DP>(tmem + COL_DP, fixed + F::TILE, rb + st.sb * F::TILE);
+        ptx::mma_commit(dpfull);
+        if (!KEYS) ptx::mma_commit(bempty + 8 * st.sb);
+    }
+    __syncwarp();
+    // the last tile's sums have been read from the columns that this one's go to
+    if (st.tile > 0 && !waits.one(ptx::smem_u32(&ctl->read), (st.tile - 1) & 1)) return false;
+    for (int j = 0; j < steps; ++j, ++st.step) {
+        const bool more = j + 1 < steps;
+        const uint32_t parity = st.step & 1;
+        const int oa = st.sa, ob = st.sb, sums = (rows + 15) / 16;
+        const uint32_t a = ra + oa * F::TILE, b = rb + ob * F::TILE;
+        work.next();
+        rows = work.rows();
+        if (++st.sa == F::SA) { st.sa = 0; st.pa ^= 1; }
+        if (++st.sb == F::SB) { st.sb = 0; st.pb ^= 1; }
+        const uint32_t a1 = ra + st.sa * F::TILE, b1 = rb + st.sb * F::TILE;
+        if (KEYS) {
+            if (!(more ? waits.two(pfull, parity, afull + 8 * st.sa, st.pa) : waits.one(pfull, parity))) return false;
+            if (more) clean_a();
+            ptx::tc_fence_after();
+            if (leader) {
+                mma_sum<DP, 32, 32>(tmem + COL_SUM_B, tmem + COL_S, b, sums, j > 0);
+                ptx::mma_commit(bempty + 8 * ob);
+                if (more) {                                         // over the P that the product in front of it has read by then
+                    mma_rows<DP>(tmem + COL_S, fixed, a1);
+                    ptx::mma_commit(sfull);
+                }
+            }
+            __syncwarp();
+            if (!(more ? waits.two(dsfull, parity, bfull + 8 * st.sb, st.pb) : waits.one(dsfull, parity))) return false;
+            if (more) clean_b();
+        } else {
+            if (more) {
+                if (!waits.three(pfull, parity, afull + 8 * st.sa, st.pa, bfull + 8 * st.sb, st.pb)) return false;
+                clean_a();
+                ptx::tc_fence_after();
+                if (leader) {
+                    mma_rows<DP>(tmem + COL_S, fixed, a1);
+                    ptx::mma_commit(sfull);
+                    mma_rows<DP>(tmem + dp_column<KEYS>(j + 1), fixed + F::TILE, b1);
+                    ptx::mma_commit(dpfull);
+                    ptx::mma_commit(bempty + 8 * st.sb);
+                }
+                __syncwarp();
+            }
+            if (!(more ? waits.one(dsfull, parity) : waits.two(pfull, parity, dsfull, parity))) return false;
+        }
+        ptx::tc_fence_after();
+        if (leader) {
+            mma_sum<DP, 32, 32>(tmem + COL_SUM_A, tmem + dp_column<KEYS>(j), a, sums, j > 0);
+            ptx::mma_commit(aempty + 8 * oa);
+            if (KEYS && more) {
+                mma_rows<DP>(tmem + COL_DP, fixed + F::TILE, b1);
+                ptx::mma_commit(dpfull);
+            }
+            if (!more) ptx::mma_commit(ptx::smem_u32(&ctl->done));
+        }
+        __syncwarp();
+    }
+    ++st.tile;
+    return true;
+}
+
+// What a warp that turns S into dS carries from tile to tile.
+struct Slopes {
+    uint32_t tmem;
+    uint32_t step = 0, of_keys = 0, tile = 0;    // steps, those of tiles of keys, tiles
+};
+
+template <int DP, bool KEYS>
+__device__ __forceinline__ bool turn(const BackwardParams& p, const Shared<DP>& x, const Waits& waits, Slopes& st, Work& work, int warp,
+                                     int lane) {
+    using F = Backward<DP>;
+    constexpr int WARPS = F::WARPS;
+    BackwardCtl* const ctl = x.ctl;
+    auto wait = [&](uint64_t& bar, uint32_t parity) { return waits.one(ptx::smem_u32(&bar), parity); };
+    const int part = warp >> 2, quad = warp & 3, r = quad * 32 + lane, c0 = part * 32;
+    const uint32_t lanes = st.tmem + (static_cast<uint32_t>(quad * 32) << 16);
+    const AttentionTile tile = work.tile;
+    const int row = tile.tile * ROWS + r;                           // in the sequence
+    const long long token = tile.begin + row;
+    const uint64_t scale = both(p.scale * kLog2e);
+    const int owners = KEYS ? p.kv_heads : p.heads, steps = work.count;
+    if (steps == 0) return true;
+    uint64_t lse = 0, delta = 0;                                    // negative, of the row
+    if (!KEYS && row < tile.length) {
+        lse = both(-p.lse[static_cast<long long>(work.owner) * p.tokens + token] * kLog2e);
+        delta = both(-p.delta[static_cast<long long>(work.owner) * p.tokens + token]);
+    }
+    // KEYS: negative lse (first 128 threads) or delta (the next) of a query of a step
+    auto stat = [&] {
+        const int q = work.at * ROWS + r;
+        if (q >= tile.length || part >= 2) return 0.0f;
+        const long long from = static_cast<long long>(work.head) * p.tokens + tile.begin + q;
+        return part == 0 ? -p.lse[from] * kLog2e : -p.delta[from];
+    };
+    float ahead = KEYS ? stat() : 0.0f;
+    for (int j = 0; j < steps; ++j, ++st.step) {
+        const uint32_t slot = st.of_keys & 1, parity = st.step & 1;
+        const ulonglong2* sl = reinterpret_cast<const ulonglong2*>(x.stats + slot * 2 * ROWS + c0);
+        const ulonglong2* sd = sl + ROWS / 4;
+        const int at = work.at, rows = work.rows();
+        work.next();
+        if (KEYS) {
+            if (part < 2) x.stats[slot * 2 * ROWS + part * ROWS + r] = ahead;
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->stats[slot]));
+            if (j + 1 < steps) ahead = stat();
+            // all warps' (a barrier whose wait is bounded); they have left the step before by then
+            if (!wait(ctl->stats[slot], (st.of_keys >> 1) & 1)) return false;
+            ++st.of_keys;
+        }
+        // which columns of this thread count: from `from` on (KEYS) up to `to`
+        int from = 0, to = 32;
+        if (KEYS) {
+            if (at == tile.tile) from = r - c0;
+            to = rows - c0;
+        } else if (at == tile.tile) {
+            to = r + 1 - c0;
+        }
+        const bool all = __all_sync(0xffffffffu, from <= 0 && to >= 32);
+        auto put = [&](uint32_t column, float (&v)[32], uint64_t& bar) {
+            if (!all) {
+#pragma unroll
+                for (int c = 0; c < 32; ++c) v[c] = c >= from && c < to ? v[c] : 0.0f;
+            }
+            uint32_t w[16];
+#pragma unroll
+            for (int c = 0; c < 16; ++c) w[c] = pack2(v[2 * c], v[2 * c + 1]);
+            ptx::tmem_st16(lanes + column + c0, w);
+            ptx::tmem_st_wait();
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar));
+        };
+        if (!wait(ctl->sfull, parity)) return false;
+        ptx::tc_fence_after();
+        uint32_t s[32];
+        ptx::tmem_ld32(lanes + COL_S + c0, s);
+        if (!KEYS) {
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull));
+        }
+        float v[32];
+#pragma unroll
+        for (int c = 0; c < 32; c += 4) {
+            const ulonglong2 l = KEYS ? sl[c / 4] : make_ulonglong2(lse, lse);
+#pragma unroll
+            for (int e = c; e < c + 4; e += 2) {
+                split(fma2(f32x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale, e == c ? l.x : l.y), v[e], v[e + 1]);
+                v[e] = ex2(v[e]);
+                v[e + 1] = ex2(v[e + 1]);
+            }
+        }
+        if (KEYS) put(COL_S, v, ctl->pfull);
+        if (!wait(ctl->dpfull, parity)) return false;
+        ptx::tc_fence_after();
+        ptx::tmem_ld32(lanes + dp_column<KEYS>(j) + c0, s);
+#pragma unroll
+        for (int c = 0; c < 32; c += 4) {
+            const ulonglong2 d = KEYS ? sd[c / 4] : make_ulonglong2(delta, delta);
+#pragma unroll
+            for (int e = c; e < c + 4; e += 2)
+                split(mul2(f32x2(v[e], v[e + 1]), add2(f32x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), e == c ? d.x : d.y)),
+                      v[e], v[e + 1]);
+        }
+        put(dp_column<KEYS>(j), v, ctl->dsfull);                    // what does not count may be infinite or NaN
+    }
+    if (!wait(ctl->done, st.tile & 1)) return false;
+    ++st.tile;
+    ptx::tc_fence_after();
+    // KEYS: the first half of the threads has dV, the second dK; otherwise all have dQ
+    constexpr int PARTS = KEYS ? WARPS / 8 : WARPS / 4, WIDTH = DP / PARTS;
+    const bool first = KEYS && part < PARTS;
+    const uint32_t src = lanes + (first ? COL_SUM_B : COL_SUM_A);
+    const float factor = first ? 1.0f : p.scale;
+    const int o0 = part % PARTS * WIDTH;
+    uint4 w[WIDTH / 8];
+#pragma unroll
+    for (int c = 0; c < WIDTH; c += 16) {
+        float o[16];
+        ptx::tmem_ld16(src + o0 + c, o);
+        if (p.split > 1) {                                          // the tiles are no longer read
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                *reinterpret_cast<float4*>(x.smem + sum_at<DP>(first, r, (o0 + c) / 4 + e)) =
+                    make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            w[c / 8 + e] = make_uint4(pack2(o[8 * e] * factor, o[8 * e + 1] * factor), pack2(o[8 * e + 2] * factor, o[8 * e + 3] * factor),
+                                      pack2(o[8 * e + 4] * factor, o[8 * e + 5] * factor),
+                                      pack2(o[8 * e + 6] * factor, o[8 * e + 7] * factor));
+    }
+    ptx::tc_fence_before();
+    __syncwarp();
+    if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->read));
+    if (p.split > 1) return true;
+    bf16* const out = (KEYS ? first ? p.dv : p.dk : p.dq) + ((token - lane) * owners + work.owner) * p.dim + o0;
+    store_rows(w, reinterpret_cast<uint8_t*>(out), static_cast<long long>(owners) * p.dim * 2, tile.length - (row - lane),
+               (p.dim - o0) * 2, lane);
+    return true;
+}
+
+template <int DP> __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(const __grid_constant__ BackwardParams p) {
     using F = Backward<DP>;
     constexpr int WARPS = F::WARPS;
     static_assert(sizeof(BackwardCtl) <= F::CTL, "the barriers fit");
     extern __shared__ __align__(1024) uint8_t smem[];              // there is no room to align it here
-    uint8_t* const ring_a = smem + 2 * F::TILE;
-    uint8_t* const ring_b = ring_a + F::SA * F::TILE;
-    float* const stats = reinterpret_cast<float*>(ring_b + F::SB * F::TILE);
-    BackwardCtl* ctl = reinterpret_cast<BackwardCtl*>(ring_b + F::SB * F::TILE + F::STATS);
+    const Shared<DP> x(smem);
+    BackwardCtl* const ctl = x.ctl;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort_flag = &ctl->abort;
     if ((ptx::smem_u32(smem) & 1023u) != 0) {                       // the same in every CTA
         if (threadIdx.x == 0) atomicCAS(p.status, 0, MOARA_ERR_ALIGN);
         return;
     }
-    const int rank = block % p.split, item = block / p.split;
-    const AttentionTile* const tiles = KEYS ? p.k_tiles : p.q_tiles;
-    const CUtensorMap *const fixed_a = KEYS ? &p.k : &p.q, *const fixed_b = KEYS ? &p.v : &p.dout;
-    const CUtensorMap *const map_a = KEYS ? &p.q : &p.k, *const map_b = KEYS ? &p.dout : &p.v;
-    bf16 *const out_a = KEYS ? p.dk : p.dq, *const out_b = p.dv;
-    const int owners = KEYS ? p.kv_heads : p.heads, owner = item % owners, kv = KEYS ? owner : owner / p.group;
-    // copies of step j, whose tile is `at` of head `h`
+    // copies of a tile of 128 tokens, of the next step, and of what a tile keeps
     auto copy = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
         for (int c = 0; c < DP / 64; ++c)
             ptx::tma_load_3d(ptx::smem_u32(to) + c * PANEL, map, ptx::smem_u32(&bar), c * 64, h, row);
     };
-    auto copy_a = [&](const AttentionTile& t, int j, int h, int at) {
-        const int slot = j % F::SA;
+    auto copy_a = [&](const Work& w, int slot) {
         ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->afull[slot]), F::TILE);
-        copy(ring_a + slot * F::TILE, map_a, ctl->afull[slot], h, t.begin + at * ROWS);
+        copy(x.ring_a + slot * F::TILE, w.keys ? &p.q : &p.k, ctl->afull[slot], w.head, w.tile.begin + w.at * ROWS);
     };
-    auto copy_b = [&](const AttentionTile& t, int j, int h, int at) {
-        const int slot = j % F::SB;
+    auto copy_b = [&](const Work& w, int slot) {
         ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->bfull[slot]), F::TILE);
-        copy(ring_b + slot * F::TILE, map_b, ctl->bfull[slot], h, t.begin + at * ROWS);
+        copy(x.ring_b + slot * F::TILE, w.keys ? &p.dout : &p.v, ctl->bfull[slot], w.head, w.tile.begin + w.at * ROWS);
+    };
+    auto copy_fixed = [&](const Work& w) {
+        ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->fixed), 2 * F::TILE);
+        copy(x.smem, w.keys ? &p.k : &p.q, ctl->fixed, w.owner, w.token());
+        copy(x.smem + F::TILE, w.keys ? &p.v : &p.dout, ctl->fixed, w.owner, w.token());
     };
     if (threadIdx.x == WARPS * 32) {
         // the thread that copies starts what the first step needs beside the others' set-up
         for (uint64_t* b : {&ctl->fixed, &ctl->sfull, &ctl->dpfull, &ctl->done, &ctl->drain}) ptx::mbar_init(ptx::smem_u32(b), 1);
-        for (int i = 0; i < 2; ++i) ptx::mbar_init(ptx::smem_u32(&ctl->stats[i]), WARPS);
-        ptx::mbar_init(ptx::smem_u32(&ctl->pfull), WARPS);
-        ptx::mbar_init(ptx::smem_u32(&ctl->dsfull), WARPS);
+        for (uint64_t* b : {&ctl->pfull, &ctl->dsfull, &ctl->stats[0], &ctl->stats[1], &ctl->read})
+            ptx::mbar_init(ptx::smem_u32(b), WARPS);
+        for (int i = 0; i < 2; ++i) {
+            ptx::mbar_init(ptx::smem_u32(&ctl->listed[i]), 1);
+            ptx::mbar_init(ptx::smem_u32(&ctl->taken[i]), WARPS + 1);
+        }
         for (int i = 0; i < F::SA; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl->afull[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl->aempty[i]), 1);
@@ -556,14 +861,14 @@ template <int DP, bool KEYS> __device__ __forceinline__ void gradient_tile(const
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
         pdl_begin();
-        const AttentionTile t = tiles[item / owners];
-        const Steps s(t, rank, p.split, kv, p.group, KEYS);
-        ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->fixed), 2 * F::TILE);
-        copy(smem, fixed_a, ctl->fixed, owner, t.begin + t.tile * ROWS);
-        if (s.count > 0) copy_a(t, 0, s.head, s.at);
-        copy(smem + F::TILE, fixed_b, ctl->fixed, owner, t.begin + t.tile * ROWS);
-        if (s.count > 0) copy_b(t, 0, s.head, s.at);
-        ctl->filled[0] = ctl->filled[1] = s.count > 0;
+        ctl->tiles[0] = blockIdx.x / p.split;
+        ptx::mbar_arrive(ptx::smem_u32(&ctl->listed[0]));
+        Work work;
+        if (work.get(p, blockIdx.x / p.split) && work.count > 0) {
+            copy_fixed(work);
+            copy_a(work, 0);
+            copy_b(work, 0);
+        }
     }
     if (warp == WARPS + 1) {
         ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
@@ -574,269 +879,87 @@ template <int DP, bool KEYS> __device__ __forceinline__ void gradient_tile(const
     ptx::tc_fence_after();
     const uint32_t tmem = ctl->tmem;
     pdl_begin();
-    const AttentionTile tile = tiles[item / owners];
-    const Steps begin(tile, rank, p.split, kv, p.group, KEYS);
-    const int steps = begin.count, last = begin.last;              // this CTA's; tile of the sequence
-    const int tail = tile.length - last * ROWS;                    // rows of the last tile
-    auto wait = [&](uint64_t& bar, uint32_t parity) {
-        return ptx::mbar_wait_warp(ptx::smem_u32(&bar), parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
+    const Waits waits{abort_flag, p.status, p.wait_limit};
+    // the CTA's tile of a round, to every warp but the one that copies
+    auto tile_of = [&](int round, Work& work, bool& ok) {
+        const int slot = round & 1;
+        ok = waits.one(ptx::smem_u32(&ctl->listed[slot]), (round >> 1) & 1);
+        if (!ok) return false;
+        const int n = ctl->tiles[slot];
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->taken[slot]));
+        return work.get(p, n);
     };
-    constexpr uint32_t S = 0, DPC = 128;                           // columns of tensor memory
-    constexpr uint32_t SUM_B = 256, SUM_A = 384;                   // KEYS: dV, dK; otherwise dQ is SUM_A
-    auto dp_at = [&](int j) { return KEYS ? DPC : DPC + static_cast<uint32_t>(j & 1) * 128; };
 
     if (warp == WARPS) {
         if (lane == 0) {
-            int na = steps > 0, nb = na;
-            Steps s = begin;
+            int na = 0, nb = 0, tiles = 0;
             auto room = [&](uint64_t& bar, int n, int slots) {
                 return n < slots || ptx::mbar_wait(ptx::smem_u32(&bar), (n / slots - 1) & 1, abort_flag, p.status,
                                                    MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
             };
-            for (int j = 1; j < steps; ++j) {
-                s.next();
-                if (!room(ctl->aempty[j % F::SA], j, F::SA)) break;
-                copy_a(tile, j, s.head, s.at);
-                ++na;
-                if (!room(ctl->bempty[j % F::SB], j, F::SB)) break;
-                copy_b(tile, j, s.head, s.at);
-                ++nb;
+            Work work;
+            bool ok = true;
+            int n = blockIdx.x / p.split;
+            for (int round = 0; ok && work.get(p, n); ++round) {
+                if (round == 0 && work.count > 0) {                 // begun above
+                    na = nb = tiles = 1;
+                    work.next();
+                }
+                for (int j = round == 0; j < work.count; ++j, work.next()) {
+                    ok = room(ctl->aempty[na % F::SA], na, F::SA);
+                    if (!ok) break;
+                    copy_a(work, na++ % F::SA);
+                    ok = room(ctl->bempty[nb % F::SB], nb, F::SB);
+                    if (!ok) break;
+                    copy_b(work, nb++ % F::SB);
+                    if (j > 0) continue;
+                    // the last tile's products are done
+                    ok = ptx::mbar_wait(ptx::smem_u32(&ctl->done), (tiles - 1) & 1, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT,
+                                        p.wait_limit);
+                    if (!ok) break;
+                    copy_fixed(work);
+                    ++tiles;
+                }
+                if (!ok) break;
+                // the next tile; a cluster has one
+                n = p.split > 1 ? INT_MAX : static_cast<int>(gridDim.x + atomicAdd(p.counter, 1u));
+                const int slot = (round + 1) & 1;
+                ok = round == 0 || ptx::mbar_wait(ptx::smem_u32(&ctl->taken[slot]), ((round - 1) >> 1) & 1, abort_flag, p.status,
+                                                  MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
+                if (!ok) break;
+                ctl->tiles[slot] = n;
+                ptx::mbar_arrive(ptx::smem_u32(&ctl->listed[slot]));
             }
             ctl->filled[0] = na;
             ctl->filled[1] = nb;
+            ctl->filled[2] = tiles;
         }
     } else if (warp == WARPS + 1) {
+        // The whole warp runs the loop, one lane issues (a lane alone takes 1650 clocks for sixteen
+        // products, whose time is 1030); what a product needs but P and dS is there ahead of them.
         const bool leader = ptx::elect_one();
-        const uint32_t fixed = ptx::smem_u32(smem), ra = ptx::smem_u32(ring_a), rb = ptx::smem_u32(ring_b);
-        auto commit = [&](uint64_t& bar) {
-            if (leader) ptx::mma_commit(ptx::smem_u32(&bar));
-            __syncwarp();
-        };
-        // The operands of a step: slots of both rings, whose phases end with theirs, and the rows
-        // of the tile that a sum runs over
-        const Waits waits{abort_flag, p.status, p.wait_limit};
-        const uint32_t afull = ptx::smem_u32(&ctl->afull[0]), bfull = ptx::smem_u32(&ctl->bfull[0]);
-        const uint32_t aempty = ptx::smem_u32(&ctl->aempty[0]), bempty = ptx::smem_u32(&ctl->bempty[0]);
-        const uint32_t pfull = ptx::smem_u32(&ctl->pfull), dsfull = ptx::smem_u32(&ctl->dsfull);
-        const uint32_t sfull = ptx::smem_u32(&ctl->sfull), dpfull = ptx::smem_u32(&ctl->dpfull);
-        int sa = 0, sb = 0;
-        uint32_t pa = 0, pb = 0;
-        Steps step = begin;
-        int rows = step.at == last ? tail : ROWS;
-        auto clean_a = [&] {
-            if (rows % 16 != 0) clear_rows<DP>(ring_a + sa * F::TILE, rows, lane);
-        };
-        auto clean_b = [&] {
-            if (KEYS && rows % 16 != 0) clear_rows<DP>(ring_b + sb * F::TILE, rows, lane);
-        };
-        bool ok = wait(ctl->fixed, 0) && steps > 0 && waits.two(afull, 0, bfull, 0);
-        if (ok) {
-            clean_a();
-            clean_b();
-            ptx::tc_fence_after();
-            if (leader) {
-                mma_rows<DP>(tmem + S, fixed, ra);
-                ptx::mma_commit(sfull);
-                mma_rows<DP>(tmem + DPC, fixed + F::TILE, rb);
-                ptx::mma_commit(dpfull);
-                if (!KEYS) ptx::mma_commit(bempty);
-            }
-            __syncwarp();
-        }
-        for (int j = 0; j < steps && ok; ++j) {
-            const bool more = j + 1 < steps;
-            const int oa = sa, ob = sb, sums = (rows + 15) / 16;
-            const uint32_t a = ra + oa * F::TILE, b = rb + ob * F::TILE;
-            step.next();
-            rows = step.at == last ? tail : ROWS;
-            if (++sa == F::SA) { sa = 0; pa ^= 1; }
-            if (++sb == F::SB) { sb = 0; pb ^= 1; }
-            const uint32_t a1 = ra + sa * F::TILE, b1 = rb + sb * F::TILE;
-            if (KEYS) {
-                ok = more ? waits.two(pfull, j & 1, afull + 8 * sa, pa) : waits.one(pfull, j & 1);
-                if (!ok) break;
-                if (more) clean_a();
-                ptx::tc_fence_after();
-                if (leader) {
-                    mma_sum<DP, 32, 32>(tmem + SUM_B, tmem + S, b, sums, j > 0);
-                    ptx::mma_commit(bempty + 8 * ob);
-                    if (more) {                                     // over the P that the product in front of it has read by then
-                        mma_rows<DP>(tmem + S, fixed, a1);
-                        ptx::mma_commit(sfull);
-                    }
-                }
-                __syncwarp();
-                ok = more ? waits.two(dsfull, j & 1, bfull + 8 * sb, pb) : waits.one(dsfull, j & 1);
-                if (!ok) break;
-                if (more) clean_b();
-            } else {
-                if (more) {
-                    ok = waits.three(pfull, j & 1, afull + 8 * sa, pa, bfull + 8 * sb, pb);
-                    if (!ok) break;
-                    clean_a();
-                    ptx::tc_fence_after();
-                    if (leader) {
-                        mma_rows<DP>(tmem + S, fixed, a1);
-                        ptx::mma_commit(sfull);
-                        mma_rows<DP>(tmem + dp_at(j + 1), fixed + F::TILE, b1);
-                        ptx::mma_commit(dpfull);
-                        ptx::mma_commit(bempty + 8 * sb);
-                    }
-                    __syncwarp();
-                }
-                ok = waits.one(dsfull, j & 1);
-                if (!ok) break;
-            }
-            ptx::tc_fence_after();
-            if (leader) {
-                mma_sum<DP, 32, 32>(tmem + SUM_A, tmem + dp_at(j), a, sums, j > 0);
-                ptx::mma_commit(aempty + 8 * oa);
-                if (KEYS && more) {
-                    mma_rows<DP>(tmem + DPC, fixed + F::TILE, b1);
-                    ptx::mma_commit(dpfull);
-                }
-                if (!more) ptx::mma_commit(ptx::smem_u32(&ctl->done));
-            }
-            __syncwarp();
-        }
-        commit(ctl->drain);
+        Products st;
+        st.tmem = tmem;
+        Work work;
+        bool ok = true;
+        for (int round = 0; ok && tile_of(round, work, ok); ++round)
+            ok = work.keys ? multiply<DP, true>(x, waits, st, work, leader, lane) : multiply<DP, false>(x, waits, st, work, leader, lane);
+        if (leader) ptx::mma_commit(ptx::smem_u32(&ctl->drain));
+        __syncwarp();
         wait_drain(ptx::smem_u32(&ctl->drain), 0);
     } else {
-        const int part = warp >> 2, quad = warp & 3, r = quad * 32 + lane, c0 = part * 32;
-        const uint32_t lanes = tmem + (static_cast<uint32_t>(quad * 32) << 16);
-        const int row = tile.tile * ROWS + r;                       // in the sequence
-        const bool real = row < tile.length;
-        const long long token = tile.begin + row;
-        const uint64_t scale = f32x2(p.scale * kLog2e, p.scale * kLog2e);
-        uint64_t lse = 0, delta = 0;                                // negative, of the row
-        if (!KEYS && real) {
-            const float l = -p.lse[static_cast<long long>(owner) * p.tokens + token] * kLog2e;
-            const float d = -p.delta[static_cast<long long>(owner) * p.tokens + token];
-            lse = f32x2(l, l);
-            delta = f32x2(d, d);
-        }
-        // KEYS: negative lse (first 128 threads) or delta (the next) of a query of a step
-        Steps step = begin;
-        auto stat = [&](const Steps& s) {
-            const int q = s.at * ROWS + r;
-            if (q >= tile.length || part >= 2) return 0.0f;
-            const long long from = static_cast<long long>(s.head) * p.tokens + tile.begin + q;
-            return part == 0 ? -p.lse[from] * kLog2e : -p.delta[from];
-        };
-        float stat_ahead = KEYS && steps > 0 ? stat(step) : 0.0f;
-        bool ok = steps > 0;
-        for (int j = 0; j < steps; ++j) {
-            const ulonglong2* sl = reinterpret_cast<const ulonglong2*>(stats + (j & 1) * 2 * ROWS + c0);
-            const ulonglong2* sd = sl + ROWS / 4;
-            const int at = step.at;
-            step.next();
-            if (KEYS) {
-                if (part < 2) stats[(j & 1) * 2 * ROWS + part * ROWS + r] = stat_ahead;
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->stats[j & 1]));
-                if (j + 1 < steps) stat_ahead = stat(step);
-                // all warps' (a barrier whose wait is bounded); they have left step j - 1 by then
-                ok = wait(ctl->stats[j & 1], (j >> 1) & 1);
-                if (!ok) break;
-            }
-            // which columns of this thread count: from `from` on (KEYS) up to `to`
-            int from = 0, to = 32;
-            if (KEYS) {
-                if (at == tile.tile) from = r - c0;
-                if (at == last) to = tail - c0;
-            } else if (at == tile.tile) {
-                to = r + 1 - c0;
-            }
-            const bool all = __all_sync(0xffffffffu, from <= 0 && to >= 32);
-            auto put = [&](uint32_t column, float (&x)[32], uint64_t& bar) {
-                if (!all) {
-#pragma unroll
-                    for (int c = 0; c < 32; ++c) x[c] = c >= from && c < to ? x[c] : 0.0f;
-                }
-                uint32_t w[16];
-#pragma unroll
-                for (int c = 0; c < 16; ++c) w[c] = pack2(x[2 * c], x[2 * c + 1]);
-                ptx::tmem_st16(lanes + column + c0, w);
-                ptx::tmem_st_wait();
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&bar));
-            };
-            ok = wait(ctl->sfull, j & 1);
-            if (!ok) break;
-            ptx::tc_fence_after();
-            uint32_t s[32];
-            ptx::tmem_ld32(lanes + S + c0, s);
-            if (!KEYS) {
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull));
-            }
-            float x[32];
-#pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-                const ulonglong2 l = KEYS ? sl[c / 4] : make_ulonglong2(lse, lse);
-#pragma unroll
-                for (int e = c; e < c + 4; e += 2) {
-                    split(fma2(f32x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), scale, e == c ? l.x : l.y), x[e], x[e + 1]);
-                    x[e] = ex2(x[e]);
-                    x[e + 1] = ex2(x[e + 1]);
-                }
-            }
-            if (KEYS) put(S, x, ctl->pfull);
-            ok = wait(ctl->dpfull, j & 1);
-            if (!ok) break;
-            ptx::tc_fence_after();
-            ptx::tmem_ld32(lanes + dp_at(j) + c0, s);
-#pragma unroll
-            for (int c = 0; c < 32; c += 4) {
-                const ulonglong2 d = KEYS ? sd[c / 4] : make_ulonglong2(delta, delta);
-#pragma unroll
-                for (int e = c; e < c + 4; e += 2)
-                    split(mul2(f32x2(x[e], x[e + 1]), add2(f32x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), e == c ? d.x : d.y)),
-                          x[e], x[e + 1]);
-            }
-            put(dp_at(j), x, ctl->dsfull);                          // what does not count may be infinite or NaN
-        }
-        if (ok) ok = wait(ctl->done, 0);
-        if (ok) {
-            ptx::tc_fence_after();
-            // KEYS: the first half of the threads has dV, the second dK; otherwise all have dQ
-            constexpr int PARTS = KEYS ? WARPS / 8 : WARPS / 4, WIDTH = DP / PARTS;
-            const bool first = KEYS && part < PARTS;
-            const uint32_t src = lanes + (first ? SUM_B : SUM_A);
-            const float factor = first ? 1.0f : p.scale;
-            const int o0 = part % PARTS * WIDTH;
-            const long long pitch = static_cast<long long>(owners) * p.dim * 2;
-            bf16* const out = (first ? out_b : out_a) + ((token - lane) * owners + owner) * p.dim + o0;
-            // the tiles are no longer read
-            uint8_t* const stage = smem + warp * (2 * F::TILE / WARPS);
-            uint4 w[WIDTH / 8];
-#pragma unroll
-            for (int c = 0; c < WIDTH; c += 16) {
-                float o[16];
-                ptx::tmem_ld16(src + o0 + c, o);
-                if (p.split > 1) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        *reinterpret_cast<float4*>(smem + sum_at<DP>(first, r, (o0 + c) / 4 + e)) =
-                            make_float4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                }
-#pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    w[c / 8 + e] = make_uint4(pack2(o[8 * e] * factor, o[8 * e + 1] * factor),
-                                              pack2(o[8 * e + 2] * factor, o[8 * e + 3] * factor),
-                                              pack2(o[8 * e + 4] * factor, o[8 * e + 5] * factor),
-                                              pack2(o[8 * e + 6] * factor, o[8 * e + 7] * factor));
-            }
-            if (p.split == 1)
-                store_rows(stage, w, reinterpret_cast<uint8_t*>(out), pitch, tile.length - (row - lane), (p.dim - o0) * 2, lane);
-        }
+        Slopes st;
+        st.tmem = tmem;
+        Work work;
+        bool ok = true;
+        for (int round = 0; ok && tile_of(round, work, ok); ++round)
+            ok = work.keys ? turn<DP, true>(p, x, waits, st, work, warp, lane) : turn<DP, false>(p, x, waits, st, work, warp, lane);
     }
     ptx::tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) {      // a wait that ran out: no copy stays in flight
-        wait_drain(ptx::smem_u32(&ctl->fixed), 0);
+        if (ctl->filled[2] > 0) wait_drain(ptx::smem_u32(&ctl->fixed), (ctl->filled[2] - 1) & 1);
         for (int n = max(0, ctl->filled[0] - F::SA); n < ctl->filled[0]; ++n)
             wait_drain(ptx::smem_u32(&ctl->afull[n % F::SA]), (n / F::SA) & 1);
         for (int n = max(0, ctl->filled[1] - F::SB); n < ctl->filled[1]; ++n)
@@ -848,14 +971,16 @@ template <int DP, bool KEYS> __device__ __forceinline__ void gradient_tile(const
     }
     __syncthreads();
     if (p.split == 1) return;
+    // a cluster has one tile
     ptx::cluster_sync();                         // every CTA's sums are in its shared memory
     const bool gave_up =
         lane < p.split && ptx::ld_cluster_u32(ptx::mapa(ptx::smem_u32(&ctl->abort), static_cast<uint32_t>(lane))) != 0;
-    if (!__any_sync(0xffffffffu, gave_up)) {
+    Work work;
+    if (work.get(p, blockIdx.x / p.split) && !__any_sync(0xffffffffu, gave_up)) {
         // a share of the rows each; ranks behind the last step have none
-        const int all = KEYS ? (last - begin.first + 1) * p.group : tile.tile + 1, ranks = min(p.split, all);
+        const int ranks = min(p.split, work.all), rank = blockIdx.x % p.split, owners = work.keys ? p.kv_heads : p.heads;
         const int share = ROWS / p.split, chunks = DP / 8;
-        for (int n = threadIdx.x; n < (KEYS ? 2 : 1) * share * chunks; n += blockDim.x) {
+        for (int n = threadIdx.x; n < (work.keys ? 2 : 1) * share * chunks; n += blockDim.x) {
             const int c = n % chunks, row = rank * share + n / chunks % share, which = n / (chunks * share);
             float o[8] = {};
             for (int k = 0; k < ranks; ++k)
@@ -864,10 +989,10 @@ template <int DP, bool KEYS> __device__ __forceinline__ void gradient_tile(const
                     const float4 v = ld_cluster_f4(ptx::mapa(ptx::smem_u32(smem + sum_at<DP>(which, row, 2 * c + e)), k));
                     o[4 * e] += v.x; o[4 * e + 1] += v.y; o[4 * e + 2] += v.z; o[4 * e + 3] += v.w;
                 }
-            if (tile.tile * ROWS + row >= tile.length || 8 * c >= p.dim) continue;
+            if (work.tile.tile * ROWS + row >= work.tile.length || 8 * c >= p.dim) continue;
             const float factor = which != 0 ? 1.0f : p.scale;
-            bf16* out = (which != 0 ? out_b : out_a) +
-                        (static_cast<long long>(tile.begin + tile.tile * ROWS + row) * owners + owner) * p.dim + 8 * c;
+            bf16* out = (which != 0 ? p.dv : work.keys ? p.dk : p.dq) +
+                        (static_cast<long long>(work.token() + row) * owners + work.owner) * p.dim + 8 * c;
             *reinterpret_cast<uint4*>(out) = make_uint4(pack2(o[0] * factor, o[1] * factor), pack2(o[2] * factor, o[3] * factor),
                                                         pack2(o[4] * factor, o[5] * factor), pack2(o[6] * factor, o[7] * factor));
         }
@@ -876,19 +1001,12 @@ template <int DP, bool KEYS> __device__ __forceinline__ void gradient_tile(const
     ptx::cluster_sync();                         // no CTA leaves while another reads its sums
 }
 
-// The keys' tiles first, of which a group of heads makes the longest; the queries' fill the GPU
-// behind them.  (Apart, 8192 packed tokens with 28 heads on 4 took 324 + 207 us.)
-template <int DP> __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_attention_grad(const __grid_constant__ BackwardParams p) {
-    const int keys = p.n_tiles * p.kv_heads * p.split, block = static_cast<int>(blockIdx.x);
-    if (block < keys) gradient_tile<DP, true>(p, block);
-    else gradient_tile<DP, false>(p, block - keys);
-}
-
 struct DeltaParams {
     const bf16* dout;
     const bf16* out;
     const bf16* rest;
     float* delta;
+    unsigned int* counter;                       // of the next launch, set to zero
     long long row, head;                         // pitches of dO
     int tokens, heads, dim;
 };
@@ -899,6 +1017,7 @@ struct DeltaParams {
 // row, heads of a token beside one another.
 __global__ void __launch_bounds__(256) k_attention_delta(const DeltaParams p) {
     pdl_begin();
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.counter = 0;
     const long long n = static_cast<long long>(blockIdx.x) * 16 + (threadIdx.x >> 4);
     const int c = (threadIdx.x & 15) * 8;
     const long long token = n / p.heads;
@@ -971,7 +1090,9 @@ template <int DP> cudaError_t forward_as(const ForwardParams& p, int ctas, cudaS
 template <int DP> cudaError_t backward_as(const BackwardParams& p, cudaStream_t s) {
     const cudaError_t e = allow_shared<DP>(k_attention_grad<DP>, Backward<DP>::SMEM);
     if (e != cudaSuccess) return e;
-    const unsigned int ctas = static_cast<unsigned int>(p.n_tiles) * (p.kv_heads + p.heads) * p.split;
+    // a CTA an SM, or a cluster a tile
+    const unsigned int tiles = static_cast<unsigned int>(p.n_tiles) * (p.kv_heads + p.heads);
+    const unsigned int ctas = p.split > 1 ? tiles * p.split : std::min(tiles, 152u);
     return launch(k_attention_grad<DP>, dim3(ctas), dim3(Backward<DP>::THREADS), Backward<DP>::SMEM, s, p.split, p);
 }
 
@@ -1006,8 +1127,10 @@ cudaError_t launch_attention_backward(const AttentionGrad& a, cudaStream_t s, in
         !encode(&p.dout, a.dout, a.tokens, a.heads, a.dim, a.do_row, a.do_head))
         return cudaErrorInvalidValue;
     const DeltaParams d{static_cast<const bf16*>(a.dout), static_cast<const bf16*>(a.out), static_cast<const bf16*>(a.rest),
-                        a.delta, a.do_row, a.do_head, a.tokens, a.heads, a.dim};
+                        a.delta, reinterpret_cast<unsigned int*>(a.delta + static_cast<long long>(a.tokens) * a.heads),
+                        a.do_row, a.do_head, a.tokens, a.heads, a.dim};
     const long long rows = static_cast<long long>(a.tokens) * a.heads;
+    p.counter = d.counter;
     ++*launches;
     cudaError_t e = launch(k_attention_delta, dim3(static_cast<unsigned int>((rows - 1) / 16 + 1)), dim3(256), 0, s, 1, d);
     if (e != cudaSuccess) return e;

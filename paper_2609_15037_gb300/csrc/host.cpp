@@ -760,7 +760,7 @@ PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t count) {
         const at::Tensor dq = fresh({q.tokens, q.heads, q.dim}, at::kBFloat16, device, zero);
         const at::Tensor dk = fresh({q.tokens, k.heads, q.dim}, at::kBFloat16, device, zero);
         const at::Tensor dv = fresh({q.tokens, k.heads, q.dim}, at::kBFloat16, device, zero);
-        const at::Tensor delta = fresh({rows}, at::kFloat, device);
+        const at::Tensor delta = fresh({rows + 1}, at::kFloat, device);
         const int code = fn(ctx, seqs, q.tokens, q.heads, k.heads, q.dim, static_cast<float>(scale), d.p, d.row, d.head, q.p, q.row,
                             q.head, k.p, k.row, k.head, v.p, v.row, v.head, out, rest, static_cast<const float*>(lse),
                             delta.data_ptr<float>(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), stream);

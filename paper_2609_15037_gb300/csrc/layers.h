@@ -105,7 +105,7 @@ struct AttentionGrad {
     const void* out;
     const void* rest;      // or null
     const float* lse;
-    float* delta;          // heads x tokens
+    float* delta;          // heads x tokens, and one more word
     void* dq;
     void* dk;
     void* dv;
