@@ -80,6 +80,28 @@ template <int DP> __device__ __forceinline__ void clear_rows(uint8_t* tile, int 
 }
 
 // ---------------------------------------------------------------------------
+// Which tile of which head entry n of a list of `heads` times its tiles is: sequence after sequence,
+// some heads at a time, the last tile of each first.  Tiles that run side by side are of few
+// heads, whose tensors the GPU's L2 holds (with a tile of all heads before the next one, the 128 heads
+// of four sequences of 4096 tokens come from DRAM again and again: 1662 us for their gradients, so 1428), and of the heads that come
+// last the shortest tiles come last.
+// ---------------------------------------------------------------------------
+struct Place {
+    AttentionTile sequence;
+    int tile, head;                              // tile: counted from the last
+    __device__ __forceinline__ Place(const AttentionTile* list, int n, int heads, int rows) {
+        sequence = list[n / heads];
+        const int tiles = (sequence.length - 1) / rows + 1, most = max(1, min(heads, kBeside / tiles));
+        int r = n - sequence.first * heads;
+        const int group = r / (most * tiles), have = min(most, heads - group * most);
+        r -= group * most * tiles;
+        tile = r / have;
+        head = group * most + r % have;
+    }
+    static constexpr int kBeside = 304;          // tiles of the heads that are taken together, two an SM
+};
+
+// ---------------------------------------------------------------------------
 // Outputs.  A CTA takes 256 queries of a head, two tiles of 128, and goes through the
 // keys in tiles of 128 from the sequence's first on.  While the four warps of one tile
 // turn its S into P, the tensor cores work for the other: S (128 columns of tensor memory),
@@ -190,7 +212,6 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     Ctl* ctl = reinterpret_cast<Ctl*>(ring + F::SLOTS * F::TILE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort_flag = &ctl->abort;
-    const int head = blockIdx.x % p.heads, kv = head / p.group;
     auto fill = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
         const uint32_t b = ptx::smem_u32(&bar);
         ptx::mbar_arrive_expect_tx(b, F::TILE);
@@ -214,10 +235,12 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
         pdl_begin();
-        const AttentionTile t = p.pairs[blockIdx.x / p.heads];
-        fill(smem, &p.q, ctl->qfull[0], head, t.begin + 2 * t.tile * ROWS);
+        const Place x(p.pairs, blockIdx.x, p.heads, 2 * ROWS);
+        const AttentionTile t = x.sequence;
+        const int tile = (t.length - 1) / (2 * ROWS) - x.tile, kv = x.head / p.group;
+        fill(smem, &p.q, ctl->qfull[0], x.head, t.begin + 2 * tile * ROWS);
         fill(ring, &p.k, ctl->full[0], kv, t.begin);
-        if ((2 * t.tile + 1) * ROWS < t.length) fill(smem + F::TILE, &p.q, ctl->qfull[1], head, t.begin + (2 * t.tile + 1) * ROWS);
+        if ((2 * tile + 1) * ROWS < t.length) fill(smem + F::TILE, &p.q, ctl->qfull[1], x.head, t.begin + (2 * tile + 1) * ROWS);
         fill(ring + F::TILE, &p.v, ctl->full[1], kv, t.begin);
     }
     if (warp == 9) {
@@ -229,8 +252,10 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     ptx::tc_fence_after();
     const uint32_t tmem = ctl->tmem;
     pdl_begin();
-    const AttentionTile pair = p.pairs[blockIdx.x / p.heads];
-    const int q0 = 2 * pair.tile;                                  // the first of the two tiles
+    const Place place(p.pairs, blockIdx.x, p.heads, 2 * ROWS);
+    const AttentionTile pair = place.sequence;
+    const int head = place.head, kv = head / p.group;
+    const int q0 = 2 * ((pair.length - 1) / (2 * ROWS) - place.tile);  // the first of the two tiles
     const bool second = (q0 + 1) * ROWS < pair.length;
     const int tiles = q0 + 1 + second;                             // of keys; tile i sees q0 + 1 + i
     auto wait = [&](uint64_t& bar, uint32_t parity) {
@@ -448,7 +473,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
 // keys: dQ += dS K.
 //
 // Sixteen warps turn S into P and dP = dO V^T into dS (32 columns of a row a thread), one
-// issues products, one copies.  A CTA takes tile after tile, the longest first, from a counter, each
+// issues products, one copies.  A CTA takes tile after tile from a counter, each
 // warp goes from one to the next on its own, and the next tile's first copies and products run
 // beside this one's last sums and stores.  The operand that
 // is used twice in a step (first in S, last in a sum) has three slots, the other two.  Where the
@@ -473,8 +498,7 @@ struct BackwardParams {
     bf16* dq;
     bf16* dk;
     bf16* dv;
-    const AttentionTile* q_tiles;
-    const AttentionTile* k_tiles;
+    const AttentionTile* tiles;
     unsigned int* counter;                       // of the tiles that have been taken, beyond one a CTA
     int n_tiles;
     int tokens, heads, kv_heads, group, dim;
@@ -492,12 +516,11 @@ struct BackwardCtl {
     int tiles[2];                                // the CTA's next tiles, of which the warps learn here
 };
 
-// Tile n: those of the keys first, of which a group of heads makes the longest, by falling work.
-// Its steps are every `split`-th of (head, tile) in order.  KEYS: tiles of queries from the keys' own
+// Tile n: those of the keys first, of which a group of heads makes the longest.  Its steps are every `split`-th of (head, tile) in order.  KEYS: tiles of queries from the keys' own
 // to the sequence's last, for each head of the group; otherwise tiles of keys up to the queries' own.
 struct Work {
-    AttentionTile tile;
-    int owner, kv;                               // head that the tile is of, its head of k and v
+    AttentionTile sequence;
+    int tile, owner, kv;                         // of the sequence, the head that it is of, its head of k and v
     bool keys;
     int at, head, count;                         // of the next step; steps
     int first, last, stride, all;
@@ -506,14 +529,15 @@ struct Work {
         if (n >= of_keys + p.n_tiles * p.heads) return false;
         keys = n < of_keys;
         if (!keys) n -= of_keys;
-        const int owners = keys ? p.kv_heads : p.heads;
-        tile = (keys ? p.k_tiles : p.q_tiles)[n / owners];
-        owner = n % owners;
+        const Place x(p.tiles, n, keys ? p.kv_heads : p.heads, ROWS);
+        sequence = x.sequence;
+        owner = x.head;
         kv = keys ? owner : owner / p.group;
-        last = (tile.length - 1) / ROWS;
-        first = keys ? tile.tile : 0;
+        last = (sequence.length - 1) / ROWS;
+        tile = keys ? x.tile : last - x.tile;
+        first = keys ? tile : 0;
         stride = p.split;
-        all = keys ? (last - first + 1) * p.group : tile.tile + 1;
+        all = keys ? (last - first + 1) * p.group : tile + 1;
         count = all > rank ? (all - rank - 1) / p.split + 1 : 0;
         at = first + rank;
         head = keys ? kv * p.group : kv;
@@ -531,9 +555,9 @@ struct Work {
         wrap();
     }
     // rows of the step's tile that exist
-    __device__ __forceinline__ int rows() const { return at == last ? tile.length - last * ROWS : ROWS; }
+    __device__ __forceinline__ int rows() const { return at == last ? sequence.length - last * ROWS : ROWS; }
     // first token of the tile
-    __device__ __forceinline__ int token() const { return tile.begin + tile.tile * ROWS; }
+    __device__ __forceinline__ int token() const { return sequence.begin + tile * ROWS; }
 };
 
 // Where a CTA of a cluster leaves four columns of a row of its first or second sum.
@@ -682,22 +706,22 @@ __device__ __forceinline__ bool turn(const BackwardParams& p, const Shared<DP>& 
     auto wait = [&](uint64_t& bar, uint32_t parity) { return waits.one(ptx::smem_u32(&bar), parity); };
     const int part = warp >> 2, quad = warp & 3, r = quad * 32 + lane, c0 = part * 32;
     const uint32_t lanes = st.tmem + (static_cast<uint32_t>(quad * 32) << 16);
-    const AttentionTile tile = work.tile;
-    const int row = tile.tile * ROWS + r;                           // in the sequence
-    const long long token = tile.begin + row;
+    const int tile = work.tile, begin = work.sequence.begin, length = work.sequence.length;
+    const int row = tile * ROWS + r;                                // in the sequence
+    const long long token = begin + row;
     const uint64_t scale = both(p.scale * kLog2e);
     const int owners = KEYS ? p.kv_heads : p.heads, steps = work.count;
     if (steps == 0) return true;
     uint64_t lse = 0, delta = 0;                                    // negative, of the row
-    if (!KEYS && row < tile.length) {
+    if (!KEYS && row < length) {
         lse = both(-p.lse[static_cast<long long>(work.owner) * p.tokens + token] * kLog2e);
         delta = both(-p.delta[static_cast<long long>(work.owner) * p.tokens + token]);
     }
     // KEYS: negative lse (first 128 threads) or delta (the next) of a query of a step
     auto stat = [&] {
         const int q = work.at * ROWS + r;
-        if (q >= tile.length || part >= 2) return 0.0f;
-        const long long from = static_cast<long long>(work.head) * p.tokens + tile.begin + q;
+        if (q >= length || part >= 2) return 0.0f;
+        const long long from = static_cast<long long>(work.head) * p.tokens + begin + q;
         return part == 0 ? -p.lse[from] * kLog2e : -p.delta[from];
     };
     float ahead = KEYS ? stat() : 0.0f;
@@ -719,9 +743,9 @@ __device__ __forceinline__ bool turn(const BackwardParams& p, const Shared<DP>& 
         // which columns of this thread count: from `from` on (KEYS) up to `to`
         int from = 0, to = 32;
         if (KEYS) {
-            if (at == tile.tile) from = r - c0;
+            if (at == tile) from = r - c0;
             to = rows - c0;
-        } else if (at == tile.tile) {
+        } else if (at == tile) {
             to = r + 1 - c0;
         }
         const bool all = __all_sync(0xffffffffu, from <= 0 && to >= 32);
@@ -804,7 +828,7 @@ __device__ __forceinline__ bool turn(const BackwardParams& p, const Shared<DP>& 
     if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->read));
     if (p.split > 1) return true;
     bf16* const out = (KEYS ? first ? p.dv : p.dk : p.dq) + ((token - lane) * owners + work.owner) * p.dim + o0;
-    store_rows(w, reinterpret_cast<uint8_t*>(out), static_cast<long long>(owners) * p.dim * 2, tile.length - (row - lane),
+    store_rows(w, reinterpret_cast<uint8_t*>(out), static_cast<long long>(owners) * p.dim * 2, length - (row - lane),
                (p.dim - o0) * 2, lane);
     return true;
 }
@@ -829,11 +853,11 @@ template <int DP> __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_
     };
     auto copy_a = [&](const Work& w, int slot) {
         ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->afull[slot]), F::TILE);
-        copy(x.ring_a + slot * F::TILE, w.keys ? &p.q : &p.k, ctl->afull[slot], w.head, w.tile.begin + w.at * ROWS);
+        copy(x.ring_a + slot * F::TILE, w.keys ? &p.q : &p.k, ctl->afull[slot], w.head, w.sequence.begin + w.at * ROWS);
     };
     auto copy_b = [&](const Work& w, int slot) {
         ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->bfull[slot]), F::TILE);
-        copy(x.ring_b + slot * F::TILE, w.keys ? &p.dout : &p.v, ctl->bfull[slot], w.head, w.tile.begin + w.at * ROWS);
+        copy(x.ring_b + slot * F::TILE, w.keys ? &p.dout : &p.v, ctl->bfull[slot], w.head, w.sequence.begin + w.at * ROWS);
     };
     auto copy_fixed = [&](const Work& w) {
         ptx::mbar_arrive_expect_tx(ptx::smem_u32(&ctl->fixed), 2 * F::TILE);
@@ -989,7 +1013,7 @@ template <int DP> __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_
                     const float4 v = ld_cluster_f4(ptx::mapa(ptx::smem_u32(smem + sum_at<DP>(which, row, 2 * c + e)), k));
                     o[4 * e] += v.x; o[4 * e + 1] += v.y; o[4 * e + 2] += v.z; o[4 * e + 3] += v.w;
                 }
-            if (work.tile.tile * ROWS + row >= work.tile.length || 8 * c >= p.dim) continue;
+            if (work.tile * ROWS + row >= work.sequence.length || 8 * c >= p.dim) continue;
             const float factor = which != 0 ? 1.0f : p.scale;
             bf16* out = (which != 0 ? p.dv : work.keys ? p.dk : p.dq) +
                         (static_cast<long long>(work.token() + row) * owners + work.owner) * p.dim + 8 * c;
@@ -1139,8 +1163,7 @@ cudaError_t launch_attention_backward(const AttentionGrad& a, cudaStream_t s, in
     p.dq = static_cast<bf16*>(a.dq);
     p.dk = static_cast<bf16*>(a.dk);
     p.dv = static_cast<bf16*>(a.dv);
-    p.q_tiles = a.q_tiles;
-    p.k_tiles = a.k_tiles;
+    p.tiles = a.tiles;
     p.n_tiles = a.n_tiles;
     p.tokens = a.tokens;
     p.heads = a.heads;

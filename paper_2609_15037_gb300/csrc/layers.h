@@ -75,9 +75,10 @@ size_t policy_loss_workspace(int rows);
 cudaError_t launch_policy_loss(const PolicyLoss& a, cudaStream_t s, int64_t* launches);
 
 // ------------------------------------------------------------------ attention
-// A tile of 128 rows of one sequence: first token of the sequence, its length, the tile.
+// One of a sequence's tiles (of 128 rows, or of 256): the sequence's first token and length, and
+// its first entry in the list.
 struct AttentionTile {
-    int begin, length, tile, pad;
+    int begin, length, first, pad;
 };
 
 struct Attention {
@@ -90,7 +91,7 @@ struct Attention {
     int64_t q_row, q_head, k_row, k_head, v_row, v_head;       // pitches in entries
     int tokens, heads, kv_heads, dim;
     float scale;
-    const AttentionTile* pairs;    // 256 rows each, by falling work
+    const AttentionTile* pairs;    // of 256 rows
     int n_pairs;
     int* status;
     long long wait_limit;
@@ -112,8 +113,7 @@ struct AttentionGrad {
     int64_t do_row, do_head, q_row, q_head, k_row, k_head, v_row, v_head;
     int tokens, heads, kv_heads, dim;
     float scale;
-    const AttentionTile* q_tiles;  // by falling work of a query tile
-    const AttentionTile* k_tiles;  // by falling work of a key tile
+    const AttentionTile* tiles;    // of 128 rows
     int n_tiles;
     int longest;           // tiles of the longest sequence
     long long work;        // pairs of a query tile and a key tile that it sees

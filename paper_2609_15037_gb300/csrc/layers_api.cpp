@@ -3,7 +3,8 @@
 #include <algorithm>
 #include <climits>
 #include <cmath>
-#include <cstring>
+#include <new>
+#include <vector>
 
 #include "ctx.h"
 #include "layers.h"
@@ -187,41 +188,42 @@ int moara_sequences_bytes(int count, const int* lengths, size_t* out) {
     if (out == nullptr) return MOARA_ERR_INVALID_ARG;
     long long tokens, tiles, pairs;
     const int rc = count_tiles(count, lengths, tokens, tiles, pairs);
-    if (rc == MOARA_OK) *out = static_cast<size_t>(2 * tiles + pairs) * sizeof(AttentionTile);
+    if (rc == MOARA_OK) *out = static_cast<size_t>(tiles + pairs) * sizeof(AttentionTile);
     return rc;
 }
 
-// Tiles by falling work, so that the longest begin first: pairs of query tiles, query
-// tiles, key tiles.
+// Pairs of tiles, then tiles, the longest sequences' first.
 int moara_sequences_init(int count, const int* lengths, void* to, size_t bytes, moara_sequences* out) {
     if (out == nullptr) return MOARA_ERR_INVALID_ARG;
     long long tokens, tiles, pairs;
     const int rc = count_tiles(count, lengths, tokens, tiles, pairs);
     if (rc != MOARA_OK) return rc;
-    const size_t need = static_cast<size_t>(2 * tiles + pairs) * sizeof(AttentionTile);
+    const size_t need = static_cast<size_t>(tiles + pairs) * sizeof(AttentionTile);
     if (bytes < need || (need > 0 && to == nullptr)) return MOARA_ERR_WORKSPACE;
     *out = moara_sequences{nullptr, static_cast<int>(tokens), static_cast<int>(tiles), static_cast<int>(pairs), 0, 0};
-    AttentionTile* pair = static_cast<AttentionTile*>(to);
-    AttentionTile* query = pair + pairs;
-    AttentionTile* key = query + tiles;
-    long long p = 0, n = 0;
-    int begin = 0;
-    for (int i = 0; i < count; ++i) {
-        for (int t = 0; t * 128LL < lengths[i]; ++t, ++n) {
-            query[n] = key[n] = AttentionTile{begin, lengths[i], t, 0};
-            if (t % 2 == 0) pair[p++] = AttentionTile{begin, lengths[i], t / 2, 0};
+    try {
+        std::vector<AttentionTile> seqs;
+        int begin = 0;
+        for (int i = 0; i < count; begin += lengths[i++])
+            if (lengths[i] > 0) seqs.push_back(AttentionTile{begin, lengths[i], 0, 0});
+        std::stable_sort(seqs.begin(), seqs.end(), [](const AttentionTile& a, const AttentionTile& b) { return a.length > b.length; });
+        AttentionTile* at = static_cast<AttentionTile*>(to);
+        for (const int rows : {256, 128}) {
+            int first = 0;
+            for (AttentionTile s : seqs) {
+                const int n = (s.length - 1) / rows + 1;
+                s.first = first;
+                at = std::fill_n(at, n, s);
+                first += n;
+                if (rows == 128) {
+                    out->longest = std::max(out->longest, n);
+                    out->work += n * (n + 1LL) / 2;
+                }
+            }
         }
-        begin += lengths[i];
-        const long long n_seq = (static_cast<long long>(lengths[i]) + 127) / 128;
-        out->longest = std::max(out->longest, static_cast<int>(n_seq));
-        out->work += n_seq * (n_seq + 1) / 2;
+    } catch (const std::bad_alloc&) {
+        return MOARA_ERR_WORKSPACE;
     }
-    const auto later = [](const AttentionTile& a, const AttentionTile& b) { return a.tile > b.tile; };
-    std::stable_sort(pair, pair + pairs, later);
-    std::stable_sort(query, query + tiles, later);
-    std::stable_sort(key, key + tiles, [](const AttentionTile& a, const AttentionTile& b) {
-        return (a.length - 1) / 128 - a.tile > (b.length - 1) / 128 - b.tile;
-    });
     return MOARA_OK;
 }
 
@@ -270,7 +272,7 @@ int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int to
     DeviceGuard g(ctx->device);
     const AttentionTile* tiles = static_cast<const AttentionTile*>(seqs->tiles) + seqs->n_pairs;
     const moara::AttentionGrad a{dout, q, k, v, out, rest, lse, delta, dq, dk, dv, do_row, do_head, q_row, q_head, k_row, k_head,
-                                 v_row, v_head, tokens, heads, kv_heads, dim, scale, tiles, tiles + seqs->n_tiles, seqs->n_tiles,
+                                 v_row, v_head, tokens, heads, kv_heads, dim, scale, tiles, seqs->n_tiles,
                                  seqs->longest, seqs->work, ctx->d_status, moara::tc_wait_limit(ctx->tc)};
     const cudaError_t e = moara::launch_attention_backward(a, static_cast<cudaStream_t>(stream), &ctx->launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "attention gradient launch");
