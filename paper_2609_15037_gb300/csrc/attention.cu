@@ -35,6 +35,12 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float y;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
+    return y;
+}
+
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -52,19 +58,29 @@ template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t 
 
 // The same tile as the operand whose rows are summed over: D (128 x DP) (+)= A B with A in
 // tensor memory, RUN entries of K in columns a .. a + RUN / 2 - 1, RUN more from a + PITCH on
-// and so on; the first 16 `steps` rows of B.
-template <int DP, int RUN, int PITCH>
+// and so on; of the first 16 `steps` rows of B those from 16 FROM up to 16 TO.
+template <int DP, int RUN, int PITCH, int FROM = 0, int TO = ROWS / 16>
 __device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint32_t b, int steps, bool add) {
     constexpr uint32_t idesc = ptx::idesc_bf16(128, DP, 0, 1);
     const auto one = [&](int k, uint32_t acc) {
         ptx::mma_f16_ta(d, a + k * 16 / RUN * PITCH + k * 16 % RUN / 2, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, acc);
     };
-    one(0, add);
-    if (steps == ROWS / 16) {                                      // a test for each would take as long as a product
+    // a test for each would take as long as a product; where the first is issued outside of the branch a
+    // forward step of two halves takes 3% longer, where it is inside one of the gradients 1.5%
+    if (FROM == 0 && TO == ROWS / 16) {
+        one(0, add);
+        if (steps >= TO) {
 #pragma unroll
-        for (int k = 1; k < ROWS / 16; ++k) one(k, 1);
+            for (int k = 1; k < TO; ++k) one(k, 1);
+        } else {
+            for (int k = 1; k < steps; ++k) one(k, 1);
+        }
+    } else if (steps >= TO) {
+        one(FROM, add);
+#pragma unroll
+        for (int k = FROM + 1; k < TO; ++k) one(k, 1);
     } else {
-        for (int k = 1; k < steps; ++k) one(k, 1);
+        for (int k = FROM; k < steps; ++k) one(k, add || k > FROM);
     }
 }
 
@@ -195,7 +211,7 @@ struct Waits {
 };
 
 template <int SLOTS> struct ForwardCtl {
-    uint64_t qfull[2], full[SLOTS], empty[SLOTS], sfull[2], pfull[2], ofull[2], drain;
+    uint64_t qfull[2], full[SLOTS], empty[SLOTS], sfull[2], pfull[2][2], ofull[2], drain;
     uint32_t tmem;
     int abort;
     int filled;
@@ -222,7 +238,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl->qfull[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl->sfull[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&ctl->pfull[i]), 4);
+            for (int h = 0; h < 2; ++h) ptx::mbar_init(ptx::smem_u32(&ctl->pfull[i][h]), 4);
             ptx::mbar_init(ptx::smem_u32(&ctl->ofull[i]), 1);
         }
         for (int i = 0; i < F::SLOTS; ++i) {
@@ -299,7 +315,7 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             if (ok) release(0);
         }
         const Waits waits{abort_flag, p.status, p.wait_limit};
-        const uint32_t full = ptx::smem_u32(&ctl->full[0]), pfull = ptx::smem_u32(&ctl->pfull[0]);
+        const uint32_t full = ptx::smem_u32(&ctl->full[0]), pfull = ptx::smem_u32(&ctl->pfull[0][0]);
         for (int j = 0; j < tiles && ok; ++j) {
             const int n = 2 * j + 1, vs = n % F::SLOTS, ks = (n + 1) % F::SLOTS;
             const bool more = j + 1 < tiles;
@@ -308,15 +324,20 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             const uint32_t v = slots + vs * F::TILE, k = slots + ks * F::TILE;
             const uint32_t vp = (n / F::SLOTS) & 1, kp = ((n + 1) / F::SLOTS) & 1;
             const bool one = j <= q0;                               // the first tile of queries sees these keys
-            const uint32_t first = pfull + (one ? 0 : 8);           // whose P comes first
+            const uint32_t first = pfull + (one ? 0 : 16);          // whose P comes first
             ok = more ? waits.three(full + 8 * vs, vp, full + 8 * ks, kp, first, j & 1)
                       : waits.two(full + 8 * vs, vp, first, j & 1);
             if (!ok) break;
             if (left < ROWS && left % 16 != 0) clear_rows<DP>(ring + vs * F::TILE, left, lane);
             if (one) {
                 ptx::tc_fence_after();
+                // P comes in halves, so that its product begins before all of it is there
+                if (leader) mma_sum<DP, ROWS, 0, 0, 4>(tmem + 256, tmem, v, steps, j > 0);
+                __syncwarp();
+                if (!(ok = waits.one(pfull + 8, j & 1))) break;
+                ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, ROWS, 0>(tmem + 256, tmem, v, steps, j > 0);
+                    mma_sum<DP, ROWS, 0, 4, 8>(tmem + 256, tmem, v, steps, true);
                     if (j == q0) {
                         ptx::mma_commit(ptx::smem_u32(&ctl->ofull[0]));
                     } else {
@@ -326,12 +347,16 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
                     }
                 }
                 __syncwarp();
-                if (second && !(ok = waits.one(pfull + 8, j & 1))) break;
+                if (second && !(ok = waits.one(pfull + 16, j & 1))) break;
             }
             if (second) {
                 ptx::tc_fence_after();
+                if (leader) mma_sum<DP, ROWS, 0, 0, 4>(tmem + 256 + DP, tmem + ROWS, v, steps, j > 0);
+                __syncwarp();
+                if (!(ok = waits.one(pfull + 24, j & 1))) break;
+                ptx::tc_fence_after();
                 if (leader) {
-                    mma_sum<DP, ROWS, 0>(tmem + 256 + DP, tmem + ROWS, v, steps, j > 0);
+                    mma_sum<DP, ROWS, 0, 4, 8>(tmem + 256 + DP, tmem + ROWS, v, steps, true);
                     if (!more) {
                         ptx::mma_commit(ptx::smem_u32(&ctl->ofull[1]));
                     } else {
@@ -373,7 +398,8 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             }
             float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int c = 0; c < ROWS; ++c) top[c % 4] = fmaxf(top[c % 4], __uint_as_float(s[c / 64][c % 64]));
+            for (int c = 0; c < ROWS; c += 2)
+                top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(s[c / 64][c % 64]), __uint_as_float(s[c / 64][c % 64 + 1]));
             float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
             if (high == -INFINITY) high = 0.0f;                     // nothing finite
             if (j == 0) {
@@ -407,14 +433,14 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
                     w[c] = pack2(a, b);
                 }
                 ptx::tmem_st32(st + 32 * h, w);
+                ptx::tmem_st_wait();
+                ptx::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull[i][h]));
             }
             float a, b;
             split(add2(part[0], part[1]), a, b);
             sum += a + b;
-            ptx::tmem_st_wait();
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull[i]));
         }
         if (ok) ok = wait(ctl->ofull[i], 0);
         if (ok) {
