@@ -401,7 +401,8 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
             for (int c = 0; c < ROWS; c += 2)
                 top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(s[c / 64][c % 64]), __uint_as_float(s[c / 64][c % 64 + 1]));
             float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-            if (high == -INFINITY) high = 0.0f;                     // nothing finite
+            // nothing but minus infinity: a reference that the first finite score replaces
+            if (high == -INFINITY) high = -1e30f;
             if (j == 0) {
                 ref = high;
             } else if (__any_sync(0xffffffffu, (high - ref) * scale > 8.0f)) {

@@ -144,6 +144,22 @@ def test_sequences_do_not_meet(layer, d):
         assert x[bad].isnan().all()
 
 
+def test_keys_without_probability(layer):
+    """A first tile of keys whose scores are minus infinity, before scores far below zero."""
+    q, k, v, _ = (x.clone() for x in inputs(600, 2, 1, 64))
+    q[:, :, 0], k[:, :, 0] = 1.0, -2000.0
+    k[:128, :, 0] = float("-inf")
+    out, lse = layer.attention(q, k, v, layer.sequences([600]))
+    want, tol = R.attention(q, k, v, [600], 0.125)
+    eS = (q.double().abs().amax() * 64 * 8 + 2000) * 0.125 * 12 * 2.0 ** -23        # of the scores that count
+    for n in range(2):
+        vs = v[128:, 0].double()
+        slack = (2.0 ** -8 + 2 * eS + 2.0 ** -20 * want["lse"][n, 128:].abs().amax()) * vs.abs().amax() * 2
+        assert (out[128:, n].double() - want["out"][128:, n]).abs().amax() <= slack
+        assert (lse[n, 128:].double() - want["lse"][n, 128:]).abs().amax() <= eS + 2.0 ** -22 * 300
+    assert out[:128].isnan().all() and want["out"][:128].isnan().all()
+
+
 def test_rest_is_what_the_rounding_dropped(layer):
     q, k, v, do = inputs(500, 2, 1, 128)
     seqs = layer.sequences([500])
