@@ -46,13 +46,20 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Descriptors of a tile, as an operand by rows and as the one whose rows are summed over, and
+// that of a tile some bytes further on (they count in 16 bytes).  A product issues in fewer clocks where its
+// descriptors are one number and constants (16384 tokens: 1202 us with each worked out, 1177 so).
+__device__ __forceinline__ uint64_t by_rows(uint32_t tile) { return ptx::smem_desc_sw128(tile, 16, 1024); }
+__device__ __forceinline__ uint64_t to_sum(uint32_t tile) { return ptx::smem_desc_sw128(tile, PANEL, 1024); }
+__device__ __forceinline__ uint64_t beside(uint64_t d, int bytes) { return d + static_cast<uint64_t>(bytes / 16); }
+
 // D = A B^T over DP columns, both tiles in shared memory by rows (K-major): 128 x 128.
-template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t a, uint32_t b) {
+template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint64_t da, uint64_t db) {
     constexpr uint32_t idesc = ptx::idesc_bf16(128, ROWS, 0, 0);
 #pragma unroll
     for (int k = 0; k < DP / 16; ++k) {
-        const uint32_t at = k / 4 * PANEL + k % 4 * 32;
-        ptx::mma_f16(d, ptx::smem_desc_sw128(a + at, 16, 1024), ptx::smem_desc_sw128(b + at, 16, 1024), idesc, k > 0);
+        const int at = k / 4 * PANEL + k % 4 * 32;
+        ptx::mma_f16(d, beside(da, at), beside(db, at), idesc, k > 0);
     }
 }
 
@@ -60,10 +67,10 @@ template <int DP> __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t 
 // tensor memory, RUN entries of K in columns a .. a + RUN / 2 - 1, RUN more from a + PITCH on
 // and so on; of the first 16 `steps` rows of B those from 16 FROM up to 16 TO.
 template <int DP, int RUN, int PITCH, int FROM = 0, int TO = ROWS / 16>
-__device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint32_t b, int steps, bool add) {
+__device__ __forceinline__ void mma_sum(uint32_t d, uint32_t a, uint64_t db, int steps, bool add) {
     constexpr uint32_t idesc = ptx::idesc_bf16(128, DP, 0, 1);
     const auto one = [&](int k, uint32_t acc) {
-        ptx::mma_f16_ta(d, a + k * 16 / RUN * PITCH + k * 16 % RUN / 2, ptx::smem_desc_sw128(b + k * 2048, PANEL, 1024), idesc, acc);
+        ptx::mma_f16_ta(d, a + k * 16 / RUN * PITCH + k * 16 % RUN / 2, beside(db, k * 2048), idesc, acc);
     };
     // a test for each would take as long as a product; where the first is issued outside of the branch a
     // forward step of two halves takes 3% longer, where it is inside one of the gradients 1.5%
@@ -128,8 +135,9 @@ struct Place {
 template <int DP> struct Forward {
     static constexpr int TILE = DP / 64 * PANEL;
     static constexpr int SLOTS = DP == 128 ? 4 : 8;                // tiles of K and V in turn
-    static constexpr int CTL = 256;
-    static constexpr int SMEM = (2 + SLOTS) * TILE + CTL + 1024;
+    static constexpr int STAGE = 8 * 2048;                         // of the warps that store O
+    static constexpr int CTL = 384;
+    static constexpr int SMEM = (2 + SLOTS) * TILE + STAGE + CTL;
     static constexpr int THREADS = 10 * 32;                        // two tiles' warps, copies, products
 };
 
@@ -140,7 +148,7 @@ struct ForwardParams {
     float* lse;
     const AttentionTile* pairs;
     int tokens, heads, group, dim;
-    float scale;
+    float scale, scale2;                         // of natural exponentials, and of powers of two
     int* status;
     long long wait_limit;
 };
@@ -210,24 +218,76 @@ struct Waits {
     }
 };
 
-template <int SLOTS> struct ForwardCtl {
-    uint64_t qfull[2], full[SLOTS], empty[SLOTS], sfull[2], pfull[2][2], ofull[2], drain;
-    uint32_t tmem;
-    int abort;
-    int filled;
+// Two tiles of 128 queries of a head.
+struct alignas(16) Pair {
+    int begin, length, head;
+    int q0;                                      // the first of the two, -1: no more of them
+    __device__ __forceinline__ bool second() const { return (q0 + 1) * ROWS < length; }
+    __device__ __forceinline__ int tiles() const { return q0 + 1 + second(); }     // of keys; tile i of the two sees q0 + 1 + i
 };
 
-template <int DP>
+__device__ __forceinline__ Pair pair_at(const ForwardParams& p, int n) {
+    const Place x(p.pairs, n, p.heads, 2 * ROWS);
+    return Pair{x.sequence.begin, x.sequence.length, x.head, 2 * ((x.sequence.length - 1) / (2 * ROWS) - x.tile)};
+}
+
+// Asks for a CTA of the grid that has not begun, in whose place this one goes on: the answer
+// comes to shared memory beside the work.  Not again behind a refusal.
+__device__ __forceinline__ void request(uint4* to, uint64_t& bar) {
+    const uint32_t b = ptx::smem_u32(&bar);
+    ptx::fence_proxy_async_smem();               // the last answer has been read
+    ptx::mbar_arrive_expect_tx(b, 16);
+    asm volatile("clusterlaunchcontrol.try_cancel.async.shared::cta.mbarrier::complete_tx::bytes.b128 [%0], [%1];" ::"r"(
+                     ptx::smem_u32(to)),
+                 "r"(b)
+                 : "memory");
+}
+
+// The index of that CTA, or -1.
+__device__ __forceinline__ int answer(const uint4* from) {
+    int n;
+    asm volatile(
+        "{\n\t.reg .b128 r;\n\t.reg .pred p;\n\t"
+        "ld.shared.b128 r, [%1];\n\t"
+        "clusterlaunchcontrol.query_cancel.is_canceled.pred.b128 p, r;\n\t"
+        "mov.b32 %0, -1;\n\t"
+        "@p clusterlaunchcontrol.query_cancel.get_first_ctaid::x.b32.b128 %0, r;\n\t}"
+        : "=r"(n)
+        : "r"(ptx::smem_u32(from))
+        : "memory");
+    return n;
+}
+
+template <int SLOTS> struct ForwardCtl {
+    alignas(16) uint4 answer;                    // to the request for another CTA's tiles
+    Pair pairs[2];                               // this CTA's, in turn
+    struct {
+        uint64_t sfull, pfull[2], ofull;
+    } of[2];                                     // the two tiles of queries
+    uint64_t qfull[2], qempty[2], full[SLOTS], empty[SLOTS], drain, answered, listed[2], taken[2];
+    uint32_t tmem;
+    int abort;
+    uint32_t filled;                             // phases of the ring's last copies
+    int filled_q[2];                             // copies of queries
+};
+
+// ONE: a CTA has one pair; otherwise it goes on with those of CTAs that have not begun, its next copies
+// beside its last steps.
+template <int DP, bool ONE>
 __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __grid_constant__ ForwardParams p) {
     using F = Forward<DP>;
     using Ctl = ForwardCtl<F::SLOTS>;
     static_assert(sizeof(Ctl) <= F::CTL, "the barriers fit");
-    extern __shared__ uint8_t raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~uintptr_t(1023));
+    extern __shared__ __align__(1024) uint8_t smem[];              // aligned here its addresses would be in registers
     uint8_t* ring = smem + 2 * F::TILE;
-    Ctl* ctl = reinterpret_cast<Ctl*>(ring + F::SLOTS * F::TILE);
+    uint8_t* stages = ring + F::SLOTS * F::TILE;
+    Ctl* ctl = reinterpret_cast<Ctl*>(stages + F::STAGE);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     volatile int* abort_flag = &ctl->abort;
+    if ((ptx::smem_u32(smem) & 1023u) != 0) {                       // the same in every CTA
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, MOARA_ERR_ALIGN);
+        return;
+    }
     auto fill = [&](uint8_t* to, const CUtensorMap* map, uint64_t& bar, int h, int row) {
         const uint32_t b = ptx::smem_u32(&bar);
         ptx::mbar_arrive_expect_tx(b, F::TILE);
@@ -236,28 +296,27 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     if (threadIdx.x == 8 * 32) {
         // the thread that copies starts what the first products need beside the others' set-up
         for (int i = 0; i < 2; ++i) {
-            ptx::mbar_init(ptx::smem_u32(&ctl->qfull[i]), 1);
-            ptx::mbar_init(ptx::smem_u32(&ctl->sfull[i]), 1);
-            for (int h = 0; h < 2; ++h) ptx::mbar_init(ptx::smem_u32(&ctl->pfull[i][h]), 4);
-            ptx::mbar_init(ptx::smem_u32(&ctl->ofull[i]), 1);
+            for (uint64_t* x : {&ctl->qfull[i], &ctl->qempty[i], &ctl->of[i].sfull, &ctl->of[i].ofull, &ctl->listed[i]})
+                ptx::mbar_init(ptx::smem_u32(x), 1);
+            for (int h = 0; h < 2; ++h) ptx::mbar_init(ptx::smem_u32(&ctl->of[i].pfull[h]), 4);
+            ptx::mbar_init(ptx::smem_u32(&ctl->taken[i]), 9);
         }
         for (int i = 0; i < F::SLOTS; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl->full[i]), 1);
             ptx::mbar_init(ptx::smem_u32(&ctl->empty[i]), 1);
         }
         ptx::mbar_init(ptx::smem_u32(&ctl->drain), 1);
+        ptx::mbar_init(ptx::smem_u32(&ctl->answered), 1);
         ctl->abort = 0;
-        ctl->filled = 2;
         ptx::fence_barrier_init();
         ptx::fence_proxy_async_smem();
         pdl_begin();
-        const Place x(p.pairs, blockIdx.x, p.heads, 2 * ROWS);
-        const AttentionTile t = x.sequence;
-        const int tile = (t.length - 1) / (2 * ROWS) - x.tile, kv = x.head / p.group;
-        fill(smem, &p.q, ctl->qfull[0], x.head, t.begin + 2 * tile * ROWS);
-        fill(ring, &p.k, ctl->full[0], kv, t.begin);
-        if ((2 * tile + 1) * ROWS < t.length) fill(smem + F::TILE, &p.q, ctl->qfull[1], x.head, t.begin + (2 * tile + 1) * ROWS);
-        fill(ring + F::TILE, &p.v, ctl->full[1], kv, t.begin);
+        const Pair x = pair_at(p, blockIdx.x);
+        ctl->pairs[0] = x;
+        fill(smem, &p.q, ctl->qfull[0], x.head, x.begin + x.q0 * ROWS);
+        fill(ring, &p.k, ctl->full[0], x.head / p.group, x.begin);
+        if (x.second()) fill(smem + F::TILE, &p.q, ctl->qfull[1], x.head, x.begin + (x.q0 + 1) * ROWS);
+        fill(ring + F::TILE, &p.v, ctl->full[1], x.head / p.group, x.begin);
     }
     if (warp == 9) {
         ptx::tmem_alloc(ptx::smem_u32(&ctl->tmem), 512);
@@ -268,221 +327,298 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
     ptx::tc_fence_after();
     const uint32_t tmem = ctl->tmem;
     pdl_begin();
-    const Place place(p.pairs, blockIdx.x, p.heads, 2 * ROWS);
-    const AttentionTile pair = place.sequence;
-    const int head = place.head, kv = head / p.group;
-    const int q0 = 2 * ((pair.length - 1) / (2 * ROWS) - place.tile);  // the first of the two tiles
-    const bool second = (q0 + 1) * ROWS < pair.length;
-    const int tiles = q0 + 1 + second;                             // of keys; tile i sees q0 + 1 + i
     auto wait = [&](uint64_t& bar, uint32_t parity) {
         return ptx::mbar_wait_warp(ptx::smem_u32(&bar), parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
     };
 
+    // the CTA's pair of a round, to every warp but the one that copies, until the warp has done with it
+    auto pair_of = [&](int round, bool& ok) {
+        if (round > 0) ok = wait(ctl->listed[round & 1], (round - 1) >> 1 & 1);
+        return ok ? ctl->pairs[round & 1] : Pair{0, 0, 0, -1};
+    };
+    auto done_with = [&](int round) {
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->taken[round & 1]));
+    };
+
     if (warp == 8) {
         if (lane == 0) {
-            int n = 2;
-            for (; n < 2 * tiles; ++n) {
-                const int slot = n % F::SLOTS;
-                if (n >= F::SLOTS && !ptx::mbar_wait(ptx::smem_u32(&ctl->empty[slot]), (n / F::SLOTS - 1) & 1, abort_flag, p.status,
-                                                     MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
+            auto until = [&](uint64_t& bar, int phase) {
+                return ptx::mbar_wait(ptx::smem_u32(&bar), phase & 1, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
+            };
+            uint32_t phases = ~0u;                                  // of the ring's slots
+            int nq[2] = {};                                         // copies of queries
+            bool ok = true;
+            Pair x = ctl->pairs[0];
+            for (int round = 0; ok && x.q0 >= 0; ++round) {
+                const int kv = x.head / p.group, copies = 2 * x.tiles();
+                auto copy_q = [&](int i) {
+                    ok = nq[i] == 0 || until(ctl->qempty[i], nq[i] - 1);
+                    if (!ok) return;
+                    if (round > 0) fill(smem + i * F::TILE, &p.q, ctl->qfull[i], x.head, x.begin + (x.q0 + i) * ROWS);
+                    ++nq[i];
+                };
+                auto copy = [&](int j) {
+                    const int slot = j % F::SLOTS;
+                    if (round > 0 || j > 1) {                       // those are begun above
+                        // of a slot that has not been filled: the phase before its first
+                        ok = until(ctl->empty[slot], phases >> slot);
+                        if (!ok) return;
+                        fill(ring + slot * F::TILE, j & 1 ? &p.v : &p.k, ctl->full[slot], kv, x.begin + j / 2 * ROWS);
+                    }
+                    phases ^= 1u << slot;
+                };
+                bool asked = false;
+                copy_q(0);
+                for (int j = 0; ok && j < copies; ++j) {
+                    // a CTA's tiles that has not begun, once this one's last step is near
+                    if (!ONE && j == copies - 2) {
+                        request(&ctl->answer, ctl->answered);
+                        asked = true;
+                    }
+                    copy(j);
+                    if (ok && j == 0 && x.second()) copy_q(1);
+                }
+                if (ONE) break;
+                if (!ok || !until(ctl->answered, round)) {
+                    if (asked) wait_drain(ptx::smem_u32(&ctl->answered), round & 1);
                     break;
-                fill(ring + slot * F::TILE, n & 1 ? &p.v : &p.k, ctl->full[slot], kv, pair.begin + n / 2 * ROWS);
+                }
+                const int next = answer(&ctl->answer);
+                if (next >= 0) x = pair_at(p, next);
+                else x.q0 = -1;
+                const int slot = (round + 1) & 1;
+                ok = round == 0 || until(ctl->taken[slot], (round - 1) >> 1);
+                if (!ok) break;
+                ctl->pairs[slot] = x;
+                ptx::mbar_arrive(ptx::smem_u32(&ctl->listed[slot]));
             }
-            ctl->filled = n;
+            ctl->filled = phases;
+            for (int i = 0; i < 2; ++i) ctl->filled_q[i] = nq[i];
         }
     } else if (warp == 9) {
         const bool leader = ptx::elect_one();
         const uint32_t base = ptx::smem_u32(smem), slots = ptx::smem_u32(ring);
-        auto score = [&](int i, int slot) {
-            if (leader) {
-                mma_rows<DP>(tmem + i * ROWS, base + i * F::TILE, slots + slot * F::TILE);
-                ptx::mma_commit(ptx::smem_u32(&ctl->sfull[i]));
-            }
-            __syncwarp();
-        };
-        auto release = [&](int slot) {
-            if (leader) ptx::mma_commit(ptx::smem_u32(&ctl->empty[slot]));
-            __syncwarp();
-        };
-        bool ok = wait(ctl->qfull[0], 0) && wait(ctl->full[0], 0);
-        if (ok) {
-            ptx::tc_fence_after();
-            score(0, 0);
-            if (second) {
-                ok = wait(ctl->qfull[1], 0);
-                if (ok) score(1, 0);
-            }
-            if (ok) release(0);
-        }
         const Waits waits{abort_flag, p.status, p.wait_limit};
-        const uint32_t full = ptx::smem_u32(&ctl->full[0]), pfull = ptx::smem_u32(&ctl->pfull[0][0]);
-        for (int j = 0; j < tiles && ok; ++j) {
-            const int n = 2 * j + 1, vs = n % F::SLOTS, ks = (n + 1) % F::SLOTS;
-            const bool more = j + 1 < tiles;
-            const int left = pair.length - j * ROWS;                // keys from this tile on
-            const int steps = left >= ROWS ? ROWS / 16 : (left + 15) / 16;
-            const uint32_t v = slots + vs * F::TILE, k = slots + ks * F::TILE;
-            const uint32_t vp = (n / F::SLOTS) & 1, kp = ((n + 1) / F::SLOTS) & 1;
-            const bool one = j <= q0;                               // the first tile of queries sees these keys
-            const uint32_t first = pfull + (one ? 0 : 16);          // whose P comes first
-            ok = more ? waits.three(full + 8 * vs, vp, full + 8 * ks, kp, first, j & 1)
-                      : waits.two(full + 8 * vs, vp, first, j & 1);
+        const uint32_t full = ptx::smem_u32(&ctl->full[0]), pfull = ptx::smem_u32(&ctl->of[0].pfull[0]);
+        uint32_t step[2] = {}, tile[2] = {};                        // of each of the two tiles, so far
+        uint32_t phases = 0;                                        // of the ring's slots, with whose first a pair begins
+        bool ok = true;
+        for (int round = 0; !ONE || round < 1; ++round) {
+            const Pair x = pair_of(round, ok);
+            if (x.q0 < 0) break;
+            const bool second = x.second();
+            const int tiles = x.tiles();
+            done_with(round);
+            {
+                // S over the last pair's P, whose product is in front; its O stays until this pair's P is there
+                const uint32_t qfull = ptx::smem_u32(&ctl->qfull[0]);
+                auto score = [&](int i) {
+                    ptx::tc_fence_after();
+                    if (leader) {
+                        mma_rows<DP>(tmem + i * ROWS, by_rows(base + i * F::TILE), by_rows(slots));
+                        ptx::mma_commit(ptx::smem_u32(&ctl->of[i].sfull));
+                        if (i == 0 && x.q0 == 0) ptx::mma_commit(ptx::smem_u32(&ctl->qempty[0]));
+                    }
+                    __syncwarp();
+                };
+                if (!(ok = waits.two(qfull, tile[0]++ & 1, full, phases & 1))) break;
+                score(0);
+                if (second) {
+                    if (!(ok = waits.one(qfull + 8, tile[1]++ & 1))) break;
+                    score(1);
+                }
+                phases ^= 1;
+                if (leader) ptx::mma_commit(ptx::smem_u32(&ctl->empty[0]));
+                __syncwarp();
+            }
+            for (int j = 0; j < tiles && ok; ++j) {
+                const int vs = (2 * j + 1) % F::SLOTS, ks = (2 * j + 2) % F::SLOTS;
+                const bool more = j + 1 < tiles;
+                const int left = x.length - j * ROWS;                // keys from this tile on
+                const int steps = left >= ROWS ? ROWS / 16 : (left + 15) / 16;
+                const uint32_t v = slots + vs * F::TILE, k = slots + ks * F::TILE;
+                const uint32_t vp = phases >> vs & 1, kp = phases >> ks & 1;
+                const bool one = j <= x.q0;                              // the first tile of queries sees these keys
+                const uint32_t first = pfull + (one ? 0 : 32), parity = (one ? step[0] : step[1]) & 1;  // whose P comes first
+                ok = more ? waits.three(full + 8 * vs, vp, full + 8 * ks, kp, first, parity)
+                          : waits.two(full + 8 * vs, vp, first, parity);
+                if (!ok) break;
+                phases ^= 1u << vs | (more ? 1u << ks : 0);
+                if (left < ROWS && left % 16 != 0) clear_rows<DP>(ring + vs * F::TILE, left, lane);
+                if (one) {
+                    ptx::tc_fence_after();
+                    // P comes in halves, so that its product begins before all of it is there
+                    if (leader) mma_sum<DP, ROWS, 0, 0, 4>(tmem + 256, tmem, to_sum(v), steps, j > 0);
+                    __syncwarp();
+                    if (!(ok = waits.one(pfull + 8, step[0] & 1))) break;
+                    ptx::tc_fence_after();
+                    if (leader) {
+                        mma_sum<DP, ROWS, 0, 4, 8>(tmem + 256, tmem, to_sum(v), steps, true);
+                        if (j == x.q0) {
+                            ptx::mma_commit(ptx::smem_u32(&ctl->of[0].ofull));
+                        } else {
+                            // S over the P that the product in front of it has read by then
+                            mma_rows<DP>(tmem, by_rows(base), by_rows(k));
+                            ptx::mma_commit(ptx::smem_u32(&ctl->of[0].sfull));
+                            if (j + 1 == x.q0) ptx::mma_commit(ptx::smem_u32(&ctl->qempty[0]));
+                        }
+                    }
+                    __syncwarp();
+                    ++step[0];
+                    if (second && !(ok = waits.one(pfull + 32, step[1] & 1))) break;
+                }
+                if (second) {
+                    ptx::tc_fence_after();
+                    if (leader) mma_sum<DP, ROWS, 0, 0, 4>(tmem + 256 + DP, tmem + ROWS, to_sum(v), steps, j > 0);
+                    __syncwarp();
+                    if (!(ok = waits.one(pfull + 40, step[1] & 1))) break;
+                    ptx::tc_fence_after();
+                    if (leader) {
+                        mma_sum<DP, ROWS, 0, 4, 8>(tmem + 256 + DP, tmem + ROWS, to_sum(v), steps, true);
+                        if (!more) {
+                            ptx::mma_commit(ptx::smem_u32(&ctl->of[1].ofull));
+                        } else {
+                            mma_rows<DP>(tmem + ROWS, by_rows(base + F::TILE), by_rows(k));
+                            ptx::mma_commit(ptx::smem_u32(&ctl->of[1].sfull));
+                            if (j + 2 == tiles) ptx::mma_commit(ptx::smem_u32(&ctl->qempty[1]));
+                        }
+                    }
+                    __syncwarp();
+                    ++step[1];
+                }
+                if (leader) {
+                    ptx::mma_commit(ptx::smem_u32(&ctl->empty[vs]));
+                    if (more) ptx::mma_commit(ptx::smem_u32(&ctl->empty[ks]));
+                }
+                __syncwarp();
+            }
             if (!ok) break;
-            if (left < ROWS && left % 16 != 0) clear_rows<DP>(ring + vs * F::TILE, left, lane);
-            if (one) {
-                ptx::tc_fence_after();
-                // P comes in halves, so that its product begins before all of it is there
-                if (leader) mma_sum<DP, ROWS, 0, 0, 4>(tmem + 256, tmem, v, steps, j > 0);
-                __syncwarp();
-                if (!(ok = waits.one(pfull + 8, j & 1))) break;
-                ptx::tc_fence_after();
-                if (leader) {
-                    mma_sum<DP, ROWS, 0, 4, 8>(tmem + 256, tmem, v, steps, true);
-                    if (j == q0) {
-                        ptx::mma_commit(ptx::smem_u32(&ctl->ofull[0]));
-                    } else {
-                        // S over the P that the product in front of it has read by then
-                        mma_rows<DP>(tmem, base, k);
-                        ptx::mma_commit(ptx::smem_u32(&ctl->sfull[0]));
-                    }
-                }
-                __syncwarp();
-                if (second && !(ok = waits.one(pfull + 16, j & 1))) break;
-            }
-            if (second) {
-                ptx::tc_fence_after();
-                if (leader) mma_sum<DP, ROWS, 0, 0, 4>(tmem + 256 + DP, tmem + ROWS, v, steps, j > 0);
-                __syncwarp();
-                if (!(ok = waits.one(pfull + 24, j & 1))) break;
-                ptx::tc_fence_after();
-                if (leader) {
-                    mma_sum<DP, ROWS, 0, 4, 8>(tmem + 256 + DP, tmem + ROWS, v, steps, true);
-                    if (!more) {
-                        ptx::mma_commit(ptx::smem_u32(&ctl->ofull[1]));
-                    } else {
-                        mma_rows<DP>(tmem + ROWS, base + F::TILE, k);
-                        ptx::mma_commit(ptx::smem_u32(&ctl->sfull[1]));
-                    }
-                }
-                __syncwarp();
-            }
-            if (leader) {
-                ptx::mma_commit(ptx::smem_u32(&ctl->empty[vs]));
-                if (more) ptx::mma_commit(ptx::smem_u32(&ctl->empty[ks]));
-            }
-            __syncwarp();
         }
         if (leader) ptx::mma_commit(ptx::smem_u32(&ctl->drain));
         __syncwarp();
         wait_drain(ptx::smem_u32(&ctl->drain), 0);
     } else {
         const int i = warp >> 2, quad = warp & 3, r = quad * 32 + lane;     // tile, lane quadrant, row
-        const int mine = i == 0 ? q0 + 1 : second ? tiles : 0;
-        const int row = (q0 + i) * ROWS + r;                        // in the sequence
         const uint32_t st = tmem + (static_cast<uint32_t>(quad * 32) << 16) + i * ROWS;
-        const uint32_t ot = tmem + (static_cast<uint32_t>(quad * 32) << 16) + 256 + i * DP;
-        const float scale = p.scale * kLog2e;
-        float ref = 0.0f, sum = 0.0f;                               // in units of S
-        bool ok = mine > 0;
-        for (int j = 0; j < mine; ++j) {
-            ok = wait(ctl->sfull[i], j & 1);
-            if (!ok) break;
-            ptx::tc_fence_after();
-            uint32_t s[2][64];
-            ptx::tmem_ld64(st, s[0]);
-            ptx::tmem_ld64(st + 64, s[1]);
-            if (j + 1 == mine) {                                    // the diagonal
-#pragma unroll
-                for (int c = 0; c < ROWS; ++c)
-                    if (c > r) s[c / 64][c % 64] = 0xFF800000u;
+        const uint32_t ot = st + 256 + i * (DP - ROWS);
+        // registers are few.  Bit 0: phase of S, bit 1: of O, bit 2: whether this pair has begun, the others: pairs so far
+        uint32_t at = 0;
+        bool ok = true;
+        for (; !ONE || at < 8; at = (at & ~4u) + 8) {
+            int left;                                               // steps
+            {
+                const Pair x = pair_of(at >> 3, ok);
+                if (x.q0 < 0) break;
+                left = i == 0 ? x.q0 + 1 : x.second() ? x.tiles() : 0;
             }
-            float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+            if (left == 0) {
+                done_with(at >> 3);
+                continue;
+            }
+            float ref = 0.0f, sum = 0.0f;                           // in units of S
+            for (; left > 0; --left, at = (at | 4) ^ 1) {
+                ok = wait(ctl->of[i].sfull, at & 1);
+                if (!ok) break;
+                ptx::tc_fence_after();
+                uint32_t s[2][64];
+                ptx::tmem_ld64(st, s[0]);
+                ptx::tmem_ld64(st + 64, s[1]);
+                if (left == 1) {                                        // the diagonal
 #pragma unroll
-            for (int c = 0; c < ROWS; c += 2)
-                top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(s[c / 64][c % 64]), __uint_as_float(s[c / 64][c % 64 + 1]));
-            float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-            // nothing but minus infinity: a reference that the first finite score replaces
-            if (high == -INFINITY) high = -1e30f;
-            if (j == 0) {
-                ref = high;
-            } else if (__any_sync(0xffffffffu, (high - ref) * scale > 8.0f)) {
-                // S of this tile is there, so the products in front of it have added to O
-                const float to = fmaxf(high, ref), f = ex2((ref - to) * scale);
-                ref = to;
-                sum *= f;
+                    for (int c = 0; c < ROWS; ++c)
+                        if (c > r) s[c / 64][c % 64] = 0xFF800000u;
+                }
+                float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int c = 0; c < ROWS; c += 2)
+                    top[c / 2 % 4] = max3(top[c / 2 % 4], __uint_as_float(s[c / 64][c % 64]), __uint_as_float(s[c / 64][c % 64 + 1]));
+                float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                // nothing but minus infinity: a reference that the first finite score replaces
+                if (high == -INFINITY) high = -1e30f;
+                if ((at & 4) == 0) {
+                    ref = high;
+                } else if (__any_sync(0xffffffffu, (high - ref) * p.scale2 > 8.0f)) {
+                    // S of this tile is there, so the products in front of it have added to O
+                    const float to = fmaxf(high, ref), f = ex2((ref - to) * p.scale2);
+                    ref = to;
+                    sum *= f;
+#pragma unroll
+                    for (int c = 0; c < DP; c += 32) {
+                        uint32_t o[32];
+                        ptx::tmem_ld32(ot + c, o);
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                        ptx::tmem_st32(ot + c, o);
+                    }
+                }
+                const uint64_t by = both(p.scale2), shift = both(-ref * p.scale2);
+                uint64_t part[2] = {};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        float a, b;
+                        split(fma2(f32x2(__uint_as_float(s[h][2 * c]), __uint_as_float(s[h][2 * c + 1])), by, shift), a, b);
+                        a = ex2(a);
+                        b = ex2(b);
+                        part[c & 1] = add2(part[c & 1], f32x2(a, b));
+                        w[c] = pack2(a, b);
+                    }
+                    ptx::tmem_st32(st + 32 * h, w);
+                    ptx::tmem_st_wait();
+                    ptx::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->of[i].pfull[h]));
+                }
+                float a, b;
+                split(add2(part[0], part[1]), a, b);
+                sum += a + b;
+            }
+            if (ok) ok = wait(ctl->of[i].ofull, at >> 1 & 1);
+            at ^= 2;
+            if (ok) {
+                ptx::tc_fence_after();
+                const Pair pair = ctl->pairs[at >> 3 & 1];
+                const int head = pair.head, row = (pair.q0 + i) * ROWS + r;     // in the sequence
+                const float inv = 1.0f / sum;
+                const long long token = pair.begin + row;
+                if (row < pair.length) p.lse[static_cast<long long>(head) * p.tokens + token] = fmaf(ref, p.scale, logf(sum));
+                const long long pitch = static_cast<long long>(p.heads) * p.dim * 2, first = ((token - lane) * p.heads + head) * p.dim;
+                const int rows = pair.length - (row - lane);
 #pragma unroll
                 for (int c = 0; c < DP; c += 32) {
                     uint32_t o[32];
                     ptx::tmem_ld32(ot + c, o);
+                    uint4 w[4], l[4];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                    ptx::tmem_st32(ot + c, o);
-                }
-            }
-            const uint64_t by = f32x2(scale, scale), shift = f32x2(-ref * scale, -ref * scale);
-            uint64_t part[2] = {};
+                    for (int e = 0; e < 4; ++e) {
+                        uint32_t a[4], b[4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t w[32];
-#pragma unroll
-                for (int c = 0; c < 32; ++c) {
-                    float a, b;
-                    split(fma2(f32x2(__uint_as_float(s[h][2 * c]), __uint_as_float(s[h][2 * c + 1])), by, shift), a, b);
-                    a = ex2(a);
-                    b = ex2(b);
-                    part[c & 1] = add2(part[c & 1], f32x2(a, b));
-                    w[c] = pack2(a, b);
-                }
-                ptx::tmem_st32(st + 32 * h, w);
-                ptx::tmem_st_wait();
-                ptx::tc_fence_before();
-                __syncwarp();
-                if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&ctl->pfull[i][h]));
-            }
-            float a, b;
-            split(add2(part[0], part[1]), a, b);
-            sum += a + b;
-        }
-        if (ok) ok = wait(ctl->ofull[i], 0);
-        if (ok) {
-            ptx::tc_fence_after();
-            const float inv = 1.0f / sum;
-            const long long token = pair.begin + row;
-            if (row < pair.length) p.lse[static_cast<long long>(head) * p.tokens + token] = fmaf(ref, p.scale, logf(sum));
-            // Q's tile is no longer read
-            uint8_t* const stage = smem + i * F::TILE + quad * (F::TILE / 4);
-            const long long pitch = static_cast<long long>(p.heads) * p.dim * 2, first = ((token - lane) * p.heads + head) * p.dim;
-            const int rows = pair.length - (row - lane);
-#pragma unroll
-            for (int c = 0; c < DP; c += 32) {
-                uint32_t o[32];
-                ptx::tmem_ld32(ot + c, o);
-                uint4 w[4], l[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    uint32_t a[4], b[4];
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        const float y = __uint_as_float(o[8 * e + 2 * x]) * inv, z = __uint_as_float(o[8 * e + 2 * x + 1]) * inv;
-                        a[x] = pack2(y, z);
-                        b[x] = pack2(y - __uint_as_float(a[x] << 16), z - __uint_as_float(a[x] & 0xFFFF0000u));
+                        for (int x = 0; x < 4; ++x) {
+                            const float y = __uint_as_float(o[8 * e + 2 * x]) * inv, z = __uint_as_float(o[8 * e + 2 * x + 1]) * inv;
+                            a[x] = pack2(y, z);
+                            b[x] = pack2(y - __uint_as_float(a[x] << 16), z - __uint_as_float(a[x] & 0xFFFF0000u));
+                        }
+                        w[e] = make_uint4(a[0], a[1], a[2], a[3]);
+                        l[e] = make_uint4(b[0], b[1], b[2], b[3]);
                     }
-                    w[e] = make_uint4(a[0], a[1], a[2], a[3]);
-                    l[e] = make_uint4(b[0], b[1], b[2], b[3]);
+                    const int bytes = (p.dim - c) * 2;
+                    store_rows(stages + warp * (F::STAGE / 8), w, reinterpret_cast<uint8_t*>(p.out + first + c), pitch, rows, bytes, lane);
+                    if (p.rest != nullptr) store_rows(stages + warp * (F::STAGE / 8), l, reinterpret_cast<uint8_t*>(p.rest + first + c), pitch, rows, bytes, lane);
                 }
-                const int bytes = (p.dim - c) * 2;
-                store_rows(stage, w, reinterpret_cast<uint8_t*>(p.out + first + c), pitch, rows, bytes, lane);
-                if (p.rest != nullptr) store_rows(stage, l, reinterpret_cast<uint8_t*>(p.rest + first + c), pitch, rows, bytes, lane);
             }
+            done_with(at >> 3);
+            if (!ok) break;
         }
     }
     ptx::tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && *abort_flag) {      // a wait that ran out: no copy stays in flight
-        wait_drain(ptx::smem_u32(&ctl->qfull[0]), 0);
-        if (second) wait_drain(ptx::smem_u32(&ctl->qfull[1]), 0);
-        for (int n = max(0, ctl->filled - F::SLOTS); n < ctl->filled; ++n)
-            wait_drain(ptx::smem_u32(&ctl->full[n % F::SLOTS]), (n / F::SLOTS) & 1);
+        for (int i = 0; i < 2; ++i)
+            if (ctl->filled_q[i] > 0) wait_drain(ptx::smem_u32(&ctl->qfull[i]), (ctl->filled_q[i] - 1) & 1);
+        for (int n = 0; n < F::SLOTS; ++n) wait_drain(ptx::smem_u32(&ctl->full[n]), ctl->filled >> n & 1);
     }
     if (warp == 9) {
         ptx::tc_fence_after();
@@ -652,9 +788,9 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
     clean_b();
     ptx::tc_fence_after();
     if (leader) {
-        mma_rows<DP>(tmem + COL_S, fixed, ra + st.sa * F::TILE);
+        mma_rows<DP>(tmem + COL_S, by_rows(fixed), by_rows(ra + st.sa * F::TILE));
         ptx::mma_commit(sfull);
-        mma_rows<DP>(tmem + COL_DP, fixed + F::TILE, rb + st.sb * F::TILE);
+        mma_rows<DP>(tmem + COL_DP, by_rows(fixed + F::TILE), by_rows(rb + st.sb * F::TILE));
         ptx::mma_commit(dpfull);
         if (!KEYS) ptx::mma_commit(bempty + 8 * st.sb);
     }
@@ -676,10 +812,10 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
             if (more) clean_a();
             ptx::tc_fence_after();
             if (leader) {
-                mma_sum<DP, 32, 32>(tmem + COL_SUM_B, tmem + COL_S, b, sums, j > 0);
+                mma_sum<DP, 32, 32>(tmem + COL_SUM_B, tmem + COL_S, to_sum(b), sums, j > 0);
                 ptx::mma_commit(bempty + 8 * ob);
                 if (more) {                                         // over the P that the product in front of it has read by then
-                    mma_rows<DP>(tmem + COL_S, fixed, a1);
+                    mma_rows<DP>(tmem + COL_S, by_rows(fixed), by_rows(a1));
                     ptx::mma_commit(sfull);
                 }
             }
@@ -692,9 +828,9 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
                 clean_a();
                 ptx::tc_fence_after();
                 if (leader) {
-                    mma_rows<DP>(tmem + COL_S, fixed, a1);
+                    mma_rows<DP>(tmem + COL_S, by_rows(fixed), by_rows(a1));
                     ptx::mma_commit(sfull);
-                    mma_rows<DP>(tmem + dp_column<KEYS>(j + 1), fixed + F::TILE, b1);
+                    mma_rows<DP>(tmem + dp_column<KEYS>(j + 1), by_rows(fixed + F::TILE), by_rows(b1));
                     ptx::mma_commit(dpfull);
                     ptx::mma_commit(bempty + 8 * st.sb);
                 }
@@ -704,10 +840,10 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
         }
         ptx::tc_fence_after();
         if (leader) {
-            mma_sum<DP, 32, 32>(tmem + COL_SUM_A, tmem + dp_column<KEYS>(j), a, sums, j > 0);
+            mma_sum<DP, 32, 32>(tmem + COL_SUM_A, tmem + dp_column<KEYS>(j), to_sum(a), sums, j > 0);
             ptx::mma_commit(aempty + 8 * oa);
             if (KEYS && more) {
-                mma_rows<DP>(tmem + COL_DP, fixed + F::TILE, b1);
+                mma_rows<DP>(tmem + COL_DP, by_rows(fixed + F::TILE), by_rows(b1));
                 ptx::mma_commit(dpfull);
             }
             if (!more) ptx::mma_commit(ptx::smem_u32(&ctl->done));
@@ -1132,10 +1268,16 @@ template <int ID, class... P> cudaError_t allow_shared(void (*fn)(P...), int byt
     return e;
 }
 
-template <int DP> cudaError_t forward_as(const ForwardParams& p, int ctas, cudaStream_t s) {
-    const cudaError_t e = allow_shared<DP>(k_attention<DP>, Forward<DP>::SMEM);
+// A pair a CTA where all of them run at once, or where a pair's steps are many: the loop around them
+// costs each some 150 clocks, and what it hides is a pair's first copies and last stores (16384
+// tokens, 28 heads of 128: 1182 us, with the loop 1244; 32 x 512, 16 heads of 128: 77 and 67; the same at 16 steps a
+// pair, of heads of 64 at 32).
+template <int DP> cudaError_t forward_as(const ForwardParams& p, int ctas, long long steps, cudaStream_t s) {
+    const bool one = ctas <= 152 || steps * DP > 2048LL * ctas;
+    const auto fn = one ? k_attention<DP, true> : k_attention<DP, false>;
+    const cudaError_t e = one ? allow_shared<DP>(fn, Forward<DP>::SMEM) : allow_shared<DP + 1>(fn, Forward<DP>::SMEM);
     if (e != cudaSuccess) return e;
-    return launch(k_attention<DP>, dim3(ctas), dim3(Forward<DP>::THREADS), Forward<DP>::SMEM, s, 1, p);
+    return launch(fn, dim3(ctas), dim3(Forward<DP>::THREADS), Forward<DP>::SMEM, s, 1, p);
 }
 
 template <int DP> cudaError_t backward_as(const BackwardParams& p, cudaStream_t s) {
@@ -1164,10 +1306,13 @@ cudaError_t launch_attention(const Attention& a, cudaStream_t s, int64_t* launch
     p.group = a.heads / a.kv_heads;
     p.dim = a.dim;
     p.scale = a.scale;
+    p.scale2 = a.scale * kLog2e;
     p.status = a.status;
     p.wait_limit = a.wait_limit;
     ++*launches;
-    return a.dim <= 64 ? forward_as<64>(p, a.n_pairs * a.heads, s) : forward_as<128>(p, a.n_pairs * a.heads, s);
+    const int ctas = a.n_pairs * a.heads;
+    const long long steps = a.work / 2 * a.heads;                  // two tiles of queries share a step
+    return a.dim <= 64 ? forward_as<64>(p, ctas, steps, s) : forward_as<128>(p, ctas, steps, s);
 }
 
 cudaError_t launch_attention_backward(const AttentionGrad& a, cudaStream_t s, int64_t* launches) {

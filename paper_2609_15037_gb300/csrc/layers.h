@@ -93,6 +93,7 @@ struct Attention {
     float scale;
     const AttentionTile* pairs;    // of 256 rows
     int n_pairs;
+    long long work;        // pairs of a tile of queries and one of keys that it sees, of a head
     int* status;
     long long wait_limit;
 };

@@ -242,7 +242,7 @@ int moara_attention(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int
     if (rc != MOARA_OK) return rc;
     DeviceGuard g(ctx->device);
     const moara::Attention a{q, k, v, out, rest, lse, q_row, q_head, k_row, k_head, v_row, v_head, tokens, heads, kv_heads, dim,
-                             scale, static_cast<const AttentionTile*>(seqs->tiles), seqs->n_pairs, ctx->d_status,
+                             scale, static_cast<const AttentionTile*>(seqs->tiles), seqs->n_pairs, seqs->work, ctx->d_status,
                              moara::tc_wait_limit(ctx->tc)};
     const cudaError_t e = moara::launch_attention(a, static_cast<cudaStream_t>(stream), &ctx->launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "attention launch");
