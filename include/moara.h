@@ -326,8 +326,8 @@ int64_t moara_launch_count(const moara_ctx* ctx);
  * word, waits (with the default bound) for its own copies and tensor-core
  * work in flight, frees its tensor memory and returns, leaving the context
  * usable.  This call sets the bound, in SM clock cycles, of the waits of the
- * tensor-core products of the projector refresh and of moara_alignment and of the MXFP4
- * products, for launches enqueued afterwards; cycles <= 0 restores
+ * tensor-core products of the projector refresh and of moara_alignment, of the MXFP4
+ * products, of the attention and of the policy loss, for launches enqueued afterwards; cycles <= 0 restores
  * the default (2^32 cycles, about 2 s).  A bound shorter than the kernels'
  * own latency (a few hundred cycles) makes them give up on purpose, which is
  * how the failure path is tested; their outputs are then undefined until the
@@ -610,8 +610,8 @@ int moara_sequences_init(int count, const int* lengths, void* tiles, size_t byte
  * pitches positive multiples of 8; dim a multiple of 8 up to 128; scale > 0; kv_heads divides
  * heads; tokens >= seqs->tokens.  out: tokens x heads x dim bf16, lse: heads x tokens
  * floats.  rest: NULL, or like out: what the rounding of out dropped, for the gradients.  Rows
- * behind the last sequence are neither read nor written.  Entries of a sequence that are not finite
- * make rows of that sequence NaN, of no other.  P is rounded to bf16 for its product. */
+ * behind the last sequence are not written, whatever they hold.  Entries of a sequence that are not
+ * finite may make rows of that sequence NaN, of no other.  P is rounded to bf16 for its product. */
 int moara_attention(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int heads, int kv_heads, int dim, float scale,
                     const void* q, int64_t q_row, int64_t q_head, const void* k, int64_t k_row, int64_t k_head,
                     const void* v, int64_t v_row, int64_t v_head, void* out, void* rest, float* lse, void* stream);

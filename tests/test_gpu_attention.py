@@ -88,6 +88,51 @@ def test_long(layer, d):
     check(layer, [2500, 1], 2, 1, d)
 
 
+MANY = [300, 1, 129, 256, 700, 128, 257, 64] * 4
+
+
+@pytest.mark.parametrize("h,hk,d", [(16, 4, 64), (8, 8, 128), (14, 2, 128), (40, 1, 40)])
+def test_more_pairs_of_tiles_than_run_at_once(layer, h, hk, d):
+    check(layer, MANY, h, hk, d)
+
+
+def test_long_and_more_than_run_at_once(layer):
+    check(layer, [4200], 9, 3, 128)
+
+
+def test_many_pairs_on_two_streams_and_replayed(layer):
+    """Kernels that take over the tiles of CTAs that have not begun, beside one another."""
+    xs = [inputs(sum(MANY), 16, 4, d, seed=7) for d in (64, 128)]
+    seqs = layer.sequences(MANY)
+
+    def both(x):
+        q, k, v, do = x
+        out, lse, rest = layer.attention(q, k, v, seqs, train=True)
+        return (out, lse, rest) + layer.attention_backward(do, q, k, v, out, lse, seqs, rest=rest)
+    want = [both(x) for x in xs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in xs]
+    graphs, made = [], []
+    for x, s in zip(xs, streams):
+        with torch.cuda.stream(s):
+            both(x)
+        s.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            made.append(both(x))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        got = []
+        for x, s, g in zip(xs, streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+                got.append(both(x))
+        torch.cuda.synchronize()
+        for a in (got, made):
+            for x, y in zip(a, want):
+                assert all(torch.equal(m, n) for m, n in zip(x, y))
+
+
 def test_scale(layer):
     """Large scores: rows that see one key with all their weight, references that rise again and
     again."""

@@ -206,7 +206,8 @@ def interrupted(M, call, surely=True):
     assert set(seen) <= {0, M.MOARA_ERR_DEVICE_TIMEOUT} and (not surely or M.MOARA_ERR_DEVICE_TIMEOUT in seen), seen
 
 
-@pytest.mark.parametrize("lengths,h,hk,d", [([2000, 300], 8, 2, 128), ([1500], 4, 4, 64), ([4096], 1, 1, 128)])
+@pytest.mark.parametrize("lengths,h,hk,d", [([2000, 300], 8, 2, 128), ([1500], 4, 4, 64), ([4096], 1, 1, 128), ([300] * 20, 16, 4, 64),
+                                              ([700, 1] * 10, 16, 4, 128)])
 def test_attention_gives_up_and_recovers(M, lengths, h, hk, d):
     t = sum(lengths)
     gen = torch.Generator(device="cuda").manual_seed(t)
