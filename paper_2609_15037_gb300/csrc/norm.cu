@@ -123,6 +123,8 @@ struct Sum {
         add(o.hi);
         lo += o.lo;
     }
+    // beside an infinite sum there is NaN
+    __device__ __forceinline__ float value() const { return fabsf(hi) < INFINITY ? hi + lo : hi; }
 };
 
 // Two of them beside one another.
@@ -466,7 +468,7 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
         const Sum dot = group_sum(dots.both(), group, parts[turn] + mine * (group >> 5));
         if (SHIFT) __syncwarp();                 // a group of one warp has no other barrier
         if (!real) continue;
-        const float mean = (dot.hi + dot.lo) * inv;
+        const float mean = dot.value() * inv;
         if constexpr (E > 0) {
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -719,7 +721,7 @@ __global__ void __launch_bounds__(512) k_norm_backward_many(const BackwardParams
         const Sum dot = group_sum(dots.both(), group, parts[turn] + mine * (group >> 5));
         if (SHIFT) __syncwarp();                 // a group of one warp has no other barrier
         if (!real) continue;
-        const uint64_t mean = both(-(dot.hi + dot.lo) * inv);
+        const uint64_t mean = both(-dot.value() * inv);
         accesses<V, A>(i, group, off, n, [&](int j, int c, auto whole) {
             constexpr bool WHOLE = decltype(whole)::value;
             RY a;
@@ -813,7 +815,7 @@ __global__ void __launch_bounds__(512) k_norm_gain(const float* partials, int co
         u.lo = __shfl_down_sync(0xffffffffu, t.lo, o);
         t.add(u);
     }
-    if (lane % 16 == 0 && blockIdx.x * 32 + k < n) dgain[blockIdx.x * 32 + k] = t.hi + t.lo;
+    if (lane % 16 == 0 && blockIdx.x * 32 + k < n) dgain[blockIdx.x * 32 + k] = t.value();
 }
 
 // Whether the rows of all arrays lie alike in their 16-byte lines: `phase` entries into one

@@ -161,6 +161,23 @@ def test_rows_that_are_not_finite_stay_alone(layer):
     assert (y[6] == 0).all() and abs(s[6].item() - 1e3) < 1e-3
 
 
+@pytest.mark.parametrize("t,n", [(6, 300), (4000, 1024), (4000, 1003)])
+def test_infinite_gradients_stay_in_their_row_and_column(layer, t, n):
+    g = gen(12)
+    h, dy = torch.randn(t, n, generator=g, device="cuda"), torch.randn(t, n, generator=g, device="cuda")
+    gain = 1 + 0.1 * torch.randn(n, generator=g, device="cuda")
+    s = R.norm(h, None, gain, EPS)[2].float()
+    h[3, 5] = h[3, 5].abs() + 0.1
+    want = layer.norm_backward(dy, h, gain, s)
+    dy[3, 5] = float("inf")
+    dx, dg = layer.norm_backward(dy, h, gain, s)
+    keep, others = torch.arange(t, device="cuda") != 3, torch.arange(n, device="cuda") != 5
+    assert torch.equal(dx[keep], want[0][keep]) and torch.equal(dg[others], want[1][others])
+    assert dg[5] == float("inf")
+    # the row's mean is infinite: what it is taken from is infinite of the other sign
+    assert (dx[3, others] == -torch.sign(h[3, others]) * float("inf")).all() and dx[3, 5].isnan()
+
+
 def test_gradient_by_differences(layer):
     """Central differences of sum(c y) + sum(e h) in the fp32 operator: second-order terms 1e-4,
     roundings 2^-24 |y| sqrt(n) / step."""
