@@ -80,7 +80,16 @@ def test_many_rows(layer, dtype, t, n):
     check(layer, t, n, DT[dtype], DT["f32" if dtype == "bf16" else "bf16"], True)
 
 
-@pytest.mark.parametrize("n", [1000, 1003])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("t,n", [(5, 8191), (3, 16001), (310, 17003), (160, 18943), (200, 27999), (3, 30001), (2, 48001), (1, 49151)])
+def test_wide_rows_on_odd_places(layer, dtype, t, n):
+    for res in (False, True):
+        check(layer, t, n, DT[dtype], DT[dtype], res)
+    check(layer, t, n, DT[dtype], DT[dtype], True, 2, 1)
+    check(layer, t, n, DT[dtype], DT["f32" if dtype == "bf16" else "bf16"], True)
+
+
+@pytest.mark.parametrize("n", [1000, 1003, 17003])
 def test_many_rows_in_place(layer, n):
     g = gen(8)
     x, r, dy, dh = (matrix(g, 3000, n, torch.bfloat16) for _ in range(4))
