@@ -674,8 +674,11 @@ struct BackwardParams {
     long long wait_limit;
 };
 
+// dpfull and dsfull are those of even and of odd steps.  In tiles of queries dP of the next step is issued
+// before this step's is waited for, and dS of the next may be there before this step's is: of a single barrier
+// two phases could pass a waiting warp by, whose parity is the old one again.
 struct BackwardCtl {
-    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull, dpfull, dsfull, stats[2], done, read, drain, listed[2], taken[2];
+    uint64_t fixed, afull[3], aempty[3], bfull[2], bempty[2], sfull, pfull, dpfull[2], dsfull[2], stats[2], done, read, drain, listed[2], taken[2];
     uint32_t tmem;
     int abort;
     int filled[3];
@@ -773,8 +776,8 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
     const uint32_t fixed = ptx::smem_u32(x.smem), ra = ptx::smem_u32(x.ring_a), rb = ptx::smem_u32(x.ring_b);
     const uint32_t afull = ptx::smem_u32(&ctl->afull[0]), bfull = ptx::smem_u32(&ctl->bfull[0]);
     const uint32_t aempty = ptx::smem_u32(&ctl->aempty[0]), bempty = ptx::smem_u32(&ctl->bempty[0]);
-    const uint32_t pfull = ptx::smem_u32(&ctl->pfull), dsfull = ptx::smem_u32(&ctl->dsfull);
-    const uint32_t sfull = ptx::smem_u32(&ctl->sfull), dpfull = ptx::smem_u32(&ctl->dpfull);
+    const uint32_t pfull = ptx::smem_u32(&ctl->pfull), sfull = ptx::smem_u32(&ctl->sfull);
+    const uint32_t dsfull = ptx::smem_u32(&ctl->dsfull[0]), dpfull = ptx::smem_u32(&ctl->dpfull[0]);
     const uint32_t tmem = st.tmem;
     const int steps = work.count;
     // rows of the tile that a sum runs over
@@ -794,7 +797,7 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
         mma_rows<DP>(tmem + COL_S, by_rows(fixed), by_rows(ra + st.sa * F::TILE));
         ptx::mma_commit(sfull);
         mma_rows<DP>(tmem + COL_DP, by_rows(fixed + F::TILE), by_rows(rb + st.sb * F::TILE));
-        ptx::mma_commit(dpfull);
+        ptx::mma_commit(dpfull + 8 * (st.step & 1));
         if (!KEYS) ptx::mma_commit(bempty + 8 * st.sb);
     }
     __syncwarp();
@@ -802,7 +805,8 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
     if (st.tile > 0 && !waits.one(ptx::smem_u32(&ctl->read), (st.tile - 1) & 1)) return false;
     for (int j = 0; j < steps; ++j, ++st.step) {
         const bool more = j + 1 < steps;
-        const uint32_t parity = st.step & 1;
+        const uint32_t parity = st.step & 1, ds_parity = st.step >> 1 & 1;
+        const uint32_t ds = dsfull + 8 * parity, dp_next = dpfull + 8 * (parity ^ 1);
         const int oa = st.sa, ob = st.sb, sums = (rows + 15) / 16;
         const uint32_t a = ra + oa * F::TILE, b = rb + ob * F::TILE;
         work.next();
@@ -823,7 +827,7 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
                 }
             }
             __syncwarp();
-            if (!(more ? waits.two(dsfull, parity, bfull + 8 * st.sb, st.pb) : waits.one(dsfull, parity))) return false;
+            if (!(more ? waits.two(ds, ds_parity, bfull + 8 * st.sb, st.pb) : waits.one(ds, ds_parity))) return false;
             if (more) clean_b();
         } else {
             if (more) {
@@ -834,12 +838,12 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
                     mma_rows<DP>(tmem + COL_S, by_rows(fixed), by_rows(a1));
                     ptx::mma_commit(sfull);
                     mma_rows<DP>(tmem + dp_column<KEYS>(j + 1), by_rows(fixed + F::TILE), by_rows(b1));
-                    ptx::mma_commit(dpfull);
+                    ptx::mma_commit(dp_next);
                     ptx::mma_commit(bempty + 8 * st.sb);
                 }
                 __syncwarp();
             }
-            if (!(more ? waits.one(dsfull, parity) : waits.two(pfull, parity, dsfull, parity))) return false;
+            if (!(more ? waits.one(ds, ds_parity) : waits.two(pfull, parity, ds, ds_parity))) return false;
         }
         ptx::tc_fence_after();
         if (leader) {
@@ -847,7 +851,7 @@ __device__ __forceinline__ bool multiply(const Shared<DP>& x, const Waits& waits
             ptx::mma_commit(aempty + 8 * oa);
             if (KEYS && more) {
                 mma_rows<DP>(tmem + COL_DP, by_rows(fixed + F::TILE), by_rows(b1));
-                ptx::mma_commit(dpfull);
+                ptx::mma_commit(dp_next);
             }
             if (!more) ptx::mma_commit(ptx::smem_u32(&ctl->done));
         }
@@ -950,7 +954,7 @@ __device__ __forceinline__ bool turn(const BackwardParams& p, const Shared<DP>& 
             }
         }
         if (KEYS) put(COL_S, v, ctl->pfull);
-        if (!wait(ctl->dpfull, parity)) return false;
+        if (!wait(ctl->dpfull[parity], st.step >> 1 & 1)) return false;
         ptx::tc_fence_after();
         ptx::tmem_ld32(lanes + dp_column<KEYS>(j) + c0, s);
 #pragma unroll
@@ -961,7 +965,7 @@ __device__ __forceinline__ bool turn(const BackwardParams& p, const Shared<DP>& 
                 split(mul2(f32x2(v[e], v[e + 1]), add2(f32x2(__uint_as_float(s[e]), __uint_as_float(s[e + 1])), e == c ? d.x : d.y)),
                       v[e], v[e + 1]);
         }
-        put(dp_column<KEYS>(j), v, ctl->dsfull);                    // what does not count may be infinite or NaN
+        put(dp_column<KEYS>(j), v, ctl->dsfull[parity]);            // what does not count may be infinite or NaN
     }
     if (!wait(ctl->done, st.tile & 1)) return false;
     ++st.tile;
@@ -1032,8 +1036,9 @@ template <int DP> __global__ void __launch_bounds__(Backward<DP>::THREADS, 1) k_
     };
     if (threadIdx.x == WARPS * 32) {
         // the thread that copies starts what the first step needs beside the others' set-up
-        for (uint64_t* b : {&ctl->fixed, &ctl->sfull, &ctl->dpfull, &ctl->done, &ctl->drain}) ptx::mbar_init(ptx::smem_u32(b), 1);
-        for (uint64_t* b : {&ctl->pfull, &ctl->dsfull, &ctl->stats[0], &ctl->stats[1], &ctl->read})
+        for (uint64_t* b : {&ctl->fixed, &ctl->sfull, &ctl->dpfull[0], &ctl->dpfull[1], &ctl->done, &ctl->drain})
+            ptx::mbar_init(ptx::smem_u32(b), 1);
+        for (uint64_t* b : {&ctl->pfull, &ctl->dsfull[0], &ctl->dsfull[1], &ctl->stats[0], &ctl->stats[1], &ctl->read})
             ptx::mbar_init(ptx::smem_u32(b), WARPS);
         for (int i = 0; i < 2; ++i) {
             ptx::mbar_init(ptx::smem_u32(&ctl->listed[i]), 1);
