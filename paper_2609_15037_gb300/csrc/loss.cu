@@ -149,13 +149,14 @@ template <> struct Line<__nv_bfloat16> {
 
 constexpr int kLossThreads = 384;
 constexpr int kChunks = 4;             // of a part, copied apart
+constexpr int kElsewhere = -1, kUncounted = -2;
 
 struct LossCtl {
     uint64_t full[kChunks];
     int abort;
     float top, sum, at;            // of this CTA's part: reference, sum, the target's logit if it is here
     float factor, gain;            // of the gradient
-    int hit;
+    int hit;                       // the target's entry of this part, kElsewhere, or kUncounted: the token counts for nothing
     float2 part[2][16];            // of the warps: reference, sum
 };
 
@@ -359,9 +360,9 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
             }
             if (rank == 0) p.logp[row] = counts ? lp.value() : 0.0f;
             ctl.gain = gain;
-            // relative to this part's reference; infinite where nothing of it is to be multiplied
-            ctl.factor = taken ? -gain * ((ctl.top == -INFINITY ? 1.0f : L::apart(mine - base0)) / total) : INFINITY;
-            ctl.hit = counts && owner == rank ? column - first : -1;
+            // relative to this part's reference
+            ctl.factor = -gain * ((ctl.top == -INFINITY ? 1.0f : L::apart(mine - base0)) / total);
+            ctl.hit = !taken ? kUncounted : owner == rank ? column - first : kElsewhere;
         }
         if (p.split > 1) {
             __syncwarp();
@@ -371,7 +372,7 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
         }
         const float factor = ctl.factor, gain = ctl.gain;
         const int hit = ctl.hit;
-        const bool zero = factor == INFINITY, wanted = p.dz != nullptr && ok;
+        const bool zero = hit == kUncounted, wanted = p.dz != nullptr && ok;
         T* const dz = static_cast<T*>(p.dz) + row * p.lddz + first;
         // whether the gradient's entries lie in lines as the logits' do
         const bool same = (reinterpret_cast<uintptr_t>(dz + x.front) & 15) == 0;

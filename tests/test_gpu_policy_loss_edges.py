@@ -1,0 +1,73 @@
+"""The policy loss where its gradient leaves fp32's range."""
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import layers_ref as R  # noqa: E402
+
+CLIP = 0.2, 0.28
+TYPES = [torch.float32, torch.bfloat16]
+SIZES = [(300, 1000), (5, 1003), (2, 32003), (2, 900001)]       # a CTA a row, and clusters; the last from L2
+
+
+@pytest.fixture(scope="module")
+def M():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2609_15037_gb300 as pkg
+    return pkg
+
+
+@pytest.fixture(scope="module")
+def layer(M):
+    g = M.LayerGroup()
+    yield g
+    assert g.status() == 0
+    g.close()
+
+
+def inputs(t, v, dtype):
+    """Of unit weight; ratios are 1, away from the clip's borders."""
+    g = torch.Generator(device="cuda").manual_seed(t + v)
+    z = (2 * torch.randn(t, v, generator=g, device="cuda")).to(dtype)
+    target = torch.randint(0, v, (t,), generator=g, device="cuda")
+    lp = torch.log_softmax(z.double(), 1).gather(1, target[:, None])[:, 0]
+    return dict(logits=z, targets=target, old=lp.float(), adv=torch.randn(t, generator=g, device="cuda"),
+                weights=torch.ones(t, device="cuda"), ref=lp.float() + 0.1)
+
+
+def unlikely(x, row, far):
+    """The target's logit so that its log-probability is some -far."""
+    z, t = x["logits"], x["targets"][row]
+    z[row, t] = float("-inf")
+    z[row, t] = torch.logsumexp(z[row].double(), 0) - far
+
+
+def logp(x, row):
+    return torch.log_softmax(x["logits"][row].double(), 0)[x["targets"][row]]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("t,v", SIZES)
+@pytest.mark.parametrize("how", ["kl", "hidden target", "advantage", "-advantage", "weight"])
+def test_an_infinite_gradient_is_no_zero(layer, dtype, t, v, how):
+    """In its own row alone."""
+    x = inputs(t, v, dtype)
+    first = layer.policy_loss(**x, clip=CLIP, kl=0.05)
+    if how == "kl":
+        unlikely(x, 1, 150)
+        x["ref"][1], x["old"][1] = 0.0, logp(x, 1)
+    elif how == "hidden target":
+        x["logits"][1, x["targets"][1]] = float("-inf")
+    elif how == "weight":
+        unlikely(x, 1, 60)
+        x["ref"][1], x["old"][1], x["weights"][1] = 0.0, logp(x, 1), 1e30
+    else:
+        x["adv"][1] = float("inf" if how == "advantage" else "-inf")
+    sums, lp, dz = layer.policy_loss(**x, clip=CLIP, kl=0.05)
+    assert not sums[0].isfinite() and not dz[1, x["targets"][1]].isfinite() and not dz[1].isfinite().all()
+    keep = [i for i in range(t) if i != 1]
+    assert torch.equal(dz[keep], first[2][keep]) and torch.equal(lp[keep], first[1][keep])
