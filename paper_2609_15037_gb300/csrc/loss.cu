@@ -343,7 +343,10 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
             float gain = 0.0f;
             const bool taken = counts && w != 0.0f;
             if (taken) {
-                const float rho = expf(lp.minus(old));
+                const float t = lp.minus(old);
+                float rho = expf(t);
+                // an advantage of zero has no part, whatever the ratio
+                if (a == 0.0f && rho == INFINITY) rho = 1.0f;
                 // NaN advantages and ratios stay NaN
                 const float bound = rho < p.low ? p.low : rho > p.high ? p.high : rho;
                 const bool clipped = bound * a < rho * a;

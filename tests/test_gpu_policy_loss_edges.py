@@ -1,4 +1,4 @@
-"""The policy loss where its gradient leaves fp32's range."""
+"""The policy loss where its exponentials or its gradient leave fp32's range."""
 
 import pytest
 
@@ -71,3 +71,20 @@ def test_an_infinite_gradient_is_no_zero(layer, dtype, t, v, how):
     assert not sums[0].isfinite() and not dz[1, x["targets"][1]].isfinite() and not dz[1].isfinite().all()
     keep = [i for i in range(t) if i != 1]
     assert torch.equal(dz[keep], first[2][keep]) and torch.equal(lp[keep], first[1][keep])
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("t,v", SIZES)
+def test_an_advantage_of_zero_has_no_part(layer, dtype, t, v):
+    """However far the policy has moved: a group of equal rewards."""
+    x = inputs(t, v, dtype)
+    x["adv"][1] = 0.0
+    for old in (-95.0, -3e3, -1e30):
+        x["old"][1] = old
+        sums, lp, dz = layer.policy_loss(**x, clip=CLIP)
+        y = {k: a.clone() for k, a in x.items()}
+        y["old"][1] = logp(x, 1)
+        want = layer.policy_loss(**y, clip=CLIP)
+        assert torch.equal(sums, want[0]) and torch.equal(lp, want[1]) and torch.equal(dz, want[2]) and (dz[1] == 0).all()
+    x["old"][1] = float("nan")
+    assert layer.policy_loss(**x, clip=CLIP)[0][0].isnan()
