@@ -634,7 +634,9 @@ int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int to
  *   dZ   = w (kl (1 - exp x) - [not clipped] rho adv) (1[j = target] - softmax(z)_j)
  * weight: a float per token, or NULL for 1 / rows.  A token of weight zero, or whose target
  * is outside 0 .. vocab - 1, counts for nothing, whatever its other inputs hold; the latter's logp is
- * 0.  An advantage of zero has no part, however large the ratio.  ref_logp: NULL without a KL term (kl = 0).  logp receives lp, dZ (of Z's type, row pitch
+ * 0.  An advantage of zero has no part, however large the ratio.  rho and exp x may pass fp32's range
+ * (their roots may not) where their products with w, adv and kl do not; what does is infinite or NaN in
+ * its own row of dZ and in sums.  ref_logp: NULL without a KL term (kl = 0).  logp receives lp, dZ (of Z's type, row pitch
  * lddz, may be Z with its pitch, or NULL) the gradient.  The sum over a row is held in fp32, those over rows
  * in two fp32 numbers, all in a fixed order.  workspace: moara_policy_loss_workspace_bytes(rows)
  * device bytes, 16-byte aligned, in use by one call at a time. */

@@ -351,15 +351,33 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
                 const float bound = rho < p.low ? p.low : rho > p.high ? p.high : rho;
                 const bool clipped = bound * a < rho * a;
                 float loss = clipped ? -bound * a : -rho * a, d = clipped ? 0.0f : -rho * a;
+                float y = 0.0f, k = 0.0f, grown = 0.0f;
                 if (p.ref_logp != nullptr) {
-                    const float y = -lp.minus(other), k = exp_beyond_linear(y);
+                    y = -lp.minus(other);
+                    k = exp_beyond_linear(y);
+                    grown = expm1f(y);
                     loss = fmaf(p.kl, k, loss);
-                    d = fmaf(-p.kl, expm1f(y), d);
-                    sums[1].add(k * w);
+                    d = fmaf(-p.kl, grown, d);
                 }
-                sums[0].add(loss * w);
-                if (clipped) sums[2].add(w);
+                float term = loss * w, extra = k * w;
                 gain = w * d;
+                if (rho == INFINITY || grown == INFINITY) {
+                    // an exponential beyond fp32's range, whose product need not be: by its root, twice
+                    const float r = expf(0.5f * t), g = expf(0.5f * y);
+                    term = clipped ? -bound * a * w : rho == INFINITY ? -(w * a) * r * r : -rho * a * w;
+                    gain = clipped ? 0.0f : term;
+                    if (grown == INFINITY) {
+                        extra = w * g * g;
+                        term += w * p.kl * g * g;
+                        gain -= w * p.kl * g * g;
+                    } else if (p.ref_logp != nullptr) {
+                        term += p.kl * extra;
+                        gain -= w * p.kl * grown;
+                    }
+                }
+                sums[0].add(term);
+                if (p.ref_logp != nullptr) sums[1].add(extra);
+                if (clipped) sums[2].add(w);
             }
             if (rank == 0) p.logp[row] = counts ? lp.value() : 0.0f;
             ctl.gain = gain;

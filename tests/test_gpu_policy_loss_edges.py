@@ -50,6 +50,19 @@ def logp(x, row):
     return torch.log_softmax(x["logits"][row].double(), 0)[x["targets"][row]]
 
 
+def within(x, kl, got):
+    """R.policy_loss of rows whose largest logit is zero (what 64 bits hold of a sum's logarithm beside logits of 1e38
+    is nothing), and what the rounding of a difference of 177 at most adds to its exponential."""
+    dtype, z = x["logits"].dtype, x["logits"].double()
+    z = z - z.amax(1, keepdim=True)
+    want, tol = R.policy_loss(z, x["targets"], x["old"], x["adv"], x["weights"], x["ref"] if kl else None, 1 - CLIP[0], 1 + CLIP[1], kl)
+    add = 177 * R.F32 + 2.0 ** -20
+    tol = tol[0] + add * want[0].abs(), tol[1], tol[2] + (add + R.half_step(dtype)) * want[2].abs()
+    for a, b, c in zip(got, want, tol):
+        R.within(a, b, c)
+    return want
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("t,v", SIZES)
 @pytest.mark.parametrize("how", ["kl", "hidden target", "advantage", "-advantage", "weight"])
@@ -88,3 +101,21 @@ def test_an_advantage_of_zero_has_no_part(layer, dtype, t, v):
         assert torch.equal(sums, want[0]) and torch.equal(lp, want[1]) and torch.equal(dz, want[2]) and (dz[1] == 0).all()
     x["old"][1] = float("nan")
     assert layer.policy_loss(**x, clip=CLIP)[0][0].isnan()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("t,v", SIZES)
+def test_an_exponential_beyond_the_range_with_a_product_inside(layer, dtype, t, v):
+    """exp(ref - lp) or the ratio alone is infinite in fp32, the gradient is not."""
+    x = inputs(t, v, dtype)
+    unlikely(x, 1, 95)
+    x["weights"][1], x["ref"][1] = 2.0 ** -13, -0.5
+    x["old"][1] = logp(x, 1)
+    want = within(x, 0.05, layer.policy_loss(**x, clip=CLIP, kl=0.05))
+    assert 1e35 < want[2][1].abs().max() < 1e37
+    x = inputs(t, v, dtype)
+    x["old"][0], x["adv"][0], x["weights"][0] = logp(x, 0) - 95, -1.0, 2.0 ** -13
+    want = within(x, 0.05, layer.policy_loss(**x, clip=CLIP, kl=0.05))
+    assert 1e35 < want[2][0].abs().max() < 1e38
+    x["adv"][0] = 1.0                                           # clipped: the ratio itself does not matter
+    within(x, 0.0, layer.policy_loss(**x, clip=CLIP))
