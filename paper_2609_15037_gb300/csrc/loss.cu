@@ -9,6 +9,7 @@
 #include <atomic>
 #include <cstddef>
 
+#include "f32x2.cuh"
 #include "launch.cuh"
 #include "layers.h"
 #include "tc_ptx.cuh"
@@ -82,10 +83,10 @@ struct Sum {
 };
 
 // 16 bytes of a row as fp32, their largest (NaN left out: it returns in the sum), and
-// exponentials relative to a reference: powers of two, whose argument is one fused
-// operation for bf16 logits, an error far below the gradient's rounding; fp32 logits take z - ref
-// exactly as far as fp32 holds it, and what the product with log2 e rounds off as a factor
-// (1 + its natural power).
+// exponentials relative to a reference logit: powers of two of (z - ref) log2 e, which no size of the
+// logits takes out of fp32's range but where the exponential is zero.  bf16 logits leave out what the two
+// operations round off, an error far below the gradient's rounding; fp32 logits take what the product
+// rounds off as a factor (1 + its natural power).
 template <class T> struct Line;
 
 template <> struct Line<float> {
@@ -93,7 +94,6 @@ template <> struct Line<float> {
     static __device__ __forceinline__ float top(const uint4& w) {
         return fmaxf(fmaxf(__uint_as_float(w.x), __uint_as_float(w.y)), fmaxf(__uint_as_float(w.z), __uint_as_float(w.w)));
     }
-    static __device__ __forceinline__ float reference(float top) { return top; }
     static __device__ __forceinline__ float exponential(float z, float ref) {
         const float t = z - ref, x = t * kLog2e, y = ex2(x);
         // of minus infinity the rest is NaN: its exponential is 0 whatever it is
@@ -107,7 +107,6 @@ template <> struct Line<float> {
         e[3] = exponential(__uint_as_float(w.w), ref);
     }
     static __device__ __forceinline__ float apart(float x) { return expf(x); }      // of a difference of references
-    static __device__ __forceinline__ void subtract(Sum& s, float ref) { s.add(-ref); }
     static __device__ __forceinline__ uint4 pack(const float (&v)[4]) {
         return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     }
@@ -125,18 +124,17 @@ template <> struct Line<__nv_bfloat16> {
         const uint32_t t = max2(max2(w.x, w.y), max2(w.z, w.w));
         return fmaxf(__uint_as_float(t << 16), __uint_as_float(t & 0xFFFF0000u));
     }
-    static __device__ __forceinline__ float reference(float top) { return top * kLog2e; }
-    static __device__ __forceinline__ float exponential(float z, float ref) { return ex2(fmaf(z, kLog2e, -ref)); }
+    static __device__ __forceinline__ float exponential(float z, float ref) { return ex2((z - ref) * kLog2e); }
     static __device__ __forceinline__ void exponentials(const uint4& w, float ref, float (&e)[8]) {
         const uint32_t a[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            e[2 * k] = exponential(__uint_as_float(a[k] << 16), ref);
-            e[2 * k + 1] = exponential(__uint_as_float(a[k] & 0xFFFF0000u), ref);
+            split(mul2(add2(widen2(a[k]), both(-ref)), both(kLog2e)), e[2 * k], e[2 * k + 1]);
+            e[2 * k] = ex2(e[2 * k]);
+            e[2 * k + 1] = ex2(e[2 * k + 1]);
         }
     }
-    static __device__ __forceinline__ float apart(float x) { return ex2(x); }
-    static __device__ __forceinline__ void subtract(Sum& s, float ref) { s.subtract_ln2(ref); }
+    static __device__ __forceinline__ float apart(float x) { return ex2(x * kLog2e); }
     static __device__ __forceinline__ uint32_t pack2(float a, float b) {
         const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
         return *reinterpret_cast<const uint32_t*>(&h);
@@ -245,11 +243,10 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
                 const uint4 v = lines[i];
                 const float high = L::top(v);
                 if (high > top + 8.0f) {
-                    const float to = L::reference(high);
                     // of a first finite logit: nothing but zeros (or NaN) has been added
-                    if (top > -INFINITY) sum = sum * L::apart(ref - to);
+                    if (top > -INFINITY) sum = sum * L::apart(top - high);
                     top = high;
-                    ref = to;
+                    ref = high;
                 }
                 float e[N];
                 L::exponentials(v, ref, e);
@@ -263,10 +260,9 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
         if (beside >= 0) {
             const float v = static_cast<float>(x.z[beside]);
             if (v > top + 8.0f) {
-                const float to = L::reference(v);
-                if (top > -INFINITY) sum *= L::apart(ref - to);
+                if (top > -INFINITY) sum *= L::apart(top - v);
                 top = v;
-                ref = to;
+                ref = v;
             }
             sum += L::exponential(v, ref);
         }
@@ -279,7 +275,7 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
             for (int o = most / 2; o > 0; o /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
             top = high;
         };
-        float base = top > -INFINITY ? ref : -INFINITY;
+        float base = top;
         join(base, sum, 32);
         float2* const part = ctl.part[phase];
         if (lane == 0) part[warp] = make_float2(base, sum);
@@ -333,7 +329,7 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
             // log(total) from its exponent and the rest, which lies in [1, 2)
             Sum lp;
             lp.add(at);
-            L::subtract(lp, base0);
+            lp.add(-base0);
             if (total > 0.0f && total < INFINITY) {
                 lp.subtract_ln2(static_cast<float>(static_cast<int>(__float_as_uint(total) >> 23) - 127));
                 lp.add(-logf(__uint_as_float((__float_as_uint(total) & 0x7FFFFFu) | 0x3F800000u)));

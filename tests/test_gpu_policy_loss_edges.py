@@ -1,4 +1,5 @@
-"""The policy loss where its exponentials or its gradient leave fp32's range."""
+"""The policy loss where its exponentials or its gradient leave fp32's range, and where a row's
+logits are the type's lowest or largest."""
 
 import pytest
 
@@ -119,3 +120,38 @@ def test_an_exponential_beyond_the_range_with_a_product_inside(layer, dtype, t, 
     assert 1e35 < want[2][0].abs().max() < 1e38
     x["adv"][0] = 1.0                                           # clipped: the ratio itself does not matter
     within(x, 0.0, layer.policy_loss(**x, clip=CLIP))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("t,v", SIZES + [(3, 7), (1, 1)])
+def test_logits_hidden_by_the_lowest_value(layer, dtype, t, v):
+    """They have no probability beside others, and are equal among themselves."""
+    low = torch.finfo(dtype).min
+    x = inputs(t, v, dtype)
+    hidden = torch.rand(t, v, device="cuda") < 0.5
+    hidden[:, :v // 3] = True                               # whole parts of a row among them
+    hidden.scatter_(1, x["targets"][:, None], False)
+    y = {k: a.clone() for k, a in x.items()}
+    x["logits"].masked_fill_(hidden, low)
+    y["logits"].masked_fill_(hidden, float("-inf"))
+    got, want = layer.policy_loss(**x, clip=CLIP, kl=0.05), layer.policy_loss(**y, clip=CLIP, kl=0.05)
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and got[2].isfinite().all()
+    x["logits"][0] = low                                    # nothing is left of the row
+    x["old"] = torch.stack([logp(x, i) for i in range(t)]).float()
+    x["ref"] = x["old"] + 0.1
+    within(x, 0.05, layer.policy_loss(**x, clip=CLIP, kl=0.05))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_logits_of_any_size(layer, dtype):
+    """Differences count, however large the logits themselves are."""
+    big = torch.finfo(dtype).max
+    for at in (1e3, -1e3, 1e30, -1e30, 2.5e38, -2.5e38, big):
+        x = inputs(6, 2003, dtype)
+        x["logits"][2] = at
+        x["logits"][4] = at
+        x["logits"][4, 77] = x["logits"][4, 77] * (1 - 2.0 ** -7)
+        x["targets"][4] = 77 if at < 0 else 78
+        x["old"] = torch.stack([logp(x, i) for i in range(6)]).float()
+        x["ref"] = x["old"] + 0.1
+        within(x, 0.05, layer.policy_loss(**x, clip=CLIP, kl=0.05))
