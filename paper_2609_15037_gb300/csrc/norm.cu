@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 #include <type_traits>
 
 #include "f32x2.cuh"
@@ -847,12 +848,25 @@ constexpr long long kFull = 152 * 2048;          // threads that the GPU holds
 // Threads of a row of n entries, e of them each.
 int group_of(int n, int e) { return (n + 32 * e - 1) / (32 * e) * 32; }
 
-template <class F> cudaError_t allow_shared(F fn, size_t bytes) {
-    if (bytes <= 40 * 1024) return cudaSuccess;
-    return cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
-}
-
 constexpr size_t kShared = 222 << 10;
+
+// A launch that may take up to kShared bytes of shared memory.  The kernel's limit is set to that once per
+// device: it belongs to the function, and one set to a call's own bytes may be lowered by another thread's
+// call before the launch.
+template <auto FN, class P> cudaError_t launch_wide(int ctas, int threads, size_t smem, cudaStream_t s, const P& p) {
+    if (smem > 40 * 1024) {
+        static std::atomic<uint64_t> done{0};
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
+        if (e != cudaSuccess) return e;
+        if (device >= 64 || !(done.load() >> device & 1)) {
+            e = cudaFuncSetAttribute(FN, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShared));
+            if (e != cudaSuccess) return e;
+            if (device < 64) done.fetch_or(1ull << device);
+        }
+    }
+    return launch(FN, dim3(ctas), dim3(threads), smem, s, 1, p);
+}
 
 template <class T, class TY, int V, bool SHIFT> cudaError_t forward_as(const ForwardParams& q, cudaStream_t s) {
     ForwardParams p = q;
@@ -869,14 +883,10 @@ template <class T, class TY, int V, bool SHIFT> cudaError_t forward_as(const For
             const int stages = room < fixed ? 0 : static_cast<int>(std::min<size_t>(3, (room - fixed) / stage));
             const size_t smem = stages * stage + gain;
             const int ctas = std::min((p.rows - 1) / per + 1, 152 * resident);
-            const auto fn = stages >= 3   ? k_norm_many<T, TY, V, 3, SHIFT>
-                            : stages == 2 ? k_norm_many<T, TY, V, 2, SHIFT>
-                                          : k_norm_many<T, TY, V, 1, SHIFT>;
-            if (stages > 0) {                // not beside the gain of a wide row
-                const cudaError_t err = allow_shared(fn, smem);
-                if (err != cudaSuccess) return err;
-                return launch(fn, dim3(ctas), dim3(threads), smem, s, 1, p);
-            }
+            if (stages >= 3) return launch_wide<k_norm_many<T, TY, V, 3, SHIFT>>(ctas, threads, smem, s, p);
+            if (stages == 2) return launch_wide<k_norm_many<T, TY, V, 2, SHIFT>>(ctas, threads, smem, s, p);
+            if (stages == 1) return launch_wide<k_norm_many<T, TY, V, 1, SHIFT>>(ctas, threads, smem, s, p);
+            // none beside the gain of a wide row
         }
     }
     const bool wide = reach > 8192;
@@ -884,10 +894,8 @@ template <class T, class TY, int V, bool SHIFT> cudaError_t forward_as(const For
     const int per = std::max(1, 256 / p.group);
     int ctas = (p.rows - 1) / per + 1;
     if (SHIFT) ctas = std::min<int>(ctas, 152 * std::max<int>(1, std::min<size_t>(2048 / (p.group * per), kShared / (gain + 1024))));
-    const auto fn = wide ? k_norm<T, TY, V, 0, SHIFT> : k_norm<T, TY, V, 8, SHIFT>;
-    const cudaError_t err = allow_shared(fn, gain);
-    if (err != cudaSuccess) return err;
-    return launch(fn, dim3(ctas), dim3(p.group * per), gain, s, 1, p);
+    return wide ? launch_wide<k_norm<T, TY, V, 0, SHIFT>>(ctas, p.group * per, gain, s, p)
+                : launch_wide<k_norm<T, TY, V, 8, SHIFT>>(ctas, p.group * per, gain, s, p);
 }
 
 template <class T, class TY> cudaError_t forward_of(ForwardParams p, cudaStream_t s) {
@@ -956,15 +964,13 @@ template <class T, class TY, int V, bool SHIFT> cudaError_t backward_as(const Ba
     const BackwardShape b = backward_shape(p.rows, p.cols, V, SHIFT, V * (2 * sizeof(T) + sizeof(TY)));
     p.group = b.group;
     ctas = b.ctas;
-    auto fn = k_norm_backward<T, TY, V, 8, SHIFT>;
-    if (b.entries == 0) fn = k_norm_backward<T, TY, V, 0, SHIFT>;
-    if constexpr (V > 1)
-        if (b.accesses > 0) fn = k_norm_backward_many<T, TY, V, kAccesses, SHIFT>;
+    const int threads = b.group * b.per;
     if constexpr (SHIFT)
-        if (b.accesses == 2) fn = k_norm_backward_many<T, TY, V, 2, SHIFT>;
-    const cudaError_t e = allow_shared(fn, b.smem);
-    if (e != cudaSuccess) return e;
-    return launch(fn, dim3(b.ctas), dim3(b.group * b.per), b.smem, s, 1, p);
+        if (b.accesses == 2) return launch_wide<k_norm_backward_many<T, TY, V, 2, SHIFT>>(ctas, threads, b.smem, s, p);
+    if constexpr (V > 1)
+        if (b.accesses > 0) return launch_wide<k_norm_backward_many<T, TY, V, kAccesses, SHIFT>>(ctas, threads, b.smem, s, p);
+    return b.entries == 0 ? launch_wide<k_norm_backward<T, TY, V, 0, SHIFT>>(ctas, threads, b.smem, s, p)
+                          : launch_wide<k_norm_backward<T, TY, V, 8, SHIFT>>(ctas, threads, b.smem, s, p);
 }
 
 template <class T, class TY> cudaError_t backward_of(BackwardParams p, int& ctas, cudaStream_t s) {

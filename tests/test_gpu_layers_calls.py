@@ -1,0 +1,99 @@
+"""Calls of the layers' operators beside one another: two host threads, graphs beside other shapes."""
+
+import threading
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+import layers_ref as R  # noqa: E402
+
+
+@pytest.fixture(scope="module")
+def M():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2609_15037_gb300 as pkg
+    return pkg
+
+
+@pytest.fixture(scope="module")
+def layer(M):
+    g = M.LayerGroup()
+    yield g
+    assert g.status() == 0
+    g.close()
+
+
+def rand(gen, *shape, dtype=torch.bfloat16):
+    return torch.randn(*shape, generator=gen, device="cuda").to(dtype)
+
+
+# rows of both shapes are taken by the same kernels, with shared memory of different sizes
+SHAPES = [(8, 16384), (1300, 4096)]
+
+
+def test_two_threads_of_different_shapes(M):
+    """Each with a context and a stream of its own, through the C entries."""
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    failed, results, threads = [], [], []
+
+    def run(rows, cols, start):
+        try:
+            layer, stream = M.LayerGroup(), torch.cuda.Stream()
+            x, dy, gain = rand(gen, rows, cols), rand(gen, rows, cols), torch.ones(cols, device="cuda")
+            y, dx, rstd, dgain = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device="cuda"), torch.empty(cols, device="cuda")
+            size = M.moara_rms_norm_backward_workspace_bytes(rows, cols)
+            ws = torch.empty(size, dtype=torch.uint8, device="cuda")
+            bf16, s = M.MOARA_DTYPE_BF16, stream.cuda_stream
+            torch.cuda.synchronize()
+            start.wait()
+            for i in range(6000):
+                M.moara_rms_norm(layer.ctx, rows, cols, x.data_ptr(), cols, 0, 0, bf16, gain.data_ptr(), 1e-6, 0, 0, y.data_ptr(), bf16,
+                                 cols, rstd.data_ptr(), s)
+                M.moara_rms_norm_backward(layer.ctx, rows, cols, dy.data_ptr(), bf16, cols, x.data_ptr(), bf16, cols, gain.data_ptr(),
+                                          rstd.data_ptr(), 0, 0, dx.data_ptr(), cols, dgain.data_ptr(), ws.data_ptr(), size, s)
+                if i % 500 == 499:
+                    stream.synchronize()
+            stream.synchronize()
+            wx, wg, ex, eg = R.norm_backward(dy, x, gain, R.norm(x, None, gain, 1e-6)[2], None)
+            results.append((dx, wx, ex * (1 + R.BF16) + R.BF16 * wx.abs() + 2.0 ** -126))
+            results.append((dgain, wg, eg))
+            assert layer.status() == 0
+            layer.close()
+        except Exception as e:                               # noqa: BLE001
+            failed.append((rows, cols, e))
+    start = threading.Barrier(len(SHAPES))
+    for shape in SHAPES:
+        threads.append(threading.Thread(target=run, args=(*shape, start)))
+        threads[-1].start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    for x in results:
+        R.within(*x)
+
+
+def test_graphs_beside_other_shapes(layer):
+    """A recorded call keeps its shared memory where a smaller one follows."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = [(rand(gen, *s), rand(gen, *s), torch.ones(s[1], device="cuda")) for s in SHAPES]
+
+    def run(a):
+        h, y, s = layer.norm(a[0], a[2])
+        return (y, s) + layer.norm_backward(a[1], h, a[2], s)
+    want = [run(a) for a in x]
+    graphs = []
+    for a in x:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            got = run(a)
+        graphs[-1].got = got
+    for first, second in ((0, 1), (1, 0)):
+        run(x[second])
+        graphs[first].replay()
+        run(x[second])
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(graphs[first].got, want[first]))
