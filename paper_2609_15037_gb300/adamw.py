@@ -56,6 +56,14 @@ def allocating_on(stream, device):
     return torch.cuda.stream(torch.cuda.ExternalStream(int(stream), device=device))
 
 
+def record_on(stream, device, tensors):
+    """torch.Tensor.record_stream of each, with a torch.cuda.Stream or a cudaStream_t handle."""
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    for x in tensors:
+        x.record_stream(stream)
+
+
 class _Ranges:
     """Disjoint ranges of addresses."""
 

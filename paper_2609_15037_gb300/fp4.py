@@ -8,7 +8,7 @@ import torch
 
 from . import _host
 from . import binding as B
-from .adamw import _TYPES, allocating_on, entry_address, stream_handle
+from .adamw import _TYPES, allocating_on, entry_address, record_on, stream_handle
 
 _QUANTIZE, _DEQUANTIZE, _PRODUCT, _LINEAR, _LINEAR_BYTES = (
     entry_address("moara_fp4_" + f) for f in ("quantize", "dequantize", "product", "linear", "linear_workspace_bytes"))
@@ -50,10 +50,7 @@ class Fp4Matrix:
         """As torch.Tensor.record_stream: once this operand is released, its memory is taken
         again only behind what `stream` (a torch.cuda.Stream or a cudaStream_t handle) has been
         given by then."""
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream), device=self.device)
-        for x in (self._q, self._sf) if self._both is None else (self._both,):
-            x.record_stream(stream)
+        record_on(stream, self.device, (self._q, self._sf) if self._both is None else (self._both,))
 
 
 def _operand(buffer, rows, cols, device):

@@ -12,7 +12,7 @@ import torch
 
 from . import _host
 from . import binding as B
-from .adamw import _TYPES, allocating_on, entry_address, stream_handle
+from .adamw import _TYPES, allocating_on, entry_address, record_on, stream_handle
 from .fp4 import _operand
 
 (_NORM, _NORM_QUANTIZE, _NORM_BACKWARD, _NORM_BYTES, _ATTENTION, _ATTENTION_BACKWARD, _LOSS, _LOSS_BYTES) = (
@@ -39,6 +39,12 @@ class Sequences:
         self._desc.tiles = self._tiles.data_ptr()
         self._at = ctypes.addressof(self._desc)
 
+    def record_stream(self, stream):
+        """As torch.Tensor.record_stream: once this list is released, its memory is taken
+        again only behind what `stream` (a torch.cuda.Stream or a cudaStream_t handle) has been
+        given by then."""
+        record_on(stream, self.device, (self._tiles,))
+
 
 class LayerGroup:
     """A context for the operators of a decoder's layers on one device.
@@ -59,7 +65,7 @@ class LayerGroup:
 
     Streams are cudaStream_t handles; None is torch's current stream.  A call orders nothing
     between streams: an input that was made on another one has to be complete, and has to live
-    until the call's work is done (record_stream)."""
+    until the call's work is done (record_stream of the tensor, operand or list)."""
 
     def __init__(self, device=0):
         self.device = device

@@ -1,4 +1,5 @@
-"""Calls of the layers' operators beside one another: two host threads, graphs beside other shapes."""
+"""Calls of the layers' operators beside one another: two host threads, graphs beside other shapes,
+lists of sequences that another stream reads when they are released."""
 
 import threading
 
@@ -97,3 +98,6 @@ def test_graphs_beside_other_shapes(layer):
         run(x[second])
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(graphs[first].got, want[first]))
+
+
+@pytest.mark.parametrize("handle", [False, True])
