@@ -158,9 +158,16 @@ template <class T, int V> __device__ __forceinline__ void add_squares(Sums& sums
 }
 
 // 1 / sqrt(sum / n + eps): a Newton step on the residual of rsqrtf, in two numbers
-// throughout, so that it adds one rounding to the sum's error.
-__device__ __forceinline__ float inverse_rms(const Sum& s, int n, float eps) {
+// throughout, so that it adds one rounding to the sum's error.  A mean that is too small for the step's squares (or
+// for fp32's normal numbers: no eps, and next to nothing in a long row) is taken 2^100 times as large.
+__device__ __forceinline__ float inverse_rms(Sum s, int n, float eps) {
     if (!(s.hi < INFINITY)) return rsqrtf(s.hi);             // lo is NaN beside it
+    const bool small = s.hi < 0x1p-40f && eps < 0x1p-60f;
+    if (small) {
+        s.hi *= 0x1p100f;
+        s.lo *= 0x1p100f;
+        eps *= 0x1p100f;
+    }
     const float f = static_cast<float>(n), total = s.hi + s.lo, rest = (s.hi - total) + s.lo;
     const float q = total / f, ql = (fmaf(-q, f, total) + rest) / f;
     Sum m;
@@ -171,8 +178,8 @@ __device__ __forceinline__ float inverse_rms(const Sum& s, int n, float eps) {
     const float r = rsqrtf(a);
     if (!(r > 0.0f && r < INFINITY)) return r;               // of infinity, zero or NaN
     const float p = r * r, pl = fmaf(r, r, -p);
-    const float e = fmaf(-a, p, 1.0f) - (a * pl + al * p);
-    return fmaf(0.5f * r, e, r);
+    const float e = fmaf(-a, p, 1.0f) - (a * pl + al * p), root = fmaf(0.5f * r, e, r);
+    return small ? root * 0x1p50f : root;
 }
 
 // Sum of a group of threads (whole warps), in every one of them.  part: two slots of 32

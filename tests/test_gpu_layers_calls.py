@@ -1,5 +1,5 @@
 """Calls of the layers' operators beside one another: two host threads, graphs beside other shapes,
-lists of sequences that another stream reads when they are released."""
+lists of sequences that another stream reads when they are released; the norm's smallest rows."""
 
 import threading
 
@@ -101,3 +101,25 @@ def test_graphs_beside_other_shapes(layer):
 
 
 @pytest.mark.parametrize("handle", [False, True])
+def test_recorded_sequences_outlive_their_release(M, handle):
+    layer = M.LayerGroup()
+    lengths, h, d = [300, 77, 1000, 5], 2, 64
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v = (rand(gen, sum(lengths), h, d) for _ in range(3))
+    want = layer.attention(q, k, v, layer.sequences(lengths))
+    torch.cuda.synchronize()
+    seqs = layer.sequences(lengths)
+    place, size = seqs._tiles.data_ptr(), seqs._tiles.numel()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)                       # some 50 ms
+    seqs.record_stream(side.cuda_stream if handle else side)
+    got = layer.attention(q, k, v, seqs, stream=side.cuda_stream)
+    del seqs
+    # what is allocated now lies elsewhere, while the call still waits for its turn
+    others = [torch.zeros(size, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    assert not side.query() and all(x.data_ptr() != place for x in others)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and layer.status() == 0
+    layer.close()
