@@ -1,5 +1,6 @@
 """Calls of the layers' operators beside one another: two host threads, graphs beside other shapes,
-lists of sequences that another stream reads when they are released; the norm's smallest rows."""
+lists of sequences that another stream reads when they are released; the norm's smallest rows and its
+gain's gradient over many rows."""
 
 import threading
 
@@ -123,3 +124,6 @@ def test_recorded_sequences_outlive_their_release(M, handle):
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and layer.status() == 0
     layer.close()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
