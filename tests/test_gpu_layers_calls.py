@@ -127,3 +127,34 @@ def test_recorded_sequences_outlive_their_release(M, handle):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,value", [(2, 49152, 3e-18), (3, 4096, 1.2e-19), (700, 4096, 1.2e-19), (5, 1003, 2e-19), (3, 8, 1e-15)])
+def test_rows_of_next_to_nothing(layer, dtype, rows, cols, value):
+    """No epsilon, and a mean square below fp32's normal numbers: the sum of the squares is inside them."""
+    x = torch.zeros(rows, cols, dtype=dtype, device="cuda")
+    x[:, 3] = value
+    x[rows - 1, 5] = -value
+    gain = torch.ones(cols, device="cuda")
+    for eps in (0.0, 1e-38):
+        _, y, s = layer.norm(x, gain, eps=eps, dtype=torch.float32)
+        _, yw, sw = R.norm(x, None, gain, eps)
+        # two squares and their sum, one fp32 rounding each, which the root halves; the root's own, and y's two.  A float's
+        # eps is not the double's
+        es = (3 / 2 + 1) * R.F32 + (0 if eps == 0 else abs(torch.tensor(eps).double().item() / eps - 1)) + 2.0 ** -30
+        R.within(s, sw, es * sw)
+        R.within(y, yw, (es + 2 * R.F32) * yw.abs())
+
+
+@pytest.mark.parametrize("cols", [1024, 1027])
+def test_gain_of_rows_far_apart(layer, cols):
+    """Rows are taken a grid apart: of 300 beside one another no CTA adds up more than two, however many rows there are."""
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    rows = 200_000
+    h, dy = rand(gen, rows, cols), torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda")
+    dy[-300:] = rand(gen, 300, cols)
+    gain = 1 + 0.1 * torch.randn(cols, generator=gen, device="cuda")
+    s = layer.norm(h, gain)[2]
+    dx, dgain = layer.norm_backward(dy, h, gain, s)
+    wx, wg, ex, eg = R.norm_backward(dy[-300:], h[-300:], gain, s[-300:].double(), None)
+    R.within(dgain, wg, eg)
+    R.within(dx[-300:], wx, ex * (1 + R.BF16) + R.BF16 * wx.abs() + 2.0 ** -126)
+    assert (dx[:-300] == 0).all()
