@@ -158,6 +158,21 @@ struct LossCtl {
     float2 part[2][16];            // of the warps: reference, sum
 };
 
+// A wait for a copy.  POLLED: for bounds that the hardware may outlast within one try, by tries that do not wait
+// (in one kernel with the others it took 186 us where this takes 179).
+template <bool POLLED> __device__ __forceinline__ bool landed(uint32_t bar, uint32_t parity, volatile int* abort_flag, const LossParams& p) {
+    if (!POLLED) return ptx::mbar_wait(bar, parity, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit);
+    for (const long long t0 = clock64(); !ptx::mbar_test_wait(bar, parity);) {
+        if (*abort_flag) return false;
+        if (clock64() - t0 > p.wait_limit) {
+            *abort_flag = 1;
+            atomicCAS(p.status, 0, MOARA_ERR_DEVICE_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
+}
+
 __device__ __forceinline__ float ld_cluster_f32(uint32_t a) { return __uint_as_float(ptx::ld_cluster_u32(a)); }
 
 // A cluster of `split` CTAs takes rows a grid apart, each CTA a part of their columns, whose
@@ -167,7 +182,7 @@ __device__ __forceinline__ float ld_cluster_f32(uint32_t a) { return __uint_as_f
 // thread.  A thread's sum is relative to the largest logit that it has met, or one that is at most
 // 8 below it, so that the row is read twice, not three times.  !STAGED: a part that is too large for
 // shared memory is read again from L2.  8192 x 32000 bf16: 180 us (floor 155).
-template <class T, bool STAGED>
+template <class T, bool STAGED, bool POLLED>
 __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_constant__ LossParams p) {
     extern __shared__ __align__(16) uint8_t raw[];
     using L = Line<T>;
@@ -236,8 +251,7 @@ __global__ void __launch_bounds__(kLossThreads, 3) k_policy_loss(const __grid_co
         // top: the thread's largest logit when its reference was taken
         float top = -INFINITY, ref = 0.0f, sum = 0.0f;
         for (int c = 0; c < kChunks; ++c) {
-            if (STAGED && !ptx::mbar_wait(full + 8 * c, phase, abort_flag, p.status, MOARA_ERR_DEVICE_TIMEOUT, p.wait_limit))
-                wait_drain(full + 8 * c, phase);
+            if (STAGED && !landed<POLLED>(full + 8 * c, phase, abort_flag, p)) wait_drain(full + 8 * c, phase);
             const int end = min(x.lines, (c + 1) * chunk);
             for (int i = c * chunk + threadIdx.x; i < end; i += blockDim.x) {
                 const uint4 v = lines[i];
@@ -478,8 +492,8 @@ __global__ void __launch_bounds__(128) k_loss_sums(const float2* terms, int coun
 constexpr int kPart = 112 * 1024;
 constexpr int kStage = 200 * 1024;     // most bytes of a part in shared memory
 
-template <class T, bool STAGED> cudaError_t launch_loss(const LossParams& p, int& clusters, cudaStream_t s) {
-    const auto fn = k_policy_loss<T, STAGED>;
+template <class T, bool STAGED, bool POLLED> cudaError_t launch_loss(const LossParams& p, int& clusters, cudaStream_t s) {
+    const auto fn = k_policy_loss<T, STAGED, POLLED>;
     const int bytes = STAGED ? (p.part * static_cast<int>(sizeof(T)) + 15) / 16 * 16 + 16 : 0;
     if (bytes > 40 * 1024) {
         static std::atomic<uint64_t> done{0};
@@ -511,8 +525,8 @@ template <class T> cudaError_t loss_as(LossParams& p, int& clusters, cudaStream_
                            (2LL * p.split * p.rows <= 304 && part(2 * p.split) * sizeof(T) >= 4096)))
         p.split *= 2;
     p.part = part(p.split);
-    return p.part * static_cast<long long>(sizeof(T)) <= kStage ? launch_loss<T, true>(p, clusters, s)
-                                                                : launch_loss<T, false>(p, clusters, s);
+    if (p.part * static_cast<long long>(sizeof(T)) > kStage) return launch_loss<T, false, false>(p, clusters, s);
+    return p.wait_limit < 1 << 20 ? launch_loss<T, true, true>(p, clusters, s) : launch_loss<T, true, false>(p, clusters, s);
 }
 
 }  // namespace
