@@ -562,7 +562,7 @@ int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_d
  * those sums in two fp32 numbers, s is off by 3 2^-24 of its value at most (for long rows it is mostly the
  * nearest fp32 number), Y is rounded once from fp32; a row's sum of squares has to lie in fp32's
  * range.  H may be X or R, and Y may be X, R or H, where
- * type and pitch are the same.  Any alignment of the types; rows that begin on 16-byte lines
+ * type and pitch are the same; an output that overlaps an input otherwise is refused.  Any alignment of the types; rows that begin on 16-byte lines
  * are read by lines.  MOARA_ERR_UNSUPPORTED for more than 49152 columns. */
 int moara_rms_norm(moara_ctx* ctx, int rows, int cols, const void* X, int64_t ldx, const void* R, int64_t ldr,
                    int x_dtype, const float* gain, float eps, void* H, int64_t ldh, void* Y, int y_dtype, int64_t ldy,
@@ -579,7 +579,7 @@ int moara_rms_norm_quantize(moara_ctx* ctx, int rows, int cols, const void* X, i
  *   dX = dH + s (d - n mean(d n)) with d = dY gain, n = H s     (h_dtype; the gradient of X and of R)
  *   dgain = sum over rows of dY n                                (floats)
  * in fp32 with one rounding of dX; the sums over rows in a fixed order.  dX may be dY, H
- * or dH where type and pitch are the same.  workspace: moara_rms_norm_backward_workspace_bytes
+ * or dH where type and pitch are the same, and overlaps none of them otherwise.  workspace: moara_rms_norm_backward_workspace_bytes
  * device bytes, 16-byte aligned, in use by one call at a time. */
 int moara_rms_norm_backward_workspace_bytes(int rows, int cols, size_t* out);
 int moara_rms_norm_backward(moara_ctx* ctx, int rows, int cols, const void* dY, int dy_dtype, int64_t lddy,
@@ -637,7 +637,7 @@ int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int to
  * 0.  An advantage of zero has no part, however large the ratio.  rho and exp x may pass fp32's range
  * (their roots may not) where their products with w, adv and kl do not; what does is infinite or NaN in
  * its own row of dZ and in sums.  ref_logp: NULL without a KL term (kl = 0).  logp receives lp, dZ (of Z's type, row pitch
- * lddz, may be Z with its pitch, or NULL) the gradient.  The sum over a row is held in fp32, those over rows
+ * lddz; Z itself with its pitch, or apart from it, or NULL) the gradient.  The sum over a row is held in fp32, those over rows
  * in two fp32 numbers, all in a fixed order.  workspace: moara_policy_loss_workspace_bytes(rows)
  * device bytes, 16-byte aligned, in use by one call at a time. */
 int moara_policy_loss_workspace_bytes(int rows, size_t* out);

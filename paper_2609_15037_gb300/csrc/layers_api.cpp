@@ -30,6 +30,30 @@ int check_rows(moara_ctx* ctx, const char* what, const void* p, int dtype, int c
     return MOARA_OK;
 }
 
+// Rows of a matrix in memory.
+struct Span {
+    const char* name;
+    uintptr_t at;
+    int64_t width, pitch;                        // bytes
+    int rows;
+    Span(const char* what, const void* p, int dtype, int rows_, int cols, int64_t ld)
+        : name(what), at(reinterpret_cast<uintptr_t>(p)), width(cols * (dtype == MOARA_DTYPE_BF16 ? 2LL : 4LL)),
+          pitch(ld * (dtype == MOARA_DTYPE_BF16 ? 2LL : 4LL)), rows(rows_) {
+        if (rows == 1) pitch = width;
+    }
+    __int128 end() const { return static_cast<__int128>(at) + static_cast<__int128>(rows - 1) * pitch + width; }
+};
+
+// An output may be the input itself, entry by entry, or lie apart from it: rows are taken in no order.
+int check_apart(moara_ctx* ctx, const Span& out, const Span& in) {
+    if (in.at == 0 || out.at == 0 || out.end() <= static_cast<__int128>(in.at) || in.end() <= static_cast<__int128>(out.at)) return MOARA_OK;
+    // columns beside one another in rows of the same pitch lie apart
+    const Span &a = out.at <= in.at ? out : in, &b = out.at <= in.at ? in : out;
+    const int64_t d = static_cast<int64_t>(b.at - a.at), off = d % a.pitch;
+    const bool ok = a.pitch == b.pitch && ((d == 0 && a.width == b.width) || (off >= a.width && off + b.width <= a.pitch));
+    return ok ? MOARA_OK : fail(ctx, MOARA_ERR_INVALID_ARG, "%s overlaps %s without being it", out.name, in.name);
+}
+
 int check_floats(moara_ctx* ctx, const char* what, const float* p) {
     if (p == nullptr) return fail(ctx, MOARA_ERR_INVALID_ARG, "%s is NULL", what);
     if (!aligned(p, 4)) return fail(ctx, MOARA_ERR_ALIGN, "%s is not aligned to its type", what);
@@ -43,8 +67,10 @@ int check_norm_size(moara_ctx* ctx, int rows, int cols) {
     return MOARA_OK;
 }
 
-int check_norm(moara_ctx* ctx, const moara::NormForward& a) {
+// wanted: whether Y is
+int check_norm(moara_ctx* ctx, const moara::NormForward& a, bool wanted) {
     int rc = check_norm_size(ctx, a.rows, a.cols);
+    if (rc == MOARA_OK && wanted) rc = check_rows(ctx, "Y", a.y, a.y_dtype, a.cols, a.ldy);
     if (rc == MOARA_OK) rc = check_rows(ctx, "X", a.x, a.dtype, a.cols, a.ldx);
     if (rc == MOARA_OK && (a.r != nullptr || a.h != nullptr)) {
         rc = check_rows(ctx, "R", a.r, a.dtype, a.cols, a.ldr);
@@ -53,6 +79,13 @@ int check_norm(moara_ctx* ctx, const moara::NormForward& a) {
     if (rc == MOARA_OK) rc = check_floats(ctx, "gain", a.gain);
     if (rc == MOARA_OK) rc = check_floats(ctx, "rstd", a.rstd);
     if (rc == MOARA_OK && !(a.eps >= 0.0f && a.eps < INFINITY)) rc = fail(ctx, MOARA_ERR_INVALID_ARG, "eps must be >= 0");
+    if (rc != MOARA_OK) return rc;
+    const Span x("X", a.x, a.dtype, a.rows, a.cols, a.ldx), r("R", a.r, a.dtype, a.rows, a.cols, a.ldr),
+        h("H", a.h, a.dtype, a.rows, a.cols, a.ldh), y("Y", a.y, a.y_dtype, a.rows, a.cols, a.ldy);
+    rc = check_apart(ctx, h, x);
+    if (rc == MOARA_OK) rc = check_apart(ctx, h, r);
+    for (const Span* in : {&x, &r, &h})
+        if (rc == MOARA_OK) rc = check_apart(ctx, y, *in);
     return rc;
 }
 
@@ -115,8 +148,7 @@ int moara_rms_norm(moara_ctx* ctx, int rows, int cols, const void* X, int64_t ld
                    float* rstd, void* stream) {
     if (ctx == nullptr) return MOARA_ERR_INVALID_ARG;
     const moara::NormForward a{rows, cols, X, R, x_dtype, gain, eps, H, Y, y_dtype, rstd, ldx, ldr, ldh, ldy};
-    int rc = check_norm(ctx, a);
-    if (rc == MOARA_OK) rc = check_rows(ctx, "Y", Y, y_dtype, cols, ldy);
+    const int rc = check_norm(ctx, a, true);
     if (rc != MOARA_OK) return rc;
     DeviceGuard g(ctx->device);
     const cudaError_t e = moara::launch_norm(a, static_cast<cudaStream_t>(stream), &ctx->launches);
@@ -129,7 +161,7 @@ int moara_rms_norm_quantize(moara_ctx* ctx, int rows, int cols, const void* X, i
                             void* sft, float* rstd, void* stream) {
     if (ctx == nullptr) return MOARA_ERR_INVALID_ARG;
     const moara::NormForward a{rows, cols, X, R, x_dtype, gain, eps, H, nullptr, x_dtype, rstd, ldx, ldr, ldh, cols};
-    int rc = check_norm(ctx, a);
+    const int rc = check_norm(ctx, a, false);
     if (rc != MOARA_OK) return rc;
     if (static_cast<long long>(moara::fp4_tiles(rows)) * moara::fp4_tiles(cols) > INT_MAX / 64)
         return fail(ctx, MOARA_ERR_SHAPE, "the matrix is too large");
@@ -170,6 +202,11 @@ int moara_rms_norm_backward(moara_ctx* ctx, int rows, int cols, const void* dY, 
     if (rc == MOARA_OK) rc = check_floats(ctx, "gain", gain);
     if (rc == MOARA_OK) rc = check_floats(ctx, "rstd", rstd);
     if (rc == MOARA_OK) rc = check_floats(ctx, "dgain", dgain);
+    if (rc != MOARA_OK) return rc;
+    const Span out("dX", dX, h_dtype, rows, cols, lddx);
+    rc = check_apart(ctx, out, Span("dY", dY, dy_dtype, rows, cols, lddy));
+    if (rc == MOARA_OK) rc = check_apart(ctx, out, Span("H", H, h_dtype, rows, cols, ldh));
+    if (rc == MOARA_OK) rc = check_apart(ctx, out, Span("dH", dH, h_dtype, rows, cols, lddh));
     if (rc != MOARA_OK) return rc;
     size_t need = 0;
     moara_rms_norm_backward_workspace_bytes(rows, cols, &need);
@@ -296,6 +333,7 @@ int moara_policy_loss(moara_ctx* ctx, int rows, int vocab, const void* Z, int dt
     int rc = check_rows(ctx, "Z", Z, dtype, vocab, ldz);
     if (rc == MOARA_OK && dZ != nullptr) rc = check_rows(ctx, "dZ", dZ, dtype, vocab, lddz);
     if (rc == MOARA_OK && dZ == Z && lddz != ldz) rc = fail(ctx, MOARA_ERR_SHAPE, "dZ is Z with another pitch");
+    if (rc == MOARA_OK) rc = check_apart(ctx, Span("dZ", dZ, dtype, rows, vocab, lddz), Span("Z", Z, dtype, rows, vocab, ldz));
     if (rc == MOARA_OK && target == nullptr) rc = fail(ctx, MOARA_ERR_INVALID_ARG, "target is NULL");
     if (rc == MOARA_OK && !aligned(target, 8)) rc = fail(ctx, MOARA_ERR_ALIGN, "target is not aligned to its type");
     if (rc == MOARA_OK) rc = check_floats(ctx, "old_logp", old_logp);
