@@ -562,8 +562,8 @@ int moara_fp4_linear(moara_ctx* ctx, int M, int N, int K, const void* X, int x_d
  * those sums in two fp32 numbers, s is off by 3 2^-24 of its value at most (for long rows it is mostly the
  * nearest fp32 number), Y is rounded once from fp32; a row's sum of squares has to lie in fp32's
  * range.  H may be X or R, and Y may be X, R or H, where
- * type and pitch are the same; an output that overlaps an input otherwise is refused.  Any alignment of the types; rows that begin on 16-byte lines
- * are read by lines.  MOARA_ERR_UNSUPPORTED for more than 49152 columns. */
+ * type and pitch are the same; an output that overlaps an input otherwise is refused.  Any alignment of the
+ * types; rows that begin on 16-byte lines are read by lines.  MOARA_ERR_UNSUPPORTED for more than 49152 columns. */
 int moara_rms_norm(moara_ctx* ctx, int rows, int cols, const void* X, int64_t ldx, const void* R, int64_t ldr,
                    int x_dtype, const float* gain, float eps, void* H, int64_t ldh, void* Y, int y_dtype, int64_t ldy,
                    float* rstd, void* stream);
@@ -578,9 +578,10 @@ int moara_rms_norm_quantize(moara_ctx* ctx, int rows, int cols, const void* X, i
  * (dH of h_dtype, NULL for none; what flows past the norm):
  *   dX = dH + s (d - n mean(d n)) with d = dY gain, n = H s     (h_dtype; the gradient of X and of R)
  *   dgain = sum over rows of dY n                                (floats)
- * in fp32 with one rounding of dX; the sums over rows in a fixed order.  dX may be dY, H
- * or dH where type and pitch are the same, and overlaps none of them otherwise.  workspace: moara_rms_norm_backward_workspace_bytes
- * device bytes, 16-byte aligned, in use by one call at a time. */
+ * in fp32 with one rounding of dX.  dgain's sums over rows are in a fixed order: each of at least 152 CTAs (or one
+ * a row) adds its own up in fp32, one row after the other, and those sums are added in two fp32 numbers.
+ * dX may be dY, H or dH where type and pitch are the same, and overlaps none of them otherwise.  workspace:
+ * moara_rms_norm_backward_workspace_bytes device bytes, 16-byte aligned, in use by one call at a time. */
 int moara_rms_norm_backward_workspace_bytes(int rows, int cols, size_t* out);
 int moara_rms_norm_backward(moara_ctx* ctx, int rows, int cols, const void* dY, int dy_dtype, int64_t lddy,
                             const void* H, int h_dtype, int64_t ldh, const float* gain, const float* rstd,
@@ -619,7 +620,9 @@ int moara_attention(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int
 /* Its gradients from dout (strided as q), with what the forward call left in out, rest (or
  * NULL: the gradient of q is less exact for long sequences) and lse: dq tokens x heads x dim,
  * dk and dv tokens x kv_heads x dim, bf16; the sums over a group's heads in fp32, every sum in
- * a fixed order.  delta: workspace of heads x tokens + 1 floats, in use by one call at a time. */
+ * a fixed order.  P and dS are rounded to bf16 for their products: gradients are 2.2e-3 to 2.7e-3 of their norm
+ * from the exact ones, where the rounding of the results alone gives 1.7e-3.  delta: workspace of heads x tokens + 1
+ * floats, in use by one call at a time. */
 int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int tokens, int heads, int kv_heads, int dim,
                              float scale, const void* dout, int64_t do_row, int64_t do_head, const void* q, int64_t q_row,
                              int64_t q_head, const void* k, int64_t k_row, int64_t k_head, const void* v, int64_t v_row,
@@ -637,9 +640,9 @@ int moara_attention_backward(moara_ctx* ctx, const moara_sequences* seqs, int to
  * 0.  An advantage of zero has no part, however large the ratio.  rho and exp x may pass fp32's range
  * (their roots may not) where their products with w, adv and kl do not; what does is infinite or NaN in
  * its own row of dZ and in sums.  ref_logp: NULL without a KL term (kl = 0).  logp receives lp, dZ (of Z's type, row pitch
- * lddz; Z itself with its pitch, or apart from it, or NULL) the gradient.  The sum over a row is held in fp32, those over rows
- * in two fp32 numbers, all in a fixed order.  workspace: moara_policy_loss_workspace_bytes(rows)
- * device bytes, 16-byte aligned, in use by one call at a time. */
+ * lddz; Z itself with its pitch, or apart from it, or NULL) the gradient.  The sum over a row is held in fp32 (a
+ * thread adds its exponentials up one after the other), those over rows in two fp32 numbers, all in a fixed order.
+ * workspace: moara_policy_loss_workspace_bytes(rows) device bytes, 16-byte aligned, in use by one call at a time. */
 int moara_policy_loss_workspace_bytes(int rows, size_t* out);
 int moara_policy_loss(moara_ctx* ctx, int rows, int vocab, const void* Z, int dtype, int64_t ldz, const int64_t* target,
                       const float* old_logp, const float* ref_logp, const float* adv, const float* weight, float low,

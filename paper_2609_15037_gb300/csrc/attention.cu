@@ -6,8 +6,8 @@
 // Bound by the tensor cores (4 D and 10 D operations a visible pair of query and key).  S
 // and dS are fp32 sums in tensor memory and never leave the SM; P and dS are rounded to bf16
 // for the products that take them, the form in which the tensor cores read them: an error
-// of 2^-9 of each term, which the sums over keys or queries average (outputs 1.7e-3 of their
-// norm from the exact ones, of which their own rounding is 1.66e-3).
+// of 2^-8 of each term at most, which the sums over keys or queries average (outputs 1.7e-3 of their
+// norm from the exact ones, of which their own rounding is 1.66e-3; gradients 2.2e-3 to 2.7e-3).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
@@ -48,7 +48,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 
 // Descriptors of a tile, as an operand by rows and as the one whose rows are summed over, and
 // that of a tile some bytes further on (they count in 16 bytes).  A product issues in fewer clocks where its
-// descriptors are one number and constants (16384 tokens: 1202 us with each worked out, 1177 so).
+// descriptors are one number and constants (16384 tokens: 2% longer with each worked out).
 __device__ __forceinline__ uint64_t by_rows(uint32_t tile) { return ptx::smem_desc_sw128(tile, 16, 1024); }
 __device__ __forceinline__ uint64_t to_sum(uint32_t tile) { return ptx::smem_desc_sw128(tile, PANEL, 1024); }
 __device__ __forceinline__ uint64_t beside(uint64_t d, int bytes) { return d + static_cast<uint64_t>(bytes / 16); }
@@ -130,9 +130,11 @@ struct Place {
 // turn its S into P, the tensor cores work for the other: S (128 columns of tensor memory),
 // over which P is written, and O (DP columns) each.  A row belongs to a thread.  A row's
 // maximum is followed lazily: O is only rescaled once S exceeds the reference by 2^8, so
-// that rows rarely wait for their O.  Q, K and V of the next pair of tiles come while this one's last steps
+// that rows rarely wait for their O.  (The method is a published one: a running maximum, Milakov and Gimelshein 2018;
+// over tiles of keys, Dao et al. 2022; two tiles of queries in turn, Shah et al. 2024.)  Q, K and V of the next pair of tiles come while this one's last steps
 // run, its first S while O is stored: the tensor cores stand still between pairs for its first P alone.
-// 16384 tokens, 28 heads on 4 of 128: 1180 us, 1.63 PFLOP/s (0.86 of the cuBLAS burst rate, 0.94 of the sustained one).
+// 16384 tokens, 28 heads on 4 of 128: 1174 to 1202 us, 1.60 to 1.64 PFLOP/s (0.85 of the cuBLAS burst rate, 0.93 of the
+// sustained one).
 // ---------------------------------------------------------------------------
 template <int DP> struct Forward {
     static constexpr int TILE = DP / 64 * PANEL;
@@ -1278,7 +1280,7 @@ template <int ID, class... P> cudaError_t allow_shared(void (*fn)(P...), int byt
 
 // A pair a CTA where all of them run at once, or where a pair's steps are many: the loop around them
 // costs each some 150 clocks, and what it hides is a pair's first copies and last stores (16384
-// tokens, 28 heads of 128: 1182 us, with the loop 1244; 32 x 512, 16 heads of 128: 77 and 67; the same at 16 steps a
+// tokens, 28 heads of 128: 5% longer with the loop; 32 x 512, 16 heads of 128: 77 and 67; the same at 16 steps a
 // pair, of heads of 64 at 32).
 template <int DP> cudaError_t forward_as(const ForwardParams& p, int ctas, long long steps, cudaStream_t s) {
     const bool one = ctas <= 152 || steps * DP > 2048LL * ctas;

@@ -529,8 +529,9 @@ __global__ void __launch_bounds__(E == 0 ? 1024 : 512) k_norm_backward(const Bac
 // copies of the next rows run into shared memory of its own while it works on this one: no
 // registers wait for DRAM, and what a thread reads it has copied itself, so that a row's sum is the
 // only barrier.  A row's first and last line are read where they lie if they are not whole.
-// 16384 x 4096 bf16 with the residual: 95 us, backward 117 with the gain (floor 79); with loads into registers
-// 107 and 108.
+// 16384 x 4096 bf16 with the residual: 95 us (floor 79; with loads into registers 107).  Its gradients: 115 us, and 6 for the
+// gain's sums; an earlier form with 32 entries a thread in registers took 108 by a profiler's clock where this takes 117, so
+// that the copies gain nothing there.
 // ---------------------------------------------------------------------------
 template <int BYTES> __device__ __forceinline__ void copy_async(void* to, const void* from) {
     const uint32_t a = static_cast<uint32_t>(__cvta_generic_to_shared(to));

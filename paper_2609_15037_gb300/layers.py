@@ -144,7 +144,8 @@ class LayerGroup:
         weight of the clipped tokens}, logp the targets' log-probabilities, dlogits (None
         without `grad`) the loss's gradient, into `out` where it is given, which may be the logits.
         targets: int64; old, adv, weights (None: 1 / tokens), ref: float32 of one entry a token.
-        The ratio is clipped to 1 - clip[0] .. 1 + clip[1].  kl: factor of the KL term to `ref`."""
+        The ratio is clipped to 1 - clip[0] .. 1 + clip[1].  kl: factor of the KL term to `ref`, which is
+        not read where the factor is 0 (the second sum is 0 then)."""
         low, high = 1.0 - clip[0], 1.0 + clip[1]
         if kl and ref is None:
             raise ValueError("a KL term needs ref")
